@@ -370,6 +370,65 @@ dc_status dc_chain_forward_host_async(const dc_layer *layers, int n_layers, cons
                                 size_t workspace_bytes, dc_stream stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * 1x1 layers in 4 bits.  (The paper measures FP32; this is what the same layers -- 1x1 convolutions, classifiers, any product of
+ * rows with weights -- cost where their maps and weights are held in microscaled 4-bit floating point.)
+ *
+ * A matrix has `rows` rows (the pixels of an NHWC map, or tokens; the output channels of weights) of `cols` columns (input channels),
+ * which both operands of a product reduce over.  Each value is a code of 4 bits, e2m1 -- sign, then 0, 0.5, 1, 1.5, 2, 3, 4 or 6 --
+ * times the scale of its block of columns; the last block of a row may be shorter.  With a = the block's largest magnitude:
+ *   DC_MX4: blocks of 32, scale 2^e, e = floor(log2 a) - 2, at least -127, held as the byte e + 127 (e8m0).
+ *   DC_NV4: blocks of 16, scale s g: s = a / (6 g) rounded to e4m3 (448 at most), g = `tensor_scale`, a power of two for the whole matrix.
+ * A value's code is the nearest to value / scale, ties to the code with an even last bit, 6 at most.  The quotients decide as in real
+ * arithmetic, so the codes are a function of the values alone.  A block with a NaN or an infinity gets the scale NaN: all of it
+ * reads as NaN, and so do the results of its row.  A block whose scale is 0 (a / (6 g) up to 2^-10) reads as 0.
+ * --------------------------------------------------------------------------------------------- */
+typedef enum { DC_MX4 = 0, DC_NV4 = 1 } dc_q4_format;
+
+/* Where things lie in a quantised matrix, one buffer of `bytes` bytes, 16-byte aligned.  Codes: row r begins at r * pitch, column c is the
+ * low (c even) or high half of byte c / 2, and columns up to 2 * pitch are 0.  Scales: one byte a block, that of row r and block b at
+ *   scale_offset + ((r / 128) * tiles + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4,
+ * and those of rows and blocks that the matrix does not have are 0.  (Tiles of 128 rows x 4 blocks, as the tensor core takes them.) */
+typedef struct { size_t pitch, tiles, scale_offset, bytes; } dc_q4_layout;
+
+/* Host only: the layout of a quantised matrix.  rows and cols >= 1; rows up to 2^31 - 256, cols up to 2^24 (DC_ERR_UNSUPPORTED). */
+dc_status dc_q4_query(long long rows, int cols, dc_q4_format format, dc_q4_layout *layout);
+
+/*
+ * Quantises x, [rows] rows of `cols` values of `dtype` that begin `stride` >= cols elements apart, into q (every byte of its layout is
+ * written).  tensor_scale: host, a power of two from 2^-100 to 2^100 for DC_NV4, 1 for DC_MX4.  x and q do not overlap.
+ */
+dc_status dc_q4_quantize(const void *x, long long rows, int cols, long long stride, dc_dtype dtype, dc_q4_format format,
+                         float tensor_scale, void *q, dc_stream stream);
+
+/* The values that q stands for, into rows of y that begin `stride` >= cols elements apart; what lies between the rows stays as it is.
+ * Exact in fp32, and in bf16. */
+dc_status dc_q4_dequantize(const void *q, long long rows, int cols, dc_q4_format format, float tensor_scale, void *y, long long stride,
+                           dc_dtype dtype, dc_stream stream);
+
+/* Host only: bytes of workspace that dc_q4_forward needs for an input of this size. */
+dc_status dc_q4_workspace_bytes(long long rows, int c_in, dc_q4_format format, size_t *bytes);
+
+/*
+ * Product of two quantised matrices of one format:  y[r][o] = act(scale * sum_i X[r][i] W[o][i] + bias[o] + residual[r][o]).
+ * x: [rows] x [c_in], w: [c_out] x [c_in], both from dc_q4_quantize, their values here without the tensor scales: `scale` is the product of
+ * the two (any finite number; 1 for DC_MX4).  y: [rows][c_out] of `dtype`, dense; residual: the same or NULL, may be y; bias: fp32 [c_out] or
+ * NULL.  On the tensor core: products exact, sums in fp32.  workspace: device, >= dc_conv_workspace_bytes(), zeroed once by the
+ * caller; a bounded wait that runs out is latched there (dc_workspace_status).  Calls that may run at once need a workspace each.
+ */
+dc_status dc_q4_product(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, float scale,
+                        const float *bias, dc_act act, const void *residual, void *y, dc_dtype dtype, void *workspace,
+                        size_t workspace_bytes, dc_stream stream);
+
+/*
+ * Forward pass of a 1x1 layer of stride 1 with weights in 4 bits: dc_q4_quantize of x ([rows][c_in] of `dtype`, dense, with x_scale), then
+ * dc_q4_product with w (quantised with w_scale) -- the same results to the bit, except that sums may be added up in another order.  Few rows are
+ * quantised in the product's own launch; many into the workspace: device, >= dc_q4_workspace_bytes, its first 256 bytes zeroed once.
+ */
+dc_status dc_q4_forward(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, float x_scale,
+                        float w_scale, const float *bias, dc_act act, const void *residual, void *y, dc_dtype dtype, void *workspace,
+                        size_t workspace_bytes, dc_stream stream);
+
+/* ---------------------------------------------------------------------------------------------
  * The selector's two dynamic programmes (Sec. 4.3).  Host only: every pointer is host memory, no
  * device call is made.  Boundaries are 0..L for a network of L layers; tables are row-major
  * (L+1) x (L+1) and only entries [i][j] with i < j are read.

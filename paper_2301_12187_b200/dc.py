@@ -21,6 +21,7 @@ F32, BF16 = 0, 1
 ACT_IDENTITY, ACT_RELU6 = 0, 1
 ALGO_AUTO, ALGO_TCGEN05, ALGO_SIMT = 0, 1, 2
 MERGE_AUTO, MERGE_STEPS = 0, 1
+MX4, NV4 = 0, 1
 
 _FP = C.POINTER(C.c_float)
 
@@ -55,6 +56,10 @@ class Block(C.Structure):
 
 class BlockPlan(C.Structure):
     _fields_ = [(name, C.c_int) for name in ("tile_w", "tile_h", "tile_images", "tiles", "chunks", "form", "groups", "operands", "stages")]
+
+
+class Q4Layout(C.Structure):
+    _fields_ = [("pitch", C.c_size_t), ("tiles", C.c_size_t), ("scale_offset", C.c_size_t), ("bytes", C.c_size_t)]
 
 
 EXPORTS = {
@@ -102,6 +107,16 @@ EXPORTS = {
     "dc_block_forward": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.POINTER(Block), C.c_void_p,
                                    C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "dc_block_plan_query": (C.c_int, [C.c_int, C.c_int, C.c_int, C.POINTER(Block), C.c_int, C.POINTER(BlockPlan)]),
+    "dc_q4_query": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.POINTER(Q4Layout)]),
+    "dc_q4_quantize": (C.c_int, [C.c_void_p, C.c_longlong, C.c_int, C.c_longlong, C.c_int, C.c_int, C.c_float, C.c_void_p,
+                                 C.c_void_p]),
+    "dc_q4_dequantize": (C.c_int, [C.c_void_p, C.c_longlong, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_longlong, C.c_int,
+                                   C.c_void_p]),
+    "dc_q4_workspace_bytes": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "dc_q4_product": (C.c_int, [C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_int,
+                                C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "dc_q4_forward": (C.c_int, [C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_float, C.c_void_p,
+                                C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "dc_workspace_status": (C.c_int, [C.c_void_p, C.c_void_p]),
     "dc_workspace_status_where": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_uint), C.POINTER(C.c_uint)]),
     "dc_selftest_bounded_wait": (C.c_int, [C.c_void_p, C.c_size_t, C.c_uint, C.c_void_p]),
@@ -475,6 +490,115 @@ def block_forward(x, blk: Block, y, workspace, stream=None):
     _check(lib().dc_block_forward(_ptr(x), n, h, w, C.byref(blk), _ptr(y), dtype_code(x.dtype),
                                   _ptr(workspace), workspace.numel() * workspace.element_size(),
                                   _stream(stream)), "dc_block_forward")
+
+
+# --------------------------------------------------------------------------- 1x1 layers in 4 bits
+
+
+def q4_layout(rows: int, cols: int, fmt: int) -> Q4Layout:
+    """Where codes and scales lie in a quantised matrix; see include/dc.h."""
+    layout = Q4Layout()
+    _check(lib().dc_q4_query(rows, cols, fmt, C.byref(layout)), "dc_q4_query")
+    return layout
+
+
+def q4_tensor_scale(top: float) -> float:
+    """For NV4: the smallest power of two with which the scales of a matrix whose largest magnitude is `top` stay in e4m3."""
+    import math
+    if not top > 0 or math.isinf(top):
+        return 1.0
+    m, e = math.frexp(top / (6.0 * 448.0))
+    return 2.0 ** min(100, max(-100, e - 1 if m == 0.5 else e))
+
+
+class Q4Matrix:
+    """A quantised matrix: rows x cols codes and their scales in one device buffer (`data`), zero until dc_q4_quantize has
+    written it."""
+
+    def __init__(self, rows: int, cols: int, fmt: int, tensor_scale: float = 1.0, device="cuda"):
+        import torch
+        self.rows, self.cols, self.fmt, self.tensor_scale = int(rows), int(cols), int(fmt), float(tensor_scale)
+        self.layout = q4_layout(self.rows, self.cols, self.fmt)
+        self.data = torch.zeros(int(self.layout.bytes), dtype=torch.uint8, device=device)
+
+
+def _rows_of(t, cols: int, what: str) -> Tuple[int, int]:
+    """(rows, elements between rows) of a tensor [..., cols] whose rows lie at one distance: a dense map or a slice of its channels."""
+    if t.dim() < 1 or t.shape[-1] != cols or (cols > 1 and t.stride(-1) != 1):
+        raise ValueError("%s: the last dimension must hold %d neighbouring values" % (what, cols))
+    rows = t.numel() // cols if cols else 0
+    if t.dim() == 1 or rows <= 1:
+        return rows, cols
+    step = None
+    n = 1                                        # rows below the dimension looked at
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if step is None:
+            step = stride
+        elif stride != step * n:
+            raise ValueError("%s: rows must lie at one distance" % what)
+        n *= size
+    return rows, step
+
+
+def _dense(t, rows: int, cols: int, dtype, what: str):
+    if t is not None and (t.dtype != dtype or t.numel() != rows * cols or t.shape[-1] != cols or not t.is_contiguous()):
+        raise ValueError("%s: a dense tensor of %d rows of %d values in %s is wanted" % (what, rows, cols, dtype))
+
+
+def q4_quantize(x, q: Q4Matrix, stream=None):
+    """Rows of x (bf16 or fp32, [..., cols]; rows at one distance) into q, with q's tensor scale."""
+    rows, stride = _rows_of(x, q.cols, "q4_quantize")
+    if rows != q.rows:
+        raise ValueError("q4_quantize: %d rows, the matrix has %d" % (rows, q.rows))
+    _check(lib().dc_q4_quantize(_ptr(x), rows, q.cols, stride, dtype_code(x.dtype), q.fmt, q.tensor_scale, _ptr(q.data),
+                                _stream(stream)), "dc_q4_quantize")
+
+
+def q4_dequantize(q: Q4Matrix, y, stream=None):
+    """The values that q stands for into y (bf16 or fp32, [..., cols])."""
+    rows, stride = _rows_of(y, q.cols, "q4_dequantize")
+    if rows != q.rows:
+        raise ValueError("q4_dequantize: %d rows, the matrix has %d" % (rows, q.rows))
+    _check(lib().dc_q4_dequantize(_ptr(q.data), rows, q.cols, q.fmt, q.tensor_scale, _ptr(y), stride, dtype_code(y.dtype),
+                                  _stream(stream)), "dc_q4_dequantize")
+
+
+def q4_workspace_bytes(rows: int, c_in: int, fmt: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().dc_q4_workspace_bytes(rows, c_in, fmt, C.byref(nbytes)), "dc_q4_workspace_bytes")
+    return int(nbytes.value)
+
+
+def _bias(t, n: int, what: str):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
+        raise ValueError("%s: the bias must be %d fp32 values" % (what, n))
+
+
+def q4_product(x: Q4Matrix, w: Q4Matrix, bias, act, residual, y, workspace, stream=None):
+    """y = act(X W^T + bias + residual) of two quantised matrices; y (and residual): [..., w.rows], bf16 or fp32, dense."""
+    if x.fmt != w.fmt or x.cols != w.cols:
+        raise ValueError("q4_product: the matrices must have one format and as many columns")
+    _dense(y, x.rows, w.rows, y.dtype, "q4_product")
+    _dense(residual, x.rows, w.rows, y.dtype, "q4_product")
+    _bias(bias, w.rows, "q4_product")
+    _check(lib().dc_q4_product(_ptr(x.data), x.rows, x.cols, _ptr(w.data), w.rows, x.fmt, x.tensor_scale * w.tensor_scale, _ptr(bias),
+                               act, _ptr(residual), _ptr(y), dtype_code(y.dtype), _ptr(workspace),
+                               workspace.numel() * workspace.element_size(), _stream(stream)), "dc_q4_product")
+
+
+def q4_forward(x, w: Q4Matrix, x_scale: float, bias, act, residual, y, workspace, stream=None):
+    """The same from rows in bf16 or fp32 (x: [..., w.cols], dense, of y's dtype), quantised on the way with tensor scale x_scale."""
+    rows = x.numel() // w.cols
+    _dense(x, rows, w.cols, y.dtype, "q4_forward")
+    _dense(y, rows, w.rows, y.dtype, "q4_forward")
+    _dense(residual, rows, w.rows, y.dtype, "q4_forward")
+    _bias(bias, w.rows, "q4_forward")
+    _check(lib().dc_q4_forward(_ptr(x), rows, w.cols, _ptr(w.data), w.rows, w.fmt, x_scale, w.tensor_scale, _ptr(bias), act,
+                               _ptr(residual), _ptr(y), dtype_code(y.dtype), _ptr(workspace),
+                               workspace.numel() * workspace.element_size(), _stream(stream)), "dc_q4_forward")
 
 
 def workspace_status(workspace, stream=None) -> int:

@@ -1,0 +1,187 @@
+"""4-bit matrices without a GPU: the layout, every refusal (before anything is launched), the binding's checks, and the oracle against the
+definitions worked by hand."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import q4_oracle as Q
+from paper_2301_12187_b200 import dc
+
+FAKE = 0x10000  # a 16-byte aligned, never dereferenced "device pointer"
+
+
+def status_of(fn, *a):
+    try:
+        fn(*a)
+    except dc.DcError as e:
+        return e.status
+    return dc.OK
+
+
+@pytest.mark.parametrize("rows,cols,fmt,pitch,tiles,offset,nbytes", [
+    (1, 1, dc.MX4, 16, 1, 256, 768),
+    (1, 1, dc.NV4, 16, 1, 256, 768),
+    (128, 24, dc.MX4, 16, 1, 2048, 2560),
+    (129, 64, dc.NV4, 32, 1, 4352, 4352 + 2 * 512),
+    (129, 65, dc.NV4, 48, 2, 6400, 6400 + 4 * 512),
+    (4096, 4096, dc.NV4, 2048, 64, 4096 * 2048, 4096 * 2048 + 32 * 64 * 512),
+    (300, 129, dc.MX4, 80, 2, 24064, 24064 + 3 * 2 * 512),
+])
+def test_layout(rows, cols, fmt, pitch, tiles, offset, nbytes):
+    lay = dc.q4_layout(rows, cols, fmt)
+    assert (lay.pitch, lay.tiles, lay.scale_offset, lay.bytes) == (pitch, tiles, offset, nbytes)
+    assert dc.q4_workspace_bytes(rows, cols, fmt) == 256 + nbytes
+
+
+def test_layout_of_large_matrices_passes_32_bits():
+    lay = dc.q4_layout(1 << 30, 8192, dc.NV4)
+    assert lay.scale_offset == (1 << 30) * 4096 and lay.bytes == lay.scale_offset + (1 << 23) * 128 * 512
+
+
+def test_query_refuses():
+    assert status_of(dc.q4_layout, 0, 8, dc.MX4) == dc.ERR_INVALID_ARG
+    assert status_of(dc.q4_layout, -1, 8, dc.MX4) == dc.ERR_INVALID_ARG
+    assert status_of(dc.q4_layout, 8, 0, dc.MX4) == dc.ERR_INVALID_ARG
+    assert status_of(dc.q4_layout, 8, 8, 2) == dc.ERR_INVALID_ARG
+    assert status_of(dc.q4_layout, (1 << 31) - 255, 8, dc.MX4) == dc.ERR_UNSUPPORTED
+    assert status_of(dc.q4_layout, 8, (1 << 24) + 1, dc.MX4) == dc.ERR_UNSUPPORTED
+    assert dc.lib().dc_q4_query(8, 8, 0, None) == dc.ERR_INVALID_ARG
+    assert dc.lib().dc_q4_workspace_bytes(8, 8, 0, None) == dc.ERR_INVALID_ARG
+    assert status_of(dc.q4_workspace_bytes, 0, 8, 0) == dc.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("name", ["dc_q4_quantize", "dc_q4_dequantize"])
+def test_quantize_and_read_back_refuse(name):
+    f = getattr(dc.lib(), name)
+
+    def call(x=FAKE, rows=4, cols=8, stride=8, dtype=dc.BF16, fmt=dc.NV4, g=1.0, q=FAKE):
+        if name == "dc_q4_quantize":
+            return f(x, rows, cols, stride, dtype, fmt, g, q, None)
+        return f(q, rows, cols, fmt, g, x, stride, dtype, None)
+
+    bad = dc.ERR_INVALID_ARG
+    assert call(x=None) == bad and call(q=None) == bad and call(rows=0) == bad and call(cols=0) == bad
+    assert call(stride=7) == bad and call(dtype=2) == bad and call(fmt=-1) == bad
+    for g in (0.0, -1.0, 3.0, 0.1, float("nan"), float("inf"), 2.0 ** -101, 2.0 ** 101, 1e-45):
+        assert call(g=g) == bad, g
+    assert call(fmt=dc.MX4, g=2.0) == bad
+    assert call(x=FAKE + 8) == dc.ERR_ALIGNMENT and call(q=FAKE + 4) == dc.ERR_ALIGNMENT
+    assert call(rows=1 << 31, stride=8) == dc.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("forward", [False, True])
+def test_products_refuse(forward):
+    lib = dc.lib()
+    size = dc.q4_workspace_bytes(4, 8, dc.NV4) if forward else dc.conv_workspace_bytes()
+
+    def call(x=FAKE, rows=4, c_in=8, w=FAKE, c_out=16, fmt=dc.NV4, scale=1.0, bias=None, act=0, residual=None, y=FAKE, dtype=dc.BF16, ws=FAKE, n=size):
+        if forward:
+            return lib.dc_q4_forward(x, rows, c_in, w, c_out, fmt, scale, 1.0, bias, act, residual, y, dtype, ws, n, None)
+        return lib.dc_q4_product(x, rows, c_in, w, c_out, fmt, scale, bias, act, residual, y, dtype, ws, n, None)
+
+    bad = dc.ERR_INVALID_ARG
+    assert call(x=None) == bad and call(w=None) == bad and call(y=None) == bad
+    assert call(rows=0) == bad and call(c_in=0) == bad and call(c_out=0) == bad and call(fmt=5) == bad
+    assert call(act=2) == bad and call(dtype=7) == bad
+    assert call(scale=float("nan")) == bad and call(scale=float("inf")) == bad
+    if forward:
+        assert call(scale=3.0) == bad and call(fmt=dc.MX4, scale=2.0) == bad
+    assert call(ws=None) == dc.ERR_WORKSPACE and call(n=255) == dc.ERR_WORKSPACE and call(n=size - 1) == dc.ERR_WORKSPACE
+    for arg in ("x", "w", "y", "bias", "residual", "ws"):
+        assert call(**{arg: FAKE + 4}) == dc.ERR_ALIGNMENT, arg
+
+
+def test_binding_checks_shapes_and_types():
+    torch = pytest.importorskip("torch")
+    q = dc.Q4Matrix(6, 40, dc.NV4, 0.5, device="cpu")
+    other = dc.Q4Matrix(6, 40, dc.MX4, device="cpu")
+    w = dc.Q4Matrix(10, 40, dc.NV4, device="cpu")
+    ws = torch.zeros(dc.q4_workspace_bytes(6, 40, dc.NV4), dtype=torch.uint8)
+    for x in (torch.zeros(6, 41), torch.zeros(5, 40), torch.zeros(40, 6).t(), torch.zeros(3, 4, 40)[:, ::2][:, :, :40].transpose(0, 1)):
+        with pytest.raises(ValueError):
+            dc.q4_quantize(x, q, stream=_NullStream())
+    with pytest.raises(ValueError):
+        dc.q4_quantize(torch.zeros(6, 40, dtype=torch.float16), q, stream=_NullStream())
+    y = torch.zeros(6, 10)
+    with pytest.raises(ValueError):
+        dc.q4_product(other, w, None, 0, None, y, ws, stream=_NullStream())
+    for args in ((None, torch.zeros(6, 9)), (None, torch.zeros(6, 20)[:, ::2]), (torch.zeros(10, dtype=torch.bfloat16), y), (torch.zeros(9), y)):
+        with pytest.raises(ValueError):
+            dc.q4_product(q, w, args[0], 0, None, args[1], ws, stream=_NullStream())
+    with pytest.raises(ValueError):
+        dc.q4_product(q, w, None, 0, torch.zeros(6, 10, dtype=torch.bfloat16), y, ws, stream=_NullStream())
+    with pytest.raises(ValueError):
+        dc.q4_forward(torch.zeros(6, 40, dtype=torch.bfloat16), w, 1.0, None, 0, None, y, ws, stream=_NullStream())
+    with pytest.raises(ValueError):
+        dc.q4_forward(torch.zeros(6, 80)[:, ::2], w, 1.0, None, 0, None, y, ws, stream=_NullStream())
+
+
+class _NullStream:
+    cuda_stream = 0
+
+
+def test_rows_at_one_distance():
+    torch = pytest.importorskip("torch")
+    rows = dc._rows_of
+    assert rows(torch.zeros(2, 3, 4, 24), 24, "") == (24, 24)
+    assert rows(torch.zeros(2, 3, 4, 40)[..., :24], 24, "") == (24, 40)
+    assert rows(torch.zeros(24), 24, "") == (1, 24)
+    assert rows(torch.zeros(1, 1, 1, 24), 24, "") == (1, 24)
+    assert rows(torch.zeros(5, 1, 24), 24, "") == (5, 24)
+    with pytest.raises(ValueError):
+        rows(torch.zeros(4, 6, 24)[:, :3], 24, "")
+
+
+def test_tensor_scale():
+    assert dc.q4_tensor_scale(2688.0) == 1.0 and dc.q4_tensor_scale(2689.0) == 2.0 and dc.q4_tensor_scale(1344.0) == 0.5
+    assert dc.q4_tensor_scale(0.0) == 1.0 and dc.q4_tensor_scale(float("nan")) == 1.0
+    for top in (1e-3, 0.7, 5.0, 1e4):
+        g = dc.q4_tensor_scale(top)
+        assert np.log2(g) == np.round(np.log2(g)) and 224 < top / (6 * g) <= 448
+
+
+def test_oracle_against_the_definition():
+    # MX4: largest magnitude 5.0 -> 2^(2-2): codes are the values themselves, rounded
+    x = np.zeros((1, 40))
+    x[0, :8] = [5.0, -0.25, 0.26, 0.75, 1.25, 2.5, -3.5, 6e-3]
+    x[0, 32] = 7.0                                                     # block of its own: 2^0, 7 is cut off at 6
+    code, byte = Q.quantize(x, Q.MX4)
+    assert byte.tolist() == [[127, 127]]
+    assert code[0, :8].tolist() == [6, 8, 1, 2, 2, 4, 14, 0] and code[0, 32] == 7
+    # NV4, g = 1/2: 9 / (6 / 2) = 3 = 1.5 * 2: byte 0x44; codes are value / 1.5
+    x = np.zeros((1, 16))
+    x[0, :3] = [9.0, 4.5, -1.5]
+    code, byte = Q.quantize(x, Q.NV4, 0.5)
+    assert byte[0, 0] == 0x44 and code[0, :3].tolist() == [7, 5, 10]
+    assert Q.values(code, byte, Q.NV4, 0.5)[0, :3].tolist() == [9.0, 4.5, -1.5]
+    # scale bytes are e4m3's own: 448 is 0x7e, the smallest one 2^-9
+    assert Q.E4M3[0x7e] == 448.0 and Q.E4M3[1] == 2.0 ** -9 and len(Q.E4M3) == 127
+
+
+def test_oracle_rounds_ties_to_even_codes():
+    for fmt in (Q.MX4, Q.NV4):
+        ties = np.array([[6.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]])
+        code, _ = Q.quantize(ties, fmt)
+        assert code[0].tolist() == [7, 0, 2, 2, 4, 4, 6, 6]
+
+
+def test_oracle_quantises_what_it_read_back_to_itself():
+    r = np.random.default_rng(3)
+    for fmt, g in ((Q.MX4, 1.0), (Q.NV4, 2.0 ** -8)):
+        v = Q.stands_for(r.standard_normal((50, 96)), fmt, g)
+        assert (Q.stands_for(v, fmt, g) == v).all()
+
+
+def test_unpack_places_scales_as_the_header_says():
+    rows, cols, fmt = 300, 200, dc.NV4
+    lay = dc.q4_layout(rows, cols, fmt)
+    buf = np.zeros(lay.bytes, dtype=np.uint8)
+    r = np.random.default_rng(5)
+    want = r.integers(0, 256, (rows, 13))
+    for i in range(rows):
+        for b in range(13):
+            buf[lay.scale_offset + ((i // 128) * lay.tiles + b // 4) * 512 + (i % 32) * 16 + (i % 128) // 32 * 4 + b % 4] = want[i, b]
+    buf[7 * lay.pitch + 3] = 0xA5
+    code, byte = Q.unpack(buf, rows, cols, fmt)
+    assert (byte[:rows, :13] == want).all() and code[7, 6] == 5 and code[7, 7] == 10

@@ -67,7 +67,7 @@ def stands_for(x, fmt, g=1.0):
 def unpack(buf, rows, cols, fmt):
     """(codes of all columns a row has room for, scale bytes of all rows and blocks its tiles have room for) of a quantised matrix."""
     b = block_of(fmt)
-    pitch = -(-cols // 32) * 16
+    pitch = -(-cols // 64) * 32
     tiles = -(-cols // (4 * b))
     off = -(-rows * pitch // 256) * 256
     raw = np.asarray(buf, dtype=np.uint8)

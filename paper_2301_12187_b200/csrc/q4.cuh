@@ -17,7 +17,7 @@ __host__ __device__ static inline int atom_cols(int format) { return 4 * block_o
 static inline dc_status layout_of(long long rows, int cols, dc_q4_format format, Layout *l) {
   if (rows < 1 || cols < 1 || (format != DC_MX4 && format != DC_NV4)) return DC_ERR_INVALID_ARG;
   if (rows > 0x7fffff00ll || cols > (1 << 24)) return DC_ERR_UNSUPPORTED;
-  l->pitch = dc_round_up((size_t)cols, 32) / 2;
+  l->pitch = dc_round_up((size_t)cols, 64) / 2;
   l->tiles = dc_round_up((size_t)cols, atom_cols(format)) / atom_cols(format);
   l->scale_offset = dc_round_up((size_t)rows * l->pitch, 256);
   l->bytes = l->scale_offset + dc_round_up((size_t)rows, 128) / 128 * l->tiles * kAtom;

@@ -1,15 +1,19 @@
 // Products of matrices in microscaled 4 bits on the tensor core (dc_q4_product, dc_q4_forward).
 //
-// tcgen05.mma.block_scale multiplies 64 columns of 128 rows x NT rows at a time: codes from shared memory (rows of 128 bytes, 256 codes, TMA
-// with the 128-byte swizzle), scales from tensor memory, where tcgen05.cp puts them from the tiles in which a quantised matrix keeps them
+// tcgen05.mma.block_scale multiplies 64 columns of 128 rows x nt rows at a time: codes from shared memory (rows of 128 bytes, 256 codes, with
+// the 128-byte swizzle), scales from tensor memory, where tcgen05.cp puts them from the tiles in which a quantised matrix keeps them
 // (32 lanes x 4 columns, one for each 32 rows of the tile; four bytes a column, which are four blocks).  DC_NV4: a tile is one instruction's
 // scales; DC_MX4: two instructions', told apart by the descriptor's scale id.  Sums are fp32 in tensor memory.
 //
 // A stage of the ring is 256 columns: codes of both operands and their scale tiles; its scales have columns of tensor memory of their own, so a
-// slot's scales are written over only behind the products that read them.  One warp loads, one issues, eight read out the accumulators
-// (two sets where they fit), each thread one row.  A CTA walks over tiles; few tiles: a cluster shares a tile's columns and adds the parts
-// up in rank order, through shared memory.  Tensor memory is given back before the CTAs of a cluster wait for one another: who holds
-// some never waits for a CTA that may be waiting for some.
+// slot's scales are written over only behind the products that read them.  One warp loads, one issues, eight read out the accumulators.
+// CTAs walk over tiles.  The forms:
+//   kOne     both operands by TMA.  Few tiles: a cluster shares a tile's columns and adds the parts up in rank order, through shared memory.
+//            Tensor memory is given back before the CTAs of a cluster wait for one another: who holds some never waits for a CTA that may be
+//            waiting for some.  One column of tiles and few stages: w stays in shared memory.
+//   kPair    two CTAs multiply 256 x 256 (cta_group::2): each loads half of either operand, which halves what an SM has to fetch of w.
+//   kRows    few rows of bf16 or fp32: quantised by the reading-out warps into shared memory, where all of them stay.
+//   kStream  many rows of bf16 or fp32 and one column of tiles: eight more warps quantise them, a stage at a time.
 #include <string.h>
 
 #include "q4.cuh"
@@ -19,32 +23,38 @@ namespace {
 using namespace tc;
 using q4::kAtom;
 
-constexpr int kEpiWarps = 8, kThreads = (2 + kEpiWarps) * 32;
+enum { kOne = 0, kPair = 1, kRows = 2, kStream = 3 };
+constexpr int kEpiWarps = 8, kCutWarps = 8;
+template <int FORM>
+constexpr int kThreadsOf = (2 + kEpiWarps + (FORM == kStream ? kCutWarps : 0)) * 32;
 constexpr int kMaxStages = 8, kMaxSplit = 8;
 constexpr int kSmemMax = 225 * 1024;
 constexpr int kStageCols = 256;                  // columns of a stage: 128 bytes of codes
+constexpr int kOut = 32;                         // columns that a warp reads out at a time
+constexpr int kOutBytes = 32 * kOut * 4;         // ... and its shared memory for them
+constexpr int kMaxRows = 32;                     // of form kRows
 
 struct Params {
   long long rows;
   int c_in, c_out, act;
   float scale;
+  float g, g6;               // kRows, kStream: x's tensor scale
+  int nt, nb;                // rows of w in a tile, 128-row scale tiles that they touch
   int tiles_m, tiles_n, items;
-  int chunks, atoms;         // stages of a row; scale tiles of a row of them
+  int chunks;                // stages of a row
   int split, chunks_per;     // CTAs that share an item, stages of each
-  int stages, acc_bufs;
+  int stages, acc_bufs, sets;                // sets: the reading-out warps take tiles in turn, four warps each
+  int stage_bytes, sf_cols;  // of a stage: shared memory, and tensor memory of its scales
+  int w_stays, w_bytes;      // w's stages stay in shared memory; bytes of one
+  int groups;                // kRows: groups of 8 rows
+  int off_sfa, off_ring, off_out;
   int vec;                   // rows of y begin on 16 bytes
-  const uint8_t *sx, *sw;    // scale tiles
+  int vec_x;                 // kRows: rows of x do
 };
 
-template <int F, int NT>
-struct Shape {
-  static constexpr int kAtoms = F == DC_NV4 ? 4 : 2;             // scale tiles of a stage, for 128 rows
-  static constexpr int kNb = NT > 128 ? 2 : 1;                   // 128-row tiles that NT rows touch
-  static constexpr int kA = 128 * 128, kB = NT * 128, kSfa = kAtoms * kAtom, kSfb = kNb * kAtoms * kAtom;
-  static constexpr int kStage = kA + kB + kSfa + kSfb;
-  static constexpr int kSfCols = 4 * kAtoms * (1 + kNb);         // tensor memory of a stage's scales
-  static_assert(kStage % 1024 == 0, "operands begin on 1024 bytes");
-};
+constexpr int kA = 128 * 128;                    // codes of x in a stage, bytes
+template <int F>
+constexpr int kAtomsOf = F == DC_NV4 ? 4 : 2;    // scale tiles of a stage, for 128 rows
 
 __device__ __forceinline__ uint64_t operand_desc(uint32_t a) {   // K-major, 128-byte swizzle, 1024 bytes between groups of 8 rows
   return ((uint64_t)((64u) | (1u << 14) | (2u << 29)) << 32) | (uint64_t)((a >> 4) & 0x3FFFu) | (1u << 16);
@@ -52,207 +62,476 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t a) {   // K-major, 128
 __device__ __forceinline__ uint64_t scales_desc(uint32_t a) {    // a scale tile: 32 rows of 16 bytes, 128 between groups of 8
   return ((uint64_t)((8u) | (1u << 14)) << 32) | (uint64_t)((a >> 4) & 0x3FFFu) | (1u << 16);
 }
+// the pair's forms act in both CTAs: each copies from its own shared to its own tensor memory, and multiplies its own 128 rows
+template <bool P>
 __device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+  if (P) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
-template <int F>
+#define Q4_MMA(GROUP, KIND)                                                                            \
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                       \
+               "tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory")
+template <int F, bool P>
 __device__ __forceinline__ void mma_q4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
-  if (F == DC_NV4)
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
-  else
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+  if (F == DC_NV4) {
+    if (P) Q4_MMA("2", "mxf4nvf4.block_scale.scale_vec::4X");
+    else Q4_MMA("1", "mxf4nvf4.block_scale.scale_vec::4X");
+  } else {
+    if (P) Q4_MMA("2", "mxf4.block_scale.scale_vec::2X");
+    else Q4_MMA("1", "mxf4.block_scale.scale_vec::2X");
+  }
 }
-// instruction descriptor: e2m1 x e2m1, N, M = 128, type of the scales; `id`: which half of a scale word (DC_MX4)
+#undef Q4_MMA
+// instruction descriptor: e2m1 x e2m1, N, M, type of the scales; `id`: which half of a scale word (DC_MX4)
 template <int F>
-__device__ __forceinline__ uint32_t q4_idesc(int n, uint32_t id) {
-  return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((F == DC_MX4 ? 1u : 0u) << 23) | (1u << 27) | (id << 29);
+__device__ __forceinline__ uint32_t q4_idesc(int n, int m, uint32_t id) {
+  return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((F == DC_MX4 ? 1u : 0u) << 23) | ((uint32_t)(m >> 7) << 27) | (id << 29);
+}
+// arrives at the barrier (of both CTAs of a pair) once all that this thread has issued is done
+template <bool P>
+__device__ __forceinline__ void commit(uint64_t *bar) {
+  if (P)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3)
+                 : "memory");
+  else
+    umma_commit(bar);
+}
+// loads that report to a barrier of the pair's first CTA (cluster address `bar`)
+__device__ __forceinline__ void pair_load_2d(uint32_t sdst, const CUtensorMap *map, uint32_t bar, int c0, int c1) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(sdst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void pair_load_3d(uint32_t sdst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(sdst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// 16 results of a row, from column `o`: bias, residual, activation, store
+// What a lane delivers: N neighbouring results of a row, 16 bytes of y.
 template <typename T>
-__device__ __forceinline__ void deliver16(const Params &p, const float *__restrict__ bias, const T *residual, T *y, long long row, int o, float *v) {
+constexpr int kPer = 16 / (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ void unpack16(uint4 w, float *r) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (sizeof(T) == 2) { r[2 * j % kPer<T>] = __uint_as_float(u[j] << 16); r[(2 * j + 1) % kPer<T>] = __uint_as_float(u[j] & 0xffff0000u); }
+    else r[j] = __uint_as_float(u[j]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack16(const float *v) {
+  constexpr int N = kPer<T>;
+  if (N == 8) return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4 % N], v[5 % N]), pack_bf16x2(v[6 % N], v[7 % N]));
+  return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ void load_bias(const float *__restrict__ bias, int o, int n, float *b) {
+#pragma unroll
+  for (int i = 0; i < n; i += 4) *reinterpret_cast<float4 *>(b + i) = bias ? __ldg(reinterpret_cast<const float4 *>(bias + o + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+}
+// columns one by one, where rows of y do not begin on 16 bytes
+template <typename T>
+__device__ __forceinline__ void deliver_one(const Params &p, float t, bool has_bias, float b, const T *residual, T *y, size_t at) {
+  t *= p.scale;
+  if (has_bias) t += b;
+  if (residual) t += (float)residual[at];
+  y[at] = (T)dc_act_apply(t, p.act);
+}
+// the same of a part's sum (form kOne, split)
+template <typename T>
+__device__ __forceinline__ void deliver(const Params &p, const float *__restrict__ bias, const T *residual, T *y, long long row, int o, float *v) {
+  constexpr int N = kPer<T>;
   const size_t at = (size_t)row * (size_t)p.c_out + (size_t)o;
-  if (o + 16 <= p.c_out && p.vec) {
-    float r[16];
-    if (residual) {
-      if (sizeof(T) == 2) {
+  if (p.vec) {                                   // rows then have whole pieces
+    float b[N], r[N];
+    load_bias(bias, o, N, b);
+    if (residual) unpack16<T>(*reinterpret_cast<const uint4 *>(residual + at), r);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint4 w = reinterpret_cast<const uint4 *>(residual + at)[i];
-          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) { r[8 * i + 2 * j] = __uint_as_float(u[j] << 16); r[8 * i + 2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u); }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(r + 4 * i) = reinterpret_cast<const float4 *>(residual + at)[i];
-      }
+    for (int i = 0; i < N; ++i) {
+      float t = v[i] * p.scale;
+      if (bias) t += b[i];
+      if (residual) t += r[i];
+      v[i] = dc_act_apply(t, p.act);
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float s = v[i] * p.scale;
-      if (bias) s += __ldg(bias + o + i);
-      if (residual) s += r[i];
-      v[i] = dc_act_apply(s, p.act);
-    }
-    if (sizeof(T) == 2) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        reinterpret_cast<uint4 *>(y + at)[i] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]),
-                                                          pack_bf16x2(v[8 * i + 4], v[8 * i + 5]), pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) reinterpret_cast<float4 *>(y + at)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-    }
+    *reinterpret_cast<uint4 *>(y + at) = pack16<T>(v);
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (o + i < p.c_out) {
-      float s = v[i] * p.scale;
-      if (bias) s += __ldg(bias + o + i);
-      if (residual) s += sizeof(T) == 2 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(residual)[at + i]) : reinterpret_cast<const float *>(residual)[at + i];
-      s = dc_act_apply(s, p.act);
-      if (sizeof(T) == 2) reinterpret_cast<__nv_bfloat16 *>(y)[at + i] = __float2bfloat16_rn(s);
-      else reinterpret_cast<float *>(y)[at + i] = s;
+  for (int i = 0; i < N; ++i)
+    if (o + i < p.c_out) deliver_one<T>(p, v[i], bias != nullptr, bias ? __ldg(bias + o + i) : 0.f, residual, y, at + i);
+}
+// 32 rows x 32 results in the warp's shared memory -> y from row `row0`, column `o`: neighbouring lanes store neighbouring columns.
+template <typename T>
+__device__ __forceinline__ void deliver32(const Params &p, const float *__restrict__ bias, const T *residual, T *y, long long row0, int o,
+                                          uint32_t sm, int lane) {
+  const int rows = p.rows - row0 < 32 ? (int)(p.rows - row0) : 32;
+  if (p.vec) {
+    constexpr int N = kPer<T>, kLanes = kOut / N, kStep = 32 / kLanes, kTimes = 32 / kStep;     // lanes to a row, rows at a time, times
+    const int c = (lane % kLanes) * N, r0 = lane / kLanes;
+    if (o + c >= p.c_out) return;
+    float b[N];
+    load_bias(bias, o + c, N, b);
+    const size_t at = (size_t)(row0 + r0) * (size_t)p.c_out + (size_t)(o + c), pitch = (size_t)p.c_out * kStep;
+#pragma unroll
+    for (int h = 0; h < kTimes; h += 4) {        // four rows at once, so that their loads overlap
+      uint4 res[4];
+      float t[4][N];
+      if (residual) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (r0 + (h + i) * kStep < rows) res[i] = *reinterpret_cast<const uint4 *>(residual + at + pitch * (h + i));
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = r0 + (h + i) * kStep;
+#pragma unroll
+        for (int j = 0; j < N; j += 4) *reinterpret_cast<uint4 *>(&t[i][j]) = lds_u4(sm + (uint32_t)(r * 128 + (((c + j) >> 2) ^ (r & 7)) * 16));
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[N];
+        if (residual) unpack16<T>(res[i], v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          float u = t[i][j] * p.scale;
+          if (bias) u += b[j];
+          if (residual) u += v[j];
+          t[i][j] = dc_act_apply(u, p.act);
+        }
+        if (r0 + (h + i) * kStep < rows) *reinterpret_cast<uint4 *>(y + at + pitch * (h + i)) = pack16<T>(t[i]);
+      }
     }
+  } else if (o + lane < p.c_out) {               // a lane to a column
+    const float b = bias ? __ldg(bias + o + lane) : 0.f;
+    size_t at = (size_t)row0 * (size_t)p.c_out + (size_t)(o + lane);
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r, at += (size_t)p.c_out)
+      deliver_one<T>(p, lds_f(sm + (uint32_t)(r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4)), bias != nullptr, b, residual, y, at);
+  }
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kBars = kDEmpty + 2 };
+// 16 columns of a row of x from column c: the values, zeros from column c_in on
+template <typename T>
+__device__ __forceinline__ void load_x16(const T *__restrict__ row, int c, int c_in, int vec, float *v) {
+  if (vec && c + 16 <= c_in) {
+#pragma unroll
+    for (int i = 0; i < 16 / kPer<T>; ++i) unpack16<T>(__ldg(reinterpret_cast<const uint4 *>(row + c) + i), v + i * kPer<T>);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16 / kPer<T>; ++i) {
+      const int o = c + i * kPer<T>;
+      if (vec && o + kPer<T> <= c_in) {
+        unpack16<T>(__ldg(reinterpret_cast<const uint4 *>(row + o)), v + i * kPer<T>);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kPer<T>; ++j) v[i * kPer<T> + j] = o + j < c_in ? (float)row[o + j] : 0.f;
+      }
+    }
+  }
+}
+// 16 columns, piece `seg` of a row, -> codes in an operand's rows and the block's scale in its tile.  `top`: largest magnitude of the piece.
+template <int F>
+__device__ __forceinline__ void put_x16(float *v, const Params &p, uint32_t a, uint32_t sfa, int row, int seg, bool valid) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  if (F == DC_MX4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  const q4::BlockScale s = q4::block_scale<F>(top, p.g, p.g6);
+  const uint2 code = q4::codes16<F>(v, s);
+  if (valid) {
+    const uint32_t at = a + (uint32_t)((row >> 3) * 1024 + (row & 7) * 128 + ((((seg & 15) >> 1) ^ (row & 7)) * 16) + (seg & 1) * 8);
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(code.x), "r"(code.y) : "memory");
+    if (F == DC_NV4 || (seg & 1) == 0) {
+      const uint32_t b = (uint32_t)(F == DC_NV4 ? seg : seg >> 1);
+      asm volatile("st.shared.b8 [%0], %1;" ::"r"(sfa + (b >> 2) * kAtom + q4::scale_at((uint32_t)row, b)), "r"(s.byte) : "memory");
+    }
+  }
+}
 
-template <int F, int NT, typename T>
-__global__ void __launch_bounds__(kThreads, 1)
-k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const float *__restrict__ bias,
-             const T *residual, T *y, const __grid_constant__ Params p, DcWsHeader *ws) {
-  using S = Shape<F, NT>;
+enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kXFull = kDEmpty + 2, kWFull, kBars };
+
+template <int F, typename T, int FORM>
+__global__ void __launch_bounds__(kThreadsOf<FORM>, 1)
+k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_sx, const __grid_constant__ CUtensorMap map_w,
+             const __grid_constant__ CUtensorMap map_sw, const T *__restrict__ x, const float *__restrict__ bias, const T *residual, T *y,
+             const __grid_constant__ Params p, DcWsHeader *ws) {
+  constexpr int kAtoms = kAtomsOf<F>;
+  constexpr bool P = FORM == kPair;
+  constexpr uint32_t kTmemCols = 512;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kBars];
   __shared__ uint32_t tmem_s, abort_s;
   volatile uint32_t *abort_flag = &abort_s;
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sm = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  constexpr uint32_t kTmemCols = 512;
   if (warp == 0) {
     if (lane == 0) {
       abort_s = 0;
-      for (int i = 0; i < kMaxStages; ++i) { mbar_init(&bar[kFull + i], 1); mbar_init(&bar[kEmpty + i], 1); }
-      for (int i = 0; i < 2; ++i) { mbar_init(&bar[kDFull + i], 1); mbar_init(&bar[kDEmpty + i], kEpiWarps); }
+      for (int i = 0; i < kMaxStages; ++i) {
+        mbar_init(&bar[kFull + i], FORM == kStream ? (p.w_stays ? 4 : 5) : 1);
+        mbar_init(&bar[kEmpty + i], 1);
+      }
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&bar[kDFull + i], 1);
+        mbar_init(&bar[kDEmpty + i], P ? 2 * kEpiWarps : (p.sets == 2 ? kEpiWarps / 2 : kEpiWarps));
+      }
+      mbar_init(&bar[kXFull], kEpiWarps);
+      mbar_init(&bar[kWFull], 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      prefetch_tensormap(&map_x);
       prefetch_tensormap(&map_w);
+      prefetch_tensormap(&map_sw);
+      if (FORM == kOne || P) { prefetch_tensormap(&map_x); prefetch_tensormap(&map_sx); }
     }
     __syncwarp();
   } else if (warp == 1) {
-    tmem_alloc(&tmem_s, kTmemCols);
-    tmem_relinquish();
+    if (P) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(kTmemCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      tmem_alloc(&tmem_s, kTmemCols);
+      tmem_relinquish();
+    }
   }
   tc_fence_before();
   __syncthreads();
+  if (P) cluster_sync();                         // the barriers of both CTAs are there
   tc_fence_after();
   const uint32_t tmem = tmem_s;
   dc_pdl_enter();
 
-  const int rank = p.split > 1 ? (int)(blockIdx.x % (unsigned)p.split) : 0;
-  const int first = (int)blockIdx.x / p.split, step = (int)gridDim.x / p.split;
-  const int c0 = rank * p.chunks_per, c1 = min(p.chunks, c0 + p.chunks_per);
-  const uint32_t sf_base = tmem + (uint32_t)(p.acc_bufs * NT);
+  const int team = P ? 2 : p.split;              // CTAs that share an item
+  const int rank = team > 1 ? (int)(blockIdx.x % (unsigned)team) : 0;
+  const int first = (int)blockIdx.x / team, step = (int)gridDim.x / team;
+  const int c0 = P ? 0 : rank * p.chunks_per, c1 = P ? p.chunks : min(p.chunks, c0 + p.chunks_per);
+  const int part_pitch = ((p.nt + 31) & ~31) * 4 + 16;         // bytes between rows of a part: no bank conflicts
+  const uint32_t sf_base = tmem + (uint32_t)(p.acc_bufs * p.nt);
+  const uint32_t ring = sm + (uint32_t)p.off_ring, w_base = ring + (uint32_t)(p.stages * p.stage_bytes);
+  const int b_rows = P ? p.nt / 2 : p.nt;
+  const uint32_t w_codes = (uint32_t)b_rows * 128u;
 
   if (warp == 0) {
+    // ---------------------------------------------------------------- load
+    if (p.w_stays && elect_one()) {
+      mbar_arrive_expect_tx(&bar[kWFull], (uint32_t)(p.chunks * p.w_bytes));
+      for (int ch = 0; ch < p.chunks; ++ch) {
+        const uint32_t b = w_base + (uint32_t)(ch * p.w_bytes);
+        tma_load_2d(b, &map_w, &bar[kWFull], ch * 128, 0);
+        tma_load_3d(b + w_codes, &map_sw, &bar[kWFull], 0, ch * kAtoms, 0);
+      }
+    }
+    __syncwarp();
     int stage = 0;
     uint32_t parity = 0;
     bool ok = true;
-    for (int item = first; ok && item < p.items; item += step) {
-      const int tm = item % p.tiles_m, tn = item / p.tiles_m;
-      for (int ch = c0; ch < c1; ++ch) {
-        ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x10000u | (uint32_t)stage);
-        if (!ok) break;
-        if (elect_one()) {
-          const uint32_t a = sm + (uint32_t)stage * S::kStage, b = a + S::kA, sfa = b + S::kB, sfb = sfa + S::kSfa;
-          const int na = min(S::kAtoms, p.atoms - ch * S::kAtoms);
-          const int wt0 = tn * NT / 128, nb = min(S::kNb, dc_div_up(p.c_out, 128) - wt0);
-          uint64_t *full = &bar[kFull + stage];
-          mbar_arrive_expect_tx(full, (uint32_t)(S::kA + S::kB + na * kAtom * (1 + nb)));
-          tma_load_2d(a, &map_x, full, ch * 128, tm * 128);
-          tma_load_2d(b, &map_w, full, ch * 128, tn * NT);
-          bulk_load(sfa, p.sx + ((size_t)tm * p.atoms + (size_t)ch * S::kAtoms) * kAtom, (uint32_t)(na * kAtom), full);
-          for (int i = 0; i < nb; ++i)
-            bulk_load(sfb + (uint32_t)(i * S::kAtoms * kAtom), p.sw + ((size_t)(wt0 + i) * p.atoms + (size_t)ch * S::kAtoms) * kAtom, (uint32_t)(na * kAtom), full);
+    if (!(FORM == kStream && p.w_stays))
+      for (int item = first; ok && item < p.items; item += step) {
+        const int tm = item % p.tiles_m, tn = item / p.tiles_m, x_tile = P ? tm * 2 + rank : tm;
+        for (int ch = c0; ch < c1; ++ch) {
+          ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x10000u | (uint32_t)stage);
+          if (!ok) break;
+          if (elect_one()) {
+            uint64_t *full = &bar[kFull + stage];
+            const uint32_t at = ring + (uint32_t)(stage * p.stage_bytes);
+            const uint32_t sfa = at + kA, b = FORM == kRows ? at : sfa + kAtoms * kAtom;
+            constexpr uint32_t kX = FORM == kOne || P ? (uint32_t)(kA + kAtoms * kAtom) : 0u;
+            const uint32_t bytes = kX + (p.w_stays ? 0u : w_codes + (uint32_t)(p.nb * kAtoms * kAtom));
+            if (P) {
+              const uint32_t to = map_cluster(smem_u32(full), 0);
+              if (rank == 0) mbar_arrive_expect_tx(full, 2 * bytes);
+              pair_load_2d(at, &map_x, to, ch * 128, x_tile * 128);
+              pair_load_3d(sfa, &map_sx, to, 0, ch * kAtoms, x_tile);
+              pair_load_2d(b, &map_w, to, ch * 128, tn * p.nt + rank * b_rows);
+              pair_load_3d(b + w_codes, &map_sw, to, 0, ch * kAtoms, tn * p.nt / 128);
+            } else {
+              mbar_arrive_expect_tx(full, bytes);
+              if (FORM == kOne) {
+                tma_load_2d(at, &map_x, full, ch * 128, x_tile * 128);
+                tma_load_3d(sfa, &map_sx, full, 0, ch * kAtoms, x_tile);
+              }
+              if (!p.w_stays) {
+                tma_load_2d(b, &map_w, full, ch * 128, tn * p.nt);
+                tma_load_3d(b + w_codes, &map_sw, full, 0, ch * kAtoms, tn * p.nt / 128);
+              }
+            }
+          }
+          __syncwarp();
+          if (++stage == p.stages) { stage = 0; parity ^= 1u; }
         }
-        __syncwarp();
-        if (++stage == p.stages) { stage = 0; parity ^= 1u; }
       }
-    }
   } else if (warp == 1) {
+    // ---------------------------------------------------------------- multiply
     int stage = 0, n = 0;
     uint32_t parity = 0;
-    bool ok = true;
+    bool ok = !P || rank == 0;
+    if (FORM == kRows && ok) ok = warp_wait(&bar[kXFull], 0, abort_flag, ws, 0x50000u);
+    if (p.w_stays && ok) ok = warp_wait(&bar[kWFull], 0, abort_flag, ws, 0x60000u);
     for (int item = first; ok && item < p.items; item += step, ++n) {
       const int buf = p.acc_bufs == 2 ? n & 1 : 0;
       const uint32_t use = (uint32_t)(p.acc_bufs == 2 ? n >> 1 : n);
       ok = warp_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x20000u | (uint32_t)buf);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t d = tmem + (uint32_t)(buf * NT);
+      const uint32_t d = tmem + (uint32_t)(buf * p.nt);
       for (int ch = c0; ch < c1; ++ch) {
         ok = warp_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x30000u | (uint32_t)stage);
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
-          const uint32_t a = sm + (uint32_t)stage * S::kStage, b = a + S::kA, sfa = b + S::kB, sfb = sfa + S::kSfa;
-          const uint32_t ta = sf_base + (uint32_t)(stage * S::kSfCols), tb = ta + 4u * S::kAtoms;
-          const int na = min(S::kAtoms, p.atoms - ch * S::kAtoms), steps = min(4, dc_div_up(p.c_in - ch * kStageCols, 64));
+          const uint32_t at = ring + (uint32_t)(stage * p.stage_bytes);
+          const uint32_t a = FORM == kRows ? sm + (uint32_t)((ch - c0) * p.groups * 1024) : at;
+          const uint32_t sfa = FORM == kRows ? sm + (uint32_t)(p.off_sfa + (ch - c0) * kAtoms * kAtom) : at + kA;
+          const uint32_t b = p.w_stays ? w_base + (uint32_t)(ch * p.w_bytes) : (FORM == kRows ? at : at + kA + kAtoms * kAtom), sfb = b + w_codes;
+          const uint32_t ta = sf_base + (uint32_t)(stage * p.sf_cols), tb = ta + 4u * kAtoms;
+          const int steps = min(4, dc_div_up(p.c_in - ch * kStageCols, 64)), na = F == DC_NV4 ? steps : (steps + 1) / 2;
           for (int i = 0; i < na; ++i) {
-            copy_scales(ta + 4u * i, scales_desc(sfa + (uint32_t)(i * kAtom)));
-#pragma unroll
-            for (int j = 0; j < S::kNb; ++j) copy_scales(tb + 4u * (uint32_t)(i * S::kNb + j), scales_desc(sfb + (uint32_t)((j * S::kAtoms + i) * kAtom)));
+            copy_scales<P>(ta + 4u * i, scales_desc(sfa + (uint32_t)(i * kAtom)));
+            for (int j = 0; j < p.nb; ++j) copy_scales<P>(tb + 4u * (uint32_t)(i * p.nb + j), scales_desc(sfb + (uint32_t)((j * kAtoms + i) * kAtom)));
           }
           const uint64_t ad = operand_desc(a), bd = operand_desc(b);
           for (int k = 0; k < steps; ++k) {
             const uint32_t atom = F == DC_NV4 ? (uint32_t)k : (uint32_t)(k >> 1), id = F == DC_NV4 ? 0u : (uint32_t)(k & 1) * 2u;
-            mma_q4<F>(d, ad + 2u * k, bd + 2u * k, q4_idesc<F>(NT, id), ta + 4u * atom, tb + 4u * S::kNb * atom, ch > c0 || k > 0 ? 1u : 0u);
+            mma_q4<F, P>(d, ad + 2u * k, bd + 2u * k, q4_idesc<F>(p.nt, P ? 256 : 128, id), ta + 4u * atom, tb + 4u * (uint32_t)p.nb * atom,
+                         ch > c0 || k > 0 ? 1u : 0u);
           }
-          umma_commit(&bar[kEmpty + stage]);
-          if (ch == c1 - 1) umma_commit(&bar[kDFull + buf]);
+          commit<P>(&bar[kEmpty + stage]);
+          if (ch == c1 - 1) commit<P>(&bar[kDFull + buf]);
         }
         __syncwarp();
         if (++stage == p.stages) { stage = 0; parity ^= 1u; }
       }
     }
-  } else {
-    const int quad = warp & 3, half = (warp - 2) >> 2, r = quad * 32 + lane;
+  } else if (warp < 2 + kEpiWarps) {
+    // ---------------------------------------------------------------- read out
+    const int quad = warp & 3, set = (warp - 2) >> 2;
+    if (FORM == kRows) {
+      // the whole rows, as far as this CTA multiplies them, in pieces of 16 columns
+      const int segs = (min(p.c_in - c0 * kStageCols, (c1 - c0) * kStageCols) + 63) / 64 * 4, total = (int)p.rows * segs;
+      for (int u0 = (warp - 2) * 32; u0 < total; u0 += kEpiWarps * 32) {
+        const int u = u0 + lane, row = u / segs, seg = u - row * segs;
+        float v[16];
+        const bool valid = u < total;
+        if (valid) {
+          load_x16<T>(x + (size_t)row * (size_t)p.c_in, c0 * kStageCols + seg * 16, p.c_in, p.vec_x, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        }
+        put_x16<F>(v, p, sm + (uint32_t)((seg >> 4) * p.groups * 1024), sm + (uint32_t)p.off_sfa, row, seg, valid);
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar[kXFull]);
+    }
+    const uint32_t out = sm + (uint32_t)(p.off_out + (warp - 2) * kOutBytes), mine = out + (uint32_t)lane * 128u;
+    const uint32_t freed = P ? map_cluster(smem_u32(&bar[kDEmpty]), 0) : 0u;
+    const int c_first = p.sets == 2 ? 0 : set * kOut, c_step = p.sets == 2 ? kOut : 2 * kOut;
     int n = 0;
     for (int item = first; item < p.items; item += step, ++n) {
+      if (p.sets == 2 && (n & 1) != set) continue;
       const int buf = p.acc_bufs == 2 ? n & 1 : 0;
       const uint32_t use = (uint32_t)(p.acc_bufs == 2 ? n >> 1 : n);
       const int tm = item % p.tiles_m, tn = item / p.tiles_m;
-      const long long row = (long long)tm * 128 + r;
+      const long long row0 = (long long)(P ? tm * 2 + rank : tm) * 128 + quad * 32;
+      const int cols = min(p.nt, p.c_out - tn * p.nt);
       if (!warp_wait(&bar[kDFull + buf], use & 1u, abort_flag, ws, 0x40000u | (uint32_t)buf)) break;
       tc_fence_after();
-      const uint32_t d = tmem + (uint32_t)(buf * NT) + ((uint32_t)(quad * 32) << 16);
+      const bool work = row0 < p.rows && c_first < cols;
+      const uint32_t d = tmem + (uint32_t)(buf * p.nt) + ((uint32_t)(quad * 32) << 16);
+      uint32_t v[kOut];
+      if (work) tmem_ld32(d + (uint32_t)c_first, v);
 #pragma unroll 1
-      for (int c = half * (NT / 2); c < (half + 1) * (NT / 2); c += 16) {
-        float v[16];
-        tmem_ld16(d + (uint32_t)c, reinterpret_cast<uint32_t *>(v));
-        tmem_ld_wait();
-        if (p.split > 1) {
-          if (row < p.rows) {
+      for (int c = c_first; c < cols || c == c_first; c += c_step) {
+        const bool last = c + c_step >= cols;
+        if (work) {
+          tmem_ld_wait();
+          if (FORM != kPair && FORM != kStream && p.split > 1) {
+            if (row0 + lane < p.rows) {
+              const uint32_t at = sm + (uint32_t)((quad * 32 + lane) * part_pitch + c * 4);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              asm volatile("st.shared.f32 [%0], %1;" ::"r"(sm + (uint32_t)(((c + i) * 128 + r) * 4)), "f"(v[i]) : "memory");
+              for (int i = 0; i < kOut / 4; ++i) sts_u4(at + (uint32_t)(i * 16), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+            }
+          } else {
+            // 16-byte pieces of a row are swapped by the row's low bits: no bank conflicts on either side
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sts_u4(mine + (uint32_t)((i ^ (lane & 7)) * 16), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+            __syncwarp();
           }
-        } else if (row < p.rows) {
-          deliver16<T>(p, bias, residual, y, row, tn * NT + c, v);
+          if (!last) tmem_ld32(d + (uint32_t)(c + c_step), v);
+        }
+        if (last) {                              // the accumulator is read: the next tile may have it
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (P) arrive_cluster(freed + (uint32_t)(buf * 8));
+            else mbar_arrive(&bar[kDEmpty + buf]);
+          }
+        }
+        if (work && (FORM == kPair || FORM == kStream || p.split == 1)) {
+          deliver32<T>(p, bias, residual, y, row0, tn * p.nt + c, out, lane);
+          __syncwarp();
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bar[kDEmpty + buf]);
+    }
+  } else {
+    // ---------------------------------------------------------------- quantise (kStream): a thread to a row, two groups of four warps take the stages in turn
+    const int group = (warp - 2 - kEpiWarps) >> 2, r = ((warp - 2 - kEpiWarps) & 3) * 32 + lane;
+    int stage = 0, n = 0;
+    uint32_t parity = 0;
+    bool ok = true;
+    for (int item = first; ok && item < p.items; item += step) {
+      const long long row = (long long)(item % p.tiles_m) * 128 + r;
+      const T *at = x + (size_t)(row < p.rows ? row : 0) * (size_t)p.c_in;
+      for (int ch = 0; ch < p.chunks; ++ch, ++n) {
+        if ((n & 1) == group) {
+          ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x70000u | (uint32_t)stage);
+          if (!ok) break;
+          const uint32_t a = ring + (uint32_t)(stage * p.stage_bytes), sfa = a + kA;
+          const int left = min(p.c_in - ch * kStageCols, kStageCols), pieces = (left + 63) / 64 * 4;
+#pragma unroll 1
+          for (int seg = 0; seg < pieces; seg += 2) {
+            // both halves of a DC_MX4 block are this thread's
+            float v[2][16];
+            uint32_t top[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (row < p.rows) {
+                load_x16<T>(at, ch * kStageCols + (seg + h) * 16, p.c_in, 1, v[h]);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[h][i] = 0.f;
+              }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              top[h] = 0;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) top[h] = max(top[h], __float_as_uint(v[h][i]) & 0x7fffffffu);
+            }
+            if (F == DC_MX4) top[0] = top[1] = max(top[0], top[1]);
+            uint2 code[2];
+            uint32_t byte[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.g6);
+              code[h] = q4::codes16<F>(v[h], s);
+              byte[h] = s.byte;
+            }
+            sts_u4(a + (uint32_t)((r >> 3) * 1024 + (r & 7) * 128 + ((seg >> 1) ^ (r & 7)) * 16), make_uint4(code[0].x, code[0].y, code[1].x, code[1].y));
+            const uint32_t blk = (uint32_t)(F == DC_NV4 ? seg : seg >> 1), to = sfa + (blk >> 2) * kAtom + q4::scale_at((uint32_t)r, blk);
+            if (F == DC_NV4) asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"((uint16_t)(byte[0] | (byte[1] << 8))) : "memory");
+            else asm volatile("st.shared.b8 [%0], %1;" ::"r"(to), "r"(byte[0]) : "memory");
+          }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar[kFull + stage]);
+        }
+        if (++stage == p.stages) { stage = 0; parity ^= 1u; }
+      }
     }
   }
   if (warp == 1 && *abort_flag) {                // copies and products may still be in flight: give them time to end
@@ -262,25 +541,36 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (P) {
+    cluster_sync();                              // neither CTA's memory is touched by the other's instructions any more
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    return;
+  }
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
-  if (p.split > 1) {
-    // the parts, [column][row], added up in rank order; each CTA delivers a share of the columns, 16 at a time
+  if (FORM != kStream && p.split > 1) {
+    // the parts, [row][column], added up in rank order; each CTA delivers a share of the 16-byte pieces of y
+    constexpr int kThreads = kThreadsOf<FORM>;
     cluster_sync();
-    const int tm = first % p.tiles_m, tn = first / p.tiles_m;
     if (abort_s == 0) {
-      for (int u = tid; u < 128 * (NT / 16); u += kThreads) {
-        const int c = (u >> 7) * 16, r = u & 127;
-        const long long row = (long long)tm * 128 + r;
-        if ((u >> 7) % p.split != rank || row >= p.rows) continue;
-        float v[16];
+      const int tm = first % p.tiles_m, tn = first / p.tiles_m;
+      const long long row0 = (long long)tm * 128;
+      const int rows = p.rows - row0 < 128 ? (int)(p.rows - row0) : 128, pieces = p.nt / kPer<T>;
+      for (int u = rank * kThreads + tid; u < rows * pieces; u += p.split * kThreads) {
+        const int r = u / pieces, c = (u - r * pieces) * kPer<T>;
+        if (tn * p.nt + c >= p.c_out) continue;
+        float v[kPer<T>];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        for (int i = 0; i < kPer<T>; ++i) v[i] = 0.f;
+        const uint32_t at = sm + (uint32_t)(r * part_pitch + c * 4);
         for (int k = 0; k < p.split; ++k) {
-          const uint32_t at = map_cluster(sm + (uint32_t)((c * 128 + r) * 4), (uint32_t)k);
+          const uint32_t from = map_cluster(at, (uint32_t)k);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] += lds_cluster_f(at + (uint32_t)(i * 512));
+          for (int i = 0; i < kPer<T>; i += 4) {
+            const uint4 w = lds_cluster_u4(from + (uint32_t)(i * 4));
+            v[i] += __uint_as_float(w.x); v[i + 1] += __uint_as_float(w.y); v[i + 2] += __uint_as_float(w.z); v[i + 3] += __uint_as_float(w.w);
+          }
         }
-        deliver16<T>(p, bias, residual, y, row, tn * NT + c, v);
+        deliver<T>(p, bias, residual, y, row0 + r, tn * p.nt + c, v);
       }
     }
     cluster_sync();                              // nobody leaves while its part may still be read
@@ -310,43 +600,143 @@ bool codes_map(EncodeTiledFn encode, CUtensorMap *map, const void *q, size_t pit
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int F, int NT, typename T>
-cudaError_t launch(Params &p, const void *x, const void *w, const q4::Layout &lx, const q4::Layout &lw, const float *bias, const void *residual,
-                   void *y, DcWsHeader *ws, int n_sm, cudaStream_t st) {
-  using S = Shape<F, NT>;
+// scale tiles: boxes of one stage of `tiles` x 128 rows
+bool scales_map(EncodeTiledFn encode, CUtensorMap *map, const void *q, const q4::Layout &l, long long rows, int atoms, int tiles) {
+  const cuuint64_t dim[3] = {kAtom / 4, (cuuint64_t)l.tiles, (cuuint64_t)((rows + 127) / 128)}, str[2] = {kAtom, (cuuint64_t)l.tiles * kAtom};
+  const cuuint32_t bx[3] = {kAtom / 4, (cuuint32_t)atoms, (cuuint32_t)tiles}, es[3] = {1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, (char *)const_cast<void *>(q) + l.scale_offset, dim, str, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Call {
+  const void *x, *w;
+  const q4::Layout *lx, *lw;
+  const float *bias;
+  const void *residual;
+  void *y;
+  DcWsHeader *ws;
+  int n_sm;
+  cudaStream_t st;
+};
+template <int F, typename T, int FORM>
+cudaError_t launch(Params &p, const Call &c) {
   static unsigned char attr_done[kDcMaxDevices];
-  const cudaError_t e = dc_set_max_smem_once(k_q4_product<F, NT, T>, kSmemMax, attr_done);
+  const cudaError_t e = dc_set_max_smem_once(k_q4_product<F, T, FORM>, kSmemMax, attr_done);
   if (e != cudaSuccess) return e;
   EncodeTiledFn encode = get_encode_fn();
   if (!encode) return cudaErrorNotSupported;
-  CUtensorMap map_x, map_w;
-  if (!codes_map(encode, &map_x, x, lx.pitch, p.rows, 128) || !codes_map(encode, &map_w, w, lw.pitch, p.c_out, NT)) return cudaErrorNotSupported;
-  p.acc_bufs = 2 * NT + 2 * S::kSfCols <= 512 ? 2 : 1;
-  p.stages = (kSmemMax - 1024) / S::kStage;
-  if (p.stages > kMaxStages) p.stages = kMaxStages;
-  while (p.acc_bufs * NT + p.stages * S::kSfCols > 512) --p.stages;
-  const int grid = p.split > 1 ? p.items * p.split : (p.items < n_sm ? p.items : n_sm);
+  CUtensorMap map_x = {}, map_sx = {}, map_w, map_sw;
+  constexpr int kAtoms = kAtomsOf<F>;
+  if (!codes_map(encode, &map_w, c.w, c.lw->pitch, p.c_out, FORM == kPair ? p.nt / 2 : p.nt) || !scales_map(encode, &map_sw, c.w, *c.lw, p.c_out, kAtoms, p.nb))
+    return cudaErrorNotSupported;
+  if ((FORM == kOne || FORM == kPair) &&
+      (!codes_map(encode, &map_x, c.x, c.lx->pitch, p.rows, 128) || !scales_map(encode, &map_sx, c.x, *c.lx, p.rows, kAtoms, 1)))
+    return cudaErrorNotSupported;
+  const int team = FORM == kPair ? 2 : p.split;
+  const int grid = team > 1 ? (p.items * team < c.n_sm / team * team ? p.items * team : c.n_sm / team * team) : (p.items < c.n_sm ? p.items : c.n_sm);
   // all of a CTA's shared memory is asked for: two CTAs on an SM would each want all of its tensor memory
-  return dc_launch_pdl_cluster(k_q4_product<F, NT, T>, dim3((unsigned)grid), dim3(kThreads), (size_t)kSmemMax, st, p.split, map_x, map_w, bias,
-                               (const T *)residual, (T *)y, p, ws);
+  return dc_launch_pdl_cluster(k_q4_product<F, T, FORM>, dim3((unsigned)grid), dim3(kThreadsOf<FORM>), (size_t)kSmemMax, c.st, team, map_x, map_sx, map_w,
+                               map_sw, FORM == kRows || FORM == kStream ? (const T *)c.x : (const T *)nullptr, c.bias, (const T *)c.residual, (T *)c.y, p, c.ws);
 }
 
-// Tile width and the CTAs that share a tile: the least of an estimate in cycles.  A stage takes its products or its loads, whichever is longer.
-void choose(const Params &p, int n_sm, int *nt, int *split) {
-  static constexpr int kClusters[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};    // of that many CTAs that run at once, on 148 SMs
-  double best = 1e30;
-  for (int n = 128; n <= 256; n *= 2) {
-    if (n > 128 && p.c_out <= 128) break;
-    const long long items = (long long)p.tiles_m * dc_div_up(p.c_out, n);
-    for (int s = 1; s <= kMaxSplit && s <= p.chunks; ++s) {
-      const int per = dc_div_up(p.chunks, s);
-      if (s > 1 && (per * (s - 1) >= p.chunks || items * s > n_sm)) continue;     // no CTA without a stage
-      const double stage = (128 + n) * 140 / 45.0, main = per * (stage > 2.0 * n ? stage : 2.0 * n), out = 6.0 * n;
-      const double waves = s > 1 ? (double)((items + kClusters[s] - 1) / kClusters[s]) : (double)((items + n_sm - 1) / n_sm);
-      const double cycles = 3000 + waves * (n == 128 && s == 1 ? (main > out ? main : out) : main + out) + (s > 1 ? 1500 : 0);
-      if (cycles < best) { best = cycles; *nt = n; *split = s; }
-    }
+// Shared and tensor memory of a form, tile width and split; false: it does not fit.
+bool lay_out(Params *p, int form, int format, int n_sm) {
+  const int atoms = format == DC_NV4 ? 4 : 2, team = form == kPair ? 2 : p->split;
+  p->nb = p->nt > 128 ? 2 : 1;
+  p->w_bytes = (form == kPair ? p->nt / 2 : p->nt) * 128 + p->nb * atoms * kAtom;
+  p->sf_cols = 4 * atoms * (1 + p->nb);
+  const bool many = form != kPair && p->split == 1 && p->items > n_sm;         // CTAs have several tiles
+  p->acc_bufs = many && 2 * p->nt + 3 * p->sf_cols <= 512 ? 2 : 1;
+  p->sets = p->acc_bufs;
+  const int x_bytes = form == kRows ? 0 : kA + atoms * kAtom;
+  int room = kSmemMax - 1024 - kEpiWarps * kOutBytes;
+  p->off_sfa = p->off_ring = 0;
+  if (form == kRows) {
+    p->groups = (int)((p->rows + 7) / 8);
+    p->off_sfa = p->chunks_per * p->groups * 1024;
+    p->off_ring = p->off_sfa + p->chunks_per * atoms * kAtom;                  // a multiple of 1024
+    room -= p->off_ring;
   }
+  p->w_stays = many && p->tiles_n == 1 && (form == kOne || form == kStream) && (long long)p->chunks * p->w_bytes + 4ll * x_bytes <= room;
+  if (p->w_stays) room -= p->chunks * p->w_bytes;
+  p->stage_bytes = x_bytes + (p->w_stays ? 0 : p->w_bytes);    // multiples of 1024: nt is one of 16, a stage's scales are of 1024
+  p->stages = room / p->stage_bytes;
+  if (p->stages > kMaxStages) p->stages = kMaxStages;
+  if (p->acc_bufs * p->nt + p->stages * p->sf_cols > 512) p->stages = (512 - p->acc_bufs * p->nt) / p->sf_cols;
+  p->off_out = p->off_ring + p->stages * p->stage_bytes + (p->w_stays ? p->chunks * p->w_bytes : 0);
+  // an operand of fewer rows than 128 is read on into what lies behind it; a part of a split tile lies where the operands were
+  if (form == kRows && kSmemMax - 1024 - p->off_sfa < kA) return false;
+  if (team > 1 && form != kPair && (form == kRows ? (int)p->rows : 128) * (((p->nt + 31) & ~31) * 4 + 16) > p->off_out) return false;
+  return p->stages >= 2;
+}
+
+// Estimated cycles of a form: a stage takes its products, its loads or its quantising, whichever is longest.
+double estimate(const Params &p, int form, int n_sm) {
+  static constexpr int kClusters[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};    // of that many CTAs that run at once, on 148 SMs
+  const int team = form == kPair ? 2 : p.split;
+  const double at_once = team > 1 ? kClusters[team] * (n_sm / 148.0) : n_sm;
+  const double products = 2.0 * p.nt, loads = p.stage_bytes / 40.0, stage = products > loads ? products : loads;
+  const double main = (form == kPair ? p.chunks : p.chunks_per) * stage, out = 4.0 * p.nt + 500;
+  double waves = p.items / at_once;
+  waves = (double)(long long)(waves + 0.999);
+  return 3000 + waves * (p.acc_bufs == 2 ? (main > out ? main : out) : main + out) + (team > 1 ? 1500 : 0) +
+         (form == kRows ? 400 + 250.0 * (double)p.rows * p.chunks_per / 16 : 0);
+}
+
+// Fills p for the form that takes the least of the estimates.  Tiles of fewer than all of w's rows begin where a scale tile does: they have
+// 128 or 256 rows.
+int choose(Params *p, bool raw, int format, int n_sm) {
+  double best = 1e30;
+  Params best_p = *p;
+  int best_form = -1;
+  const int whole = (int)dc_round_up((size_t)p->c_out, 16);
+  auto look = [&](int form, int nt, int split) {
+    Params q = *p;
+    q.nt = nt;
+    q.split = split;
+    q.chunks_per = dc_div_up(q.chunks, split);
+    q.tiles_n = dc_div_up(q.c_out, nt);
+    q.tiles_m = (int)(form == kPair ? (q.rows + 255) / 256 : (q.rows + 127) / 128);
+    if ((long long)q.tiles_m * q.tiles_n > 0x3fffffffll) return;
+    q.items = q.tiles_m * q.tiles_n;
+    if (split > 1 && (q.chunks_per * (split - 1) >= q.chunks || (long long)q.items * split > n_sm)) return;     // no CTA without a stage
+    if (!lay_out(&q, form, format, n_sm)) return;
+    const double cycles = estimate(q, form, n_sm);
+    if (cycles < best) { best = cycles; best_p = q; best_form = form; }
+  };
+  if (raw && p->rows <= kMaxRows) {
+    for (int s = 1; s <= kMaxSplit; ++s) look(kRows, whole < 128 ? whole : 128, s);
+  } else if (raw) {
+    if (p->c_in <= kStageCols && whole <= 256 && p->vec_x) look(kStream, whole, 1);
+  } else {
+    for (int n = 128; n <= 256; n += 128) {
+      for (int s = 1; s <= kMaxSplit; ++s) look(kOne, whole < n ? whole : n, s);
+      if (whole <= n) break;
+    }
+    if (p->rows > 128 && whole > 128) look(kPair, 256, 1);
+  }
+  *p = best_p;
+  return best_form;
+}
+
+template <int F, typename T>
+cudaError_t launch_form(int form, Params &p, const Call &c) {
+  switch (form) {
+    case kOne: return launch<F, T, kOne>(p, c);
+    case kPair: return launch<F, T, kPair>(p, c);
+    case kRows: return launch<F, T, kRows>(p, c);
+    default: return launch<F, T, kStream>(p, c);
+  }
+}
+// DC_ERR_UNSUPPORTED: no form takes rows of this size as they are (raw), or at all
+dc_status run(Params &p, bool raw, dc_q4_format format, dc_dtype dtype, Call &c) {
+  c.n_sm = dc_sm_count();
+  const int form = choose(&p, raw, format, c.n_sm);
+  if (form < 0) return DC_ERR_UNSUPPORTED;
+  cudaError_t e;
+  if (format == DC_MX4) e = dtype == DC_BF16 ? launch_form<DC_MX4, __nv_bfloat16>(form, p, c) : launch_form<DC_MX4, float>(form, p, c);
+  else e = dtype == DC_BF16 ? launch_form<DC_NV4, __nv_bfloat16>(form, p, c) : launch_form<DC_NV4, float>(form, p, c);
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? DC_OK : DC_ERR_CUDA;
 }
 
 dc_status check(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, const void *bias, dc_act act,
@@ -361,13 +751,19 @@ dc_status check(const void *x, long long rows, int c_in, const void *w, int c_ou
   return DC_OK;
 }
 
-template <int F, typename T>
-cudaError_t launch_nt(int nt, Params &p, const void *x, const void *w, const q4::Layout &lx, const q4::Layout &lw, const float *bias,
-                      const void *residual, void *y, DcWsHeader *ws, int n_sm, cudaStream_t st) {
-  switch (nt) {
-    case 128: return launch<F, 128, T>(p, x, w, lx, lw, bias, residual, y, ws, n_sm, st);
-    default: return launch<F, 256, T>(p, x, w, lx, lw, bias, residual, y, ws, n_sm, st);
-  }
+Params params_of(long long rows, int c_in, int c_out, dc_act act, dc_dtype dtype, float scale) {
+  Params p = {};
+  p.rows = rows;
+  p.c_in = c_in;
+  p.c_out = c_out;
+  p.act = (int)act;
+  p.scale = scale;
+  p.g = p.g6 = 1.f;
+  p.chunks = dc_div_up(c_in, kStageCols);
+  const size_t es = dtype == DC_F32 ? 4 : 2;
+  p.vec = (size_t)c_out * es % 16 == 0;
+  p.vec_x = (size_t)c_in * es % 16 == 0;
+  return p;
 }
 
 }  // namespace
@@ -388,35 +784,9 @@ extern "C" dc_status dc_q4_product(const void *x, long long rows, int c_in, cons
   const dc_status s = check(x, rows, c_in, w, c_out, format, bias, act, residual, y, dtype, workspace, workspace_bytes, &lx, &lw);
   if (s != DC_OK) return s;
   if (!(scale - scale == 0.f)) return DC_ERR_INVALID_ARG;
-  const int n_sm = dc_sm_count();
-  Params p = {};
-  p.rows = rows;
-  p.c_in = c_in;
-  p.c_out = c_out;
-  p.act = (int)act;
-  p.scale = scale;
-  p.tiles_m = (int)((rows + 127) / 128);
-  p.chunks = dc_div_up(c_in, kStageCols);
-  p.atoms = (int)lx.tiles;
-  p.vec = (size_t)c_out * (dtype == DC_F32 ? 4 : 2) % 16 == 0;
-  p.sx = (const uint8_t *)x + lx.scale_offset;
-  p.sw = (const uint8_t *)w + lw.scale_offset;
-  int nt = 128;
-  choose(p, n_sm, &nt, &p.split);
-  p.tiles_n = dc_div_up(c_out, nt);
-  if ((long long)p.tiles_m * p.tiles_n * p.split > 0x3fffffffll) return DC_ERR_UNSUPPORTED;
-  p.items = p.tiles_m * p.tiles_n;
-  p.chunks_per = dc_div_up(p.chunks, p.split);
-  cudaStream_t st = (cudaStream_t)stream;
-  DcWsHeader *ws = (DcWsHeader *)workspace;
-  cudaError_t e;
-  if (format == DC_MX4)
-    e = dtype == DC_BF16 ? launch_nt<DC_MX4, __nv_bfloat16>(nt, p, x, w, lx, lw, bias, residual, y, ws, n_sm, st)
-                         : launch_nt<DC_MX4, float>(nt, p, x, w, lx, lw, bias, residual, y, ws, n_sm, st);
-  else
-    e = dtype == DC_BF16 ? launch_nt<DC_NV4, __nv_bfloat16>(nt, p, x, w, lx, lw, bias, residual, y, ws, n_sm, st)
-                         : launch_nt<DC_NV4, float>(nt, p, x, w, lx, lw, bias, residual, y, ws, n_sm, st);
-  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? DC_OK : DC_ERR_CUDA;
+  Params p = params_of(rows, c_in, c_out, act, dtype, scale);
+  Call c = {x, w, &lx, &lw, bias, residual, y, (DcWsHeader *)workspace, 0, (cudaStream_t)stream};
+  return run(p, false, format, dtype, c);
 }
 
 extern "C" dc_status dc_q4_forward(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, float x_scale,
@@ -426,9 +796,19 @@ extern "C" dc_status dc_q4_forward(const void *x, long long rows, int c_in, cons
   dc_status s = check(x, rows, c_in, w, c_out, format, bias, act, residual, y, dtype, workspace, workspace_bytes, &lx, &lw);
   if (s != DC_OK) return s;
   if (!q4::tensor_scale_ok(x_scale, format) || !q4::tensor_scale_ok(w_scale, format)) return DC_ERR_INVALID_ARG;
+  const float scale = x_scale * w_scale;
+  if (!(scale - scale == 0.f)) return DC_ERR_INVALID_ARG;
   if (workspace_bytes < sizeof(DcWsHeader) + lx.bytes) return DC_ERR_WORKSPACE;
+  Params p = params_of(rows, c_in, c_out, act, dtype, scale);
+  p.g = x_scale;
+  p.g6 = 6.f * x_scale;
+  Call c = {x, w, &lx, &lw, bias, residual, y, (DcWsHeader *)workspace, 0, (cudaStream_t)stream};
+  s = run(p, true, format, dtype, c);
+  if (s != DC_ERR_UNSUPPORTED) return s;
   uint8_t *xq = (uint8_t *)workspace + sizeof(DcWsHeader);
   s = dc_q4_quantize(x, rows, c_in, c_in, dtype, format, x_scale, xq, stream);
   if (s != DC_OK) return s;
-  return dc_q4_product(xq, rows, c_in, w, c_out, format, x_scale * w_scale, bias, act, residual, y, dtype, workspace, workspace_bytes, stream);
+  Params q = params_of(rows, c_in, c_out, act, dtype, scale);
+  c.x = xq;
+  return run(q, false, format, dtype, c);
 }

@@ -156,7 +156,7 @@ dc_status prepare(const void *x, long long rows, int cols, long long stride, dc_
   p->rows = rows;
   p->stride = stride;
   p->cols = cols;
-  p->segs_log2 = 1;
+  p->segs_log2 = 2;          // pitch: whole runs of 64 columns
   while ((16 << p->segs_log2) < kCols && (16 << p->segs_log2) < cols) ++p->segs_log2;
   p->vec = stride % (long long)(16 / es) == 0;
   p->g = g;

@@ -20,13 +20,13 @@ def status_of(fn, *a):
 
 
 @pytest.mark.parametrize("rows,cols,fmt,pitch,tiles,offset,nbytes", [
-    (1, 1, dc.MX4, 16, 1, 256, 768),
-    (1, 1, dc.NV4, 16, 1, 256, 768),
-    (128, 24, dc.MX4, 16, 1, 2048, 2560),
+    (1, 1, dc.MX4, 32, 1, 256, 768),
+    (1, 1, dc.NV4, 32, 1, 256, 768),
+    (128, 24, dc.MX4, 32, 1, 4096, 4608),
     (129, 64, dc.NV4, 32, 1, 4352, 4352 + 2 * 512),
-    (129, 65, dc.NV4, 48, 2, 6400, 6400 + 4 * 512),
+    (129, 65, dc.NV4, 64, 2, 8448, 8448 + 4 * 512),
     (4096, 4096, dc.NV4, 2048, 64, 4096 * 2048, 4096 * 2048 + 32 * 64 * 512),
-    (300, 129, dc.MX4, 80, 2, 24064, 24064 + 3 * 2 * 512),
+    (300, 129, dc.MX4, 96, 2, 28928, 28928 + 3 * 2 * 512),
 ])
 def test_layout(rows, cols, fmt, pitch, tiles, offset, nbytes):
     lay = dc.q4_layout(rows, cols, fmt)

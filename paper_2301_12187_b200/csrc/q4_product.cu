@@ -83,10 +83,43 @@ __device__ __forceinline__ void mma_q4(uint32_t d, uint64_t a, uint64_t b, uint3
   }
 }
 #undef Q4_MMA
-// instruction descriptor: e2m1 x e2m1, N, M, type of the scales; `id`: which half of a scale word (DC_MX4)
+// instruction descriptor: e2m1 x e2m1, N, M, type of the scales
 template <int F>
-__device__ __forceinline__ uint32_t q4_idesc(int n, int m, uint32_t id) {
-  return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((F == DC_MX4 ? 1u : 0u) << 23) | ((uint32_t)(m >> 7) << 27) | (id << 29);
+__device__ __forceinline__ uint32_t q4_idesc(int n, int m) {
+  return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((F == DC_MX4 ? 1u : 0u) << 23) | ((uint32_t)(m >> 7) << 27);
+}
+// ... with the half of a scale word that product k of a stage takes (DC_MX4)
+template <int F>
+__device__ __forceinline__ uint32_t with_id(uint32_t idesc, int k) {
+  return F == DC_MX4 && (k & 1) ? idesc | (2u << 4) | (2u << 29) : idesc;
+}
+// A stage: its scales to tensor memory (columns from `ta`), then its products.  One thread issues all of it, and the tensor core takes 512 cycles for
+// 256 columns of w: with descriptors worked out in loops the issuing thread was what bound large products (8192^3 in nv4 389 us).
+template <int F, bool P, int NB, int STEPS>
+__device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, uint32_t sfa, uint32_t sfb, uint32_t ta, uint32_t idesc, bool accumulate) {
+  constexpr int kAtoms = kAtomsOf<F>;
+  const uint64_t da = scales_desc(sfa), db = scales_desc(sfb), ad = operand_desc(a), bd = operand_desc(b);
+  const uint32_t tb = ta + 4u * kAtoms;
+#pragma unroll
+  for (int i = 0; i < kAtoms; ++i) {
+    copy_scales<P>(ta + 4u * i, da + (uint64_t)(i * (kAtom / 16)));
+#pragma unroll
+    for (int j = 0; j < NB; ++j) copy_scales<P>(tb + 4u * (i * NB + j), db + (uint64_t)((j * kAtoms + i) * (kAtom / 16)));
+  }
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    const uint32_t atom = F == DC_NV4 ? (uint32_t)k : (uint32_t)(k >> 1);
+    mma_q4<F, P>(d, ad + 2u * k, bd + 2u * k, with_id<F>(idesc, k), ta + 4u * atom, tb + 4u * NB * atom, accumulate || k > 0 ? 1u : 0u);
+  }
+}
+template <int F, bool P>
+__device__ __forceinline__ void multiply_last(uint32_t d, uint32_t a, uint32_t b, uint32_t sfa, uint32_t sfb, uint32_t ta, uint32_t tb, int nb, uint32_t idesc,
+                                              int k, bool accumulate) {
+  if (F == DC_NV4 || (k & 1) == 0) {
+    copy_scales<P>(ta, scales_desc(sfa));
+    for (int j = 0; j < nb; ++j) copy_scales<P>(tb + 4u * j, scales_desc(sfb + (uint32_t)(j * kAtomsOf<F> * kAtom)));
+  }
+  mma_q4<F, P>(d, operand_desc(a), operand_desc(b), with_id<F>(idesc, k), ta, tb, accumulate ? 1u : 0u);
 }
 // arrives at the barrier (of both CTAs of a pair) once all that this thread has issued is done
 template <bool P>
@@ -376,7 +409,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       ok = warp_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x20000u | (uint32_t)buf);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t d = tmem + (uint32_t)(buf * p.nt);
+      const uint32_t d = tmem + (uint32_t)(buf * p.nt), idesc = q4_idesc<F>(p.nt, P ? 256 : 128);
       for (int ch = c0; ch < c1; ++ch) {
         ok = warp_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x30000u | (uint32_t)stage);
         if (!ok) break;
@@ -386,17 +419,16 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           const uint32_t a = FORM == kRows ? sm + (uint32_t)((ch - c0) * p.groups * 1024) : at;
           const uint32_t sfa = FORM == kRows ? sm + (uint32_t)(p.off_sfa + (ch - c0) * kAtoms * kAtom) : at + kA;
           const uint32_t b = p.w_stays ? w_base + (uint32_t)(ch * p.w_bytes) : (FORM == kRows ? at : at + kA + kAtoms * kAtom), sfb = b + w_codes;
-          const uint32_t ta = sf_base + (uint32_t)(stage * p.sf_cols), tb = ta + 4u * kAtoms;
-          const int steps = min(4, dc_div_up(p.c_in - ch * kStageCols, 64)), na = F == DC_NV4 ? steps : (steps + 1) / 2;
-          for (int i = 0; i < na; ++i) {
-            copy_scales<P>(ta + 4u * i, scales_desc(sfa + (uint32_t)(i * kAtom)));
-            for (int j = 0; j < p.nb; ++j) copy_scales<P>(tb + 4u * (uint32_t)(i * p.nb + j), scales_desc(sfb + (uint32_t)((j * kAtoms + i) * kAtom)));
-          }
-          const uint64_t ad = operand_desc(a), bd = operand_desc(b);
-          for (int k = 0; k < steps; ++k) {
-            const uint32_t atom = F == DC_NV4 ? (uint32_t)k : (uint32_t)(k >> 1), id = F == DC_NV4 ? 0u : (uint32_t)(k & 1) * 2u;
-            mma_q4<F, P>(d, ad + 2u * k, bd + 2u * k, q4_idesc<F>(p.nt, P ? 256 : 128, id), ta + 4u * atom, tb + 4u * (uint32_t)p.nb * atom,
-                         ch > c0 || k > 0 ? 1u : 0u);
+          const uint32_t ta = sf_base + (uint32_t)(stage * p.sf_cols);
+          const int steps = min(4, dc_div_up(p.c_in - ch * kStageCols, 64));
+          if (steps == 4) {
+            if (p.nb == 2) multiply<F, P, 2, 4>(d, a, b, sfa, sfb, ta, idesc, ch > c0);
+            else multiply<F, P, 1, 4>(d, a, b, sfa, sfb, ta, idesc, ch > c0);
+          } else {                               // the last columns
+            for (int k = 0; k < steps; ++k) {
+              const uint32_t atom = F == DC_NV4 ? (uint32_t)k : (uint32_t)(k >> 1), tile = atom * kAtom;
+              multiply_last<F, P>(d, a + 32u * k, b + 32u * k, sfa + tile, sfb + tile, ta + 4u * atom, ta + 4u * (kAtoms + p.nb * atom), p.nb, idesc, k, ch > c0 || k > 0);
+            }
           }
           commit<P>(&bar[kEmpty + stage]);
           if (ch == c1 - 1) commit<P>(&bar[kDFull + buf]);

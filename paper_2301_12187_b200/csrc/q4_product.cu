@@ -167,36 +167,48 @@ __device__ __forceinline__ void load_bias(const float *__restrict__ bias, int o,
 #pragma unroll
   for (int i = 0; i < n; i += 4) *reinterpret_cast<float4 *>(b + i) = bias ? __ldg(reinterpret_cast<const float4 *>(bias + o + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
 }
+// sums -> 16 bytes of y: scale and bias, residual, activation
+template <typename T>
+__device__ __forceinline__ uint4 finish16(const Params &p, const float *b, bool has_residual, uint4 residual, float *v) {
+  constexpr int N = kPer<T>;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = fmaf(v[i], p.scale, b[i]);
+  if (has_residual) {
+    float r[N];
+    unpack16<T>(residual, r);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += r[i];
+  }
+  if (p.act == DC_ACT_RELU6) {
+    if (N == 8) return make_uint4(relu6_bf16x2(v[0], v[1]), relu6_bf16x2(v[2], v[3]), relu6_bf16x2(v[4 % N], v[5 % N]), relu6_bf16x2(v[6 % N], v[7 % N]));
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = dc_act_apply(v[i], DC_ACT_RELU6);
+  }
+  return pack16<T>(v);
+}
 // columns one by one, where rows of y do not begin on 16 bytes
 template <typename T>
-__device__ __forceinline__ void deliver_one(const Params &p, float t, bool has_bias, float b, const T *residual, T *y, size_t at) {
-  t *= p.scale;
-  if (has_bias) t += b;
+__device__ __forceinline__ void deliver_one(const Params &p, float t, float b, const T *residual, T *y, size_t at) {
+  t = fmaf(t, p.scale, b);
   if (residual) t += (float)residual[at];
   y[at] = (T)dc_act_apply(t, p.act);
 }
-// the same of a part's sum (form kOne, split)
+// the same of a part's sum (split tiles)
 template <typename T>
 __device__ __forceinline__ void deliver(const Params &p, const float *__restrict__ bias, const T *residual, T *y, long long row, int o, float *v) {
   constexpr int N = kPer<T>;
   const size_t at = (size_t)row * (size_t)p.c_out + (size_t)o;
   if (p.vec) {                                   // rows then have whole pieces
-    float b[N], r[N];
+    float b[N];
     load_bias(bias, o, N, b);
-    if (residual) unpack16<T>(*reinterpret_cast<const uint4 *>(residual + at), r);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float t = v[i] * p.scale;
-      if (bias) t += b[i];
-      if (residual) t += r[i];
-      v[i] = dc_act_apply(t, p.act);
-    }
-    *reinterpret_cast<uint4 *>(y + at) = pack16<T>(v);
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (residual) r = *reinterpret_cast<const uint4 *>(residual + at);
+    *reinterpret_cast<uint4 *>(y + at) = finish16<T>(p, b, residual != nullptr, r, v);
     return;
   }
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    if (o + i < p.c_out) deliver_one<T>(p, v[i], bias != nullptr, bias ? __ldg(bias + o + i) : 0.f, residual, y, at + i);
+    if (o + i < p.c_out) deliver_one<T>(p, v[i], bias ? __ldg(bias + o + i) : 0.f, residual, y, at + i);
 }
 // 32 rows x 32 results in the warp's shared memory -> y from row `row0`, column `o`: neighbouring lanes store neighbouring columns.
 template <typename T>
@@ -227,24 +239,16 @@ __device__ __forceinline__ void deliver32(const Params &p, const float *__restri
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float v[N];
-        if (residual) unpack16<T>(res[i], v);
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          float u = t[i][j] * p.scale;
-          if (bias) u += b[j];
-          if (residual) u += v[j];
-          t[i][j] = dc_act_apply(u, p.act);
-        }
-        if (r0 + (h + i) * kStep < rows) *reinterpret_cast<uint4 *>(y + at + pitch * (h + i)) = pack16<T>(t[i]);
+        const uint4 w = finish16<T>(p, b, residual != nullptr, res[i], t[i]);
+        if (r0 + (h + i) * kStep < rows) *reinterpret_cast<uint4 *>(y + at + pitch * (h + i)) = w;
       }
     }
   } else if (o + lane < p.c_out) {               // a lane to a column
     const float b = bias ? __ldg(bias + o + lane) : 0.f;
     size_t at = (size_t)row0 * (size_t)p.c_out + (size_t)(o + lane);
-#pragma unroll 4
+#pragma unroll 8
     for (int r = 0; r < rows; ++r, at += (size_t)p.c_out)
-      deliver_one<T>(p, lds_f(sm + (uint32_t)(r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4)), bias != nullptr, b, residual, y, at);
+      deliver_one<T>(p, lds_f(sm + (uint32_t)(r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4)), b, residual, y, at);
   }
 }
 
@@ -266,6 +270,18 @@ __device__ __forceinline__ void load_x16(const T *__restrict__ row, int c, int c
       }
     }
   }
+}
+// largest magnitude of 16 values, its bits as fp32
+template <typename T>
+__device__ __forceinline__ uint32_t largest16(const uint4 *raw) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16 / kPer<T>; ++i) {
+    const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = sizeof(T) == 2 ? __vmaxu2(top, u[j] & 0x7fff7fffu) : max(top, u[j] & 0x7fffffffu);
+  }
+  return sizeof(T) == 2 ? max(top & 0xffff0000u, top << 16) : top;
 }
 // 16 columns, piece `seg` of a row, -> codes in an operand's rows and the block's scale in its tile.  `top`: largest magnitude of the piece.
 template <int F>
@@ -510,60 +526,67 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
     }
   } else {
-    // ---------------------------------------------------------------- quantise (kStream): a thread to a row, two groups of four warps take the stages in turn
+    // ---------------------------------------------------------------- quantise (kStream): a thread to a row, two groups of four warps take the stages
+    // in turn, 32 columns at a time; the next 32, of the next stage or tile too, are asked for before these are worked on
     const int group = (warp - 2 - kEpiWarps) >> 2, r = ((warp - 2 - kEpiWarps) & 3) * 32 + lane;
-    int stage = 0, n = 0;
+    constexpr int kRaw = 32 / kPer<T>;
+    uint4 next[kRaw];
+    auto ask = [&](int item, int ch, int c) {    // columns c .. c + 31 of a stage
+      const long long row = (long long)(item % p.tiles_m) * 128 + r;
+      const int col = ch * kStageCols + c;
+      const T *at = x + (size_t)row * (size_t)p.c_in + col;
+#pragma unroll
+      for (int i = 0; i < kRaw; ++i)
+        next[i] = row < p.rows && col + i * kPer<T> < p.c_in ? __ldg(reinterpret_cast<const uint4 *>(at) + i) : make_uint4(0, 0, 0, 0);
+    };
+    // this group's stages: numbers group, group + 2, ... of those of the CTA
+    int item = first, ch = group, stage = group;
     uint32_t parity = 0;
     bool ok = true;
-    for (int item = first; ok && item < p.items; item += step) {
-      const long long row = (long long)(item % p.tiles_m) * 128 + r;
-      const T *at = x + (size_t)(row < p.rows ? row : 0) * (size_t)p.c_in;
-      for (int ch = 0; ch < p.chunks; ++ch, ++n) {
-        if ((n & 1) == group) {
-          ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x70000u | (uint32_t)stage);
-          if (!ok) break;
-          const uint32_t a = ring + (uint32_t)(stage * p.stage_bytes), sfa = a + kA;
-          const int left = min(p.c_in - ch * kStageCols, kStageCols), pieces = (left + 63) / 64 * 4;
+    auto settle = [&]() {
+      while (ch >= p.chunks) { ch -= p.chunks; item += step; }
+    };
+    settle();
+    if (item < p.items) ask(item, ch, 0);
+    while (ok && item < p.items) {
+      ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x70000u | (uint32_t)stage);
+      if (!ok) break;
+      const uint32_t a = ring + (uint32_t)(stage * p.stage_bytes) + (uint32_t)((r >> 3) * 1024 + (r & 7) * 128);
+      const uint32_t sfa = ring + (uint32_t)(stage * p.stage_bytes) + kA;
+      const int item0 = item, ch0 = ch, end = (min(p.c_in - ch * kStageCols, kStageCols) + 63) / 64 * 64;
+      ch += 2;
+      settle();
 #pragma unroll 1
-          for (int seg = 0; seg < pieces; seg += 2) {
-            // both halves of a DC_MX4 block are this thread's
-            float v[2][16];
-            uint32_t top[2];
+      for (int c = 0; c < end; c += 32) {
+        uint4 raw[kRaw];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (row < p.rows) {
-                load_x16<T>(at, ch * kStageCols + (seg + h) * 16, p.c_in, 1, v[h]);
-              } else {
+        for (int i = 0; i < kRaw; ++i) raw[i] = next[i];
+        if (c + 32 < end) ask(item0, ch0, c + 32);
+        else if (item < p.items) ask(item, ch, 0);
+        uint2 code[2];
+        uint32_t top[2], byte[2];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[h][i] = 0.f;
-              }
-            }
+        for (int h = 0; h < 2; ++h) top[h] = largest16<T>(raw + h * kRaw / 2);
+        if (F == DC_MX4) top[0] = top[1] = max(top[0], top[1]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              top[h] = 0;
+        for (int h = 0; h < 2; ++h) {
+          float v[16];
 #pragma unroll
-              for (int i = 0; i < 16; ++i) top[h] = max(top[h], __float_as_uint(v[h][i]) & 0x7fffffffu);
-            }
-            if (F == DC_MX4) top[0] = top[1] = max(top[0], top[1]);
-            uint2 code[2];
-            uint32_t byte[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.g6);
-              code[h] = q4::codes16<F>(v[h], s);
-              byte[h] = s.byte;
-            }
-            sts_u4(a + (uint32_t)((r >> 3) * 1024 + (r & 7) * 128 + ((seg >> 1) ^ (r & 7)) * 16), make_uint4(code[0].x, code[0].y, code[1].x, code[1].y));
-            const uint32_t blk = (uint32_t)(F == DC_NV4 ? seg : seg >> 1), to = sfa + (blk >> 2) * kAtom + q4::scale_at((uint32_t)r, blk);
-            if (F == DC_NV4) asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"((uint16_t)(byte[0] | (byte[1] << 8))) : "memory");
-            else asm volatile("st.shared.b8 [%0], %1;" ::"r"(to), "r"(byte[0]) : "memory");
-          }
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bar[kFull + stage]);
+          for (int i = 0; i < kRaw / 2; ++i) unpack16<T>(raw[h * kRaw / 2 + i], v + i * kPer<T>);
+          const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.g6);
+          code[h] = q4::codes16<F>(v, s);
+          byte[h] = s.byte;
         }
-        if (++stage == p.stages) { stage = 0; parity ^= 1u; }
+        sts_u4(a + (uint32_t)(((c >> 5) ^ (r & 7)) * 16), make_uint4(code[0].x, code[0].y, code[1].x, code[1].y));
+        const uint32_t blk = (uint32_t)(F == DC_NV4 ? c >> 4 : c >> 5), to = sfa + (blk >> 2) * kAtom + q4::scale_at((uint32_t)r, blk);
+        if (F == DC_NV4) asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"((uint16_t)(byte[0] | (byte[1] << 8))) : "memory");
+        else asm volatile("st.shared.b8 [%0], %1;" ::"r"(to), "r"(byte[0]) : "memory");
       }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar[kFull + stage]);
+      stage += 2;
+      if (stage >= p.stages) { stage -= p.stages; parity ^= 1u; }
     }
   }
   if (warp == 1 && *abort_flag) {                // copies and products may still be in flight: give them time to end

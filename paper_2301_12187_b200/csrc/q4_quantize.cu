@@ -22,67 +22,128 @@ struct Params {
   size_t scale_offset;
 };
 
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+template <typename T>
+constexpr int kPer = 16 / (int)sizeof(T);        // values in 16 bytes
+template <typename T>
+__device__ __forceinline__ void unpack(uint4 w, float *v) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (sizeof(T) == 2) { v[2 * j % kPer<T>] = __uint_as_float(u[j] << 16); v[(2 * j + 1) % kPer<T>] = __uint_as_float(u[j] & 0xffff0000u); }
+    else v[j] = __uint_as_float(u[j]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float *v) {
+  constexpr int N = kPer<T>;
+  if (N == 4) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i % N], v[(2 * i + 1) % N]);
+    w[i] = *reinterpret_cast<const uint32_t *>(&t);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Rows that do not begin on 16 bytes go through shared memory, 4096 columns at a time: neighbouring threads then load and store neighbouring
+// columns.  One word of padding behind 16 keeps the threads, 16 columns apart, out of one another's banks.
+struct Staged {
+  float at[4096 + 256];
+  __device__ __forceinline__ float &operator()(int row, int col, int span_log2) { return at[(row << span_log2) + (row << (span_log2 - 4)) + col + (col >> 4)]; }
+};
 
-template <int F, typename T>
+template <int F, typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_q4_quantize(const T *__restrict__ x, uint8_t *__restrict__ q, const Params p) {
   __shared__ __align__(16) uint8_t scales[4 * kAtom];
+  extern __shared__ uint8_t staged_s[];            // Staged, where !VEC
   dc_pdl_enter();
-  const int tid = (int)threadIdx.x, segs = 1 << p.segs_log2;
+  const int tid = (int)threadIdx.x, segs = 1 << p.segs_log2, span_log2 = p.segs_log2 + 4;
   const uint32_t tile = blockIdx.x / p.col_tiles, col_tile = blockIdx.x - tile * p.col_tiles;
-  const int seg = tid & (segs - 1), c = (int)(col_tile << (p.segs_log2 + 4)) + seg * 16;
+  const int seg = tid & (segs - 1), c0 = (int)(col_tile << span_log2), c = c0 + seg * 16;
   const long long row0 = (long long)tile * 128;
-  constexpr int kBlock = F == DC_MX4 ? 32 : 16;
+  const int rows = p.rows - row0 < 128 ? (int)(p.rows - row0) : 128;
+  constexpr int kBlock = F == DC_MX4 ? 32 : 16, kPieces = 16 / kPer<T>;
   // scale tiles of this CTA; the bytes that no row or block writes are 0
-  const int atoms = (1 << (p.segs_log2 + 4)) <= 4 * kBlock ? 1 : (1 << (p.segs_log2 + 4)) / (4 * kBlock);
+  const int atoms = (1 << span_log2) <= 4 * kBlock ? 1 : (1 << span_log2) / (4 * kBlock);
   for (int i = tid; i < atoms * (kAtom / 16); i += kThreads) reinterpret_cast<uint4 *>(scales)[i] = make_uint4(0, 0, 0, 0);
   __syncthreads();
-#pragma unroll 1
-  for (int r = tid >> p.segs_log2; r < 128; r += kThreads >> p.segs_log2) {
-    const long long row = row0 + r;
-    const bool in = row < p.rows && c < (int)(p.pitch * 2);
-    float v[16];
-    if (in) {
-      const T *at = x + row * p.stride + c;
-      if (p.vec && c + 16 <= p.cols) {
-        if (sizeof(T) == 2) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(at) + i);
-            v[8 * i] = bf16_lo(w.x); v[8 * i + 1] = bf16_hi(w.x); v[8 * i + 2] = bf16_lo(w.y); v[8 * i + 3] = bf16_hi(w.y);
-            v[8 * i + 4] = bf16_lo(w.z); v[8 * i + 5] = bf16_hi(w.z); v[8 * i + 6] = bf16_lo(w.w); v[8 * i + 7] = bf16_hi(w.w);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 w = __ldg(reinterpret_cast<const float4 *>(at) + i);
-            v[4 * i] = w.x; v[4 * i + 1] = w.y; v[4 * i + 2] = w.z; v[4 * i + 3] = w.w;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          v[i] = 0.f;
-          if (c + i < p.cols) v[i] = sizeof(T) == 2 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(at)[i]) : reinterpret_cast<const float *>(at)[i];
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = 0.f;
-    }
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  const int step = kThreads >> p.segs_log2, mine = tid >> p.segs_log2;           // rows at a time; this thread's of them
+  const bool wanted = c < (int)(p.pitch * 2);
+  auto put = [&](int r, uint32_t top, float *v) {
     if (F == DC_MX4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     const BlockScale s = block_scale<F>(top, p.g, p.g6);
     const uint2 code = codes16<F>(v, s);
-    if (in) {
-      *reinterpret_cast<uint2 *>(q + (size_t)row * p.pitch + (c >> 1)) = code;
+    if (r < rows && wanted) {
+      *reinterpret_cast<uint2 *>(q + (size_t)(row0 + r) * p.pitch + (c >> 1)) = code;
       if (c < p.cols && (F == DC_NV4 || (seg & 1) == 0)) {
         const uint32_t b = (uint32_t)(seg * 16 / kBlock);
         scales[(b >> 2) * kAtom + scale_at((uint32_t)r, b)] = (uint8_t)s.byte;
       }
+    }
+  };
+  if (VEC) {
+    constexpr int U = 2;                         // rows of a thread at once, so that their loads overlap
+#pragma unroll 1
+    for (int r = mine; r - mine < rows; r += U * step) {
+      uint4 raw[U][kPieces];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int ru = r + u * step;
+        const T *at = x + (row0 + ru) * p.stride + c;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          raw[u][i] = make_uint4(0, 0, 0, 0);
+          if (ru < rows) {
+            const int left = p.cols - (c + i * kPer<T>);
+            if (left >= kPer<T>) {
+              raw[u][i] = __ldg(reinterpret_cast<const uint4 *>(at) + i);
+            } else if (left > 0) {               // the last columns
+              float t[kPer<T>];
+#pragma unroll
+              for (int j = 0; j < kPer<T>; ++j) t[j] = j < left ? (float)at[i * kPer<T> + j] : 0.f;
+              raw[u][i] = pack<T>(t);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u > 0 && r + u * step - mine >= 128) break;        // the same for all threads
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const uint32_t w[4] = {raw[u][i].x, raw[u][i].y, raw[u][i].z, raw[u][i].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) top = sizeof(T) == 2 ? __vmaxu2(top, w[j] & 0x7fff7fffu) : max(top, w[j] & 0x7fffffffu);
+        }
+        if (sizeof(T) == 2) top = max(top & 0xffff0000u, top << 16);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) unpack<T>(raw[u][i], v + i * kPer<T>);
+        put(r + u * step, top, v);
+      }
+    }
+  } else {
+    Staged &staged = *reinterpret_cast<Staged *>(staged_s);
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += step) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int at = tid + i * kThreads, r = at >> span_log2, col = at & ((1 << span_log2) - 1);
+        float v = 0.f;
+        if (r0 + r < rows && c0 + col < p.cols) v = (float)x[(row0 + r0 + r) * p.stride + c0 + col];
+        staged(r, col, span_log2) = v;
+      }
+      __syncthreads();
+      float v[16];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        v[i] = staged(mine, seg * 16 + i, span_log2);
+        top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+      }
+      put(r0 + mine, top, v);
+      __syncthreads();
     }
   }
   __syncthreads();
@@ -92,54 +153,87 @@ __global__ void __launch_bounds__(kThreads) k_q4_quantize(const T *__restrict__ 
   for (uint32_t i = tid; i < n * (kAtom / 16); i += kThreads) out[i] = reinterpret_cast<const uint4 *>(scales)[i];
 }
 
-template <int F, typename T>
+template <int F, typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_q4_dequantize(const uint8_t *__restrict__ q, T *__restrict__ y, const Params p) {
+  __shared__ __align__(16) uint8_t scales[4 * kAtom];
+  extern __shared__ uint8_t staged_s[];            // Staged, where !VEC
   dc_pdl_enter();
-  const int tid = (int)threadIdx.x, segs = 1 << p.segs_log2;
+  const int tid = (int)threadIdx.x, segs = 1 << p.segs_log2, span_log2 = p.segs_log2 + 4;
   const uint32_t tile = blockIdx.x / p.col_tiles, col_tile = blockIdx.x - tile * p.col_tiles;
-  const int c = (int)(col_tile << (p.segs_log2 + 4)) + (tid & (segs - 1)) * 16;
-  if (c >= p.cols) return;
+  const int seg = tid & (segs - 1), c0 = (int)(col_tile << span_log2), c = c0 + seg * 16;
+  const long long row0 = (long long)tile * 128;
+  const int rows = p.rows - row0 < 128 ? (int)(p.rows - row0) : 128;
   constexpr int kBlock = F == DC_MX4 ? 32 : 16;
-  const uint32_t b = (uint32_t)(c / kBlock);
-#pragma unroll 1
-  for (int r = tid >> p.segs_log2; r < 128; r += kThreads >> p.segs_log2) {
-    const long long row = (long long)tile * 128 + r;
-    if (row >= p.rows) return;
-    const uint2 code = __ldg(reinterpret_cast<const uint2 *>(q + (size_t)row * p.pitch + (c >> 1)));
-    const uint32_t byte = __ldg(q + p.scale_offset + ((size_t)tile * p.tiles + (b >> 2)) * kAtom + scale_at((uint32_t)r, b));
-    const float s = scale_value(byte, F, p.g);
+  const int atoms = (1 << span_log2) <= 4 * kBlock ? 1 : (1 << span_log2) / (4 * kBlock);
+  {
+    const uint32_t atom0 = col_tile * (uint32_t)atoms;
+    const uint32_t left = p.tiles - atom0, n = left < (uint32_t)atoms ? left : (uint32_t)atoms;
+    const uint4 *in = reinterpret_cast<const uint4 *>(q + p.scale_offset + ((size_t)tile * p.tiles + atom0) * kAtom);
+    for (uint32_t i = tid; i < n * (kAtom / 16); i += kThreads) reinterpret_cast<uint4 *>(scales)[i] = __ldg(in + i);
+  }
+  const int step = kThreads >> p.segs_log2, mine = tid >> p.segs_log2;
+  const bool wanted = c < p.cols;
+  const uint32_t b = (uint32_t)(seg * 16 / kBlock);
+  auto codes_of = [&](int r) { return wanted && r < rows ? __ldg(reinterpret_cast<const uint2 *>(q + (size_t)(row0 + r) * p.pitch + (c >> 1))) : make_uint2(0, 0); };
+  auto values = [&](int r, uint2 code, float *v) {
+    const float s = scale_value(scales[(b >> 2) * kAtom + scale_at((uint32_t)r, b)], F, p.g);
     uint32_t h[8];
     values8(code.x, h);
     values8(code.y, h + 4);
-    float v[16];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[i]));
       v[2 * i] = f.x * s;
       v[2 * i + 1] = f.y * s;
     }
-    T *at = y + row * p.stride + c;
-    if (p.vec && c + 16 <= p.cols) {
-      if (sizeof(T) == 2) {
-        uint32_t w[8];
+  };
+  if (VEC) {
+    constexpr int U = 4;
+    __syncthreads();
+    if (!wanted) return;
+#pragma unroll 1
+    for (int r = mine; r < rows; r += U * step) {
+      uint2 code[U];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-          w[i] = *reinterpret_cast<const uint32_t *>(&t);
+      for (int u = 0; u < U; ++u) code[u] = codes_of(r + u * step);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int ru = r + u * step;
+        if (ru >= rows) break;
+        float v[16];
+        values(ru, code[u], v);
+        T *at = y + (row0 + ru) * p.stride + c;
+#pragma unroll
+        for (int i = 0; i < 16 / kPer<T>; ++i) {
+          const int left = p.cols - (c + i * kPer<T>);
+          if (left >= kPer<T>) {
+            reinterpret_cast<uint4 *>(at)[i] = pack<T>(v + i * kPer<T>);
+          } else {
+#pragma unroll
+            for (int j = 0; j < kPer<T>; ++j)
+              if (j < left) at[i * kPer<T> + j] = (T)v[i * kPer<T> + j];
+          }
         }
-        reinterpret_cast<uint4 *>(at)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        reinterpret_cast<uint4 *>(at)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) reinterpret_cast<float4 *>(at)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
       }
-    } else {
+    }
+  } else {
+    Staged &staged = *reinterpret_cast<Staged *>(staged_s);
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += step) {
+      const uint2 code = codes_of(r0 + mine);
+      __syncthreads();
+      if (wanted && r0 + mine < rows) {
+        float v[16];
+        values(r0 + mine, code, v);
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (c + i < p.cols) {
-          if (sizeof(T) == 2) reinterpret_cast<__nv_bfloat16 *>(at)[i] = __float2bfloat16_rn(v[i]);
-          else reinterpret_cast<float *>(at)[i] = v[i];
-        }
+        for (int i = 0; i < 16; ++i) staged(mine, seg * 16 + i, span_log2) = v[i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int at = tid + i * kThreads, r = at >> span_log2, col = at & ((1 << span_log2) - 1);
+        if (r0 + r < rows && c0 + col < p.cols) y[(row0 + r0 + r) * p.stride + c0 + col] = (T)staged(r, col, span_log2);
+      }
     }
   }
 }
@@ -182,6 +276,17 @@ extern "C" dc_status dc_q4_query(long long rows, int cols, dc_q4_format format, 
   return DC_OK;
 }
 
+template <int F, typename T>
+static cudaError_t quantize(const void *x, void *q, const Params &p, dim3 grid, cudaStream_t st) {
+  return p.vec ? dc_launch_pdl(k_q4_quantize<F, T, true>, grid, dim3(kThreads), 0, st, (const T *)x, (uint8_t *)q, p)
+               : dc_launch_pdl(k_q4_quantize<F, T, false>, grid, dim3(kThreads), sizeof(Staged), st, (const T *)x, (uint8_t *)q, p);
+}
+template <int F, typename T>
+static cudaError_t dequantize(const void *q, void *y, const Params &p, dim3 grid, cudaStream_t st) {
+  return p.vec ? dc_launch_pdl(k_q4_dequantize<F, T, true>, grid, dim3(kThreads), 0, st, (const uint8_t *)q, (T *)y, p)
+               : dc_launch_pdl(k_q4_dequantize<F, T, false>, grid, dim3(kThreads), sizeof(Staged), st, (const uint8_t *)q, (T *)y, p);
+}
+
 extern "C" dc_status dc_q4_quantize(const void *x, long long rows, int cols, long long stride, dc_dtype dtype, dc_q4_format format,
                                     float tensor_scale, void *q, dc_stream stream) {
   Params p;
@@ -189,17 +294,9 @@ extern "C" dc_status dc_q4_quantize(const void *x, long long rows, int cols, lon
   const dc_status s = prepare(x, rows, cols, stride, dtype, format, tensor_scale, q, &p, &grid);
   if (s != DC_OK) return s;
   cudaStream_t st = (cudaStream_t)stream;
-  uint8_t *out = (uint8_t *)q;
   cudaError_t e;
-  if (dtype == DC_BF16) {
-    const __nv_bfloat16 *in = (const __nv_bfloat16 *)x;
-    e = format == DC_MX4 ? dc_launch_pdl(k_q4_quantize<DC_MX4, __nv_bfloat16>, grid, dim3(kThreads), 0, st, in, out, p)
-                         : dc_launch_pdl(k_q4_quantize<DC_NV4, __nv_bfloat16>, grid, dim3(kThreads), 0, st, in, out, p);
-  } else {
-    const float *in = (const float *)x;
-    e = format == DC_MX4 ? dc_launch_pdl(k_q4_quantize<DC_MX4, float>, grid, dim3(kThreads), 0, st, in, out, p)
-                         : dc_launch_pdl(k_q4_quantize<DC_NV4, float>, grid, dim3(kThreads), 0, st, in, out, p);
-  }
+  if (format == DC_MX4) e = dtype == DC_BF16 ? quantize<DC_MX4, __nv_bfloat16>(x, q, p, grid, st) : quantize<DC_MX4, float>(x, q, p, grid, st);
+  else e = dtype == DC_BF16 ? quantize<DC_NV4, __nv_bfloat16>(x, q, p, grid, st) : quantize<DC_NV4, float>(x, q, p, grid, st);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? DC_OK : DC_ERR_CUDA;
 }
 
@@ -210,16 +307,8 @@ extern "C" dc_status dc_q4_dequantize(const void *q, long long rows, int cols, d
   const dc_status s = prepare(y, rows, cols, stride, dtype, format, tensor_scale, q, &p, &grid);
   if (s != DC_OK) return s;
   cudaStream_t st = (cudaStream_t)stream;
-  const uint8_t *in = (const uint8_t *)q;
   cudaError_t e;
-  if (dtype == DC_BF16) {
-    __nv_bfloat16 *out = (__nv_bfloat16 *)y;
-    e = format == DC_MX4 ? dc_launch_pdl(k_q4_dequantize<DC_MX4, __nv_bfloat16>, grid, dim3(kThreads), 0, st, in, out, p)
-                         : dc_launch_pdl(k_q4_dequantize<DC_NV4, __nv_bfloat16>, grid, dim3(kThreads), 0, st, in, out, p);
-  } else {
-    float *out = (float *)y;
-    e = format == DC_MX4 ? dc_launch_pdl(k_q4_dequantize<DC_MX4, float>, grid, dim3(kThreads), 0, st, in, out, p)
-                         : dc_launch_pdl(k_q4_dequantize<DC_NV4, float>, grid, dim3(kThreads), 0, st, in, out, p);
-  }
+  if (format == DC_MX4) e = dtype == DC_BF16 ? dequantize<DC_MX4, __nv_bfloat16>(q, y, p, grid, st) : dequantize<DC_MX4, float>(q, y, p, grid, st);
+  else e = dtype == DC_BF16 ? dequantize<DC_NV4, __nv_bfloat16>(q, y, p, grid, st) : dequantize<DC_NV4, float>(q, y, p, grid, st);
   return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? DC_OK : DC_ERR_CUDA;
 }

@@ -24,14 +24,15 @@ using namespace tc;
 using q4::kAtom;
 
 enum { kOne = 0, kPair = 1, kRows = 2, kStream = 3 };
-constexpr int kEpiWarps = 8, kCutWarps = 8;
+constexpr int kEpiWarps = 8;                     // reading out
+constexpr int kCutWarps = 4;                     // quantising, form kStream
 template <int FORM>
 constexpr int kThreadsOf = (2 + kEpiWarps + (FORM == kStream ? kCutWarps : 0)) * 32;
-constexpr int kMaxStages = 8, kMaxSplit = 8;
+constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxAcc = 4;
 constexpr int kSmemMax = 225 * 1024;
 constexpr int kStageCols = 256;                  // columns of a stage: 128 bytes of codes
 constexpr int kOut = 32;                         // columns that a warp reads out at a time
-constexpr int kOutBytes = 32 * kOut * 4;         // ... and its shared memory for them
+constexpr int kOutBytes = 32 * kOut * 4;         // ... and its shared memory for them: once in fp32, twice in bf16
 constexpr int kMaxRows = 32;                     // of form kRows
 
 struct Params {
@@ -43,7 +44,7 @@ struct Params {
   int tiles_m, tiles_n, items;
   int chunks;                // stages of a row
   int split, chunks_per;     // CTAs that share an item, stages of each
-  int stages, acc_bufs, sets;                // sets: the reading-out warps take tiles in turn, four warps each
+  int stages, acc_bufs;
   int stage_bytes, sf_cols;  // of a stage: shared memory, and tensor memory of its scales
   int w_stays, w_bytes;      // w's stages stay in shared memory; bytes of one
   int groups;                // kRows: groups of 8 rows
@@ -167,24 +168,69 @@ __device__ __forceinline__ void load_bias(const float *__restrict__ bias, int o,
 #pragma unroll
   for (int i = 0; i < n; i += 4) *reinterpret_cast<float4 *>(b + i) = bias ? __ldg(reinterpret_cast<const float4 *>(bias + o + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
 }
-// sums -> 16 bytes of y: scale and bias, residual, activation
 template <typename T>
 __device__ __forceinline__ uint4 finish16(const Params &p, const float *b, bool has_residual, uint4 residual, float *v) {
   constexpr int N = kPer<T>;
+  float r[N];
+  if (has_residual) unpack16<T>(residual, r);
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = fmaf(v[i], p.scale, b[i]);
-  if (has_residual) {
-    float r[N];
-    unpack16<T>(residual, r);
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += r[i];
-  }
-  if (p.act == DC_ACT_RELU6) {
-    if (N == 8) return make_uint4(relu6_bf16x2(v[0], v[1]), relu6_bf16x2(v[2], v[3]), relu6_bf16x2(v[4 % N], v[5 % N]), relu6_bf16x2(v[6 % N], v[7 % N]));
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = dc_act_apply(v[i], DC_ACT_RELU6);
+  for (int i = 0; i < N; ++i) {
+    float t = fmaf(v[i], p.scale, b[i]);
+    if (has_residual) t += r[i];
+    v[i] = dc_act_apply(t, p.act);
   }
   return pack16<T>(v);
+}
+__device__ __forceinline__ unsigned long long pair_of(float lo, float hi) {
+  unsigned long long d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+// two FMAs in one instruction
+__device__ __forceinline__ void fma2(float &lo, float &hi, unsigned long long s, unsigned long long b) {
+  unsigned long long d = pair_of(lo, hi);
+  asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(d) : "l"(s), "l"(b));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d));
+}
+// A thread's row of 32 sums: scale and bias (shared memory, the same for all lanes), residual (in place in the staged row), activation, and into
+// the staged row: pieces of 16 bytes at i ^ swap, as the tensor map of y swaps them.
+template <typename T, bool RES, bool RELU6>
+__device__ __forceinline__ void stage_row(float scale, uint32_t bias, float *v, uint32_t row, uint32_t swap) {
+  constexpr int N = kPer<T>;
+  const unsigned long long s = pair_of(scale, scale);
+#pragma unroll
+  for (int i = 0; i < kOut / N; ++i) {
+    float *u = v + i * N;
+    const uint32_t at = row + ((uint32_t)i ^ swap) * 16u;
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+      const uint4 b = lds_u4(bias + (uint32_t)((i * N + j) * 4));
+      fma2(u[j], u[j + 1], s, pair_of(__uint_as_float(b.x), __uint_as_float(b.y)));
+      fma2(u[j + 2], u[j + 3], s, pair_of(__uint_as_float(b.z), __uint_as_float(b.w)));
+    }
+    if (RES) {
+      float r[N];
+      unpack16<T>(lds_u4(at), r);
+#pragma unroll
+      for (int j = 0; j < N; ++j) u[j] += r[j];
+    }
+    uint4 w;
+    if (RELU6 && N == 8) {
+      w = make_uint4(relu6_bf16x2(u[0], u[1]), relu6_bf16x2(u[2], u[3]), relu6_bf16x2(u[4 % N], u[5 % N]), relu6_bf16x2(u[6 % N], u[7 % N]));
+    } else {
+      if (RELU6) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) u[j] = dc_act_apply(u[j], DC_ACT_RELU6);
+      }
+      w = pack16<T>(u);
+    }
+    sts_u4(at, w);
+  }
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t ssrc, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(ssrc), "r"(c0),
+               "r"(c1)
+               : "memory");
 }
 // columns one by one, where rows of y do not begin on 16 bytes
 template <typename T>
@@ -210,46 +256,12 @@ __device__ __forceinline__ void deliver(const Params &p, const float *__restrict
   for (int i = 0; i < N; ++i)
     if (o + i < p.c_out) deliver_one<T>(p, v[i], bias ? __ldg(bias + o + i) : 0.f, residual, y, at + i);
 }
-// 32 rows x 32 results in the warp's shared memory -> y from row `row0`, column `o`: neighbouring lanes store neighbouring columns.
+// a lane to a column, where rows of y do not begin on 16 bytes
 template <typename T>
-__device__ __forceinline__ void deliver32(const Params &p, const float *__restrict__ bias, const T *residual, T *y, long long row0, int o,
-                                          uint32_t sm, int lane) {
-  const int rows = p.rows - row0 < 32 ? (int)(p.rows - row0) : 32;
-  if (p.vec) {
-    constexpr int N = kPer<T>, kLanes = kOut / N, kStep = 32 / kLanes, kTimes = 32 / kStep;     // lanes to a row, rows at a time, times
-    const int c = (lane % kLanes) * N, r0 = lane / kLanes;
-    if (o + c >= p.c_out) return;
-    float b[N];
-    load_bias(bias, o + c, N, b);
-    const size_t at = (size_t)(row0 + r0) * (size_t)p.c_out + (size_t)(o + c), pitch = (size_t)p.c_out * kStep;
-#pragma unroll
-    for (int h = 0; h < kTimes; h += 4) {        // four rows at once, so that their loads overlap
-      uint4 res[4];
-      float t[4][N];
-      if (residual) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (r0 + (h + i) * kStep < rows) res[i] = *reinterpret_cast<const uint4 *>(residual + at + pitch * (h + i));
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = r0 + (h + i) * kStep;
-#pragma unroll
-        for (int j = 0; j < N; j += 4) *reinterpret_cast<uint4 *>(&t[i][j]) = lds_u4(sm + (uint32_t)(r * 128 + (((c + j) >> 2) ^ (r & 7)) * 16));
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 w = finish16<T>(p, b, residual != nullptr, res[i], t[i]);
-        if (r0 + (h + i) * kStep < rows) *reinterpret_cast<uint4 *>(y + at + pitch * (h + i)) = w;
-      }
-    }
-  } else if (o + lane < p.c_out) {               // a lane to a column
-    const float b = bias ? __ldg(bias + o + lane) : 0.f;
-    size_t at = (size_t)row0 * (size_t)p.c_out + (size_t)(o + lane);
-#pragma unroll 8
-    for (int r = 0; r < rows; ++r, at += (size_t)p.c_out)
-      deliver_one<T>(p, lds_f(sm + (uint32_t)(r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4)), b, residual, y, at);
-  }
+__device__ __forceinline__ void deliver_columns(const Params &p, float b, const T *residual, T *y, size_t at, int rows, uint32_t sm, int lane) {
+#pragma unroll 4
+  for (int r = 0; r < rows; ++r, at += (size_t)p.c_out)
+    deliver_one<T>(p, lds_f(sm + (uint32_t)(r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4)), b, residual, y, at);
 }
 
 // 16 columns of a row of x from column c: the values, zeros from column c_in on
@@ -302,18 +314,20 @@ __device__ __forceinline__ void put_x16(float *v, const Params &p, uint32_t a, u
   }
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kXFull = kDEmpty + 2, kWFull, kBars };
+enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + kMaxAcc, kXFull = kDEmpty + kMaxAcc, kWFull, kRes, kBars = kRes + kEpiWarps };
 
 template <int F, typename T, int FORM>
 __global__ void __launch_bounds__(kThreadsOf<FORM>, 1)
 k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_sx, const __grid_constant__ CUtensorMap map_w,
-             const __grid_constant__ CUtensorMap map_sw, const T *__restrict__ x, const float *__restrict__ bias, const T *residual, T *y,
+             const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_res,
+             const T *__restrict__ x, const float *__restrict__ bias, const T *residual, T *y,
              const __grid_constant__ Params p, DcWsHeader *ws) {
   constexpr int kAtoms = kAtomsOf<F>;
   constexpr bool P = FORM == kPair;
   constexpr uint32_t kTmemCols = 512;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kBars];
+  __shared__ __align__(16) float bias_s[kEpiWarps][kOut];
   __shared__ uint32_t tmem_s, abort_s;
   volatile uint32_t *abort_flag = &abort_s;
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -322,15 +336,16 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     if (lane == 0) {
       abort_s = 0;
       for (int i = 0; i < kMaxStages; ++i) {
-        mbar_init(&bar[kFull + i], FORM == kStream ? (p.w_stays ? 4 : 5) : 1);
+        mbar_init(&bar[kFull + i], FORM == kStream ? kCutWarps + (p.w_stays ? 0 : 1) : 1);
         mbar_init(&bar[kEmpty + i], 1);
       }
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < kMaxAcc; ++i) {
         mbar_init(&bar[kDFull + i], 1);
-        mbar_init(&bar[kDEmpty + i], P ? 2 * kEpiWarps : (p.sets == 2 ? kEpiWarps / 2 : kEpiWarps));
+        mbar_init(&bar[kDEmpty + i], P ? 2 * kEpiWarps : kEpiWarps / p.acc_bufs);
       }
       mbar_init(&bar[kXFull], kEpiWarps);
       mbar_init(&bar[kWFull], 1);
+      for (int i = 0; i < kEpiWarps; ++i) mbar_init(&bar[kRes + i], 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
       prefetch_tensormap(&map_w);
       prefetch_tensormap(&map_sw);
@@ -414,14 +429,12 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- multiply
-    int stage = 0, n = 0;
-    uint32_t parity = 0;
+    int stage = 0, buf = 0;
+    uint32_t parity = 0, use = 0;                // use: of the accumulators, how many times round
     bool ok = !P || rank == 0;
     if (FORM == kRows && ok) ok = warp_wait(&bar[kXFull], 0, abort_flag, ws, 0x50000u);
     if (p.w_stays && ok) ok = warp_wait(&bar[kWFull], 0, abort_flag, ws, 0x60000u);
-    for (int item = first; ok && item < p.items; item += step, ++n) {
-      const int buf = p.acc_bufs == 2 ? n & 1 : 0;
-      const uint32_t use = (uint32_t)(p.acc_bufs == 2 ? n >> 1 : n);
+    for (int item = first; ok && item < p.items; item += step) {
       ok = warp_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x20000u | (uint32_t)buf);
       if (!ok) break;
       tc_fence_after();
@@ -452,6 +465,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         __syncwarp();
         if (++stage == p.stages) { stage = 0; parity ^= 1u; }
       }
+      if (++buf == p.acc_bufs) { buf = 0; ++use; }
     }
   } else if (warp < 2 + kEpiWarps) {
     // ---------------------------------------------------------------- read out
@@ -475,41 +489,50 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar[kXFull]);
     }
-    const uint32_t out = sm + (uint32_t)(p.off_out + (warp - 2) * kOutBytes), mine = out + (uint32_t)lane * 128u;
+    constexpr int kBufs = 4 / (int)sizeof(T);    // of staged results
+    constexpr uint32_t kRow = kOut * sizeof(T);
+    const uint32_t out = sm + (uint32_t)(p.off_out + (warp - 2) * kOutBytes), bias_w = smem_u32(bias_s[warp - 2]);
+    const uint32_t mine = out + (uint32_t)lane * kRow, swap = sizeof(T) == 2 ? (uint32_t)(lane >> 1) & 3u : (uint32_t)lane & 7u;
     const uint32_t freed = P ? map_cluster(smem_u32(&bar[kDEmpty]), 0) : 0u;
-    const int c_first = p.sets == 2 ? 0 : set * kOut, c_step = p.sets == 2 ? kOut : 2 * kOut;
-    int n = 0;
-    for (int item = first; item < p.items; item += step, ++n) {
-      if (p.sets == 2 && (n & 1) != set) continue;
-      const int buf = p.acc_bufs == 2 ? n & 1 : 0;
-      const uint32_t use = (uint32_t)(p.acc_bufs == 2 ? n >> 1 : n);
+    // sets of four warps: each takes every acc_bufs-th tile, an accumulator of its own, and shares its columns with the other sets on it
+    const int buf = set % p.acc_bufs, c_first = set / p.acc_bufs * kOut, c_step = kEpiWarps / 4 / p.acc_bufs * kOut;
+    const bool parts = FORM != kPair && FORM != kStream && p.split > 1;
+    uint32_t use = 0, turn = 0, res_parity = 0;
+    for (int item = first + buf * step; item < p.items; item += p.acc_bufs * step, ++use) {
       const int tm = item % p.tiles_m, tn = item / p.tiles_m;
       const long long row0 = (long long)(P ? tm * 2 + rank : tm) * 128 + quad * 32;
       const int cols = min(p.nt, p.c_out - tn * p.nt);
-      if (!warp_wait(&bar[kDFull + buf], use & 1u, abort_flag, ws, 0x40000u | (uint32_t)buf)) break;
-      tc_fence_after();
       const bool work = row0 < p.rows && c_first < cols;
       const uint32_t d = tmem + (uint32_t)(buf * p.nt) + ((uint32_t)(quad * 32) << 16);
-      uint32_t v[kOut];
-      if (work) tmem_ld32(d + (uint32_t)c_first, v);
+      bool ok = true;
 #pragma unroll 1
       for (int c = c_first; c < cols || c == c_first; c += c_step) {
         const bool last = c + c_step >= cols;
-        if (work) {
-          tmem_ld_wait();
-          if (FORM != kPair && FORM != kStream && p.split > 1) {
-            if (row0 + lane < p.rows) {
-              const uint32_t at = sm + (uint32_t)((quad * 32 + lane) * part_pitch + c * 4);
-#pragma unroll
-              for (int i = 0; i < kOut / 4; ++i) sts_u4(at + (uint32_t)(i * 16), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+        const int col = tn * p.nt + c;
+        const uint32_t at = kBufs == 2 && (turn & 1u) ? 2048u : 0u;
+        if (work && !parts) {
+          // what does not depend on the sums first: the bias, a free buffer, the residual into it
+          const float b = bias && col + lane < p.c_out ? __ldg(bias + col + lane) : 0.f;
+          if (p.vec && lane == 0) {
+            if (kBufs == 2) bulk_wait_read1();
+            else bulk_wait_read0();
+            if (residual) {
+              mbar_arrive_expect_tx(&bar[kRes + warp - 2], 32 * kRow);
+              tma_load_2d(out + at, &map_res, &bar[kRes + warp - 2], col, (int)row0);
             }
-          } else {
-            // 16-byte pieces of a row are swapped by the row's low bits: no bank conflicts on either side
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sts_u4(mine + (uint32_t)((i ^ (lane & 7)) * 16), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
-            __syncwarp();
           }
-          if (!last) tmem_ld32(d + (uint32_t)(c + c_step), v);
+          bias_s[warp - 2][lane] = b;
+          __syncwarp();
+        }
+        if (c == c_first) {
+          ok = warp_wait(&bar[kDFull + buf], use & 1u, abort_flag, ws, 0x40000u | (uint32_t)buf);
+          if (!ok) break;
+          tc_fence_after();
+        }
+        float v[kOut];
+        if (work) {
+          tmem_ld32(d + (uint32_t)c, reinterpret_cast<uint32_t *>(v));
+          tmem_ld_wait();
         }
         if (last) {                              // the accumulator is read: the next tile may have it
           tc_fence_before();
@@ -519,16 +542,51 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             else mbar_arrive(&bar[kDEmpty + buf]);
           }
         }
-        if (work && (FORM == kPair || FORM == kStream || p.split == 1)) {
-          deliver32<T>(p, bias, residual, y, row0, tn * p.nt + c, out, lane);
+        if (!work) continue;
+        if (parts) {
+          if (row0 + lane < p.rows) {
+            const uint32_t to = sm + (uint32_t)((quad * 32 + lane) * part_pitch + c * 4);
+#pragma unroll
+            for (int i = 0; i < kOut / 4; ++i)
+              sts_u4(to + (uint32_t)(i * 16), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+          }
+        } else if (p.vec) {
+          if (residual) {
+            ok = warp_wait(&bar[kRes + warp - 2], res_parity, abort_flag, ws, 0xA0000u | (uint32_t)warp);
+            if (!ok) break;
+            res_parity ^= 1u;
+            if (p.act == DC_ACT_RELU6) stage_row<T, true, true>(p.scale, bias_w, v, mine + at, swap);
+            else stage_row<T, true, false>(p.scale, bias_w, v, mine + at, swap);
+          } else {
+            if (p.act == DC_ACT_RELU6) stage_row<T, false, true>(p.scale, bias_w, v, mine + at, swap);
+            else stage_row<T, false, false>(p.scale, bias_w, v, mine + at, swap);
+          }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(&map_y, out + at, col, (int)row0);
+            bulk_commit();
+          }
+          ++turn;
+        } else {
+          const uint32_t row = out + (uint32_t)lane * 128u;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            sts_u4(row + (uint32_t)((i ^ (lane & 7)) * 16), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+          __syncwarp();
+          if (col + lane < p.c_out)
+            deliver_columns<T>(p, bias_s[warp - 2][lane], residual, y, (size_t)row0 * (size_t)p.c_out + (size_t)(col + lane),
+                               p.rows - row0 < 32 ? (int)(p.rows - row0) : 32, out, lane);
           __syncwarp();
         }
       }
+      if (!ok) break;
     }
+    if (lane == 0) bulk_wait_all();              // the last results are read, and written
   } else {
-    // ---------------------------------------------------------------- quantise (kStream): a thread to a row, two groups of four warps take the stages
-    // in turn, 32 columns at a time; the next 32, of the next stage or tile too, are asked for before these are worked on
-    const int group = (warp - 2 - kEpiWarps) >> 2, r = ((warp - 2 - kEpiWarps) & 3) * 32 + lane;
+    // ---------------------------------------------------------------- quantise (kStream): a thread to a row, 32 columns at a time; the next 32, of the
+    // next stage or tile too, are asked for before these are worked on
+    const int r = (warp - 2 - kEpiWarps) * 32 + lane;
     constexpr int kRaw = 32 / kPer<T>;
     uint4 next[kRaw];
     auto ask = [&](int item, int ch, int c) {    // columns c .. c + 31 of a stage
@@ -539,14 +597,9 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       for (int i = 0; i < kRaw; ++i)
         next[i] = row < p.rows && col + i * kPer<T> < p.c_in ? __ldg(reinterpret_cast<const uint4 *>(at) + i) : make_uint4(0, 0, 0, 0);
     };
-    // this group's stages: numbers group, group + 2, ... of those of the CTA
-    int item = first, ch = group, stage = group;
+    int item = first, ch = 0, stage = 0;
     uint32_t parity = 0;
     bool ok = true;
-    auto settle = [&]() {
-      while (ch >= p.chunks) { ch -= p.chunks; item += step; }
-    };
-    settle();
     if (item < p.items) ask(item, ch, 0);
     while (ok && item < p.items) {
       ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x70000u | (uint32_t)stage);
@@ -554,8 +607,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       const uint32_t a = ring + (uint32_t)(stage * p.stage_bytes) + (uint32_t)((r >> 3) * 1024 + (r & 7) * 128);
       const uint32_t sfa = ring + (uint32_t)(stage * p.stage_bytes) + kA;
       const int item0 = item, ch0 = ch, end = (min(p.c_in - ch * kStageCols, kStageCols) + 63) / 64 * 64;
-      ch += 2;
-      settle();
+      if (++ch == p.chunks) { ch = 0; item += step; }
 #pragma unroll 1
       for (int c = 0; c < end; c += 32) {
         uint4 raw[kRaw];
@@ -585,8 +637,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar[kFull + stage]);
-      stage += 2;
-      if (stage >= p.stages) { stage -= p.stages; parity ^= 1u; }
+      if (++stage == p.stages) { stage = 0; parity ^= 1u; }
     }
   }
   if (warp == 1 && *abort_flag) {                // copies and products may still be in flight: give them time to end
@@ -663,6 +714,16 @@ bool scales_map(EncodeTiledFn encode, CUtensorMap *map, const void *q, const q4:
                 CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// y, or the residual: boxes of what a warp reads out at a time
+template <typename T>
+bool results_map(EncodeTiledFn encode, CUtensorMap *map, const void *y, const Params &p) {
+  const cuuint64_t dim[2] = {(cuuint64_t)p.c_out, (cuuint64_t)p.rows}, str[1] = {(cuuint64_t)p.c_out * sizeof(T)};
+  const cuuint32_t bx[2] = {kOut, 32}, es[2] = {1, 1};
+  return encode(map, sizeof(T) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void *>(y), dim, str, bx, es,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, sizeof(T) == 2 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct Call {
   const void *x, *w;
   const q4::Layout *lx, *lw;
@@ -680,18 +741,19 @@ cudaError_t launch(Params &p, const Call &c) {
   if (e != cudaSuccess) return e;
   EncodeTiledFn encode = get_encode_fn();
   if (!encode) return cudaErrorNotSupported;
-  CUtensorMap map_x = {}, map_sx = {}, map_w, map_sw;
+  CUtensorMap map_x = {}, map_sx = {}, map_w, map_sw, map_y = {}, map_res = {};
   constexpr int kAtoms = kAtomsOf<F>;
   if (!codes_map(encode, &map_w, c.w, c.lw->pitch, p.c_out, FORM == kPair ? p.nt / 2 : p.nt) || !scales_map(encode, &map_sw, c.w, *c.lw, p.c_out, kAtoms, p.nb))
     return cudaErrorNotSupported;
   if ((FORM == kOne || FORM == kPair) &&
       (!codes_map(encode, &map_x, c.x, c.lx->pitch, p.rows, 128) || !scales_map(encode, &map_sx, c.x, *c.lx, p.rows, kAtoms, 1)))
     return cudaErrorNotSupported;
+  if (p.vec && (!results_map<T>(encode, &map_y, c.y, p) || (c.residual && !results_map<T>(encode, &map_res, c.residual, p)))) return cudaErrorNotSupported;
   const int team = FORM == kPair ? 2 : p.split;
   const int grid = team > 1 ? (p.items * team < c.n_sm / team * team ? p.items * team : c.n_sm / team * team) : (p.items < c.n_sm ? p.items : c.n_sm);
   // all of a CTA's shared memory is asked for: two CTAs on an SM would each want all of its tensor memory
   return dc_launch_pdl_cluster(k_q4_product<F, T, FORM>, dim3((unsigned)grid), dim3(kThreadsOf<FORM>), (size_t)kSmemMax, c.st, team, map_x, map_sx, map_w,
-                               map_sw, FORM == kRows || FORM == kStream ? (const T *)c.x : (const T *)nullptr, c.bias, (const T *)c.residual, (T *)c.y, p, c.ws);
+                               map_sw, map_y, map_res, FORM == kRows || FORM == kStream ? (const T *)c.x : (const T *)nullptr, c.bias, (const T *)c.residual, (T *)c.y, p, c.ws);
 }
 
 // Shared and tensor memory of a form, tile width and split; false: it does not fit.
@@ -701,8 +763,9 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   p->w_bytes = (form == kPair ? p->nt / 2 : p->nt) * 128 + p->nb * atoms * kAtom;
   p->sf_cols = 4 * atoms * (1 + p->nb);
   const bool many = form != kPair && p->split == 1 && p->items > n_sm;         // CTAs have several tiles
-  p->acc_bufs = many && 2 * p->nt + 3 * p->sf_cols <= 512 ? 2 : 1;
-  p->sets = p->acc_bufs;
+  p->acc_bufs = 1;
+  for (int n = 2; many && n <= kEpiWarps / 4; n *= 2)
+    if (n * p->nt + 3 * p->sf_cols <= 512) p->acc_bufs = n;
   const int x_bytes = form == kRows ? 0 : kA + atoms * kAtom;
   int room = kSmemMax - 1024 - kEpiWarps * kOutBytes;
   p->off_sfa = p->off_ring = 0;
@@ -734,7 +797,7 @@ double estimate(const Params &p, int form, int n_sm) {
   const double main = (form == kPair ? p.chunks : p.chunks_per) * stage, out = 4.0 * p.nt + 500;
   double waves = p.items / at_once;
   waves = (double)(long long)(waves + 0.999);
-  return 3000 + waves * (p.acc_bufs == 2 ? (main > out ? main : out) : main + out) + (team > 1 ? 1500 : 0) +
+  return 3000 + waves * (p.acc_bufs > 1 ? (main > out ? main : out) : main + out) + (team > 1 ? 1500 : 0) +
          (form == kRows ? 400 + 250.0 * (double)p.rows * p.chunks_per / 16 : 0);
 }
 

@@ -29,10 +29,11 @@ constexpr int kCutWarps = 4;                     // quantising, form kStream
 template <int FORM>
 constexpr int kThreadsOf = (2 + kEpiWarps + (FORM == kStream ? kCutWarps : 0)) * 32;
 constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxAcc = 4;
-constexpr int kSmemMax = 225 * 1024;
+constexpr int kSmemMax = 224 * 1024;
 constexpr int kStageCols = 256;                  // columns of a stage: 128 bytes of codes
-constexpr int kOut = 32;                         // columns that a warp reads out at a time
-constexpr int kOutBytes = 32 * kOut * 4;         // ... and its shared memory for them: once in fp32, twice in bf16
+constexpr int kOutBytes = 32 * 128;              // of a reading-out warp: 32 rows of 128 bytes of results
+template <typename T>
+constexpr int kOut = 128 / (int)sizeof(T);       // ... which are so many columns
 constexpr int kMaxRows = 32;                     // of form kRows
 
 struct Params {
@@ -102,7 +103,7 @@ __device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, uin
   const uint64_t da = scales_desc(sfa), db = scales_desc(sfb), ad = operand_desc(a), bd = operand_desc(b);
   const uint32_t tb = ta + 4u * kAtoms;
 #pragma unroll
-  for (int i = 0; i < kAtoms; ++i) {
+  for (int i = 0; i < (F == DC_NV4 ? STEPS : (STEPS + 1) / 2); ++i) {
     copy_scales<P>(ta + 4u * i, da + (uint64_t)(i * (kAtom / 16)));
 #pragma unroll
     for (int j = 0; j < NB; ++j) copy_scales<P>(tb + 4u * (i * NB + j), db + (uint64_t)((j * kAtoms + i) * (kAtom / 16)));
@@ -113,14 +114,12 @@ __device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint32_t b, uin
     mma_q4<F, P>(d, ad + 2u * k, bd + 2u * k, with_id<F>(idesc, k), ta + 4u * atom, tb + 4u * NB * atom, accumulate || k > 0 ? 1u : 0u);
   }
 }
-template <int F, bool P>
-__device__ __forceinline__ void multiply_last(uint32_t d, uint32_t a, uint32_t b, uint32_t sfa, uint32_t sfb, uint32_t ta, uint32_t tb, int nb, uint32_t idesc,
-                                              int k, bool accumulate) {
-  if (F == DC_NV4 || (k & 1) == 0) {
-    copy_scales<P>(ta, scales_desc(sfa));
-    for (int j = 0; j < nb; ++j) copy_scales<P>(tb + 4u * j, scales_desc(sfb + (uint32_t)(j * kAtomsOf<F> * kAtom)));
-  }
-  mma_q4<F, P>(d, operand_desc(a), operand_desc(b), with_id<F>(idesc, k), ta, tb, accumulate ? 1u : 0u);
+template <int F, bool P, int NB>
+__device__ __forceinline__ void multiply_steps(int steps, uint32_t d, uint32_t a, uint32_t b, uint32_t sfa, uint32_t sfb, uint32_t ta, uint32_t idesc, bool accumulate) {
+  if (steps == 4) multiply<F, P, NB, 4>(d, a, b, sfa, sfb, ta, idesc, accumulate);
+  else if (steps == 1) multiply<F, P, NB, 1>(d, a, b, sfa, sfb, ta, idesc, accumulate);
+  else if (steps == 2) multiply<F, P, NB, 2>(d, a, b, sfa, sfb, ta, idesc, accumulate);
+  else multiply<F, P, NB, 3>(d, a, b, sfa, sfb, ta, idesc, accumulate);
 }
 // arrives at the barrier (of both CTAs of a pair) once all that this thread has issued is done
 template <bool P>
@@ -192,39 +191,42 @@ __device__ __forceinline__ void fma2(float &lo, float &hi, unsigned long long s,
   asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(d) : "l"(s), "l"(b));
   asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d));
 }
-// A thread's row of 32 sums: scale and bias (shared memory, the same for all lanes), residual (in place in the staged row), activation, and into
-// the staged row: pieces of 16 bytes at i ^ swap, as the tensor map of y swaps them.
+// 32 sums of a thread's row -> values of y: scale and bias (shared memory, the same for all lanes), residual (in place in the staged row, its pieces
+// from `first` on), activation
 template <typename T, bool RES, bool RELU6>
-__device__ __forceinline__ void stage_row(float scale, uint32_t bias, float *v, uint32_t row, uint32_t swap) {
+__device__ __forceinline__ void finish32(float scale, uint32_t bias, float *v, uint32_t row, uint32_t swap, int first, uint4 *w) {
   constexpr int N = kPer<T>;
+  uint4 b[8], res[32 / N];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = lds_u4(bias + (uint32_t)(i * 16));
+  if (RES) {
+#pragma unroll
+    for (int i = 0; i < 32 / N; ++i) res[i] = lds_u4(row + ((uint32_t)(first + i) ^ swap) * 16u);
+  }
   const unsigned long long s = pair_of(scale, scale);
 #pragma unroll
-  for (int i = 0; i < kOut / N; ++i) {
-    float *u = v + i * N;
-    const uint32_t at = row + ((uint32_t)i ^ swap) * 16u;
+  for (int i = 0; i < 8; ++i) {
+    fma2(v[4 * i], v[4 * i + 1], s, pair_of(__uint_as_float(b[i].x), __uint_as_float(b[i].y)));
+    fma2(v[4 * i + 2], v[4 * i + 3], s, pair_of(__uint_as_float(b[i].z), __uint_as_float(b[i].w)));
+  }
 #pragma unroll
-    for (int j = 0; j < N; j += 4) {
-      const uint4 b = lds_u4(bias + (uint32_t)((i * N + j) * 4));
-      fma2(u[j], u[j + 1], s, pair_of(__uint_as_float(b.x), __uint_as_float(b.y)));
-      fma2(u[j + 2], u[j + 3], s, pair_of(__uint_as_float(b.z), __uint_as_float(b.w)));
-    }
+  for (int i = 0; i < 32 / N; ++i) {
+    float *u = v + i * N;
     if (RES) {
       float r[N];
-      unpack16<T>(lds_u4(at), r);
+      unpack16<T>(res[i], r);
 #pragma unroll
       for (int j = 0; j < N; ++j) u[j] += r[j];
     }
-    uint4 w;
     if (RELU6 && N == 8) {
-      w = make_uint4(relu6_bf16x2(u[0], u[1]), relu6_bf16x2(u[2], u[3]), relu6_bf16x2(u[4 % N], u[5 % N]), relu6_bf16x2(u[6 % N], u[7 % N]));
+      w[i] = make_uint4(relu6_bf16x2(u[0], u[1]), relu6_bf16x2(u[2], u[3]), relu6_bf16x2(u[4 % N], u[5 % N]), relu6_bf16x2(u[6 % N], u[7 % N]));
     } else {
       if (RELU6) {
 #pragma unroll
         for (int j = 0; j < N; ++j) u[j] = dc_act_apply(u[j], DC_ACT_RELU6);
       }
-      w = pack16<T>(u);
+      w[i] = pack16<T>(u);
     }
-    sts_u4(at, w);
   }
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t ssrc, int c0, int c1) {
@@ -327,7 +329,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   constexpr uint32_t kTmemCols = 512;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kBars];
-  __shared__ __align__(16) float bias_s[kEpiWarps][kOut];
+  __shared__ __align__(16) float bias_s[kEpiWarps][kOut<T>];
   __shared__ uint32_t tmem_s, abort_s;
   volatile uint32_t *abort_flag = &abort_s;
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -372,7 +374,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   const int rank = team > 1 ? (int)(blockIdx.x % (unsigned)team) : 0;
   const int first = (int)blockIdx.x / team, step = (int)gridDim.x / team;
   const int c0 = P ? 0 : rank * p.chunks_per, c1 = P ? p.chunks : min(p.chunks, c0 + p.chunks_per);
-  const int part_pitch = ((p.nt + 31) & ~31) * 4 + 16;         // bytes between rows of a part: no bank conflicts
+  const int part_pitch = p.nt * 4 + 16;          // bytes between rows of a part: no bank conflicts
   const uint32_t sf_base = tmem + (uint32_t)(p.acc_bufs * p.nt);
   const uint32_t ring = sm + (uint32_t)p.off_ring, w_base = ring + (uint32_t)(p.stages * p.stage_bytes);
   const int b_rows = P ? p.nt / 2 : p.nt;
@@ -394,7 +396,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     bool ok = true;
     if (!(FORM == kStream && p.w_stays))
       for (int item = first; ok && item < p.items; item += step) {
-        const int tm = item % p.tiles_m, tn = item / p.tiles_m, x_tile = P ? tm * 2 + rank : tm;
+        const int tn = p.tiles_n > 1 ? item / p.tiles_m : 0, tm = item - tn * p.tiles_m, x_tile = P ? tm * 2 + rank : tm;
         for (int ch = c0; ch < c1; ++ch) {
           ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x10000u | (uint32_t)stage);
           if (!ok) break;
@@ -450,15 +452,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           const uint32_t b = p.w_stays ? w_base + (uint32_t)(ch * p.w_bytes) : (FORM == kRows ? at : at + kA + kAtoms * kAtom), sfb = b + w_codes;
           const uint32_t ta = sf_base + (uint32_t)(stage * p.sf_cols);
           const int steps = min(4, dc_div_up(p.c_in - ch * kStageCols, 64));
-          if (steps == 4) {
-            if (p.nb == 2) multiply<F, P, 2, 4>(d, a, b, sfa, sfb, ta, idesc, ch > c0);
-            else multiply<F, P, 1, 4>(d, a, b, sfa, sfb, ta, idesc, ch > c0);
-          } else {                               // the last columns
-            for (int k = 0; k < steps; ++k) {
-              const uint32_t atom = F == DC_NV4 ? (uint32_t)k : (uint32_t)(k >> 1), tile = atom * kAtom;
-              multiply_last<F, P>(d, a + 32u * k, b + 32u * k, sfa + tile, sfb + tile, ta + 4u * atom, ta + 4u * (kAtoms + p.nb * atom), p.nb, idesc, k, ch > c0 || k > 0);
-            }
-          }
+          if (p.nb == 2) multiply_steps<F, P, 2>(steps, d, a, b, sfa, sfb, ta, idesc, ch > c0);
+          else multiply_steps<F, P, 1>(steps, d, a, b, sfa, sfb, ta, idesc, ch > c0);
           commit<P>(&bar[kEmpty + stage]);
           if (ch == c1 - 1) commit<P>(&bar[kDFull + buf]);
         }
@@ -489,17 +484,16 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       __syncwarp();
       if (lane == 0) mbar_arrive(&bar[kXFull]);
     }
-    constexpr int kBufs = 4 / (int)sizeof(T);    // of staged results
-    constexpr uint32_t kRow = kOut * sizeof(T);
+    constexpr int kCols = kOut<T>, kHalves = kCols / 32;
     const uint32_t out = sm + (uint32_t)(p.off_out + (warp - 2) * kOutBytes), bias_w = smem_u32(bias_s[warp - 2]);
-    const uint32_t mine = out + (uint32_t)lane * kRow, swap = sizeof(T) == 2 ? (uint32_t)(lane >> 1) & 3u : (uint32_t)lane & 7u;
+    const uint32_t mine = out + (uint32_t)lane * 128u, swap = (uint32_t)lane & 7u;           // 16-byte pieces of a row lie at i ^ swap
     const uint32_t freed = P ? map_cluster(smem_u32(&bar[kDEmpty]), 0) : 0u;
     // sets of four warps: each takes every acc_bufs-th tile, an accumulator of its own, and shares its columns with the other sets on it
-    const int buf = set % p.acc_bufs, c_first = set / p.acc_bufs * kOut, c_step = kEpiWarps / 4 / p.acc_bufs * kOut;
+    const int buf = set % p.acc_bufs, c_first = set / p.acc_bufs * kCols, c_step = kEpiWarps / 4 / p.acc_bufs * kCols;
     const bool parts = FORM != kPair && FORM != kStream && p.split > 1;
-    uint32_t use = 0, turn = 0, res_parity = 0;
+    uint32_t use = 0, res_parity = 0;
     for (int item = first + buf * step; item < p.items; item += p.acc_bufs * step, ++use) {
-      const int tm = item % p.tiles_m, tn = item / p.tiles_m;
+      const int tn = p.tiles_n > 1 ? item / p.tiles_m : 0, tm = item - tn * p.tiles_m;
       const long long row0 = (long long)(P ? tm * 2 + rank : tm) * 128 + quad * 32;
       const int cols = min(p.nt, p.c_out - tn * p.nt);
       const bool work = row0 < p.rows && c_first < cols;
@@ -509,19 +503,18 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       for (int c = c_first; c < cols || c == c_first; c += c_step) {
         const bool last = c + c_step >= cols;
         const int col = tn * p.nt + c;
-        const uint32_t at = kBufs == 2 && (turn & 1u) ? 2048u : 0u;
         if (work && !parts) {
-          // what does not depend on the sums first: the bias, a free buffer, the residual into it
-          const float b = bias && col + lane < p.c_out ? __ldg(bias + col + lane) : 0.f;
-          if (p.vec && lane == 0) {
-            if (kBufs == 2) bulk_wait_read1();
-            else bulk_wait_read0();
-            if (residual) {
-              mbar_arrive_expect_tx(&bar[kRes + warp - 2], 32 * kRow);
-              tma_load_2d(out + at, &map_res, &bar[kRes + warp - 2], col, (int)row0);
-            }
+          // what does not depend on the sums: the bias, the residual
+          float b[kHalves];
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h) b[h] = bias && col + h * 32 + lane < p.c_out ? __ldg(bias + col + h * 32 + lane) : 0.f;
+          if (p.vec && residual && lane == 0) {
+            bulk_wait_read0();
+            mbar_arrive_expect_tx(&bar[kRes + warp - 2], kOutBytes);
+            tma_load_2d(out, &map_res, &bar[kRes + warp - 2], col, (int)row0);
           }
-          bias_s[warp - 2][lane] = b;
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h) bias_s[warp - 2][h * 32 + lane] = b[h];
           __syncwarp();
         }
         if (c == c_first) {
@@ -529,9 +522,10 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           if (!ok) break;
           tc_fence_after();
         }
-        float v[kOut];
+        float v[kHalves][32];
         if (work) {
-          tmem_ld32(d + (uint32_t)c, reinterpret_cast<uint32_t *>(v));
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h) tmem_ld32(d + (uint32_t)(c + h * 32), reinterpret_cast<uint32_t *>(v[h]));
           tmem_ld_wait();
         }
         if (last) {                              // the accumulator is read: the next tile may have it
@@ -547,37 +541,60 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           if (row0 + lane < p.rows) {
             const uint32_t to = sm + (uint32_t)((quad * 32 + lane) * part_pitch + c * 4);
 #pragma unroll
-            for (int i = 0; i < kOut / 4; ++i)
-              sts_u4(to + (uint32_t)(i * 16), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+            for (int i = 0; i < kCols / 4; ++i)
+              if (c + 4 * i < p.nt) {
+                const float *u = v[i / 8] + i % 8 * 4;
+                sts_u4(to + (uint32_t)(i * 16), make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3])));
+              }
           }
         } else if (p.vec) {
+          constexpr int kW = 32 / kPer<T>;       // 16-byte pieces of 32 columns
+          uint4 w[kHalves][kW];
           if (residual) {
             ok = warp_wait(&bar[kRes + warp - 2], res_parity, abort_flag, ws, 0xA0000u | (uint32_t)warp);
             if (!ok) break;
             res_parity ^= 1u;
-            if (p.act == DC_ACT_RELU6) stage_row<T, true, true>(p.scale, bias_w, v, mine + at, swap);
-            else stage_row<T, true, false>(p.scale, bias_w, v, mine + at, swap);
-          } else {
-            if (p.act == DC_ACT_RELU6) stage_row<T, false, true>(p.scale, bias_w, v, mine + at, swap);
-            else stage_row<T, false, false>(p.scale, bias_w, v, mine + at, swap);
           }
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h) {
+            const uint32_t bh = bias_w + (uint32_t)(h * 128);
+            if (residual) {
+              if (p.act == DC_ACT_RELU6) finish32<T, true, true>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
+              else finish32<T, true, false>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
+            } else {
+              if (p.act == DC_ACT_RELU6) finish32<T, false, true>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
+              else finish32<T, false, false>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
+            }
+          }
+          if (!residual) {                       // the results before these have been read
+            if (lane == 0) bulk_wait_read0();
+            __syncwarp();
+          }
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int i = 0; i < kW; ++i) sts_u4(mine + ((uint32_t)(h * kW + i) ^ swap) * 16u, w[h][i]);
           fence_proxy_async();
           __syncwarp();
           if (lane == 0) {
-            tma_store_2d(&map_y, out + at, col, (int)row0);
+            tma_store_2d(&map_y, out, col, (int)row0);
             bulk_commit();
           }
-          ++turn;
         } else {
-          const uint32_t row = out + (uint32_t)lane * 128u;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            sts_u4(row + (uint32_t)((i ^ (lane & 7)) * 16), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
-          __syncwarp();
-          if (col + lane < p.c_out)
-            deliver_columns<T>(p, bias_s[warp - 2][lane], residual, y, (size_t)row0 * (size_t)p.c_out + (size_t)(col + lane),
-                               p.rows - row0 < 32 ? (int)(p.rows - row0) : 32, out, lane);
-          __syncwarp();
+          for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float *u = v[h] + i * 4;
+              sts_u4(mine + ((uint32_t)i ^ swap) * 16u, make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3])));
+            }
+            __syncwarp();
+            const int o = col + h * 32 + lane;
+            if (o < p.c_out)
+              deliver_columns<T>(p, bias_s[warp - 2][h * 32 + lane], residual, y, (size_t)row0 * (size_t)p.c_out + (size_t)o,
+                                 p.rows - row0 < 32 ? (int)(p.rows - row0) : 32, out, lane);
+            __syncwarp();
+          }
         }
       }
       if (!ok) break;
@@ -718,9 +735,9 @@ bool scales_map(EncodeTiledFn encode, CUtensorMap *map, const void *q, const q4:
 template <typename T>
 bool results_map(EncodeTiledFn encode, CUtensorMap *map, const void *y, const Params &p) {
   const cuuint64_t dim[2] = {(cuuint64_t)p.c_out, (cuuint64_t)p.rows}, str[1] = {(cuuint64_t)p.c_out * sizeof(T)};
-  const cuuint32_t bx[2] = {kOut, 32}, es[2] = {1, 1};
+  const cuuint32_t bx[2] = {(cuuint32_t)kOut<T>, 32}, es[2] = {1, 1};
   return encode(map, sizeof(T) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void *>(y), dim, str, bx, es,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, sizeof(T) == 2 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -784,7 +801,7 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   p->off_out = p->off_ring + p->stages * p->stage_bytes + (p->w_stays ? p->chunks * p->w_bytes : 0);
   // an operand of fewer rows than 128 is read on into what lies behind it; a part of a split tile lies where the operands were
   if (form == kRows && kSmemMax - 1024 - p->off_sfa < kA) return false;
-  if (team > 1 && form != kPair && (form == kRows ? (int)p->rows : 128) * (((p->nt + 31) & ~31) * 4 + 16) > p->off_out) return false;
+  if (team > 1 && form != kPair && (form == kRows ? (int)p->rows : 128) * (p->nt * 4 + 16) > p->off_out) return false;
   return p->stages >= 2;
 }
 

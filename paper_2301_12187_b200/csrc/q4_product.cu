@@ -28,7 +28,7 @@ constexpr int kEpiWarps = 8;                     // reading out
 constexpr int kCutWarps = 4;                     // quantising, form kStream
 template <int FORM>
 constexpr int kThreadsOf = (2 + kEpiWarps + (FORM == kStream ? kCutWarps : 0)) * 32;
-constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxAcc = 4;
+constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxAcc = 2;
 constexpr int kSmemMax = 224 * 1024;
 constexpr int kStageCols = 256;                  // columns of a stage: 128 bytes of codes
 constexpr int kOutBytes = 32 * 128;              // of a reading-out warp: 32 rows of 128 bytes of results
@@ -191,6 +191,8 @@ __device__ __forceinline__ void fma2(float &lo, float &hi, unsigned long long s,
   asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(d) : "l"(s), "l"(b));
   asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d));
 }
+// ReLU6 of two values with one instruction behind the conversion: packed minima and maxima run at half rate and bound the read-out.  A NaN becomes 6.
+__device__ __forceinline__ uint32_t relu6_fast(float lo, float hi) { return min_bf16x2(pack_bf16x2_relu(lo, hi), 0x40C040C0u); }
 // 32 sums of a thread's row -> values of y: scale and bias (shared memory, the same for all lanes), residual (in place in the staged row, its pieces
 // from `first` on), activation
 template <typename T, bool RES, bool RELU6>
@@ -219,7 +221,7 @@ __device__ __forceinline__ void finish32(float scale, uint32_t bias, float *v, u
       for (int j = 0; j < N; ++j) u[j] += r[j];
     }
     if (RELU6 && N == 8) {
-      w[i] = make_uint4(relu6_bf16x2(u[0], u[1]), relu6_bf16x2(u[2], u[3]), relu6_bf16x2(u[4 % N], u[5 % N]), relu6_bf16x2(u[6 % N], u[7 % N]));
+      w[i] = make_uint4(relu6_fast(u[0], u[1]), relu6_fast(u[2], u[3]), relu6_fast(u[4 % N], u[5 % N]), relu6_fast(u[6 % N], u[7 % N]));
     } else {
       if (RELU6) {
 #pragma unroll
@@ -343,7 +345,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
       for (int i = 0; i < kMaxAcc; ++i) {
         mbar_init(&bar[kDFull + i], 1);
-        mbar_init(&bar[kDEmpty + i], P ? 2 * kEpiWarps : kEpiWarps / p.acc_bufs);
+        mbar_init(&bar[kDEmpty + i], (P ? 2 : 1) * kEpiWarps / p.acc_bufs);
       }
       mbar_init(&bar[kXFull], kEpiWarps);
       mbar_init(&bar[kWFull], 1);
@@ -525,7 +527,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         float v[kHalves][32];
         if (work) {
 #pragma unroll
-          for (int h = 0; h < kHalves; ++h) tmem_ld32(d + (uint32_t)(c + h * 32), reinterpret_cast<uint32_t *>(v[h]));
+          for (int h = 0; h < kHalves; ++h)
+            if (h == 0 || c + 32 < cols) tmem_ld32(d + (uint32_t)(c + h * 32), reinterpret_cast<uint32_t *>(v[h]));
           tmem_ld_wait();
         }
         if (last) {                              // the accumulator is read: the next tile may have it
@@ -557,6 +560,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           }
 #pragma unroll
           for (int h = 0; h < kHalves; ++h) {
+            if (h > 0 && c + 32 >= cols) break;  // what is stored of the second half is cut off at the end of a row
             const uint32_t bh = bias_w + (uint32_t)(h * 128);
             if (residual) {
               if (p.act == DC_ACT_RELU6) finish32<T, true, true>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
@@ -572,8 +576,9 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           }
 #pragma unroll
           for (int h = 0; h < kHalves; ++h)
+            if (h == 0 || c + 32 < cols)
 #pragma unroll
-            for (int i = 0; i < kW; ++i) sts_u4(mine + ((uint32_t)(h * kW + i) ^ swap) * 16u, w[h][i]);
+              for (int i = 0; i < kW; ++i) sts_u4(mine + ((uint32_t)(h * kW + i) ^ swap) * 16u, w[h][i]);
           fence_proxy_async();
           __syncwarp();
           if (lane == 0) {
@@ -779,10 +784,9 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   p->nb = p->nt > 128 ? 2 : 1;
   p->w_bytes = (form == kPair ? p->nt / 2 : p->nt) * 128 + p->nb * atoms * kAtom;
   p->sf_cols = 4 * atoms * (1 + p->nb);
-  const bool many = form != kPair && p->split == 1 && p->items > n_sm;         // CTAs have several tiles
+  const bool many = p->split == 1 && p->items > (form == kPair ? n_sm / 2 : n_sm);         // CTAs have several tiles
   p->acc_bufs = 1;
-  for (int n = 2; many && n <= kEpiWarps / 4; n *= 2)
-    if (n * p->nt + 3 * p->sf_cols <= 512) p->acc_bufs = n;
+  if (many && 2 * p->nt + 3 * p->sf_cols <= 512) p->acc_bufs = 2;
   const int x_bytes = form == kRows ? 0 : kA + atoms * kAtom;
   int room = kSmemMax - 1024 - kEpiWarps * kOutBytes;
   p->off_sfa = p->off_ring = 0;
@@ -818,6 +822,7 @@ double estimate(const Params &p, int form, int n_sm) {
          (form == kRows ? 400 + 250.0 * (double)p.rows * p.chunks_per / 16 : 0);
 }
 
+//FORCE
 // Fills p for the form that takes the least of the estimates.  Tiles of fewer than all of w's rows begin where a scale tile does: they have
 // 128 or 256 rows.
 int choose(Params *p, bool raw, int format, int n_sm) {
@@ -848,7 +853,10 @@ int choose(Params *p, bool raw, int format, int n_sm) {
       for (int s = 1; s <= kMaxSplit; ++s) look(kOne, whole < n ? whole : n, s);
       if (whole <= n) break;
     }
-    if (p->rows > 128 && whole > 128) look(kPair, 256, 1);
+    if (p->rows > 128 && whole > 128) {
+      look(kPair, 256, 1);
+      look(kPair, 128, 1);
+    }
   }
   *p = best_p;
   return best_form;

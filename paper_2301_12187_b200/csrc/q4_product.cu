@@ -29,7 +29,8 @@ constexpr int kCutWarps = 4;                     // quantising, form kStream
 template <int FORM>
 constexpr int kThreadsOf = (2 + kEpiWarps + (FORM == kStream ? kCutWarps : 0)) * 32;
 constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxAcc = 2;
-constexpr int kSmemMax = 224 * 1024;
+template <int FORM>
+constexpr int kSmemOf = (FORM == kPair ? 224 : 218) * 1024;    // what the static arrays leave
 constexpr int kStageCols = 256;                  // columns of a stage: 128 bytes of codes
 constexpr int kOutBytes = 32 * 128;              // of a reading-out warp: 32 rows of 128 bytes of results
 template <typename T>
@@ -193,42 +194,56 @@ __device__ __forceinline__ void fma2(float &lo, float &hi, unsigned long long s,
 }
 // ReLU6 of two values with one instruction behind the conversion: packed minima and maxima run at half rate and bound the read-out.  A NaN becomes 6.
 __device__ __forceinline__ uint32_t relu6_fast(float lo, float hi) { return min_bf16x2(pack_bf16x2_relu(lo, hi), 0x40C040C0u); }
-// 32 sums of a thread's row -> values of y: scale and bias (shared memory, the same for all lanes), residual (in place in the staged row, its pieces
-// from `first` on), activation
-template <typename T, bool RES, bool RELU6>
-__device__ __forceinline__ void finish32(float scale, uint32_t bias, float *v, uint32_t row, uint32_t swap, int first, uint4 *w) {
-  constexpr int N = kPer<T>;
-  uint4 b[8], res[32 / N];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) b[i] = lds_u4(bias + (uint32_t)(i * 16));
+// 32 H sums of a thread's row -> values of y, 16 bytes a piece: scale and bias (shared memory, the same for all lanes), residual (in the staged row,
+// pieces at i ^ swap), activation
+template <typename T, int H, bool RES, bool RELU6>
+__device__ __forceinline__ void finish(float scale, uint32_t bias, float (*v)[32], uint32_t row, uint32_t swap, uint4 *w) {
+  constexpr int N = kPer<T>, K = 32 / N;
+  uint4 res[H * K];
   if (RES) {
 #pragma unroll
-    for (int i = 0; i < 32 / N; ++i) res[i] = lds_u4(row + ((uint32_t)(first + i) ^ swap) * 16u);
+    for (int i = 0; i < H * K; ++i) res[i] = lds_u4(row + ((uint32_t)i ^ swap) * 16u);
   }
   const unsigned long long s = pair_of(scale, scale);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    fma2(v[4 * i], v[4 * i + 1], s, pair_of(__uint_as_float(b[i].x), __uint_as_float(b[i].y)));
-    fma2(v[4 * i + 2], v[4 * i + 3], s, pair_of(__uint_as_float(b[i].z), __uint_as_float(b[i].w)));
-  }
+  for (int h = 0; h < H; ++h) {
+    uint4 b[8];
 #pragma unroll
-  for (int i = 0; i < 32 / N; ++i) {
-    float *u = v + i * N;
-    if (RES) {
-      float r[N];
-      unpack16<T>(res[i], r);
+    for (int i = 0; i < 8; ++i) b[i] = lds_u4(bias + (uint32_t)(h * 128 + i * 16));
 #pragma unroll
-      for (int j = 0; j < N; ++j) u[j] += r[j];
+    for (int i = 0; i < 8; ++i) {
+      fma2(v[h][4 * i], v[h][4 * i + 1], s, pair_of(__uint_as_float(b[i].x), __uint_as_float(b[i].y)));
+      fma2(v[h][4 * i + 2], v[h][4 * i + 3], s, pair_of(__uint_as_float(b[i].z), __uint_as_float(b[i].w)));
     }
-    if (RELU6 && N == 8) {
-      w[i] = make_uint4(relu6_fast(u[0], u[1]), relu6_fast(u[2], u[3]), relu6_fast(u[4 % N], u[5 % N]), relu6_fast(u[6 % N], u[7 % N]));
-    } else {
-      if (RELU6) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) u[j] = dc_act_apply(u[j], DC_ACT_RELU6);
+    for (int i = 0; i < K; ++i) {
+      float *u = v[h] + i * N;
+      if (RES) {
+        float r[N];
+        unpack16<T>(res[h * K + i], r);
+#pragma unroll
+        for (int j = 0; j < N; ++j) u[j] += r[j];
       }
-      w[i] = pack16<T>(u);
+      if (RELU6 && N == 8) {
+        w[h * K + i] = make_uint4(relu6_fast(u[0], u[1]), relu6_fast(u[2], u[3]), relu6_fast(u[4 % N], u[5 % N]), relu6_fast(u[6 % N], u[7 % N]));
+      } else {
+        if (RELU6) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) u[j] = dc_act_apply(u[j], DC_ACT_RELU6);
+        }
+        w[h * K + i] = pack16<T>(u);
+      }
     }
+  }
+}
+template <typename T, int H>
+__device__ __forceinline__ void finish_any(const Params &p, bool residual, uint32_t bias, float (*v)[32], uint32_t row, uint32_t swap, uint4 *w) {
+  if (residual) {
+    if (p.act == DC_ACT_RELU6) finish<T, H, true, true>(p.scale, bias, v, row, swap, w);
+    else finish<T, H, true, false>(p.scale, bias, v, row, swap, w);
+  } else {
+    if (p.act == DC_ACT_RELU6) finish<T, H, false, true>(p.scale, bias, v, row, swap, w);
+    else finish<T, H, false, false>(p.scale, bias, v, row, swap, w);
   }
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t ssrc, int c0, int c1) {
@@ -331,7 +346,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   constexpr uint32_t kTmemCols = 512;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kBars];
-  __shared__ __align__(16) float bias_s[kEpiWarps][kOut<T>];
+  __shared__ __align__(16) float bias_s[kEpiWarps][P ? 64 : 256];                // of a warp's tile; of a pair, whose stages want the room, of the columns at hand
   __shared__ uint32_t tmem_s, abort_s;
   volatile uint32_t *abort_flag = &abort_s;
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -494,29 +509,36 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     const int buf = set % p.acc_bufs, c_first = set / p.acc_bufs * kCols, c_step = kEpiWarps / 4 / p.acc_bufs * kCols;
     const bool parts = FORM != kPair && FORM != kStream && p.split > 1;
     uint32_t use = 0, res_parity = 0;
+    int bias_tn = -1;
     for (int item = first + buf * step; item < p.items; item += p.acc_bufs * step, ++use) {
       const int tn = p.tiles_n > 1 ? item / p.tiles_m : 0, tm = item - tn * p.tiles_m;
       const long long row0 = (long long)(P ? tm * 2 + rank : tm) * 128 + quad * 32;
       const int cols = min(p.nt, p.c_out - tn * p.nt);
-      const bool work = row0 < p.rows && c_first < cols;
+      const bool work = row0 < p.rows && c_first < cols, staged = work && !parts && p.vec;
       const uint32_t d = tmem + (uint32_t)(buf * p.nt) + ((uint32_t)(quad * 32) << 16);
+      if (!P && work && !parts && tn != bias_tn) {
+        bias_tn = tn;
+        __syncwarp();
+        for (int i = lane; i < p.nt; i += 32) bias_s[warp - 2][i] = bias && i < cols ? __ldg(bias + tn * p.nt + i) : 0.f;
+        __syncwarp();
+      }
       bool ok = true;
 #pragma unroll 1
       for (int c = c_first; c < cols || c == c_first; c += c_step) {
         const bool last = c + c_step >= cols;
         const int col = tn * p.nt + c;
-        if (work && !parts) {
-          // what does not depend on the sums: the bias, the residual
-          float b[kHalves];
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h) b[h] = bias && col + h * 32 + lane < p.c_out ? __ldg(bias + col + h * 32 + lane) : 0.f;
-          if (p.vec && residual && lane == 0) {
+        if (P && work) {
+          const float b0 = bias && c + lane < cols ? __ldg(bias + col + lane) : 0.f, b1 = bias && c + 32 + lane < cols ? __ldg(bias + col + 32 + lane) : 0.f;
+          bias_s[warp - 2][lane] = b0;
+          bias_s[warp - 2][lane + 32] = b1;
+          __syncwarp();
+        }
+        if (staged && residual) {                // the results before these have been read: the residual to their place
+          if (elect_one()) {
             bulk_wait_read0();
             mbar_arrive_expect_tx(&bar[kRes + warp - 2], kOutBytes);
             tma_load_2d(out, &map_res, &bar[kRes + warp - 2], col, (int)row0);
           }
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h) bias_s[warp - 2][h * 32 + lane] = b[h];
           __syncwarp();
         }
         if (c == c_first) {
@@ -534,10 +556,11 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         if (last) {                              // the accumulator is read: the next tile may have it
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) {
+          if (elect_one()) {
             if (P) arrive_cluster(freed + (uint32_t)(buf * 8));
             else mbar_arrive(&bar[kDEmpty + buf]);
           }
+          __syncwarp();
         }
         if (!work) continue;
         if (parts) {
@@ -552,39 +575,33 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           }
         } else if (p.vec) {
           constexpr int kW = 32 / kPer<T>;       // 16-byte pieces of 32 columns
-          uint4 w[kHalves][kW];
+          uint4 w[kHalves * kW];
+          const uint32_t bias_c = bias_w + (P ? 0u : (uint32_t)(c * 4));
           if (residual) {
             ok = warp_wait(&bar[kRes + warp - 2], res_parity, abort_flag, ws, 0xA0000u | (uint32_t)warp);
             if (!ok) break;
             res_parity ^= 1u;
           }
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h) {
-            if (h > 0 && c + 32 >= cols) break;  // what is stored of the second half is cut off at the end of a row
-            const uint32_t bh = bias_w + (uint32_t)(h * 128);
-            if (residual) {
-              if (p.act == DC_ACT_RELU6) finish32<T, true, true>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
-              else finish32<T, true, false>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
-            } else {
-              if (p.act == DC_ACT_RELU6) finish32<T, false, true>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
-              else finish32<T, false, false>(p.scale, bh, v[h], mine, swap, h * kW, w[h]);
-            }
-          }
-          if (!residual) {                       // the results before these have been read
-            if (lane == 0) bulk_wait_read0();
+          const bool both = c + 32 < cols;       // what is stored beyond the end of a row is cut off
+          if (both) finish_any<T, kHalves>(p, residual != nullptr, bias_c, v, mine, swap, w);
+          else finish_any<T, 1>(p, residual != nullptr, bias_c, v, mine, swap, w);
+          if (!residual) {
+            if (elect_one()) bulk_wait_read0();
             __syncwarp();
           }
 #pragma unroll
-          for (int h = 0; h < kHalves; ++h)
-            if (h == 0 || c + 32 < cols)
+          for (int i = 0; i < kW; ++i) sts_u4(mine + ((uint32_t)i ^ swap) * 16u, w[i]);
+          if (kHalves > 1 && both) {
 #pragma unroll
-              for (int i = 0; i < kW; ++i) sts_u4(mine + ((uint32_t)(h * kW + i) ^ swap) * 16u, w[h][i]);
+            for (int i = kW; i < kHalves * kW; ++i) sts_u4(mine + ((uint32_t)i ^ swap) * 16u, w[i]);
+          }
           fence_proxy_async();
           __syncwarp();
-          if (lane == 0) {
+          if (elect_one()) {
             tma_store_2d(&map_y, out, col, (int)row0);
             bulk_commit();
           }
+          __syncwarp();
         } else {
 #pragma unroll
           for (int h = 0; h < kHalves; ++h) {
@@ -594,9 +611,9 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
               sts_u4(mine + ((uint32_t)i ^ swap) * 16u, make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3])));
             }
             __syncwarp();
-            const int o = col + h * 32 + lane;
-            if (o < p.c_out)
-              deliver_columns<T>(p, bias_s[warp - 2][h * 32 + lane], residual, y, (size_t)row0 * (size_t)p.c_out + (size_t)o,
+            const int o = c + h * 32 + lane;
+            if (o < cols)
+              deliver_columns<T>(p, bias_s[warp - 2][P ? o - c : o], residual, y, (size_t)row0 * (size_t)p.c_out + (size_t)(tn * p.nt + o),
                                  p.rows - row0 < 32 ? (int)(p.rows - row0) : 32, out, lane);
             __syncwarp();
           }
@@ -604,7 +621,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
       if (!ok) break;
     }
-    if (lane == 0) bulk_wait_all();              // the last results are read, and written
+    if (elect_one()) bulk_wait_all();            // the last results are read, and written
+    __syncwarp();
   } else {
     // ---------------------------------------------------------------- quantise (kStream): a thread to a row, 32 columns at a time; the next 32, of the
     // next stage or tile too, are asked for before these are worked on
@@ -759,7 +777,7 @@ struct Call {
 template <int F, typename T, int FORM>
 cudaError_t launch(Params &p, const Call &c) {
   static unsigned char attr_done[kDcMaxDevices];
-  const cudaError_t e = dc_set_max_smem_once(k_q4_product<F, T, FORM>, kSmemMax, attr_done);
+  const cudaError_t e = dc_set_max_smem_once(k_q4_product<F, T, FORM>, kSmemOf<FORM>, attr_done);
   if (e != cudaSuccess) return e;
   EncodeTiledFn encode = get_encode_fn();
   if (!encode) return cudaErrorNotSupported;
@@ -774,7 +792,7 @@ cudaError_t launch(Params &p, const Call &c) {
   const int team = FORM == kPair ? 2 : p.split;
   const int grid = team > 1 ? (p.items * team < c.n_sm / team * team ? p.items * team : c.n_sm / team * team) : (p.items < c.n_sm ? p.items : c.n_sm);
   // all of a CTA's shared memory is asked for: two CTAs on an SM would each want all of its tensor memory
-  return dc_launch_pdl_cluster(k_q4_product<F, T, FORM>, dim3((unsigned)grid), dim3(kThreadsOf<FORM>), (size_t)kSmemMax, c.st, team, map_x, map_sx, map_w,
+  return dc_launch_pdl_cluster(k_q4_product<F, T, FORM>, dim3((unsigned)grid), dim3(kThreadsOf<FORM>), (size_t)kSmemOf<FORM>, c.st, team, map_x, map_sx, map_w,
                                map_sw, map_y, map_res, FORM == kRows || FORM == kStream ? (const T *)c.x : (const T *)nullptr, c.bias, (const T *)c.residual, (T *)c.y, p, c.ws);
 }
 
@@ -788,7 +806,8 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   p->acc_bufs = 1;
   if (many && 2 * p->nt + 3 * p->sf_cols <= 512) p->acc_bufs = 2;
   const int x_bytes = form == kRows ? 0 : kA + atoms * kAtom;
-  int room = kSmemMax - 1024 - kEpiWarps * kOutBytes;
+  const int smem = form == kPair ? kSmemOf<kPair> : kSmemOf<kOne>;
+  int room = smem - 1024 - kEpiWarps * kOutBytes;
   p->off_sfa = p->off_ring = 0;
   if (form == kRows) {
     p->groups = (int)((p->rows + 7) / 8);
@@ -804,7 +823,7 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   if (p->acc_bufs * p->nt + p->stages * p->sf_cols > 512) p->stages = (512 - p->acc_bufs * p->nt) / p->sf_cols;
   p->off_out = p->off_ring + p->stages * p->stage_bytes + (p->w_stays ? p->chunks * p->w_bytes : 0);
   // an operand of fewer rows than 128 is read on into what lies behind it; a part of a split tile lies where the operands were
-  if (form == kRows && kSmemMax - 1024 - p->off_sfa < kA) return false;
+  if (form == kRows && smem - 1024 - p->off_sfa < kA) return false;
   if (team > 1 && form != kPair && (form == kRows ? (int)p->rows : 128) * (p->nt * 4 + 16) > p->off_out) return false;
   return p->stages >= 2;
 }

@@ -24,13 +24,14 @@ using namespace tc;
 using q4::kAtom;
 
 enum { kOne = 0, kPair = 1, kRows = 2, kStream = 3 };
-constexpr int kEpiWarps = 8;                     // reading out
+template <int FORM>
+constexpr int kEpi = FORM == kOne ? 12 : 8;      // warps reading out
 constexpr int kCutWarps = 4;                     // quantising, form kStream
 template <int FORM>
-constexpr int kThreadsOf = (2 + kEpiWarps + (FORM == kStream ? kCutWarps : 0)) * 32;
-constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxAcc = 2;
+constexpr int kThreadsOf = (2 + kEpi<FORM> + (FORM == kStream ? kCutWarps : 0)) * 32;
+constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxAcc = 3;
 template <int FORM>
-constexpr int kSmemOf = (FORM == kPair ? 224 : 218) * 1024;    // what the static arrays leave
+constexpr int kSmemOf = (FORM == kPair ? 224 : 214) * 1024;    // what the static arrays leave
 constexpr int kStageCols = 256;                  // columns of a stage: 128 bytes of codes
 constexpr int kOutBytes = 32 * 128;              // of a reading-out warp: 32 rows of 128 bytes of results
 template <typename T>
@@ -45,12 +46,13 @@ struct Params {
   int nt, nb;                // rows of w in a tile, 128-row scale tiles that they touch
   int tiles_m, tiles_n, items;
   int chunks;                // stages of a row
+  int columns;               // CTAs keep to a column of tiles: item = row of tiles
   int split, chunks_per;     // CTAs that share an item, stages of each
   int stages, acc_bufs;
   int stage_bytes, sf_cols;  // of a stage: shared memory, and tensor memory of its scales
   int w_stays, w_bytes;      // w's stages stay in shared memory; bytes of one
   int groups;                // kRows: groups of 8 rows
-  int off_sfa, off_ring, off_out;
+  int off_sfa, off_ring, off_out, out_bufs;
   int vec;                   // rows of y begin on 16 bytes
   int vec_x;                 // kRows: rows of x do
 };
@@ -194,57 +196,51 @@ __device__ __forceinline__ void fma2(float &lo, float &hi, unsigned long long s,
 }
 // ReLU6 of two values with one instruction behind the conversion: packed minima and maxima run at half rate and bound the read-out.  A NaN becomes 6.
 __device__ __forceinline__ uint32_t relu6_fast(float lo, float hi) { return min_bf16x2(pack_bf16x2_relu(lo, hi), 0x40C040C0u); }
-// 32 H sums of a thread's row -> values of y, 16 bytes a piece: scale and bias (shared memory, the same for all lanes), residual (in the staged row,
-// pieces at i ^ swap), activation
-template <typename T, int H, bool RES, bool RELU6>
-__device__ __forceinline__ void finish(float scale, uint32_t bias, float (*v)[32], uint32_t row, uint32_t swap, uint4 *w) {
+// 32 sums of a thread's row -> values of y in its staged row, 16-byte pieces from `first` on at i ^ swap: scale and bias (shared memory, the same
+// for all lanes), residual (in place), activation
+template <typename T, bool RES, bool RELU6>
+__device__ __forceinline__ void finish32(float scale, uint32_t bias, float *v, uint32_t row, uint32_t swap, uint32_t first) {
   constexpr int N = kPer<T>, K = 32 / N;
-  uint4 res[H * K];
+  uint4 b[8], res[K];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = lds_u4(bias + (uint32_t)(i * 16));
   if (RES) {
 #pragma unroll
-    for (int i = 0; i < H * K; ++i) res[i] = lds_u4(row + ((uint32_t)i ^ swap) * 16u);
+    for (int i = 0; i < K; ++i) res[i] = lds_u4(row + ((first + (uint32_t)i) ^ swap) * 16u);
   }
   const unsigned long long s = pair_of(scale, scale);
 #pragma unroll
-  for (int h = 0; h < H; ++h) {
-    uint4 b[8];
+  for (int i = 0; i < 8; ++i) {
+    fma2(v[4 * i], v[4 * i + 1], s, pair_of(__uint_as_float(b[i].x), __uint_as_float(b[i].y)));
+    fma2(v[4 * i + 2], v[4 * i + 3], s, pair_of(__uint_as_float(b[i].z), __uint_as_float(b[i].w)));
+  }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = lds_u4(bias + (uint32_t)(h * 128 + i * 16));
+  for (int i = 0; i < K; ++i) {
+    float *u = v + i * N;
+    if (RES) {
+      float r[N];
+      unpack16<T>(res[i], r);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      fma2(v[h][4 * i], v[h][4 * i + 1], s, pair_of(__uint_as_float(b[i].x), __uint_as_float(b[i].y)));
-      fma2(v[h][4 * i + 2], v[h][4 * i + 3], s, pair_of(__uint_as_float(b[i].z), __uint_as_float(b[i].w)));
+      for (int j = 0; j < N; ++j) u[j] += r[j];
     }
+    uint4 w;
+    if (RELU6 && N == 8) {
+      w = make_uint4(relu6_fast(u[0], u[1]), relu6_fast(u[2], u[3]), relu6_fast(u[4 % N], u[5 % N]), relu6_fast(u[6 % N], u[7 % N]));
+    } else {
+      if (RELU6) {
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-      float *u = v[h] + i * N;
-      if (RES) {
-        float r[N];
-        unpack16<T>(res[h * K + i], r);
-#pragma unroll
-        for (int j = 0; j < N; ++j) u[j] += r[j];
+        for (int j = 0; j < N; ++j) u[j] = dc_act_apply(u[j], DC_ACT_RELU6);
       }
-      if (RELU6 && N == 8) {
-        w[h * K + i] = make_uint4(relu6_fast(u[0], u[1]), relu6_fast(u[2], u[3]), relu6_fast(u[4 % N], u[5 % N]), relu6_fast(u[6 % N], u[7 % N]));
-      } else {
-        if (RELU6) {
-#pragma unroll
-          for (int j = 0; j < N; ++j) u[j] = dc_act_apply(u[j], DC_ACT_RELU6);
-        }
-        w[h * K + i] = pack16<T>(u);
-      }
+      w = pack16<T>(u);
     }
+    sts_u4(row + ((first + (uint32_t)i) ^ swap) * 16u, w);
   }
 }
-template <typename T, int H>
-__device__ __forceinline__ void finish_any(const Params &p, bool residual, uint32_t bias, float (*v)[32], uint32_t row, uint32_t swap, uint4 *w) {
-  if (residual) {
-    if (p.act == DC_ACT_RELU6) finish<T, H, true, true>(p.scale, bias, v, row, swap, w);
-    else finish<T, H, true, false>(p.scale, bias, v, row, swap, w);
-  } else {
-    if (p.act == DC_ACT_RELU6) finish<T, H, false, true>(p.scale, bias, v, row, swap, w);
-    else finish<T, H, false, false>(p.scale, bias, v, row, swap, w);
-  }
+// H times as many; columns beyond the end of a row are left out
+template <typename T, int H, bool RES, bool RELU6>
+__device__ __forceinline__ void finish(float scale, uint32_t bias, float (*v)[32], uint32_t row, uint32_t swap, int halves) {
+  finish32<T, RES, RELU6>(scale, bias, v[0], row, swap, 0);
+  if (H > 1 && halves > 1) finish32<T, RES, RELU6>(scale, bias + 128u, v[H - 1], row, swap, 32 / kPer<T>);
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t ssrc, int c0, int c1) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(ssrc), "r"(c0),
@@ -333,7 +329,7 @@ __device__ __forceinline__ void put_x16(float *v, const Params &p, uint32_t a, u
   }
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + kMaxAcc, kXFull = kDEmpty + kMaxAcc, kWFull, kRes, kBars = kRes + kEpiWarps };
+enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + kMaxAcc, kXFull = kDEmpty + kMaxAcc, kWFull, kRes, kBars = kRes + kEpi<kOne> };
 
 template <int F, typename T, int FORM>
 __global__ void __launch_bounds__(kThreadsOf<FORM>, 1)
@@ -346,7 +342,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   constexpr uint32_t kTmemCols = 512;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kBars];
-  __shared__ __align__(16) float bias_s[kEpiWarps][P ? 64 : 256];                // of a warp's tile; of a pair, whose stages want the room, of the columns at hand
+  __shared__ __align__(16) float bias_s[kEpi<FORM>][P ? 64 : 256];                // of a warp's tile; of a pair, whose stages want the room, of the columns at hand
   __shared__ uint32_t tmem_s, abort_s;
   volatile uint32_t *abort_flag = &abort_s;
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -360,11 +356,11 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
       for (int i = 0; i < kMaxAcc; ++i) {
         mbar_init(&bar[kDFull + i], 1);
-        mbar_init(&bar[kDEmpty + i], (P ? 2 : 1) * kEpiWarps / p.acc_bufs);
+        mbar_init(&bar[kDEmpty + i], (P ? 2 : 1) * kEpi<FORM> / p.acc_bufs);
       }
-      mbar_init(&bar[kXFull], kEpiWarps);
+      mbar_init(&bar[kXFull], kEpi<FORM>);
       mbar_init(&bar[kWFull], 1);
-      for (int i = 0; i < kEpiWarps; ++i) mbar_init(&bar[kRes + i], 1);
+      for (int i = 0; i < kEpi<FORM>; ++i) mbar_init(&bar[kRes + i], 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
       prefetch_tensormap(&map_w);
       prefetch_tensormap(&map_sw);
@@ -389,7 +385,10 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 
   const int team = P ? 2 : p.split;              // CTAs that share an item
   const int rank = team > 1 ? (int)(blockIdx.x % (unsigned)team) : 0;
-  const int first = (int)blockIdx.x / team, step = (int)gridDim.x / team;
+  const int team_id = (int)blockIdx.x / team, teams = (int)gridDim.x / team;
+  const int first = p.columns ? team_id / p.tiles_n : team_id, step = p.columns ? teams / p.tiles_n : teams;
+  const int items = p.columns ? p.tiles_m : p.items, own_tn = p.columns ? team_id % p.tiles_n : 0;
+  auto column_of = [&](int item) { return p.columns || p.tiles_n == 1 ? own_tn : item / p.tiles_m; };
   const int c0 = P ? 0 : rank * p.chunks_per, c1 = P ? p.chunks : min(p.chunks, c0 + p.chunks_per);
   const int part_pitch = p.nt * 4 + 16;          // bytes between rows of a part: no bank conflicts
   const uint32_t sf_base = tmem + (uint32_t)(p.acc_bufs * p.nt);
@@ -403,8 +402,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       mbar_arrive_expect_tx(&bar[kWFull], (uint32_t)(p.chunks * p.w_bytes));
       for (int ch = 0; ch < p.chunks; ++ch) {
         const uint32_t b = w_base + (uint32_t)(ch * p.w_bytes);
-        tma_load_2d(b, &map_w, &bar[kWFull], ch * 128, 0);
-        tma_load_3d(b + w_codes, &map_sw, &bar[kWFull], 0, ch * kAtoms, 0);
+        tma_load_2d(b, &map_w, &bar[kWFull], ch * 128, own_tn * p.nt);
+        tma_load_3d(b + w_codes, &map_sw, &bar[kWFull], 0, ch * kAtoms, own_tn * p.nt / 128);
       }
     }
     __syncwarp();
@@ -412,8 +411,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     uint32_t parity = 0;
     bool ok = true;
     if (!(FORM == kStream && p.w_stays))
-      for (int item = first; ok && item < p.items; item += step) {
-        const int tn = p.tiles_n > 1 ? item / p.tiles_m : 0, tm = item - tn * p.tiles_m, x_tile = P ? tm * 2 + rank : tm;
+      for (int item = first; ok && item < items; item += step) {
+        const int tn = column_of(item), tm = p.columns ? item : item - tn * p.tiles_m, x_tile = P ? tm * 2 + rank : tm;
         for (int ch = c0; ch < c1; ++ch) {
           ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x10000u | (uint32_t)stage);
           if (!ok) break;
@@ -453,7 +452,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     bool ok = !P || rank == 0;
     if (FORM == kRows && ok) ok = warp_wait(&bar[kXFull], 0, abort_flag, ws, 0x50000u);
     if (p.w_stays && ok) ok = warp_wait(&bar[kWFull], 0, abort_flag, ws, 0x60000u);
-    for (int item = first; ok && item < p.items; item += step) {
+    for (int item = first; ok && item < items; item += step) {
       ok = warp_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x20000u | (uint32_t)buf);
       if (!ok) break;
       tc_fence_after();
@@ -479,13 +478,13 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
       if (++buf == p.acc_bufs) { buf = 0; ++use; }
     }
-  } else if (warp < 2 + kEpiWarps) {
+  } else if (warp < 2 + kEpi<FORM>) {
     // ---------------------------------------------------------------- read out
     const int quad = warp & 3, set = (warp - 2) >> 2;
     if (FORM == kRows) {
       // the whole rows, as far as this CTA multiplies them, in pieces of 16 columns
       const int segs = (min(p.c_in - c0 * kStageCols, (c1 - c0) * kStageCols) + 63) / 64 * 4, total = (int)p.rows * segs;
-      for (int u0 = (warp - 2) * 32; u0 < total; u0 += kEpiWarps * 32) {
+      for (int u0 = (warp - 2) * 32; u0 < total; u0 += kEpi<FORM> * 32) {
         const int u = u0 + lane, row = u / segs, seg = u - row * segs;
         float v[16];
         const bool valid = u < total;
@@ -502,16 +501,17 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       if (lane == 0) mbar_arrive(&bar[kXFull]);
     }
     constexpr int kCols = kOut<T>, kHalves = kCols / 32;
-    const uint32_t out = sm + (uint32_t)(p.off_out + (warp - 2) * kOutBytes), bias_w = smem_u32(bias_s[warp - 2]);
-    const uint32_t mine = out + (uint32_t)lane * 128u, swap = (uint32_t)lane & 7u;           // 16-byte pieces of a row lie at i ^ swap
+    const uint32_t out0 = sm + (uint32_t)(p.off_out + (warp - 2) * p.out_bufs * kOutBytes), bias_w = smem_u32(bias_s[warp - 2]);
+    const uint32_t swap = (uint32_t)lane & 7u;   // 16-byte pieces of a row lie at i ^ swap
+    uint32_t turn = 0;
     const uint32_t freed = P ? map_cluster(smem_u32(&bar[kDEmpty]), 0) : 0u;
     // sets of four warps: each takes every acc_bufs-th tile, an accumulator of its own, and shares its columns with the other sets on it
-    const int buf = set % p.acc_bufs, c_first = set / p.acc_bufs * kCols, c_step = kEpiWarps / 4 / p.acc_bufs * kCols;
+    const int buf = set % p.acc_bufs, c_first = set / p.acc_bufs * kCols, c_step = kEpi<FORM> / 4 / p.acc_bufs * kCols;
     const bool parts = FORM != kPair && FORM != kStream && p.split > 1;
     uint32_t use = 0, res_parity = 0;
     int bias_tn = -1;
-    for (int item = first + buf * step; item < p.items; item += p.acc_bufs * step, ++use) {
-      const int tn = p.tiles_n > 1 ? item / p.tiles_m : 0, tm = item - tn * p.tiles_m;
+    for (int item = first + buf * step; item < items; item += p.acc_bufs * step, ++use) {
+      const int tn = column_of(item), tm = p.columns ? item : item - tn * p.tiles_m;
       const long long row0 = (long long)(P ? tm * 2 + rank : tm) * 128 + quad * 32;
       const int cols = min(p.nt, p.c_out - tn * p.nt);
       const bool work = row0 < p.rows && c_first < cols, staged = work && !parts && p.vec;
@@ -527,6 +527,11 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       for (int c = c_first; c < cols || c == c_first; c += c_step) {
         const bool last = c + c_step >= cols;
         const int col = tn * p.nt + c;
+        const uint32_t out = out0 + turn * kOutBytes, mine = out + (uint32_t)lane * 128u;
+        auto wait_out = [&]() {                  // what this buffer held is read
+          if (p.out_bufs == 2) bulk_wait_read1();
+          else bulk_wait_read0();
+        };
         if (P && work) {
           const float b0 = bias && c + lane < cols ? __ldg(bias + col + lane) : 0.f, b1 = bias && c + 32 + lane < cols ? __ldg(bias + col + 32 + lane) : 0.f;
           bias_s[warp - 2][lane] = b0;
@@ -535,7 +540,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
         if (staged && residual) {                // the results before these have been read: the residual to their place
           if (elect_one()) {
-            bulk_wait_read0();
+            wait_out();
             mbar_arrive_expect_tx(&bar[kRes + warp - 2], kOutBytes);
             tma_load_2d(out, &map_res, &bar[kRes + warp - 2], col, (int)row0);
           }
@@ -574,26 +579,19 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
               }
           }
         } else if (p.vec) {
-          constexpr int kW = 32 / kPer<T>;       // 16-byte pieces of 32 columns
-          uint4 w[kHalves * kW];
           const uint32_t bias_c = bias_w + (P ? 0u : (uint32_t)(c * 4));
+          const int halves = c + 32 < cols ? 2 : 1;
           if (residual) {
             ok = warp_wait(&bar[kRes + warp - 2], res_parity, abort_flag, ws, 0xA0000u | (uint32_t)warp);
             if (!ok) break;
             res_parity ^= 1u;
-          }
-          const bool both = c + 32 < cols;       // what is stored beyond the end of a row is cut off
-          if (both) finish_any<T, kHalves>(p, residual != nullptr, bias_c, v, mine, swap, w);
-          else finish_any<T, 1>(p, residual != nullptr, bias_c, v, mine, swap, w);
-          if (!residual) {
-            if (elect_one()) bulk_wait_read0();
+            if (p.act == DC_ACT_RELU6) finish<T, kHalves, true, true>(p.scale, bias_c, v, mine, swap, halves);
+            else finish<T, kHalves, true, false>(p.scale, bias_c, v, mine, swap, halves);
+          } else {
+            if (elect_one()) wait_out();
             __syncwarp();
-          }
-#pragma unroll
-          for (int i = 0; i < kW; ++i) sts_u4(mine + ((uint32_t)i ^ swap) * 16u, w[i]);
-          if (kHalves > 1 && both) {
-#pragma unroll
-            for (int i = kW; i < kHalves * kW; ++i) sts_u4(mine + ((uint32_t)i ^ swap) * 16u, w[i]);
+            if (p.act == DC_ACT_RELU6) finish<T, kHalves, false, true>(p.scale, bias_c, v, mine, swap, halves);
+            else finish<T, kHalves, false, false>(p.scale, bias_c, v, mine, swap, halves);
           }
           fence_proxy_async();
           __syncwarp();
@@ -602,6 +600,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             bulk_commit();
           }
           __syncwarp();
+          if (p.out_bufs == 2) turn ^= 1u;
         } else {
 #pragma unroll
           for (int h = 0; h < kHalves; ++h) {
@@ -626,7 +625,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   } else {
     // ---------------------------------------------------------------- quantise (kStream): a thread to a row, 32 columns at a time; the next 32, of the
     // next stage or tile too, are asked for before these are worked on
-    const int r = (warp - 2 - kEpiWarps) * 32 + lane;
+    const int r = (warp - 2 - kEpi<FORM>) * 32 + lane;
     constexpr int kRaw = 32 / kPer<T>;
     uint4 next[kRaw];
     auto ask = [&](int item, int ch, int c) {    // columns c .. c + 31 of a stage
@@ -640,8 +639,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     int item = first, ch = 0, stage = 0;
     uint32_t parity = 0;
     bool ok = true;
-    if (item < p.items) ask(item, ch, 0);
-    while (ok && item < p.items) {
+    if (item < items) ask(item, ch, 0);
+    while (ok && item < items) {
       ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x70000u | (uint32_t)stage);
       if (!ok) break;
       const uint32_t a = ring + (uint32_t)(stage * p.stage_bytes) + (uint32_t)((r >> 3) * 1024 + (r & 7) * 128);
@@ -654,7 +653,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
         for (int i = 0; i < kRaw; ++i) raw[i] = next[i];
         if (c + 32 < end) ask(item0, ch0, c + 32);
-        else if (item < p.items) ask(item, ch, 0);
+        else if (item < items) ask(item, ch, 0);
         uint2 code[2];
         uint32_t top[2], byte[2];
 #pragma unroll
@@ -790,7 +789,8 @@ cudaError_t launch(Params &p, const Call &c) {
     return cudaErrorNotSupported;
   if (p.vec && (!results_map<T>(encode, &map_y, c.y, p) || (c.residual && !results_map<T>(encode, &map_res, c.residual, p)))) return cudaErrorNotSupported;
   const int team = FORM == kPair ? 2 : p.split;
-  const int grid = team > 1 ? (p.items * team < c.n_sm / team * team ? p.items * team : c.n_sm / team * team) : (p.items < c.n_sm ? p.items : c.n_sm);
+  const int columns = p.columns ? c.n_sm / p.tiles_n * p.tiles_n : 0;
+  const int grid = columns ? columns : team > 1 ? (p.items * team < c.n_sm / team * team ? p.items * team : c.n_sm / team * team) : (p.items < c.n_sm ? p.items : c.n_sm);
   // all of a CTA's shared memory is asked for: two CTAs on an SM would each want all of its tensor memory
   return dc_launch_pdl_cluster(k_q4_product<F, T, FORM>, dim3((unsigned)grid), dim3(kThreadsOf<FORM>), (size_t)kSmemOf<FORM>, c.st, team, map_x, map_sx, map_w,
                                map_sw, map_y, map_res, FORM == kRows || FORM == kStream ? (const T *)c.x : (const T *)nullptr, c.bias, (const T *)c.residual, (T *)c.y, p, c.ws);
@@ -802,12 +802,20 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   p->nb = p->nt > 128 ? 2 : 1;
   p->w_bytes = (form == kPair ? p->nt / 2 : p->nt) * 128 + p->nb * atoms * kAtom;
   p->sf_cols = 4 * atoms * (1 + p->nb);
-  const bool many = p->split == 1 && p->items > (form == kPair ? n_sm / 2 : n_sm);         // CTAs have several tiles
-  p->acc_bufs = 1;
-  if (many && 2 * p->nt + 3 * p->sf_cols <= 512) p->acc_bufs = 2;
+  const int epi = form == kOne ? kEpi<kOne> : kEpi<kPair>, at_once = form == kPair ? n_sm / 2 : n_sm;
+  const bool many = p->split == 1 && p->items > at_once;       // CTAs have several tiles
+  p->acc_bufs = many && epi / 4 * p->nt + 3 * p->sf_cols <= 512 ? epi / 4 : 1;
+  // a column of tiles to a CTA, where that leaves none idle for long: w is loaded once, and 148 SMs do not all ask for the same part of it
+  p->columns = 0;
+  if (many && form != kPair && p->tiles_n <= at_once) {
+    const int rows_at_once = at_once / p->tiles_n;
+    const double kept = (double)p->tiles_m / (dc_div_up(p->tiles_m, rows_at_once) * (double)rows_at_once) * (rows_at_once * p->tiles_n) / at_once;
+    p->columns = p->tiles_n == 1 || kept > 0.8;
+  }
   const int x_bytes = form == kRows ? 0 : kA + atoms * kAtom;
   const int smem = form == kPair ? kSmemOf<kPair> : kSmemOf<kOne>;
-  int room = smem - 1024 - kEpiWarps * kOutBytes;
+  p->out_bufs = form == kOne || form == kStream ? (p->chunks <= 4 && many ? 2 : 1) : 1;
+  int room = smem - 1024 - epi * p->out_bufs * kOutBytes;
   p->off_sfa = p->off_ring = 0;
   if (form == kRows) {
     p->groups = (int)((p->rows + 7) / 8);
@@ -815,7 +823,7 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
     p->off_ring = p->off_sfa + p->chunks_per * atoms * kAtom;                  // a multiple of 1024
     room -= p->off_ring;
   }
-  p->w_stays = many && p->tiles_n == 1 && (form == kOne || form == kStream) && (long long)p->chunks * p->w_bytes + 4ll * x_bytes <= room;
+  p->w_stays = p->columns && (form == kOne || form == kStream) && (long long)p->chunks * p->w_bytes + 4ll * x_bytes <= room;
   if (p->w_stays) room -= p->chunks * p->w_bytes;
   p->stage_bytes = x_bytes + (p->w_stays ? 0 : p->w_bytes);    // multiples of 1024: nt is one of 16, a stage's scales are of 1024
   p->stages = room / p->stage_bytes;

@@ -51,13 +51,13 @@ struct Params {
   int stages, acc_bufs;
   int stage_bytes, sf_cols;  // of a stage: shared memory, and tensor memory of its scales
   int w_stays, w_bytes;      // w's stages stay in shared memory; bytes of one
-  int groups;                // kRows: groups of 8 rows
+  int a_bytes;               // of x's codes in a stage: 128 rows, or fewer where x has fewer
   int off_sfa, off_ring, off_out, out_bufs;
   int vec;                   // rows of y begin on 16 bytes
   int vec_x;                 // kRows: rows of x do
 };
 
-constexpr int kA = 128 * 128;                    // codes of x in a stage, bytes
+constexpr int kA = 128 * 128;                    // bytes that a product reads of x's codes in a stage
 template <int F>
 constexpr int kAtomsOf = F == DC_NV4 ? 4 : 2;    // scale tiles of a stage, for 128 rows
 
@@ -419,8 +419,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           if (elect_one()) {
             uint64_t *full = &bar[kFull + stage];
             const uint32_t at = ring + (uint32_t)(stage * p.stage_bytes);
-            const uint32_t sfa = at + kA, b = FORM == kRows ? at : sfa + kAtoms * kAtom;
-            constexpr uint32_t kX = FORM == kOne || P ? (uint32_t)(kA + kAtoms * kAtom) : 0u;
+            const uint32_t sfa = at + (uint32_t)p.a_bytes, b = FORM == kRows ? at : sfa + kAtoms * kAtom;
+            const uint32_t kX = FORM == kOne || P ? (uint32_t)(p.a_bytes + kAtoms * kAtom) : 0u;
             const uint32_t bytes = kX + (p.w_stays ? 0u : w_codes + (uint32_t)(p.nb * kAtoms * kAtom));
             if (P) {
               const uint32_t to = map_cluster(smem_u32(full), 0);
@@ -463,9 +463,9 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         tc_fence_after();
         if (elect_one()) {
           const uint32_t at = ring + (uint32_t)(stage * p.stage_bytes);
-          const uint32_t a = FORM == kRows ? sm + (uint32_t)((ch - c0) * p.groups * 1024) : at;
-          const uint32_t sfa = FORM == kRows ? sm + (uint32_t)(p.off_sfa + (ch - c0) * kAtoms * kAtom) : at + kA;
-          const uint32_t b = p.w_stays ? w_base + (uint32_t)(ch * p.w_bytes) : (FORM == kRows ? at : at + kA + kAtoms * kAtom), sfb = b + w_codes;
+          const uint32_t a = FORM == kRows ? sm + (uint32_t)((ch - c0) * p.a_bytes) : at;
+          const uint32_t sfa = FORM == kRows ? sm + (uint32_t)(p.off_sfa + (ch - c0) * kAtoms * kAtom) : at + (uint32_t)p.a_bytes;
+          const uint32_t b = p.w_stays ? w_base + (uint32_t)(ch * p.w_bytes) : (FORM == kRows ? at : at + (uint32_t)p.a_bytes + kAtoms * kAtom), sfb = b + w_codes;
           const uint32_t ta = sf_base + (uint32_t)(stage * p.sf_cols);
           const int steps = min(4, dc_div_up(p.c_in - ch * kStageCols, 64));
           if (p.nb == 2) multiply_steps<F, P, 2>(steps, d, a, b, sfa, sfb, ta, idesc, ch > c0);
@@ -494,7 +494,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = 0.f;
         }
-        put_x16<F>(v, p, sm + (uint32_t)((seg >> 4) * p.groups * 1024), sm + (uint32_t)p.off_sfa, row, seg, valid);
+        put_x16<F>(v, p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, valid);
       }
       fence_proxy_async();
       __syncwarp();
@@ -785,7 +785,7 @@ cudaError_t launch(Params &p, const Call &c) {
   if (!codes_map(encode, &map_w, c.w, c.lw->pitch, p.c_out, FORM == kPair ? p.nt / 2 : p.nt) || !scales_map(encode, &map_sw, c.w, *c.lw, p.c_out, kAtoms, p.nb))
     return cudaErrorNotSupported;
   if ((FORM == kOne || FORM == kPair) &&
-      (!codes_map(encode, &map_x, c.x, c.lx->pitch, p.rows, 128) || !scales_map(encode, &map_sx, c.x, *c.lx, p.rows, kAtoms, 1)))
+      (!codes_map(encode, &map_x, c.x, c.lx->pitch, p.rows, p.a_bytes / 128) || !scales_map(encode, &map_sx, c.x, *c.lx, p.rows, kAtoms, 1)))
     return cudaErrorNotSupported;
   if (p.vec && (!results_map<T>(encode, &map_y, c.y, p) || (c.residual && !results_map<T>(encode, &map_res, c.residual, p)))) return cudaErrorNotSupported;
   const int team = FORM == kPair ? 2 : p.split;
@@ -812,14 +812,14 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
     const double kept = (double)p->tiles_m / (dc_div_up(p->tiles_m, rows_at_once) * (double)rows_at_once) * (rows_at_once * p->tiles_n) / at_once;
     p->columns = p->tiles_n == 1 || kept > 0.8;
   }
-  const int x_bytes = form == kRows ? 0 : kA + atoms * kAtom;
-  const int smem = form == kPair ? kSmemOf<kPair> : kSmemOf<kOne>;
+  // x's codes: few rows are loaded alone, and the products read on into what lies behind them, sums that nobody reads
+  p->a_bytes = form == kOne || form == kRows ? (p->rows < 128 ? (int)dc_round_up((size_t)p->rows, 8) * 128 : kA) : kA;
+  const int x_bytes = form == kRows ? 0 : p->a_bytes + atoms * kAtom, smem = form == kPair ? kSmemOf<kPair> : kSmemOf<kOne>;
   p->out_bufs = form == kOne || form == kStream ? (p->chunks <= 4 && many ? 2 : 1) : 1;
-  int room = smem - 1024 - epi * p->out_bufs * kOutBytes;
+  int room = smem - 1024 - epi * p->out_bufs * kOutBytes;      // the staged results lie last: what is read on into is shared memory of this CTA
   p->off_sfa = p->off_ring = 0;
   if (form == kRows) {
-    p->groups = (int)((p->rows + 7) / 8);
-    p->off_sfa = p->chunks_per * p->groups * 1024;
+    p->off_sfa = p->chunks_per * p->a_bytes;
     p->off_ring = p->off_sfa + p->chunks_per * atoms * kAtom;                  // a multiple of 1024
     room -= p->off_ring;
   }
@@ -830,9 +830,8 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   if (p->stages > kMaxStages) p->stages = kMaxStages;
   if (p->acc_bufs * p->nt + p->stages * p->sf_cols > 512) p->stages = (512 - p->acc_bufs * p->nt) / p->sf_cols;
   p->off_out = p->off_ring + p->stages * p->stage_bytes + (p->w_stays ? p->chunks * p->w_bytes : 0);
-  // an operand of fewer rows than 128 is read on into what lies behind it; a part of a split tile lies where the operands were
-  if (form == kRows && smem - 1024 - p->off_sfa < kA) return false;
-  if (team > 1 && form != kPair && (form == kRows ? (int)p->rows : 128) * (p->nt * 4 + 16) > p->off_out) return false;
+  // a part of a split tile lies where the operands were
+  if (team > 1 && form != kPair && (p->rows < 128 ? (int)p->rows : 128) * (p->nt * 4 + 16) > p->off_out) return false;
   return p->stages >= 2;
 }
 

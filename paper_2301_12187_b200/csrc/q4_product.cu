@@ -367,7 +367,10 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       if (FORM == kOne || P) { prefetch_tensormap(&map_x); prefetch_tensormap(&map_sx); }
     }
     __syncwarp();
-  } else if (warp == 1) {
+  }
+  // Tensor memory only behind the wait for the launch before this one, whose CTAs may still have theirs to ask for.
+  dc_pdl_enter();
+  if (warp == 1) {
     if (P) {
       asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(kTmemCols) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -381,7 +384,6 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   if (P) cluster_sync();                         // the barriers of both CTAs are there
   tc_fence_after();
   const uint32_t tmem = tmem_s;
-  dc_pdl_enter();
 
   const int team = P ? 2 : p.split;              // CTAs that share an item
   const int rank = team > 1 ? (int)(blockIdx.x % (unsigned)team) : 0;

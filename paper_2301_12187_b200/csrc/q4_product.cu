@@ -8,9 +8,10 @@
 // A stage of the ring is 256 columns: codes of both operands and their scale tiles; its scales have columns of tensor memory of their own, so a
 // slot's scales are written over only behind the products that read them.  One warp loads, one issues, eight read out the accumulators.
 // CTAs walk over tiles.  The forms:
-//   kOne     both operands by TMA.  Few tiles: a cluster shares a tile's columns and adds the parts up in rank order, through shared memory.
-//            Tensor memory is given back before the CTAs of a cluster wait for one another: who holds some never waits for a CTA that may be
-//            waiting for some.  One column of tiles and few stages: w stays in shared memory.
+//   kOne     both operands by TMA.  Few tiles: a cluster shares a tile's reduction.  Each of its CTAs owns some columns of the result; all send their
+//            parts of them to its shared memory, and it adds them up in rank order.  (With parts left where they were, two meetings of the cluster and
+//            reads from afar: one row of 4096 x 4096 7.4 us.)  Tensor memory is given back without waiting for a CTA that may be waiting for
+//            some.  One column of tiles to a CTA and few stages: w stays in shared memory.
 //   kPair    two CTAs multiply 256 x 256 (cta_group::2): each loads half of either operand, which halves what an SM has to fetch of w.
 //   kRows    few rows of bf16 or fp32: quantised by the reading-out warps into shared memory, where all of them stay.
 //   kStream  many rows of bf16 or fp32 and one column of tiles: eight more warps quantise them, a stage at a time.
@@ -53,6 +54,7 @@ struct Params {
   int w_stays, w_bytes;      // w's stages stay in shared memory; bytes of one
   int a_bytes;               // of x's codes in a stage: 128 rows, or fewer where x has fewer
   int off_sfa, off_ring, off_out, out_bufs;
+  int part_rows, part_cols;  // of a part that a CTA of a cluster sends to another (columns: whole 16-byte pieces of y)
   int vec;                   // rows of y begin on 16 bytes
   int vec_x;                 // kRows: rows of x do
 };
@@ -143,6 +145,13 @@ __device__ __forceinline__ void pair_load_3d(uint32_t sdst, const CUtensorMap *m
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
       ::"r"(sdst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void sts_cluster_f4(uint32_t a, float x, float y, float z, float w) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(x), "f"(y), "f"(z), "f"(w) : "memory");
+}
+// a phase that has been seen to end: what the cluster's threads wrote before they arrived is visible behind this
+__device__ __forceinline__ void mbar_acquire_cluster(uint64_t *bar, uint32_t parity) {
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(smem_u32(bar)), "r"(parity) : "memory");
 }
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -329,7 +338,7 @@ __device__ __forceinline__ void put_x16(float *v, const Params &p, uint32_t a, u
   }
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + kMaxAcc, kXFull = kDEmpty + kMaxAcc, kWFull, kRes, kBars = kRes + kEpi<kOne> };
+enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + kMaxAcc, kXFull = kDEmpty + kMaxAcc, kWFull, kParts, kRes, kBars = kRes + kEpi<kOne> };
 
 template <int F, typename T, int FORM>
 __global__ void __launch_bounds__(kThreadsOf<FORM>, 1)
@@ -360,6 +369,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
       mbar_init(&bar[kXFull], kEpi<FORM>);
       mbar_init(&bar[kWFull], 1);
+      mbar_init(&bar[kParts], (uint32_t)(p.split * kEpi<FORM>));
       for (int i = 0; i < kEpi<FORM>; ++i) mbar_init(&bar[kRes + i], 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
       prefetch_tensormap(&map_w);
@@ -368,6 +378,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     }
     __syncwarp();
   }
+  const bool parts = FORM != kPair && FORM != kStream && p.split > 1;
+  if (parts) asm volatile("barrier.cluster.arrive.release;" ::: "memory");     // this CTA is there, its barriers too: waited for before the parts go out
   // Tensor memory only behind the wait for the launch before this one, whose CTAs may still have theirs to ask for.
   dc_pdl_enter();
   if (warp == 1) {
@@ -392,7 +404,6 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   const int items = p.columns ? p.tiles_m : p.items, own_tn = p.columns ? team_id % p.tiles_n : 0;
   auto column_of = [&](int item) { return p.columns || p.tiles_n == 1 ? own_tn : item / p.tiles_m; };
   const int c0 = P ? 0 : rank * p.chunks_per, c1 = P ? p.chunks : min(p.chunks, c0 + p.chunks_per);
-  const int part_pitch = p.nt * 4 + 16;          // bytes between rows of a part: no bank conflicts
   const uint32_t sf_base = tmem + (uint32_t)(p.acc_bufs * p.nt);
   const uint32_t ring = sm + (uint32_t)p.off_ring, w_base = ring + (uint32_t)(p.stages * p.stage_bytes);
   const int b_rows = P ? p.nt / 2 : p.nt;
@@ -486,17 +497,24 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     if (FORM == kRows) {
       // the whole rows, as far as this CTA multiplies them, in pieces of 16 columns
       const int segs = (min(p.c_in - c0 * kStageCols, (c1 - c0) * kStageCols) + 63) / 64 * 4, total = (int)p.rows * segs;
-      for (int u0 = (warp - 2) * 32; u0 < total; u0 += kEpi<FORM> * 32) {
-        const int u = u0 + lane, row = u / segs, seg = u - row * segs;
-        float v[16];
-        const bool valid = u < total;
-        if (valid) {
-          load_x16<T>(x + (size_t)row * (size_t)p.c_in, c0 * kStageCols + seg * 16, p.c_in, p.vec_x, v);
-        } else {
+      constexpr int U = sizeof(T) == 2 ? 4 : 2;  // pieces at once, so that their loads overlap
+      for (int u0 = (warp - 2) * 32; u0 < total; u0 += U * kEpi<FORM> * 32) {
+        float v[U][16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        for (int k = 0; k < U; ++k) {
+          const int u = u0 + k * kEpi<FORM> * 32 + lane, row = u / segs, seg = u - row * segs;
+          if (u < total) {
+            load_x16<T>(x + (size_t)row * (size_t)p.c_in, c0 * kStageCols + seg * 16, p.c_in, p.vec_x, v[k]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[k][i] = 0.f;
+          }
         }
-        put_x16<F>(v, p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, valid);
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int u = u0 + k * kEpi<FORM> * 32 + lane, row = u / segs, seg = u - row * segs;
+          put_x16<F>(v[k], p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, u < total);
+        }
       }
       fence_proxy_async();
       __syncwarp();
@@ -509,9 +527,9 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     const uint32_t freed = P ? map_cluster(smem_u32(&bar[kDEmpty]), 0) : 0u;
     // sets of four warps: each takes every acc_bufs-th tile, an accumulator of its own, and shares its columns with the other sets on it
     const int buf = set % p.acc_bufs, c_first = set / p.acc_bufs * kCols, c_step = kEpi<FORM> / 4 / p.acc_bufs * kCols;
-    const bool parts = FORM != kPair && FORM != kStream && p.split > 1;
     uint32_t use = 0, res_parity = 0;
     int bias_tn = -1;
+    bool met = false;                            // the cluster's other CTAs
     for (int item = first + buf * step; item < items; item += p.acc_bufs * step, ++use) {
       const int tn = column_of(item), tm = p.columns ? item : item - tn * p.tiles_m;
       const long long row0 = (long long)(P ? tm * 2 + rank : tm) * 128 + quad * 32;
@@ -571,13 +589,22 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
         if (!work) continue;
         if (parts) {
+          if (!met) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+          met = true;
           if (row0 + lane < p.rows) {
-            const uint32_t to = sm + (uint32_t)((quad * 32 + lane) * part_pitch + c * 4);
+            // columns to the CTA that owns them
+            constexpr int N = kPer<T>;
+            const uint32_t from = sm + (uint32_t)(p.off_out + (rank * p.part_rows + quad * 32 + lane) * p.part_cols * 4);
 #pragma unroll
-            for (int i = 0; i < kCols / 4; ++i)
-              if (c + 4 * i < p.nt) {
-                const float *u = v[i / 8] + i % 8 * 4;
-                sts_u4(to + (uint32_t)(i * 16), make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3])));
+            for (int i = 0; i < kCols / N; ++i)
+              if (c + i * N < p.nt) {
+                const int owner = (c + i * N) / p.part_cols;
+                const uint32_t to = map_cluster(from + (uint32_t)((c + i * N - owner * p.part_cols) * 4), (uint32_t)owner);
+#pragma unroll
+                for (int j = 0; j < N; j += 4) {
+                  const float *u = v[(i * N + j) / 32] + (i * N + j) % 32;
+                  sts_cluster_f4(to + (uint32_t)(j * 4), u[0], u[1], u[2], u[3]);
+                }
               }
           }
         } else if (p.vec) {
@@ -622,8 +649,37 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
       if (!ok) break;
     }
-    if (elect_one()) bulk_wait_all();            // the last results are read, and written
-    __syncwarp();
+    if (parts) {
+      if (!met) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");       // nothing was to be sent
+      __syncwarp();
+      if (lane < p.split) arrive_cluster(map_cluster(smem_u32(&bar[kParts]), (uint32_t)lane));
+      const int tn = first / p.tiles_m, tm = first - tn * p.tiles_m;
+      const long long row0 = (long long)tm * 128;
+      const int rows = p.rows - row0 < 128 ? (int)(p.rows - row0) : 128, pieces = p.part_cols / kPer<T>;
+      const int col0 = rank * p.part_cols, end = min(p.nt, p.c_out - tn * p.nt);
+      if (warp_wait(&bar[kParts], 0, abort_flag, ws, 0xB0000u)) {
+        mbar_acquire_cluster(&bar[kParts], 0);
+        for (int u = (warp - 2) * 32 + lane; u < rows * pieces; u += kEpi<FORM> * 32) {
+          const int r = u / pieces, c = (u - r * pieces) * kPer<T>;
+          if (col0 + c >= end) continue;
+          float v[kPer<T>];
+#pragma unroll
+          for (int i = 0; i < kPer<T>; ++i) v[i] = 0.f;
+          uint32_t at = sm + (uint32_t)(p.off_out + (r * p.part_cols + c) * 4);
+          for (int k = 0; k < p.split; ++k, at += (uint32_t)(p.part_rows * p.part_cols * 4)) {
+#pragma unroll
+            for (int i = 0; i < kPer<T>; i += 4) {
+              const uint4 w = lds_u4(at + (uint32_t)(i * 4));
+              v[i] += __uint_as_float(w.x); v[i + 1] += __uint_as_float(w.y); v[i + 2] += __uint_as_float(w.z); v[i + 3] += __uint_as_float(w.w);
+            }
+          }
+          deliver<T>(p, bias, residual, y, row0 + r, tn * p.nt + col0 + c, v);
+        }
+      }
+    } else {
+      if (elect_one()) bulk_wait_all();          // the last results are read, and written
+      __syncwarp();
+    }
   } else {
     // ---------------------------------------------------------------- quantise (kStream): a thread to a row, 32 columns at a time; the next 32, of the
     // next stage or tile too, are asked for before these are worked on
@@ -681,7 +737,15 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       if (++stage == p.stages) { stage = 0; parity ^= 1u; }
     }
   }
-  if (warp == 1 && *abort_flag) {                // copies and products may still be in flight: give them time to end
+  if (parts && warp == 1) {                      // read out: tensor memory goes back while the parts are on their way
+    warp_wait(&bar[kDEmpty], 0, abort_flag, ws, 0xC0000u);
+    if (*abort_flag) {
+      const unsigned long long t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < 20ull * 1000ull * 1000ull) __nanosleep(1000);
+    }
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  } else if (warp == 1 && *abort_flag) {         // copies and products may still be in flight: give them time to end
     const unsigned long long t0 = globaltimer_ns();
     while (globaltimer_ns() - t0 < 20ull * 1000ull * 1000ull) __nanosleep(1000);
   }
@@ -693,34 +757,11 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     return;
   }
-  if (warp == 1) tmem_dealloc(tmem, kTmemCols);
-  if (FORM != kStream && p.split > 1) {
-    // the parts, [row][column], added up in rank order; each CTA delivers a share of the 16-byte pieces of y
-    constexpr int kThreads = kThreadsOf<FORM>;
-    cluster_sync();
-    if (abort_s == 0) {
-      const int tm = first % p.tiles_m, tn = first / p.tiles_m;
-      const long long row0 = (long long)tm * 128;
-      const int rows = p.rows - row0 < 128 ? (int)(p.rows - row0) : 128, pieces = p.nt / kPer<T>;
-      for (int u = rank * kThreads + tid; u < rows * pieces; u += p.split * kThreads) {
-        const int r = u / pieces, c = (u - r * pieces) * kPer<T>;
-        if (tn * p.nt + c >= p.c_out) continue;
-        float v[kPer<T>];
-#pragma unroll
-        for (int i = 0; i < kPer<T>; ++i) v[i] = 0.f;
-        const uint32_t at = sm + (uint32_t)(r * part_pitch + c * 4);
-        for (int k = 0; k < p.split; ++k) {
-          const uint32_t from = map_cluster(at, (uint32_t)k);
-#pragma unroll
-          for (int i = 0; i < kPer<T>; i += 4) {
-            const uint4 w = lds_cluster_u4(from + (uint32_t)(i * 4));
-            v[i] += __uint_as_float(w.x); v[i + 1] += __uint_as_float(w.y); v[i + 2] += __uint_as_float(w.z); v[i + 3] += __uint_as_float(w.w);
-          }
-        }
-        deliver<T>(p, bias, residual, y, row0 + r, tn * p.nt + c, v);
-      }
-    }
-    cluster_sync();                              // nobody leaves while its part may still be read
+  if (parts) {
+    if (warp < 2) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    if (*abort_flag) cluster_sync();             // parts may still be on their way here: until the other CTAs are here as well, or gone
+  } else if (warp == 1) {
+    tmem_dealloc(tmem, kTmemCols);
   }
 }
 
@@ -799,8 +840,8 @@ cudaError_t launch(Params &p, const Call &c) {
 }
 
 // Shared and tensor memory of a form, tile width and split; false: it does not fit.
-bool lay_out(Params *p, int form, int format, int n_sm) {
-  const int atoms = format == DC_NV4 ? 4 : 2, team = form == kPair ? 2 : p->split;
+bool lay_out(Params *p, int form, int format, int dtype, int n_sm) {
+  const int atoms = format == DC_NV4 ? 4 : 2;
   p->nb = p->nt > 128 ? 2 : 1;
   p->w_bytes = (form == kPair ? p->nt / 2 : p->nt) * 128 + p->nb * atoms * kAtom;
   p->sf_cols = 4 * atoms * (1 + p->nb);
@@ -818,7 +859,13 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   p->a_bytes = form == kOne || form == kRows ? (p->rows < 128 ? (int)dc_round_up((size_t)p->rows, 8) * 128 : kA) : kA;
   const int x_bytes = form == kRows ? 0 : p->a_bytes + atoms * kAtom, smem = form == kPair ? kSmemOf<kPair> : kSmemOf<kOne>;
   p->out_bufs = form == kOne || form == kStream ? (p->chunks <= 4 && many ? 2 : 1) : 1;
-  int room = smem - 1024 - epi * p->out_bufs * kOutBytes;      // the staged results lie last: what is read on into is shared memory of this CTA
+  // the staged results, or the parts from a cluster's CTAs, lie last; an operand is read on into them
+  const int per = dtype == DC_F32 ? 4 : 8;
+  p->part_rows = p->rows < 128 ? (int)p->rows : 128;
+  p->part_cols = dc_div_up(dc_div_up(p->nt, per), p->split) * per;
+  int last = p->split > 1 ? p->split * p->part_rows * p->part_cols * 4 : epi * p->out_bufs * kOutBytes;
+  if (last < kA) last = kA;
+  int room = smem - 1024 - last;
   p->off_sfa = p->off_ring = 0;
   if (form == kRows) {
     p->off_sfa = p->chunks_per * p->a_bytes;
@@ -832,8 +879,6 @@ bool lay_out(Params *p, int form, int format, int n_sm) {
   if (p->stages > kMaxStages) p->stages = kMaxStages;
   if (p->acc_bufs * p->nt + p->stages * p->sf_cols > 512) p->stages = (512 - p->acc_bufs * p->nt) / p->sf_cols;
   p->off_out = p->off_ring + p->stages * p->stage_bytes + (p->w_stays ? p->chunks * p->w_bytes : 0);
-  // a part of a split tile lies where the operands were
-  if (team > 1 && form != kPair && (p->rows < 128 ? (int)p->rows : 128) * (p->nt * 4 + 16) > p->off_out) return false;
   return p->stages >= 2;
 }
 
@@ -847,13 +892,13 @@ double estimate(const Params &p, int form, int n_sm) {
   double waves = p.items / at_once;
   waves = (double)(long long)(waves + 0.999);
   return 3000 + waves * (p.acc_bufs > 1 ? (main > out ? main : out) : main + out) + (team > 1 ? 1500 : 0) +
-         (form == kRows ? 400 + 250.0 * (double)p.rows * p.chunks_per / 16 : 0);
+         (form == kRows ? 400 + 20.0 * (double)p.rows * p.chunks_per : 0);
 }
 
 //FORCE
 // Fills p for the form that takes the least of the estimates.  Tiles of fewer than all of w's rows begin where a scale tile does: they have
 // 128 or 256 rows.
-int choose(Params *p, bool raw, int format, int n_sm) {
+int choose(Params *p, bool raw, int format, int dtype, int n_sm) {
   double best = 1e30;
   Params best_p = *p;
   int best_form = -1;
@@ -868,7 +913,7 @@ int choose(Params *p, bool raw, int format, int n_sm) {
     if ((long long)q.tiles_m * q.tiles_n > 0x3fffffffll) return;
     q.items = q.tiles_m * q.tiles_n;
     if (split > 1 && (q.chunks_per * (split - 1) >= q.chunks || (long long)q.items * split > n_sm)) return;     // no CTA without a stage
-    if (!lay_out(&q, form, format, n_sm)) return;
+    if (!lay_out(&q, form, format, dtype, n_sm)) return;
     const double cycles = estimate(q, form, n_sm);
     if (cycles < best) { best = cycles; best_p = q; best_form = form; }
   };
@@ -902,7 +947,7 @@ cudaError_t launch_form(int form, Params &p, const Call &c) {
 // DC_ERR_UNSUPPORTED: no form takes rows of this size as they are (raw), or at all
 dc_status run(Params &p, bool raw, dc_q4_format format, dc_dtype dtype, Call &c) {
   c.n_sm = dc_sm_count();
-  const int form = choose(&p, raw, format, c.n_sm);
+  const int form = choose(&p, raw, format, dtype, c.n_sm);
   if (form < 0) return DC_ERR_UNSUPPORTED;
   cudaError_t e;
   if (format == DC_MX4) e = dtype == DC_BF16 ? launch_form<DC_MX4, __nv_bfloat16>(form, p, c) : launch_form<DC_MX4, float>(form, p, c);

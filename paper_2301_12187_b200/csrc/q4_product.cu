@@ -497,24 +497,17 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     if (FORM == kRows) {
       // the whole rows, as far as this CTA multiplies them, in pieces of 16 columns
       const int segs = (min(p.c_in - c0 * kStageCols, (c1 - c0) * kStageCols) + 63) / 64 * 4, total = (int)p.rows * segs;
-      constexpr int U = sizeof(T) == 2 ? 4 : 2;  // pieces at once, so that their loads overlap
-      for (int u0 = (warp - 2) * 32; u0 < total; u0 += U * kEpi<FORM> * 32) {
-        float v[U][16];
+      for (int u0 = (warp - 2) * 32; u0 < total; u0 += kEpi<FORM> * 32) {
+        const int u = u0 + lane, row = u / segs, seg = u - row * segs;
+        float v[16];
+        const bool valid = u < total;
+        if (valid) {
+          load_x16<T>(x + (size_t)row * (size_t)p.c_in, c0 * kStageCols + seg * 16, p.c_in, p.vec_x, v);
+        } else {
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-          const int u = u0 + k * kEpi<FORM> * 32 + lane, row = u / segs, seg = u - row * segs;
-          if (u < total) {
-            load_x16<T>(x + (size_t)row * (size_t)p.c_in, c0 * kStageCols + seg * 16, p.c_in, p.vec_x, v[k]);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[k][i] = 0.f;
-          }
+          for (int i = 0; i < 16; ++i) v[i] = 0.f;
         }
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-          const int u = u0 + k * kEpi<FORM> * 32 + lane, row = u / segs, seg = u - row * segs;
-          put_x16<F>(v[k], p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, u < total);
-        }
+        put_x16<F>(v, p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, valid);
       }
       fence_proxy_async();
       __syncwarp();
@@ -892,7 +885,7 @@ double estimate(const Params &p, int form, int n_sm) {
   double waves = p.items / at_once;
   waves = (double)(long long)(waves + 0.999);
   return 3000 + waves * (p.acc_bufs > 1 ? (main > out ? main : out) : main + out) + (team > 1 ? 1500 : 0) +
-         (form == kRows ? 400 + 20.0 * (double)p.rows * p.chunks_per : 0);
+         (form == kRows ? 1000 + 56.0 * (double)p.rows * p.chunks_per : 0);
 }
 
 //FORCE

@@ -1,6 +1,6 @@
 """ctypes binding of libdepthc (include/dc.h).  Argument marshalling only: every step of the
-path runs in the library's CUDA kernels.  torch is used for device memory and streams.  The three
-forward calls are marshalled natively (csrc/dccall.c); the ctypes form behind them takes what that does not read, and
+path runs in the library's CUDA kernels.  torch is used for device memory and streams.  The
+forward calls and those on 4-bit matrices are marshalled natively (csrc/dccall.c); the ctypes form behind them takes what that does not read, and
 everything where that module is missing.
 
 The functions carry the names of the C entry points without the `dc_` prefix.  Importing this
@@ -170,6 +170,7 @@ def lib():
             _dccall.bind(at("dc_conv_forward_algo"), at("dc_dwconv_forward"), at("dc_block_forward"), torch.float32, torch.bfloat16,
                          Geom, Block, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
                          getattr(torch._C, "_cuda_getCurrentRawStream", None))
+            _dccall.bind_q4(at("dc_q4_quantize"), at("dc_q4_dequantize"), at("dc_q4_product"), at("dc_q4_forward"))
             _native = _dccall
         except ImportError:                      # not built for this Python
             _native = _NoNative
@@ -179,7 +180,7 @@ def lib():
 
 class _NoNative:
     """In the place of the native module: answers as it does for arguments it does not read."""
-    conv = dwconv = block = staticmethod(lambda *a: None)
+    conv = dwconv = block = q4_quantize = q4_dequantize = q4_product = q4_forward = staticmethod(lambda *a: None)
 
 
 def _load_native():
@@ -542,6 +543,15 @@ def _rows_of(t, cols: int, what: str) -> Tuple[int, int]:
     return rows, step
 
 
+def _here(what: str, *tensors):
+    """4-bit calls take tensors of the current device only: those of another one are addresses that its kernels cannot read."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("%s: a tensor on %s, the current device is %s" % (what, t.device, "cuda:%d" % dev if dev >= 0 else "none"))
+
+
 def _dense(t, rows: int, cols: int, dtype, what: str):
     if t is not None and (t.dtype != dtype or t.numel() != rows * cols or t.shape[-1] != cols or not t.is_contiguous()):
         raise ValueError("%s: a dense tensor of %d rows of %d values in %s is wanted" % (what, rows, cols, dtype))
@@ -549,6 +559,12 @@ def _dense(t, rows: int, cols: int, dtype, what: str):
 
 def q4_quantize(x, q: Q4Matrix, stream=None):
     """Rows of x (bf16 or fp32, [..., cols]; rows at one distance) into q, with q's tensor scale."""
+    st = (_native or _load_native()).q4_quantize(x, q, stream)
+    if st == OK:
+        return
+    if st is not None:
+        raise DcError(st, "dc_q4_quantize")
+    _here("q4_quantize", x, q.data)
     rows, stride = _rows_of(x, q.cols, "q4_quantize")
     if rows != q.rows:
         raise ValueError("q4_quantize: %d rows, the matrix has %d" % (rows, q.rows))
@@ -558,6 +574,12 @@ def q4_quantize(x, q: Q4Matrix, stream=None):
 
 def q4_dequantize(q: Q4Matrix, y, stream=None):
     """The values that q stands for into y (bf16 or fp32, [..., cols])."""
+    st = (_native or _load_native()).q4_dequantize(q, y, stream)
+    if st == OK:
+        return
+    if st is not None:
+        raise DcError(st, "dc_q4_dequantize")
+    _here("q4_dequantize", q.data, y)
     rows, stride = _rows_of(y, q.cols, "q4_dequantize")
     if rows != q.rows:
         raise ValueError("q4_dequantize: %d rows, the matrix has %d" % (rows, q.rows))
@@ -579,6 +601,12 @@ def _bias(t, n: int, what: str):
 
 def q4_product(x: Q4Matrix, w: Q4Matrix, bias, act, residual, y, workspace, stream=None):
     """y = act(X W^T + bias + residual) of two quantised matrices; y (and residual): [..., w.rows], bf16 or fp32, dense."""
+    st = (_native or _load_native()).q4_product(x, w, bias, act, residual, y, workspace, stream)
+    if st == OK:
+        return
+    if st is not None:
+        raise DcError(st, "dc_q4_product")
+    _here("q4_product", x.data, w.data, bias, residual, y, workspace)
     if x.fmt != w.fmt or x.cols != w.cols:
         raise ValueError("q4_product: the matrices must have one format and as many columns")
     _dense(y, x.rows, w.rows, y.dtype, "q4_product")
@@ -591,6 +619,12 @@ def q4_product(x: Q4Matrix, w: Q4Matrix, bias, act, residual, y, workspace, stre
 
 def q4_forward(x, w: Q4Matrix, x_scale: float, bias, act, residual, y, workspace, stream=None):
     """The same from rows in bf16 or fp32 (x: [..., w.cols], dense, of y's dtype), quantised on the way with tensor scale x_scale."""
+    st = (_native or _load_native()).q4_forward(x, w, x_scale, bias, act, residual, y, workspace, stream)
+    if st == OK:
+        return
+    if st is not None:
+        raise DcError(st, "dc_q4_forward")
+    _here("q4_forward", x, w.data, bias, residual, y, workspace)
     rows = x.numel() // w.cols
     _dense(x, rows, w.cols, y.dtype, "q4_forward")
     _dense(y, rows, w.rows, y.dtype, "q4_forward")

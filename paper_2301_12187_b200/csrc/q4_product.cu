@@ -280,12 +280,36 @@ __device__ __forceinline__ void deliver(const Params &p, const float *__restrict
   for (int i = 0; i < N; ++i)
     if (o + i < p.c_out) deliver_one<T>(p, v[i], bias ? __ldg(bias + o + i) : 0.f, residual, y, at + i);
 }
-// a lane to a column, where rows of y do not begin on 16 bytes
-template <typename T>
-__device__ __forceinline__ void deliver_columns(const Params &p, float b, const T *residual, T *y, size_t at, int rows, uint32_t sm, int lane) {
-#pragma unroll 4
-  for (int r = 0; r < rows; ++r, at += (size_t)p.c_out)
-    deliver_one<T>(p, lds_f(sm + (uint32_t)(r * 128 + ((lane >> 2) ^ (r & 7)) * 16 + (lane & 3) * 4)), b, residual, y, at);
+// a lane to a column, where rows of y do not begin on 16 bytes; eight rows at once, so that what one waits for the others do not add to
+template <typename T, bool RES>
+__device__ __forceinline__ void deliver_columns(const Params &p, float b, const T *residual, T *y, int rows, uint32_t sm, int lane) {
+  const size_t pitch = (size_t)p.c_out;
+  const uint32_t at = sm + (uint32_t)((lane & 3) * 4), piece = (uint32_t)lane >> 2;
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += 8, y += 8 * pitch) {
+    float t[8], r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = lds_f(at + (uint32_t)((r0 + i) * 128) + ((piece ^ (uint32_t)i) << 4));
+    if (RES) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = r0 + i < rows ? (float)residual[i * pitch] : 0.f;
+      residual += 8 * pitch;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      t[i] = fmaf(t[i], p.scale, b);
+      if (RES) t[i] += r[i];
+      t[i] = dc_act_apply(t[i], p.act);
+    }
+    if (r0 + 8 <= rows) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i * pitch] = (T)t[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r0 + i < rows) y[i * pitch] = (T)t[i];
+    }
+  }
 }
 
 // 16 columns of a row of x from column c: the values, zeros from column c_in on
@@ -633,9 +657,13 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             }
             __syncwarp();
             const int o = c + h * 32 + lane;
-            if (o < cols)
-              deliver_columns<T>(p, bias_s[warp - 2][P ? o - c : o], residual, y, (size_t)row0 * (size_t)p.c_out + (size_t)(tn * p.nt + o),
-                                 p.rows - row0 < 32 ? (int)(p.rows - row0) : 32, out, lane);
+            if (o < cols) {
+              const size_t to = (size_t)row0 * (size_t)p.c_out + (size_t)(tn * p.nt + o);
+              const int rows = p.rows - row0 < 32 ? (int)(p.rows - row0) : 32;
+              const float b = bias_s[warp - 2][P ? o - c : o];
+              if (residual) deliver_columns<T, true>(p, b, residual + to, y + to, rows, out, lane);
+              else deliver_columns<T, false>(p, b, nullptr, y + to, rows, out, lane);
+            }
             __syncwarp();
           }
         }
@@ -875,23 +903,32 @@ bool lay_out(Params *p, int form, int format, int dtype, int n_sm) {
   return p->stages >= 2;
 }
 
-// Estimated cycles of a form: a stage takes its products, its loads or its quantising, whichever is longest.
-double estimate(const Params &p, int form, int n_sm) {
+// Estimated time of a form in microseconds, fitted to 60 products in all their forms (1 to 200704 rows, 16 to 8192 columns of either operand).
+// A stage takes its products or its loads; a tile's results go out beside the next tile's products where they have an accumulator of their own.
+// A cluster costs its meetings, and its parts their way between SMs.  Of the start 3.2 us, launch and first loads.
+double estimate(const Params &p, int form, int dtype, int n_sm) {
   static constexpr int kClusters[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};    // of that many CTAs that run at once, on 148 SMs
-  const int team = form == kPair ? 2 : p.split;
-  const double at_once = team > 1 ? kClusters[team] * (n_sm / 148.0) : n_sm;
-  const double products = 2.0 * p.nt, loads = p.stage_bytes / 40.0, stage = products > loads ? products : loads;
-  const double main = (form == kPair ? p.chunks : p.chunks_per) * stage, out = 4.0 * p.nt + 500;
-  double waves = p.items / at_once;
-  waves = (double)(long long)(waves + 0.999);
-  return 3000 + waves * (p.acc_bufs > 1 ? (main > out ? main : out) : main + out) + (team > 1 ? 1500 : 0) +
-         (form == kRows ? 1000 + 56.0 * (double)p.rows * p.chunks_per : 0);
+  const double wide = p.nt / 128.0, type = dtype == DC_F32 ? 1.8 : 1.0;
+  const double stage = form == kPair ? (p.nt > 128 ? 0.47 : 0.39) : p.nt > 128 ? 0.44 + 0.16 * (wide - 1) : 0.3 + 0.14 * wide;
+  const double w_total = (double)p.tiles_n * p.w_bytes * p.chunks * (form == kPair ? 2 : 1) / 4.5e6;
+  if (p.split > 1) {
+    const double main = p.chunks_per * stage, waves = dc_div_up(p.items, kClusters[p.split]);
+    return 3.2 + waves * ((main > w_total ? main : w_total) + 2.5 + p.part_rows * p.nt * 4 / 20e3) +
+           (form == kRows ? 256.0 * p.rows * p.chunks_per * 115e-6 : 0);
+  }
+  const int at_once = form == kPair ? n_sm / 2 : n_sm;
+  const double waves = p.columns ? dc_div_up(p.tiles_m, at_once / p.tiles_n) : dc_div_up(p.items, at_once);
+  double main = p.chunks * stage, out = (form == kPair ? (p.nt > 128 ? 3.0 : 2.0) : wide) * type;
+  if (form == kStream) main = 0.4 + 0.8 * dc_div_up(p.c_in, 32);
+  if (form == kRows) main += 256.0 * p.rows * p.chunks_per * 115e-6;
+  if (!p.vec) out *= 1.5;
+  const double total = 3.2 + (p.acc_bufs > 1 ? waves * (main > out ? main : out) : waves * (main + out));
+  return total > 3.2 + w_total ? total : 3.2 + w_total;
 }
 
-//FORCE
 // Fills p for the form that takes the least of the estimates.  Tiles of fewer than all of w's rows begin where a scale tile does: they have
 // 128 or 256 rows.
-int choose(Params *p, bool raw, int format, int dtype, int n_sm) {
+int choose(Params *p, bool raw, int format, int dtype, int n_sm, double *us_of) {
   double best = 1e30;
   Params best_p = *p;
   int best_form = -1;
@@ -907,13 +944,13 @@ int choose(Params *p, bool raw, int format, int dtype, int n_sm) {
     q.items = q.tiles_m * q.tiles_n;
     if (split > 1 && (q.chunks_per * (split - 1) >= q.chunks || (long long)q.items * split > n_sm)) return;     // no CTA without a stage
     if (!lay_out(&q, form, format, dtype, n_sm)) return;
-    const double cycles = estimate(q, form, n_sm);
-    if (cycles < best) { best = cycles; best_p = q; best_form = form; }
+    const double us = estimate(q, form, dtype, n_sm);
+    if (us < best) { best = us; best_p = q; best_form = form; }
   };
   if (raw && p->rows <= kMaxRows) {
     for (int s = 1; s <= kMaxSplit; ++s) look(kRows, whole < 128 ? whole : 128, s);
   } else if (raw) {
-    if (p->c_in <= kStageCols && whole <= 256 && p->vec_x) look(kStream, whole, 1);
+    if (p->c_in <= 64 && whole <= 256 && p->vec_x) look(kStream, whole, 1);
   } else {
     for (int n = 128; n <= 256; n += 128) {
       for (int s = 1; s <= kMaxSplit; ++s) look(kOne, whole < n ? whole : n, s);
@@ -925,6 +962,7 @@ int choose(Params *p, bool raw, int format, int dtype, int n_sm) {
     }
   }
   *p = best_p;
+  *us_of = best;
   return best_form;
 }
 
@@ -937,10 +975,7 @@ cudaError_t launch_form(int form, Params &p, const Call &c) {
     default: return launch<F, T, kStream>(p, c);
   }
 }
-// DC_ERR_UNSUPPORTED: no form takes rows of this size as they are (raw), or at all
-dc_status run(Params &p, bool raw, dc_q4_format format, dc_dtype dtype, Call &c) {
-  c.n_sm = dc_sm_count();
-  const int form = choose(&p, raw, format, dtype, c.n_sm);
+dc_status run(int form, Params &p, dc_q4_format format, dc_dtype dtype, Call &c) {
   if (form < 0) return DC_ERR_UNSUPPORTED;
   cudaError_t e;
   if (format == DC_MX4) e = dtype == DC_BF16 ? launch_form<DC_MX4, __nv_bfloat16>(form, p, c) : launch_form<DC_MX4, float>(form, p, c);
@@ -994,8 +1029,10 @@ extern "C" dc_status dc_q4_product(const void *x, long long rows, int c_in, cons
   if (s != DC_OK) return s;
   if (!(scale - scale == 0.f)) return DC_ERR_INVALID_ARG;
   Params p = params_of(rows, c_in, c_out, act, dtype, scale);
-  Call c = {x, w, &lx, &lw, bias, residual, y, (DcWsHeader *)workspace, 0, (cudaStream_t)stream};
-  return run(p, false, format, dtype, c);
+  Call c = {x, w, &lx, &lw, bias, residual, y, (DcWsHeader *)workspace, dc_sm_count(), (cudaStream_t)stream};
+  double us;
+  const int form = choose(&p, false, format, dtype, c.n_sm, &us);
+  return run(form, p, format, dtype, c);
 }
 
 extern "C" dc_status dc_q4_forward(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, float x_scale,
@@ -1011,13 +1048,15 @@ extern "C" dc_status dc_q4_forward(const void *x, long long rows, int c_in, cons
   Params p = params_of(rows, c_in, c_out, act, dtype, scale);
   p.g = x_scale;
   p.g6 = 6.f * x_scale;
-  Call c = {x, w, &lx, &lw, bias, residual, y, (DcWsHeader *)workspace, 0, (cudaStream_t)stream};
-  s = run(p, true, format, dtype, c);
-  if (s != DC_ERR_UNSUPPORTED) return s;
+  Call c = {x, w, &lx, &lw, bias, residual, y, (DcWsHeader *)workspace, dc_sm_count(), (cudaStream_t)stream};
+  Params q = params_of(rows, c_in, c_out, act, dtype, scale);
+  // in the product's launch, or in one of its own before it (2 us, and its bytes)
+  double us, us_apart;
+  const int form = choose(&p, true, format, dtype, c.n_sm, &us), apart = choose(&q, false, format, dtype, c.n_sm, &us_apart);
+  if (form >= 0 && us <= us_apart + 2.0 + (double)rows * c_in * (dtype == DC_F32 ? 4.5 : 2.5) / 4.5e6) return run(form, p, format, dtype, c);
   uint8_t *xq = (uint8_t *)workspace + sizeof(DcWsHeader);
   s = dc_q4_quantize(x, rows, c_in, c_in, dtype, format, x_scale, xq, stream);
   if (s != DC_OK) return s;
-  Params q = params_of(rows, c_in, c_out, act, dtype, scale);
   c.x = xq;
-  return run(q, false, format, dtype, c);
+  return run(apart, q, format, dtype, c);
 }

@@ -647,7 +647,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           }
           __syncwarp();
           if (p.out_bufs == 2) turn ^= 1u;
-        } else {
+        } else if (FORM != kStream) {            // (which is for rows of y that begin on 16 bytes)
 #pragma unroll
           for (int h = 0; h < kHalves; ++h) {
 #pragma unroll
@@ -950,7 +950,7 @@ int choose(Params *p, bool raw, int format, int dtype, int n_sm, double *us_of) 
   if (raw && p->rows <= kMaxRows) {
     for (int s = 1; s <= kMaxSplit; ++s) look(kRows, whole < 128 ? whole : 128, s);
   } else if (raw) {
-    if (p->c_in <= 64 && whole <= 256 && p->vec_x) look(kStream, whole, 1);
+    if (p->c_in <= 64 && whole <= 256 && p->vec_x && p->vec) look(kStream, whole, 1);
   } else {
     for (int n = 128; n <= 256; n += 128) {
       for (int s = 1; s <= kMaxSplit; ++s) look(kOne, whole < n ? whole : n, s);

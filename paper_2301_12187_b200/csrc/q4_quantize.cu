@@ -1,7 +1,8 @@
 // Quantising matrices to microscaled 4 bits and reading them back (dc_q4_quantize, dc_q4_dequantize).
 //
-// A thread takes 16 columns of a row: a block of DC_NV4, half of one of DC_MX4 (the other half is in the neighbouring lane).  A CTA takes 128
-// rows x up to 256 columns, the rows of whole scale tiles, collects their scale bytes in shared memory and writes them as 16-byte words.
+// A thread takes 16 columns of a row: a block of DC_NV4, half of one of DC_MX4 (the other half is in the neighbouring lane).  A CTA takes up to 256
+// columns of 128 rows, whole scale tiles, whose bytes it collects in shared memory and writes 16 at a time -- or, where that gives too few CTAs,
+// of the 32 rows that share a word of every 16 bytes of a scale tile.
 #include <string.h>
 
 #include "q4.cuh"
@@ -17,6 +18,7 @@ struct Params {
   int cols;
   int segs_log2;             // log2 of the 16-column pieces of a row that a CTA takes
   int vec;                   // rows begin on 16 bytes: whole pieces are loaded and stored in 16-byte words
+  int groups;                // CTAs that share 128 rows: 1 or 4
   float g, g6;
   uint32_t pitch, tiles, col_tiles;
   size_t scale_offset;
@@ -53,15 +55,17 @@ struct Staged {
 };
 
 template <int F, typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_q4_quantize(const T *__restrict__ x, uint8_t *__restrict__ q, const Params p) {
+__global__ void __launch_bounds__(kThreads, VEC ? 4 : 2) k_q4_quantize(const T *__restrict__ x, uint8_t *__restrict__ q, const Params p) {
   __shared__ __align__(16) uint8_t scales[4 * kAtom];
   extern __shared__ uint8_t staged_s[];            // Staged, where !VEC
   dc_pdl_enter();
   const int tid = (int)threadIdx.x, segs = 1 << p.segs_log2, span_log2 = p.segs_log2 + 4;
-  const uint32_t tile = blockIdx.x / p.col_tiles, col_tile = blockIdx.x - tile * p.col_tiles;
+  const uint32_t strip = blockIdx.x / p.col_tiles, col_tile = blockIdx.x - strip * p.col_tiles;
+  const uint32_t tile = strip / (uint32_t)p.groups, group = strip - tile * (uint32_t)p.groups;
   const int seg = tid & (segs - 1), c0 = (int)(col_tile << span_log2), c = c0 + seg * 16;
-  const long long row0 = (long long)tile * 128;
-  const int rows = p.rows - row0 < 128 ? (int)(p.rows - row0) : 128;
+  const int most = 128 / p.groups, in_tile = (int)group * most;                  // rows of this CTA, and the first one's place in its scale tile
+  const long long row0 = (long long)tile * 128 + in_tile;
+  const int rows = p.rows - row0 < most ? (int)(p.rows - row0) : most;           // none or fewer: the scales of such rows are 0
   constexpr int kBlock = F == DC_MX4 ? 32 : 16, kPieces = 16 / kPer<T>;
   // scale tiles of this CTA; the bytes that no row or block writes are 0
   const int atoms = (1 << span_log2) <= 4 * kBlock ? 1 : (1 << span_log2) / (4 * kBlock);
@@ -77,7 +81,7 @@ __global__ void __launch_bounds__(kThreads) k_q4_quantize(const T *__restrict__ 
       *reinterpret_cast<uint2 *>(q + (size_t)(row0 + r) * p.pitch + (c >> 1)) = code;
       if (c < p.cols && (F == DC_NV4 || (seg & 1) == 0)) {
         const uint32_t b = (uint32_t)(seg * 16 / kBlock);
-        scales[(b >> 2) * kAtom + scale_at((uint32_t)r, b)] = (uint8_t)s.byte;
+        scales[(b >> 2) * kAtom + scale_at((uint32_t)(in_tile + r), b)] = (uint8_t)s.byte;
       }
     }
   };
@@ -108,7 +112,7 @@ __global__ void __launch_bounds__(kThreads) k_q4_quantize(const T *__restrict__ 
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (u > 0 && r + u * step - mine >= 128) break;        // the same for all threads
+        if (u > 0 && r + u * step - mine >= most) break;       // the same for all threads
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
@@ -149,8 +153,13 @@ __global__ void __launch_bounds__(kThreads) k_q4_quantize(const T *__restrict__ 
   __syncthreads();
   const uint32_t atom0 = col_tile * (uint32_t)atoms;
   const uint32_t left = p.tiles - atom0, n = left < (uint32_t)atoms ? left : (uint32_t)atoms;
-  uint4 *out = reinterpret_cast<uint4 *>(q + p.scale_offset + ((size_t)tile * p.tiles + atom0) * kAtom);
-  for (uint32_t i = tid; i < n * (kAtom / 16); i += kThreads) out[i] = reinterpret_cast<const uint4 *>(scales)[i];
+  uint8_t *out = q + p.scale_offset + ((size_t)tile * p.tiles + atom0) * kAtom;
+  if (p.groups == 1) {
+    for (uint32_t i = tid; i < n * (kAtom / 16); i += kThreads) reinterpret_cast<uint4 *>(out)[i] = reinterpret_cast<const uint4 *>(scales)[i];
+  } else {
+    for (uint32_t i = tid; i < n * (kAtom / 16); i += kThreads)
+      reinterpret_cast<uint32_t *>(out)[i * 4 + group] = reinterpret_cast<const uint32_t *>(scales)[i * 4 + group];
+  }
 }
 
 template <int F, typename T, bool VEC>
@@ -159,10 +168,12 @@ __global__ void __launch_bounds__(kThreads) k_q4_dequantize(const uint8_t *__res
   extern __shared__ uint8_t staged_s[];            // Staged, where !VEC
   dc_pdl_enter();
   const int tid = (int)threadIdx.x, segs = 1 << p.segs_log2, span_log2 = p.segs_log2 + 4;
-  const uint32_t tile = blockIdx.x / p.col_tiles, col_tile = blockIdx.x - tile * p.col_tiles;
+  const uint32_t strip = blockIdx.x / p.col_tiles, col_tile = blockIdx.x - strip * p.col_tiles;
+  const uint32_t tile = strip / (uint32_t)p.groups, group = strip - tile * (uint32_t)p.groups;
   const int seg = tid & (segs - 1), c0 = (int)(col_tile << span_log2), c = c0 + seg * 16;
-  const long long row0 = (long long)tile * 128;
-  const int rows = p.rows - row0 < 128 ? (int)(p.rows - row0) : 128;
+  const int most = 128 / p.groups, in_tile = (int)group * most;                  // rows of this CTA, and the first one's place in its scale tile
+  const long long row0 = (long long)tile * 128 + in_tile;
+  const int rows = p.rows - row0 < most ? (int)(p.rows - row0) : most;           // none or fewer: the scales of such rows are 0
   constexpr int kBlock = F == DC_MX4 ? 32 : 16;
   const int atoms = (1 << span_log2) <= 4 * kBlock ? 1 : (1 << span_log2) / (4 * kBlock);
   {
@@ -176,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) k_q4_dequantize(const uint8_t *__res
   const uint32_t b = (uint32_t)(seg * 16 / kBlock);
   auto codes_of = [&](int r) { return wanted && r < rows ? __ldg(reinterpret_cast<const uint2 *>(q + (size_t)(row0 + r) * p.pitch + (c >> 1))) : make_uint2(0, 0); };
   auto values = [&](int r, uint2 code, float *v) {
-    const float s = scale_value(scales[(b >> 2) * kAtom + scale_at((uint32_t)r, b)], F, p.g);
+    const float s = scale_value(scales[(b >> 2) * kAtom + scale_at((uint32_t)(in_tile + r), b)], F, p.g);
     uint32_t h[8];
     values8(code.x, h);
     values8(code.y, h + 4);
@@ -188,31 +199,22 @@ __global__ void __launch_bounds__(kThreads) k_q4_dequantize(const uint8_t *__res
     }
   };
   if (VEC) {
-    constexpr int U = 4;
     __syncthreads();
     if (!wanted) return;
-#pragma unroll 1
-    for (int r = mine; r < rows; r += U * step) {
-      uint2 code[U];
+#pragma unroll 2
+    for (int r = mine; r < rows; r += step) {
+      float v[16];
+      values(r, codes_of(r), v);
+      T *at = y + (row0 + r) * p.stride + c;
 #pragma unroll
-      for (int u = 0; u < U; ++u) code[u] = codes_of(r + u * step);
+      for (int i = 0; i < 16 / kPer<T>; ++i) {
+        const int left = p.cols - (c + i * kPer<T>);
+        if (left >= kPer<T>) {
+          reinterpret_cast<uint4 *>(at)[i] = pack<T>(v + i * kPer<T>);
+        } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int ru = r + u * step;
-        if (ru >= rows) break;
-        float v[16];
-        values(ru, code[u], v);
-        T *at = y + (row0 + ru) * p.stride + c;
-#pragma unroll
-        for (int i = 0; i < 16 / kPer<T>; ++i) {
-          const int left = p.cols - (c + i * kPer<T>);
-          if (left >= kPer<T>) {
-            reinterpret_cast<uint4 *>(at)[i] = pack<T>(v + i * kPer<T>);
-          } else {
-#pragma unroll
-            for (int j = 0; j < kPer<T>; ++j)
-              if (j < left) at[i * kPer<T> + j] = (T)v[i * kPer<T> + j];
-          }
+          for (int j = 0; j < kPer<T>; ++j)
+            if (j < left) at[i * kPer<T> + j] = (T)v[i * kPer<T> + j];
         }
       }
     }
@@ -259,7 +261,9 @@ dc_status prepare(const void *x, long long rows, int cols, long long stride, dc_
   p->tiles = (uint32_t)l.tiles;
   p->scale_offset = l.scale_offset;
   p->col_tiles = (uint32_t)dc_div_up(cols, 16 << p->segs_log2);
-  const long long ctas = (rows + 127) / 128 * p->col_tiles;
+  const long long tiles = (rows + 127) / 128 * p->col_tiles;
+  p->groups = tiles < 4ll * dc_sm_count() ? 4 : 1;
+  const long long ctas = tiles * p->groups;
   if (ctas > 0x7fffffffll) return DC_ERR_UNSUPPORTED;
   *grid = dim3((unsigned)ctas);
   return DC_OK;

@@ -16,7 +16,7 @@ constexpr int kCols = 256;                       // columns of a CTA, at most
 struct Params {
   long long rows, stride;
   int cols;
-  int segs_log2;             // log2 of the 16-column pieces of a row that a CTA takes
+  int segs, segs_log2;       // 16-column pieces of a row that a CTA takes; their log2 where rows go through shared memory
   int vec;                   // rows begin on 16 bytes: whole pieces are loaded and stored in 16-byte words
   int groups;                // CTAs that share 128 rows: 1 or 4
   float g, g6;
@@ -55,24 +55,24 @@ struct Staged {
 };
 
 template <int F, typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads, VEC ? 4 : 2) k_q4_quantize(const T *__restrict__ x, uint8_t *__restrict__ q, const Params p) {
+__global__ void __launch_bounds__(kThreads, VEC ? 4 : 3) k_q4_quantize(const T *__restrict__ x, uint8_t *__restrict__ q, const Params p) {
   __shared__ __align__(16) uint8_t scales[4 * kAtom];
   extern __shared__ uint8_t staged_s[];            // Staged, where !VEC
   dc_pdl_enter();
-  const int tid = (int)threadIdx.x, segs = 1 << p.segs_log2, span_log2 = p.segs_log2 + 4;
+  const int tid = (int)threadIdx.x, segs = VEC ? p.segs : 1 << p.segs_log2, span_log2 = p.segs_log2 + 4, span = segs * 16;
   const uint32_t strip = blockIdx.x / p.col_tiles, col_tile = blockIdx.x - strip * p.col_tiles;
   const uint32_t tile = strip / (uint32_t)p.groups, group = strip - tile * (uint32_t)p.groups;
-  const int seg = tid & (segs - 1), c0 = (int)(col_tile << span_log2), c = c0 + seg * 16;
+  const int mine = VEC ? tid / segs : tid >> p.segs_log2, seg = tid - mine * segs, step = kThreads / segs;     // this thread's row of the `step` at a time
+  const int c0 = (int)col_tile * span, c = c0 + seg * 16;
   const int most = 128 / p.groups, in_tile = (int)group * most;                  // rows of this CTA, and the first one's place in its scale tile
   const long long row0 = (long long)tile * 128 + in_tile;
   const int rows = p.rows - row0 < most ? (int)(p.rows - row0) : most;           // none or fewer: the scales of such rows are 0
   constexpr int kBlock = F == DC_MX4 ? 32 : 16, kPieces = 16 / kPer<T>;
   // scale tiles of this CTA; the bytes that no row or block writes are 0
-  const int atoms = (1 << span_log2) <= 4 * kBlock ? 1 : (1 << span_log2) / (4 * kBlock);
+  const int atoms = (span + 4 * kBlock - 1) / (4 * kBlock);
   for (int i = tid; i < atoms * (kAtom / 16); i += kThreads) reinterpret_cast<uint4 *>(scales)[i] = make_uint4(0, 0, 0, 0);
   __syncthreads();
-  const int step = kThreads >> p.segs_log2, mine = tid >> p.segs_log2;           // rows at a time; this thread's of them
-  const bool wanted = c < (int)(p.pitch * 2);
+  const bool wanted = c < (int)(p.pitch * 2) && mine < step;
   auto put = [&](int r, uint32_t top, float *v) {
     if (F == DC_MX4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     const BlockScale s = block_scale<F>(top, p.g, p.g6);
@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(kThreads, VEC ? 4 : 2) k_q4_quantize(const T *
   };
   if (VEC) {
     constexpr int U = 2;                         // rows of a thread at once, so that their loads overlap
+    const bool whole = c + 16 <= p.cols && wanted;
 #pragma unroll 1
     for (int r = mine; r - mine < rows; r += U * step) {
       uint4 raw[U][kPieces];
@@ -97,7 +98,9 @@ __global__ void __launch_bounds__(kThreads, VEC ? 4 : 2) k_q4_quantize(const T *
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
           raw[u][i] = make_uint4(0, 0, 0, 0);
-          if (ru < rows) {
+          if (whole) {
+            if (ru < rows) raw[u][i] = __ldg(reinterpret_cast<const uint4 *>(at) + i);
+          } else if (ru < rows && wanted) {
             const int left = p.cols - (c + i * kPer<T>);
             if (left >= kPer<T>) {
               raw[u][i] = __ldg(reinterpret_cast<const uint4 *>(at) + i);
@@ -163,31 +166,24 @@ __global__ void __launch_bounds__(kThreads, VEC ? 4 : 2) k_q4_quantize(const T *
 }
 
 template <int F, typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_q4_dequantize(const uint8_t *__restrict__ q, T *__restrict__ y, const Params p) {
-  __shared__ __align__(16) uint8_t scales[4 * kAtom];
+__global__ void __launch_bounds__(kThreads, VEC ? 4 : 3) k_q4_dequantize(const uint8_t *__restrict__ q, T *__restrict__ y, const Params p) {
   extern __shared__ uint8_t staged_s[];            // Staged, where !VEC
   dc_pdl_enter();
-  const int tid = (int)threadIdx.x, segs = 1 << p.segs_log2, span_log2 = p.segs_log2 + 4;
+  const int tid = (int)threadIdx.x, segs = VEC ? p.segs : 1 << p.segs_log2, span_log2 = p.segs_log2 + 4, span = segs * 16;
   const uint32_t strip = blockIdx.x / p.col_tiles, col_tile = blockIdx.x - strip * p.col_tiles;
   const uint32_t tile = strip / (uint32_t)p.groups, group = strip - tile * (uint32_t)p.groups;
-  const int seg = tid & (segs - 1), c0 = (int)(col_tile << span_log2), c = c0 + seg * 16;
+  const int mine = VEC ? tid / segs : tid >> p.segs_log2, seg = tid - mine * segs, step = kThreads / segs;     // this thread's row of the `step` at a time
+  const int c0 = (int)col_tile * span, c = c0 + seg * 16;
   const int most = 128 / p.groups, in_tile = (int)group * most;                  // rows of this CTA, and the first one's place in its scale tile
   const long long row0 = (long long)tile * 128 + in_tile;
   const int rows = p.rows - row0 < most ? (int)(p.rows - row0) : most;           // none or fewer: the scales of such rows are 0
   constexpr int kBlock = F == DC_MX4 ? 32 : 16;
-  const int atoms = (1 << span_log2) <= 4 * kBlock ? 1 : (1 << span_log2) / (4 * kBlock);
-  {
-    const uint32_t atom0 = col_tile * (uint32_t)atoms;
-    const uint32_t left = p.tiles - atom0, n = left < (uint32_t)atoms ? left : (uint32_t)atoms;
-    const uint4 *in = reinterpret_cast<const uint4 *>(q + p.scale_offset + ((size_t)tile * p.tiles + atom0) * kAtom);
-    for (uint32_t i = tid; i < n * (kAtom / 16); i += kThreads) reinterpret_cast<uint4 *>(scales)[i] = __ldg(in + i);
-  }
-  const int step = kThreads >> p.segs_log2, mine = tid >> p.segs_log2;
-  const bool wanted = c < p.cols;
-  const uint32_t b = (uint32_t)(seg * 16 / kBlock);
+  const bool wanted = c < p.cols && mine < step;
+  const uint32_t b = (uint32_t)(c / kBlock);
+  const uint8_t *scales = q + p.scale_offset + ((size_t)tile * p.tiles + (b >> 2)) * kAtom;
   auto codes_of = [&](int r) { return wanted && r < rows ? __ldg(reinterpret_cast<const uint2 *>(q + (size_t)(row0 + r) * p.pitch + (c >> 1))) : make_uint2(0, 0); };
   auto values = [&](int r, uint2 code, float *v) {
-    const float s = scale_value(scales[(b >> 2) * kAtom + scale_at((uint32_t)(in_tile + r), b)], F, p.g);
+    const float s = scale_value(__ldg(scales + scale_at((uint32_t)(in_tile + r), b)), F, p.g);
     uint32_t h[8];
     values8(code.x, h);
     values8(code.y, h + 4);
@@ -199,13 +195,17 @@ __global__ void __launch_bounds__(kThreads) k_q4_dequantize(const uint8_t *__res
     }
   };
   if (VEC) {
-    __syncthreads();
     if (!wanted) return;
-#pragma unroll 2
+#pragma unroll 1
     for (int r = mine; r < rows; r += step) {
       float v[16];
       values(r, codes_of(r), v);
       T *at = y + (row0 + r) * p.stride + c;
+      if (c + 16 <= p.cols) {
+#pragma unroll
+        for (int i = 0; i < 16 / kPer<T>; ++i) reinterpret_cast<uint4 *>(at)[i] = pack<T>(v + i * kPer<T>);
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < 16 / kPer<T>; ++i) {
         const int left = p.cols - (c + i * kPer<T>);
@@ -260,7 +260,8 @@ dc_status prepare(const void *x, long long rows, int cols, long long stride, dc_
   p->pitch = (uint32_t)l.pitch;
   p->tiles = (uint32_t)l.tiles;
   p->scale_offset = l.scale_offset;
-  p->col_tiles = (uint32_t)dc_div_up(cols, 16 << p->segs_log2);
+  p->segs = p->vec ? (l.pitch < kCols / 2 ? (int)(l.pitch / 8) : kCols / 16) : 1 << p->segs_log2;
+  p->col_tiles = (uint32_t)dc_div_up(cols, 16 * p->segs);
   const long long tiles = (rows + 127) / 128 * p->col_tiles;
   p->groups = tiles < 4ll * dc_sm_count() ? 4 : 1;
   const long long ctas = tiles * p->groups;

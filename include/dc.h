@@ -380,7 +380,7 @@ dc_status dc_chain_forward_host_async(const dc_layer *layers, int n_layers, cons
  *   DC_NV4: blocks of 16, scale s g: s = a / (6 g) rounded to e4m3 (448 at most), g = `tensor_scale`, a power of two for the whole matrix.
  * A value's code is the nearest to value / scale, ties to the code with an even last bit, 6 at most.  The quotients decide as in real
  * arithmetic, so the codes are a function of the values alone.  A block with a NaN or an infinity gets the scale NaN: all of it
- * reads as NaN, and so do the results of its row.  A block whose scale is 0 (a / (6 g) up to 2^-10) reads as 0.
+ * reads as NaN, and so do the results of its row (a NaN leaves DC_ACT_RELU6 as 0, or as 6 in bf16).  A block whose scale is 0 (a / (6 g) up to 2^-10) reads as 0.
  * --------------------------------------------------------------------------------------------- */
 typedef enum { DC_MX4 = 0, DC_NV4 = 1 } dc_q4_format;
 
@@ -427,6 +427,24 @@ dc_status dc_q4_product(const void *x, long long rows, int c_in, const void *w, 
 dc_status dc_q4_forward(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, float x_scale,
                         float w_scale, const float *bias, dc_act act, const void *residual, void *y, dc_dtype dtype, void *workspace,
                         size_t workspace_bytes, dc_stream stream);
+
+/*
+ * Host only, launches nothing: how dc_q4_forward (forward = 1) or dc_q4_product (0) would run, for reports and tests.
+ */
+typedef enum {
+  DC_Q4_TILES = 0,           /* tiles of 128 rows, each by one CTA, or its reduction by a cluster of `split` */
+  DC_Q4_PAIRS = 1,           /* tiles of 256 rows by two CTAs */
+  DC_Q4_FEW_ROWS = 2,        /* dc_q4_forward: rows quantised in the product's launch, and kept in shared memory */
+  DC_Q4_STREAM = 3           /* dc_q4_forward: rows quantised in the product's launch, tile by tile */
+} dc_q4_form;
+typedef struct {
+  dc_q4_form form;
+  int launches;              /* 2: quantised apart, into the workspace */
+  int tile_cols, split;      /* columns of y to a tile; CTAs that share a tile's reduction */
+  int stages, accumulators;  /* of 256 columns of the operands; of a CTA */
+  int columns, w_stays;      /* CTAs keep to a column of tiles; and load its weights once */
+} dc_q4_plan;
+dc_status dc_q4_plan_query(long long rows, int c_in, int c_out, dc_q4_format format, dc_dtype dtype, int forward, dc_q4_plan *plan);
 
 /* ---------------------------------------------------------------------------------------------
  * The selector's two dynamic programmes (Sec. 4.3).  Host only: every pointer is host memory, no

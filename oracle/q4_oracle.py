@@ -15,6 +15,11 @@ def block_of(fmt):
 def nearest(v, grid):
     """Index of the grid point nearest to each v >= 0, ties to the even index, the last one beyond the grid."""
     mid = (grid[1:] + grid[:-1]) / 2              # exact: grid points have few bits
+    if len(mid) < 10:                             # few borders: counted one by one, which is faster on large arrays
+        n = np.zeros(v.shape, dtype=np.int64)
+        for i, m in enumerate(mid):
+            n += v > m if i % 2 == 0 else v >= m  # a border between an even index and the odd one above it belongs to the even one
+        return n
     below, upto = np.searchsorted(mid, v, side="left"), np.searchsorted(mid, v, side="right")
     return np.where((below != upto) & (upto % 2 == 0), upto, below)
 
@@ -79,9 +84,9 @@ def unpack(buf, rows, cols, fmt):
     return code, t.transpose(0, 3, 2, 1, 4).reshape(-1, tiles * 4).astype(np.int64)
 
 
-def product(xv, wv, bias=None, residual=None, relu6=False):
-    """act(X W^T + bias + residual) of values, in 64 bits."""
-    y = xv @ wv.T
+def product(xv, wv, bias=None, residual=None, relu6=False, matmul=lambda a, b: a @ b.T):
+    """act(X W^T + bias + residual) of values, in 64 bits (`matmul`: a faster a b^T in 64 bits)."""
+    y = matmul(xv, wv)
     if bias is not None:
         y = y + np.asarray(bias, dtype=np.float64)
     if residual is not None:

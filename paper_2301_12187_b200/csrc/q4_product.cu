@@ -24,7 +24,7 @@ namespace {
 using namespace tc;
 using q4::kAtom;
 
-enum { kOne = 0, kPair = 1, kRows = 2, kStream = 3 };
+enum { kOne = DC_Q4_TILES, kPair = DC_Q4_PAIRS, kRows = DC_Q4_FEW_ROWS, kStream = DC_Q4_STREAM };
 template <int FORM>
 constexpr int kEpi = FORM == kOne ? 12 : 8;      // warps reading out
 constexpr int kCutWarps = 4;                     // quantising, form kStream
@@ -1010,7 +1010,41 @@ Params params_of(long long rows, int c_in, int c_out, dc_act act, dc_dtype dtype
   return p;
 }
 
+// Whether a forward call quantises in the product's launch (p, form) or in one of its own before it (q, apart: 2 us, and its bytes).
+bool in_one_launch(Params *p, Params *q, dc_q4_format format, dc_dtype dtype, int n_sm, int *form, int *apart) {
+  double us, us_apart;
+  *form = choose(p, true, format, dtype, n_sm, &us);
+  *apart = choose(q, false, format, dtype, n_sm, &us_apart);
+  return *form >= 0 && us <= us_apart + 2.0 + (double)p->rows * p->c_in * (dtype == DC_F32 ? 4.5 : 2.5) / 4.5e6;
+}
+
 }  // namespace
+
+extern "C" dc_status dc_q4_plan_query(long long rows, int c_in, int c_out, dc_q4_format format, dc_dtype dtype, int forward, dc_q4_plan *plan) {
+  q4::Layout lx, lw;
+  dc_status s = q4::layout_of(rows, c_in, format, &lx);
+  if (s == DC_OK) s = q4::layout_of(c_out, c_in, format, &lw);
+  if (s != DC_OK) return s;
+  if (!plan || (dtype != DC_F32 && dtype != DC_BF16)) return DC_ERR_INVALID_ARG;
+  const int n_sm = dc_sm_count();
+  Params p = params_of(rows, c_in, c_out, DC_ACT_IDENTITY, dtype, 1.f), q = p;
+  int form = -1, apart;
+  double us;
+  if (!forward || !in_one_launch(&p, &q, format, dtype, n_sm, &form, &apart)) {
+    p = params_of(rows, c_in, c_out, DC_ACT_IDENTITY, dtype, 1.f);
+    form = choose(&p, false, format, dtype, n_sm, &us);
+  }
+  if (form < 0) return DC_ERR_UNSUPPORTED;
+  plan->form = (dc_q4_form)form;
+  plan->launches = forward && form != kRows && form != kStream ? 2 : 1;
+  plan->tile_cols = p.nt;
+  plan->split = p.split;
+  plan->stages = p.stages;
+  plan->accumulators = p.acc_bufs;
+  plan->columns = p.columns;
+  plan->w_stays = p.w_stays;
+  return DC_OK;
+}
 
 extern "C" dc_status dc_q4_workspace_bytes(long long rows, int c_in, dc_q4_format format, size_t *bytes) {
   q4::Layout l;
@@ -1050,10 +1084,8 @@ extern "C" dc_status dc_q4_forward(const void *x, long long rows, int c_in, cons
   p.g6 = 6.f * x_scale;
   Call c = {x, w, &lx, &lw, bias, residual, y, (DcWsHeader *)workspace, dc_sm_count(), (cudaStream_t)stream};
   Params q = params_of(rows, c_in, c_out, act, dtype, scale);
-  // in the product's launch, or in one of its own before it (2 us, and its bytes)
-  double us, us_apart;
-  const int form = choose(&p, true, format, dtype, c.n_sm, &us), apart = choose(&q, false, format, dtype, c.n_sm, &us_apart);
-  if (form >= 0 && us <= us_apart + 2.0 + (double)rows * c_in * (dtype == DC_F32 ? 4.5 : 2.5) / 4.5e6) return run(form, p, format, dtype, c);
+  int form, apart;
+  if (in_one_launch(&p, &q, format, dtype, c.n_sm, &form, &apart)) return run(form, p, format, dtype, c);
   uint8_t *xq = (uint8_t *)workspace + sizeof(DcWsHeader);
   s = dc_q4_quantize(x, rows, c_in, c_in, dtype, format, x_scale, xq, stream);
   if (s != DC_OK) return s;

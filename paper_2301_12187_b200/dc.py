@@ -22,6 +22,7 @@ ACT_IDENTITY, ACT_RELU6 = 0, 1
 ALGO_AUTO, ALGO_TCGEN05, ALGO_SIMT = 0, 1, 2
 MERGE_AUTO, MERGE_STEPS = 0, 1
 MX4, NV4 = 0, 1
+Q4_TILES, Q4_PAIRS, Q4_FEW_ROWS, Q4_STREAM = range(4)
 
 _FP = C.POINTER(C.c_float)
 
@@ -56,6 +57,10 @@ class Block(C.Structure):
 
 class BlockPlan(C.Structure):
     _fields_ = [(name, C.c_int) for name in ("tile_w", "tile_h", "tile_images", "tiles", "chunks", "form", "groups", "operands", "stages")]
+
+
+class Q4Plan(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("form", "launches", "tile_cols", "split", "stages", "accumulators", "columns", "w_stays")]
 
 
 class Q4Layout(C.Structure):
@@ -117,6 +122,7 @@ EXPORTS = {
                                 C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "dc_q4_forward": (C.c_int, [C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_float, C.c_void_p,
                                 C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "dc_q4_plan_query": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(Q4Plan)]),
     "dc_workspace_status": (C.c_int, [C.c_void_p, C.c_void_p]),
     "dc_workspace_status_where": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_uint), C.POINTER(C.c_uint)]),
     "dc_selftest_bounded_wait": (C.c_int, [C.c_void_p, C.c_size_t, C.c_uint, C.c_void_p]),
@@ -633,6 +639,13 @@ def q4_forward(x, w: Q4Matrix, x_scale: float, bias, act, residual, y, workspace
     _check(lib().dc_q4_forward(_ptr(x), rows, w.cols, _ptr(w.data), w.rows, w.fmt, x_scale, w.tensor_scale, _ptr(bias), act,
                                _ptr(residual), _ptr(y), dtype_code(y.dtype), _ptr(workspace),
                                workspace.numel() * workspace.element_size(), _stream(stream)), "dc_q4_forward")
+
+
+def q4_plan(rows: int, c_in: int, c_out: int, fmt: int, dtype: int, forward: bool) -> Q4Plan:
+    """How q4_forward (or q4_product) would run a call of this size; see include/dc.h."""
+    plan = Q4Plan()
+    _check(lib().dc_q4_plan_query(rows, c_in, c_out, fmt, dtype, int(forward), C.byref(plan)), "dc_q4_plan_query")
+    return plan
 
 
 def workspace_status(workspace, stream=None) -> int:

@@ -124,8 +124,12 @@ def test_edges_of_the_formats(fmt):
         assert (have[~odd] == Q.values(code[~odd], byte[~odd], fmt, scale)).all()
 
 
+def matmul64(a, b):
+    return (torch.from_numpy(a).cuda() @ torch.from_numpy(b).cuda().t()).cpu().numpy()
+
+
 def bound(xv, wv, scale_s, ref, dtype, k):
-    s = np.abs(xv) @ np.abs(wv).T
+    s = matmul64(np.abs(xv), np.abs(wv))
     eps = torch.finfo(TYPES[dtype]).eps / 2
     return eps * np.abs(ref) + (k + 3) * 2.0 ** -23 * (s + np.abs(scale_s) + np.abs(ref)) + 1e-37
 
@@ -154,7 +158,7 @@ def run_product(rows, c_in, c_out, fmt, dtype, bias, residual, act, forward, see
     assert dc.workspace_status(ws) == dc.OK
     y.check("result")
     xv, wv = Q.stands_for(np64(x), fmt, gx), Q.stands_for(np64(w), fmt, gw)
-    ref = Q.product(xv, wv, None if b is None else np64(b), None if res is None else np64(res), act == dc.ACT_RELU6)
+    ref = Q.product(xv, wv, None if b is None else np64(b), None if res is None else np64(res), act == dc.ACT_RELU6, matmul64)
     extra = (0 if b is None else np.abs(np64(b))[None, :]) + (0 if res is None else np.abs(np64(res)))
     err = np.abs(np64(y.t) - ref)
     lim = bound(xv, wv, extra, ref, dtype, c_in)
@@ -165,6 +169,16 @@ def run_product(rows, c_in, c_out, fmt, dtype, bias, residual, act, forward, see
     return rel
 
 
+# every form of the products, each with results that begin on 16 bytes and that do not, with residual and without: see test_q4_host.py
+FORMS = [
+    (2000, 4096, 1500), (2100, 6000, 1536), (513, 8192, 2056), (700, 6000, 1101),          # pairs of CTAs
+    (1200, 4100, 1208), (520, 4096, 4099),
+    (1000, 8192, 304), (250, 8192, 130), (70, 9000, 130), (16, 16384, 96), (127, 2600, 512), (3, 5000, 1024),     # tiles shared by clusters
+    (20000, 24, 144), (19111, 200, 520), (30000, 64, 40), (12345, 100, 101), (25000, 300, 136), (9000, 700, 1024),
+    (9100, 1500, 260), (22000, 72, 137), (23001, 520, 255), (20500, 40, 203),
+]
+FORWARD_FORMS = [(1, 256, 136), (8, 3000, 520), (32, 2048, 512), (17, 1001, 130), (2, 16384, 40), (31, 64, 20000), (20000, 24, 144), (40000, 64, 256),
+                 (30001, 40, 16), (25000, 8, 72), (500, 1000, 200)]
 PRODUCTS = [(128, 256, 256), (128, 64, 32), (1, 16, 8), (1, 1, 1), (5, 24, 144), (130, 320, 1280), (257, 1000, 1003), (16, 4096, 512), (1, 8192, 200), (384, 520, 300),
             (1000, 96, 64), (64, 33, 31), (129, 255, 257), (2048, 512, 2048), (3, 700, 40)]
 
@@ -179,7 +193,197 @@ def test_product(rows, c_in, c_out, fmt, dtype):
 
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows,c_in,c_out", FORMS)
+def test_product_in_every_form(rows, c_in, c_out, fmt, dtype):
+    for residual in (False, True):
+        run_product(rows, c_in, c_out, fmt, dtype, bias=not residual, residual=residual, act=dc.ACT_IDENTITY if residual else dc.ACT_RELU6, forward=False,
+                    inplace=residual and rows % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows,c_in,c_out", FORWARD_FORMS)
+def test_forward_in_every_form(rows, c_in, c_out, fmt, dtype):
+    run_product(rows, c_in, c_out, fmt, dtype, bias=True, residual=True, act=dc.ACT_RELU6, forward=True, seed=5)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("rows,c_in,c_out", [(1, 4096, 4096), (2, 24, 144), (7, 1003, 77), (16, 8192, 1024), (33, 640, 640), (64, 256, 1000), (600, 24, 144),
                                              (9, 20000, 64), (1, 40, 3), (300, 200, 72)])
 def test_forward(rows, c_in, c_out, fmt, dtype):
     run_product(rows, c_in, c_out, fmt, dtype, bias=False, residual=True, act=dc.ACT_IDENTITY, forward=True)
+
+
+def test_small_and_ragged_sizes_at_random():
+    r = np.random.default_rng(11)
+    for _ in range(60):
+        rows, c_in, c_out = (int(np.exp(r.uniform(0, np.log(n)))) for n in (700, 1500, 900))
+        run_product(rows, c_in, c_out, int(r.integers(0, 2)), "bf16" if r.random() < 0.6 else "f32", bias=r.random() < 0.5, residual=r.random() < 0.5,
+                    act=int(r.integers(0, 2)), forward=r.random() < 0.5, seed=int(r.integers(0, 1000)))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows,c_in,c_out,forward", [(40, 512, 96, False), (40, 512, 96, True), (300, 4096, 1100, False), (8, 4096, 64, True), (30000, 64, 48, True)])
+def test_nan_and_infinity_stay_in_their_row_and_column(rows, c_in, c_out, forward, fmt):
+    x, w = rand(rows, c_in, 3).cuda(), rand(c_out, c_in, 4, 0.05).cuda()
+    clean_x, clean_w = x.clone(), w.clone()
+    x[rows // 2, c_in // 3], x[1, c_in - 1] = float("inf"), float("nan")
+    w[c_out // 2, 5] = float("-inf")
+    g = 1.0 if fmt == dc.MX4 else 2.0 ** -8
+    out = []
+    for a, b in ((x, w), (clean_x, clean_w)):
+        wq, xq = dc.Q4Matrix(c_out, c_in, fmt, g), dc.Q4Matrix(rows, c_in, fmt, g)
+        dc.q4_quantize(b, wq)
+        y = torch.empty(rows, c_out, device="cuda")
+        ws = torch.zeros(dc.q4_workspace_bytes(rows, c_in, fmt), dtype=torch.uint8, device="cuda")
+        if forward:
+            dc.q4_forward(a, wq, g, None, dc.ACT_IDENTITY, None, y, ws)
+        else:
+            dc.q4_quantize(a, xq)
+            dc.q4_product(xq, wq, None, dc.ACT_IDENTITY, None, y, ws)
+        out.append(y.cpu())
+    bad = torch.zeros(rows, c_out, dtype=torch.bool)
+    bad[[1, rows // 2]] = True
+    bad[:, c_out // 2] = True
+    assert torch.isnan(out[0][bad]).all()
+    assert torch.equal(out[0][~bad], out[1][~bad])
+
+
+def test_results_at_any_16_byte_address():
+    """y, the residual and x may begin on any 16 bytes of a larger buffer."""
+    for rows, c_in, c_out in ((300, 64, 72), (4000, 32, 40), (6, 256, 64)):
+        for off in (8, 24, 56):
+            xbuf = torch.zeros(rows * c_in + 64, dtype=torch.bfloat16, device="cuda")
+            ybuf = torch.full((rows * c_out + 128,), 9.0, dtype=torch.bfloat16, device="cuda")
+            x, y = xbuf[off:off + rows * c_in].view(rows, c_in), ybuf[off:off + rows * c_out].view(rows, c_out)
+            x.copy_(rand(rows, c_in, off, dtype="bf16"))
+            w = rand(c_out, c_in, 2, 0.1).cuda()
+            wq = dc.Q4Matrix(c_out, c_in, dc.MX4)
+            dc.q4_quantize(w, wq)
+            ws = torch.zeros(dc.q4_workspace_bytes(rows, c_in, dc.MX4), dtype=torch.uint8, device="cuda")
+            dc.q4_forward(x, wq, 1.0, None, dc.ACT_IDENTITY, None, y, ws)
+            xv, wv = Q.stands_for(np64(x), dc.MX4), Q.stands_for(np64(w), dc.MX4)
+            ref = Q.product(xv, wv)
+            assert (np.abs(np64(y) - ref) <= bound(xv, wv, 0, ref, "bf16", c_in)).all()
+            assert (ybuf[:off] == 9.0).all() and (ybuf[off + rows * c_out:] == 9.0).all()
+
+
+def layer(c_out, c_in, fmt, seed):
+    w = rand(c_out, c_in, seed, 1.0 / np.sqrt(c_in)).cuda()
+    q = dc.Q4Matrix(c_out, c_in, fmt, 1.0 if fmt == dc.MX4 else dc.q4_tensor_scale(float(w.abs().max())))
+    dc.q4_quantize(w, q)
+    return w, q
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_a_run_of_layers_on_an_nhwc_map(fmt):
+    """Expansion, projection with its skip, and a classifier, as a network calls them: 4-D maps, one workspace, one stream, one graph; each
+    layer is compared with the oracle's on what it really read."""
+    n, h, w, c, hid, classes = 3, 14, 13, 32, 192, 1000
+    g = 1.0 if fmt == dc.MX4 else 2.0 ** -7
+    (we, qe), (wp, qp), (wc, qc) = layer(hid, c, fmt, 1), layer(c, hid, fmt, 2), layer(classes, c, fmt, 3)
+    bias = torch.linspace(-1, 1, hid, device="cuda")
+    x = torch.empty(n, h, w, c, dtype=torch.bfloat16, device="cuda")
+    mid, out = torch.empty(n, h, w, hid, dtype=torch.bfloat16, device="cuda"), torch.empty_like(x)
+    logits = torch.empty(n, classes, dtype=torch.bfloat16, device="cuda")
+    rows = n * h * w
+    ws = torch.zeros(max(dc.q4_workspace_bytes(rows, k, fmt) for k in (c, hid)), dtype=torch.uint8, device="cuda")
+    mq = dc.Q4Matrix(rows, hid, fmt, g)
+
+    def run():
+        dc.q4_forward(x, qe, g, bias, dc.ACT_RELU6, None, mid, ws)
+        dc.q4_quantize(mid, mq)
+        dc.q4_product(mq, qp, None, dc.ACT_IDENTITY, x, out, ws)
+        dc.q4_forward(out[:, 0, 0, :].contiguous(), qc, g, None, dc.ACT_IDENTITY, None, logits, ws)
+
+    def check():
+        xe, em = Q.stands_for(np64(x).reshape(rows, c), fmt, g), Q.stands_for(np64(we), fmt, qe.tensor_scale)
+        ref = Q.product(xe, em, np64(bias), None, True)
+        assert (np.abs(np64(mid).reshape(rows, hid) - ref) <= bound(xe, em, np.abs(np64(bias)), ref, "bf16", c)).all()
+        xm, pm, res = Q.stands_for(np64(mid).reshape(rows, hid), fmt, g), Q.stands_for(np64(wp), fmt, qp.tensor_scale), np64(x).reshape(rows, c)
+        ref = Q.product(xm, pm, None, res)
+        assert (np.abs(np64(out).reshape(rows, c) - ref) <= bound(xm, pm, np.abs(res), ref, "bf16", hid)).all()
+        xc, cm = Q.stands_for(np64(out)[:, 0, 0, :], fmt, g), Q.stands_for(np64(wc), fmt, qc.tensor_scale)
+        ref = Q.product(xc, cm)
+        assert (np.abs(np64(logits) - ref) <= bound(xc, cm, 0, ref, "bf16", c)).all()
+        assert dc.workspace_status(ws) == dc.OK
+
+    x.copy_(rand(rows, c, 7, dtype="bf16").view_as(x))
+    run()
+    check()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        run()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            run()
+    for seed in (8, 9):                          # other inputs through the same graph
+        x.copy_(rand(rows, c, seed, 2.0, dtype="bf16").view_as(x))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check()
+
+
+@pytest.mark.parametrize("rows,c_in,c_out,forward", [(1, 4096, 512, True), (16, 4096, 512, False), (700, 6000, 1100, False), (20000, 24, 144, True),
+                                                     (6272, 320, 1280, False)])
+def test_the_same_bits_every_time_and_beside_other_streams(rows, c_in, c_out, forward):
+    fmt, g = dc.NV4, 2.0 ** -7
+    x, (w, wq) = rand(rows, c_in, 1, dtype="bf16").cuda(), layer(c_out, c_in, fmt, 2)
+    xq = dc.Q4Matrix(rows, c_in, fmt, g)
+    dc.q4_quantize(x, xq)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    ys = [[torch.empty(rows, c_out, dtype=torch.bfloat16, device="cuda") for _ in range(6)] for _ in streams]
+    wss = [torch.zeros(dc.q4_workspace_bytes(rows, c_in, fmt), dtype=torch.uint8, device="cuda") for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(6):
+        for st, y, ws in zip(streams, ys, wss):
+            if forward:
+                dc.q4_forward(x, wq, g, None, dc.ACT_IDENTITY, None, y[i], ws, stream=st)
+            else:
+                dc.q4_product(xq, wq, None, dc.ACT_IDENTITY, None, y[i], ws, stream=st)
+    torch.cuda.synchronize()
+    assert all(dc.workspace_status(ws) == dc.OK for ws in wss)
+    for y in ys:
+        for t in y:
+            assert torch.equal(t, ys[0][0])
+
+
+def test_results_beyond_32_bit_offsets():
+    """More than 2^32 bytes of results, and more than 2^31 elements of a map to quantise."""
+    fmt, rows, c_in, c_out = dc.MX4, 70000, 40, 32768
+    x, (w, wq) = rand(rows, c_in, 1, dtype="bf16").cuda(), layer(c_out, c_in, fmt, 2)
+    y = torch.empty(rows, c_out, dtype=torch.bfloat16, device="cuda")
+    ws = torch.zeros(dc.q4_workspace_bytes(rows, c_in, fmt), dtype=torch.uint8, device="cuda")
+    dc.q4_forward(x, wq, 1.0, None, dc.ACT_IDENTITY, None, y, ws)
+    assert dc.workspace_status(ws) == dc.OK
+    pick = torch.tensor([0, 1, 127, 128, 32768, 65535, 65536, 69871, 69999], device="cuda")
+    xv, wv = Q.stands_for(np64(x[pick]), fmt), Q.stands_for(np64(w), fmt)
+    ref = Q.product(xv, wv)
+    assert (np.abs(np64(y[pick]) - ref) <= bound(xv, wv, 0, ref, "bf16", c_in)).all()
+    q = dc.Q4Matrix(rows, c_out, fmt)
+    dc.q4_quantize(y, q)
+    back = torch.full_like(y, 5.0)
+    dc.q4_dequantize(q, back)
+    assert (np64(back[pick]) == Q.stands_for(np64(y[pick]), fmt)).all()
+    assert int((back == 5.0).all(dim=1).sum()) == 0
+
+
+def test_what_is_not_written_stays():
+    """Results of a call that is refused, and rows behind the last one."""
+    x, (w, wq) = rand(5, 64, 1, dtype="bf16").cuda(), layer(24, 64, dc.MX4, 2)
+    y = torch.full((9, 24), 3.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.zeros(dc.q4_workspace_bytes(5, 64, dc.MX4), dtype=torch.uint8, device="cuda")
+    dc.q4_forward(x, wq, 1.0, None, dc.ACT_IDENTITY, None, y[:5], ws)
+    assert (y[5:] == 3.0).all()
+    with pytest.raises(dc.DcError):
+        dc.q4_forward(x, wq, 1.0, None, 0, None, y[:5], ws[:300])
+    with pytest.raises(dc.DcError):
+        dc.q4_forward(x, wq, 3.0, None, 0, None, y[:5], ws)
+    with pytest.raises(ValueError):
+        dc.q4_forward(x.cpu(), wq, 1.0, None, 0, None, y[:5], ws)
+    torch.cuda.synchronize()
+    assert (y[5:] == 3.0).all()

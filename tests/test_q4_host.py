@@ -185,3 +185,52 @@ def test_unpack_places_scales_as_the_header_says():
     buf[7 * lay.pitch + 3] = 0xA5
     code, byte = Q.unpack(buf, rows, cols, fmt)
     assert (byte[:rows, :13] == want).all() and code[7, 6] == 5 and code[7, 7] == 10
+
+
+def test_plans():
+    q = dc.q4_plan
+    # few rows: in the product's launch, a cluster to a tile where tiles alone would leave SMs idle; many rows: apart, except of narrow layers
+    p = q(1, 4096, 4096, dc.NV4, dc.BF16, True)
+    assert p.form == dc.Q4_FEW_ROWS and p.launches == 1 and p.split > 1
+    assert q(64, 4096, 4096, dc.NV4, dc.BF16, True).launches == 2
+    assert q(16, 8192, 8192, dc.MX4, dc.BF16, True).launches == 2
+    p = q(200704, 24, 144, dc.MX4, dc.BF16, True)
+    assert p.form == dc.Q4_STREAM and p.launches == 1 and p.tile_cols == 144 and p.w_stays
+    p = q(8192, 8192, 8192, dc.NV4, dc.BF16, False)
+    assert p.form == dc.Q4_PAIRS and p.tile_cols == 256 and p.stages >= 5
+    p = q(6272, 320, 1280, dc.MX4, dc.BF16, False)
+    assert p.form == dc.Q4_TILES and p.accumulators == 3 and p.columns and p.w_stays
+    assert status_of(q, 0, 8, 8, dc.MX4, dc.BF16, False) == dc.ERR_INVALID_ARG
+    assert status_of(q, 8, 8, 8, dc.MX4, 5, False) == dc.ERR_INVALID_ARG
+    assert dc.lib().dc_q4_plan_query(8, 8, 8, 0, 1, 0, None) == dc.ERR_INVALID_ARG
+
+
+def test_every_size_has_a_plan():
+    r = np.random.default_rng(1)
+    for _ in range(4000):
+        rows, c_in, c_out = (int(np.exp(r.uniform(0, np.log(n)))) for n in (1 << 24, 1 << 17, 1 << 17))
+        for fmt in (dc.MX4, dc.NV4):
+            for dtype in (dc.F32, dc.BF16):
+                for forward in (False, True):
+                    p = dc.q4_plan(rows, c_in, c_out, fmt, dtype, forward)
+                    assert p.stages >= 2 and 1 <= p.split <= 8 and p.tile_cols in range(16, 257, 16), (rows, c_in, c_out, fmt, dtype)
+                    assert p.accumulators * p.tile_cols <= 512 - 32
+
+
+def test_the_gpu_tests_reach_every_form():
+    torch = pytest.importorskip("torch")
+    from tests import test_gpu_q4 as t
+    seen = {}
+    for rows, c_in, c_out in t.FORMS + t.PRODUCTS:
+        for fmt in (dc.MX4, dc.NV4):
+            for dtype in (dc.F32, dc.BF16):
+                p = dc.q4_plan(rows, c_in, c_out, fmt, dtype, False)
+                whole = c_out * (4 if dtype == dc.F32 else 2) % 16 == 0
+                for what in ("pairs %d" % p.tile_cols if p.form == dc.Q4_PAIRS else "split" if p.split > 1 else "tiles %d" % p.accumulators,
+                             "columns, w %s" % ("stays" if p.w_stays else "not") if p.columns else "", "two scale tiles" if p.tile_cols > 128 else ""):
+                    seen.setdefault((what, whole), (rows, c_in, c_out))
+    for what in ("pairs 256", "split", "tiles 1", "tiles 3", "columns, w stays", "two scale tiles"):
+        for whole in (False, True):
+            assert (what, whole) in seen, (what, whole)
+    forms = {dc.q4_plan(r, i, o, f, d, True).form for r, i, o in t.FORWARD_FORMS for f in (0, 1) for d in (0, 1)}
+    assert {dc.Q4_FEW_ROWS, dc.Q4_STREAM, dc.Q4_TILES} <= forms

@@ -312,25 +312,6 @@ __device__ __forceinline__ void deliver_columns(const Params &p, float b, const 
   }
 }
 
-// 16 columns of a row of x from column c: the values, zeros from column c_in on
-template <typename T>
-__device__ __forceinline__ void load_x16(const T *__restrict__ row, int c, int c_in, int vec, float *v) {
-  if (vec && c + 16 <= c_in) {
-#pragma unroll
-    for (int i = 0; i < 16 / kPer<T>; ++i) unpack16<T>(__ldg(reinterpret_cast<const uint4 *>(row + c) + i), v + i * kPer<T>);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16 / kPer<T>; ++i) {
-      const int o = c + i * kPer<T>;
-      if (vec && o + kPer<T> <= c_in) {
-        unpack16<T>(__ldg(reinterpret_cast<const uint4 *>(row + o)), v + i * kPer<T>);
-      } else {
-#pragma unroll
-        for (int j = 0; j < kPer<T>; ++j) v[i * kPer<T> + j] = o + j < c_in ? (float)row[o + j] : 0.f;
-      }
-    }
-  }
-}
 // largest magnitude of 16 values, its bits as fp32
 template <typename T>
 __device__ __forceinline__ uint32_t largest16(const uint4 *raw) {
@@ -381,26 +362,19 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sm = (smem_u32(smem_raw) + 1023u) & ~1023u;
   if (warp == 0) {
-    if (lane == 0) {
-      abort_s = 0;
-      for (int i = 0; i < kMaxStages; ++i) {
-        mbar_init(&bar[kFull + i], FORM == kStream ? kCutWarps + (p.w_stays ? 0 : 1) : 1);
-        mbar_init(&bar[kEmpty + i], 1);
-      }
-      for (int i = 0; i < kMaxAcc; ++i) {
-        mbar_init(&bar[kDFull + i], 1);
-        mbar_init(&bar[kDEmpty + i], (P ? 2 : 1) * kEpi<FORM> / p.acc_bufs);
-      }
-      mbar_init(&bar[kXFull], kEpi<FORM>);
-      mbar_init(&bar[kWFull], 1);
-      mbar_init(&bar[kParts], (uint32_t)(p.split * kEpi<FORM>));
-      for (int i = 0; i < kEpi<FORM>; ++i) mbar_init(&bar[kRes + i], 1);
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      prefetch_tensormap(&map_w);
-      prefetch_tensormap(&map_sw);
-      if (FORM == kOne || P) { prefetch_tensormap(&map_x); prefetch_tensormap(&map_sx); }
+    // a lane to a barrier: one after the other they took 0.4 us
+    for (int i = lane; i < kBars; i += 32) {
+      const uint32_t arrivals = i < kEmpty ? (FORM == kStream ? kCutWarps + (p.w_stays ? 0 : 1) : 1)
+                                : i >= kDEmpty && i < kXFull ? (P ? 2 : 1) * kEpi<FORM> / p.acc_bufs
+                                : i == kXFull ? kEpi<FORM> : i == kParts ? p.split * kEpi<FORM> : 1;
+      mbar_init(&bar[i], arrivals);
     }
+    if (lane == 0) abort_s = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
+  } else if (warp == 1 && lane < 4) {
+    if (lane < 2) prefetch_tensormap(lane ? &map_sw : &map_w);
+    else if (FORM == kOne || P) prefetch_tensormap(lane == 2 ? &map_x : &map_sx);
   }
   const bool parts = FORM != kPair && FORM != kStream && p.split > 1;
   if (parts) asm volatile("barrier.cluster.arrive.release;" ::: "memory");     // this CTA is there, its barriers too: waited for before the parts go out
@@ -521,17 +495,37 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     if (FORM == kRows) {
       // the whole rows, as far as this CTA multiplies them, in pieces of 16 columns
       const int segs = (min(p.c_in - c0 * kStageCols, (c1 - c0) * kStageCols) + 63) / 64 * 4, total = (int)p.rows * segs;
-      for (int u0 = (warp - 2) * 32; u0 < total; u0 += kEpi<FORM> * 32) {
-        const int u = u0 + lane, row = u / segs, seg = u - row * segs;
-        float v[16];
-        const bool valid = u < total;
-        if (valid) {
-          load_x16<T>(x + (size_t)row * (size_t)p.c_in, c0 * kStageCols + seg * 16, p.c_in, p.vec_x, v);
-        } else {
+      constexpr int kRaw = 16 / kPer<T>, kStep = kEpi<FORM> * 32;
+      uint4 next[2][kRaw];                       // the next two pieces of this thread, on their way
+      auto ask = [&](int k, int u) {
+        const int row = u / segs, col = c0 * kStageCols + (u - row * segs) * 16;
+        const uint4 *at = reinterpret_cast<const uint4 *>(x + (size_t)row * (size_t)p.c_in + col);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = 0.f;
+        for (int i = 0; i < kRaw; ++i) next[k][i] = u < total && col + i * kPer<T> < p.c_in ? __ldg(at + i) : make_uint4(0, 0, 0, 0);
+      };
+      const int u_first = (warp - 2) * 32 + lane;
+      if (p.vec_x) {
+        ask(0, u_first);
+        ask(1, u_first + kStep);
+      }
+#pragma unroll 1
+      for (int u = u_first; u - lane < total; u += 2 * kStep) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int uk = u + k * kStep, row = uk / segs, seg = uk - row * segs;
+          if (uk - lane >= total) break;         // the same for all lanes
+          float v[16];
+          if (p.vec_x) {
+#pragma unroll
+            for (int i = 0; i < kRaw; ++i) unpack16<T>(next[k][i], v + i * kPer<T>);
+            ask(k, uk + 2 * kStep);
+          } else {
+            const int col = c0 * kStageCols + seg * 16;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = uk < total && col + i < p.c_in ? (float)x[(size_t)row * (size_t)p.c_in + col + i] : 0.f;
+          }
+          put_x16<F>(v, p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, uk < total);
         }
-        put_x16<F>(v, p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, valid);
       }
       fence_proxy_async();
       __syncwarp();
@@ -612,11 +606,12 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             // columns to the CTA that owns them
             constexpr int N = kPer<T>;
             const uint32_t from = sm + (uint32_t)(p.off_out + (rank * p.part_rows + quad * 32 + lane) * p.part_cols * 4);
+            int owner = c / p.part_cols, at = c - owner * p.part_cols;         // of the next columns: whose, and their place there
 #pragma unroll
-            for (int i = 0; i < kCols / N; ++i)
+            for (int i = 0; i < kCols / N; ++i, at += N)
               if (c + i * N < p.nt) {
-                const int owner = (c + i * N) / p.part_cols;
-                const uint32_t to = map_cluster(from + (uint32_t)((c + i * N - owner * p.part_cols) * 4), (uint32_t)owner);
+                if (at == p.part_cols) { at = 0; ++owner; }
+                const uint32_t to = map_cluster(from + (uint32_t)(at * 4), (uint32_t)owner);
 #pragma unroll
                 for (int j = 0; j < N; j += 4) {
                   const float *u = v[(i * N + j) / 32] + (i * N + j) % 32;

@@ -377,9 +377,9 @@ dc_status dc_chain_forward_host_async(const dc_layer *layers, int n_layers, cons
  * which both operands of a product reduce over.  Each value is a code of 4 bits, e2m1 -- sign, then 0, 0.5, 1, 1.5, 2, 3, 4 or 6 --
  * times the scale of its block of columns; the last block of a row may be shorter.  With a = the block's largest magnitude:
  *   DC_MX4: blocks of 32, scale 2^e, e = floor(log2 a) - 2, at least -127, held as the byte e + 127 (e8m0).
- *   DC_NV4: blocks of 16, scale s g: s = a / (6 g) rounded to e4m3 (448 at most), g = `tensor_scale`, a power of two for the whole matrix.
- * A value's code is the nearest to value / scale, ties to the code with an even last bit, 6 at most.  The quotients decide as in real
- * arithmetic, so the codes are a function of the values alone.  A block with a NaN or an infinity gets the scale NaN: all of it
+ *   DC_NV4: blocks of 16, scale s g: s = a times the fp32 number 1 / (6 g), rounded to fp32, then to e4m3 (448 at most; nearest, ties to even),
+ *   g = `tensor_scale`, a power of two for the whole matrix.
+ * A value's code is the nearest to value / scale in real arithmetic, ties to the code with an even last bit, 6 at most.  A block with a NaN or an infinity gets the scale NaN: all of it
  * reads as NaN, and so do the results of its row (a NaN leaves DC_ACT_RELU6 as 0, or as 6 in bf16).  A block whose scale is 0 (a / (6 g) up to 2^-10) reads as 0.
  * --------------------------------------------------------------------------------------------- */
 typedef enum { DC_MX4 = 0, DC_NV4 = 1 } dc_q4_format;

@@ -41,7 +41,8 @@ def quantize(x, fmt, g=1.0):
         byte, scale = (e + 127).astype(np.int64), np.ldexp(1.0, e)
         byte = np.where(odd, 255, byte)
     else:
-        byte = nearest(top / (6.0 * g), E4M3)     # a quotient of 24 by 25 bits in 64 decides as the exact one
+        with np.errstate(over="ignore"):
+            byte = nearest((np.float32(top) * (np.float32(1) / np.float32(6.0 * g))).astype(np.float64), E4M3)     # in fp32, as the format is defined
         scale = E4M3[byte] * g
         byte = np.where(odd, 127, byte)
     with np.errstate(divide="ignore", invalid="ignore"):

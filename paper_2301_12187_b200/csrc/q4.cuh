@@ -86,7 +86,7 @@ struct BlockScale {
   bool cut;                  // values beyond 7 p: cut them before the division, which would overflow
 };
 template <int F>
-__device__ __forceinline__ BlockScale block_scale(uint32_t top, float g, float g6) {
+__device__ __forceinline__ BlockScale block_scale(uint32_t top, float g, float r6) {
   BlockScale s;
   if (F == DC_MX4) {
     const uint32_t e = top >> 23;
@@ -95,34 +95,76 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t top, float g, float g
     s.r = e == 255u ? 0.f : __uint_as_float((254u - s.byte) << 23);
     s.cut = false;
   } else {
-    // The quotient, rounded to fp32, lies on the same side of every border of e4m3 as the exact one, or on the border with it: a border
-    // times 6 g has at most 7 significant bits, `top` has 24, so where they differ they do by more than the rounding of the quotient.
-    // The same holds for value / (s g) and the borders of e2m1.
+    // A product with 1 / (6 g), rounded, in the place of a division.  6 g is three times a power of two, and the rounded third is 2^-25 of it above a
+    // third: where `top` is 6 g times a border of e4m3 the product rounds to the border itself, and the tie is seen as one.  Of bf16 values every
+    // scale is so the one of real arithmetic (other quotients are 2^-8 from a border), of fp32 values those further than 2^-23 from one.
+    // value / (s g) is divided: its quotient, rounded to fp32, lies on the same side of every border of e2m1 as the exact one, or on the border with
+    // it, since a border times s g has at most 7 significant bits and the value 24.
     const bool odd = top >= 0x7f800000u;
-    s.byte = odd ? 0x7fu : e4m3_of(__fdiv_rn(__uint_as_float(top), g6));
+    s.byte = odd ? 0x7fu : e4m3_of(__uint_as_float(top) * r6);
     s.p = odd ? 0.f : e4m3_value(s.byte) * g;
     s.r = s.p > 0.f ? __frcp_rn(s.p) : 0.f;
     s.cut = __uint_as_float(top) > 7.f * s.p;
   }
   return s;
 }
-// sixteen values -> their codes, in two words.  Values of a block whose scale is NaN get some code.
-template <int F>
+// the largest magnitude of three numbers, NaN if one of them is
+__device__ __forceinline__ float largest3(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// of sixteen values; its bits
+__device__ __forceinline__ uint32_t largest16(const float *v) {
+  const float a = largest3(v[0], v[1], v[2]), b = largest3(v[3], v[4], v[5]), c = largest3(v[6], v[7], v[8]), d = largest3(v[9], v[10], v[11]),
+              e = largest3(v[12], v[13], v[14]);
+  return __float_as_uint(largest3(largest3(a, b, c), largest3(d, e, v[15]), 0.f));
+}
+// pairs of floats in one instruction
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void unpair(uint64_t d, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+// sixteen values -> their codes, in two words.  Values of a block whose scale is NaN get some code.  BF16: they are bf16 numbers.
+template <int F, bool BF16>
 __device__ __forceinline__ uint2 codes16(float *v, const BlockScale &s) {
-  if (F == DC_MX4) {
+  if (F == DC_NV4 && s.cut) {
+    const float m = 7.f * s.p;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] *= s.r;    // exact
-  } else {
-    if (s.cut) {
-      const float m = 7.f * s.p;
+    for (int i = 0; i < 16; ++i) v[i] = fminf(fmaxf(v[i], -m), m);
+  }
+  const uint64_t r = pair(s.r, s.r), p = pair(-s.p, -s.p);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = fminf(fmaxf(v[i], -m), m);
+  for (int i = 0; i < 16; i += 2) {
+    const uint64_t x = pair(v[i], v[i + 1]);
+    uint64_t u;
+    if (F == DC_MX4) {
+      u = mul2(x, r);                            // exact
+    } else if (BF16) {
+      // x r on a grid of 2^-14 (768 has that unit in its last place): a quotient is a border of e2m1, which the grid has, or at least 2^-11 from all
+      u = add2(fma2(x, r, pair(768.f, 768.f)), pair(-768.f, -768.f));
+    } else {
+      u = mul2(x, r);                            // x / p rounded: one step of Newton's method from x r
+      u = fma2(fma2(u, p, x), r, u);
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {               // v / p rounded: one step of Newton's method from v * r
-      const float u = v[i] * s.r;
-      v[i] = fmaf(fmaf(-u, s.p, v[i]), s.r, u);
-    }
+    unpair(u, v[i], v[i + 1]);
   }
   return make_uint2(codes8(v), codes8(v + 8));
 }

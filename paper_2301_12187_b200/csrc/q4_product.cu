@@ -43,7 +43,7 @@ struct Params {
   long long rows;
   int c_in, c_out, act;
   float scale;
-  float g, g6;               // kRows, kStream: x's tensor scale
+  float g, r6;               // kRows, kStream: x's tensor scale
   int nt, nb;                // rows of w in a tile, 128-row scale tiles that they touch
   int tiles_m, tiles_n, items;
   int chunks;                // stages of a row
@@ -325,14 +325,12 @@ __device__ __forceinline__ uint32_t largest16(const uint4 *raw) {
   return sizeof(T) == 2 ? max(top & 0xffff0000u, top << 16) : top;
 }
 // 16 columns, piece `seg` of a row, -> codes in an operand's rows and the block's scale in its tile.  `top`: largest magnitude of the piece.
-template <int F>
+template <int F, typename T>
 __device__ __forceinline__ void put_x16(float *v, const Params &p, uint32_t a, uint32_t sfa, int row, int seg, bool valid) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  uint32_t top = q4::largest16(v);
   if (F == DC_MX4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  const q4::BlockScale s = q4::block_scale<F>(top, p.g, p.g6);
-  const uint2 code = q4::codes16<F>(v, s);
+  const q4::BlockScale s = q4::block_scale<F>(top, p.g, p.r6);
+  const uint2 code = q4::codes16<F, sizeof(T) == 2>(v, s);
   if (valid) {
     const uint32_t at = a + (uint32_t)((row >> 3) * 1024 + (row & 7) * 128 + ((((seg & 15) >> 1) ^ (row & 7)) * 16) + (seg & 1) * 8);
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(code.x), "r"(code.y) : "memory");
@@ -524,7 +522,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = uk < total && col + i < p.c_in ? (float)x[(size_t)row * (size_t)p.c_in + col + i] : 0.f;
           }
-          put_x16<F>(v, p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, uk < total);
+          put_x16<F, T>(v, p, sm + (uint32_t)((seg >> 4) * p.a_bytes), sm + (uint32_t)p.off_sfa, row, seg, uk < total);
         }
       }
       fence_proxy_async();
@@ -738,8 +736,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           float v[16];
 #pragma unroll
           for (int i = 0; i < kRaw / 2; ++i) unpack16<T>(raw[h * kRaw / 2 + i], v + i * kPer<T>);
-          const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.g6);
-          code[h] = q4::codes16<F>(v, s);
+          const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.r6);
+          code[h] = q4::codes16<F, sizeof(T) == 2>(v, s);
           byte[h] = s.byte;
         }
         sts_u4(a + (uint32_t)(((c >> 5) ^ (r & 7)) * 16), make_uint4(code[0].x, code[0].y, code[1].x, code[1].y));
@@ -997,7 +995,8 @@ Params params_of(long long rows, int c_in, int c_out, dc_act act, dc_dtype dtype
   p.c_out = c_out;
   p.act = (int)act;
   p.scale = scale;
-  p.g = p.g6 = 1.f;
+  p.g = 1.f;
+  p.r6 = 1.f / 6.f;
   p.chunks = dc_div_up(c_in, kStageCols);
   const size_t es = dtype == DC_F32 ? 4 : 2;
   p.vec = (size_t)c_out * es % 16 == 0;
@@ -1076,7 +1075,7 @@ extern "C" dc_status dc_q4_forward(const void *x, long long rows, int c_in, cons
   if (workspace_bytes < sizeof(DcWsHeader) + lx.bytes) return DC_ERR_WORKSPACE;
   Params p = params_of(rows, c_in, c_out, act, dtype, scale);
   p.g = x_scale;
-  p.g6 = 6.f * x_scale;
+  p.r6 = 1.f / (6.f * x_scale);
   Call c = {x, w, &lx, &lw, bias, residual, y, (DcWsHeader *)workspace, dc_sm_count(), (cudaStream_t)stream};
   Params q = params_of(rows, c_in, c_out, act, dtype, scale);
   int form, apart;

@@ -19,7 +19,7 @@ struct Params {
   int segs, segs_log2;       // 16-column pieces of a row that a CTA takes; their log2 where rows go through shared memory
   int vec;                   // rows begin on 16 bytes: whole pieces are loaded and stored in 16-byte words
   int groups;                // CTAs that share 128 rows: 1 or 4
-  float g, g6;
+  float g, r6;
   uint32_t pitch, tiles, col_tiles;
   size_t scale_offset;
 };
@@ -75,8 +75,8 @@ __global__ void __launch_bounds__(kThreads, VEC ? 4 : 3) k_q4_quantize(const T *
   const bool wanted = c < (int)(p.pitch * 2) && mine < step;
   auto put = [&](int r, uint32_t top, float *v) {
     if (F == DC_MX4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const BlockScale s = block_scale<F>(top, p.g, p.g6);
-    const uint2 code = codes16<F>(v, s);
+    const BlockScale s = block_scale<F>(top, p.g, p.r6);
+    const uint2 code = codes16<F, sizeof(T) == 2>(v, s);
     if (r < rows && wanted) {
       *reinterpret_cast<uint2 *>(q + (size_t)(row0 + r) * p.pitch + (c >> 1)) = code;
       if (c < p.cols && (F == DC_NV4 || (seg & 1) == 0)) {
@@ -116,18 +116,10 @@ __global__ void __launch_bounds__(kThreads, VEC ? 4 : 3) k_q4_quantize(const T *
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (u > 0 && r + u * step - mine >= most) break;       // the same for all threads
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-          const uint32_t w[4] = {raw[u][i].x, raw[u][i].y, raw[u][i].z, raw[u][i].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) top = sizeof(T) == 2 ? __vmaxu2(top, w[j] & 0x7fff7fffu) : max(top, w[j] & 0x7fffffffu);
-        }
-        if (sizeof(T) == 2) top = max(top & 0xffff0000u, top << 16);
         float v[16];
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) unpack<T>(raw[u][i], v + i * kPer<T>);
-        put(r + u * step, top, v);
+        put(r + u * step, largest16(v), v);
       }
     }
   } else {
@@ -143,13 +135,9 @@ __global__ void __launch_bounds__(kThreads, VEC ? 4 : 3) k_q4_quantize(const T *
       }
       __syncthreads();
       float v[16];
-      uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        v[i] = staged(mine, seg * 16 + i, span_log2);
-        top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-      }
-      put(r0 + mine, top, v);
+      for (int i = 0; i < 16; ++i) v[i] = staged(mine, seg * 16 + i, span_log2);
+      put(r0 + mine, largest16(v), v);
       __syncthreads();
     }
   }
@@ -256,7 +244,7 @@ dc_status prepare(const void *x, long long rows, int cols, long long stride, dc_
   while ((16 << p->segs_log2) < kCols && (16 << p->segs_log2) < cols) ++p->segs_log2;
   p->vec = stride % (long long)(16 / es) == 0;
   p->g = g;
-  p->g6 = 6.f * g;
+  p->r6 = 1.f / (6.f * g);
   p->pitch = (uint32_t)l.pitch;
   p->tiles = (uint32_t)l.tiles;
   p->scale_offset = l.scale_offset;

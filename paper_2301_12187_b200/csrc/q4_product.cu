@@ -552,114 +552,125 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         __syncwarp();
       }
       bool ok = true;
+      // A pair reads all of a warp's columns before it works on them: its one accumulator is then free for the next tile's products.
+      constexpr int kAhead = P ? 128 / kCols : 1;
 #pragma unroll 1
-      for (int c = c_first; c < cols || c == c_first; c += c_step) {
-        const bool last = c + c_step >= cols;
-        const int col = tn * p.nt + c;
-        const uint32_t out = out0 + turn * kOutBytes, mine = out + (uint32_t)lane * 128u;
-        auto wait_out = [&]() {                  // what this buffer held is read
-          if (p.out_bufs == 2) bulk_wait_read1();
-          else bulk_wait_read0();
-        };
-        if (P && work) {
-          const float b0 = bias && c + lane < cols ? __ldg(bias + col + lane) : 0.f, b1 = bias && c + 32 + lane < cols ? __ldg(bias + col + 32 + lane) : 0.f;
-          bias_s[warp - 2][lane] = b0;
-          bias_s[warp - 2][lane + 32] = b1;
-          __syncwarp();
-        }
-        if (staged && residual) {                // the results before these have been read: the residual to their place
-          if (elect_one()) {
-            wait_out();
-            mbar_arrive_expect_tx(&bar[kRes + warp - 2], kOutBytes);
-            tma_load_2d(out, &map_res, &bar[kRes + warp - 2], col, (int)row0);
+      for (int cc = c_first; cc < cols || cc == c_first; cc += kAhead * c_step) {
+        float va[kAhead][kHalves][32];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int c = cc + k * c_step, col = tn * p.nt + c;
+          const bool here = work && c < cols;
+          float (*v)[32] = va[k];
+          const uint32_t out = out0 + turn * kOutBytes, mine = out + (uint32_t)lane * 128u;
+          auto wait_out = [&]() {                // what this buffer held is read
+            if (p.out_bufs == 2) bulk_wait_read1();
+            else bulk_wait_read0();
+          };
+          if (P && here) {
+            const float b0 = bias && c + lane < cols ? __ldg(bias + col + lane) : 0.f, b1 = bias && c + 32 + lane < cols ? __ldg(bias + col + 32 + lane) : 0.f;
+            bias_s[warp - 2][lane] = b0;
+            bias_s[warp - 2][lane + 32] = b1;
+            __syncwarp();
           }
-          __syncwarp();
-        }
-        if (c == c_first) {
-          ok = warp_wait(&bar[kDFull + buf], use & 1u, abort_flag, ws, 0x40000u | (uint32_t)buf);
-          if (!ok) break;
-          tc_fence_after();
-        }
-        float v[kHalves][32];
-        if (work) {
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h)
-            if (h == 0 || c + 32 < cols) tmem_ld32(d + (uint32_t)(c + h * 32), reinterpret_cast<uint32_t *>(v[h]));
-          tmem_ld_wait();
-        }
-        if (last) {                              // the accumulator is read: the next tile may have it
-          tc_fence_before();
-          __syncwarp();
-          if (elect_one()) {
-            if (P) arrive_cluster(freed + (uint32_t)(buf * 8));
-            else mbar_arrive(&bar[kDEmpty + buf]);
+          if (staged && c < cols && residual) {  // the results before these have been read: the residual to their place
+            if (elect_one()) {
+              wait_out();
+              mbar_arrive_expect_tx(&bar[kRes + warp - 2], kOutBytes);
+              tma_load_2d(out, &map_res, &bar[kRes + warp - 2], col, (int)row0);
+            }
+            __syncwarp();
           }
-          __syncwarp();
-        }
-        if (!work) continue;
-        if (parts) {
-          if (!met) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-          met = true;
-          if (row0 + lane < p.rows) {
-            // columns to the CTA that owns them
-            constexpr int N = kPer<T>;
-            const uint32_t from = sm + (uint32_t)(p.off_out + (rank * p.part_rows + quad * 32 + lane) * p.part_cols * 4);
-            int owner = c / p.part_cols, at = c - owner * p.part_cols;         // of the next columns: whose, and their place there
+          if (k == 0) {
+            if (cc == c_first) {
+              ok = warp_wait(&bar[kDFull + buf], use & 1u, abort_flag, ws, 0x40000u | (uint32_t)buf);
+              if (!ok) break;
+              tc_fence_after();
+            }
+            if (work) {
 #pragma unroll
-            for (int i = 0; i < kCols / N; ++i, at += N)
-              if (c + i * N < p.nt) {
-                if (at == p.part_cols) { at = 0; ++owner; }
-                const uint32_t to = map_cluster(from + (uint32_t)(at * 4), (uint32_t)owner);
+              for (int a = 0; a < kAhead; ++a)
 #pragma unroll
-                for (int j = 0; j < N; j += 4) {
-                  const float *u = v[(i * N + j) / 32] + (i * N + j) % 32;
-                  sts_cluster_f4(to + (uint32_t)(j * 4), u[0], u[1], u[2], u[3]);
-                }
+                for (int h = 0; h < kHalves; ++h)
+                  if (cc + a * c_step + h * 32 < cols) tmem_ld32(d + (uint32_t)(cc + a * c_step + h * 32), reinterpret_cast<uint32_t *>(va[a][h]));
+              tmem_ld_wait();
+            }
+            if (cc + kAhead * c_step >= cols) {  // the accumulator is read: the next tile may have it
+              tc_fence_before();
+              __syncwarp();
+              if (elect_one()) {
+                if (P) arrive_cluster(freed + (uint32_t)(buf * 8));
+                else mbar_arrive(&bar[kDEmpty + buf]);
               }
+              __syncwarp();
+            }
           }
-        } else if (p.vec) {
-          const uint32_t bias_c = bias_w + (P ? 0u : (uint32_t)(c * 4));
-          const int halves = c + 32 < cols ? 2 : 1;
-          if (residual) {
-            ok = warp_wait(&bar[kRes + warp - 2], res_parity, abort_flag, ws, 0xA0000u | (uint32_t)warp);
-            if (!ok) break;
-            res_parity ^= 1u;
-            if (p.act == DC_ACT_RELU6) finish<T, kHalves, true, true>(p.scale, bias_c, v, mine, swap, halves);
-            else finish<T, kHalves, true, false>(p.scale, bias_c, v, mine, swap, halves);
-          } else {
-            if (elect_one()) wait_out();
+          if (!here) continue;
+          if (parts) {
+            if (!met) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+            met = true;
+            if (row0 + lane < p.rows) {
+              // columns to the CTA that owns them
+              constexpr int N = kPer<T>;
+              const uint32_t from = sm + (uint32_t)(p.off_out + (rank * p.part_rows + quad * 32 + lane) * p.part_cols * 4);
+              int owner = c / p.part_cols, at = c - owner * p.part_cols;         // of the next columns: whose, and their place there
+#pragma unroll
+              for (int i = 0; i < kCols / N; ++i, at += N)
+                if (c + i * N < p.nt) {
+                  if (at == p.part_cols) { at = 0; ++owner; }
+                  const uint32_t to = map_cluster(from + (uint32_t)(at * 4), (uint32_t)owner);
+#pragma unroll
+                  for (int j = 0; j < N; j += 4) {
+                    const float *u = v[(i * N + j) / 32] + (i * N + j) % 32;
+                    sts_cluster_f4(to + (uint32_t)(j * 4), u[0], u[1], u[2], u[3]);
+                  }
+                }
+            }
+          } else if (p.vec) {
+            const uint32_t bias_c = bias_w + (P ? 0u : (uint32_t)(c * 4));
+            const int halves = c + 32 < cols ? 2 : 1;
+            if (residual) {
+              ok = warp_wait(&bar[kRes + warp - 2], res_parity, abort_flag, ws, 0xA0000u | (uint32_t)warp);
+              if (!ok) break;
+              res_parity ^= 1u;
+              if (p.act == DC_ACT_RELU6) finish<T, kHalves, true, true>(p.scale, bias_c, v, mine, swap, halves);
+              else finish<T, kHalves, true, false>(p.scale, bias_c, v, mine, swap, halves);
+            } else {
+              if (elect_one()) wait_out();
+              __syncwarp();
+              if (p.act == DC_ACT_RELU6) finish<T, kHalves, false, true>(p.scale, bias_c, v, mine, swap, halves);
+              else finish<T, kHalves, false, false>(p.scale, bias_c, v, mine, swap, halves);
+            }
+            fence_proxy_async();
             __syncwarp();
-            if (p.act == DC_ACT_RELU6) finish<T, kHalves, false, true>(p.scale, bias_c, v, mine, swap, halves);
-            else finish<T, kHalves, false, false>(p.scale, bias_c, v, mine, swap, halves);
-          }
-          fence_proxy_async();
-          __syncwarp();
-          if (elect_one()) {
-            tma_store_2d(&map_y, out, col, (int)row0);
-            bulk_commit();
-          }
-          __syncwarp();
-          if (p.out_bufs == 2) turn ^= 1u;
-        } else if (FORM != kStream) {            // (which is for rows of y that begin on 16 bytes)
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float *u = v[h] + i * 4;
-              sts_u4(mine + ((uint32_t)i ^ swap) * 16u, make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3])));
+            if (elect_one()) {
+              tma_store_2d(&map_y, out, col, (int)row0);
+              bulk_commit();
             }
             __syncwarp();
-            const int o = c + h * 32 + lane;
-            if (o < cols) {
-              const size_t to = (size_t)row0 * (size_t)p.c_out + (size_t)(tn * p.nt + o);
-              const int rows = p.rows - row0 < 32 ? (int)(p.rows - row0) : 32;
-              const float b = bias_s[warp - 2][P ? o - c : o];
-              if (residual) deliver_columns<T, true>(p, b, residual + to, y + to, rows, out, lane);
-              else deliver_columns<T, false>(p, b, nullptr, y + to, rows, out, lane);
+            if (p.out_bufs == 2) turn ^= 1u;
+          } else if (FORM != kStream) {            // (which is for rows of y that begin on 16 bytes)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float *u = v[h] + i * 4;
+                sts_u4(mine + ((uint32_t)i ^ swap) * 16u, make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3])));
+              }
+              __syncwarp();
+              const int o = c + h * 32 + lane;
+              if (o < cols) {
+                const size_t to = (size_t)row0 * (size_t)p.c_out + (size_t)(tn * p.nt + o);
+                const int rows = p.rows - row0 < 32 ? (int)(p.rows - row0) : 32;
+                const float b = bias_s[warp - 2][P ? o - c : o];
+                if (residual) deliver_columns<T, true>(p, b, residual + to, y + to, rows, out, lane);
+                else deliver_columns<T, false>(p, b, nullptr, y + to, rows, out, lane);
+              }
+              __syncwarp();
             }
-            __syncwarp();
           }
         }
+        if (!ok) break;
       }
       if (!ok) break;
     }
@@ -902,7 +913,7 @@ bool lay_out(Params *p, int form, int format, int dtype, int n_sm) {
 double estimate(const Params &p, int form, int dtype, int n_sm) {
   static constexpr int kClusters[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};    // of that many CTAs that run at once, on 148 SMs
   const double wide = p.nt / 128.0, type = dtype == DC_F32 ? 1.8 : 1.0;
-  const double stage = form == kPair ? (p.nt > 128 ? 0.47 : 0.39) : p.nt > 128 ? 0.44 + 0.16 * (wide - 1) : 0.3 + 0.14 * wide;
+  const double stage = form == kPair ? (p.nt > 128 ? 0.47 : 0.43) : p.nt > 128 ? 0.44 + 0.16 * (wide - 1) : 0.3 + 0.14 * wide;
   const double w_total = (double)p.tiles_n * p.w_bytes * p.chunks * (form == kPair ? 2 : 1) / 4.5e6;
   if (p.split > 1) {
     const double main = p.chunks_per * stage, waves = dc_div_up(p.items, kClusters[p.split]);
@@ -911,7 +922,7 @@ double estimate(const Params &p, int form, int dtype, int n_sm) {
   }
   const int at_once = form == kPair ? n_sm / 2 : n_sm;
   const double waves = p.columns ? dc_div_up(p.tiles_m, at_once / p.tiles_n) : dc_div_up(p.items, at_once);
-  double main = p.chunks * stage, out = (form == kPair ? (p.nt > 128 ? 3.0 : 2.0) : wide) * type;
+  double main = p.chunks * stage, out = (form == kPair ? (p.nt > 128 ? 2.2 : 2.0) : wide) * type;
   if (form == kStream) main = 0.4 + 0.8 * dc_div_up(p.c_in, 32);
   if (form == kRows) main += 256.0 * p.rows * p.chunks_per * 115e-6;
   if (!p.vec) out *= 1.5;

@@ -26,7 +26,7 @@ using q4::kAtom;
 
 enum { kOne = DC_Q4_TILES, kPair = DC_Q4_PAIRS, kRows = DC_Q4_FEW_ROWS, kStream = DC_Q4_STREAM };
 template <int FORM>
-constexpr int kEpi = FORM == kOne ? 12 : 8;      // warps reading out
+constexpr int kEpi = FORM == kOne || FORM == kStream ? 12 : 8;                 // warps reading out
 constexpr int kCutWarps = 4;                     // quantising, form kStream
 template <int FORM>
 constexpr int kThreadsOf = (2 + kEpi<FORM> + (FORM == kStream ? kCutWarps : 0)) * 32;
@@ -250,6 +250,16 @@ template <typename T, int H, bool RES, bool RELU6>
 __device__ __forceinline__ void finish(float scale, uint32_t bias, float (*v)[32], uint32_t row, uint32_t swap, int halves) {
   finish32<T, RES, RELU6>(scale, bias, v[0], row, swap, 0);
   if (H > 1 && halves > 1) finish32<T, RES, RELU6>(scale, bias + 128u, v[H - 1], row, swap, 32 / kPer<T>);
+}
+template <typename T>
+__device__ __forceinline__ void finish_any(const Params &p, bool residual, uint32_t bias, float *v, uint32_t row, uint32_t swap, uint32_t first) {
+  if (residual) {
+    if (p.act == DC_ACT_RELU6) finish32<T, true, true>(p.scale, bias, v, row, swap, first);
+    else finish32<T, true, false>(p.scale, bias, v, row, swap, first);
+  } else {
+    if (p.act == DC_ACT_RELU6) finish32<T, false, true>(p.scale, bias, v, row, swap, first);
+    else finish32<T, false, false>(p.scale, bias, v, row, swap, first);
+  }
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t ssrc, int c0, int c1) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(ssrc), "r"(c0),
@@ -552,11 +562,23 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         __syncwarp();
       }
       bool ok = true;
+      auto release = [&](int c) {                // the columns from c on are read: where they are the last of this warp, the next tile may have the accumulator
+        constexpr int kRead = P ? 128 / kCols : 1;
+        if (c + kRead * c_step < cols) return;
+        tc_fence_before();
+        __syncwarp();
+        if (elect_one()) {
+          if (P) arrive_cluster(freed + (uint32_t)(buf * 8));
+          else mbar_arrive(&bar[kDEmpty + buf]);
+        }
+        __syncwarp();
+      };
       // A pair reads all of a warp's columns before it works on them: its one accumulator is then free for the next tile's products.
       constexpr int kAhead = P ? 128 / kCols : 1;
 #pragma unroll 1
       for (int cc = c_first; cc < cols || cc == c_first; cc += kAhead * c_step) {
-        float va[kAhead][kHalves][32];
+        constexpr int kNow = FORM == kStream ? 1 : kHalves;    // 32 columns at a time where registers are few
+        float va[kAhead][kNow][32];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
           const int c = cc + k * c_step, col = tn * p.nt + c;
@@ -591,19 +613,11 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
               for (int a = 0; a < kAhead; ++a)
 #pragma unroll
-                for (int h = 0; h < kHalves; ++h)
+                for (int h = 0; h < kNow; ++h)
                   if (cc + a * c_step + h * 32 < cols) tmem_ld32(d + (uint32_t)(cc + a * c_step + h * 32), reinterpret_cast<uint32_t *>(va[a][h]));
               tmem_ld_wait();
             }
-            if (cc + kAhead * c_step >= cols) {  // the accumulator is read: the next tile may have it
-              tc_fence_before();
-              __syncwarp();
-              if (elect_one()) {
-                if (P) arrive_cluster(freed + (uint32_t)(buf * 8));
-                else mbar_arrive(&bar[kDEmpty + buf]);
-              }
-              __syncwarp();
-            }
+            if (FORM != kStream || !work) release(cc);
           }
           if (!here) continue;
           if (parts) {
@@ -633,11 +647,25 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
               ok = warp_wait(&bar[kRes + warp - 2], res_parity, abort_flag, ws, 0xA0000u | (uint32_t)warp);
               if (!ok) break;
               res_parity ^= 1u;
-              if (p.act == DC_ACT_RELU6) finish<T, kHalves, true, true>(p.scale, bias_c, v, mine, swap, halves);
-              else finish<T, kHalves, true, false>(p.scale, bias_c, v, mine, swap, halves);
             } else {
               if (elect_one()) wait_out();
               __syncwarp();
+            }
+            if (FORM == kStream) {
+#pragma unroll
+              for (int h = 0; h < kHalves; ++h) {
+                if (h > 0 && halves > 1) {
+                  tmem_ld32(d + (uint32_t)(c + 32), reinterpret_cast<uint32_t *>(v[0]));
+                  tmem_ld_wait();
+                }
+                if (h == kHalves - 1) release(c);
+                if (h > 0 && halves < 2) break;
+                finish_any<T>(p, residual != nullptr, bias_c + (uint32_t)(h * 128), v[0], mine, swap, (uint32_t)(h * 32 / kPer<T>));
+              }
+            } else if (residual) {
+              if (p.act == DC_ACT_RELU6) finish<T, kHalves, true, true>(p.scale, bias_c, v, mine, swap, halves);
+              else finish<T, kHalves, true, false>(p.scale, bias_c, v, mine, swap, halves);
+            } else {
               if (p.act == DC_ACT_RELU6) finish<T, kHalves, false, true>(p.scale, bias_c, v, mine, swap, halves);
               else finish<T, kHalves, false, false>(p.scale, bias_c, v, mine, swap, halves);
             }
@@ -728,28 +756,31 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       if (!ok) break;
       const uint32_t a = ring + (uint32_t)(stage * p.stage_bytes) + (uint32_t)((r >> 3) * 1024 + (r & 7) * 128);
       const uint32_t sfa = ring + (uint32_t)(stage * p.stage_bytes) + kA;
-      const int item0 = item, ch0 = ch, end = (min(p.c_in - ch * kStageCols, kStageCols) + 63) / 64 * 64;
+      const int item0 = item, ch0 = ch, some = min(p.c_in - ch * kStageCols, kStageCols), end = (some + 63) / 64 * 64;     // columns; whole runs of 64
       if (++ch == p.chunks) { ch = 0; item += step; }
 #pragma unroll 1
       for (int c = 0; c < end; c += 32) {
         uint4 raw[kRaw];
 #pragma unroll
         for (int i = 0; i < kRaw; ++i) raw[i] = next[i];
-        if (c + 32 < end) ask(item0, ch0, c + 32);
-        else if (item < items) ask(item, ch, 0);
-        uint2 code[2];
-        uint32_t top[2], byte[2];
+        if (c + 32 < some) ask(item0, ch0, c + 32);
+        else if (c < some && item < items) ask(item, ch, 0);
+        uint2 code[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+        uint32_t byte[2] = {0, 0};
+        if (c < some) {                          // what a run of 64 columns has behind the last one is 0
+          uint32_t top[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) top[h] = largest16<T>(raw + h * kRaw / 2);
-        if (F == DC_MX4) top[0] = top[1] = max(top[0], top[1]);
+          for (int h = 0; h < 2; ++h) top[h] = largest16<T>(raw + h * kRaw / 2);
+          if (F == DC_MX4) top[0] = top[1] = max(top[0], top[1]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[16];
+          for (int h = 0; h < 2; ++h) {
+            float v[16];
 #pragma unroll
-          for (int i = 0; i < kRaw / 2; ++i) unpack16<T>(raw[h * kRaw / 2 + i], v + i * kPer<T>);
-          const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.r6);
-          code[h] = q4::codes16<F, sizeof(T) == 2>(v, s);
-          byte[h] = s.byte;
+            for (int i = 0; i < kRaw / 2; ++i) unpack16<T>(raw[h * kRaw / 2 + i], v + i * kPer<T>);
+            const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.r6);
+            code[h] = q4::codes16<F, sizeof(T) == 2>(v, s);
+            byte[h] = s.byte;
+          }
         }
         sts_u4(a + (uint32_t)(((c >> 5) ^ (r & 7)) * 16), make_uint4(code[0].x, code[0].y, code[1].x, code[1].y));
         const uint32_t blk = (uint32_t)(F == DC_NV4 ? c >> 4 : c >> 5), to = sfa + (blk >> 2) * kAtom + q4::scale_at((uint32_t)r, blk);
@@ -870,7 +901,7 @@ bool lay_out(Params *p, int form, int format, int dtype, int n_sm) {
   p->nb = p->nt > 128 ? 2 : 1;
   p->w_bytes = (form == kPair ? p->nt / 2 : p->nt) * 128 + p->nb * atoms * kAtom;
   p->sf_cols = 4 * atoms * (1 + p->nb);
-  const int epi = form == kOne ? kEpi<kOne> : kEpi<kPair>, at_once = form == kPair ? n_sm / 2 : n_sm;
+  const int epi = form == kOne || form == kStream ? kEpi<kOne> : kEpi<kPair>, at_once = form == kPair ? n_sm / 2 : n_sm;
   const bool many = p->split == 1 && p->items > at_once;       // CTAs have several tiles
   p->acc_bufs = many && epi / 4 * p->nt + 3 * p->sf_cols <= 512 ? epi / 4 : 1;
   // a column of tiles to a CTA, where that leaves none idle for long: w is loaded once, and 148 SMs do not all ask for the same part of it
@@ -923,9 +954,9 @@ double estimate(const Params &p, int form, int dtype, int n_sm) {
   const int at_once = form == kPair ? n_sm / 2 : n_sm;
   const double waves = p.columns ? dc_div_up(p.tiles_m, at_once / p.tiles_n) : dc_div_up(p.items, at_once);
   double main = p.chunks * stage, out = (form == kPair ? (p.nt > 128 ? 2.2 : 2.0) : wide) * type;
-  if (form == kStream) main = 0.4 + 0.8 * dc_div_up(p.c_in, 32);
   if (form == kRows) main += 256.0 * p.rows * p.chunks_per * 115e-6;
   if (!p.vec) out *= 1.5;
+  if (form == kStream) return 3.2 + waves * (0.2 + 0.6 * dc_div_up(p.c_in, 32) + 0.8 * out);   // quantising and reading out share the SM's ALUs
   const double total = 3.2 + (p.acc_bufs > 1 ? waves * (main > out ? main : out) : waves * (main + out));
   return total > 3.2 + w_total ? total : 3.2 + w_total;
 }

@@ -1046,12 +1046,13 @@ Params params_of(long long rows, int c_in, int c_out, dc_act act, dc_dtype dtype
   return p;
 }
 
-// Whether a forward call quantises in the product's launch (p, form) or in one of its own before it (q, apart: 2 us, and its bytes).
+// Whether a forward call quantises in the product's launch (p, form) or in one of its own before it (q, apart: 2 us, and its bytes at what it moves of them).
 bool in_one_launch(Params *p, Params *q, dc_q4_format format, dc_dtype dtype, int n_sm, int *form, int *apart) {
   double us, us_apart;
   *form = choose(p, true, format, dtype, n_sm, &us);
   *apart = choose(q, false, format, dtype, n_sm, &us_apart);
-  return *form >= 0 && us <= us_apart + 2.0 + (double)p->rows * p->c_in * (dtype == DC_F32 ? 4.5 : 2.5) / 4.5e6;
+  const double row = p->c_in * (dtype == DC_F32 ? 4.0 : 2.0) + (p->c_in < 64 ? 36.0 : p->c_in * 0.57);
+  return *form >= 0 && us <= us_apart + 2.0 + (double)p->rows * row / 3.5e6;
 }
 
 }  // namespace

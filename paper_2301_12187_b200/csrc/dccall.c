@@ -16,6 +16,7 @@ typedef int (*q4_product_fn)(const void *, long long, int, const void *, int, in
                              void *);
 typedef int (*q4_forward_fn)(const void *, long long, int, const void *, int, int, float, float, const void *, int, const void *, void *, int, void *,
                              size_t, void *);
+typedef int (*q4_query_fn)(long long, int, int, size_t *);
 typedef int (*block_fn)(const void *, int, int, int, const void *, void *, int, void *, size_t, void *);
 
 static conv_fn g_conv;
@@ -25,6 +26,7 @@ static q4_quantize_fn g_q4_quantize;
 static q4_dequantize_fn g_q4_dequantize;
 static q4_product_fn g_q4_product;
 static q4_forward_fn g_q4_forward;
+static q4_query_fn g_q4_query;
 static PyObject *g_f32, *g_bf16, *g_geom, *g_block_type, *g_get_device, *g_get_stream;
 static PyObject *s_data_ptr, *s_shape, *s_dtype, *s_numel, *s_element_size, *s_cuda_stream;
 static PyObject *s_stride, *s_is_contiguous, *s_get_device, *s_rows, *s_cols, *s_fmt, *s_tensor_scale, *s_data;
@@ -178,7 +180,14 @@ static int read_matrix(PyObject *q, long long dev, matrix *m) {
   if (read_ll(PyObject_GetAttr(q, s_rows), &m->rows) || read_ll(PyObject_GetAttr(q, s_cols), &m->cols) || read_ll(PyObject_GetAttr(q, s_fmt), &m->fmt) ||
       read_float(PyObject_GetAttr(q, s_tensor_scale), &m->scale) || !(d = PyObject_GetAttr(q, s_data)))
     return -1;
-  const int bad = read_here(d, dev, &m->data) || !m->data || m->cols < 1 || m->cols > 2147483647LL;
+  size_t have, layout[4];                        /* dc_q4_layout; the last one its bytes */
+  int bad = read_here(d, dev, &m->data) || !m->data || m->cols < 1 || m->cols > 2147483647LL || m->fmt < 0 || m->fmt > 1 || read_bytes(d, &have) ||
+            g_q4_query(m->rows, (int)m->cols, (int)m->fmt, layout) || have < layout[3];
+  if (!bad) {
+    PyObject *dense = PyObject_CallMethodNoArgs(d, s_is_contiguous);
+    bad = dense != Py_True;
+    Py_XDECREF(dense);
+  }
   Py_DECREF(d);
   return bad ? -1 : 0;
 }
@@ -300,15 +309,16 @@ static PyObject *q4_forward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
-/* bind_q4(addresses of quantize, dequantize, product, forward) */
+/* bind_q4(addresses of quantize, dequantize, product, forward, query) */
 static PyObject *bind_q4(PyObject *self, PyObject *args) {
-  unsigned long long q, d, p, f;
+  unsigned long long q, d, p, f, l;
   (void)self;
-  if (!PyArg_ParseTuple(args, "KKKK", &q, &d, &p, &f)) return NULL;
+  if (!PyArg_ParseTuple(args, "KKKKK", &q, &d, &p, &f, &l)) return NULL;
   g_q4_quantize = (q4_quantize_fn)(uintptr_t)q;
   g_q4_dequantize = (q4_dequantize_fn)(uintptr_t)d;
   g_q4_product = (q4_product_fn)(uintptr_t)p;
   g_q4_forward = (q4_forward_fn)(uintptr_t)f;
+  g_q4_query = (q4_query_fn)(uintptr_t)l;
   Py_RETURN_NONE;
 }
 

@@ -1,8 +1,9 @@
 // Quantising matrices to microscaled 4 bits and reading them back (dc_q4_quantize, dc_q4_dequantize).
 //
-// A thread takes 16 columns of a row: a block of DC_NV4, half of one of DC_MX4 (the other half is in the neighbouring lane).  A CTA takes up to 256
-// columns of 128 rows, whole scale tiles, whose bytes it collects in shared memory and writes 16 at a time -- or, where that gives too few CTAs,
-// of the 32 rows that share a word of every 16 bytes of a scale tile.
+// Quantising, a thread takes 16 columns of a row: a block of DC_NV4, half of one of DC_MX4 (the other half is in the neighbouring lane).  A CTA takes
+// up to 256 columns of 128 rows, whole scale tiles, whose bytes it collects in shared memory and writes 16 at a time -- or, where that gives too few
+// CTAs, of the 32 rows that share a word of every 16 bytes of a scale tile (2048 x 4096: 6.0 us).  In all sizes that many CTAs would cost what
+// the scales' 4-byte pieces do (16384 x 8192 71 us in the place of 61); reading back has no such cost.
 #include <string.h>
 
 #include "q4.cuh"
@@ -63,8 +64,11 @@ __device__ __forceinline__ void shift16(uint32_t *w, uint32_t off) {
   }
 }
 
+// A row at a time, so that six CTAs fit an SM: 16001 x 4096 in fp32 52.2 us, 100352 x 192 in bf16 11.9, 16384 x 8192 61.2 (344 MB: 53 at the rate of a
+// copy).  Two rows at once and four CTAs: 57.4, 13.5, 61.6.  Eight CTAs, of 32 registers a thread: 49.7, 15.2, 57.5.  The next row asked for ahead: 51.5,
+// 13.0, 59.2, and narrow maps 1 us more.
 template <int F, typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads, VEC ? 4 : 3) k_q4_quantize(const T *__restrict__ x, uint8_t *__restrict__ q, const Params p) {
+__global__ void __launch_bounds__(kThreads, VEC ? 6 : 5) k_q4_quantize(const T *__restrict__ x, uint8_t *__restrict__ q, const Params p) {
   __shared__ __align__(16) uint8_t scales[4 * kAtom];
   dc_pdl_enter();
   const int tid = (int)threadIdx.x, segs = p.segs, span = segs * 16;
@@ -82,54 +86,45 @@ __global__ void __launch_bounds__(kThreads, VEC ? 4 : 3) k_q4_quantize(const T *
   __syncthreads();
   const bool wanted = c < (int)(p.pitch * 2) && mine < step;
   const int some = wanted ? (p.cols - c < 16 ? p.cols - c : 16) : 0;             // values of this thread's pieces; none or fewer: codes 0
-  constexpr int U = 2;                           // rows of a thread at once, so that their loads overlap
   const long long end = (p.rows - 1) * p.stride + p.cols;                        // of x
   auto offset = [&](long long row) { return VEC ? 0u : (uint32_t)((row * p.stride + c) * (long long)sizeof(T)) & 15u; };   // of the first value in its word
 #pragma unroll 1
-  for (int r = mine; r - mine < rows; r += U * step) {
-    uint4 raw[U][kPieces];
+  for (int r = mine; r - mine < rows; r += step) {
+    uint4 raw[kPieces];
+    const long long row = row0 + r;
+    const int lead = VEC ? 0 : (int)offset(row) / (int)sizeof(T);                // values of the first word that come before this thread's
+    const T *at = x + row * p.stride + c - lead;
+    const int to = r < rows ? lead + some : 0;                                   // `lead` to here: of the values from `at` on
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long long row = row0 + r + u * step;
-      const int lead = VEC ? 0 : (int)offset(row) / (int)sizeof(T);              // values of the first word that come before this thread's
-      const T *at = x + row * p.stride + c - lead;
-      const int from = lead, to = r + u * step < rows ? lead + some : 0;         // of the values from `at` on
+    for (int i = 0; i < kPieces; ++i) {
+      raw[i] = make_uint4(0, 0, 0, 0);
+      if (i * kPer<T> >= to) continue;
+      if ((i + 1) * kPer<T> <= to || (!VEC && (i + 1) * kPer<T> <= end - (row * p.stride + c - lead))) {      // a whole word of x
+        raw[i] = __ldg(reinterpret_cast<const uint4 *>(at) + i);
+      } else {
+        float t[kPer<T>];
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        raw[u][i] = make_uint4(0, 0, 0, 0);
-        if (i * kPer<T> >= to) continue;
-        if ((i + 1) * kPer<T> <= to || (!VEC && (i + 1) * kPer<T> <= end - (row * p.stride + c - lead))) {      // a whole word of x
-          raw[u][i] = __ldg(reinterpret_cast<const uint4 *>(at) + i);
-        } else {
-          float t[kPer<T>];
-#pragma unroll
-          for (int j = 0; j < kPer<T>; ++j) t[j] = i * kPer<T> + j >= from && i * kPer<T> + j < to ? (float)at[i * kPer<T> + j] : 0.f;
-          raw[u][i] = pack<T>(t);
-        }
+        for (int j = 0; j < kPer<T>; ++j) t[j] = i * kPer<T> + j >= lead && i * kPer<T> + j < to ? (float)at[i * kPer<T> + j] : 0.f;
+        raw[i] = pack<T>(t);
       }
     }
+    if (!VEC) shift16<T>(reinterpret_cast<uint32_t *>(raw), offset(row));
+    float v[16];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u > 0 && r + u * step - mine >= most) break;         // the same for all threads
-      const int ru = r + u * step;
-      if (!VEC) shift16<T>(reinterpret_cast<uint32_t *>(raw[u]), offset(row0 + ru));
-      float v[16];
+    for (int i = 0; i < 16 / kPer<T>; ++i) unpack<T>(raw[i], v + i * kPer<T>);
+    if (!VEC && some < 16) {
 #pragma unroll
-      for (int i = 0; i < 16 / kPer<T>; ++i) unpack<T>(raw[u][i], v + i * kPer<T>);
-      if (!VEC && some < 16) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = i < some ? v[i] : 0.f;
-      }
-      uint32_t top = largest16(v);
-      if (F == DC_MX4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      const BlockScale s = block_scale<F>(top, p.g, p.r6);
-      const uint2 code = codes16<F, sizeof(T) == 2>(v, s);
-      if (ru < rows && wanted) {
-        *reinterpret_cast<uint2 *>(q + (size_t)(row0 + ru) * p.pitch + (c >> 1)) = code;
-        if (some > 0 && (F == DC_NV4 || (seg & 1) == 0)) {
-          const uint32_t b = (uint32_t)(seg * 16 / kBlock);
-          scales[(b >> 2) * kAtom + scale_at((uint32_t)(in_tile + ru), b)] = (uint8_t)s.byte;
-        }
+      for (int i = 0; i < 16; ++i) v[i] = i < some ? v[i] : 0.f;
+    }
+    uint32_t top = largest16(v);
+    if (F == DC_MX4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    const BlockScale s = block_scale<F>(top, p.g, p.r6);
+    const uint2 code = codes16<F, sizeof(T) == 2>(v, s);
+    if (r < rows && wanted) {
+      *reinterpret_cast<uint2 *>(q + (size_t)row * p.pitch + (c >> 1)) = code;
+      if (some > 0 && (F == DC_NV4 || (seg & 1) == 0)) {
+        const uint32_t b = (uint32_t)(seg * 16 / kBlock);
+        scales[(b >> 2) * kAtom + scale_at((uint32_t)(in_tile + r), b)] = (uint8_t)s.byte;
       }
     }
   }
@@ -145,7 +140,8 @@ __global__ void __launch_bounds__(kThreads, VEC ? 4 : 3) k_q4_quantize(const T *
   }
 }
 
-// A thread writes 32 bytes of a row.  Rows of y that do not begin on 16 bytes: its columns begin up to 7 earlier, where they do, with codes and a
+// Bound by what goes out: 8192 x 8192 to bf16 35.9 us, 16001 x 4096 to fp32 69.7 (a fill of as many bytes: 34.5, 67).  A thread writes 32 bytes of
+// a row: with 64, which fp32's 16 columns are, the second took 84.7.  Rows of y that do not begin on 16 bytes: its columns begin up to 7 earlier, where they do, with codes and a
 // scale of the piece before its own.  (Through shared memory, stored value by value: 5001 x 1003 in fp32 12.1 us.)
 template <typename T>
 constexpr int kTake = 32 / (int)sizeof(T);
@@ -254,7 +250,7 @@ dc_status prepare(const void *x, long long rows, int cols, long long stride, dc_
     p->col_tiles = (uint32_t)dc_div_up(cols, 16 * p->segs);
   }
   const long long tiles = (rows + 127) / 128 * p->col_tiles;
-  p->groups = tiles < 4ll * dc_sm_count() ? 4 : 1;
+  p->groups = tiles < (reads ? 8ll : 4ll) * dc_sm_count() ? 4 : 1;
   const long long ctas = tiles * p->groups;
   if (ctas > 0x7fffffffll) return DC_ERR_UNSUPPORTED;
   *grid = dim3((unsigned)ctas);

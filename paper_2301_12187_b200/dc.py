@@ -176,7 +176,7 @@ def lib():
             _dccall.bind(at("dc_conv_forward_algo"), at("dc_dwconv_forward"), at("dc_block_forward"), torch.float32, torch.bfloat16,
                          Geom, Block, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
                          getattr(torch._C, "_cuda_getCurrentRawStream", None))
-            _dccall.bind_q4(at("dc_q4_quantize"), at("dc_q4_dequantize"), at("dc_q4_product"), at("dc_q4_forward"))
+            _dccall.bind_q4(at("dc_q4_quantize"), at("dc_q4_dequantize"), at("dc_q4_product"), at("dc_q4_forward"), at("dc_q4_query"))
             _native = _dccall
         except ImportError:                      # not built for this Python
             _native = _NoNative
@@ -563,6 +563,13 @@ def _dense(t, rows: int, cols: int, dtype, what: str):
         raise ValueError("%s: a dense tensor of %d rows of %d values in %s is wanted" % (what, rows, cols, dtype))
 
 
+def _whole(what: str, *matrices):
+    """A matrix's buffer may be one of the caller's (`q.data = ...`): it has to hold what the sizes say."""
+    for q in matrices:
+        if q.data.numel() * q.data.element_size() < q4_layout(q.rows, q.cols, q.fmt).bytes or not q.data.is_contiguous():
+            raise ValueError("%s: a matrix of %d x %d in a buffer that does not hold it" % (what, q.rows, q.cols))
+
+
 def q4_quantize(x, q: Q4Matrix, stream=None):
     """Rows of x (bf16 or fp32, [..., cols]; rows at one distance) into q, with q's tensor scale."""
     st = (_native or _load_native()).q4_quantize(x, q, stream)
@@ -571,6 +578,7 @@ def q4_quantize(x, q: Q4Matrix, stream=None):
     if st is not None:
         raise DcError(st, "dc_q4_quantize")
     _here("q4_quantize", x, q.data)
+    _whole("q4_quantize", q)
     rows, stride = _rows_of(x, q.cols, "q4_quantize")
     if rows != q.rows:
         raise ValueError("q4_quantize: %d rows, the matrix has %d" % (rows, q.rows))
@@ -586,6 +594,7 @@ def q4_dequantize(q: Q4Matrix, y, stream=None):
     if st is not None:
         raise DcError(st, "dc_q4_dequantize")
     _here("q4_dequantize", q.data, y)
+    _whole("q4_dequantize", q)
     rows, stride = _rows_of(y, q.cols, "q4_dequantize")
     if rows != q.rows:
         raise ValueError("q4_dequantize: %d rows, the matrix has %d" % (rows, q.rows))
@@ -613,6 +622,7 @@ def q4_product(x: Q4Matrix, w: Q4Matrix, bias, act, residual, y, workspace, stre
     if st is not None:
         raise DcError(st, "dc_q4_product")
     _here("q4_product", x.data, w.data, bias, residual, y, workspace)
+    _whole("q4_product", x, w)
     if x.fmt != w.fmt or x.cols != w.cols:
         raise ValueError("q4_product: the matrices must have one format and as many columns")
     _dense(y, x.rows, w.rows, y.dtype, "q4_product")
@@ -631,6 +641,7 @@ def q4_forward(x, w: Q4Matrix, x_scale: float, bias, act, residual, y, workspace
     if st is not None:
         raise DcError(st, "dc_q4_forward")
     _here("q4_forward", x, w.data, bias, residual, y, workspace)
+    _whole("q4_forward", w)
     rows = x.numel() // w.cols
     _dense(x, rows, w.cols, y.dtype, "q4_forward")
     _dense(y, rows, w.rows, y.dtype, "q4_forward")

@@ -387,3 +387,28 @@ def test_what_is_not_written_stays():
         dc.q4_forward(x.cpu(), wq, 1.0, None, 0, None, y[:5], ws)
     torch.cuda.synchronize()
     assert (y[5:] == 3.0).all()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("cols", [1, 2, 3, 5, 7, 15, 16, 17, 31, 33, 63, 64, 65, 127, 250, 257])
+def test_rows_that_begin_anywhere(cols, fmt, dtype):
+    """Rows at every distance of 16 bytes' values, of a tensor that ends with the last one; what lies around them is NaN, and stays."""
+    for slack in range(8):
+        rows, stride = 37, cols + slack
+        n = (rows - 1) * stride + cols
+        whole = Guarded(torch, (n,), TYPES[dtype], fill=float("nan"))
+        x = whole.t.as_strided((rows, cols), (stride, 1))
+        x.copy_(rand(rows, cols, cols * 8 + slack, dtype=dtype))
+        g = 1.0 if fmt == dc.MX4 else 2.0 ** -7
+        q, guard = matrix(rows, cols, fmt, g)
+        dc.q4_quantize(x, q)
+        code, byte = check_quantized(x, fmt, g, q, guard)
+        back = Guarded(torch, (n,), TYPES[dtype], fill=7.0)
+        y = back.t.as_strided((rows, cols), (stride, 1))
+        dc.q4_dequantize(q, y)
+        torch.cuda.synchronize()
+        back.check("values")
+        assert (np64(y) == Q.values(code, byte, fmt, g)).all()
+        y.fill_(7.0)
+        assert (back.t == 7.0).all()

@@ -234,3 +234,23 @@ def test_the_gpu_tests_reach_every_form():
             assert (what, whole) in seen, (what, whole)
     forms = {dc.q4_plan(r, i, o, f, d, True).form for r, i, o in t.FORWARD_FORMS for f in (0, 1) for d in (0, 1)}
     assert {dc.Q4_FEW_ROWS, dc.Q4_STREAM, dc.Q4_TILES} <= forms
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refuses_a_buffer_that_does_not_hold_its_matrix(native, monkeypatch):
+    """A matrix's buffer may be replaced by the caller, by a loaded one for instance."""
+    torch = pytest.importorskip("torch")
+    dc.lib()
+    if not native:
+        monkeypatch.setattr(dc, "_native", dc._NoNative)
+    x, y, ws = torch.zeros(4, 40), torch.zeros(4, 16), torch.zeros(1 << 16, dtype=torch.uint8)
+    good_x, good_w = dc.Q4Matrix(4, 40, dc.NV4, device="cpu"), dc.Q4Matrix(16, 40, dc.NV4, device="cpu")
+    n = int(good_w.layout.bytes)
+    for data in (torch.zeros(n - 1, dtype=torch.uint8), torch.zeros(2 * n, dtype=torch.uint8)[::2]):
+        w = dc.Q4Matrix(16, 40, dc.NV4, device="cpu")
+        w.data = data
+        for call in (lambda: dc.q4_quantize(torch.zeros(16, 40), w), lambda: dc.q4_dequantize(w, torch.zeros(16, 40)),
+                     lambda: dc.q4_product(good_x, w, None, 0, None, y, ws), lambda: dc.q4_product(w, good_x, None, 0, None, torch.zeros(16, 4), ws),
+                     lambda: dc.q4_forward(x, w, 1.0, None, 0, None, y, ws)):
+            with pytest.raises(ValueError, match="buffer"):
+                call()

@@ -29,7 +29,7 @@ static q4_forward_fn g_q4_forward;
 static q4_query_fn g_q4_query;
 static PyObject *g_f32, *g_bf16, *g_geom, *g_block_type, *g_get_device, *g_get_stream;
 static PyObject *s_data_ptr, *s_shape, *s_dtype, *s_numel, *s_element_size, *s_cuda_stream;
-static PyObject *s_stride, *s_is_contiguous, *s_get_device, *s_rows, *s_cols, *s_fmt, *s_tensor_scale, *s_data;
+static PyObject *s_stride, *s_is_contiguous, *s_get_device, *s_rows, *s_cols, *s_fmt, *s_tensor_scale, *s_data, *s_nbytes;
 
 /* each reader: 0 on success, -1 when the argument has another form (any Python error is cleared by the caller) */
 static int read_size(PyObject *o, size_t *v) {
@@ -180,9 +180,10 @@ static int read_matrix(PyObject *q, long long dev, matrix *m) {
   if (read_ll(PyObject_GetAttr(q, s_rows), &m->rows) || read_ll(PyObject_GetAttr(q, s_cols), &m->cols) || read_ll(PyObject_GetAttr(q, s_fmt), &m->fmt) ||
       read_float(PyObject_GetAttr(q, s_tensor_scale), &m->scale) || !(d = PyObject_GetAttr(q, s_data)))
     return -1;
-  size_t have, layout[4];                        /* dc_q4_layout; the last one its bytes */
-  int bad = read_here(d, dev, &m->data) || !m->data || m->cols < 1 || m->cols > 2147483647LL || m->fmt < 0 || m->fmt > 1 || read_bytes(d, &have) ||
-            g_q4_query(m->rows, (int)m->cols, (int)m->fmt, layout) || have < layout[3];
+  long long have;
+  size_t layout[4];                              /* dc_q4_layout; the last one its bytes */
+  int bad = read_here(d, dev, &m->data) || !m->data || m->cols < 1 || m->cols > 2147483647LL || m->fmt < 0 || m->fmt > 1 ||
+            read_ll(PyObject_GetAttr(d, s_nbytes), &have) || g_q4_query(m->rows, (int)m->cols, (int)m->fmt, layout) || have < 0 || (size_t)have < layout[3];
   if (!bad) {
     PyObject *dense = PyObject_CallMethodNoArgs(d, s_is_contiguous);
     bad = dense != Py_True;
@@ -363,7 +364,8 @@ PyMODINIT_FUNC PyInit__dccall(void) {
   s_fmt = PyUnicode_InternFromString("fmt");
   s_tensor_scale = PyUnicode_InternFromString("tensor_scale");
   s_data = PyUnicode_InternFromString("data");
-  if (!s_stride || !s_is_contiguous || !s_get_device || !s_rows || !s_cols || !s_fmt || !s_tensor_scale || !s_data) return NULL;
+  s_nbytes = PyUnicode_InternFromString("nbytes");
+  if (!s_stride || !s_is_contiguous || !s_get_device || !s_rows || !s_cols || !s_fmt || !s_tensor_scale || !s_data || !s_nbytes) return NULL;
   if (!s_data_ptr || !s_shape || !s_dtype || !s_numel || !s_element_size || !s_cuda_stream) return NULL;
   return PyModule_Create(&module);
 }

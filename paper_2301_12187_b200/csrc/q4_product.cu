@@ -6,15 +6,17 @@
 // scales; DC_MX4: two instructions', told apart by the descriptor's scale id.  Sums are fp32 in tensor memory.
 //
 // A stage of the ring is 256 columns: codes of both operands and their scale tiles; its scales have columns of tensor memory of their own, so a
-// slot's scales are written over only behind the products that read them.  One warp loads, one issues, eight read out the accumulators.
+// slot's scales are written over only behind the products that read them.  One warp loads, one issues, eight or twelve read out the accumulators.
 // CTAs walk over tiles.  The forms:
 //   kOne     both operands by TMA.  Few tiles: a cluster shares a tile's reduction.  Each of its CTAs owns some columns of the result; all send their
 //            parts of them to its shared memory, and it adds them up in rank order.  (With parts left where they were, two meetings of the cluster and
 //            reads from afar: one row of 4096 x 4096 7.4 us.)  Tensor memory is given back without waiting for a CTA that may be waiting for
 //            some.  One column of tiles to a CTA and few stages: w stays in shared memory.
+//            Narrow tiles, of 32 or 64 columns: the products are those of 128 rows of w around the tile's, of which only the tile's are there; the rest is
+//            what lies around them in shared memory, and is not read out.
 //   kPair    two CTAs multiply 256 x 256 (cta_group::2): each loads half of either operand, which halves what an SM has to fetch of w.
-//   kRows    few rows of bf16 or fp32: quantised by the reading-out warps into shared memory, where all of them stay.
-//   kStream  many rows of bf16 or fp32 and one column of tiles: eight more warps quantise them, a stage at a time.
+//   kRows    up to 32 rows of bf16 or fp32: quantised by the reading-out warps into shared memory, where all of them stay.
+//   kStream  many rows of bf16 or fp32 and one column of tiles: four more warps quantise them, a stage at a time.
 #include <string.h>
 
 #include "q4.cuh"
@@ -45,6 +47,7 @@ struct Params {
   float scale;
   float g, r6;               // kRows, kStream: x's tensor scale
   int nt, nb;                // rows of w in a tile, 128-row scale tiles that they touch
+  int acc;                   // columns of an accumulator: nt, or 128 around a narrow tile's
   int tiles_m, tiles_n, items;
   int chunks;                // stages of a row
   int columns;               // CTAs keep to a column of tiles: item = row of tiles
@@ -192,17 +195,8 @@ __device__ __forceinline__ uint4 finish16(const Params &p, const float *b, bool 
   }
   return pack16<T>(v);
 }
-__device__ __forceinline__ unsigned long long pair_of(float lo, float hi) {
-  unsigned long long d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
-  return d;
-}
 // two FMAs in one instruction
-__device__ __forceinline__ void fma2(float &lo, float &hi, unsigned long long s, unsigned long long b) {
-  unsigned long long d = pair_of(lo, hi);
-  asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(d) : "l"(s), "l"(b));
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(d));
-}
+__device__ __forceinline__ void fma2(float &lo, float &hi, uint64_t s, uint64_t b) { q4::unpair(q4::fma2(q4::pair(lo, hi), s, b), lo, hi); }
 // ReLU6 of two values with one instruction behind the conversion: packed minima and maxima run at half rate and bound the read-out.  A NaN becomes 6.
 __device__ __forceinline__ uint32_t relu6_fast(float lo, float hi) { return min_bf16x2(pack_bf16x2_relu(lo, hi), 0x40C040C0u); }
 // 32 sums of a thread's row -> values of y in its staged row, 16-byte pieces from `first` on at i ^ swap: scale and bias (shared memory, the same
@@ -217,11 +211,11 @@ __device__ __forceinline__ void finish32(float scale, uint32_t bias, float *v, u
 #pragma unroll
     for (int i = 0; i < K; ++i) res[i] = lds_u4(row + ((first + (uint32_t)i) ^ swap) * 16u);
   }
-  const unsigned long long s = pair_of(scale, scale);
+  const uint64_t s = q4::pair(scale, scale);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    fma2(v[4 * i], v[4 * i + 1], s, pair_of(__uint_as_float(b[i].x), __uint_as_float(b[i].y)));
-    fma2(v[4 * i + 2], v[4 * i + 3], s, pair_of(__uint_as_float(b[i].z), __uint_as_float(b[i].w)));
+    fma2(v[4 * i], v[4 * i + 1], s, q4::pair(__uint_as_float(b[i].x), __uint_as_float(b[i].y)));
+    fma2(v[4 * i + 2], v[4 * i + 3], s, q4::pair(__uint_as_float(b[i].z), __uint_as_float(b[i].w)));
   }
 #pragma unroll
   for (int i = 0; i < K; ++i) {
@@ -334,7 +328,7 @@ __device__ __forceinline__ uint32_t largest16(const uint4 *raw) {
   }
   return sizeof(T) == 2 ? max(top & 0xffff0000u, top << 16) : top;
 }
-// 16 columns, piece `seg` of a row, -> codes in an operand's rows and the block's scale in its tile.  `top`: largest magnitude of the piece.
+// 16 columns, piece `seg` of a row, -> codes in an operand's rows and the block's scale in its tile.
 template <int F, typename T>
 __device__ __forceinline__ void put_x16(float *v, const Params &p, uint32_t a, uint32_t sfa, int row, int seg, bool valid) {
   uint32_t top = q4::largest16(v);
@@ -410,7 +404,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   const int items = p.columns ? p.tiles_m : p.items, own_tn = p.columns ? team_id % p.tiles_n : 0;
   auto column_of = [&](int item) { return p.columns || p.tiles_n == 1 ? own_tn : item / p.tiles_m; };
   const int c0 = P ? 0 : rank * p.chunks_per, c1 = P ? p.chunks : min(p.chunks, c0 + p.chunks_per);
-  const uint32_t sf_base = tmem + (uint32_t)(p.acc_bufs * p.nt);
+  const uint32_t sf_base = tmem + (uint32_t)(p.acc_bufs * p.acc);
+  auto inside = [&](int tn) { return !P && p.nt < p.acc ? tn * p.nt & 127 : 0; };          // a narrow tile's place among its scale tile's rows
   const uint32_t ring = sm + (uint32_t)p.off_ring, w_base = ring + (uint32_t)(p.stages * p.stage_bytes);
   const int b_rows = P ? p.nt / 2 : p.nt;
   const uint32_t w_codes = (uint32_t)b_rows * 128u;
@@ -475,7 +470,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       ok = warp_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x20000u | (uint32_t)buf);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t d = tmem + (uint32_t)(buf * p.nt), idesc = q4_idesc<F>(p.nt, P ? 256 : 128);
+      const uint32_t d = tmem + (uint32_t)(buf * p.acc), idesc = q4_idesc<F>(p.acc, P ? 256 : 128);
+      const uint32_t shift = (uint32_t)inside(p.nt < p.acc ? column_of(item) : 0) * 128u;
       for (int ch = c0; ch < c1; ++ch) {
         ok = warp_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x30000u | (uint32_t)stage);
         if (!ok) break;
@@ -488,7 +484,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           const uint32_t ta = sf_base + (uint32_t)(stage * p.sf_cols);
           const int steps = min(4, dc_div_up(p.c_in - ch * kStageCols, 64));
           if (p.nb == 2) multiply_steps<F, P, 2>(steps, d, a, b, sfa, sfb, ta, idesc, ch > c0);
-          else multiply_steps<F, P, 1>(steps, d, a, b, sfa, sfb, ta, idesc, ch > c0);
+          else multiply_steps<F, P, 1>(steps, d, a, b - shift, sfa, sfb, ta, idesc, ch > c0);
           commit<P>(&bar[kEmpty + stage]);
           if (ch == c1 - 1) commit<P>(&bar[kDFull + buf]);
         }
@@ -554,7 +550,7 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       const long long row0 = (long long)(P ? tm * 2 + rank : tm) * 128 + quad * 32;
       const int cols = min(p.nt, p.c_out - tn * p.nt);
       const bool work = row0 < p.rows && c_first < cols, staged = work && !parts && p.vec;
-      const uint32_t d = tmem + (uint32_t)(buf * p.nt) + ((uint32_t)(quad * 32) << 16);
+      const uint32_t d = tmem + (uint32_t)(buf * p.acc + inside(tn)) + ((uint32_t)(quad * 32) << 16);
       if (!P && work && !parts && tn != bias_tn) {
         bias_tn = tn;
         __syncwarp();
@@ -904,6 +900,10 @@ bool lay_out(Params *p, int form, int format, int dtype, int n_sm) {
   const int epi = form == kOne || form == kStream ? kEpi<kOne> : kEpi<kPair>, at_once = form == kPair ? n_sm / 2 : n_sm;
   const bool many = p->split == 1 && p->items > at_once;       // CTAs have several tiles
   p->acc_bufs = many && epi / 4 * p->nt + 3 * p->sf_cols <= 512 ? epi / 4 : 1;
+  const bool narrow = p->tiles_n > 1 && p->nt < 128;
+  if (narrow && (many || p->split > 1)) return false;
+  p->acc = narrow ? 128 : p->nt;
+  if (narrow) p->vec = 0;
   // a column of tiles to a CTA, where that leaves none idle for long: w is loaded once, and 148 SMs do not all ask for the same part of it
   p->columns = 0;
   if (many && form != kPair && p->tiles_n <= at_once) {
@@ -926,14 +926,15 @@ bool lay_out(Params *p, int form, int format, int dtype, int n_sm) {
   if (form == kRows) {
     p->off_sfa = p->chunks_per * p->a_bytes;
     p->off_ring = p->off_sfa + p->chunks_per * atoms * kAtom;                  // a multiple of 1024
-    room -= p->off_ring;
   }
+  if (narrow && p->off_ring < (128 - p->nt) * 128) p->off_ring = (128 - p->nt) * 128;     // what a narrow tile's products read in front of its codes
+  room -= p->off_ring;
   p->w_stays = p->columns && (form == kOne || form == kStream) && (long long)p->chunks * p->w_bytes + 4ll * x_bytes <= room;
   if (p->w_stays) room -= p->chunks * p->w_bytes;
   p->stage_bytes = x_bytes + (p->w_stays ? 0 : p->w_bytes);    // multiples of 1024: nt is one of 16, a stage's scales are of 1024
   p->stages = room / p->stage_bytes;
   if (p->stages > kMaxStages) p->stages = kMaxStages;
-  if (p->acc_bufs * p->nt + p->stages * p->sf_cols > 512) p->stages = (512 - p->acc_bufs * p->nt) / p->sf_cols;
+  if (p->acc_bufs * p->acc + p->stages * p->sf_cols > 512) p->stages = (512 - p->acc_bufs * p->acc) / p->sf_cols;
   p->off_out = p->off_ring + p->stages * p->stage_bytes + (p->w_stays ? p->chunks * p->w_bytes : 0);
   return p->stages >= 2;
 }
@@ -943,26 +944,31 @@ bool lay_out(Params *p, int form, int format, int dtype, int n_sm) {
 // A cluster costs its meetings, and its parts their way between SMs.  Of the start 3.2 us, launch and first loads.
 double estimate(const Params &p, int form, int dtype, int n_sm) {
   static constexpr int kClusters[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};    // of that many CTAs that run at once, on 148 SMs
-  const double wide = p.nt / 128.0, type = dtype == DC_F32 ? 1.8 : 1.0;
+  const bool narrow = p.nt < p.acc;
+  const double wide = p.acc / 128.0, type = dtype == DC_F32 ? 1.8 : 1.0;
   const double stage = form == kPair ? (p.nt > 128 ? 0.47 : 0.43) : p.nt > 128 ? 0.44 + 0.16 * (wide - 1) : 0.3 + 0.14 * wide;
   const double w_total = (double)p.tiles_n * p.w_bytes * p.chunks * (form == kPair ? 2 : 1) / 4.5e6;
+  double cut = form == kRows ? 256.0 * p.rows * p.chunks_per * 115e-6 - 1.0 : 0;      // quantising; beside the first loads
+  if (cut < 0) cut = 0;
   if (p.split > 1) {
     const double main = p.chunks_per * stage, waves = dc_div_up(p.items, kClusters[p.split]);
-    return 3.2 + waves * ((main > w_total ? main : w_total) + 2.5 + p.part_rows * p.nt * 4 / 20e3) +
-           (form == kRows ? 256.0 * p.rows * p.chunks_per * 115e-6 : 0);
+    return 3.2 + waves * ((main > w_total ? main : w_total) + 1.2 + 0.4 * p.split + p.part_rows * p.nt * 4 / 16e3) +
+           cut;
   }
   const int at_once = form == kPair ? n_sm / 2 : n_sm;
   const double waves = p.columns ? dc_div_up(p.tiles_m, at_once / p.tiles_n) : dc_div_up(p.items, at_once);
   double main = p.chunks * stage, out = (form == kPair ? (p.nt > 128 ? 2.2 : 2.0) : wide) * type;
-  if (form == kRows) main += 256.0 * p.rows * p.chunks_per * 115e-6;
-  if (!p.vec) out *= 1.5;
+  main += cut;
+  if (narrow) out = 0.7 + (dtype == DC_F32 ? 0.2 : 0.7) * p.nt / 32;
+  else if (!p.vec) out *= dtype == DC_F32 ? 1.5 : 2.3;
   if (form == kStream) return 3.2 + waves * (0.2 + 0.6 * dc_div_up(p.c_in, 32) + 0.8 * out);   // quantising and reading out share the SM's ALUs
   const double total = 3.2 + (p.acc_bufs > 1 ? waves * (main > out ? main : out) : waves * (main + out));
   return total > 3.2 + w_total ? total : 3.2 + w_total;
 }
 
-// Fills p for the form that takes the least of the estimates.  Tiles of fewer than all of w's rows begin where a scale tile does: they have
-// 128 or 256 rows.
+// Fills p for the form that takes the least of the estimates.  Tiles of fewer than all of w's rows begin where a scale tile does, with 128 or
+// 256 rows, or are narrow, a part of one: where few tiles leave SMs idle and reading out is most of the time, more CTAs then read out (1001 x 1000 -> 1003
+// in fp32 7.1 us; tiles of 128 columns 9.2, halves of their reductions in a cluster 14).
 int choose(Params *p, bool raw, int format, int dtype, int n_sm, double *us_of) {
   double best = 1e30;
   Params best_p = *p;
@@ -991,6 +997,7 @@ int choose(Params *p, bool raw, int format, int dtype, int n_sm, double *us_of) 
       for (int s = 1; s <= kMaxSplit; ++s) look(kOne, whole < n ? whole : n, s);
       if (whole <= n) break;
     }
+    for (int n = 32; n < 128 && n < whole; n *= 2) look(kOne, n, 1);
     if (p->rows > 128 && whole > 128) {
       look(kPair, 256, 1);
       look(kPair, 128, 1);

@@ -412,3 +412,25 @@ def test_rows_that_begin_anywhere(cols, fmt, dtype):
         assert (np64(y) == Q.values(code, byte, fmt, g)).all()
         y.fill_(7.0)
         assert (back.t == 7.0).all()
+
+
+# a part of a scale tile's columns to a tile; see test_q4_host.py
+NARROW = [(1001, 1000, 1003), (300, 320, 1001), (100, 320, 1001), (700, 640, 516), (129, 100, 260), (40, 3000, 333), (1, 64, 137)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows,c_in,c_out", NARROW)
+def test_narrow_tiles(rows, c_in, c_out, fmt, dtype):
+    """Such products read what lies around a tile's weights in shared memory: here what products of NaN left there."""
+    n = 600
+    bad = torch.full((n, 2048), float("nan"), device="cuda")
+    q = dc.Q4Matrix(n, 2048, fmt)
+    dc.q4_quantize(bad, q)
+    ws = torch.zeros(dc.conv_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    for residual in (False, True):
+        y = torch.empty(n, n, device="cuda")
+        dc.q4_product(q, q, None, dc.ACT_IDENTITY, None, y, ws)
+        assert torch.isnan(y).all()
+        run_product(rows, c_in, c_out, fmt, dtype, bias=not residual, residual=residual, act=dc.ACT_RELU6 if residual else dc.ACT_IDENTITY, forward=False,
+                    inplace=residual and rows % 2 == 0)

@@ -254,3 +254,21 @@ def test_binding_refuses_a_buffer_that_does_not_hold_its_matrix(native, monkeypa
                      lambda: dc.q4_forward(x, w, 1.0, None, 0, None, y, ws)):
             with pytest.raises(ValueError, match="buffer"):
                 call()
+
+
+def test_narrow_tiles_are_for_few_tiles_of_fp32_or_ragged_rows():
+    torch = pytest.importorskip("torch")
+    from tests import test_gpu_q4 as t
+    seen = set()
+    for rows, c_in, c_out in t.NARROW:
+        for fmt in (dc.MX4, dc.NV4):
+            for dtype in (dc.F32, dc.BF16):
+                p = dc.q4_plan(rows, c_in, c_out, fmt, dtype, False)
+                if p.tile_cols < 128:
+                    assert p.form == dc.Q4_TILES and p.split == 1 and p.accumulators == 1 and not p.columns
+                    seen.add((p.tile_cols, fmt, dtype))
+    assert seen >= {(n, f, d) for n, d in ((32, dc.F32), (32, dc.BF16), (64, dc.F32)) for f in (0, 1)}
+    # many tiles, and bf16 rows that begin on 16 bytes: whole scale tiles
+    for rows, c_in, c_out in ((128, 4096, 4096), (256, 1280, 1000), (6272, 320, 1280), (20000, 200, 520)):
+        assert dc.q4_plan(rows, c_in, c_out, dc.NV4, dc.BF16, False).tile_cols >= 128
+    assert dc.q4_plan(20000, 200, 521, dc.NV4, dc.F32, False).tile_cols >= 128

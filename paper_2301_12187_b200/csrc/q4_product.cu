@@ -466,17 +466,20 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     bool ok = !P || rank == 0;
     if (FORM == kRows && ok) ok = warp_wait(&bar[kXFull], 0, abort_flag, ws, 0x50000u);
     if (p.w_stays && ok) ok = warp_wait(&bar[kWFull], 0, abort_flag, ws, 0x60000u);
-    for (int item = first; ok && item < items; item += step) {
-      ok = warp_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x20000u | (uint32_t)buf);
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t d = tmem + (uint32_t)(buf * p.acc), idesc = q4_idesc<F>(p.acc, P ? 256 : 128);
-      const uint32_t shift = (uint32_t)inside(p.nt < p.acc ? column_of(item) : 0) * 128u;
-      for (int ch = c0; ch < c1; ++ch) {
-        ok = warp_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x30000u | (uint32_t)stage);
+    // One lane, without the others: with a meeting of the warp for each stage a stage of 128 x 128 took 750 cycles, of which the products are 264.  The next
+    // stage's barrier is asked for ahead of this one's instructions.
+    if (elect_one()) {
+      uint32_t ready = 0;
+      for (int item = first; ok && item < items; item += step) {
+        ok = mbar_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x20000u | (uint32_t)buf);
         if (!ok) break;
         tc_fence_after();
-        if (elect_one()) {
+        const uint32_t d = tmem + (uint32_t)(buf * p.acc), idesc = q4_idesc<F>(p.acc, P ? 256 : 128);
+        const uint32_t shift = (uint32_t)inside(p.nt < p.acc ? column_of(item) : 0) * 128u;
+        for (int ch = c0; ch < c1; ++ch) {
+          if (!ready) ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x30000u | (uint32_t)stage);
+          if (!ok) break;
+          ready = stage + 1 < p.stages ? mbar_test(&bar[kFull + stage + 1], parity) : mbar_test(&bar[kFull], parity ^ 1u);
           const uint32_t at = ring + (uint32_t)(stage * p.stage_bytes);
           const uint32_t a = FORM == kRows ? sm + (uint32_t)((ch - c0) * p.a_bytes) : at;
           const uint32_t sfa = FORM == kRows ? sm + (uint32_t)(p.off_sfa + (ch - c0) * kAtoms * kAtom) : at + (uint32_t)p.a_bytes;
@@ -487,12 +490,12 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           else multiply_steps<F, P, 1>(steps, d, a, b - shift, sfa, sfb, ta, idesc, ch > c0);
           commit<P>(&bar[kEmpty + stage]);
           if (ch == c1 - 1) commit<P>(&bar[kDFull + buf]);
+          if (++stage == p.stages) { stage = 0; parity ^= 1u; }
         }
-        __syncwarp();
-        if (++stage == p.stages) { stage = 0; parity ^= 1u; }
+        if (++buf == p.acc_bufs) { buf = 0; ++use; }
       }
-      if (++buf == p.acc_bufs) { buf = 0; ++use; }
     }
+    __syncwarp();
   } else if (warp < 2 + kEpi<FORM>) {
     // ---------------------------------------------------------------- read out
     const int quad = warp & 3, set = (warp - 2) >> 2;

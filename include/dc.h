@@ -412,7 +412,7 @@ dc_status dc_q4_workspace_bytes(long long rows, int c_in, dc_q4_format format, s
  * Product of two quantised matrices of one format:  y[r][o] = act(scale * sum_i X[r][i] W[o][i] + bias[o] + residual[r][o]).
  * x: [rows] x [c_in], w: [c_out] x [c_in], both from dc_q4_quantize, their values here without the tensor scales: `scale` is the product of
  * the two (any finite number; 1 for DC_MX4).  y: [rows][c_out] of `dtype`, dense; residual: the same or NULL, may be y; bias: fp32 [c_out] or
- * NULL.  On the tensor core: products exact, sums in fp32.  workspace: device, >= dc_conv_workspace_bytes(), zeroed once by the
+ * NULL.  y overlaps nothing else.  On the tensor core: products exact, sums in fp32.  workspace: device, >= dc_conv_workspace_bytes(), zeroed once by the
  * caller; a bounded wait that runs out is latched there (dc_workspace_status).  Calls that may run at once need a workspace each.
  */
 dc_status dc_q4_product(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, float scale,
@@ -421,7 +421,7 @@ dc_status dc_q4_product(const void *x, long long rows, int c_in, const void *w, 
 
 /*
  * Forward pass of a 1x1 layer of stride 1 with weights in 4 bits: dc_q4_quantize of x ([rows][c_in] of `dtype`, dense, with x_scale), then
- * dc_q4_product with w (quantised with w_scale) -- the same results to the bit, except that sums may be added up in another order.  Few rows are
+ * dc_q4_product with w (quantised with w_scale) -- the same results to the bit, except that sums may be added up in another order.  y overlaps nothing but residual.  Few rows are
  * quantised in the product's own launch; many into the workspace: device, >= dc_q4_workspace_bytes, its first 256 bytes zeroed once.
  */
 dc_status dc_q4_forward(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, float x_scale,
@@ -432,7 +432,7 @@ dc_status dc_q4_forward(const void *x, long long rows, int c_in, const void *w, 
  * Host only, launches nothing: how dc_q4_forward (forward = 1) or dc_q4_product (0) would run, for reports and tests.
  */
 typedef enum {
-  DC_Q4_TILES = 0,           /* tiles of 128 rows, each by one CTA, or its reduction by a cluster of `split` */
+  DC_Q4_TILES = 0,           /* tiles of 128 rows and 32 to 256 columns, each by one CTA, or its reduction by a cluster of `split` */
   DC_Q4_PAIRS = 1,           /* tiles of 256 rows by two CTAs */
   DC_Q4_FEW_ROWS = 2,        /* dc_q4_forward: rows quantised in the product's launch, and kept in shared memory */
   DC_Q4_STREAM = 3           /* dc_q4_forward: rows quantised in the product's launch, tile by tile */

@@ -733,63 +733,66 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       __syncwarp();
     }
   } else {
-    // ---------------------------------------------------------------- quantise (kStream): a thread to a row, 32 columns at a time; the next 32, of the
-    // next stage or tile too, are asked for before these are worked on
+    // ---------------------------------------------------------------- quantise (kStream): a thread to a row, 32 of its up to 64 columns at a time.  The next
+    // kDeep runs of 32, of the next tiles, are on their way: with one the loads' latency was a tile's time (200704 x 24 -> 48 20.0 us).
     const int r = (warp - 2 - kEpi<FORM>) * 32 + lane;
-    constexpr int kRaw = 32 / kPer<T>;
-    uint4 next[kRaw];
-    auto ask = [&](int item, int ch, int c) {    // columns c .. c + 31 of a stage
-      const long long row = (long long)(item % p.tiles_m) * 128 + r;
-      const int col = ch * kStageCols + c;
-      const T *at = x + (size_t)row * (size_t)p.c_in + col;
+    constexpr int kRaw = 32 / kPer<T>, kDeep = sizeof(T) == 2 ? 3 : 2;
+    uint4 next[kDeep][kRaw];
+    int ask_item = first, ask_c = 0;
+    auto ask = [&](uint4 *to) {
+      const long long row = (long long)ask_item * 128 + r;
+      const uint4 *at = reinterpret_cast<const uint4 *>(x + (size_t)row * (size_t)p.c_in + ask_c);
+      const bool here = ask_item < items && row < p.rows;
 #pragma unroll
-      for (int i = 0; i < kRaw; ++i)
-        next[i] = row < p.rows && col + i * kPer<T> < p.c_in ? __ldg(reinterpret_cast<const uint4 *>(at) + i) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < kRaw; ++i) to[i] = here && ask_c + i * kPer<T> < p.c_in ? __ldg(at + i) : make_uint4(0, 0, 0, 0);
+      ask_c += 32;
+      if (ask_c >= p.c_in) { ask_c = 0; ask_item += step; }
     };
-    int item = first, ch = 0, stage = 0;
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) ask(next[k]);
+    int item = first, c = 0, stage = 0;
     uint32_t parity = 0;
     bool ok = true;
-    if (item < items) ask(item, ch, 0);
     while (ok && item < items) {
-      ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x70000u | (uint32_t)stage);
-      if (!ok) break;
-      const uint32_t a = ring + (uint32_t)(stage * p.stage_bytes) + (uint32_t)((r >> 3) * 1024 + (r & 7) * 128);
-      const uint32_t sfa = ring + (uint32_t)(stage * p.stage_bytes) + kA;
-      const int item0 = item, ch0 = ch, some = min(p.c_in - ch * kStageCols, kStageCols), end = (some + 63) / 64 * 64;     // columns; whole runs of 64
-      if (++ch == p.chunks) { ch = 0; item += step; }
-#pragma unroll 1
-      for (int c = 0; c < end; c += 32) {
-        uint4 raw[kRaw];
 #pragma unroll
-        for (int i = 0; i < kRaw; ++i) raw[i] = next[i];
-        if (c + 32 < some) ask(item0, ch0, c + 32);
-        else if (c < some && item < items) ask(item, ch, 0);
-        uint2 code[2] = {make_uint2(0, 0), make_uint2(0, 0)};
-        uint32_t byte[2] = {0, 0};
-        if (c < some) {                          // what a run of 64 columns has behind the last one is 0
-          uint32_t top[2];
+      for (int k = 0; k < kDeep; ++k) {
+        if (!ok || item >= items) break;         // the same for all lanes
+        if (c == 0) ok = warp_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x70000u | (uint32_t)stage);
+        if (!ok) break;
+        const uint32_t at = ring + (uint32_t)(stage * p.stage_bytes), a = at + (uint32_t)((r >> 3) * 1024 + (r & 7) * 128), sfa = at + kA;
+        auto put = [&](int col, uint4 code, uint32_t byte) {
+          sts_u4(a + (uint32_t)(((col >> 5) ^ (r & 7)) * 16), code);
+          const uint32_t to = sfa + q4::scale_at((uint32_t)r, (uint32_t)(F == DC_NV4 ? col >> 4 : col >> 5));
+          if (F == DC_NV4) asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"((uint16_t)byte) : "memory");
+          else asm volatile("st.shared.b8 [%0], %1;" ::"r"(to), "r"(byte) : "memory");
+        };
+        uint32_t top[2];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) top[h] = largest16<T>(raw + h * kRaw / 2);
-          if (F == DC_MX4) top[0] = top[1] = max(top[0], top[1]);
+        for (int h = 0; h < 2; ++h) top[h] = largest16<T>(next[k] + h * kRaw / 2);
+        if (F == DC_MX4) top[0] = top[1] = max(top[0], top[1]);
+        uint2 code[2];
+        uint32_t byte = 0;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float v[16];
+        for (int h = 0; h < 2; ++h) {
+          float v[16];
 #pragma unroll
-            for (int i = 0; i < kRaw / 2; ++i) unpack16<T>(raw[h * kRaw / 2 + i], v + i * kPer<T>);
-            const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.r6);
-            code[h] = q4::codes16<F, sizeof(T) == 2>(v, s);
-            byte[h] = s.byte;
-          }
+          for (int i = 0; i < kRaw / 2; ++i) unpack16<T>(next[k][h * kRaw / 2 + i], v + i * kPer<T>);
+          const q4::BlockScale s = q4::block_scale<F>(top[h], p.g, p.r6);
+          code[h] = q4::codes16<F, sizeof(T) == 2>(v, s);
+          byte |= F == DC_NV4 ? s.byte << (8 * h) : s.byte;
         }
-        sts_u4(a + (uint32_t)(((c >> 5) ^ (r & 7)) * 16), make_uint4(code[0].x, code[0].y, code[1].x, code[1].y));
-        const uint32_t blk = (uint32_t)(F == DC_NV4 ? c >> 4 : c >> 5), to = sfa + (blk >> 2) * kAtom + q4::scale_at((uint32_t)r, blk);
-        if (F == DC_NV4) asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"((uint16_t)(byte[0] | (byte[1] << 8))) : "memory");
-        else asm volatile("st.shared.b8 [%0], %1;" ::"r"(to), "r"(byte[0]) : "memory");
+        ask(next[k]);
+        put(c, make_uint4(code[0].x, code[0].y, code[1].x, code[1].y), byte);
+        if (c == 0 && p.c_in <= 32) put(32, make_uint4(0, 0, 0, 0), 0);        // what a run of 64 columns has behind the last one is 0
+        c += 32;
+        if (c < p.c_in) continue;
+        c = 0;
+        item += step;
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar[kFull + stage]);
+        if (++stage == p.stages) { stage = 0; parity ^= 1u; }
       }
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bar[kFull + stage]);
-      if (++stage == p.stages) { stage = 0; parity ^= 1u; }
     }
   }
   if (parts && warp == 1) {                      // read out: tensor memory goes back while the parts are on their way

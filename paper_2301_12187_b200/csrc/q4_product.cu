@@ -968,7 +968,7 @@ double estimate(const Params &p, int form, int dtype, int n_sm) {
   main += cut;
   if (narrow) out = 0.7 + (dtype == DC_F32 ? 0.2 : 0.7) * p.nt / 32;
   else if (!p.vec) out *= dtype == DC_F32 ? 1.5 : 2.3;
-  if (form == kStream) return 3.2 + waves * (0.2 + 0.6 * dc_div_up(p.c_in, 32) + 0.8 * out);   // quantising and reading out share the SM's ALUs
+  if (form == kStream) return 3.2 + waves * ((dtype == DC_F32 ? 1.2 : 0.65) * dc_div_up(p.c_in, 32) + 0.95 * out);   // quantising and reading out share the SM's ALUs
   const double total = 3.2 + (p.acc_bufs > 1 ? waves * (main > out ? main : out) : waves * (main + out));
   return total > 3.2 + w_total ? total : 3.2 + w_total;
 }
@@ -1066,7 +1066,8 @@ bool in_one_launch(Params *p, Params *q, dc_q4_format format, dc_dtype dtype, in
   *form = choose(p, true, format, dtype, n_sm, &us);
   *apart = choose(q, false, format, dtype, n_sm, &us_apart);
   const double row = p->c_in * (dtype == DC_F32 ? 4.0 : 2.0) + (p->c_in < 64 ? 36.0 : p->c_in * 0.57);
-  return *form >= 0 && us <= us_apart + 2.0 + (double)p->rows * row / 3.5e6;
+  // a product that keeps all of w waits 2 us for it behind the launch that quantised
+  return *form >= 0 && us <= us_apart + (q->w_stays && q->tiles_n == 1 ? 4.0 : 2.0) + (double)p->rows * row / 3.5e6;
 }
 
 }  // namespace

@@ -9,8 +9,8 @@
 // slot's scales are written over only behind the products that read them.  One warp loads, one issues, eight or twelve read out the accumulators.
 // CTAs walk over tiles.  The forms:
 //   kOne     both operands by TMA.  Few tiles: a cluster shares a tile's reduction.  Each of its CTAs owns some columns of the result; all send their
-//            parts of them to its shared memory, and it adds them up in rank order.  (With parts left where they were, two meetings of the cluster and
-//            reads from afar: one row of 4096 x 4096 7.4 us.)  Tensor memory is given back without waiting for a CTA that may be waiting for
+//            parts of them to its shared memory, and it adds them up in rank order.  (Parts left where they were would take two meetings of the
+//            cluster and reads from afar.)  Tensor memory is given back without waiting for a CTA that may be waiting for
 //            some.  One column of tiles to a CTA and few stages: w stays in shared memory.
 //            Narrow tiles, of 32 or 64 columns: the products are those of 128 rows of w around the tile's, of which only the tile's are there; the rest is
 //            what lies around them in shared memory, and is not read out.

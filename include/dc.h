@@ -411,7 +411,8 @@ dc_status dc_q4_workspace_bytes(long long rows, int c_in, dc_q4_format format, s
 /*
  * Product of two quantised matrices of one format:  y[r][o] = act(scale * sum_i X[r][i] W[o][i] + bias[o] + residual[r][o]).
  * x: [rows] x [c_in], w: [c_out] x [c_in], both from dc_q4_quantize, their values here without the tensor scales: `scale` is the product of
- * the two (any finite number; 1 for DC_MX4).  y: [rows][c_out] of `dtype`, dense; residual: the same or NULL, may be y; bias: fp32 [c_out] or
+ * the two (any finite number; 1 for DC_MX4.  Below 2^-126 fp32 has fewer bits and then none: a product of scales that it does not hold loses
+ * results that it could).  y: [rows][c_out] of `dtype`, dense; residual: the same or NULL, may be y; bias: fp32 [c_out] or
  * NULL.  y overlaps nothing else.  On the tensor core: products exact, sums in fp32.  workspace: device, >= dc_conv_workspace_bytes(), zeroed once by the
  * caller; a bounded wait that runs out is latched there (dc_workspace_status).  Calls that may run at once need a workspace each.
  */
@@ -421,8 +422,9 @@ dc_status dc_q4_product(const void *x, long long rows, int c_in, const void *w, 
 
 /*
  * Forward pass of a 1x1 layer of stride 1 with weights in 4 bits: dc_q4_quantize of x ([rows][c_in] of `dtype`, dense, with x_scale), then
- * dc_q4_product with w (quantised with w_scale) -- the same results to the bit, except that sums may be added up in another order.  y overlaps nothing but residual.  Few rows are
- * quantised in the product's own launch; many into the workspace: device, >= dc_q4_workspace_bytes, its first 256 bytes zeroed once.
+ * dc_q4_product with w (quantised with w_scale) -- the same results to the bit, except that sums may be added up in another order.
+ * x_scale * w_scale: 2^-149 to 2^127, what fp32 holds of powers of two (DC_ERR_INVALID_ARG beyond).  y overlaps nothing but residual.
+ * Few rows are quantised in the product's own launch; many into the workspace: device, >= dc_q4_workspace_bytes, its first 256 bytes zeroed once.
  */
 dc_status dc_q4_forward(const void *x, long long rows, int c_in, const void *w, int c_out, dc_q4_format format, float x_scale,
                         float w_scale, const float *bias, dc_act act, const void *residual, void *y, dc_dtype dtype, void *workspace,

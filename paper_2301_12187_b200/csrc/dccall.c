@@ -6,6 +6,7 @@
  * is no int, ...): dc.py then makes the call through ctypes, which reports what is wrong with them. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <float.h>
 
 typedef int (*conv_fn)(const void *, int, int, int, const void *, const void *, const void *, int, const void *, void *, int,
                        void *, size_t, void *, int);
@@ -272,6 +273,11 @@ static PyObject *q4_dequantize(PyObject *self, PyObject *const *a, Py_ssize_t n)
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(st);
 }
+/* a product of two tensor scales that fp32 rounds to 0, or to a subnormal number with fewer bits */
+static int is_lost(double a, double b) {
+  const double p = a * b;
+  return (p == 0 && a != 0 && b != 0) || (p < FLT_MIN && p > -FLT_MIN && (double)(float)p != p);
+}
 /* q4_product(x, w, bias, act, residual, y, workspace, stream) */
 static PyObject *q4_product(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   (void)self;
@@ -281,6 +287,7 @@ static PyObject *q4_product(PyObject *self, PyObject *const *a, Py_ssize_t n) {
   void *b, *r, *y, *ws, *stream;
   size_t bytes;
   if (n != 8 || !g_q4_product || current_device(&dev) || read_matrix(a[0], dev, &x) || read_matrix(a[1], dev, &w) || x.fmt != w.fmt || x.cols != w.cols ||
+      is_lost(x.scale, w.scale) ||
       w.rows > 2147483647LL || read_dtype(a[5], &code) || read_bias(a[2], dev, w.rows, &b) || read_int(a[3], &act) ||
       read_dense(a[4], dev, &x.rows, w.rows, code, 1, &r) || read_dense(a[5], dev, &x.rows, w.rows, code, 0, &y) || read_here(a[6], dev, &ws) ||
       read_bytes(a[6], &bytes) || read_stream(a[7], &stream))

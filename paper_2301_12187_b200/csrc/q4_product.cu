@@ -1133,7 +1133,7 @@ extern "C" dc_status dc_q4_forward(const void *x, long long rows, int c_in, cons
   if (s != DC_OK) return s;
   if (!q4::tensor_scale_ok(x_scale, format) || !q4::tensor_scale_ok(w_scale, format)) return DC_ERR_INVALID_ARG;
   const float scale = x_scale * w_scale;
-  if (!(scale - scale == 0.f)) return DC_ERR_INVALID_ARG;
+  if (!(scale - scale == 0.f) || scale == 0.f) return DC_ERR_INVALID_ARG;         // powers of two: exact from 2^-149 on
   if (workspace_bytes < sizeof(DcWsHeader) + lx.bytes) return DC_ERR_WORKSPACE;
   Params p = params_of(rows, c_in, c_out, act, dtype, scale);
   p.g = x_scale;

@@ -628,7 +628,10 @@ def q4_product(x: Q4Matrix, w: Q4Matrix, bias, act, residual, y, workspace, stre
     _dense(y, x.rows, w.rows, y.dtype, "q4_product")
     _dense(residual, x.rows, w.rows, y.dtype, "q4_product")
     _bias(bias, w.rows, "q4_product")
-    _check(lib().dc_q4_product(_ptr(x.data), x.rows, x.cols, _ptr(w.data), w.rows, x.fmt, x.tensor_scale * w.tensor_scale, _ptr(bias),
+    scale = x.tensor_scale * w.tensor_scale
+    if (scale == 0 and x.tensor_scale != 0 != w.tensor_scale) or (abs(scale) < 2.0 ** -126 and C.c_float(scale).value != scale):
+        raise ValueError("q4_product: fp32 does not hold the product of the tensor scales, %g and %g" % (x.tensor_scale, w.tensor_scale))
+    _check(lib().dc_q4_product(_ptr(x.data), x.rows, x.cols, _ptr(w.data), w.rows, x.fmt, scale, _ptr(bias),
                                act, _ptr(residual), _ptr(y), dtype_code(y.dtype), _ptr(workspace),
                                workspace.numel() * workspace.element_size(), _stream(stream)), "dc_q4_product")
 

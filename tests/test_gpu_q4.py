@@ -434,3 +434,29 @@ def test_narrow_tiles(rows, c_in, c_out, fmt, dtype):
         assert torch.isnan(y).all()
         run_product(rows, c_in, c_out, fmt, dtype, bias=not residual, residual=residual, act=dc.ACT_RELU6 if residual else dc.ACT_IDENTITY, forward=False,
                     inplace=residual and rows % 2 == 0)
+
+
+@pytest.mark.parametrize("forward", [False, True])
+@pytest.mark.parametrize("a,b", [(-100, -49), (-100, -40), (-49, -100), (100, 27), (27, 100)])
+def test_both_ends_of_the_tensor_scales(a, b, forward):
+    """Products of tensor scales at either end of fp32.  Below, results are fp32 sums times a subnormal power of two: exact but for one rounding, by at
+    most half of the smallest subnormal number, or of a unit in the last place."""
+    rows, c_in, c_out, fmt = 5, 64, 24, dc.NV4
+    r = np.random.default_rng(abs(a * 3 + b))
+    up = a > 0
+    size = 2.0 ** -7 if up else 300.0            # of block scales: a sum times 2^127 has to stay finite (64 * 36 * 2^-14 < 1)
+    x, w = (torch.from_numpy((r.uniform(-6, 6, (n, c_in)) * size).astype(np.float32) * np.float32(2.0 ** e)).cuda() for n, e in ((rows, a), (c_out, b)))
+    xq, wq = dc.Q4Matrix(rows, c_in, fmt, 2.0 ** a), dc.Q4Matrix(c_out, c_in, fmt, 2.0 ** b)
+    dc.q4_quantize(w, wq)
+    y = torch.empty(rows, c_out, device="cuda")
+    ws = torch.zeros(dc.q4_workspace_bytes(rows, c_in, fmt), dtype=torch.uint8, device="cuda")
+    if forward:
+        dc.q4_forward(x, wq, 2.0 ** a, None, dc.ACT_IDENTITY, None, y, ws)
+    else:
+        dc.q4_quantize(x, xq)
+        dc.q4_product(xq, wq, None, dc.ACT_IDENTITY, None, y, ws)
+    xv, wv = Q.stands_for(np64(x), fmt, 2.0 ** a), Q.stands_for(np64(w), fmt, 2.0 ** b)
+    ref, s = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    assert (np.abs(ref) > 2.0 ** -149).mean() > 0.9 and np.abs(ref).max() < 2.0 ** 128
+    err = np.abs(np64(y) - ref)
+    assert (err <= c_in * 2.0 ** -23 * s + 2.0 ** -24 * np.abs(ref) + 2.0 ** -150).all(), err.max()

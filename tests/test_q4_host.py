@@ -272,3 +272,29 @@ def test_narrow_tiles_are_for_few_tiles_of_fp32_or_ragged_rows():
     for rows, c_in, c_out in ((128, 4096, 4096), (256, 1280, 1000), (6272, 320, 1280), (20000, 200, 520)):
         assert dc.q4_plan(rows, c_in, c_out, dc.NV4, dc.BF16, False).tile_cols >= 128
     assert dc.q4_plan(20000, 200, 521, dc.NV4, dc.F32, False).tile_cols >= 128
+
+
+@pytest.mark.parametrize("fmt", [dc.NV4])
+def test_forward_refuses_tensor_scales_whose_product_fp32_does_not_hold(fmt):
+    """Sums of codes times block scales pass 2^22: a product of scales that fp32 rounds to 0 would leave bias + residual of results that it can hold."""
+    size = dc.q4_workspace_bytes(4, 64, fmt)
+
+    def call(x_scale, w_scale):
+        return dc.lib().dc_q4_forward(FAKE, 4, 64, FAKE, 16, fmt, x_scale, w_scale, None, 0, None, FAKE, dc.BF16, FAKE, size, None)
+
+    for a, b in ((100, 28), (100, 100), (-100, -50), (-50, -100), (-100, -60), (-100, -100)):
+        assert call(2.0 ** a, 2.0 ** b) == dc.ERR_INVALID_ARG, (a, b)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_product_refuses_tensor_scales_whose_product_fp32_does_not_hold(native, monkeypatch):
+    torch = pytest.importorskip("torch")
+    dc.lib()
+    if not native:
+        monkeypatch.setattr(dc, "_native", dc._NoNative)
+    y, ws = torch.zeros(4, 16), torch.zeros(1 << 16, dtype=torch.uint8)
+    # the last one: subnormal in fp32, with bits that it does not have there
+    for a, b in ((2.0 ** -100, 2.0 ** -50), (2.0 ** -100, -(2.0 ** -60)), (2.0 ** -100, 2.0 ** -100), (2.0 ** -60, 1e-300), (1.25 * 2.0 ** -100, 2.0 ** -48)):
+        x, w = dc.Q4Matrix(4, 40, dc.NV4, a, device="cpu"), dc.Q4Matrix(16, 40, dc.NV4, b, device="cpu")
+        with pytest.raises(ValueError, match="tensor scales"):
+            dc.q4_product(x, w, None, 0, None, y, ws, stream=_NullStream())

@@ -387,7 +387,8 @@ typedef enum { DC_MX4 = 0, DC_NV4 = 1 } dc_q4_format;
 /* Where things lie in a quantised matrix, one buffer of `bytes` bytes, 16-byte aligned.  Codes: row r begins at r * pitch, column c is the
  * low (c even) or high half of byte c / 2, and columns up to 2 * pitch are 0.  Scales: one byte a block, that of row r and block b at
  *   scale_offset + ((r / 128) * tiles + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4,
- * and those of rows and blocks that the matrix does not have are 0.  (Tiles of 128 rows x 4 blocks, as the tensor core takes them.) */
+ * and those of rows and blocks that the matrix does not have are 0, as is what lies between the last row's codes and scale_offset.
+ * (Tiles of 128 rows x 4 blocks, as the tensor core takes them.) */
 typedef struct { size_t pitch, tiles, scale_offset, bytes; } dc_q4_layout;
 
 /* Host only: the layout of a quantised matrix.  rows and cols >= 1; rows up to 2^31 - 256, cols up to 2^24 (DC_ERR_UNSUPPORTED). */

@@ -131,6 +131,10 @@ __global__ void __launch_bounds__(kThreads, VEC ? 6 : 5) k_q4_quantize(const T *
   __syncthreads();
   const uint32_t atom0 = col_tile * (uint32_t)atoms;
   const uint32_t left = p.tiles - atom0, n = left < (uint32_t)atoms ? left : (uint32_t)atoms;
+  if (blockIdx.x == 0) {                         // between the codes and the scales: up to 14 pieces of 16 bytes
+    const size_t at = (size_t)p.rows * p.pitch + (size_t)tid * 16;
+    if (at < p.scale_offset) *reinterpret_cast<uint4 *>(q + at) = make_uint4(0, 0, 0, 0);
+  }
   uint8_t *out = q + p.scale_offset + ((size_t)tile * p.tiles + atom0) * kAtom;
   if (p.groups == 1) {
     for (uint32_t i = tid; i < n * (kAtom / 16); i += kThreads) reinterpret_cast<uint4 *>(out)[i] = reinterpret_cast<const uint4 *>(scales)[i];

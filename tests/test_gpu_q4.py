@@ -460,3 +460,23 @@ def test_both_ends_of_the_tensor_scales(a, b, forward):
     assert (np.abs(ref) > 2.0 ** -149).mean() > 0.9 and np.abs(ref).max() < 2.0 ** 128
     err = np.abs(np64(y) - ref)
     assert (err <= c_in * 2.0 ** -23 * s + 2.0 ** -24 * np.abs(ref) + 2.0 ** -150).all(), err.max()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 24), (2, 64), (3, 65), (5, 64), (7, 1003), (127, 100), (128, 64), (129, 24), (1001, 1000), (40001, 33)])
+def test_every_byte_of_the_layout_is_written(rows, cols, fmt, dtype):
+    """Two buffers of other contents hold the same bytes behind it, and 0 between the codes and the scales."""
+    x = rand(rows, cols, 1, dtype=dtype).cuda()
+    g = 1.0 if fmt == dc.MX4 else 2.0 ** -7
+    got = []
+    for fill in (0x5A, 0xFF):
+        q = dc.Q4Matrix(rows, cols, fmt, g)
+        guard = Guarded(torch, (int(q.layout.bytes),), torch.uint8, fill=fill)
+        q.data = guard.t
+        dc.q4_quantize(x, q)
+        torch.cuda.synchronize()
+        guard.check("quantised matrix")
+        got.append(q.data.cpu())
+        assert (got[-1][rows * q.layout.pitch:q.layout.scale_offset] == 0).all()
+    assert torch.equal(*got)

@@ -380,7 +380,7 @@ dc_status dc_chain_forward_host_async(const dc_layer *layers, int n_layers, cons
  *   DC_NV4: blocks of 16, scale s g: s = a times the fp32 number 1 / (6 g), rounded to fp32, then to e4m3 (448 at most; nearest, ties to even),
  *   g = `tensor_scale`, a power of two for the whole matrix.
  * A value's code is the nearest to value / scale in real arithmetic, ties to the code with an even last bit, 6 at most.  A block with a NaN or an infinity gets the scale NaN: all of it
- * reads as NaN, and so do the results of its row (a NaN leaves DC_ACT_RELU6 as 0, or as 6 in bf16).  A block whose scale is 0 (a / (6 g) up to 2^-10) reads as 0.
+ * reads as NaN, and so do the results of its row (DC_ACT_RELU6 makes a NaN 0 where results are fp32, 6 where they are bf16).  A block whose scale is 0 (a / (6 g) up to 2^-10) reads as 0.
  * --------------------------------------------------------------------------------------------- */
 typedef enum { DC_MX4 = 0, DC_NV4 = 1 } dc_q4_format;
 

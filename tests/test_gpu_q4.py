@@ -480,3 +480,43 @@ def test_every_byte_of_the_layout_is_written(rows, cols, fmt, dtype):
         got.append(q.data.cpu())
         assert (got[-1][rows * q.layout.pitch:q.layout.scale_offset] == 0).all()
     assert torch.equal(*got)
+
+
+# whole tiles, pairs of CTAs, clusters and narrow tiles, with rows of y off 16 bytes too, few rows quantised in the launch (in a cluster, and not), streamed maps
+NAN_FORMS = [(300, 64, 72, False), (2000, 4096, 1536, False), (2000, 4096, 1501, False), (100, 8192, 128, False), (70, 9000, 131, False), (127, 2600, 511, False),
+             (700, 640, 517, False), (3000, 64, 101, False), (19111, 200, 521, False),
+             (1, 4096, 4096, True), (16, 256, 64, True), (7, 256, 133, True), (20000, 24, 144, True), (500, 1000, 200, True)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows,c_in,c_out,forward", NAN_FORMS)
+def test_a_nan_under_relu6_is_the_same_in_every_form(rows, c_in, c_out, forward, fmt, dtype):
+    """0 in fp32, 6 in bf16; from x, from the weights, from the bias and from the residual."""
+    x, w = rand(rows, c_in, 3, dtype=dtype).cuda(), rand(c_out, c_in, 4, 0.05).cuda()
+    bias, residual = torch.zeros(c_out, device="cuda"), torch.zeros(rows, c_out, dtype=TYPES[dtype], device="cuda")
+    bad = torch.zeros(rows, c_out, dtype=torch.bool, device="cuda")
+    x[rows // 2, c_in // 3] = float("nan")
+    bad[rows // 2] = True
+    w[c_out - 1, 5] = float("inf")
+    bad[:, c_out - 1] = True
+    bias[1] = float("nan")
+    bad[:, 1] = True
+    residual[0, c_out // 2] = float("nan")
+    g = 1.0 if fmt == dc.MX4 else 2.0 ** -8
+    wq, xq = dc.Q4Matrix(c_out, c_in, fmt, g), dc.Q4Matrix(rows, c_in, fmt, g)
+    dc.q4_quantize(w, wq)
+    dc.q4_quantize(x, xq)
+    ws = torch.zeros(dc.q4_workspace_bytes(rows, c_in, fmt), dtype=torch.uint8, device="cuda")
+    want = 0.0 if dtype == "f32" else 6.0
+    for res in (None, residual):
+        y = torch.full((rows, c_out), 3.5, dtype=TYPES[dtype], device="cuda")
+        if forward:
+            dc.q4_forward(x, wq, g, bias, dc.ACT_RELU6, res, y, ws)
+        else:
+            dc.q4_product(xq, wq, bias, dc.ACT_RELU6, res, y, ws)
+        if res is not None:
+            bad[0, c_out // 2] = True
+        assert dc.workspace_status(ws) == dc.OK
+        assert (y[bad] == want).all(), y[bad].unique()
+        assert ((y >= 0) & (y <= 6)).all()

@@ -170,6 +170,8 @@ def run_product(rows, c_in, c_out, fmt, dtype, bias, residual, act, forward, see
 
 
 # every form of the products, each with results that begin on 16 bytes and that do not, with residual and without: see test_q4_host.py
+# (As the estimate is now, (2000, 4096, 1500), (2100, 6000, 1536) and (520, 4096, 4099) run as pairs, one tile to each; test_gpu_q4_plans.py has the rest of
+# what it can pick.)
 FORMS = [
     (2000, 4096, 1500), (2100, 6000, 1536), (513, 8192, 2056), (700, 6000, 1101),          # pairs of CTAs
     (1200, 4100, 1208), (520, 4096, 4099),

@@ -1,6 +1,7 @@
-"""Oracle of the 4-bit matrices, in numpy and 64 bits, from the definitions: MX4 blocks of 32 with a power-of-two scale, NV4 blocks of
-16 with an e4m3 scale and a power of two for the whole matrix, codes e2m1, nearest, ties to the even code.  Shares nothing
-with the library but the layout of a quantised matrix, which include/dc.h fixes."""
+"""Oracle of the 4-bit matrices, in numpy, from the definitions: MX4 blocks of 32 with a power-of-two scale, NV4 blocks of
+16 with an e4m3 scale and a power of two for the whole matrix, codes e2m1, nearest, ties to the even code.  All in 64 bits but one step: NV4's
+scale comes from a product in fp32 with the fp32 number 1 / (6 g), as the format defines it (`exact_scale_byte` has the quotient of real arithmetic,
+to judge that step by).  Shares nothing with the library but the layout of a quantised matrix, which include/dc.h fixes."""
 import numpy as np
 
 E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
@@ -51,6 +52,12 @@ def quantize(x, fmt, g=1.0):
     code = nearest(u, E2M1) + np.where(np.signbit(v), 8, 0)
     code = np.where(odd[..., None], -1, code)     # any code: the block reads as NaN
     return code.reshape(rows, blocks * b)[:, :cols], byte
+
+
+def exact_scale_byte(top, g):
+    """NV4: e4m3 nearest to the quotient top / (6 g) of real arithmetic, 448 at most.  In 64 bits that is on the quotient's side of each border, or on the
+    border with it: top has at most 24 bits, and a border times 6 g at most 7."""
+    return nearest(np.asarray(top, dtype=np.float64) / (6.0 * g), E4M3)
 
 
 def scales(byte, fmt, g=1.0):

@@ -522,3 +522,18 @@ def test_a_nan_under_relu6_is_the_same_in_every_form(rows, c_in, c_out, forward,
         assert dc.workspace_status(ws) == dc.OK
         assert (y[bad] == want).all(), y[bad].unique()
         assert ((y >= 0) & (y <= 6)).all()
+
+
+@pytest.mark.parametrize("g", [1.0, 2.0 ** -8, 2.0 ** 13, 2.0 ** -100, 2.0 ** 100])
+def test_scales_of_every_bf16_magnitude_are_those_of_real_arithmetic(g):
+    """NV4's scale is a product with a rounded 1 / (6 g): for blocks of bf16 values that makes no difference."""
+    top = torch.from_numpy((np.arange(0x7f80, dtype=np.uint32) << 16).view(np.float32))
+    x = torch.zeros(top.numel(), 16, dtype=torch.bfloat16)
+    x[:, 5] = -top
+    want = Q.exact_scale_byte(top.numpy(), g)
+    for dtype in TYPES.values():
+        q, guard = matrix(top.numel(), 16, dc.NV4, g)
+        dc.q4_quantize(x.to(dtype).cuda(), q)
+        torch.cuda.synchronize()
+        guard.check("quantised matrix")
+        assert (Q.unpack(q.data.cpu().numpy(), top.numel(), 16, Q.NV4)[1][:top.numel(), 0] == want).all()

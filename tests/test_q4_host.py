@@ -298,3 +298,31 @@ def test_product_refuses_tensor_scales_whose_product_fp32_does_not_hold(native, 
         x, w = dc.Q4Matrix(4, 40, dc.NV4, a, device="cpu"), dc.Q4Matrix(16, 40, dc.NV4, b, device="cpu")
         with pytest.raises(ValueError, match="tensor scales"):
             dc.q4_product(x, w, None, 0, None, y, ws, stream=_NullStream())
+
+
+def all_bf16_magnitudes():
+    return (np.arange(0x7f80, dtype=np.uint32) << 16).view(np.float32)
+
+
+@pytest.mark.parametrize("g", [1.0, 2.0 ** -8, 2.0 ** 13, 2.0 ** -100, 2.0 ** 100])
+def test_oracle_scales_against_the_quotient_of_real_arithmetic(g):
+    """NV4's scale is a product in fp32 with 1 / (6 g): of a block of bf16 values the same byte as the quotient's, of fp32 values unless that lies within
+    2^-23 of a border.  (1 / (6 g) is rounded by 2^-25 of it, g being a power of two, and the product by at most 2^-24; a product below 2^-126, which loses
+    more, is far below the first border, 2^-10.)"""
+    top = all_bf16_magnitudes().astype(np.float64)
+    x = np.zeros((top.size, 16))
+    x[:, 3] = -top
+    assert (Q.quantize(x, Q.NV4, g)[1][:, 0] == Q.exact_scale_byte(top, g)).all()
+    r = np.random.default_rng(9)
+    mid = (Q.E4M3[1:] + Q.E4M3[:-1]) / 2
+    near = np.repeat((6.0 * g * mid).astype(np.float32)[:, None], 9, 1)                # borders, and the next numbers on either side
+    for i in range(4):
+        near[:, i] = np.nextafter(near[:, i + 1] if i else near[:, 8], np.float32(0))
+        near[:, 4 + i] = np.nextafter(near[:, 3 + i] if i else near[:, 8], np.float32(np.inf))
+    top = np.concatenate([near.ravel(), (np.exp(r.uniform(-8, 7, 20000)) * 6 * g).astype(np.float32)]).astype(np.float64)
+    x = np.zeros((top.size, 16))
+    x[:, 15] = top
+    byte, exact = Q.quantize(x, Q.NV4, g)[1][:, 0], Q.exact_scale_byte(top, g)
+    off = byte != exact
+    border = mid[np.minimum(byte, exact)[off]]
+    assert (np.abs(byte - exact) <= 1).all() and (np.abs(top[off] / (6 * g) / border - 1) <= 2.0 ** -23).all()

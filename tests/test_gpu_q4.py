@@ -537,3 +537,30 @@ def test_scales_of_every_bf16_magnitude_are_those_of_real_arithmetic(g):
         torch.cuda.synchronize()
         guard.check("quantised matrix")
         assert (Q.unpack(q.data.cpu().numpy(), top.numel(), 16, Q.NV4)[1][:top.numel(), 0] == want).all()
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows,c_in,c_out,forward", [(130, 200, 72, False), (40, 4096, 256, False), (3, 1000, 136, True), (20000, 48, 64, True)])
+def test_scales_of_far_magnitudes_multiply_exactly(rows, c_in, c_out, forward, fmt):
+    """x times a power of two and w divided by it: the same codes, other scales, the same results to the bit."""
+    x, w = rand(rows, c_in, 3, dtype="bf16").cuda(), rand(c_out, c_in, 4, 0.05).cuda()
+    g = 1.0 if fmt == dc.MX4 else 2.0 ** -7
+    got = []
+    for up in (0, 1, -40, 40, -90, 90, -110, 110):
+        gx, gw = (1.0, 1.0) if fmt == dc.MX4 else (g * 2.0 ** up, g * 2.0 ** -up)
+        if not 2.0 ** -100 <= min(gx, gw) <= max(gx, gw) <= 2.0 ** 100:
+            continue                             # (beyond what a tensor scale may be)
+        xs, ws = x * 2.0 ** up, w * 2.0 ** -up
+        xq, wq = dc.Q4Matrix(rows, c_in, fmt, gx), dc.Q4Matrix(c_out, c_in, fmt, gw)
+        dc.q4_quantize(ws, wq)
+        work = torch.zeros(dc.q4_workspace_bytes(rows, c_in, fmt), dtype=torch.uint8, device="cuda")
+        y = torch.empty(rows, c_out, dtype=torch.bfloat16, device="cuda")
+        if forward:
+            dc.q4_forward(xs, wq, gx, None, dc.ACT_IDENTITY, None, y, work)
+        else:
+            dc.q4_quantize(xs, xq)
+            dc.q4_product(xq, wq, None, dc.ACT_IDENTITY, None, y, work)
+        got.append(y)
+    assert len(got) >= 6 and torch.isfinite(got[0]).all() and (got[0] != 0).any()
+    for y in got[1:]:
+        assert torch.equal(y, got[0])

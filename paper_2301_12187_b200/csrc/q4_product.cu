@@ -14,13 +14,13 @@
 //            some.  One column of tiles to a CTA and few stages: w stays in shared memory.
 //            Narrow tiles, of 32 or 64 columns: the products are those of 128 rows of w around the tile's, of which only the tile's are there; the rest is
 //            what lies around them in shared memory, and is not read out.
-//            (6272 x 320 -> 1280 in mx4 8.8 us, results going out at 1.9 TB/s; 128 x 4096 -> 4096 in nv4 9.5.)
-//   kPair    two CTAs multiply 256 x 256 (cta_group::2): each loads half of either operand, which halves what an SM has to fetch of w.  8192^3 in nv4 203 to
-//            212 us, 5.2 to 5.4 PFLOP/s (178 without loads of codes; in long runs 246, the clock falls under the power cap).
+//            (6272 x 320 -> 1280 in mx4 8.8 us, a fill of as many bytes as its results 5.1; 128 x 4096 -> 4096 in nv4 9.5.)
+//   kPair    two CTAs multiply 256 x 256 (cta_group::2): each loads half of either operand, which halves what an SM has to fetch of w.  8192^3 in nv4 242 to
+//            246 us, 4.5 PFLOP/s, in calls one behind the other, the clock falls under the power cap; 203 to 212 in short runs (178 without loads of codes).
 //   kRows    up to 32 rows of bf16 or fp32: quantised by the reading-out warps into shared memory, where all of them stay.  One row of 4096 -> 4096 7.5 us:
 //            3.2 until the first products, four stages, the cluster's meeting.
 //   kStream  many rows of bf16 or fp32 and one column of tiles: four more warps quantise them, a stage at a time.
-//            200704 x 24 -> 144 21.2 us, results at 2.7 TB/s (quantised apart 26.2).
+//            200704 x 24 -> 144 21.2 us (quantised apart 26.2; a fill of as many bytes as its results 15.9).
 #include <string.h>
 
 #include "q4.cuh"
@@ -584,7 +584,8 @@ k_q4_product(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
         __syncwarp();
       };
-      // A pair reads all of a warp's columns before it works on them: its one accumulator is then free for the next tile's products.
+      // A pair reads all of a warp's columns before it works on them: its one accumulator is then free for the next tile's products.  These are 128 sums a
+      // lane, of 168 registers: 336 to 352 bytes of them are spilled (66 in the bf16 kernels of single tiles, at 128 registers).
       constexpr int kAhead = P ? 128 / kCols : 1;
 #pragma unroll 1
       for (int cc = c_first; cc < cols || cc == c_first; cc += kAhead * c_step) {
@@ -957,8 +958,8 @@ bool lay_out(Params *p, int form, int format, int dtype, int n_sm) {
   return p->stages >= 2;
 }
 
-// Estimated time of a form in microseconds, fitted to products in all their forms (1 to 200704 rows, 16 to 8192 columns of either operand): of 83
-// calls the chosen form took 1.4 % longer than the best one on average, 15 % at most.
+// Estimated time of a form in microseconds, fitted to products in all their forms (1 to 200704 rows, 16 to 8192 columns of either operand): of 106
+// calls timed in all their forms (1 to 401408 rows; products and forward calls) the chosen one took 1.2 % longer than the best on average, 14 % at most.
 // A stage takes its products or its loads; a tile's results go out beside the next tile's products where they have an accumulator of their own.
 // A cluster costs its meetings, and its parts their way between SMs.  Of the start 3.2 us, launch and first loads.
 double estimate(const Params &p, int form, int dtype, int n_sm) {
@@ -980,7 +981,7 @@ double estimate(const Params &p, int form, int dtype, int n_sm) {
   main += cut;
   if (narrow) out = 0.7 + (dtype == DC_F32 ? 0.2 : 0.7) * p.nt / 32;
   else if (!p.vec) out *= dtype == DC_F32 ? 1.5 : 2.3;
-  if (form == kStream) return 3.2 + waves * ((dtype == DC_F32 ? 1.2 : 0.65) * dc_div_up(p.c_in, 32) + 0.95 * out);   // quantising and reading out share the SM's ALUs
+  if (form == kStream) return 3.2 + waves * ((dtype == DC_F32 ? 1.2 : 0.65) * dc_div_up(p.c_in, 32) + 0.95 * out);   // fitted as a sum: the two take turns on a tile, no pipe is busy for more than a third of the time
   const double total = 3.2 + (p.acc_bufs > 1 ? waves * (main > out ? main : out) : waves * (main + out));
   return total > 3.2 + w_total ? total : 3.2 + w_total;
 }

@@ -450,6 +450,77 @@ typedef struct {
 dc_status dc_q4_plan_query(long long rows, int c_in, int c_out, dc_q4_format format, dc_dtype dtype, int forward, dc_q4_plan *plan);
 
 /* ---------------------------------------------------------------------------------------------
+ * Rows with weights of their own: products of rows that are grouped by the weights they go through (experts, tasks), and low-rank adapters
+ * beside a layer that all rows share (a request's, a task's), with their gradients.  (The paper has no counterpart: these are 1x1 layers --
+ * products of rows with weights, as in the section above -- whose weights depend on the row.)
+ *
+ * Runs.  Rows come sorted: run s is rows offsets[s] <= r < offsets[s + 1], offsets an array of 32-bit integers on the DEVICE, not
+ * decreasing, from 0 to at most `rows`.  A run may be empty, and rows in front of the first or behind the last run belong to none.  (Offsets are cut to
+ * [0, rows]; where they decrease, rows may be written twice, with no order between the two, and none outside the arrays.)
+ * Rows are dense, of `dtype`: DC_BF16 multiplies on the tensor core with fp32 sums, DC_F32 in fp32 FMAs; results are rounded once.
+ * rows: 0 to 2^30; without rows, forward calls write nothing.  Widths: 1 to 2^20.  Workspaces: device, the bytes that the query
+ * says, the first 256 zeroed once by the caller; a bounded wait that runs out is latched there (dc_workspace_status).  Calls that may run at
+ * once need a workspace each.
+ * --------------------------------------------------------------------------------------------- */
+
+/* Host only: bytes of workspace that dc_group_forward and dc_group_backward need. */
+dc_status dc_group_workspace_bytes(long long rows, int groups, int c_in, int c_out, dc_dtype dtype, size_t *bytes);
+
+/*
+ * y[r] = act(W_g x[r] + bias_g) for the rows r of each group g; rows of y that belong to no group stay as they are.  groups: 1 to 2^20.
+ * x: [rows][c_in]; offsets: [groups + 1]; w: [groups][c_out][c_in] of `dtype`; bias: fp32 [groups][c_out] or NULL; y: [rows][c_out].
+ * y overlaps nothing.
+ */
+dc_status dc_group_forward(const void *x, long long rows, int c_in, const int *offsets, int groups, const void *w, int c_out,
+                           const float *bias, dc_act act, void *y, dc_dtype dtype, void *workspace, size_t workspace_bytes,
+                           dc_stream stream);
+
+/*
+ * The gradients of dc_group_forward without activation, dy that of its results (behind an activation: of what the activation is given):
+ *   dx[r] = W_g^T dy[r] for the rows of each group (others stay as they are),  dw_g = sum_r dy[r] x[r]^T,  db_g = sum_r dy[r],
+ * all 0 of a group without rows.  dx: [rows][c_in], dw: [groups][c_out][c_in], of `dtype`; db: fp32 [groups][c_out].  What is not wanted is
+ * NULL, and so may be what it is made of (w for dx, x for dw).  Outputs overlap nothing.
+ */
+dc_status dc_group_backward(const void *dy, const void *x, long long rows, int c_in, const int *offsets, int groups, const void *w,
+                            int c_out, void *dx, void *dw, float *db, dc_dtype dtype, void *workspace, size_t workspace_bytes,
+                            dc_stream stream);
+
+/* Low-rank adapters of one rank for a layer c_in -> c_out; adapters of a lower rank have zeros in the rest. */
+typedef struct {
+  int count, rank;           /* 1 to 2^20 adapters; rank 1 to 128 */
+  const void *a;             /* device [count][rank][c_in] of the call's dtype */
+  const void *b;             /* device [count][c_out][rank] */
+  const float *scale;        /* device fp32 [count], or NULL: 1 */
+} dc_adapters;
+
+/* Host only: bytes of the buffer that dc_adapter_forward leaves for dc_adapter_backward, and of their workspace. */
+dc_status dc_adapter_saved_bytes(long long rows, int rank, dc_dtype dtype, size_t *bytes);
+dc_status dc_adapter_workspace_bytes(long long rows, int c_in, int c_out, const dc_adapters *adapters, dc_dtype dtype, size_t *bytes);
+
+/*
+ * y[r] = act(W x[r] + bias + residual[r] + B_a t[r]),  t[r] = scale_a A_a x[r],  a = which[s] the adapter of the run s that r is in; rows in no run, and
+ * those of a run whose `which` names none of the adapters (-1), go without.  Runs may have the same adapter.
+ * x: [rows][c_in]; w: [c_out][c_in] of `dtype`, or NULL: no such product (the adapters' part of a layer whose own part is
+ * in `residual`, of 4-bit weights for instance); offsets: [runs + 1], which: [runs], 32-bit integers on the device, runs 0 to 2^20;
+ * bias: fp32 [c_out] or NULL; residual: as y or NULL, may be y; y: [rows][c_out], overlaps nothing else.  saved: device, dc_adapter_saved_bytes,
+ * 16-byte aligned; keeps t of the rows that have an adapter (in 16 bits each, and not one bf16, where rows are bf16) for dc_adapter_backward.
+ */
+dc_status dc_adapter_forward(const void *x, long long rows, int c_in, const void *w, int c_out, const dc_adapters *adapters,
+                             const int *offsets, const int *which, int runs, const float *bias, dc_act act, const void *residual,
+                             void *saved, void *y, dc_dtype dtype, void *workspace, size_t workspace_bytes, dc_stream stream);
+
+/*
+ * The gradients of dc_adapter_forward without activation, dy that of its results, `saved` from the forward call with the same x, adapters and runs:
+ *   dx[r] = W^T dy[r] + A_a^T u[r],  u[r] = scale_a B_a^T dy[r];  da_a = sum_r u[r] x[r]^T,  db_a = sum_r dy[r] t[r]^T over the rows of all
+ * runs with the adapter, 0 of an adapter without rows.  W is frozen, and so is the scale.  dx: [rows][c_in] (w NULL: the adapters' part
+ * alone); da: [count][rank][c_in], db: [count][c_out][rank], of `dtype`.  What is not wanted is NULL, and so may be what it alone is made
+ * of (x for da, saved for db, w for dx).  Outputs overlap nothing.
+ */
+dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int c_in, const void *w, int c_out,
+                              const dc_adapters *adapters, const int *offsets, const int *which, int runs, const void *saved, void *dx,
+                              void *da, void *db, dc_dtype dtype, void *workspace, size_t workspace_bytes, dc_stream stream);
+
+/* ---------------------------------------------------------------------------------------------
  * The selector's two dynamic programmes (Sec. 4.3).  Host only: every pointer is host memory, no
  * device call is made.  Boundaries are 0..L for a network of L layers; tables are row-major
  * (L+1) x (L+1) and only entries [i][j] with i < j are read.

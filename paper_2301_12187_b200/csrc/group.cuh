@@ -1,0 +1,127 @@
+// Products of rows that belong to runs, each run with a weight matrix of its own, and low-rank adapters beside a shared matrix: what the
+// kernels of both families share.  The operators are described in include/dc.h.
+#pragma once
+
+#include "common.cuh"
+
+namespace grp {
+
+constexpr int kMaxRank = 128;
+constexpr int kMaxRuns = 1 << 20;
+
+// Runs of rows: run s is rows [offsets[s], offsets[s + 1]), cut to [0, rows), and belongs to weight which[s] where runs are mapped, else to
+// weight s.  Without offsets there is one run of all rows, of weight 0.
+struct Runs {
+  const int *offsets, *which;
+  int count;
+  int rows;
+  int weights;               // a run whose weight is not one of them has none
+  int mapped;
+};
+struct Run {
+  int begin, end, weight;    // weight < 0: none
+};
+__device__ __forceinline__ Run run_at(const Runs &r, int s) {
+  Run o;
+  if (!r.offsets) {
+    o.begin = 0;
+    o.end = s == 0 ? r.rows : 0;
+    o.weight = 0;
+    return o;
+  }
+  o.begin = min(max(__ldg(r.offsets + s), 0), r.rows);
+  o.end = min(max(__ldg(r.offsets + s + 1), o.begin), r.rows);
+  o.weight = r.mapped ? __ldg(r.which + s) : s;
+  if ((unsigned)o.weight >= (unsigned)r.weights) o.weight = -1;
+  return o;
+}
+
+// Finds a row tile among the runs' tiles of `tile` rows each, for callers that ask in increasing order.  All lanes of a warp call it and get
+// the same answer; 32 runs are looked at at a time.
+struct Walk {
+  int base;                  // runs before it are behind us
+  long long before;          // tiles of theirs
+  __device__ void start() { base = 0; before = 0; }
+  // items of a run: row tiles x per_tile.  false: there is no such item
+  __device__ bool find(const Runs &r, int tile, int per_tile, long long item, Run *run, int *index, long long *inside) {
+    const int lane = (int)(threadIdx.x & 31u);
+    for (; base < r.count; base += 32) {
+      Run o = {0, 0, -1};
+      if (base + lane < r.count) o = run_at(r, base + lane);
+      const int tiles = o.weight < 0 ? 0 : (int)(((unsigned)(o.end - o.begin) + (unsigned)tile - 1u) / (unsigned)tile);
+      const long long mine = (long long)tiles * per_tile;
+      long long upto = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += v;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, before + upto > item);
+      if (past) {
+        const int at = __ffs(past) - 1;
+        run->begin = __shfl_sync(0xffffffffu, o.begin, at);
+        run->end = __shfl_sync(0xffffffffu, o.end, at);
+        run->weight = __shfl_sync(0xffffffffu, o.weight, at);
+        *index = base + at;
+        *inside = item - (before + __shfl_sync(0xffffffffu, upto - mine, at));
+        return true;
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return false;
+  }
+};
+
+// The first run that ends behind `row` (runs in order: the one that holds it, or the next); runs.count: none.  One thread.
+__device__ __forceinline__ int first_run_behind(const Runs &r, int row) {
+  if (!r.offsets) return row < r.rows ? 0 : 1;
+  int lo = 0, hi = r.count;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(r.offsets + mid + 1) > row) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// What a row keeps of an adapter: `rank` numbers, padded with zeros to a multiple of 16.  fp32 rows: fp32.  bf16 rows: two bf16 terms, all the
+// high ones and then all the low ones, 16 bits together: with one bf16 alone the adapter's part of a result would be as far off as the
+// result's own rounding (2^-9), and so would its gradients.
+__host__ __device__ static inline int rank_pad(int rank) { return (rank + 15) / 16 * 16; }
+
+// y[r][o] = act(alpha_w * sum_k x[r][k] W_w(o, k) + sum_j t[r][j] E_e(o, j) + bias_w[o] + residual[r][o]) for the rows r of runs with a
+// weight w; e is the weight of the run of `ext` that r is in.
+struct RowsJob {
+  const void *x;
+  int rows, k, n;
+  const void *w;             // [weights][n][k], or with w_across [weights][k][n]; NULL: no such sum
+  int w_across;
+  Runs runs;
+  const float *alpha;        // one for each weight, or NULL
+  const void *t;             // [rows][rank_pad] as above, or NULL
+  const void *e;             // [weights][n][rank], or with e_across [weights][rank][n]
+  int rank, e_across;
+  Runs ext;
+  const float *bias;         // [n], or with bias_each [weights][n]
+  int bias_each, act;
+  const void *residual;
+  void *y;                   // [rows][n], or with y_terms what a row keeps of an adapter, n its rank
+  int y_terms;
+  dc_dtype dtype;
+};
+
+// out_w(i, j) = sum over the rows r of the runs of weight w of p[r][i] q[r][j]; 0 without rows
+struct GradJob {
+  const void *p, *q;         // [rows][m], [rows][n]; or with p_terms, q_terms what a row keeps of an adapter, m or n its rank
+  int m, n, p_terms, q_terms;
+  Runs runs;
+  void *out;                 // [weights][m][n]
+  float *sums;               // [weights][m]: sums of p over the rows, or NULL
+  dc_dtype dtype;
+};
+
+// kernels on CUDA cores, for any sizes (group_any.cu)
+cudaError_t rows_any(const RowsJob &j, cudaStream_t st);
+cudaError_t grad_any(const GradJob &j, cudaStream_t st);
+
+}  // namespace grp

@@ -63,6 +63,10 @@ class Q4Plan(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("form", "launches", "tile_cols", "split", "stages", "accumulators", "columns", "w_stays")]
 
 
+class AdapterSet(C.Structure):
+    _fields_ = [("count", C.c_int), ("rank", C.c_int), ("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p)]
+
+
 class Q4Layout(C.Structure):
     _fields_ = [("pitch", C.c_size_t), ("tiles", C.c_size_t), ("scale_offset", C.c_size_t), ("bytes", C.c_size_t)]
 
@@ -123,6 +127,19 @@ EXPORTS = {
     "dc_q4_forward": (C.c_int, [C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_float, C.c_void_p,
                                 C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
     "dc_q4_plan_query": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(Q4Plan)]),
+    "dc_group_workspace_bytes": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "dc_group_forward": (C.c_int, [C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_int,
+                                   C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "dc_group_backward": (C.c_int, [C.c_void_p, C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p,
+                                    C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "dc_adapter_saved_bytes": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.POINTER(C.c_size_t)]),
+    "dc_adapter_workspace_bytes": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.POINTER(AdapterSet), C.c_int, C.POINTER(C.c_size_t)]),
+    "dc_adapter_forward": (C.c_int, [C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.POINTER(AdapterSet), C.c_void_p, C.c_void_p,
+                                     C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t,
+                                     C.c_void_p]),
+    "dc_adapter_backward": (C.c_int, [C.c_void_p, C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.POINTER(AdapterSet), C.c_void_p,
+                                      C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t,
+                                      C.c_void_p]),
     "dc_workspace_status": (C.c_int, [C.c_void_p, C.c_void_p]),
     "dc_workspace_status_where": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_uint), C.POINTER(C.c_uint)]),
     "dc_selftest_bounded_wait": (C.c_int, [C.c_void_p, C.c_size_t, C.c_uint, C.c_void_p]),
@@ -660,6 +677,157 @@ def q4_plan(rows: int, c_in: int, c_out: int, fmt: int, dtype: int, forward: boo
     plan = Q4Plan()
     _check(lib().dc_q4_plan_query(rows, c_in, c_out, fmt, dtype, int(forward), C.byref(plan)), "dc_q4_plan_query")
     return plan
+
+
+# --------------------------------------------------------------------------- rows with weights of their own
+
+
+def _same_type(what: str, dtype, *tensors):
+    for t in tensors:
+        if t is not None and t.dtype != dtype:
+            raise ValueError("%s: tensors of %s and %s" % (what, dtype, t.dtype))
+
+
+def _numbers(t, n: int, what: str):
+    """An array of `n` 32-bit integers (offsets, or which weights)."""
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: %d neighbouring int32 values are wanted" % (what, n))
+
+
+def _shaped(t, shape, what: str):
+    if t is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError("%s: a dense tensor of %s is wanted, not %s" % (what, tuple(shape), tuple(t.shape)))
+
+
+def _fp32(t, what: str):
+    import torch
+    if t is not None and t.dtype != torch.float32:
+        raise ValueError("%s: must be fp32" % what)
+
+
+def _nbytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+def group_workspace_bytes(rows: int, groups: int, c_in: int, c_out: int, dtype: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().dc_group_workspace_bytes(rows, groups, c_in, c_out, dtype, C.byref(nbytes)), "dc_group_workspace_bytes")
+    return int(nbytes.value)
+
+
+def group_forward(x, offsets, w, bias, act, y, workspace, stream=None):
+    """y[r] = act(w[g] x[r] + bias[g]) for the rows offsets[g] <= r < offsets[g + 1] of every group; other rows of y stay as they are.
+    x: [..., c_in], w: [groups, c_out, c_in], y: [..., c_out], dense, of one dtype; bias: fp32 [groups, c_out] or None."""
+    if w.dim() != 3:
+        raise ValueError("group_forward: weights [groups, c_out, c_in] are wanted")
+    groups, c_out, c_in = w.shape
+    rows = x.numel() // c_in if c_in else 0
+    _here("group_forward", x, offsets, w, bias, y, workspace)
+    _same_type("group_forward", x.dtype, w, y)
+    _dense(x, rows, c_in, x.dtype, "group_forward")
+    _dense(y, rows, c_out, x.dtype, "group_forward")
+    _shaped(w, (groups, c_out, c_in), "group_forward")
+    _shaped(bias, (groups, c_out), "group_forward")
+    _fp32(bias, "group_forward: the bias")
+    _numbers(offsets, groups + 1, "group_forward: offsets")
+    _check(lib().dc_group_forward(_ptr(x), rows, c_in, _ptr(offsets), groups, _ptr(w), c_out, _ptr(bias), act, _ptr(y), dtype_code(x.dtype),
+                                  _ptr(workspace), _nbytes(workspace), _stream(stream)), "dc_group_forward")
+
+
+def group_backward(dy, x, offsets, w, dx, dw, db, workspace, stream=None):
+    """The gradients of group_forward (without activation) for dy: dx as x, dw as w, db fp32 [groups, c_out]; each may be None.  w gives the
+    sizes, and is read where dx is wanted."""
+    if w.dim() != 3:
+        raise ValueError("group_backward: weights [groups, c_out, c_in] are wanted")
+    groups, c_out, c_in = w.shape
+    rows = dy.numel() // c_out if c_out else 0
+    _here("group_backward", dy, x, offsets, w, dx, dw, db, workspace)
+    _same_type("group_backward", dy.dtype, x, w, dx, dw)
+    _dense(dy, rows, c_out, dy.dtype, "group_backward")
+    _dense(x, rows, c_in, dy.dtype, "group_backward")
+    _dense(dx, rows, c_in, dy.dtype, "group_backward")
+    _shaped(w, (groups, c_out, c_in), "group_backward")
+    _shaped(dw, (groups, c_out, c_in), "group_backward")
+    _shaped(db, (groups, c_out), "group_backward")
+    _fp32(db, "group_backward: the bias's gradient")
+    _numbers(offsets, groups + 1, "group_backward: offsets")
+    _check(lib().dc_group_backward(_ptr(dy), _ptr(x), rows, c_in, _ptr(offsets), groups, _ptr(w), c_out, _ptr(dx), _ptr(dw), _ptr(db),
+                                   dtype_code(dy.dtype), _ptr(workspace), _nbytes(workspace), _stream(stream)), "dc_group_backward")
+
+
+class Adapters:
+    """Low-rank adapters of a layer: a [count, rank, c_in], b [count, c_out, rank] of one dtype, scale fp32 [count] or None; `.c` is the
+    dc_adapters.  The tensors are the caller's, and are read by each call."""
+
+    def __init__(self, a, b, scale=None):
+        import torch
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2] or a.dtype != b.dtype:
+            raise ValueError("Adapters: a [count, rank, c_in] and b [count, c_out, rank] of one dtype are wanted")
+        if not a.is_contiguous() or not b.is_contiguous():
+            raise ValueError("Adapters: dense tensors are wanted")
+        if scale is not None and (scale.dtype != torch.float32 or tuple(scale.shape) != (a.shape[0],) or not scale.is_contiguous()):
+            raise ValueError("Adapters: scales must be %d fp32 values" % a.shape[0])
+        self.a, self.b, self.scale = a, b, scale
+        self.count, self.rank, self.c_in = (int(v) for v in a.shape)
+        self.c_out = int(b.shape[1])
+        self.dtype = dtype_code(a.dtype)
+        self.c = AdapterSet(self.count, self.rank, _ptr(a), _ptr(b), _ptr(scale))
+
+    def saved(self, rows: int):
+        """A buffer in which adapter_forward leaves for adapter_backward what its gradients need."""
+        import torch
+        nbytes = C.c_size_t(0)
+        _check(lib().dc_adapter_saved_bytes(rows, self.rank, self.dtype, C.byref(nbytes)), "dc_adapter_saved_bytes")
+        return torch.empty(int(nbytes.value), dtype=torch.uint8, device=self.a.device)
+
+
+def adapter_workspace_bytes(rows: int, c_in: int, c_out: int, adapters: Adapters, dtype: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().dc_adapter_workspace_bytes(rows, c_in, c_out, C.byref(adapters.c), dtype, C.byref(nbytes)), "dc_adapter_workspace_bytes")
+    return int(nbytes.value)
+
+
+def _adapter_call(what: str, rows: int, w, adapters: Adapters, offsets, which, saved, dtype):
+    _same_type(what, dtype, w, adapters.a, adapters.b)
+    _shaped(w, (adapters.c_out, adapters.c_in), what)
+    _numbers(which, which.numel(), what + ": which")
+    _numbers(offsets, which.numel() + 1, what + ": offsets")
+    if saved is not None:
+        need = rows * (-(-adapters.rank // 16) * 16) * 4
+        if _nbytes(saved) < need or not saved.is_contiguous():
+            raise ValueError("%s: a saved buffer of %d bytes is wanted" % (what, need))
+
+
+def adapter_forward(x, w, adapters: Adapters, offsets, which, bias, act, residual, saved, y, workspace, stream=None):
+    """y = act(x w^T + bias + residual + the adapters' part): the rows offsets[s] <= r < offsets[s + 1] have adapter which[s] (-1: none).
+    w: [c_out, c_in] or None; x: [..., c_in], y (and residual): [..., c_out], dense; bias: fp32 [c_out] or None; saved: adapters.saved(rows)."""
+    rows = x.numel() // adapters.c_in
+    _here("adapter_forward", x, w, adapters.a, adapters.b, adapters.scale, offsets, which, bias, residual, saved, y, workspace)
+    _adapter_call("adapter_forward", rows, w, adapters, offsets, which, saved, x.dtype)
+    _dense(x, rows, adapters.c_in, x.dtype, "adapter_forward")
+    _dense(y, rows, adapters.c_out, x.dtype, "adapter_forward")
+    _dense(residual, rows, adapters.c_out, x.dtype, "adapter_forward")
+    _bias(bias, adapters.c_out, "adapter_forward")
+    _check(lib().dc_adapter_forward(_ptr(x), rows, adapters.c_in, _ptr(w), adapters.c_out, C.byref(adapters.c), _ptr(offsets), _ptr(which),
+                                    which.numel(), _ptr(bias), act, _ptr(residual), _ptr(saved), _ptr(y), dtype_code(x.dtype),
+                                    _ptr(workspace), _nbytes(workspace), _stream(stream)), "dc_adapter_forward")
+
+
+def adapter_backward(dy, x, w, adapters: Adapters, offsets, which, saved, dx, da, db, workspace, stream=None):
+    """The gradients of adapter_forward (without activation) for dy: dx as x, da and db as the adapters' a and b; each may be None."""
+    rows = dy.numel() // adapters.c_out
+    _here("adapter_backward", dy, x, w, adapters.a, adapters.b, adapters.scale, offsets, which, saved, dx, da, db, workspace)
+    _same_type("adapter_backward", dy.dtype, da, db)
+    _adapter_call("adapter_backward", rows, w, adapters, offsets, which, saved, dy.dtype)
+    _dense(dy, rows, adapters.c_out, dy.dtype, "adapter_backward")
+    _dense(x, rows, adapters.c_in, dy.dtype, "adapter_backward")
+    _dense(dx, rows, adapters.c_in, dy.dtype, "adapter_backward")
+    _shaped(da, adapters.a.shape, "adapter_backward")
+    _shaped(db, adapters.b.shape, "adapter_backward")
+    _check(lib().dc_adapter_backward(_ptr(dy), _ptr(x), rows, adapters.c_in, _ptr(w), adapters.c_out, C.byref(adapters.c), _ptr(offsets),
+                                     _ptr(which), which.numel(), _ptr(saved), _ptr(dx), _ptr(da), _ptr(db), dtype_code(dy.dtype),
+                                     _ptr(workspace), _nbytes(workspace), _stream(stream)), "dc_adapter_backward")
 
 
 def workspace_status(workspace, stream=None) -> int:

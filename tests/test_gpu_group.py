@@ -1,0 +1,326 @@
+"""Grouped products and adapters on the GPU against the formulas in 64 bits, element by element.
+
+Tolerance of an element.  Products of two bf16 or fp32 numbers enter sums in fp32: each of the K additions of a sum loses at most 2^-23 of
+the sum S of its terms' magnitudes (additions that cut off) and each product of fp32 numbers 2^-24 of itself, so a sum may be off by (K + 1) 2^-23 S.
+Behind it come up to three roundings of fp32 (scale, bias, residual: 2^-23 of the magnitudes added, together with K + 4 in the place of K + 1) and the
+rounding to the result's type, finfo.eps / 2 of the value.  What a row keeps of an adapter (t, u) is a sum as above, of magnitudes T, held in
+fp32 or in two bf16 terms, which leaves 2^-16 of it at most (each of the two roundings halves of a last place: 2^-9 of 2^-9, with margin 2^-16); of
+what is made of it, each term may then be off by that share of its own magnitude.
+A gradient is also held against differences of the 64-bit forward formula."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2301_12187_b200 import dc
+from tests.parity_util import Guarded
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+U = 2.0 ** -23
+
+
+def rand(*shape, seed, dtype, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def check(got, want, slack, what):
+    """`slack`: what sums may lose; the result's rounding is added."""
+    got = got.double()
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    room = slack + half_step_of(got, want)
+    bad = ~((got - want).abs() <= room)
+    assert not bool(bad.any()), "%s: %d of %d off, first at %s: %r, not %r (room %.3g)" % (
+        what, int(bad.sum()), bad.numel(), bad.nonzero()[0].tolist(), float(got[bad][0]), float(want[bad][0]), float(room[bad][0]))
+
+
+_TYPE = {}
+
+
+def half_step_of(got, want):
+    return want.abs() * _TYPE["eps"] * 1.0001 + 1e-37
+
+
+def of_type(dtype):
+    _TYPE["eps"] = half_step(dtype)
+
+
+def runs_of(offsets):
+    o = offsets.tolist()
+    return list(zip(o[:-1], o[1:]))
+
+
+def group_want(x, off, w, bias, act):
+    """(y, slack, mask of rows that belong to a group), 64 bits."""
+    x, rows = x.double(), x.shape[0]
+    y = torch.zeros(rows, w.shape[1], dtype=torch.float64, device="cuda")
+    s, mine = torch.zeros_like(y), torch.zeros(rows, dtype=torch.bool, device="cuda")
+    k = x.shape[1]
+    for g, (lo, hi) in enumerate(runs_of(off)):
+        wg = w[g].double()
+        y[lo:hi] = x[lo:hi] @ wg.t()
+        s[lo:hi] = x[lo:hi].abs() @ wg.abs().t()
+        if bias is not None:
+            y[lo:hi] += bias[g].double()
+            s[lo:hi] += bias[g].double().abs()
+        mine[lo:hi] = True
+    return (y.clamp(0, 6) if act else y), (k + 4) * U * s, mine
+
+
+def offsets_of(sizes):
+    return torch.tensor(np.concatenate([[0], np.cumsum(sizes)]).tolist(), dtype=torch.int32, device="cuda")
+
+
+def workspace(nbytes):
+    g = Guarded(torch, (nbytes,), torch.uint8, fill=0)
+    return g
+
+
+# sizes of groups; rows behind the last one; c_in, c_out
+GROUPS = [
+    ([1], 0, 8, 8),
+    ([1], 0, 1, 1),
+    ([3, 0, 5], 2, 64, 64),
+    ([0, 0, 0, 7], 3, 72, 40),
+    ([1, 1, 1, 1, 1, 1, 1, 1], 0, 128, 136),
+    ([17, 1, 64, 65], 5, 200, 264),
+    ([130, 127, 0, 129, 1], 1, 96, 512),
+    ([300], 0, 1000, 320),
+    ([5, 9, 33], 4, 65, 131),
+    ([200, 3], 0, 67, 300),
+    ([2] * 40 + [0] * 30 + [9], 7, 256, 192),
+    ([16, 16, 31, 15], 0, 1024, 128),
+    ([700, 260, 515], 9, 520, 776),
+]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", range(len(GROUPS)))
+def test_group_forward(case, dtype):
+    sizes, tail, c_in, c_out = GROUPS[case]
+    dt, rows, n = TYPES[dtype], sum(sizes) + tail, len(sizes)
+    of_type(dt)
+    for bias_too, act in ((False, 0), (True, 1)):
+        x, w = rand(rows, c_in, seed=case, dtype=dt), rand(n, c_out, c_in, seed=case + 50, dtype=dt, scale=2.0 / c_in ** 0.5)
+        bias = rand(n, c_out, seed=case + 99, dtype=torch.float32) if bias_too else None
+        off = offsets_of(sizes)
+        want, slack, mine = group_want(x, off, w, bias, act)
+        y, ws = Guarded(torch, (rows, c_out), dt, fill=77.0), workspace(dc.group_workspace_bytes(rows, n, c_in, c_out, dc.dtype_code(dt)))
+        if tail:
+            x[-tail:] = float("nan")             # rows of no group
+        dc.group_forward(x, off, w, bias, act, y.t, ws.t)
+        torch.cuda.synchronize()
+        y.check("y"), ws.check("workspace")
+        assert dc.workspace_status(ws.t) == dc.OK
+        check(y.t[mine], want[mine], slack[mine], "y")
+        assert bool((y.t[~mine] == 77.0).all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", range(len(GROUPS)))
+def test_group_backward(case, dtype):
+    sizes, tail, c_in, c_out = GROUPS[case]
+    dt, rows, n = TYPES[dtype], sum(sizes) + tail, len(sizes)
+    of_type(dt)
+    x, dy = rand(rows, c_in, seed=case + 3, dtype=dt), rand(rows, c_out, seed=case + 4, dtype=dt)
+    w = rand(n, c_out, c_in, seed=case + 5, dtype=dt, scale=2.0 / c_in ** 0.5)
+    if tail:
+        x[-tail:] = float("nan")
+        dy[-tail:] = float("inf")
+    off = offsets_of(sizes)
+    dx, dw = Guarded(torch, (rows, c_in), dt, fill=55.0), Guarded(torch, (n, c_out, c_in), dt, fill=float("nan"))
+    db, ws = Guarded(torch, (n, c_out), torch.float32, fill=float("nan")), workspace(dc.group_workspace_bytes(rows, n, c_in, c_out, dc.dtype_code(dt)))
+    dc.group_backward(dy, x, off, w, dx.t, dw.t, db.t, ws.t)
+    torch.cuda.synchronize()
+    for g in (dx, dw, db, ws):
+        g.check("group_backward")
+    assert dc.workspace_status(ws.t) == dc.OK
+    mine = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    for g, (lo, hi) in enumerate(runs_of(off)):
+        a, b, wg = dy[lo:hi].double(), x[lo:hi].double(), w[g].double()
+        check(dx.t[lo:hi], a @ wg, (c_out + 4) * U * (a.abs() @ wg.abs()), "dx")
+        check(dw.t[g], a.t() @ b, (hi - lo + 4) * U * (a.abs().t() @ b.abs()), "dw")
+        assert bool(((db.t[g].double() - a.sum(0)).abs() <= (hi - lo + 4) * U * a.abs().sum(0)).all())
+        mine[lo:hi] = True
+    assert bool((dx.t[~mine] == 55.0).all())
+
+
+def test_group_backward_parts_alone():
+    """Each gradient without the others, and without what it does not need, gives the same bits."""
+    sizes, c_in, c_out = [33, 0, 130], 72, 264
+    x, dy = rand(163, c_in, seed=1, dtype=torch.bfloat16), rand(163, c_out, seed=2, dtype=torch.bfloat16)
+    w, off = rand(3, c_out, c_in, seed=3, dtype=torch.bfloat16), offsets_of(sizes)
+    ws = torch.zeros(dc.group_workspace_bytes(163, 3, c_in, c_out, dc.BF16), dtype=torch.uint8, device="cuda")
+    dx, dw, db = torch.zeros_like(x), torch.zeros_like(w), torch.zeros(3, c_out, device="cuda")
+    dc.group_backward(dy, x, off, w, dx, dw, db, ws)
+    dx1, dw1, db1 = torch.ones_like(x), torch.ones_like(w), torch.ones(3, c_out, device="cuda")
+    dc.group_backward(dy, None, off, w, dx1, None, None, ws)
+    dc.group_backward(dy, x, off, w, None, dw1, None, ws)
+    dc.group_backward(dy, None, off, w, None, None, db1, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, dx1) and torch.equal(dw, dw1) and torch.equal(db, db1)
+
+
+def test_group_without_rows():
+    w, off = rand(3, 24, 16, seed=3, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32, device="cuda")
+    x, dy = torch.empty(0, 16, dtype=torch.bfloat16, device="cuda"), torch.empty(0, 24, dtype=torch.bfloat16, device="cuda")
+    ws = torch.zeros(dc.group_workspace_bytes(0, 3, 16, 24, dc.BF16), dtype=torch.uint8, device="cuda")
+    dc.group_forward(x, off, w, None, 0, dy, ws)
+    dw, db = torch.full_like(w, 9.0), torch.full((3, 24), 9.0, device="cuda")
+    dc.group_backward(dy, x, off, w, torch.empty_like(x), dw, db, ws)
+    torch.cuda.synchronize()
+    assert not bool(dw.any()) and not bool(db.any())
+
+
+# runs: (rows, adapter); rows in front and behind without one; adapters, rank, c_in, c_out
+ADAPTERS = [
+    ([(1, 0)], 0, 1, 8, 8, 8),
+    ([(1, 0)], 0, 1, 1, 1, 1),
+    ([(1, 2), (1, 0), (1, -1), (1, 2)], 0, 3, 16, 256, 136),
+    ([(1, i % 5) for i in range(64)], 0, 5, 16, 128, 264),
+    ([(1, i % 7 - 1) for i in range(100)], 3, 6, 32, 200, 128),
+    ([(2, 1), (3, 0), (0, 1), (40, 1), (5, 9)], 2, 2, 8, 64, 72),
+    ([(300, 1), (1, 0), (17, -1), (129, 1)], 6, 2, 64, 136, 320),
+    ([(128, 0), (128, 1), (256, 0)], 0, 2, 16, 512, 256),
+    ([(61, 3), (70, 2)], 0, 4, 5, 96, 104),
+    ([(33, 0), (120, 1)], 1, 2, 128, 72, 520),
+    ([(20, 1), (90, 0)], 4, 2, 100, 131, 67),
+    ([(1, 0), (1, 1)], 0, 2, 12, 33, 1001),
+    ([], 9, 2, 16, 64, 64),
+    ([(450, 0)], 0, 1, 48, 264, 1032),
+]
+
+
+def adapter_inputs(case, dtype, shared=True):
+    runs, tail, n, r, c_in, c_out = ADAPTERS[case]
+    dt, rows = TYPES[dtype], sum(k for k, _ in runs) + tail
+    x = rand(rows, c_in, seed=case + 11, dtype=dt)
+    w = rand(c_out, c_in, seed=case + 12, dtype=dt, scale=1.0 / c_in ** 0.5) if shared else None
+    a, b = rand(n, r, c_in, seed=case + 13, dtype=dt, scale=1.0 / c_in ** 0.5), rand(n, c_out, r, seed=case + 14, dtype=dt, scale=1.0 / r ** 0.5)
+    scale = 0.25 + rand(n, seed=case + 15, dtype=torch.float32).abs()
+    off = offsets_of([k for k, _ in runs])
+    which = torch.tensor([k for _, k in runs], dtype=torch.int32, device="cuda")
+    return x, w, a, b, scale, off, which
+
+
+def keeps(dt):
+    """Share of a term's magnitude that holding t (or u) may lose."""
+    return 2.0 ** -16 if dt == torch.bfloat16 else 2.0 ** -24
+
+
+def adapter_want(x, w, a, b, scale, off, which):
+    """(y, slack) of the products and the adapters' part, in 64 bits; (t, its magnitudes) of every run with an adapter."""
+    dt, rows, r = x.dtype, x.shape[0], a.shape[1]
+    xd = x.double()
+    y, s = torch.zeros(rows, b.shape[1], dtype=torch.float64, device="cuda"), torch.zeros(rows, b.shape[1], dtype=torch.float64, device="cuda")
+    k = x.shape[1]
+    if w is not None:
+        y, s = xd @ w.double().t(), (xd.abs() @ w.double().abs().t()) * (k + r + 8) * U
+    kept = []
+    for (lo, hi), i in zip(runs_of(off), which.tolist()):
+        if not 0 <= i < a.shape[0]:
+            continue
+        ad, bd, f = a[i].double(), b[i].double(), float(scale[i]) if scale is not None else 1.0
+        t, m = f * (xd[lo:hi] @ ad.t()), f * (xd[lo:hi].abs() @ ad.abs().t())
+        off_t = (k + 4) * U * m + keeps(dt) * t.abs()
+        y[lo:hi] += t @ bd.t()
+        s[lo:hi] += off_t @ bd.abs().t() + (k + 2 * r + 8) * U * (t.abs() @ bd.abs().t())
+        kept.append((lo, hi, i, t, off_t))
+    return y, s, kept
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", range(len(ADAPTERS)))
+@pytest.mark.parametrize("form", ["plain", "all", "beside"])
+def test_adapter_forward(form, case, dtype):
+    x, w, a, b, scale, off, which = adapter_inputs(case, dtype, form != "beside")
+    dt, rows, c_out = x.dtype, x.shape[0], b.shape[1]
+    of_type(dt)
+    want, slack, _ = adapter_want(x, w, a, b, scale if form != "plain" else None, off, which)
+    bias = rand(c_out, seed=case, dtype=torch.float32) if form == "all" else None
+    residual = rand(rows, c_out, seed=case + 1, dtype=dt) if form != "plain" else None
+    if bias is not None:
+        want, slack = want + bias.double(), slack + 4 * U * bias.double().abs()
+    if residual is not None:
+        want, slack = want + residual.double(), slack + 4 * U * (residual.double().abs() + want.abs())
+    act = int(form == "all")
+    ad = dc.Adapters(a, b, scale if form != "plain" else None)
+    y, ws = Guarded(torch, (rows, c_out), dt, fill=float("nan")), workspace(dc.adapter_workspace_bytes(rows, ad.c_in, c_out, ad, ad.dtype))
+    saved = Guarded(torch, (ad.saved(rows).numel(),), torch.uint8, fill=0xFF)
+    if form == "beside":                         # in place
+        y.t.copy_(residual)
+        residual = y.t
+    dc.adapter_forward(x, w, ad, off, which, bias, act, residual, saved.t, y.t, ws.t)
+    torch.cuda.synchronize()
+    y.check("y"), ws.check("workspace"), saved.check("saved")
+    assert dc.workspace_status(ws.t) == dc.OK
+    check(y.t, want.clamp(0, 6) if act else want, slack, "y")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", range(len(ADAPTERS)))
+@pytest.mark.parametrize("shared", [True, False])
+def test_adapter_backward(shared, case, dtype):
+    x, w, a, b, scale, off, which = adapter_inputs(case, dtype, shared)
+    dt, rows, c_in, c_out, r = x.dtype, x.shape[0], x.shape[1], b.shape[1], a.shape[1]
+    of_type(dt)
+    dy = rand(rows, c_out, seed=case + 77, dtype=dt)
+    ad = dc.Adapters(a, b, scale)
+    ws, saved = workspace(dc.adapter_workspace_bytes(rows, c_in, c_out, ad, ad.dtype)), Guarded(torch, (ad.saved(rows).numel(),), torch.uint8, fill=0xFF)
+    dc.adapter_forward(x, w, ad, off, which, None, 0, None, saved.t, torch.empty(rows, c_out, dtype=dt, device="cuda"), ws.t)
+    ws.t[256:] = 0xFF                            # nothing is expected of it
+    dx, da, db = Guarded(torch, (rows, c_in), dt, fill=float("nan")), Guarded(torch, tuple(a.shape), dt, fill=float("nan")), Guarded(torch, tuple(b.shape), dt, fill=float("nan"))
+    dc.adapter_backward(dy, x, w, ad, off, which, saved.t, dx.t, da.t, db.t, ws.t)
+    torch.cuda.synchronize()
+    for g in (dx, da, db, ws, saved):
+        g.check("adapter_backward")
+    assert dc.workspace_status(ws.t) == dc.OK
+    # dx is the forward formula of dy with the matrices turned round
+    want, slack, back = adapter_want(dy, w.t().contiguous() if shared else None, b.transpose(1, 2).contiguous(), a.transpose(1, 2).contiguous(), scale, off, which)
+    check(dx.t, want, slack, "dx")
+    _, _, ahead = adapter_want(x, None, a, b, scale, off, which)
+    da_want, da_slack = torch.zeros(a.shape, dtype=torch.float64, device="cuda"), torch.zeros(a.shape, dtype=torch.float64, device="cuda")
+    db_want, db_slack = torch.zeros(b.shape, dtype=torch.float64, device="cuda"), torch.zeros(b.shape, dtype=torch.float64, device="cuda")
+    for (lo, hi, i, t, off_t), (_, _, _, u, off_u) in zip(ahead, back):
+        xs, ds = x[lo:hi].double(), dy[lo:hi].double()
+        da_want[i] += u.t() @ xs
+        da_slack[i] += off_u.t() @ xs.abs() + (rows + 8) * U * (u.abs().t() @ xs.abs())
+        db_want[i] += ds.t() @ t
+        db_slack[i] += ds.abs().t() @ off_t + (rows + 8) * U * (ds.abs().t() @ t.abs())
+    check(da.t, da_want, da_slack, "da")
+    check(db.t, db_want, db_slack, "db")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_gradients_against_differences(dtype):
+    """d/de of <forward(p + e v), dy> in 64 bits against <gradient, v>: the formula is linear in x, and in a and b apart."""
+    x, w, a, b, scale, off, which = adapter_inputs(6, dtype)
+    dt, rows, c_out = x.dtype, x.shape[0], b.shape[1]
+    dy, ad = rand(rows, c_out, seed=5, dtype=dt), dc.Adapters(a, b, scale)
+    ws, saved = torch.zeros(dc.adapter_workspace_bytes(rows, ad.c_in, c_out, ad, ad.dtype), dtype=torch.uint8, device="cuda"), ad.saved(rows)
+    dc.adapter_forward(x, w, ad, off, which, None, 0, None, saved, torch.empty_like(dy), ws)
+    dx, da, db = torch.empty_like(x), torch.empty_like(a), torch.empty_like(b)
+    dc.adapter_backward(dy, x, w, ad, off, which, saved, dx, da, db, ws)
+    torch.cuda.synchronize()
+
+    def f(x, a, b):
+        y = x @ w.double().t()
+        for (lo, hi), i in zip(runs_of(off), which.tolist()):
+            if i >= 0:
+                y[lo:hi] += float(scale[i]) * (x[lo:hi] @ a[i].t()) @ b[i].t()
+        return float((y * dy.double()).sum())
+
+    p = [x.double(), a.double(), b.double()]
+    for k, grad in enumerate((dx, da, db)):
+        v = rand(*grad.shape, seed=40 + k, dtype=torch.float64)
+        up, down = list(p), list(p)
+        up[k], down[k] = p[k] + v, p[k] - v
+        slope = (f(*up) - f(*down)) / 2
+        # each element of the gradient is off by its rounding and a little; signs are random, the sum of all is a bound
+        room = float((grad.double() * v).abs().sum()) * (half_step(dt) + 2.0 ** -15)
+        assert abs(float((grad.double() * v).sum()) - slope) <= room, (k, slope, room)

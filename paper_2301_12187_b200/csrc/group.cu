@@ -28,14 +28,34 @@ dc_status status(cudaError_t e) { return e == cudaSuccess && cudaGetLastError() 
 
 size_t saved_bytes(long long rows, int rank) { return (size_t)rows * (size_t)rank_pad(rank) * 4; }
 
-struct Need {
+// A workspace's parts, one behind the other: `base` NULL where only their bytes are wanted.  bf16 rows that do not begin on 16 bytes are copied to rows that do: the tensor core's
+// kernels read by TMA, and a copy takes a tenth of the time that reading value by value cost.
+struct Parts {
+  uint8_t *base;
+  dc_dtype dtype;
+  cudaStream_t st;
   size_t bytes = sizeof(DcWsHeader);
-  size_t add(size_t n) {
-    const size_t at = bytes;
+  cudaError_t e = cudaSuccess;
+  void *add(size_t n) {
+    uint8_t *at = base ? base + bytes : nullptr;
     bytes += dc_round_up(n, 256);
     return at;
   }
+  bool apart(int cols) const { return dtype == DC_BF16 && cols % 8 != 0; }
+  int pitch(int cols) const { return apart(cols) ? (int)dc_round_up((size_t)cols, 8) : cols; }
+  void reserve(long long rows, int cols) {
+    if (apart(cols)) add((size_t)rows * (size_t)pitch(cols) * 2);
+  }
+  const void *rows_of(const void *x, long long rows, int cols) {
+    if (!x || rows == 0 || !apart(cols)) return x;
+    void *to = add((size_t)rows * (size_t)pitch(cols) * 2);
+    if (e == cudaSuccess) e = pitch_tc(x, to, rows, cols, pitch(cols), st);
+    return to;
+  }
 };
+cudaError_t rows_any_or_tc(const RowsJob &j, bool behind_narrow, void *workspace, cudaStream_t st) {
+  return j.dtype == DC_BF16 ? rows_tc(j, behind_narrow, (DcWsHeader *)workspace, st) : rows_any(j, st);
+}
 
 }  // namespace
 
@@ -44,7 +64,11 @@ extern "C" dc_status dc_group_workspace_bytes(long long rows, int groups, int c_
   if (s != DC_OK) return s;
   if (!bytes || groups < 1) return DC_ERR_INVALID_ARG;
   if (groups > kMaxRuns) return DC_ERR_UNSUPPORTED;
-  *bytes = Need().bytes;
+  Parts need = {nullptr, dtype, nullptr};
+  need.reserve(rows, c_in);
+  need.reserve(rows, c_out);
+  need.reserve((long long)groups * c_out, c_in);
+  *bytes = need.bytes;
   return DC_OK;
 }
 
@@ -59,19 +83,22 @@ extern "C" dc_status dc_group_forward(const void *x, long long rows, int c_in, c
   if (!workspace || workspace_bytes < need) return DC_ERR_WORKSPACE;
   if (!aligned({x, w, bias, y, workspace}) || (reinterpret_cast<uintptr_t>(offsets) & 3u)) return DC_ERR_ALIGNMENT;
   if (rows == 0) return DC_OK;
+  Parts parts = {(uint8_t *)workspace, dtype, (cudaStream_t)stream};
   RowsJob j = {};
-  j.x = x;
+  j.x = parts.rows_of(x, rows, c_in);
   j.rows = (int)rows;
   j.k = c_in;
   j.n = c_out;
-  j.w = w;
+  j.w = parts.rows_of(w, (long long)groups * c_out, c_in);
+  j.x_pitch = j.w_pitch = parts.pitch(c_in);
+  if (parts.e != cudaSuccess) return status(parts.e);
   j.runs = {offsets, nullptr, groups, (int)rows, groups, 0};
   j.bias = bias;
   j.bias_each = 1;
   j.act = (int)act;
   j.y = y;
   j.dtype = dtype;
-  return status(rows_any(j, (cudaStream_t)stream));
+  return status(rows_any_or_tc(j, false, workspace, (cudaStream_t)stream));
 }
 
 extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long rows, int c_in, const int *offsets, int groups,
@@ -85,31 +112,38 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
   if (!aligned({dy, x, w, dx, dw, db, workspace}) || (reinterpret_cast<uintptr_t>(offsets) & 3u)) return DC_ERR_ALIGNMENT;
   if (rows == 0 && !dw && !db) return DC_OK;
   const Runs runs = {offsets, nullptr, groups, (int)rows, groups, 0};
-  cudaError_t e = cudaSuccess;
-  if (dx && rows) {
+  Parts parts = {(uint8_t *)workspace, dtype, (cudaStream_t)stream};
+  const void *dy_at = parts.rows_of(dy, rows, c_out), *x_at = dw ? parts.rows_of(x, rows, c_in) : nullptr;
+  const void *w_at = dx ? parts.rows_of(w, (long long)groups * c_out, c_in) : nullptr;
+  cudaError_t e = parts.e;
+  if (dx && rows && e == cudaSuccess) {
     RowsJob j = {};
-    j.x = dy;
+    j.x = dy_at;
     j.rows = (int)rows;
     j.k = c_out;
     j.n = c_in;
-    j.w = w;
+    j.w = w_at;
     j.w_across = 1;
+    j.x_pitch = parts.pitch(c_out);
+    j.w_pitch = parts.pitch(c_in);
     j.runs = runs;
     j.y = dx;
     j.dtype = dtype;
-    e = rows_any(j, (cudaStream_t)stream);
+    e = rows_any_or_tc(j, false, workspace, (cudaStream_t)stream);
   }
   if ((dw || db) && e == cudaSuccess) {
     GradJob j = {};
-    j.p = dy;
-    j.q = x;
+    j.p = dy_at;
+    j.q = x_at;
+    j.p_pitch = parts.pitch(c_out);
+    j.q_pitch = parts.pitch(c_in);
     j.m = c_out;
     j.n = c_in;
     j.runs = runs;
     j.out = dw;
     j.sums = db;
     j.dtype = dtype;
-    e = grad_any(j, (cudaStream_t)stream);
+    e = dtype == DC_BF16 ? grad_tc(j, (DcWsHeader *)workspace, (cudaStream_t)stream) : grad_any(j, (cudaStream_t)stream);
   }
   return status(e);
 }
@@ -127,9 +161,14 @@ extern "C" dc_status dc_adapter_workspace_bytes(long long rows, int c_in, int c_
   if (s == DC_OK) s = check_adapters(adapters);
   if (s != DC_OK) return s;
   if (!bytes) return DC_ERR_INVALID_ARG;
-  Need n;
-  n.add(saved_bytes(rows, adapters->rank));      // u
-  *bytes = n.bytes;
+  Parts need = {nullptr, dtype, nullptr};
+  need.add(saved_bytes(rows, adapters->rank));   // u
+  need.reserve(rows, c_in);
+  need.reserve(rows, c_out);
+  need.reserve(c_out, c_in);
+  need.reserve((long long)adapters->count * adapters->rank, c_in);
+  need.reserve((long long)adapters->count * c_out, adapters->rank);
+  *bytes = need.bytes;
   return DC_OK;
 }
 
@@ -148,23 +187,26 @@ dc_status check_adapter_call(long long rows, int c_in, int c_out, const void *w,
     return DC_ERR_ALIGNMENT;
   return DC_OK;
 }
-// out = rows of x through the adapters' first matrices (a, or in the backward pass b read across), scaled
-cudaError_t narrow(const void *x, int rows, int k, const dc_adapters *ad, bool backward, const Runs &runs, void *out, dc_dtype dtype,
-                   cudaStream_t st) {
-  if (runs.count == 0) return cudaSuccess;
+// Rows through the adapters' first matrices -- a, or in the backward pass b read across -- scaled, to `out`.  *apart: by the kernel behind which the next launch may start early.
+cudaError_t narrow(const void *x, int x_pitch, int rows, int k, const void *m, int m_pitch, bool backward, const dc_adapters *ad, const Runs &runs, void *out,
+                   dc_dtype dtype, void *workspace, cudaStream_t st, bool *apart) {
   RowsJob j = {};
   j.x = x;
   j.rows = rows;
   j.k = k;
   j.n = ad->rank;
-  j.w = backward ? ad->b : ad->a;
+  j.w = m;
   j.w_across = backward;
+  j.x_pitch = x_pitch;
+  j.w_pitch = m_pitch;
   j.runs = runs;
   j.alpha = ad->scale;
   j.y = out;
   j.y_terms = 1;
   j.dtype = dtype;
-  return rows_any(j, st);
+  *apart = dtype == DC_BF16 && runs.count && narrow_apart(j);
+  if (runs.count == 0) return cudaSuccess;
+  return *apart ? narrow_tc(j, st) : rows_any_or_tc(j, false, workspace, st);
 }
 }  // namespace
 
@@ -179,17 +221,27 @@ extern "C" dc_status dc_adapter_forward(const void *x, long long rows, int c_in,
   if (!aligned({x, bias, residual, saved, y})) return DC_ERR_ALIGNMENT;
   if (rows == 0) return DC_OK;
   const Runs of = {offsets, which, runs, (int)rows, adapters->count, 1}, all = {nullptr, nullptr, 1, (int)rows, 1, 0};
-  cudaError_t e = narrow(x, (int)rows, c_in, adapters, false, of, saved, dtype, (cudaStream_t)stream);
+  const cudaStream_t st = (cudaStream_t)stream;
+  Parts parts = {(uint8_t *)workspace, dtype, st};
+  const void *x_at = parts.rows_of(x, rows, c_in), *w_at = parts.rows_of(w, c_out, c_in);
+  const void *a_at = parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in);
+  const void *b_at = parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank);
+  const int in = parts.pitch(c_in), of_rank = parts.pitch(adapters->rank);
+  bool apart = false;
+  cudaError_t e = parts.e;
+  if (e == cudaSuccess) e = narrow(x_at, in, (int)rows, c_in, a_at, in, false, adapters, of, saved, dtype, workspace, st, &apart);
   if (e != cudaSuccess) return status(e);
   RowsJob j = {};
-  j.x = x;
+  j.x = x_at;
   j.rows = (int)rows;
   j.k = c_in;
   j.n = c_out;
-  j.w = w;
+  j.w = w_at;
+  j.x_pitch = j.w_pitch = in;
   j.runs = all;
   j.t = runs ? saved : nullptr;
-  j.e = adapters->b;
+  j.e = b_at;
+  j.e_pitch = of_rank;
   j.rank = adapters->rank;
   j.ext = of;
   j.bias = bias;
@@ -197,7 +249,7 @@ extern "C" dc_status dc_adapter_forward(const void *x, long long rows, int c_in,
   j.residual = residual;
   j.y = y;
   j.dtype = dtype;
-  return status(rows_any(j, (cudaStream_t)stream));
+  return status(rows_any_or_tc(j, apart, workspace, st));
 }
 
 extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int c_in, const void *w, int c_out,
@@ -211,49 +263,70 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
   if (rows == 0 && !da && !db) return DC_OK;
   const Runs of = {offsets, which, runs, (int)rows, adapters->count, 1}, all = {nullptr, nullptr, 1, (int)rows, 1, 0};
   const cudaStream_t st = (cudaStream_t)stream;
-  void *u = (uint8_t *)workspace + sizeof(DcWsHeader);
-  cudaError_t e = cudaSuccess;
-  if ((dx || da) && rows) e = narrow(dy, (int)rows, c_out, adapters, true, of, u, dtype, st);
+  Parts parts = {(uint8_t *)workspace, dtype, st};
+  void *u = parts.add(saved_bytes(rows, adapters->rank));
+  const bool with_u = (dx || da) && rows;
+  const void *dy_at = parts.rows_of(dy, rows, c_out), *x_at = da ? parts.rows_of(x, rows, c_in) : nullptr, *w_at = dx ? parts.rows_of(w, c_out, c_in) : nullptr;
+  const void *a_at = dx ? parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in) : nullptr;
+  const void *b_at = with_u ? parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank) : nullptr;
+  const int in = parts.pitch(c_in), out = parts.pitch(c_out), of_rank = parts.pitch(adapters->rank);
+  cudaError_t e = parts.e;
+  bool apart = false;
+  if (with_u && e == cudaSuccess) e = narrow(dy_at, out, (int)rows, c_out, b_at, of_rank, true, adapters, of, u, dtype, workspace, st, &apart);
   if (dx && rows && e == cudaSuccess) {
     RowsJob j = {};
-    j.x = dy;
+    j.x = dy_at;
     j.rows = (int)rows;
     j.k = c_out;
     j.n = c_in;
-    j.w = w;
+    j.w = w_at;
     j.w_across = 1;
+    j.x_pitch = out;
+    j.w_pitch = in;
     j.runs = all;
     j.t = runs ? u : nullptr;
-    j.e = adapters->a;
+    j.e = a_at;
     j.e_across = 1;
+    j.e_pitch = in;
     j.rank = adapters->rank;
     j.ext = of;
     j.y = dx;
     j.dtype = dtype;
-    e = rows_any(j, st);
+    e = rows_any_or_tc(j, apart, workspace, st);
   }
   GradJob g = {};
   g.runs = of;
   g.dtype = dtype;
-  if (da && e == cudaSuccess) {
+  if (da && e == cudaSuccess && dtype == DC_BF16) {    // as x^T u, so that the long side is the instructions' 128 rows
+    g.p = x_at;
+    g.m = c_in;
+    g.p_pitch = in;
+    g.q = u;
+    g.q_terms = 1;
+    g.n = adapters->rank;
+    g.out = da;
+    g.out_across = 1;
+    e = grad_tc(g, (DcWsHeader *)workspace, st);
+  } else if (da && e == cudaSuccess) {
     g.p = u;
     g.p_terms = 1;
     g.m = adapters->rank;
     g.q = x;
-    g.q_terms = 0;
     g.n = c_in;
     g.out = da;
     e = grad_any(g, st);
   }
   if (db && e == cudaSuccess) {
-    g.p = dy;
+    g.p = dy_at;
     g.p_terms = 0;
     g.m = c_out;
+    g.p_pitch = out;
     g.q = saved;
     g.q_terms = 1;
     g.n = adapters->rank;
     g.out = db;
-    e = grad_any(g, st);
+    g.out_across = 0;
+    e = dtype == DC_BF16 ? grad_tc(g, (DcWsHeader *)workspace, st) : grad_any(g, st);
   }
   return status(e);
 }

@@ -108,6 +108,7 @@ struct RowsJob {
   void *y;                   // [rows][n], or with y_terms what a row keeps of an adapter, n its rank
   int y_terms;
   dc_dtype dtype;
+  int x_pitch, w_pitch, e_pitch;     // elements from row to row of x, w and e, as the tensor core's kernels read them
 };
 
 // out_w(i, j) = sum over the rows r of the runs of weight w of p[r][i] q[r][j]; 0 without rows
@@ -118,10 +119,19 @@ struct GradJob {
   void *out;                 // [weights][m][n]
   float *sums;               // [weights][m]: sums of p over the rows, or NULL
   dc_dtype dtype;
+  int out_across;            // out is [weights][n][m]
+  int p_pitch, q_pitch;
 };
 
 // kernels on CUDA cores, for any sizes (group_any.cu)
 cudaError_t rows_any(const RowsJob &j, cudaStream_t st);
 cudaError_t grad_any(const GradJob &j, cudaStream_t st);
+
+// kernels on the tensor core (group_tc.cu): bf16, rows on 16 bytes (their pitches multiples of 8); of a GradJob only q may be what rows keep
+cudaError_t pitch_tc(const void *x, void *y, long long rows, int cols, int pitch, cudaStream_t st);
+bool narrow_apart(const RowsJob &j);             // y_terms: by a kernel for short runs, behind which rows_tc may start early
+cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st);
+cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaStream_t st);
+cudaError_t grad_tc(const GradJob &j, DcWsHeader *ws, cudaStream_t st);
 
 }  // namespace grp

@@ -457,7 +457,8 @@ dc_status dc_q4_plan_query(long long rows, int c_in, int c_out, dc_q4_format for
  * Runs.  Rows come sorted: run s is rows offsets[s] <= r < offsets[s + 1], offsets an array of 32-bit integers on the DEVICE, not
  * decreasing, from 0 to at most `rows`.  A run may be empty, and rows in front of the first or behind the last run belong to none.  (Offsets are cut to
  * [0, rows]; where they decrease, rows may be written twice, with no order between the two, and none outside the arrays.)
- * Rows are dense, of `dtype`: DC_BF16 multiplies on the tensor core with fp32 sums, DC_F32 in fp32 FMAs; results are rounded once.
+ * Rows are dense, of `dtype`, and multiplied on the tensor core with fp32 sums: DC_BF16 as they are, DC_F32 as products of bf16 terms as described at
+ * dc_merge_chain (results that are no numbers come out as FMAs give them, which takes long).  Results are rounded once.
  * rows: 0 to 2^30; without rows, forward calls write nothing.  Widths: 1 to 2^20.  Workspaces: device, the bytes that the query
  * says, the first 256 zeroed once by the caller; a bounded wait that runs out is latched there (dc_workspace_status).  Calls that may run at
  * once need a workspace each.
@@ -503,7 +504,7 @@ dc_status dc_adapter_workspace_bytes(long long rows, int c_in, int c_out, const 
  * x: [rows][c_in]; w: [c_out][c_in] of `dtype`, or NULL: no such product (the adapters' part of a layer whose own part is
  * in `residual`, of 4-bit weights for instance); offsets: [runs + 1], which: [runs], 32-bit integers on the device, runs 0 to 2^20;
  * bias: fp32 [c_out] or NULL; residual: as y or NULL, may be y; y: [rows][c_out], overlaps nothing else.  saved: device, dc_adapter_saved_bytes,
- * 16-byte aligned; keeps t of the rows that have an adapter (in 16 bits each, and not one bf16, where rows are bf16) for dc_adapter_backward.
+ * 16-byte aligned; keeps t of the rows that have an adapter (to 16 bits each where rows are bf16, else 24) for dc_adapter_backward.
  */
 dc_status dc_adapter_forward(const void *x, long long rows, int c_in, const void *w, int c_out, const dc_adapters *adapters,
                              const int *offsets, const int *which, int runs, const float *bias, dc_act act, const void *residual,

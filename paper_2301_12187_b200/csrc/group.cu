@@ -26,37 +26,36 @@ bool aligned(std::initializer_list<const void *> all) {
 }
 dc_status status(cudaError_t e) { return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? DC_OK : DC_ERR_CUDA; }
 
-size_t saved_bytes(long long rows, int rank) { return (size_t)rows * (size_t)rank_pad(rank) * 4; }
+size_t saved_bytes(long long rows, int rank, dc_dtype dtype) { return (size_t)rows * (size_t)rank_pad(rank) * (dtype == DC_BF16 ? 4 : 6); }
 
-// A workspace's parts, one behind the other: `base` NULL where only their bytes are wanted.  bf16 rows that do not begin on 16 bytes are copied to rows that do: the tensor core's
-// kernels read by TMA, and a copy takes a tenth of the time that reading value by value cost.
+// A workspace's parts, one behind the other: `base` NULL where only their bytes are wanted.  bf16 rows that do not begin on 16 bytes are copied to rows
+// that do, fp32 ones are cut into terms: the tensor core's kernels read by TMA.  (A copy takes a tenth of the time that reading value by value cost.)
 struct Parts {
   uint8_t *base;
   dc_dtype dtype;
-  cudaStream_t st;
   size_t bytes = sizeof(DcWsHeader);
-  cudaError_t e = cudaSuccess;
+  Copy copies[kMaxCopies];
+  int count = 0;
+  Parts(void *workspace, dc_dtype type) : base((uint8_t *)workspace), dtype(type) {}
   void *add(size_t n) {
     uint8_t *at = base ? base + bytes : nullptr;
     bytes += dc_round_up(n, 256);
     return at;
   }
-  bool apart(int cols) const { return dtype == DC_BF16 && cols % 8 != 0; }
-  int pitch(int cols) const { return apart(cols) ? (int)dc_round_up((size_t)cols, 8) : cols; }
+  bool apart(int cols) const { return dtype == DC_F32 || cols % 8 != 0; }
+  int pitch(int cols) const { return (int)dc_round_up((size_t)cols, 8); }
+  void *room(long long rows, int cols) { return add((size_t)rows * (size_t)pitch(cols) * (dtype == DC_BF16 ? 2 : 6)); }
   void reserve(long long rows, int cols) {
-    if (apart(cols)) add((size_t)rows * (size_t)pitch(cols) * 2);
+    if (apart(cols)) room(rows, cols);
   }
   const void *rows_of(const void *x, long long rows, int cols) {
     if (!x || rows == 0 || !apart(cols)) return x;
-    void *to = add((size_t)rows * (size_t)pitch(cols) * 2);
-    if (e == cudaSuccess) e = pitch_tc(x, to, rows, cols, pitch(cols), st);
+    void *to = room(rows, cols);
+    copies[count++] = {x, to, rows, cols, pitch(cols)};
     return to;
   }
+  cudaError_t copy(cudaStream_t st) { return copies_tc(copies, count, dtype, st); }
 };
-cudaError_t rows_any_or_tc(const RowsJob &j, bool behind_narrow, void *workspace, cudaStream_t st) {
-  return j.dtype == DC_BF16 ? rows_tc(j, behind_narrow, (DcWsHeader *)workspace, st) : rows_any(j, st);
-}
-
 }  // namespace
 
 extern "C" dc_status dc_group_workspace_bytes(long long rows, int groups, int c_in, int c_out, dc_dtype dtype, size_t *bytes) {
@@ -64,7 +63,7 @@ extern "C" dc_status dc_group_workspace_bytes(long long rows, int groups, int c_
   if (s != DC_OK) return s;
   if (!bytes || groups < 1) return DC_ERR_INVALID_ARG;
   if (groups > kMaxRuns) return DC_ERR_UNSUPPORTED;
-  Parts need = {nullptr, dtype, nullptr};
+  Parts need(nullptr, dtype);
   need.reserve(rows, c_in);
   need.reserve(rows, c_out);
   need.reserve((long long)groups * c_out, c_in);
@@ -83,7 +82,7 @@ extern "C" dc_status dc_group_forward(const void *x, long long rows, int c_in, c
   if (!workspace || workspace_bytes < need) return DC_ERR_WORKSPACE;
   if (!aligned({x, w, bias, y, workspace}) || (reinterpret_cast<uintptr_t>(offsets) & 3u)) return DC_ERR_ALIGNMENT;
   if (rows == 0) return DC_OK;
-  Parts parts = {(uint8_t *)workspace, dtype, (cudaStream_t)stream};
+  Parts parts(workspace, dtype);
   RowsJob j = {};
   j.x = parts.rows_of(x, rows, c_in);
   j.rows = (int)rows;
@@ -91,14 +90,17 @@ extern "C" dc_status dc_group_forward(const void *x, long long rows, int c_in, c
   j.n = c_out;
   j.w = parts.rows_of(w, (long long)groups * c_out, c_in);
   j.x_pitch = j.w_pitch = parts.pitch(c_in);
-  if (parts.e != cudaSuccess) return status(parts.e);
+  j.raw_x = x;
+  j.raw_w = w;
   j.runs = {offsets, nullptr, groups, (int)rows, groups, 0};
   j.bias = bias;
   j.bias_each = 1;
   j.act = (int)act;
   j.y = y;
   j.dtype = dtype;
-  return status(rows_any_or_tc(j, false, workspace, (cudaStream_t)stream));
+  cudaError_t e = parts.copy((cudaStream_t)stream);
+  if (e == cudaSuccess) e = rows_tc(j, false, (DcWsHeader *)workspace, (cudaStream_t)stream);
+  return status(e);
 }
 
 extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long rows, int c_in, const int *offsets, int groups,
@@ -112,10 +114,10 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
   if (!aligned({dy, x, w, dx, dw, db, workspace}) || (reinterpret_cast<uintptr_t>(offsets) & 3u)) return DC_ERR_ALIGNMENT;
   if (rows == 0 && !dw && !db) return DC_OK;
   const Runs runs = {offsets, nullptr, groups, (int)rows, groups, 0};
-  Parts parts = {(uint8_t *)workspace, dtype, (cudaStream_t)stream};
+  Parts parts(workspace, dtype);
   const void *dy_at = parts.rows_of(dy, rows, c_out), *x_at = dw ? parts.rows_of(x, rows, c_in) : nullptr;
   const void *w_at = dx ? parts.rows_of(w, (long long)groups * c_out, c_in) : nullptr;
-  cudaError_t e = parts.e;
+  cudaError_t e = parts.copy((cudaStream_t)stream);
   if (dx && rows && e == cudaSuccess) {
     RowsJob j = {};
     j.x = dy_at;
@@ -129,7 +131,9 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
     j.runs = runs;
     j.y = dx;
     j.dtype = dtype;
-    e = rows_any_or_tc(j, false, workspace, (cudaStream_t)stream);
+    j.raw_x = dy;
+    j.raw_w = w;
+    e = rows_tc(j, false, (DcWsHeader *)workspace, (cudaStream_t)stream);
   }
   if ((dw || db) && e == cudaSuccess) {
     GradJob j = {};
@@ -143,7 +147,9 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
     j.out = dw;
     j.sums = db;
     j.dtype = dtype;
-    e = dtype == DC_BF16 ? grad_tc(j, (DcWsHeader *)workspace, (cudaStream_t)stream) : grad_any(j, (cudaStream_t)stream);
+    j.raw_p = dy;
+    j.raw_q = x;
+    e = grad_tc(j, (DcWsHeader *)workspace, (cudaStream_t)stream);
   }
   return status(e);
 }
@@ -151,7 +157,7 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
 extern "C" dc_status dc_adapter_saved_bytes(long long rows, int rank, dc_dtype dtype, size_t *bytes) {
   if (rows < 0 || rank < 1 || !bytes || (dtype != DC_F32 && dtype != DC_BF16)) return DC_ERR_INVALID_ARG;
   if (rows > kMaxRows || rank > kMaxRank) return DC_ERR_UNSUPPORTED;
-  *bytes = saved_bytes(rows, rank);
+  *bytes = saved_bytes(rows, rank, dtype);
   return DC_OK;
 }
 
@@ -161,8 +167,8 @@ extern "C" dc_status dc_adapter_workspace_bytes(long long rows, int c_in, int c_
   if (s == DC_OK) s = check_adapters(adapters);
   if (s != DC_OK) return s;
   if (!bytes) return DC_ERR_INVALID_ARG;
-  Parts need = {nullptr, dtype, nullptr};
-  need.add(saved_bytes(rows, adapters->rank));   // u
+  Parts need(nullptr, dtype);
+  need.add(saved_bytes(rows, adapters->rank, dtype));   // u
   need.reserve(rows, c_in);
   need.reserve(rows, c_out);
   need.reserve(c_out, c_in);
@@ -187,9 +193,11 @@ dc_status check_adapter_call(long long rows, int c_in, int c_out, const void *w,
     return DC_ERR_ALIGNMENT;
   return DC_OK;
 }
-// Rows through the adapters' first matrices -- a, or in the backward pass b read across -- scaled, to `out`.  *apart: by the kernel behind which the next launch may start early.
-cudaError_t narrow(const void *x, int x_pitch, int rows, int k, const void *m, int m_pitch, bool backward, const dc_adapters *ad, const Runs &runs, void *out,
-                   dc_dtype dtype, void *workspace, cudaStream_t st, bool *apart) {
+// Rows through the adapters' first matrices -- a, or in the backward pass b read across -- scaled, to `out`.  *apart: by the kernel behind which
+// the next launch may start early.
+cudaError_t narrow(const void *raw_x, const void *x, int x_pitch, int rows, int k, const void *m, int m_pitch, bool backward, const dc_adapters *ad, const Runs &runs,
+                   void *out, dc_dtype dtype, void *workspace, cudaStream_t st, bool *apart) {
+  if (runs.count == 0) return cudaSuccess;
   RowsJob j = {};
   j.x = x;
   j.rows = rows;
@@ -199,14 +207,15 @@ cudaError_t narrow(const void *x, int x_pitch, int rows, int k, const void *m, i
   j.w_across = backward;
   j.x_pitch = x_pitch;
   j.w_pitch = m_pitch;
+  j.raw_x = raw_x;
+  j.raw_w = backward ? ad->b : ad->a;
   j.runs = runs;
   j.alpha = ad->scale;
   j.y = out;
   j.y_terms = 1;
   j.dtype = dtype;
-  *apart = dtype == DC_BF16 && runs.count && narrow_apart(j);
-  if (runs.count == 0) return cudaSuccess;
-  return *apart ? narrow_tc(j, st) : rows_any_or_tc(j, false, workspace, st);
+  *apart = narrow_apart(j);
+  return *apart ? narrow_tc(j, st) : rows_tc(j, false, (DcWsHeader *)workspace, st);
 }
 }  // namespace
 
@@ -222,14 +231,14 @@ extern "C" dc_status dc_adapter_forward(const void *x, long long rows, int c_in,
   if (rows == 0) return DC_OK;
   const Runs of = {offsets, which, runs, (int)rows, adapters->count, 1}, all = {nullptr, nullptr, 1, (int)rows, 1, 0};
   const cudaStream_t st = (cudaStream_t)stream;
-  Parts parts = {(uint8_t *)workspace, dtype, st};
+  Parts parts(workspace, dtype);
   const void *x_at = parts.rows_of(x, rows, c_in), *w_at = parts.rows_of(w, c_out, c_in);
   const void *a_at = parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in);
   const void *b_at = parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank);
   const int in = parts.pitch(c_in), of_rank = parts.pitch(adapters->rank);
   bool apart = false;
-  cudaError_t e = parts.e;
-  if (e == cudaSuccess) e = narrow(x_at, in, (int)rows, c_in, a_at, in, false, adapters, of, saved, dtype, workspace, st, &apart);
+  cudaError_t e = parts.copy((cudaStream_t)stream);
+  if (e == cudaSuccess) e = narrow(x, x_at, in, (int)rows, c_in, a_at, in, false, adapters, of, saved, dtype, workspace, st, &apart);
   if (e != cudaSuccess) return status(e);
   RowsJob j = {};
   j.x = x_at;
@@ -242,6 +251,9 @@ extern "C" dc_status dc_adapter_forward(const void *x, long long rows, int c_in,
   j.t = runs ? saved : nullptr;
   j.e = b_at;
   j.e_pitch = of_rank;
+  j.raw_x = x;
+  j.raw_w = w;
+  j.raw_e = adapters->b;
   j.rank = adapters->rank;
   j.ext = of;
   j.bias = bias;
@@ -249,7 +261,7 @@ extern "C" dc_status dc_adapter_forward(const void *x, long long rows, int c_in,
   j.residual = residual;
   j.y = y;
   j.dtype = dtype;
-  return status(rows_any_or_tc(j, apart, workspace, st));
+  return status(rows_tc(j, apart, (DcWsHeader *)workspace, st));
 }
 
 extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int c_in, const void *w, int c_out,
@@ -263,16 +275,16 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
   if (rows == 0 && !da && !db) return DC_OK;
   const Runs of = {offsets, which, runs, (int)rows, adapters->count, 1}, all = {nullptr, nullptr, 1, (int)rows, 1, 0};
   const cudaStream_t st = (cudaStream_t)stream;
-  Parts parts = {(uint8_t *)workspace, dtype, st};
-  void *u = parts.add(saved_bytes(rows, adapters->rank));
+  Parts parts(workspace, dtype);
+  void *u = parts.add(saved_bytes(rows, adapters->rank, dtype));
   const bool with_u = (dx || da) && rows;
   const void *dy_at = parts.rows_of(dy, rows, c_out), *x_at = da ? parts.rows_of(x, rows, c_in) : nullptr, *w_at = dx ? parts.rows_of(w, c_out, c_in) : nullptr;
   const void *a_at = dx ? parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in) : nullptr;
   const void *b_at = with_u ? parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank) : nullptr;
   const int in = parts.pitch(c_in), out = parts.pitch(c_out), of_rank = parts.pitch(adapters->rank);
-  cudaError_t e = parts.e;
+  cudaError_t e = parts.copy((cudaStream_t)stream);
   bool apart = false;
-  if (with_u && e == cudaSuccess) e = narrow(dy_at, out, (int)rows, c_out, b_at, of_rank, true, adapters, of, u, dtype, workspace, st, &apart);
+  if (with_u && e == cudaSuccess) e = narrow(dy, dy_at, out, (int)rows, c_out, b_at, of_rank, true, adapters, of, u, dtype, workspace, st, &apart);
   if (dx && rows && e == cudaSuccess) {
     RowsJob j = {};
     j.x = dy_at;
@@ -288,45 +300,39 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
     j.e = a_at;
     j.e_across = 1;
     j.e_pitch = in;
+    j.raw_x = dy;
+    j.raw_w = w;
+    j.raw_e = adapters->a;
     j.rank = adapters->rank;
     j.ext = of;
     j.y = dx;
     j.dtype = dtype;
-    e = rows_any_or_tc(j, apart, workspace, st);
+    e = rows_tc(j, apart, (DcWsHeader *)workspace, st);
   }
   GradJob g = {};
   g.runs = of;
   g.dtype = dtype;
-  if (da && e == cudaSuccess && dtype == DC_BF16) {    // as x^T u, so that the long side is the instructions' 128 rows
+  g.q_terms = 1;
+  g.n = adapters->rank;
+  if (da && e == cudaSuccess) {                  // as x^T u, so that the long side is the instructions' 128 rows
     g.p = x_at;
+    g.raw_p = x;
     g.m = c_in;
     g.p_pitch = in;
     g.q = u;
-    g.q_terms = 1;
-    g.n = adapters->rank;
     g.out = da;
     g.out_across = 1;
     e = grad_tc(g, (DcWsHeader *)workspace, st);
-  } else if (da && e == cudaSuccess) {
-    g.p = u;
-    g.p_terms = 1;
-    g.m = adapters->rank;
-    g.q = x;
-    g.n = c_in;
-    g.out = da;
-    e = grad_any(g, st);
   }
   if (db && e == cudaSuccess) {
     g.p = dy_at;
-    g.p_terms = 0;
+    g.raw_p = dy;
     g.m = c_out;
     g.p_pitch = out;
     g.q = saved;
-    g.q_terms = 1;
-    g.n = adapters->rank;
     g.out = db;
     g.out_across = 0;
-    e = dtype == DC_BF16 ? grad_tc(g, (DcWsHeader *)workspace, st) : grad_any(g, st);
+    e = grad_tc(g, (DcWsHeader *)workspace, st);
   }
   return status(e);
 }

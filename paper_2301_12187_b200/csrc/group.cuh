@@ -84,51 +84,57 @@ __device__ __forceinline__ int first_run_behind(const Runs &r, int row) {
   return lo;
 }
 
-// What a row keeps of an adapter: `rank` numbers, padded with zeros to a multiple of 16.  fp32 rows: fp32.  bf16 rows: two bf16 terms, all the
-// high ones and then all the low ones, 16 bits together: with one bf16 alone the adapter's part of a result would be as far off as the
-// result's own rounding (2^-9), and so would its gradients.
+// What a row keeps of an adapter: `rank` numbers, padded with zeros to a multiple of 16, as terms of bf16 that add up to them: all high ones, then all
+// low ones.  bf16 rows: two, 16 bits together (with one bf16 the adapter's part of a result would be as far off as the result's own rounding, 2^-9,
+// and so would its gradients); fp32 rows: three.
 __host__ __device__ static inline int rank_pad(int rank) { return (rank + 15) / 16 * 16; }
 
 // y[r][o] = act(alpha_w * sum_k x[r][k] W_w(o, k) + sum_j t[r][j] E_e(o, j) + bias_w[o] + residual[r][o]) for the rows r of runs with a
 // weight w; e is the weight of the run of `ext` that r is in.
 struct RowsJob {
-  const void *x;
+  const void *x;             // x, w and e as the kernels read them (Copy), their pitches below
   int rows, k, n;
   const void *w;             // [weights][n][k], or with w_across [weights][k][n]; NULL: no such sum
   int w_across;
   Runs runs;
   const float *alpha;        // one for each weight, or NULL
-  const void *t;             // [rows][rank_pad] as above, or NULL
+  const void *t;             // what rows keep, or NULL
   const void *e;             // [weights][n][rank], or with e_across [weights][rank][n]
   int rank, e_across;
   Runs ext;
   const float *bias;         // [n], or with bias_each [weights][n]
   int bias_each, act;
   const void *residual;
-  void *y;                   // [rows][n], or with y_terms what a row keeps of an adapter, n its rank
+  void *y;                   // [rows][n], or with y_terms what rows keep of an adapter, n its rank
   int y_terms;
   dc_dtype dtype;
-  int x_pitch, w_pitch, e_pitch;     // elements from row to row of x, w and e, as the tensor core's kernels read them
+  int x_pitch, w_pitch, e_pitch;
+  const void *raw_x, *raw_w, *raw_e;             // as the caller has them
 };
 
 // out_w(i, j) = sum over the rows r of the runs of weight w of p[r][i] q[r][j]; 0 without rows
 struct GradJob {
-  const void *p, *q;         // [rows][m], [rows][n]; or with p_terms, q_terms what a row keeps of an adapter, m or n its rank
-  int m, n, p_terms, q_terms;
+  const void *p, *q;         // [rows][m], [rows][n], as the kernels read them; with q_terms q is what rows keep of an adapter, n its rank
+  int m, n, q_terms;
   Runs runs;
-  void *out;                 // [weights][m][n]
+  void *out;                 // [weights][m][n], or with out_across [weights][n][m]; NULL: sums alone
   float *sums;               // [weights][m]: sums of p over the rows, or NULL
   dc_dtype dtype;
-  int out_across;            // out is [weights][n][m]
+  int out_across;
   int p_pitch, q_pitch;
+  const void *raw_p, *raw_q;
 };
 
-// kernels on CUDA cores, for any sizes (group_any.cu)
-cudaError_t rows_any(const RowsJob &j, cudaStream_t st);
-cudaError_t grad_any(const GradJob &j, cudaStream_t st);
+// An array's rows for the tensor core's loads: bf16 ones beginning on 16 bytes (pitch: a multiple of 8 elements), fp32 ones as three rows of bf16 terms.
+struct Copy {
+  const void *from;
+  void *to;
+  long long rows;
+  int cols, pitch;
+};
+constexpr int kMaxCopies = 5;
 
-// kernels on the tensor core (group_tc.cu): bf16, rows on 16 bytes (their pitches multiples of 8); of a GradJob only q may be what rows keep
-cudaError_t pitch_tc(const void *x, void *y, long long rows, int cols, int pitch, cudaStream_t st);
+cudaError_t copies_tc(const Copy *c, int count, dc_dtype dtype, cudaStream_t st);
 bool narrow_apart(const RowsJob &j);             // y_terms: by a kernel for short runs, behind which rows_tc may start early
 cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st);
 cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaStream_t st);

@@ -1,4 +1,4 @@
-// Grouped products, adapters and their gradients on the tensor core, for bf16 rows that begin on 16 bytes (group.cu sees to that).
+// Grouped products, adapters and their gradients on the tensor core.
 //
 // tcgen05.mma multiplies 128 x N x 16 at a time; operands come by TMA in pieces of 64 along the sum (128-byte rows, swizzled), through a ring of
 // stages.  One warp loads, one thread issues, eight warps read out the accumulators, of which there are two: a tile's results go out while
@@ -7,11 +7,18 @@
 // neighbouring columns of 64 rows, and the instruction takes them the other way round.
 //   kTile   128 rows of a run x up to 256 columns of its matrix.
 //   kFew    runs of few rows: 128 columns of the matrix take the place of the 128 rows, so that an instruction is as wide as there are rows and
-//           the matrix streams through once.  Few tiles: a cluster shares a tile's sum.
+//           the matrix streams through once.
 //   kGrad   128 x up to 256 of a gradient: the sum runs over the rows of a weight's runs.  The last piece of a run holds rows of the next one, which a warp
 //           sets to zero in both operands (0 times a NaN is a NaN).
+// kTile and kGrad in pairs (cta_group::2): two CTAs multiply 256 x 256, each loads half of either operand.
+// Few tiles: a cluster shares a tile's sum, and adds up its parts through its shared memory.
 // Adapters (kTile): each run's part is added to the same accumulator by instructions that leave the lanes of other rows alone, so that an
 // infinity in one request's adapter stays in its own rows.  (kFew: by the warps that read out, while the matrix streams.)
+//
+// fp32: a value is three bf16 terms that add up to it (split_tc), laid out one behind the other, and a stage holds all three of both operands: six of
+// their nine products are above 2^-24 of the result, small ones first.  The tensor core cuts its sums instead of rounding them, so a piece's
+// sum is read out and added up in fp32 registers.  A result that is a NaN is worked out again by FMAs: an infinity, or a value
+// beyond the largest bf16, has a NaN among its terms.
 #include <string.h>
 
 #include "group.cuh"
@@ -27,23 +34,26 @@ constexpr int kEpi = 8;                          // warps reading out
 template <int FORM>
 constexpr int kThreadsOf = (2 + kEpi + (FORM == kGrad ? 1 : 0)) * 32;
 constexpr int kMaxStages = 8, kMaxSplit = 8;
-constexpr int kSmem = 220 * 1024;
+constexpr int kSmem = 226 * 1024;                // what the static arrays leave
 constexpr int kPiece = 64;                       // of the sum, 128 bytes of bf16
 constexpr int kP = 128 * 128;                    // bytes of the 128-row operand in a stage
 constexpr int kBox = 64 * 128;                   // 64 columns of 64 rows
+constexpr int kOut = kEpi * 32 * 128;            // staged results: 32 rows x 32 sums a warp
 constexpr int kSuper = 16;                       // rows of tiles that are walked together: 16 x 9 tiles at once read a twelfth of what a row or column of them would
-constexpr unsigned long long kLongNs = 20ull * 1000ull * 1000ull * 1000ull;      // a gradient's tile may take seconds: a sum over 2^30 rows
 constexpr int kFewMost = 64;                     // rows of a tile of kFew
+constexpr unsigned long long kLongNs = 20ull * 1000ull * 1000ull * 1000ull;      // a gradient's tile may take seconds (a sum over 2^30 rows), and so may NaN by FMAs
 
 typedef __nv_bfloat16 bf16;
+template <typename T>
+constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;
 
 struct Params {
   int rows, k, n;            // kGrad: m in the place of k
   Runs runs, ext;
   const float *alpha, *bias;
   int bias_each, act;
-  const bf16 *residual;
-  bf16 *y;
+  const void *residual;
+  void *y;
   int y_terms, vec;          // vec: rows of y begin on 16 bytes
   int nt, acc;               // columns of an instruction; of an accumulator
   int tiles_m, tiles_n;      // kGrad: both of a weight; else tiles_n
@@ -52,14 +62,15 @@ struct Params {
   int stages, q_bytes, tmem_cols;
   int maps;                  // bits of the tensor maps that there are
   int rank, rank_pieces;     // adapters: pieces of 64 of the rank
-  const bf16 *t, *e;         // kFew: what the reading-out warps take of them
-  int e_pitch;
+  const bf16 *t;             // what rows keep
+  const void *e;             // kFew: what the reading-out warps take of the adapters
+  int e_pitch, e_vec;
   int early;                 // kFew: what is loaded by TMA was there before the launch in front of this one began
-  int off_t;                 // kFew: t's numbers in shared memory
+  int off_out, off_t;        // staged results; kFew: t's numbers in shared memory
   // kGrad
   float *sums;
-  int p_terms, q_terms;
-  int out_across;            // out is [n][m]
+  int q_terms, out_across;   // out_across: out is [n][m]
+  const void *raw_p, *raw_q; // fp32: the operands themselves
 };
 
 __device__ __forceinline__ uint64_t desc_along(uint32_t a) {     // rows of 64 along the sum, 1024 bytes between groups of 8 rows
@@ -72,26 +83,74 @@ template <bool ACROSS>
 __device__ __forceinline__ uint64_t desc_of(uint32_t a) { return ACROSS ? desc_across(a) : desc_along(a); }
 template <bool ACROSS>
 constexpr uint32_t kStepOf = ACROSS ? 16 * 128 / 16 : 32 / 16;   // 16 terms further on, in units of 16 bytes
-// D += A B with the lanes of `off` left as they are
-__device__ __forceinline__ void umma_lanes(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, const uint32_t (&off)[4]) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8}, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3])
-      : "memory");
+
+template <bool P>
+__device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if (P)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    umma_bf16(d, a, b, idesc, accumulate);
 }
+// D += A B with the lanes of `off` left as they are
+template <bool P>
+__device__ __forceinline__ void umma_lanes(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, const uint32_t (&off)[8]) {
+  if (P)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8, %9, %10, %11, %12}, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3]), "r"(off[4]), "r"(off[5]), "r"(off[6]), "r"(off[7])
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8}, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3])
+        : "memory");
+}
+// arrives at the barrier (of both CTAs of a pair) once all that this thread has issued is done
+template <bool P>
+__device__ __forceinline__ void commit(uint64_t *bar) {
+  if (P)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3)
+                 : "memory");
+  else
+    umma_commit(bar);
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// a phase that has been seen to end: what the cluster's threads wrote before they arrived is visible behind this
+__device__ __forceinline__ void mbar_acquire_cluster(uint64_t *bar, uint32_t parity) {
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(smem_u32(bar)), "r"(parity) : "memory");
+}
+// columns from c0 on of term `term`, rows from `row` on, of matrix `outer`; a pair's loads report to its first CTA (cluster address `bar`)
+template <bool P>
+__device__ __forceinline__ void load_box(uint32_t to, const CUtensorMap *map, uint32_t bar, int c0, int term, int row, int outer) {
+  if (P)
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(to), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(term), "r"(row), "r"(outer) : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(to), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(term), "r"(row), "r"(outer) : "memory");
+}
+__device__ __forceinline__ void sts_f(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
 
 // The tile of an item: tiles of a run are walked column by column in bands of kSuper rows of tiles.
 struct Tile {
   int row0, end, weight, tn;
 };
-template <int FORM>
-__device__ __forceinline__ bool find_tile(const Params &p, grp::Walk &walk, long long item, Tile *t) {
+__device__ __forceinline__ bool find_tile(const Params &p, int tile, grp::Walk &walk, long long item, Tile *t) {
   Run run;
   int index;
   long long inside;
-  const int tile = FORM == kFew ? p.nt : 128;
   if (!walk.find(p.runs, tile, p.tiles_n, item, &run, &index, &inside)) return false;
   const int tiles_m = (run.end - run.begin + tile - 1) / tile;
   const int band = (int)(inside / ((long long)kSuper * p.tiles_n)), rem = (int)(inside - (long long)band * kSuper * p.tiles_n);
@@ -133,20 +192,38 @@ __device__ __forceinline__ void each_run(const Runs &r, int row0, int end, F f) 
     if (__any_sync(0xffffffffu, stop)) return;
   }
 }
+// the adapter of a row, -1: none.  One thread.
+__device__ __forceinline__ int adapter_of(const Runs &r, int row) {
+  for (int s = grp::first_run_behind(r, row); s < r.count; ++s) {        // empty runs in between
+    const Run run = grp::run_at(r, s);
+    if (run.begin > row) break;
+    if (run.end > row) return run.weight;
+  }
+  return -1;
+}
 
-// Calls f(first row, rows, last) for the pieces of 64 rows of a weight's runs.
+// Calls f(first row, rows) for this CTA's pieces of 64 rows of a weight's runs: pieces go round the CTAs of a cluster that share a sum.
 template <typename F>
-__device__ __forceinline__ void each_piece(const Params &p, int weight, int rank, F f) {
+__device__ __forceinline__ void each_piece(const Params &p, int weight, int share, F f) {
   const int first = p.runs.mapped ? 0 : weight, last = p.runs.mapped ? p.runs.count : weight + 1;
-  int turn = 0;                                  // pieces go round the CTAs of a cluster
+  int turn = 0;
   for (int s = first; s < last; ++s) {
     const Run run = grp::run_at(p.runs, s);
     if (run.weight != weight) continue;
     for (int r = run.begin; r < run.end; r += kPiece) {
-      if (turn == rank && !f(r, min(kPiece, run.end - r))) return;
+      if (turn == share && !f(r, min(kPiece, run.end - r))) return;
       if (++turn == p.split) turn = 0;
     }
   }
+}
+__device__ __forceinline__ int count_pieces(const Params &p, int weight, int share) {
+  const int first = p.runs.mapped ? 0 : weight, last = p.runs.mapped ? p.runs.count : weight + 1;
+  int all = 0;
+  for (int s = first; s < last; ++s) {
+    const Run run = grp::run_at(p.runs, s);
+    if (run.weight == weight) all += (run.end - run.begin + kPiece - 1) / kPiece;
+  }
+  return all <= share ? 0 : (all - share - 1) / p.split + 1;
 }
 
 __device__ __forceinline__ void unpack8(uint4 w, float *v) {
@@ -157,27 +234,146 @@ __device__ __forceinline__ void unpack8(uint4 w, float *v) {
 __device__ __forceinline__ uint4 pack8(const float *v) {
   return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
-// what is left of a value behind its bf16; of an infinity or a NaN nothing
-__device__ __forceinline__ float left_of(float v) {
-  const float low = v - __bfloat162float(__float2bfloat16(v));
-  return low == low ? low : 0.f;
+// What a row keeps, as terms of bf16 that add up: two (16 bits together), or of fp32 rows three.  Of an infinity or a NaN the first is itself, the others 0.
+template <typename T>
+__device__ __forceinline__ void terms_of(float v, float (&t)[3]) {
+  t[0] = __bfloat162float(__float2bfloat16(v));
+  float left = v - t[0];
+  left = left - left == 0.f ? left : 0.f;
+  t[1] = __bfloat162float(__float2bfloat16(left));
+  t[2] = left - t[1];
+}
+template <typename T>
+__device__ __forceinline__ float kept(const bf16 *t, int row, int pad, int j) {
+  constexpr int N = sizeof(T) == 4 ? 3 : 2;
+  const bf16 *at = t + (size_t)row * (size_t)(N * pad) + (size_t)j;
+  float v = __bfloat162float(at[0]), low = __bfloat162float(at[pad]);
+  if (N == 3) low += __bfloat162float(at[2 * pad]);
+  return v + low;
+}
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(bf16 v) { return __bfloat162float(v); }
+
+__device__ __forceinline__ bool any_nan(const float (&v)[32]) {
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) nan |= !(v[i] == v[i]);
+  return nan;
+}
+// A result that came out as a NaN, by FMAs.  It stays one as soon as it is one.
+template <bool ACROSS>
+static __device__ __noinline__ float again(const Params &p, int row, int weight, int o) {
+  float s = 0.f;
+  if (p.pieces) {
+    const float *x = reinterpret_cast<const float *>(p.raw_p) + (size_t)row * (size_t)p.k;
+    const float *w = reinterpret_cast<const float *>(p.raw_q) + (size_t)weight * (size_t)p.n * (size_t)p.k + (ACROSS ? (size_t)o : (size_t)o * (size_t)p.k);
+    for (int i = 0; i < p.k && s == s; ++i) s = fmaf(x[i], w[(size_t)i * (size_t)(ACROSS ? p.n : 1)], s);
+    if (p.alpha) s *= __ldg(p.alpha + weight);
+  }
+  if (p.rank) {
+    const int a = adapter_of(p.ext, row);
+    if (a >= 0) {
+      const float *e = reinterpret_cast<const float *>(p.e) + (size_t)a * (size_t)p.n * (size_t)p.rank + (ACROSS ? (size_t)o : (size_t)o * (size_t)p.rank);
+      for (int j = 0; j < p.rank && s == s; ++j) s = fmaf(kept<float>(p.t, row, grp::rank_pad(p.rank), j), e[(size_t)j * (size_t)(ACROSS ? p.n : 1)], s);
+    }
+  }
+  return s;
+}
+static __device__ __noinline__ float again_grad(const Params &p, int weight, int i, int j, bool sums) {
+  float s = 0.f;
+  const int first = p.runs.mapped ? 0 : weight, last = p.runs.mapped ? p.runs.count : weight + 1;
+  for (int r = first; r < last; ++r) {
+    const Run run = grp::run_at(p.runs, r);
+    if (run.weight != weight) continue;
+    for (int row = run.begin; row < run.end && s == s; ++row) {
+      const float a = reinterpret_cast<const float *>(p.raw_p)[(size_t)row * (size_t)p.k + (size_t)i];
+      s = sums ? s + a : fmaf(a, p.q_terms ? kept<float>(p.t, row, grp::rank_pad(p.n), j) : reinterpret_cast<const float *>(p.raw_q)[(size_t)row * (size_t)p.n + (size_t)j], s);
+    }
+  }
+  return s;
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kOnes = kDEmpty + 2, kAsk, kFixed, kBars };
+// 32 sums of each lane's row -> rows of y, `rows` x `cols` of them, through shared memory: a row's results then go out side by side
+template <typename T>
+__device__ __forceinline__ void store_block(const Params &p, uint32_t stage, const float (&v)[32], T *y, size_t pitch, int rows, int cols, const float *bias, const T *residual) {
+  const int lane = (int)(threadIdx.x & 31u);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    sts_u4(stage + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) * 16)),
+           make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+  __syncwarp();
+  if (p.vec) {
+    const int piece = lane & 7, r0 = lane >> 3;
+    if (piece * 4 >= cols) return;
+    const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias) + piece) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float r[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = i * 4 + r0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) r[i][x] = 0.f;
+      if (residual && row < rows) {
+        const T *at = residual + (size_t)row * pitch + (size_t)(piece * 4);
+        if (sizeof(T) == 4) {
+          const float4 f = *reinterpret_cast<const float4 *>(at);
+          r[i][0] = f.x; r[i][1] = f.y; r[i][2] = f.z; r[i][3] = f.w;
+        } else {
+          const uint2 u = *reinterpret_cast<const uint2 *>(at);
+          r[i][0] = __uint_as_float(u.x << 16); r[i][1] = __uint_as_float(u.x & 0xffff0000u);
+          r[i][2] = __uint_as_float(u.y << 16); r[i][3] = __uint_as_float(u.y & 0xffff0000u);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = i * 4 + r0;
+      if (row >= rows) break;
+      const uint4 w = lds_u4(stage + (uint32_t)(row * 128 + ((piece ^ (row & 7)) * 16)));
+      float f[4] = {__uint_as_float(w.x) + b.x, __uint_as_float(w.y) + b.y, __uint_as_float(w.z) + b.z, __uint_as_float(w.w) + b.w};
+#pragma unroll
+      for (int x = 0; x < 4; ++x) f[x] = dc_act_apply(f[x] + r[i][x], p.act);
+      T *at = y + (size_t)row * pitch + (size_t)(piece * 4);
+      if (sizeof(T) == 4) *reinterpret_cast<float4 *>(at) = make_float4(f[0], f[1], f[2], f[3]);
+      else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+    }
+    return;
+  }
+  if (lane >= cols) return;
+  const float b = bias ? __ldg(bias + lane) : 0.f;
+#pragma unroll 8
+  for (int row = 0; row < 32; ++row) {
+    if (row >= rows) break;
+    float f = lds_f(stage + (uint32_t)(row * 128 + (((lane >> 2) ^ (row & 7)) * 16) + (lane & 3) * 4)) + b;
+    const size_t at = (size_t)row * pitch + (size_t)lane;
+    if (residual) f += to_float(residual[at]);
+    y[at] = (T)dc_act_apply(f, p.act);
+  }
+}
 
-template <int FORM, bool ACROSS>
+enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kAsk = kDEmpty + 2, kFixed, kBars };
+
+// P: in pairs.  ACROSS: the matrices' sums run across their rows (of both operands of a gradient always).
+template <int FORM, bool ACROSS, typename T, bool P>
 __global__ void __launch_bounds__(kThreadsOf<FORM>, 1)
 k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_t,
            const __grid_constant__ CUtensorMap map_e, const __grid_constant__ Params p, DcWsHeader *ws) {
+  constexpr int N = kTerms<T>;
+  constexpr bool kShort = N == 3;                // sums of a piece
+  constexpr unsigned long long kLimit = FORM == kGrad || kShort ? kLongNs : kWaitLimitNs;
+  // products of terms, small ones first
+  constexpr int kPairs = N == 3 ? 6 : 1;
+  constexpr int kTermP[6] = {N == 3 ? 2 : 0, 0, 1, 1, 0, 0}, kTermQ[6] = {0, 2, 1, 0, 1, 0};
+  constexpr int kRows = P ? 256 : 128;           // of a tile
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kBars];
   __shared__ uint32_t tmem_s, abort_s;
-  __shared__ int weight_s[kFewMost], ask_s[3];
+  __shared__ int weight_s[kFewMost];
   volatile uint32_t *abort_flag = &abort_s;
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sm = (smem_u32(smem_raw) + 1023u) & ~1023u;
   if (warp == 0) {
-    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? kEpi : 1);
+    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? (P ? 2 : 1) * kEpi : i == kFixed && P ? 2 : 1);
     if (lane == 0) abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   } else if (warp == 1 && lane < 4) {
@@ -188,43 +384,64 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   if (FORM == kFew && p.early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   else dc_pdl_enter();
   if (warp == 1) {
-    tmem_alloc(&tmem_s, (uint32_t)p.tmem_cols);
-    tmem_relinquish();
+    if (P) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"((uint32_t)p.tmem_cols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      tmem_alloc(&tmem_s, (uint32_t)p.tmem_cols);
+      tmem_relinquish();
+    }
+  }
+  const uint32_t stage_bytes = (uint32_t)(N * (kP + p.q_bytes)), ones = sm + (uint32_t)p.stages * stage_bytes;
+  if (FORM == kGrad && p.sums) {                 // a block of ones: sums are products with it
+    for (int i = tid; i < kBox / 16; i += kThreadsOf<FORM>) sts_u4(ones + (uint32_t)(i * 16), make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
+    fence_proxy_async();
   }
   tc_fence_before();
   __syncthreads();
+  if (P) cluster_sync();                         // the barriers of both CTAs are there
   tc_fence_after();
   const uint32_t tmem = tmem_s;
-  const int rank = p.split > 1 ? (int)blockIdx.x % p.split : 0;
-  const int team = (int)blockIdx.x / p.split, teams = (int)gridDim.x / p.split;
-  const uint32_t stage_bytes = (uint32_t)(kP + p.q_bytes);
-  const int c0 = rank * p.pieces_per, c1 = min(p.pieces, c0 + p.pieces_per);
+  const int group = P ? 2 : p.split;             // CTAs to an item
+  const int rank = group > 1 ? (int)blockIdx.x % group : 0;
+  const int share = P ? 0 : rank, half = P ? rank : 0;             // of a split sum; of a pair's tile
+  const int team = (int)blockIdx.x / group, teams = (int)gridDim.x / group;
+  const int c0 = share * p.pieces_per, c1 = min(p.pieces, c0 + p.pieces_per), own_pieces = max(c1 - c0, 0);
   const int per_weight = p.tiles_m * p.tiles_n;  // kGrad; with sums a column of tiles more
-  const uint32_t ones = sm + (uint32_t)p.stages * stage_bytes;
-  int met = 0;                                   // meetings of the cluster that this thread was at: two, whatever happens
+  const int tile_rows = FORM == kFew ? p.nt : kRows;
+  int met = 0;                                   // meetings of a cluster that shares a sum: two, whatever happens
+  int stage = 0;
+  uint32_t parity = 0, turn = 0;                 // of the ring; of the accumulators
+  bool ok = true;
+  auto next = [&]() { if (++stage == p.stages) { stage = 0; parity ^= 1u; } };
+  // ring uses of an adapter's part: both terms of up to 32 numbers at once, else 64 numbers of one term at a time; fp32 all terms of 64
+  const int ext_uses = N == 3 ? p.rank_pieces : p.rank <= 32 ? 1 : 2 * p.rank_pieces;
 
   if (warp == 0) {
     // ---------------------------------------------------------------- load
     const bool lead = elect_one();
-    int stage = 0;
-    uint32_t parity = 0;
-    bool ok = true;
-    auto next = [&]() { if (++stage == p.stages) { stage = 0; parity ^= 1u; } };
+    // waits for the next stage: its barrier's address for loads, or 0
+    auto open = [&](uint32_t bytes, uint32_t site) -> uint32_t {
+      ok = mbar_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, site | (uint32_t)stage, kLimit);
+      if (!ok) return 0u;
+      if (!P || rank == 0) mbar_arrive_expect_tx(&bar[kFull + stage], (P ? 2u : 1u) * bytes);
+      return P ? map_cluster(smem_u32(&bar[kFull + stage]), 0) : smem_u32(&bar[kFull + stage]);
+    };
     if (FORM == kGrad) {
       for (long long item = team; ok && item < p.most; item += teams) {
         const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n, tn = at - tm * p.tiles_n;
         const bool sums = p.sums && tn == p.tiles_n - 1;
+        const int i0 = tm * kRows + half * 128, j0 = tn * p.nt + half * (p.nt / 2);
         if (lead)
-          each_piece(p, weight, rank, [&](int r, int) {
-            ok = mbar_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x10000u | (uint32_t)stage);
-            if (!ok) return false;
-            uint64_t *full = &bar[kFull + stage];
-            const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-            mbar_arrive_expect_tx(full, sums ? (uint32_t)kP : stage_bytes);
-            tma_load_2d(a, &map_p, full, tm * 128, r);
-            tma_load_2d(a + kBox, &map_p, full, tm * 128 + 64, r);
+          each_piece(p, weight, share, [&](int r, int) {
+            const uint32_t full = open(sums ? (uint32_t)(N * kP) : stage_bytes, 0x10000u);
+            if (!full) return false;
+            uint32_t a = sm + (uint32_t)stage * stage_bytes;
+            for (int t = 0; t < N; ++t)
+              for (int b = 0; b < 2; ++b, a += kBox) load_box<P>(a, &map_p, full, i0 + b * 64, t, r, 0);
             if (!sums)
-              for (int b = 0; b < p.q_bytes / kBox; ++b) tma_load_2d(a + kP + (uint32_t)(b * kBox), &map_q, full, tn * p.nt + b * 64, r);
+              for (int t = 0; t < N; ++t)
+                for (int b = 0; b < p.q_bytes / kBox; ++b, a += kBox) load_box<P>(a, &map_q, full, j0 + b * 64, t, r, 0);
             next();
             return true;
           });
@@ -234,42 +451,42 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       grp::Walk walk;
       walk.start();
       Tile t;
-      for (long long item = team; ok && item < p.most && find_tile<FORM>(p, walk, item, &t); item += teams) {
-        if (lead) {
-          for (int c = c0; c < c1; ++c, next()) {
-            ok = mbar_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x10000u | (uint32_t)stage);
-            if (!ok) break;
-            uint64_t *full = &bar[kFull + stage];
-            const uint32_t a = sm + (uint32_t)stage * stage_bytes, rows_at = FORM == kFew ? a + kP : a, w_at = FORM == kFew ? a : a + kP;
-            mbar_arrive_expect_tx(full, stage_bytes);
-            tma_load_2d(rows_at, &map_p, full, c * kPiece, t.row0);
-            const int n0 = t.tn * (FORM == kFew ? 128 : p.nt);
-            if (ACROSS) {
-              for (int b = 0; b < (FORM == kFew ? 2 : p.q_bytes / kBox); ++b)
-                tma_load_3d(w_at + (uint32_t)(b * kBox), &map_q, full, n0 + b * 64, c * kPiece, t.weight);
+      for (long long item = team; ok && item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
+        const int n0 = t.tn * (FORM == kFew ? 128 : p.nt) + half * (p.nt / 2), row0 = t.row0 + half * 128;
+        auto load_w = [&](const CUtensorMap *map, uint32_t at, uint32_t full, int c, int term, int weight) {
+          if (ACROSS) {
+            for (int b = 0; b < (FORM == kFew ? 2 : p.q_bytes / kBox); ++b) load_box<P>(at + (uint32_t)(b * kBox), map, full, n0 + b * 64, term, c, weight);
+          } else {
+            load_box<P>(at, map, full, c, term, n0, weight);
+          }
+        };
+        for (int c = c0; c < c1; ++c, next()) {
+          if (!lead || !ok) continue;
+          const uint32_t full = open(stage_bytes, 0x10000u);
+          if (!full) continue;
+          const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
+          for (int term = 0; term < N; ++term) {
+            if (FORM == kFew) {
+              load_box<P>(b + (uint32_t)(term * p.q_bytes), &map_p, full, c * kPiece, term, row0, 0);
+              load_w(&map_q, a + (uint32_t)(term * kP), full, c * kPiece, term, t.weight);
             } else {
-              tma_load_3d(w_at, &map_q, full, c * kPiece, n0, t.weight);
+              load_box<P>(a + (uint32_t)(term * kP), &map_p, full, c * kPiece, term, row0, 0);
+              load_w(&map_q, b + (uint32_t)(term * p.q_bytes), full, c * kPiece, term, t.weight);
             }
           }
-        } else {
-          for (int c = c0; c < c1; ++c) next();
         }
         __syncwarp();
         if (FORM == kTile && p.rank)
-          each_run(p.ext, t.row0, min(t.end, t.row0 + 128), [&](int, int, int weight) {
-            for (int c = 0; c < 2 * p.rank_pieces; ++c, next()) {
+          each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](int, int, int weight) {
+            for (int c = 0; c < ext_uses; ++c, next()) {
               if (!lead || !ok) continue;
-              ok = mbar_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, 0x20000u | (uint32_t)stage);
-              if (!ok) continue;
+              const uint32_t full = open(stage_bytes, 0x20000u);
+              if (!full) continue;
               const int cc = c % p.rank_pieces;
-              uint64_t *full = &bar[kFull + stage];
-              const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-              mbar_arrive_expect_tx(full, stage_bytes);
-              tma_load_2d(a, &map_t, full, (c < p.rank_pieces ? 0 : grp::rank_pad(p.rank)) + cc * kPiece, t.row0);
-              if (ACROSS) {
-                for (int b = 0; b < p.q_bytes / kBox; ++b) tma_load_3d(a + kP + (uint32_t)(b * kBox), &map_e, full, t.tn * p.nt + b * 64, cc * kPiece, weight);
-              } else {
-                tma_load_3d(a + kP, &map_e, full, cc * kPiece, t.tn * p.nt, weight);
+              const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
+              for (int term = 0; term < N; ++term) {
+                load_box<P>(a + (uint32_t)(term * kP), &map_t, full, (c < p.rank_pieces ? 0 : grp::rank_pad(p.rank)) + cc * kPiece, term, row0, 0);
+                load_w(&map_e, b + (uint32_t)(term * p.q_bytes), full, cc * kPiece, term, weight);
               }
             }
           });
@@ -277,86 +494,109 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       }
     }
   } else if (warp == 1) {
-    // ---------------------------------------------------------------- multiply: one lane issues, without the others
-    const bool lead = elect_one();
-    int stage = 0, buf = 0;
-    uint32_t parity = 0, use = 0, fixed = 0;     // fixed: pieces with rows that were set to zero
-    bool ok = true;
-    auto next = [&]() { if (++stage == p.stages) { stage = 0; parity ^= 1u; } };
-    auto next_item = [&]() { if (++buf == 2) { buf = 0; ++use; } };
-    const uint32_t base = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24) | ((uint32_t)(p.nt >> 3) << 17);
+    // ---------------------------------------------------------------- multiply: one lane issues, without the others (of a pair, the first CTA's)
+    const bool lead = elect_one() && (!P || rank == 0);
+    uint32_t fixed = 0;                          // pieces with rows that were set to zero
+    const uint32_t base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows >> 4) << 24) | ((uint32_t)(p.nt >> 3) << 17);
+    uint32_t d = 0;
+    auto begin = [&]() {                         // the next accumulator
+      ok = ok && mbar_wait(&bar[kDEmpty + (turn & 1u)], (turn >> 1 & 1u) ^ 1u, abort_flag, ws, 0x30000u | (turn & 1u), kLimit);
+      tc_fence_after();
+      d = tmem + (turn & 1u) * (uint32_t)p.acc;
+    };
+    auto end = [&](bool any) {
+      if (any) {
+        commit<P>(&bar[kDFull + (turn & 1u)]);
+      } else {
+        mbar_arrive(&bar[kDFull + (turn & 1u)]);
+        if (P) arrive_cluster(map_cluster(smem_u32(&bar[kDFull + (turn & 1u)]), 1));
+      }
+      ++turn;
+    };
     if (FORM == kGrad) {
       for (long long item = team; ok && item < p.most; item += teams) {
         const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n;
         const bool sums = p.sums && at - tm * p.tiles_n == p.tiles_n - 1;
         if (lead) {
           bool any = false;
-          if (p.sums) ok = mbar_wait(&bar[kOnes], 0, abort_flag, ws, 0x90000u);
-          if (ok) ok = mbar_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x30000u | (uint32_t)buf);
-          tc_fence_after();
-          const uint32_t d = tmem + (uint32_t)(buf * p.acc), idesc = (sums ? (base & ~(0x3Fu << 17)) | (2u << 17) : base) | (1u << 15) | (1u << 16);
+          begin();
+          const uint32_t idesc = (sums ? (base & ~(0x3Fu << 17)) | (uint32_t)(kRows / 64) << 17 : base) | (1u << 15) | (1u << 16);
           if (ok)
-            each_piece(p, weight, rank, [&](int, int rows) {
-              ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x40000u | (uint32_t)stage);
+            each_piece(p, weight, share, [&](int, int rows) {
+              if (kShort && any) {
+                end(true);
+                begin();
+                any = false;
+              }
+              if (ok) ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x40000u | (uint32_t)stage, kLimit);
               if (ok && rows < kPiece) {         // rows of the next run
-                ask_s[0] = stage;
-                ask_s[1] = rows;
-                ask_s[2] = 2 + (sums ? 0 : p.q_bytes / kBox);
+                if (P) arrive_cluster(map_cluster(smem_u32(&bar[kAsk]), 1));
                 mbar_arrive(&bar[kAsk]);
                 ok = mbar_wait(&bar[kFixed], fixed & 1u, abort_flag, ws, 0x50000u | (uint32_t)stage);
+                if (P) mbar_acquire_cluster(&bar[kFixed], fixed & 1u);
                 ++fixed;
               }
               if (!ok) return false;
               tc_fence_after();
-              const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-              const uint64_t ad = desc_across(a), bd = desc_across(sums ? ones : a + kP);
+              const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
               const int steps = (rows + 15) / 16;
-              for (int k = 0; k < steps; ++k, any = true) umma_bf16(d, ad + kStepOf<true> * k, bd + kStepOf<true> * k, idesc, any ? 1u : 0u);
-              umma_commit(&bar[kEmpty + stage]);
+#pragma unroll
+              for (int x = 0; x < kPairs; ++x) {
+                if (sums && kTermQ[x] != 0) continue;              // of the block of ones there is one term
+                const uint64_t ad = desc_across(a + (uint32_t)(kTermP[x] * kP)), bd = desc_across(sums ? ones : b + (uint32_t)(kTermQ[x] * p.q_bytes));
+                if (steps == 4) {
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) umma<P>(d, ad + kStepOf<true> * k, bd + kStepOf<true> * k, idesc, any || k > 0 ? 1u : 0u);
+                } else {
+                  for (int k = 0; k < steps; ++k) umma<P>(d, ad + kStepOf<true> * k, bd + kStepOf<true> * k, idesc, any || k > 0 ? 1u : 0u);
+                }
+                any = true;
+              }
+              commit<P>(&bar[kEmpty + stage]);
               next();
               return true;
             });
-          if (ok) {
-            if (any) umma_commit(&bar[kDFull + buf]);
-            else mbar_arrive(&bar[kDFull + buf]);
-          }
+          if (ok) end(any);
         }
-        next_item();
         ok = __all_sync(0xffffffffu, ok);
-      }
-      if (lead) {                                // no more
-        ask_s[0] = -1;
-        mbar_arrive(&bar[kAsk]);
       }
     } else {
       grp::Walk walk;
       walk.start();
       Tile t;
       const uint32_t idesc = base | (!ACROSS ? 0u : FORM == kFew ? 1u << 15 : 1u << 16);
-      for (long long item = team; ok && item < p.most && find_tile<FORM>(p, walk, item, &t); item += teams) {
+      constexpr bool kA = FORM == kFew && ACROSS, kB = FORM != kFew && ACROSS;     // operands that the sum runs across
+      for (long long item = team; ok && item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
         bool any = false;
-        const uint32_t d = tmem + (uint32_t)(buf * p.acc);
         if (lead) {
-          ok = mbar_wait(&bar[kDEmpty + buf], (use & 1u) ^ 1u, abort_flag, ws, 0x30000u | (uint32_t)buf);
-          tc_fence_after();
+          begin();
           uint32_t ready = 0;
           for (int c = c0; ok && c < c1; ++c) {
-            if (!ready) ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x40000u | (uint32_t)stage);
+            if (kShort && any) {
+              end(true);
+              begin();
+              any = false;
+            }
+            if (ok && !ready) ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x40000u | (uint32_t)stage, kLimit);
             if (!ok) break;
             ready = stage + 1 < p.stages ? mbar_test(&bar[kFull + stage + 1], parity) : mbar_test(&bar[kFull], parity ^ 1u);
             tc_fence_after();
-            const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-            const uint64_t ad = FORM == kFew ? desc_of<ACROSS>(a) : desc_along(a), bd = FORM == kFew ? desc_along(a + kP) : desc_of<ACROSS>(a + kP);
-            constexpr uint32_t kStepA = FORM == kFew ? kStepOf<ACROSS> : kStepOf<false>, kStepB = FORM == kFew ? kStepOf<false> : kStepOf<ACROSS>;
+            const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
             const int steps = min(4, (p.k - c * kPiece + 15) / 16);
-            if (steps == 4) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k) umma_bf16(d, ad + kStepA * k, bd + kStepB * k, idesc, any || k > 0 ? 1u : 0u);
-            } else {
-              for (int k = 0; k < steps; ++k) umma_bf16(d, ad + kStepA * k, bd + kStepB * k, idesc, any || k > 0 ? 1u : 0u);
+            for (int x = 0; x < kPairs; ++x) {
+              // the matrix is the first operand of kFew
+              const int tp = FORM == kFew ? kTermQ[x] : kTermP[x], tq = FORM == kFew ? kTermP[x] : kTermQ[x];
+              const uint64_t ad = desc_of<kA>(a + (uint32_t)(tp * kP)), bd = desc_of<kB>(b + (uint32_t)(tq * p.q_bytes));
+              if (steps == 4) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) umma<P>(d, ad + kStepOf<kA> * k, bd + kStepOf<kB> * k, idesc, any || k > 0 ? 1u : 0u);
+              } else {
+                for (int k = 0; k < steps; ++k) umma<P>(d, ad + kStepOf<kA> * k, bd + kStepOf<kB> * k, idesc, any || k > 0 ? 1u : 0u);
+              }
+              any = true;
             }
-            any = true;
-            umma_commit(&bar[kEmpty + stage]);
+            commit<P>(&bar[kEmpty + stage]);
             next();
           }
         } else {
@@ -364,231 +604,269 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         }
         __syncwarp();
         if (FORM == kTile && p.rank)
-          each_run(p.ext, t.row0, min(t.end, t.row0 + 128), [&](int begin, int end, int) {
-            uint32_t off[4];
+          each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](int first_row, int last_row, int) {
+            uint32_t off[8];                     // lanes of other rows
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {        // lanes of other rows
-              const int lo = max(begin - t.row0 - 32 * i, 0), hi = min(end - t.row0 - 32 * i, 32);
+            for (int i = 0; i < 8; ++i) {
+              const int lo = max(first_row - t.row0 - 32 * i, 0), hi = min(last_row - t.row0 - 32 * i, 32);
               off[i] = lo >= hi ? 0xffffffffu : ~((hi - lo == 32 ? 0xffffffffu : (1u << (hi - lo)) - 1u) << lo);
             }
-            bool first = c0 >= c1;               // without a shared matrix the run's first instruction sets its lanes
-            for (int c = 0; c < 2 * p.rank_pieces; ++c, next()) {
+            bool first = own_pieces == 0;        // without a shared matrix the run's first instruction sets its lanes
+            for (int c = 0; c < ext_uses; ++c, next()) {
               if (!lead || !ok) continue;
-              ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x60000u | (uint32_t)stage);
+              ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x60000u | (uint32_t)stage, kLimit);
               if (!ok) continue;
               tc_fence_after();
-              const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-              const uint64_t ad = desc_along(a), bd = desc_of<ACROSS>(a + kP);
+              const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
               const int steps = min(4, (p.rank - c % p.rank_pieces * kPiece + 15) / 16);
-              for (int k = 0; k < steps; ++k, first = false) umma_lanes(d, ad + kStepOf<false> * k, bd + kStepOf<ACROSS> * k, idesc, first ? 0u : 1u, off);
+              if (N == 3) {
+#pragma unroll
+                for (int x = 0; x < kPairs; ++x)
+                  for (int k = 0; k < steps; ++k, first = false)
+                    umma_lanes<P>(d, desc_along(a + (uint32_t)(kTermP[x] * kP)) + kStepOf<false> * k, desc_of<kB>(b + (uint32_t)(kTermQ[x] * p.q_bytes)) + kStepOf<kB> * k, idesc, first ? 0u : 1u, off);
+              } else {
+                const uint64_t ad = desc_along(a), bd = desc_of<kB>(b);
+                for (int k = 0; k < steps; ++k, first = false) umma_lanes<P>(d, ad + kStepOf<false> * k, bd + kStepOf<kB> * k, idesc, first ? 0u : 1u, off);
+                if (p.rank <= 32)                // the low terms lie behind the high ones
+                  for (int k = 0; k < steps; ++k) umma_lanes<P>(d, ad + kStepOf<false> * (steps + k), bd + kStepOf<kB> * k, idesc, 1u, off);
+              }
               any = true;
-              umma_commit(&bar[kEmpty + stage]);
+              commit<P>(&bar[kEmpty + stage]);
             }
           });
-        if (lead && ok) {
-          if (any) umma_commit(&bar[kDFull + buf]);
-          else mbar_arrive(&bar[kDFull + buf]);
-        }
-        next_item();
+        if (lead && ok) end(any);
         ok = __all_sync(0xffffffffu, ok);
       }
     }
   } else if (warp < 2 + kEpi) {
     // ---------------------------------------------------------------- read out
-    const int quad = warp & 3, set = (warp - 2) >> 2, own = quad * 32 + lane;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    int buf = 0;
-    uint32_t use = 0;
-    bool ok = true;
-    auto next_item = [&]() { if (++buf == 2) { buf = 0; ++use; } };
-    auto release = [&]() {
+    const int quad = warp & 3, set = (warp - 2) >> 2, own = quad * 32 + lane, unit = (warp - 2) * 32 + lane;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16, staged = sm + (uint32_t)(p.off_out + (warp - 2) * 32 * 128);
+    const uint32_t freed = P ? map_cluster(smem_u32(&bar[kDEmpty]), 0) : 0u;
+    auto wait_sums = [&]() {
+      const bool there = warp_wait(&bar[kDFull + (turn & 1u)], turn >> 1 & 1u, abort_flag, ws, 0x70000u | (turn & 1u), kLimit);
+      tc_fence_after();
+      return there;
+    };
+    auto sums_at = [&]() { return tmem + (turn & 1u) * (uint32_t)p.acc + lanes; };
+    auto release = [&]() {                       // the accumulator is read
       tc_fence_before();
       __syncwarp();
-      if (elect_one()) mbar_arrive(&bar[kDEmpty + buf]);
+      if (elect_one()) {
+        if (P) arrive_cluster(freed + (turn & 1u) * 8u);
+        else mbar_arrive(&bar[kDEmpty + (turn & 1u)]);
+      }
       __syncwarp();
     };
-    if (FORM == kGrad) {
-      if (p.sums) {                              // a block of ones: sums are products with it
-        for (int i = (warp - 2) * 32 + lane; i < kBox / 16; i += kEpi * 32) sts_u4(ones + (uint32_t)(i * 16), make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u));
-        fence_proxy_async();
-        bar_sync(1, kEpi * 32);
-        if (warp == 2 && lane == 0) mbar_arrive(&bar[kOnes]);
-      }
-      for (long long item = team; ok && item < p.most; item += teams) {
-        const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n, tn = at - tm * p.tiles_n;
-        const bool sums = p.sums && tn == p.tiles_n - 1;
-        ok = warp_wait(&bar[kDFull + buf], use & 1u, abort_flag, ws, 0x70000u | (uint32_t)buf, kLongNs);
-        if (!ok) break;
-        tc_fence_after();
-        // whether there is anything to read: with none of this CTA's pieces nothing was multiplied
-        int have = 0;
-        each_piece(p, weight, rank, [&](int, int) { have = 1; return false; });
-        const int i = tm * 128 + own, cols = sums ? 16 : p.nt, pad = p.nt / 2;
-        const uint32_t d = tmem + (uint32_t)(buf * p.acc) + lanes;
-        bf16 *out = p.y + (size_t)weight * (size_t)p.k * (size_t)p.n;
-        auto deliver = [&](int c, const float (&v)[16]) {            // columns c on of this thread's row
-          if (i >= p.k) return;
-          if (sums) {
-            if (c == 0) p.sums[(size_t)weight * (size_t)p.k + (size_t)i] = v[0];
-            return;
-          }
-          const int j0 = tn * p.nt + c;
-          if (p.out_across) {
+    constexpr int kBlocks = kShort ? 2 : 4;      // of 32 columns, of a set
+    // parts of a tile's sum in shared memory, [columns][128]; the ring is not in use any more
+    auto part_at = [&](uint32_t from, int c) { return from + (uint32_t)((c * 128 + own) * 4); };
+    float all[kShort ? kBlocks : 1][32];         // fp32: pieces' sums added up
+    // Reads a tile's sums block by block: got(block's first column, sums).  `pieces` of them where they are short; `zero`: nothing was multiplied.
+    // `low`: columns from there on hold a second part of each sum.
+    auto read_out = [&](int pieces, bool zero, int cols, int low, auto got) -> bool {
+      if (kShort) {
 #pragma unroll
-            for (int x = 0; x < 16; ++x)
-              if (j0 + x < p.n) out[(size_t)(j0 + x) * (size_t)p.k + (size_t)i] = __float2bfloat16(v[x]);
-            return;
-          }
-          bf16 *to = out + (size_t)i * (size_t)p.n + (size_t)j0;
-          if (p.vec) {
+        for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int x = 0; x < 16; x += 8)
-              if (j0 + x < p.n) *reinterpret_cast<uint4 *>(to + x) = pack8(v + x);
-          } else {
+          for (int x = 0; x < 32; ++x) all[b < (kShort ? kBlocks : 1) ? b : 0][x] = 0.f;
+        for (int i = 0; i < pieces; ++i) {
+          if (!wait_sums()) return false;
+          const uint32_t d = sums_at();
 #pragma unroll
-            for (int x = 0; x < 16; ++x)
-              if (j0 + x < p.n) to[x] = __float2bfloat16(v[x]);
-          }
-        };
-        if (p.split == 1) {
-          const int half = p.q_terms ? pad : cols;
-          for (int c = set * 16; c < half; c += 32) {
-            float v[16], w[16];
-            __syncwarp();
-            tmem_ld16(d + (uint32_t)c, reinterpret_cast<uint32_t *>(v));
-            if (p.q_terms && !sums) tmem_ld16(d + (uint32_t)(pad + c), reinterpret_cast<uint32_t *>(w));
+          for (int b = 0; b < kBlocks; ++b) {
+            const int c = set * 32 + b * 64;
+            if (c >= cols) break;
+            float v[32];
+            tmem_ld32(d + (uint32_t)c, reinterpret_cast<uint32_t *>(v));
             tmem_ld_wait();
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              if (p.q_terms && !sums) v[x] += w[x];
-              if (!have) v[x] = 0.f;
-            }
-            deliver(c, v);
+            for (int x = 0; x < 32; ++x) all[b < (kShort ? kBlocks : 1) ? b : 0][x] += zero ? 0.f : v[x];
           }
           release();
-        } else {
-          // the part to shared memory, [columns][128]; the ring is not in use any more
-          for (int c = set * 16; c < cols; c += 32) {
-            uint32_t v[16];
-            __syncwarp();
-            tmem_ld16(d + (uint32_t)c, v);
-            tmem_ld_wait();
+          ++turn;
+        }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sm + (uint32_t)(((c + x) * 128 + own) * 4)), "r"(have ? v[x] : 0u) : "memory");
+        for (int b = 0; b < kBlocks; ++b) {
+          const int c = set * 32 + b * 64;
+          if (c >= cols) break;
+          __syncwarp();
+          got(c, all[b < (kShort ? kBlocks : 1) ? b : 0]);
+        }
+        return true;
+      }
+      if (!wait_sums()) return false;
+      const uint32_t d = sums_at();
+      bool held = true;
+#pragma unroll 1
+      for (int c = set * 32; c < cols; c += 64) {
+        float v[32];
+        __syncwarp();
+        tmem_ld32(d + (uint32_t)c, reinterpret_cast<uint32_t *>(v));
+        if (low) {
+          float w[32];
+          tmem_ld32(d + (uint32_t)(low + c), reinterpret_cast<uint32_t *>(w));
+          tmem_ld_wait();
+#pragma unroll
+          for (int x = 0; x < 32; ++x) v[x] += w[x];
+        } else {
+          tmem_ld_wait();
+        }
+        if (c + 64 >= cols) { release(); held = false; }
+        if (zero) {
+#pragma unroll
+          for (int x = 0; x < 32; ++x) v[x] = 0.f;
+        }
+        got(c, v);
+      }
+      if (held) release();
+      ++turn;
+      return true;
+    };
+    // the cluster's parts of block c: added up in the order of their CTAs
+    auto add_parts = [&](int c, int low, float (&v)[32]) {
+#pragma unroll
+      for (int x = 0; x < 32; ++x) v[x] = 0.f;
+      for (int k = 0; k < p.split; ++k) {
+        const uint32_t from = map_cluster(sm, (uint32_t)k);
+#pragma unroll
+        for (int x = 0; x < 32; ++x) v[x] += lds_cluster_f(part_at(from, c + x));
+        if (low) {
+#pragma unroll
+          for (int x = 0; x < 32; ++x) v[x] += lds_cluster_f(part_at(from, low + c + x));
+        }
+      }
+    };
+    auto put_part = [&](int c, const float (&v)[32]) {
+#pragma unroll
+      for (int x = 0; x < 32; ++x) sts_f(part_at(sm, c + x), v[x]);
+    };
+    if (FORM == kGrad) {
+      for (long long item = team; item < p.most; item += teams) {
+        const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n, tn = at - tm * p.tiles_n;
+        const bool sums = p.sums && tn == p.tiles_n - 1;
+        const int mine = count_pieces(p, weight, share);
+        const int i0 = tm * kRows + half * 128 + quad * 32, i = i0 + lane, low = p.q_terms && !kShort && !sums ? p.nt / 2 : 0;
+        const int cols = sums ? 16 : low ? low : p.nt;
+        T *out = reinterpret_cast<T *>(p.y) + (size_t)weight * (size_t)p.k * (size_t)p.n;
+        auto deliver = [&](int c, float (&v)[32]) {                 // columns c on of this thread's row
+          const int j0 = tn * p.nt + c;
+          if (kShort && i < p.k && any_nan(v)) {
+#pragma unroll 1
+            for (int x = 0; x < 32; ++x) {
+              float f = 0.f;
+#pragma unroll
+              for (int u = 0; u < 32; ++u) f = u == x ? v[u] : f;
+              if (f == f || (sums ? x > 0 : j0 + x >= p.n || c + x >= cols)) continue;
+              f = again_grad(p, weight, i, j0 + x, sums);
+#pragma unroll
+              for (int u = 0; u < 32; ++u) v[u] = u == x ? f : v[u];
+            }
           }
+          if (sums) {
+            if (c == 0 && i < p.k) p.sums[(size_t)weight * (size_t)p.k + (size_t)i] = v[0];
+          } else if (p.out_across) {
+            if (i < p.k) {
+#pragma unroll
+              for (int x = 0; x < 32; ++x)
+                if (j0 + x < p.n && c + x < cols) out[(size_t)(j0 + x) * (size_t)p.k + (size_t)i] = (T)v[x];
+            }
+          } else if (i0 < p.k) {
+            store_block<T>(p, staged, v, out + (size_t)i0 * (size_t)p.n + (size_t)j0, (size_t)p.n, min(32, p.k - i0), min(min(32, cols - c), p.n - j0), nullptr, nullptr);
+          }
+        };
+        if (P || p.split == 1) {
+          ok = read_out(max(mine, 1), mine == 0, cols, low, deliver);
+          if (!ok) break;
+        } else {
+          ok = read_out(max(mine, 1), mine == 0, sums ? 16 : p.nt, 0, put_part);
           __syncwarp();
           cluster_sync();
           ++met;
-          const int half = p.q_terms && !sums ? pad : cols, blocks = half / 16;
-          for (int b = rank + set * p.split; b < blocks; b += 2 * p.split) {
-            float v[16];
-#pragma unroll
-            for (int x = 0; x < 16; ++x) v[x] = 0.f;
-            for (int k = 0; k < p.split; ++k) {
-              const uint32_t from = map_cluster(sm, (uint32_t)k);
-#pragma unroll
-              for (int x = 0; x < 16; ++x) {
-                v[x] += lds_cluster_f(from + (uint32_t)(((b * 16 + x) * 128 + own) * 4));
-                if (p.q_terms && !sums) v[x] += lds_cluster_f(from + (uint32_t)(((pad + b * 16 + x) * 128 + own) * 4));
-              }
-            }
-            deliver(b * 16, v);
+          if (!ok) break;
+          for (int c = (rank + set * p.split) * 32; c < cols; c += 64 * p.split) {
+            float v[32];
+            add_parts(c, low, v);
+            deliver(c, v);
           }
-          release();
         }
-        next_item();
       }
     } else if (FORM == kTile) {
       grp::Walk walk;
       walk.start();
       Tile t;
-      for (long long item = team; ok && item < p.most && find_tile<FORM>(p, walk, item, &t); item += teams) {
-        const int row = t.row0 + own;
-        const bool mine = row < t.end;
-        float alpha = p.alpha ? __ldg(p.alpha + t.weight) : 1.f;
+      for (long long item = team; item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
+        const int row0 = t.row0 + half * 128 + quad * 32, row = row0 + lane;
+        const float alpha = p.alpha ? __ldg(p.alpha + t.weight) : 1.f;
         bool filled = true;                      // without a shared matrix: whether an adapter has set this lane
-        if (p.rank && c0 >= c1) {
-          const int s = mine ? grp::first_run_behind(p.ext, row) : p.ext.count;
-          filled = false;
-          for (int r = s; r < p.ext.count; ++r) {      // empty runs in between
-            const Run run = grp::run_at(p.ext, r);
-            if (run.begin > row) break;
-            if (run.end > row) { filled = run.weight >= 0; break; }
-          }
-        }
+        if (p.rank && p.pieces == 0) filled = row < t.end && adapter_of(p.ext, row) >= 0;
         const float *bias = p.bias ? p.bias + (p.bias_each ? (size_t)t.weight * (size_t)p.n : 0) : nullptr;
-        const uint32_t d = tmem + (uint32_t)(buf * p.acc) + lanes;
-        ok = warp_wait(&bar[kDFull + buf], use & 1u, abort_flag, ws, 0x70000u | (uint32_t)buf);
-        if (!ok) break;
-        tc_fence_after();
-        const int o0 = t.tn * p.nt;
-#pragma unroll 1
-        for (int c = set * 32; c < p.nt; c += 64) {
-          float v[32];
-          __syncwarp();
-          tmem_ld32(d + (uint32_t)c, reinterpret_cast<uint32_t *>(v));
-          tmem_ld_wait();
-          if (c + 64 >= p.nt) release();
-          if (!mine) continue;
+        auto deliver = [&](int c, float (&v)[32]) {
+          const int o0 = t.tn * p.nt + c;
+          if (row0 >= t.end) return;
 #pragma unroll
           for (int x = 0; x < 32; ++x) v[x] = filled ? v[x] * alpha : 0.f;
-          if (p.y_terms) {
-            const int pad = grp::rank_pad(p.n);
-            bf16 *to = p.y + (size_t)row * (size_t)(2 * pad) + (size_t)(o0 + c);
-#pragma unroll
-            for (int x = 0; x < 32; x += 8) {
-              if (o0 + c + x >= pad) break;
-              float low[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                if (o0 + c + x + i >= p.n) v[x + i] = 0.f;         // what the padding holds
-                low[i] = left_of(v[x + i]);
-              }
-              *reinterpret_cast<uint4 *>(to + x) = pack8(v + x);
-              *reinterpret_cast<uint4 *>(to + pad + x) = pack8(low);
-            }
-            continue;
-          }
-          const size_t at = (size_t)row * (size_t)p.n + (size_t)(o0 + c);
-          if (p.vec) {
-#pragma unroll
-            for (int x = 0; x < 32; x += 8) {
-              if (o0 + c + x >= p.n || c + x >= p.nt) break;
-              if (bias) {
-                const float4 b0 = __ldg(reinterpret_cast<const float4 *>(bias + o0 + c + x)), b1 = __ldg(reinterpret_cast<const float4 *>(bias + o0 + c + x + 4));
-                v[x] += b0.x; v[x + 1] += b0.y; v[x + 2] += b0.z; v[x + 3] += b0.w;
-                v[x + 4] += b1.x; v[x + 5] += b1.y; v[x + 6] += b1.z; v[x + 7] += b1.w;
-              }
-              if (p.residual) {
-                float r[8];
-                unpack8(*reinterpret_cast<const uint4 *>(p.residual + at + x), r);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[x + i] += r[i];
-              }
-#pragma unroll
-              for (int i = 0; i < 8; ++i) v[x + i] = dc_act_apply(v[x + i], p.act);
-              *reinterpret_cast<uint4 *>(p.y + at + x) = pack8(v + x);
-            }
-          } else {
-#pragma unroll
+          if (kShort && row < t.end && any_nan(v)) {
+#pragma unroll 1
             for (int x = 0; x < 32; ++x) {
-              if (o0 + c + x >= p.n || c + x >= p.nt) break;
-              if (bias) v[x] += __ldg(bias + o0 + c + x);
-              if (p.residual) v[x] += __bfloat162float(p.residual[at + x]);
-              p.y[at + x] = __float2bfloat16(dc_act_apply(v[x], p.act));
+              float f = 0.f;
+#pragma unroll
+              for (int u = 0; u < 32; ++u) f = u == x ? v[u] : f;
+              if (f == f || o0 + x >= p.n || c + x >= p.nt) continue;
+              f = again<ACROSS>(p, row, t.weight, o0 + x);
+#pragma unroll
+              for (int u = 0; u < 32; ++u) v[u] = u == x ? f : v[u];
             }
+          }
+          if (p.y_terms) {
+            constexpr int kKept = N == 3 ? 3 : 2;
+            const int pad = grp::rank_pad(p.n);
+            bf16 *to = reinterpret_cast<bf16 *>(p.y) + (size_t)row * (size_t)(kKept * pad) + (size_t)o0;
+            if (row < t.end) {
+#pragma unroll
+              for (int x = 0; x < 32; x += 8) {
+                if (o0 + x >= pad) break;
+                float term[3][8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  float f[3];
+                  terms_of<T>(o0 + x + i < p.n ? v[x + i] : 0.f, f);         // what the padding holds: zeros
+#pragma unroll
+                  for (int k = 0; k < 3; ++k) term[k][i] = f[k];
+                }
+#pragma unroll
+                for (int k = 0; k < kKept; ++k) *reinterpret_cast<uint4 *>(to + k * pad + x) = pack8(term[k]);
+              }
+            }
+            return;
+          }
+          const size_t at = (size_t)row0 * (size_t)p.n + (size_t)o0;
+          store_block<T>(p, staged, v, reinterpret_cast<T *>(p.y) + at, (size_t)p.n, min(32, t.end - row0), min(min(32, p.nt - c), p.n - o0), bias ? bias + o0 : nullptr,
+                         p.residual ? reinterpret_cast<const T *>(p.residual) + at : nullptr);
+        };
+        if (P || p.split == 1) {
+          ok = read_out(max(own_pieces, 1), false, p.nt, 0, deliver);
+          if (!ok) break;
+        } else {
+          ok = read_out(max(own_pieces, 1), false, p.nt, 0, put_part);
+          __syncwarp();
+          cluster_sync();
+          ++met;
+          if (!ok) break;
+          for (int c = (rank + set * p.split) * 32; c < p.nt; c += 64 * p.split) {
+            float v[32];
+            add_parts(c, 0, v);
+            deliver(c, v);
           }
         }
-        if (set * 32 >= p.nt) release();
-        next_item();
       }
     } else {
       if (p.early) asm volatile("griddepcontrol.wait;" ::: "memory");
       grp::Walk walk;
       walk.start();
       Tile t;
-      const int half = p.nt / 2;                 // of a set of four warps: rows of x
-      for (long long item = team; item < p.most && find_tile<FORM>(p, walk, item, &t); item += teams) {
+      const int half_rows = p.nt / 2;            // of a set of four warps
+      for (long long item = team; item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
         const int o = t.tn * 128 + own, count = min(p.nt, t.end - t.row0);
         float part[kFewMost / 2];
 #pragma unroll
@@ -596,37 +874,24 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         if (p.rank) {
           // the adapters' part of the rows that this CTA delivers, while the shared matrix is multiplied
           const uint32_t ts = sm + (uint32_t)p.off_t;
-          const int pad = grp::rank_pad(p.rank), u = (warp - 2) * 32 + lane;
+          const int pad = grp::rank_pad(p.rank);
           bar_sync(1, kEpi * 32);                // the last item's are read
-          if (u < p.nt) {
-            int w = -1;
-            const int row = t.row0 + u;
-            if (u < count)
-              for (int r = grp::first_run_behind(p.ext, row); r < p.ext.count; ++r) {
-                const Run run = grp::run_at(p.ext, r);
-                if (run.begin > row) break;
-                if (run.end > row) { w = run.weight; break; }
-              }
-            weight_s[u] = w;
-          }
-          for (int i = u; i < count * pad; i += kEpi * 32) {
-            const int r = i / pad, jj = i - r * pad;
-            const bf16 *at = p.t + (size_t)(t.row0 + r) * (size_t)(2 * pad) + (size_t)jj;
-            const float v = __bfloat162float(at[0]) + __bfloat162float(at[pad]);
-            asm volatile("st.shared.f32 [%0], %1;" ::"r"(ts + (uint32_t)(i * 4)), "f"(v) : "memory");
+          if (unit < p.nt) weight_s[unit] = unit < count ? adapter_of(p.ext, t.row0 + unit) : -1;
+          for (int i = unit; i < count * pad; i += kEpi * 32) {
+            const int r = i / pad;
+            sts_f(ts + (uint32_t)(i * 4), kept<T>(p.t, t.row0 + r, pad, i - r * pad));
           }
           bar_sync(1, kEpi * 32);
           if (o < p.n) {
-            const int o_of = o;
 #pragma unroll
             for (int i0 = 0; i0 < kFewMost / 2; i0 += 4) {
-              if (i0 >= half) break;
+              if (i0 >= half_rows) break;
               int w[4];
               bool any = false;
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const int r = set * half + i0 + i;
-                w[i] = r < count && (p.split == 1 || r % p.split == rank) ? weight_s[r] : -1;
+                const int r = set * half_rows + i0 + i;
+                w[i] = r < count && r % p.split == share ? weight_s[r] : -1;
                 any |= w[i] >= 0;
               }
               if (!any) continue;
@@ -634,98 +899,125 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
                 float e[4][8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                  if (ACROSS) {
+                  const T *at = reinterpret_cast<const T *>(p.e) + (ACROSS ? ((size_t)max(w[i], 0) * (size_t)p.rank + (size_t)j0) * (size_t)p.e_pitch + (size_t)o
+                                                                           : ((size_t)max(w[i], 0) * (size_t)p.n + (size_t)o) * (size_t)p.e_pitch + (size_t)j0);
+                  if (ACROSS || !p.e_vec) {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                      e[i][x] = w[i] >= 0 && j0 + x < p.rank ? __bfloat162float(p.e[((size_t)w[i] * (size_t)p.rank + (size_t)(j0 + x)) * (size_t)p.e_pitch + (size_t)o_of]) : 0.f;
-                  } else {
+                    for (int x = 0; x < 8; ++x) e[i][x] = w[i] >= 0 && j0 + x < p.rank ? to_float(at[(size_t)x * (size_t)(ACROSS ? p.e_pitch : 1)]) : 0.f;
+                  } else if (sizeof(T) == 2) {
                     uint4 raw = make_uint4(0, 0, 0, 0);
-                    if (w[i] >= 0) raw = __ldg(reinterpret_cast<const uint4 *>(p.e + ((size_t)w[i] * (size_t)p.n + (size_t)o_of) * (size_t)p.e_pitch + (size_t)j0));
+                    if (w[i] >= 0) raw = __ldg(reinterpret_cast<const uint4 *>(at));
                     unpack8(raw, e[i]);
+                  } else {
+#pragma unroll
+                    for (int x = 0; x < 8; x += 4) {
+                      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+                      if (w[i] >= 0 && j0 + x < p.rank) f = __ldg(reinterpret_cast<const float4 *>(at + x));
+                      e[i][x] = f.x; e[i][x + 1] = f.y; e[i][x + 2] = f.z; e[i][x + 3] = f.w;
+                    }
                   }
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                   if (w[i] < 0) continue;
-                  const uint32_t at = ts + (uint32_t)(((set * half + i0 + i) * pad + j0) * 4);
+                  const uint32_t at = ts + (uint32_t)(((set * half_rows + i0 + i) * pad + j0) * 4);
                   const uint4 t0 = lds_u4(at), t1 = lds_u4(at + 16);
                   const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
-                  for (int x = 0; x < 8; ++x) part[i0 + i] = fmaf(__uint_as_float(tv[x]), e[i][x], part[i0 + i]);
+                  for (int x = 0; x < 8; ++x)
+                    if (sizeof(T) == 2 || j0 + x < p.rank) part[i0 + i] = fmaf(__uint_as_float(tv[x]), e[i][x], part[i0 + i]);
                 }
               }
             }
           }
         }
         const float b = p.bias && o < p.n ? __ldg(p.bias + (p.bias_each ? (size_t)t.weight * (size_t)p.n : 0) + (size_t)o) : 0.f;
-        const uint32_t d = tmem + (uint32_t)(buf * p.acc) + lanes;
-        // a wait that ran out does not end the loop: the barriers above are of all these warps
-        if (!warp_wait(&bar[kDFull + buf], use & 1u, abort_flag, ws, 0x70000u | (uint32_t)buf)) {
-          next_item();
-          continue;
-        }
-        tc_fence_after();
-        auto deliver = [&](int r, float v) {     // row r of the tile: its part of the sum
+        auto deliver = [&](int r, float v, float adapters) {       // row r of the tile: its sum, its adapter's part
           if (r >= count || o >= p.n) return;
           const size_t at = (size_t)(t.row0 + r) * (size_t)p.n + (size_t)o;
+          v += adapters;
+          if (kShort && !(v == v)) v = again<ACROSS>(p, t.row0 + r, t.weight, o);
           v += b;
-          if (p.residual) v += __bfloat162float(p.residual[at]);
-          p.y[at] = __float2bfloat16(dc_act_apply(v, p.act));
+          if (p.residual) v += to_float(reinterpret_cast<const T *>(p.residual)[at]);
+          reinterpret_cast<T *>(p.y)[at] = (T)dc_act_apply(v, p.act);
         };
-        if (p.split == 1) {
+        float sum[kFewMost / 2];
+        // a wait that ran out does not end the loop: the barriers above are of all these warps
+        ok = true;
+#pragma unroll
+        for (int i = 0; i < kFewMost / 2; ++i) sum[i] = 0.f;
+        for (int s = 0; s < (kShort ? max(own_pieces, 1) : 1); ++s, ++turn) {
+          ok = wait_sums();
+          if (!ok) break;
+          const uint32_t d = sums_at() + (uint32_t)(set * half_rows);
 #pragma unroll
           for (int i0 = 0; i0 < kFewMost / 2; i0 += 8) {
-            if (i0 >= half) break;
+            if (i0 >= half_rows) break;
             float v[8];
             __syncwarp();
-            tmem_ld8(d + (uint32_t)(set * half + i0), reinterpret_cast<uint32_t *>(v));
+            tmem_ld8(d + (uint32_t)i0, reinterpret_cast<uint32_t *>(v));
             tmem_ld_wait();
-            if (i0 + 8 >= half) release();
+            if (own_pieces) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) deliver(set * half + i0 + i, (p.pieces ? v[i] : 0.f) + part[i0 + i]);
+              for (int i = 0; i < 8; ++i) sum[i0 + i] += v[i];
+            }
+          }
+          release();
+        }
+        if (p.split == 1) {
+          if (ok) {
+#pragma unroll
+            for (int i = 0; i < kFewMost / 2; ++i)
+              if (i < half_rows) deliver(set * half_rows + i, sum[i], part[i]);
           }
         } else {
-          // parts to shared memory, [rows][128]; the ring is not in use any more
-          for (int i0 = 0; i0 < half; i0 += 8) {
-            uint32_t v[8];
-            __syncwarp();
-            tmem_ld8(d + (uint32_t)(set * half + i0), v);
-            tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sm + (uint32_t)(((set * half + i0 + i) * 128 + own) * 4)), "r"(v[i]) : "memory");
-          }
+          for (int i = 0; i < kFewMost / 2; ++i)
+            if (i < half_rows) sts_f(part_at(sm, set * half_rows + i), sum[i]);
           __syncwarp();
           cluster_sync();
           ++met;
 #pragma unroll
           for (int i = 0; i < kFewMost / 2; ++i) {
-            const int r = set * half + i;
-            if (i >= half || r % p.split != rank || r >= count) continue;
-            float v = part[i];
-            for (int k = 0; k < p.split; ++k) v += lds_cluster_f(map_cluster(sm, (uint32_t)k) + (uint32_t)((r * 128 + own) * 4));
-            deliver(r, v);
+            const int r = set * half_rows + i;
+            if (!ok || i >= half_rows || r % p.split != share || r >= count) continue;
+            float v = 0.f;
+            for (int k = 0; k < p.split; ++k) v += lds_cluster_f(part_at(map_cluster(sm, (uint32_t)k), r));
+            deliver(r, v, part[i]);
           }
-          release();
         }
-        next_item();
       }
     }
   } else {
-    // ---------------------------------------------------------------- kGrad: rows behind the end of a run are set to zero
-    for (uint32_t asked = 0;; ++asked) {
-      if (!warp_wait(&bar[kAsk], asked & 1u, abort_flag, ws, 0x80000u, kLongNs)) break;
-      const int stage = ask_s[0], rows = ask_s[1], boxes = ask_s[2], per = (kPiece - rows) * 8;       // 16 bytes each
-      if (stage < 0) break;
-      const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-      for (int b = 0; b < boxes; ++b)
-        for (int i = lane; i < per; i += 32) sts_u4(a + (uint32_t)(b * kBox + rows * 128 + i * 16), make_uint4(0, 0, 0, 0));
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bar[kFixed]);
+    // ---------------------------------------------------------------- kGrad: rows behind the end of a run are set to zero, once they are there
+    uint32_t asked = 0;
+    for (long long item = team; ok && item < p.most; item += teams) {
+      const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n;
+      const bool sums = p.sums && at - tm * p.tiles_n == p.tiles_n - 1;
+      each_piece(p, weight, share, [&](int, int rows) {
+        if (rows < kPiece) {
+          ok = warp_wait(&bar[kAsk], asked & 1u, abort_flag, ws, 0x80000u, kLongNs);
+          if (!ok) return false;
+          if (P) mbar_acquire_cluster(&bar[kAsk], asked & 1u);
+          ++asked;
+          const uint32_t a = sm + (uint32_t)stage * stage_bytes;
+          const int boxes = N * (2 + (sums ? 0 : p.q_bytes / kBox)), per = (kPiece - rows) * 8;      // 16 bytes each
+          for (int b = 0; b < boxes; ++b)
+            for (int i = lane; i < per; i += 32) sts_u4(a + (uint32_t)(b * kBox + rows * 128 + i * 16), make_uint4(0, 0, 0, 0));
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            if (P) arrive_cluster(map_cluster(smem_u32(&bar[kFixed]), 0));
+            else mbar_arrive(&bar[kFixed]);
+          }
+        }
+        next();
+        return true;
+      });
     }
   }
   __syncwarp();
-  if (p.split > 1)
+  if (!P && p.split > 1)
     for (; met < 2; ++met) cluster_sync();       // the parts are there; and read
   if (warp == 1 && *abort_flag) {                // copies and products may still be in flight: give them time to end
     const unsigned long long t0 = globaltimer_ns();
@@ -734,29 +1026,70 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 1) tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
+  if (P) {
+    cluster_sync();                              // neither CTA's memory is touched by the other's instructions any more
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)p.tmem_cols) : "memory");
+  } else if (warp == 1) {
+    tmem_dealloc(tmem, (uint32_t)p.tmem_cols);
+  }
 }
 
-// x [rows][cols], bf16 -> rows that begin on 16 bytes, zeros behind them
-__global__ void __launch_bounds__(256) k_group_pitch(const bf16 *__restrict__ x, bf16 *__restrict__ y, long long rows, int cols, int pitch) {
+// Rows as the tensor core's kernels read them: bf16 rows begin on 16 bytes, with zeros behind them; fp32 rows are three terms of bf16, one row of
+// each behind the other.  (Two rounded, what is left has 8 bits: tc_ptx.cuh.)  Several arrays in one launch.
+struct Copies {
+  int count;
+  grp::Copy c[grp::kMaxCopies];
+  long long units[grp::kMaxCopies];              // of 8 columns, with those of the arrays before
+};
+template <typename T>
+__global__ void __launch_bounds__(256) k_group_rows_of(const __grid_constant__ Copies all) {
   dc_pdl_enter();
-  const int per = pitch / 8;
-  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < rows * per; u += (long long)gridDim.x * 256) {
-    const long long row = u / per;
-    const int c = (int)(u - row * per) * 8;
-    const unsigned short *from = reinterpret_cast<const unsigned short *>(x) + (size_t)row * (size_t)cols + (size_t)c;
-    uint32_t v[8];
+  const long long total = all.units[all.count - 1];
+  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < total; u += (long long)gridDim.x * 256) {
+    int k = 0;
+    while (u >= all.units[k]) ++k;
+    const grp::Copy &j = all.c[k];
+    const long long v = k ? u - all.units[k - 1] : u;
+    const int per = j.pitch / 8;
+    const long long row = v / per;
+    const int c = (int)(v - row * per) * 8;
+    const T *from = reinterpret_cast<const T *>(j.from) + (size_t)row * (size_t)j.cols + (size_t)c;
+    if (sizeof(T) == 2) {
+      const unsigned short *at = reinterpret_cast<const unsigned short *>(from);
+      uint32_t x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? from[i] : 0;
-    *reinterpret_cast<uint4 *>(y + (size_t)row * (size_t)pitch + (size_t)c) =
-        make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+      for (int i = 0; i < 8; ++i) x[i] = c + i < j.cols ? at[i] : 0;
+      *reinterpret_cast<uint4 *>(reinterpret_cast<bf16 *>(j.to) + (size_t)row * (size_t)j.pitch + (size_t)c) =
+          make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
+    } else {
+      float x[8];
+      if (j.cols % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+          float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (c + i < j.cols) f = *reinterpret_cast<const float4 *>(from + i);
+          x[i] = f.x; x[i + 1] = f.y; x[i + 2] = f.z; x[i + 3] = f.w;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = c + i < j.cols ? to_float(from[i]) : 0.f;
+      }
+      uint4 h, m, l;
+      bf16_terms8(x, h, m, l);
+      uint4 *to = reinterpret_cast<uint4 *>(reinterpret_cast<bf16 *>(j.to) + (size_t)row * (size_t)(3 * j.pitch) + (size_t)c);
+      to[0] = h;
+      to[per] = m;
+      to[2 * per] = l;
+    }
   }
 }
 
 // What rows keep of their adapters where runs are short: a warp to two numbers of a row, the adapter's rows read straight through.
 // The next launch starts only behind the wait for the one before this: what that one wrote is there for it.
-__global__ void __launch_bounds__(256) k_adapter_narrow(const bf16 *__restrict__ x, int x_pitch, const bf16 *__restrict__ a, int a_pitch, int k, int rank,
+template <typename T>
+__global__ void __launch_bounds__(256) k_adapter_narrow(const T *__restrict__ x, int x_pitch, const T *__restrict__ a, int a_pitch, int k, int rank,
                                                         const __grid_constant__ Runs runs, const float *__restrict__ scale, bf16 *__restrict__ t) {
+  constexpr int kPer = 16 / (int)sizeof(T);
   __shared__ int weight_s;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -771,30 +1104,35 @@ __global__ void __launch_bounds__(256) k_adapter_narrow(const bf16 *__restrict__
   if (w < 0) return;
   const int j = (int)blockIdx.y * 16 + warp * 2, pad = grp::rank_pad(rank);
   float s[2] = {0.f, 0.f};
-  const bf16 *xr = x + (size_t)row * (size_t)x_pitch, *ar = a + ((size_t)w * (size_t)rank + (size_t)j) * (size_t)a_pitch;
+  const T *xr = x + (size_t)row * (size_t)x_pitch, *ar = a + ((size_t)w * (size_t)rank + (size_t)j) * (size_t)a_pitch;
   const bool two = j + 1 < rank;
   if (j < rank) {
     constexpr int kAhead = 4;
-    for (int i0 = lane * 8; i0 < k; i0 += kAhead * 256) {
-      uint4 xv[kAhead], av[kAhead], bv[kAhead];
+    for (int i0 = lane * kPer; i0 < k; i0 += kAhead * 32 * kPer) {
+      uint4 v[3][kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int i = i0 + u * 256;
-        xv[u] = av[u] = bv[u] = make_uint4(0, 0, 0, 0);
+        const int i = i0 + u * 32 * kPer;
+        v[0][u] = v[1][u] = v[2][u] = make_uint4(0, 0, 0, 0);
         if (i < k) {
-          xv[u] = *reinterpret_cast<const uint4 *>(xr + i);
-          av[u] = *reinterpret_cast<const uint4 *>(ar + i);
-          if (two) bv[u] = *reinterpret_cast<const uint4 *>(ar + (size_t)a_pitch + i);
+          v[0][u] = *reinterpret_cast<const uint4 *>(xr + i);
+          v[1][u] = *reinterpret_cast<const uint4 *>(ar + i);
+          if (two) v[2][u] = *reinterpret_cast<const uint4 *>(ar + (size_t)a_pitch + i);
         }
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        float xf[8], af[8], bf_[8];
-        unpack8(xv[u], xf);
-        unpack8(av[u], af);
-        unpack8(bv[u], bf_);
+        float f[3][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { s[0] = fmaf(xf[i], af[i], s[0]); s[1] = fmaf(xf[i], bf_[i], s[1]); }
+        for (int y = 0; y < 3; ++y) {
+          if (sizeof(T) == 2) unpack8(v[y][u], f[y]);
+          else {
+            f[y][0] = __uint_as_float(v[y][u].x); f[y][1] = __uint_as_float(v[y][u].y);
+            f[y][2] = __uint_as_float(v[y][u].z); f[y][3] = __uint_as_float(v[y][u].w);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) { s[0] = fmaf(f[0][i], f[1][i], s[0]); s[1] = fmaf(f[0][i], f[2][i], s[1]); }
       }
     }
   }
@@ -804,13 +1142,15 @@ __global__ void __launch_bounds__(256) k_adapter_narrow(const bf16 *__restrict__
     s[1] += __shfl_xor_sync(0xffffffffu, s[1], d);
   }
   if (lane == 0) {
+    constexpr int kKept = sizeof(T) == 4 ? 3 : 2;
     const float f = scale ? __ldg(scale + w) : 1.f;
-    bf16 *to = t + (size_t)row * (size_t)(2 * pad) + (size_t)j;
+    bf16 *to = t + (size_t)row * (size_t)(kKept * pad) + (size_t)j;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float v = j + i < rank ? s[i] * f : 0.f;
-      to[i] = __float2bfloat16(v);
-      to[pad + i] = __float2bfloat16(left_of(v));
+      float term[3];
+      terms_of<T>(j + i < rank ? s[i] * f : 0.f, term);
+#pragma unroll
+      for (int y = 0; y < kKept; ++y) to[y * pad + i] = __float2bfloat16(term[y]);
     }
   }
 }
@@ -829,50 +1169,62 @@ EncodeTiledFn get_encode_fn() {
   }
   return fn;
 }
-// [outer][rows][cols] with rows `pitch` elements apart: boxes of 64 columns x `box` rows, zeros outside
-bool map_of(CUtensorMap *map, const void *at, long long cols, long long rows, long long outer, long long pitch, int box) {
+// [outer][rows][terms][cols], rows of a term `pitch` elements: boxes of 64 columns x `box` rows, zeros outside
+bool map_of(CUtensorMap *map, const void *at, long long cols, int terms, long long rows, long long outer, long long pitch, int box) {
   EncodeTiledFn encode = get_encode_fn();
   if (!encode) return false;
-  const cuuint64_t dim[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)outer}, str[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)pitch * 2 * (cuuint64_t)rows};
-  const cuuint32_t bx[3] = {kPiece, (cuuint32_t)box, 1}, es[3] = {1, 1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, outer ? 3 : 2, const_cast<void *>(at), dim, str, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint64_t one = (cuuint64_t)pitch * 2;
+  const cuuint64_t dim[4] = {(cuuint64_t)cols, (cuuint64_t)terms, (cuuint64_t)rows, (cuuint64_t)outer}, str[3] = {one, one * (cuuint64_t)terms, one * (cuuint64_t)terms * (cuuint64_t)rows};
+  const cuuint32_t bx[4] = {kPiece, 1, (cuuint32_t)box, 1}, es[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(at), dim, str, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int FORM, bool ACROSS>
-cudaError_t launch(const Params &p, int grid, const CUtensorMap (&m)[4], DcWsHeader *ws, cudaStream_t st) {
+template <int FORM, bool ACROSS, typename T, bool P>
+cudaError_t launch(Params &p, long long items, int n_sm, const CUtensorMap (&m)[4], DcWsHeader *ws, cudaStream_t st) {
   static unsigned char attr_done[kDcMaxDevices];
-  const cudaError_t e = dc_set_max_smem_once(k_group_tc<FORM, ACROSS>, kSmem, attr_done);
+  const cudaError_t e = dc_set_max_smem_once(k_group_tc<FORM, ACROSS, T, P>, kSmem, attr_done);
   if (e != cudaSuccess) return e;
-  return dc_launch_pdl_cluster(k_group_tc<FORM, ACROSS>, dim3((unsigned)grid), dim3(kThreadsOf<FORM>), (size_t)kSmem, st, p.split, m[0], m[1], m[2], m[3], p, ws);
+  const int group = P ? 2 : p.split;
+  const long long teams = items < n_sm / group ? items : n_sm / group;
+  p.most = FORM == kGrad ? items : group > 1 && !P ? teams : 1ll << 62;
+  return dc_launch_pdl_cluster(k_group_tc<FORM, ACROSS, T, P>, dim3((unsigned)(teams * group)), dim3(kThreadsOf<FORM>), (size_t)kSmem, st, group, m[0], m[1], m[2], m[3], p, ws);
+}
+template <int FORM, bool ACROSS>
+cudaError_t launch_any(Params &p, bool wide, bool pair, long long items, int n_sm, const CUtensorMap (&m)[4], DcWsHeader *ws, cudaStream_t st) {
+  if (wide) return launch<FORM, ACROSS, float, false>(p, items, n_sm, m, ws, st);
+  if (FORM != kFew && pair) return launch<FORM, ACROSS, bf16, FORM != kFew>(p, items, n_sm, m, ws, st);
+  return launch<FORM, ACROSS, bf16, false>(p, items, n_sm, m, ws, st);
 }
 
-// Shared and tensor memory; `apart`: bytes beside the ring
-void lay_out(Params *p, int apart) {
+// Shared and tensor memory; `apart`: bytes beside the ring and the staged results
+void lay_out(Params *p, int terms, int apart) {
   p->acc = (int)dc_round_up((size_t)p->nt, 32);
   p->tmem_cols = 32;
   while (p->tmem_cols < 2 * p->acc) p->tmem_cols *= 2;
-  p->stages = (kSmem - 1024 - apart) / (kP + p->q_bytes);
+  const int stage = terms * (kP + p->q_bytes);
+  p->stages = (kSmem - 1024 - apart) / stage;
   if (p->stages > kMaxStages) p->stages = kMaxStages;
-  p->off_t = p->stages * (kP + p->q_bytes);
+  p->off_out = p->off_t = p->stages * stage;
 }
 // CTAs that share a tile's sum of `pieces`: as many as keep all SMs busy, each with `least` pieces at least
 int split_of(long long items, int pieces, int least, int n_sm) {
-  int s = items > 0 ? (int)(n_sm / items) : 1;
-  if (s > kMaxSplit) s = kMaxSplit;
+  int s = items > 0 ? (int)(n_sm / items < kMaxSplit ? n_sm / items : kMaxSplit) : 1;
   if (s > pieces / least) s = pieces / least;
-  if (s < 1) s = 1;
-  return s;
+  return s < 1 ? 1 : s;
 }
-// columns to a tile: the fewest rounds of tiles, each as long as its instructions (narrower ones wait for shared memory)
-int columns_of(int n, double tiles_m, int n_sm) {
-  static constexpr struct { int nt; double cost; } kinds[3] = {{256, 1.0}, {128, 0.58}, {64, 0.42}};
-  int best = 256;
+// Columns to a tile, and whether CTAs work in pairs: the fewest rounds of tiles, each as long as its loads take (an SM takes in some 45 bytes a cycle; of
+// 64 terms of 128 x 256 that is 48 KB, of a pair's half tile 32).
+struct Shape { int nt; bool pair; };
+Shape shape_of(int n, double rows, double runs, bool wide, int n_sm) {
+  static constexpr struct { int nt; bool pair; double cost; } kinds[4] = {{256, true, 0.72}, {256, false, 1.0}, {128, false, 0.62}, {64, false, 0.45}};
+  Shape best = {64, false};
   double least = 1e30;
   for (const auto &k : kinds) {
-    if (k.nt > 64 && n <= k.nt / 2) continue;
-    const double rounds = tiles_m * dc_div_up(n, k.nt) / n_sm, time = (rounds < 1 ? 1 : rounds + 0.5) * k.cost;
-    if (time < least) { least = time; best = k.nt; }
+    if ((wide && k.nt > 128) || (k.nt > 64 && n <= k.nt / 2)) continue;
+    const double tiles = (rows / (k.pair ? 256 : 128) + 0.5 * runs) * dc_div_up(n, k.nt), rounds = tiles / (k.pair ? n_sm / 2 : n_sm);
+    const double time = (rounds < 1 ? 1 : rounds + 0.4) * k.cost;
+    if (time < least) { least = time; best = {k.nt, k.pair}; }
   }
   return best;
 }
@@ -881,32 +1233,44 @@ int columns_of(int n, double tiles_m, int n_sm) {
 
 namespace grp {
 
-static long long row_tiles(const Runs &r, int tile) {
-  const long long runs = r.offsets ? (r.count < r.rows ? r.count : r.rows) : 1;
-  return r.rows / tile + runs;
-}
+static int runs_with_rows(const Runs &r) { return !r.offsets ? 1 : r.count < r.rows ? r.count : r.rows; }
+// no more row tiles than this: every run may end inside one
+static long long row_tiles(const Runs &r, int tile) { return r.offsets ? r.rows / tile + runs_with_rows(r) : (r.rows + tile - 1) / tile; }
 
-cudaError_t pitch_tc(const void *x, void *y, long long rows, int cols, int pitch, cudaStream_t st) {
-  const long long blocks = (rows * (pitch / 8) + 255) / 256;
-  return dc_launch_pdl(k_group_pitch, dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))), dim3(256), 0, st, (const bf16 *)x, (bf16 *)y, rows, cols, pitch);
+cudaError_t copies_tc(const Copy *c, int count, dc_dtype dtype, cudaStream_t st) {
+  Copies all = {};
+  long long units = 0;
+  for (int i = 0; i < count; ++i) {
+    if (c[i].rows == 0) continue;
+    units += c[i].rows * (c[i].pitch / 8);
+    all.c[all.count] = c[i];
+    all.units[all.count++] = units;
+  }
+  if (!all.count) return cudaSuccess;
+  const long long blocks = (units + 255) / 256;
+  const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
+  return dtype == DC_BF16 ? dc_launch_pdl(k_group_rows_of<bf16>, grid, dim3(256), 0, st, all) : dc_launch_pdl(k_group_rows_of<float>, grid, dim3(256), 0, st, all);
 }
 
 // Rows whose runs are this short go by kFew (rows through it again for each tile of 64; 128 columns of a matrix are a tile's whatever its rows).
 static bool few(const RowsJob &j) {
   if (j.y_terms) return false;
-  if (!j.runs.offsets) return j.rows <= 128;
-  const int runs = j.runs.count < j.rows ? j.runs.count : j.rows;
-  return j.rows / runs <= 48;
+  return j.runs.offsets ? j.rows / runs_with_rows(j.runs) <= 48 : j.rows <= 128;
 }
-bool narrow_apart(const RowsJob &j) { return j.y_terms && !j.w_across && j.rows <= 1024 && j.rows / (j.runs.count < j.rows ? j.runs.count : j.rows) <= 8; }
-
+bool narrow_apart(const RowsJob &j) {
+  return j.y_terms && !j.w_across && j.rows <= 1024 && j.rows / runs_with_rows(j.runs) <= 8 && (j.dtype == DC_BF16 || j.k % 4 == 0);
+}
 cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st) {
-  return dc_launch_pdl(k_adapter_narrow, dim3((unsigned)j.rows, (unsigned)dc_div_up(rank_pad(j.n), 16)), dim3(256), 0, st, (const bf16 *)j.x, j.x_pitch, (const bf16 *)j.w,
-                       j.w_pitch, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
+  const dim3 grid((unsigned)j.rows, (unsigned)dc_div_up(rank_pad(j.n), 16));
+  if (j.dtype == DC_BF16)
+    return dc_launch_pdl(k_adapter_narrow<bf16>, grid, dim3(256), 0, st, (const bf16 *)j.x, j.x_pitch, (const bf16 *)j.w, j.w_pitch, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
+  return dc_launch_pdl(k_adapter_narrow<float>, grid, dim3(256), 0, st, (const float *)j.raw_x, j.k, (const float *)j.raw_w, j.k, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
 }
 
 cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaStream_t st) {
   const int n_sm = dc_sm_count();
+  const bool wide = j.dtype == DC_F32;
+  const int terms = wide ? 3 : 1;
   Params p = {};
   p.rows = j.rows;
   p.k = j.k;
@@ -916,10 +1280,12 @@ cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaSt
   p.bias = j.bias;
   p.bias_each = j.bias_each;
   p.act = j.act;
-  p.residual = (const bf16 *)j.residual;
-  p.y = (bf16 *)j.y;
+  p.residual = j.residual;
+  p.y = j.y;
   p.y_terms = j.y_terms;
-  p.vec = j.n % 8 == 0;
+  p.vec = j.n % 4 == 0;
+  p.raw_p = j.raw_x;
+  p.raw_q = j.raw_w;
   p.pieces = j.w ? dc_div_up(j.k, kPiece) : 0;
   p.split = 1;
   if (j.t) {
@@ -927,83 +1293,112 @@ cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaSt
     p.rank = j.rank;
     p.rank_pieces = dc_div_up(j.rank, kPiece);
     p.t = (const bf16 *)j.t;
-    p.e = (const bf16 *)j.e;
-    p.e_pitch = j.e_pitch;
+    p.e = wide ? j.raw_e : j.e;
+    p.e_pitch = wide ? (j.e_across ? j.n : j.rank) : j.e_pitch;
+    p.e_vec = !wide || j.rank % 4 == 0;
   }
   const bool by_few = few(j);
+  const int runs = runs_with_rows(j.runs);
   long long items;
+  bool pair = false;
   if (by_few) {
-    const int runs = j.runs.offsets ? (j.runs.count < j.rows ? j.runs.count : j.rows) : 1, mean = j.rows / runs;
+    const int mean = j.rows / runs;
     p.nt = mean <= (runs == 1 ? 16 : 12) ? 16 : mean <= (runs == 1 ? 32 : 24) ? 32 : 64;
     p.q_bytes = p.nt * 128;
     p.tiles_n = dc_div_up(j.n, 128);
     items = row_tiles(j.runs, p.nt) * p.tiles_n;
-    if (runs == 1) items = (long long)dc_div_up(j.rows, p.nt) * p.tiles_n;
     p.split = split_of(items, p.pieces, 4, n_sm);
     p.early = behind_narrow && !j.runs.offsets;
-    lay_out(&p, p.rank ? p.nt * rank_pad(p.rank) * 4 : 0);
+    lay_out(&p, terms, p.rank ? p.nt * rank_pad(p.rank) * 4 : 0);
   } else {
-    const int runs = j.runs.offsets ? (j.runs.count < j.rows ? j.runs.count : j.rows) : 1;
-    p.nt = j.y_terms ? rank_pad(j.n) : columns_of(j.n, j.rows / 128.0 + 0.5 * runs, n_sm);
-    p.q_bytes = j.w_across ? dc_div_up(p.nt, 64) * kBox : p.nt * 128;
+    if (j.y_terms) {
+      p.nt = rank_pad(j.n);
+    } else {
+      const Shape s = shape_of(j.n, j.rows, runs, wide, n_sm);
+      p.nt = s.nt;
+      pair = s.pair;
+    }
+    const int wide_nt = pair ? p.nt / 2 : p.nt;  // of a CTA
+    p.q_bytes = j.w_across || (!j.w && j.e_across) ? dc_div_up(wide_nt, 64) * kBox : wide_nt * 128;
     p.tiles_n = dc_div_up(j.n, p.nt);
-    items = row_tiles(j.runs, 128) * p.tiles_n;
-    lay_out(&p, 0);
+    items = row_tiles(j.runs, pair ? 256 : 128) * p.tiles_n;
+    if (j.y_terms) p.split = split_of(items, p.pieces, 4, n_sm);
+    lay_out(&p, terms, kOut);
   }
   p.pieces_per = dc_div_up(p.pieces, p.split);
   while (p.split > 1 && p.pieces_per * (p.split - 1) >= p.pieces) { --p.split; p.pieces_per = dc_div_up(p.pieces, p.split); }
   CUtensorMap m[4] = {};
   p.maps = (j.w ? 3 : 0) | (j.t && !by_few ? 12 : 0);
-  const int of_w = j.w_across ? 64 : by_few ? 128 : p.nt;
+  const int box = pair ? p.nt / 2 : p.nt;
   if (j.w) {
-    if (!map_of(&m[0], j.x, j.k, j.rows, 0, j.x_pitch, by_few ? p.nt : 128)) return cudaErrorNotSupported;
-    if (!(j.w_across ? map_of(&m[1], j.w, j.n, j.k, j.runs.weights, j.w_pitch, of_w) : map_of(&m[1], j.w, j.k, j.n, j.runs.weights, j.w_pitch, of_w)))
+    if (!map_of(&m[0], j.x, j.k, terms, j.rows, 1, j.x_pitch, by_few ? p.nt : 128)) return cudaErrorNotSupported;
+    if (!(j.w_across ? map_of(&m[1], j.w, j.n, terms, j.k, j.runs.weights, j.w_pitch, 64) : map_of(&m[1], j.w, j.k, terms, j.n, j.runs.weights, j.w_pitch, by_few ? 128 : box)))
       return cudaErrorNotSupported;
   }
   if (j.t && !by_few) {
-    if (!map_of(&m[2], j.t, 2 * rank_pad(j.rank), j.rows, 0, 2 * rank_pad(j.rank), 128)) return cudaErrorNotSupported;
-    if (!(j.e_across ? map_of(&m[3], j.e, j.n, j.rank, j.ext.weights, j.e_pitch, 64) : map_of(&m[3], j.e, j.rank, j.n, j.ext.weights, j.e_pitch, p.nt)))
+    const int pad = rank_pad(j.rank);            // bf16: both terms as one row
+    if (!(wide ? map_of(&m[2], j.t, pad, 3, j.rows, 1, pad, 128) : map_of(&m[2], j.t, 2 * pad, 1, j.rows, 1, 2 * pad, 128))) return cudaErrorNotSupported;
+    if (!(j.e_across ? map_of(&m[3], j.e, j.n, terms, j.rank, j.ext.weights, j.e_pitch, 64) : map_of(&m[3], j.e, j.rank, terms, j.n, j.ext.weights, j.e_pitch, box)))
       return cudaErrorNotSupported;
   }
-  const long long teams = items < n_sm / p.split ? items : n_sm / p.split;
-  const int grid = (int)teams * p.split;
-  p.most = p.split > 1 ? teams : 1ll << 62;
   const bool across = j.w ? j.w_across : j.e_across;
-  if (by_few) return across ? launch<kFew, true>(p, grid, m, ws, st) : launch<kFew, false>(p, grid, m, ws, st);
-  return across ? launch<kTile, true>(p, grid, m, ws, st) : launch<kTile, false>(p, grid, m, ws, st);
+  if (by_few) return across ? launch_any<kFew, true>(p, wide, false, items, n_sm, m, ws, st) : launch_any<kFew, false>(p, wide, false, items, n_sm, m, ws, st);
+  return across ? launch_any<kTile, true>(p, wide, pair, items, n_sm, m, ws, st) : launch_any<kTile, false>(p, wide, pair, items, n_sm, m, ws, st);
 }
 
-// out_w = p^T q of the rows of each weight.  p plain, q plain or what rows keep of an adapter; out [m][n], or [n][m] with out_across.
 cudaError_t grad_tc(const GradJob &j, DcWsHeader *ws, cudaStream_t st) {
   const int n_sm = dc_sm_count();
+  const bool wide = j.dtype == DC_F32;
+  if (wide && j.out && j.sums) {                 // two stages of fp32 terms leave no room for the block of ones
+    GradJob apart = j;
+    apart.out = nullptr;
+    const cudaError_t e = grad_tc(apart, ws, st);
+    if (e != cudaSuccess) return e;
+    apart = j;
+    apart.sums = nullptr;
+    return grad_tc(apart, ws, st);
+  }
+  const int terms = wide ? 3 : 1, pad = rank_pad(j.n), weights = j.runs.weights;
   Params p = {};
   p.rows = j.runs.rows;
   p.k = j.m;
   p.n = j.n;
   p.runs = j.runs;
-  p.y = (bf16 *)j.out;
+  p.y = j.out;
   p.sums = j.sums;
   p.q_terms = j.q_terms;
+  p.t = (const bf16 *)j.q;
   p.out_across = j.out_across;
-  p.vec = j.n % 8 == 0;
-  const int pad = rank_pad(j.n), weights = j.runs.weights;
-  p.tiles_m = dc_div_up(j.m, 128);
-  p.nt = !j.out ? 64 : j.q_terms ? 2 * pad : columns_of(j.n, (double)p.tiles_m * weights, n_sm);
-  p.q_bytes = dc_div_up(p.nt, 64) * kBox;
-  p.tiles_n = (j.out ? dc_div_up(j.q_terms ? 1 : j.n, j.q_terms ? 1 : p.nt) : 0) + (j.sums ? 1 : 0);
+  p.vec = j.n % 4 == 0;
+  p.raw_p = j.raw_p;
+  p.raw_q = j.raw_q;
+  bool pair = false;
+  if (!j.out) {
+    p.nt = 64;
+  } else if (j.q_terms) {
+    p.nt = wide ? pad : 2 * pad;
+  } else {
+    const Shape s = shape_of(j.n, (double)j.m * weights, 0, wide, n_sm);
+    p.nt = s.nt;
+    pair = s.pair && j.m > 128;
+  }
+  p.tiles_m = dc_div_up(j.m, pair ? 256 : 128);
+  p.q_bytes = dc_div_up(pair ? p.nt / 2 : p.nt, 64) * kBox;
+  p.tiles_n = (j.out ? (j.q_terms ? 1 : dc_div_up(j.n, p.nt)) : 0) + (j.sums ? 1 : 0);
   const long long items = (long long)p.tiles_m * p.tiles_n * weights;
-  const int pieces = j.runs.rows / kPiece / weights;
-  p.split = split_of(items, pieces, 4, n_sm);
-  lay_out(&p, j.sums ? kBox : 0);
+  p.split = pair ? 1 : split_of(items, j.runs.rows / kPiece / weights, 4, n_sm);
+  lay_out(&p, terms, kOut + (j.sums ? kBox : 0));
+  if (j.sums) p.off_out += kBox;
   CUtensorMap m[4] = {};
   p.maps = j.runs.rows ? (j.out ? 3 : 1) : 0;
   if (j.runs.rows) {                             // without rows nothing is loaded
-    if (!map_of(&m[0], j.p, j.m, j.runs.rows, 0, j.p_pitch, 64)) return cudaErrorNotSupported;
-    if (j.out && !map_of(&m[1], j.q, j.q_terms ? 2 * pad : j.n, j.runs.rows, 0, j.q_terms ? 2 * pad : j.q_pitch, 64)) return cudaErrorNotSupported;
+    if (!map_of(&m[0], j.p, j.m, terms, j.runs.rows, 1, j.p_pitch, 64)) return cudaErrorNotSupported;
+    if (j.out && !(!j.q_terms ? map_of(&m[1], j.q, j.n, terms, j.runs.rows, 1, j.q_pitch, 64)
+                   : wide     ? map_of(&m[1], j.q, pad, 3, j.runs.rows, 1, pad, 64)
+                              : map_of(&m[1], j.q, 2 * pad, 1, j.runs.rows, 1, 2 * pad, 64)))
+      return cudaErrorNotSupported;
   }
-  const long long teams = items < n_sm / p.split ? items : n_sm / p.split;
-  p.most = items;
-  return launch<kGrad, true>(p, (int)teams * p.split, m, ws, st);
+  return launch_any<kGrad, true>(p, wide, pair, items, n_sm, m, ws, st);
 }
 
 }  // namespace grp

@@ -777,9 +777,13 @@ class Adapters:
     def saved(self, rows: int):
         """A buffer in which adapter_forward leaves for adapter_backward what its gradients need."""
         import torch
-        nbytes = C.c_size_t(0)
-        _check(lib().dc_adapter_saved_bytes(rows, self.rank, self.dtype, C.byref(nbytes)), "dc_adapter_saved_bytes")
-        return torch.empty(int(nbytes.value), dtype=torch.uint8, device=self.a.device)
+        return torch.empty(adapter_saved_bytes(rows, self.rank, self.dtype), dtype=torch.uint8, device=self.a.device)
+
+
+def adapter_saved_bytes(rows: int, rank: int, dtype: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().dc_adapter_saved_bytes(rows, rank, dtype, C.byref(nbytes)), "dc_adapter_saved_bytes")
+    return int(nbytes.value)
 
 
 def adapter_workspace_bytes(rows: int, c_in: int, c_out: int, adapters: Adapters, dtype: int) -> int:
@@ -794,7 +798,7 @@ def _adapter_call(what: str, rows: int, w, adapters: Adapters, offsets, which, s
     _numbers(which, which.numel(), what + ": which")
     _numbers(offsets, which.numel() + 1, what + ": offsets")
     if saved is not None:
-        need = rows * (-(-adapters.rank // 16) * 16) * 4
+        need = adapter_saved_bytes(rows, adapters.rank, dtype_code(dtype))
         if _nbytes(saved) < need or not saved.is_contiguous():
             raise ValueError("%s: a saved buffer of %d bytes is wanted" % (what, need))
 

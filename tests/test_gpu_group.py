@@ -96,6 +96,8 @@ GROUPS = [
     ([2] * 40 + [0] * 30 + [9], 7, 256, 192),
     ([16, 16, 31, 15], 0, 1024, 128),
     ([700, 260, 515], 9, 520, 776),
+    ([2500, 1, 0, 1303], 5, 1032, 2056),         # pairs of CTAs
+    ([1900, 1501], 3, 1031, 1100),
 ]
 
 
@@ -193,6 +195,8 @@ ADAPTERS = [
     ([(1, 0), (1, 1)], 0, 2, 12, 33, 1001),
     ([], 9, 2, 16, 64, 64),
     ([(450, 0)], 0, 1, 48, 264, 1032),
+    ([(2500, 0), (3, 1), (1300, 1), (200, -1)], 7, 2, 48, 1032, 2056),         # pairs of CTAs
+    ([(1, 0)] * 30 + [(1900, 2), (1, 1), (1, -1), (1500, 0)], 3, 3, 16, 1100, 1032),
 ]
 
 

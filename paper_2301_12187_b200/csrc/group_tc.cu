@@ -40,7 +40,7 @@ constexpr int kP = 128 * 128;                    // bytes of the 128-row operand
 constexpr int kBox = 64 * 128;                   // 64 columns of 64 rows
 constexpr int kOut = kEpi * 32 * 128;            // staged results: 32 rows x 32 sums a warp
 constexpr int kSuper = 16;                       // rows of tiles that are walked together: 16 x 9 tiles at once read a twelfth of what a row or column of them would
-constexpr int kFewMost = 64;                     // rows of a tile of kFew
+constexpr int kFewMost = 64, kFewWide = 32;     // rows of a tile of kFew; of fp32, whose sums are kept in registers
 constexpr unsigned long long kLongNs = 20ull * 1000ull * 1000ull * 1000ull;      // a gradient's tile may take seconds (a sum over 2^30 rows), and so may NaN by FMAs
 
 typedef __nv_bfloat16 bf16;
@@ -293,9 +293,31 @@ static __device__ __noinline__ float again_grad(const Params &p, int weight, int
   return s;
 }
 
+// What a lane delivers of a block of 32 rows x 32 columns: 4 columns of every fourth row.  Its part of the residual, asked for ahead:
+template <typename T>
+struct Ahead { uint4 v[sizeof(T) == 4 ? 8 : 4]; };
+template <typename T>
+__device__ __forceinline__ void ask_block(const Params &p, Ahead<T> &a, const T *residual, size_t pitch, int rows, int cols) {
+  const int lane = (int)(threadIdx.x & 31u), piece = lane & 7, r0 = lane >> 3;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = i * 4 + r0;
+    const bool here = residual && row < rows && piece * 4 < cols;
+    const T *at = residual + (size_t)row * pitch + (size_t)(piece * 4);
+    if (sizeof(T) == 4) {
+      a.v[sizeof(T) == 4 ? i : 0] = here ? *reinterpret_cast<const uint4 *>(at) : make_uint4(0, 0, 0, 0);
+    } else {
+      const uint2 u = here ? *reinterpret_cast<const uint2 *>(at) : make_uint2(0, 0);
+      uint4 &w = a.v[i >> 1];
+      if (i & 1) { w.z = u.x; w.w = u.y; }
+      else { w.x = u.x; w.y = u.y; }
+    }
+  }
+}
 // 32 sums of each lane's row -> rows of y, `rows` x `cols` of them, through shared memory: a row's results then go out side by side
 template <typename T>
-__device__ __forceinline__ void store_block(const Params &p, uint32_t stage, const float (&v)[32], T *y, size_t pitch, int rows, int cols, const float *bias, const T *residual) {
+__device__ __forceinline__ void store_block(const Params &p, uint32_t stage, const float (&v)[32], T *y, size_t pitch, int rows, int cols, const float *bias, const T *residual,
+                                            const Ahead<T> *ahead) {
   const int lane = (int)(threadIdx.x & 31u);
   __syncwarp();
 #pragma unroll
@@ -307,32 +329,25 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
     const int piece = lane & 7, r0 = lane >> 3;
     if (piece * 4 >= cols) return;
     const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias) + piece) : make_float4(0.f, 0.f, 0.f, 0.f);
-    float r[8][4];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = i * 4 + r0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) r[i][x] = 0.f;
-      if (residual && row < rows) {
-        const T *at = residual + (size_t)row * pitch + (size_t)(piece * 4);
-        if (sizeof(T) == 4) {
-          const float4 f = *reinterpret_cast<const float4 *>(at);
-          r[i][0] = f.x; r[i][1] = f.y; r[i][2] = f.z; r[i][3] = f.w;
-        } else {
-          const uint2 u = *reinterpret_cast<const uint2 *>(at);
-          r[i][0] = __uint_as_float(u.x << 16); r[i][1] = __uint_as_float(u.x & 0xffff0000u);
-          r[i][2] = __uint_as_float(u.y << 16); r[i][3] = __uint_as_float(u.y & 0xffff0000u);
-        }
-      }
-    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int row = i * 4 + r0;
       if (row >= rows) break;
       const uint4 w = lds_u4(stage + (uint32_t)(row * 128 + ((piece ^ (row & 7)) * 16)));
       float f[4] = {__uint_as_float(w.x) + b.x, __uint_as_float(w.y) + b.y, __uint_as_float(w.z) + b.z, __uint_as_float(w.w) + b.w};
+      if (ahead) {
+        if (sizeof(T) == 4) {
+          const uint4 u = ahead->v[sizeof(T) == 4 ? i : 0];
+          f[0] += __uint_as_float(u.x); f[1] += __uint_as_float(u.y); f[2] += __uint_as_float(u.z); f[3] += __uint_as_float(u.w);
+        } else {
+          const uint4 w2 = ahead->v[i >> 1];
+          const uint2 u = i & 1 ? make_uint2(w2.z, w2.w) : make_uint2(w2.x, w2.y);
+          f[0] += __uint_as_float(u.x << 16); f[1] += __uint_as_float(u.x & 0xffff0000u);
+          f[2] += __uint_as_float(u.y << 16); f[3] += __uint_as_float(u.y & 0xffff0000u);
+        }
+      }
 #pragma unroll
-      for (int x = 0; x < 4; ++x) f[x] = dc_act_apply(f[x] + r[i][x], p.act);
+      for (int x = 0; x < 4; ++x) f[x] = dc_act_apply(f[x], p.act);
       T *at = y + (size_t)row * pitch + (size_t)(piece * 4);
       if (sizeof(T) == 4) *reinterpret_cast<float4 *>(at) = make_float4(f[0], f[1], f[2], f[3]);
       else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
@@ -351,7 +366,7 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
   }
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kAsk = kDEmpty + 2, kFixed, kBars };
+enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kAsk = kDEmpty + 2, kFixed, kParts, kBars };
 
 // P: in pairs.  ACROSS: the matrices' sums run across their rows (of both operands of a gradient always).
 template <int FORM, bool ACROSS, typename T, bool P>
@@ -373,12 +388,13 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sm = (smem_u32(smem_raw) + 1023u) & ~1023u;
   if (warp == 0) {
-    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? (P ? 2 : 1) * kEpi : i == kFixed && P ? 2 : 1);
+    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? (P ? 2 : 1) * kEpi : i == kFixed && P ? 2 : i == kParts ? p.split * kEpi : 1);
     if (lane == 0) abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   } else if (warp == 1 && lane < 4) {
     if (p.maps >> lane & 1) prefetch_tensormap(lane == 0 ? &map_p : lane == 1 ? &map_q : lane == 2 ? &map_t : &map_e);
   }
+  if (FORM == kFew && p.split > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");   // this CTA is there, its barriers too: waited for before parts go out
   // Tensor memory only behind the wait for the launch before this one, whose CTAs may still have theirs to ask for; the one in front of an
   // early launch has none.
   if (FORM == kFew && p.early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -772,7 +788,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
                 if (j0 + x < p.n && c + x < cols) out[(size_t)(j0 + x) * (size_t)p.k + (size_t)i] = (T)v[x];
             }
           } else if (i0 < p.k) {
-            store_block<T>(p, staged, v, out + (size_t)i0 * (size_t)p.n + (size_t)j0, (size_t)p.n, min(32, p.k - i0), min(min(32, cols - c), p.n - j0), nullptr, nullptr);
+            store_block<T>(p, staged, v, out + (size_t)i0 * (size_t)p.n + (size_t)j0, (size_t)p.n, min(32, p.k - i0), min(min(32, cols - c), p.n - j0), nullptr, nullptr, nullptr);
           }
         };
         if (P || p.split == 1) {
@@ -801,8 +817,20 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         bool filled = true;                      // without a shared matrix: whether an adapter has set this lane
         if (p.rank && p.pieces == 0) filled = row < t.end && adapter_of(p.ext, row) >= 0;
         const float *bias = p.bias ? p.bias + (p.bias_each ? (size_t)t.weight * (size_t)p.n : 0) : nullptr;
+        Ahead<T> next_residual;
+        const bool residual = p.residual && p.vec;
+        auto ask = [&](int c) {
+          const int o0 = t.tn * p.nt + c;
+          if (residual && row0 < t.end && c < p.nt && o0 < p.n)
+            ask_block<T>(p, next_residual, reinterpret_cast<const T *>(p.residual) + (size_t)row0 * (size_t)p.n + (size_t)o0, (size_t)p.n, min(32, t.end - row0), min(min(32, p.nt - c), p.n - o0));
+        };
+        const int c_first = p.split > 1 ? (rank + set * p.split) * 32 : set * 32, c_step = 64 * p.split;
+        if (!kShort) ask(c_first);               // (fp32 has no registers to spare)
         auto deliver = [&](int c, float (&v)[32]) {
           const int o0 = t.tn * p.nt + c;
+          if (kShort) ask(c);
+          const Ahead<T> now = next_residual;
+          if (!kShort) ask(c + c_step);
           if (row0 >= t.end) return;
 #pragma unroll
           for (int x = 0; x < 32; ++x) v[x] = filled ? v[x] * alpha : 0.f;
@@ -842,7 +870,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           }
           const size_t at = (size_t)row0 * (size_t)p.n + (size_t)o0;
           store_block<T>(p, staged, v, reinterpret_cast<T *>(p.y) + at, (size_t)p.n, min(32, t.end - row0), min(min(32, p.nt - c), p.n - o0), bias ? bias + o0 : nullptr,
-                         p.residual ? reinterpret_cast<const T *>(p.residual) + at : nullptr);
+                         p.residual ? reinterpret_cast<const T *>(p.residual) + at : nullptr, residual ? &now : nullptr);
         };
         if (P || p.split == 1) {
           ok = read_out(max(own_pieces, 1), false, p.nt, 0, deliver);
@@ -853,7 +881,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           cluster_sync();
           ++met;
           if (!ok) break;
-          for (int c = (rank + set * p.split) * 32; c < p.nt; c += 64 * p.split) {
+          for (int c = c_first; c < p.nt; c += c_step) {
             float v[32];
             add_parts(c, 0, v);
             deliver(c, v);
@@ -866,127 +894,161 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       walk.start();
       Tile t;
       const int half_rows = p.nt / 2;            // of a set of four warps
+      const uint32_t ts = sm + (uint32_t)p.off_t, es = ts + (uint32_t)(p.rank ? p.nt * grp::rank_pad(p.rank) * 4 : 0), parts = es + (uint32_t)(p.rank ? p.nt * 512 : 0);
+      const int part_rows = (p.nt + p.split - 1) / p.split;
+      // The rows that this thread delivers, one after the other: of a cluster's CTAs each has every split-th row of the tile.
+      auto row_of = [&](int v) { return p.split == 1 ? set * half_rows + v : share + p.split * (2 * v + set); };
+      auto rows_here = [&](int count) { return p.split == 1 ? min(half_rows, count - set * half_rows) : (count - share - set * p.split + 2 * p.split - 1) / (2 * p.split); };
       for (long long item = team; item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
-        const int o = t.tn * 128 + own, count = min(p.nt, t.end - t.row0);
-        float part[kFewMost / 2];
-#pragma unroll
-        for (int i = 0; i < kFewMost / 2; ++i) part[i] = 0.f;
+        const int o = t.tn * 128 + own, count = min(p.nt, t.end - t.row0), here = rows_here(count);
         if (p.rank) {
-          // the adapters' part of the rows that this CTA delivers, while the shared matrix is multiplied
-          const uint32_t ts = sm + (uint32_t)p.off_t;
+          // the adapters' part of the rows that this thread delivers, while the shared matrix is multiplied
           const int pad = grp::rank_pad(p.rank);
           bar_sync(1, kEpi * 32);                // the last item's are read
           if (unit < p.nt) weight_s[unit] = unit < count ? adapter_of(p.ext, t.row0 + unit) : -1;
+#pragma unroll 1
           for (int i = unit; i < count * pad; i += kEpi * 32) {
             const int r = i / pad;
             sts_f(ts + (uint32_t)(i * 4), kept<T>(p.t, t.row0 + r, pad, i - r * pad));
           }
           bar_sync(1, kEpi * 32);
-          if (o < p.n) {
+          constexpr int kAtOnce = 4;             // rows, for as many loads on their way
+#pragma unroll 1
+          for (int v0 = 0; v0 < here; v0 += kAtOnce) {
+            int w[kAtOnce], r[kAtOnce];
+            float sum[kAtOnce];
 #pragma unroll
-            for (int i0 = 0; i0 < kFewMost / 2; i0 += 4) {
-              if (i0 >= half_rows) break;
-              int w[4];
-              bool any = false;
+            for (int i = 0; i < kAtOnce; ++i) {
+              r[i] = row_of(v0 + i);
+              w[i] = v0 + i < here && o < p.n ? weight_s[r[i]] : -1;
+              sum[i] = 0.f;
+            }
+#pragma unroll 2
+            for (int j0 = 0; j0 < p.rank; j0 += 8) {
+              float e[kAtOnce][8];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int r = set * half_rows + i0 + i;
-                w[i] = r < count && r % p.split == share ? weight_s[r] : -1;
-                any |= w[i] >= 0;
-              }
-              if (!any) continue;
-              for (int j0 = 0; j0 < p.rank; j0 += 8) {
-                float e[4][8];
+              for (int i = 0; i < kAtOnce; ++i) {
+                const T *at = reinterpret_cast<const T *>(p.e) + (ACROSS ? ((size_t)max(w[i], 0) * (size_t)p.rank + (size_t)j0) * (size_t)p.e_pitch + (size_t)o
+                                                                         : ((size_t)max(w[i], 0) * (size_t)p.n + (size_t)o) * (size_t)p.e_pitch + (size_t)j0);
+                if (ACROSS || (sizeof(T) == 4 && !p.e_vec)) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const T *at = reinterpret_cast<const T *>(p.e) + (ACROSS ? ((size_t)max(w[i], 0) * (size_t)p.rank + (size_t)j0) * (size_t)p.e_pitch + (size_t)o
-                                                                           : ((size_t)max(w[i], 0) * (size_t)p.n + (size_t)o) * (size_t)p.e_pitch + (size_t)j0);
-                  if (ACROSS || !p.e_vec) {
+                  for (int x = 0; x < 8; ++x) e[i][x] = w[i] >= 0 && j0 + x < p.rank ? to_float(at[(size_t)x * (size_t)(ACROSS ? p.e_pitch : 1)]) : 0.f;
+                } else if (sizeof(T) == 2) {
+                  uint4 raw = make_uint4(0, 0, 0, 0);
+                  if (w[i] >= 0) raw = __ldg(reinterpret_cast<const uint4 *>(at));
+                  unpack8(raw, e[i]);
+                } else {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) e[i][x] = w[i] >= 0 && j0 + x < p.rank ? to_float(at[(size_t)x * (size_t)(ACROSS ? p.e_pitch : 1)]) : 0.f;
-                  } else if (sizeof(T) == 2) {
-                    uint4 raw = make_uint4(0, 0, 0, 0);
-                    if (w[i] >= 0) raw = __ldg(reinterpret_cast<const uint4 *>(at));
-                    unpack8(raw, e[i]);
-                  } else {
-#pragma unroll
-                    for (int x = 0; x < 8; x += 4) {
-                      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-                      if (w[i] >= 0 && j0 + x < p.rank) f = __ldg(reinterpret_cast<const float4 *>(at + x));
-                      e[i][x] = f.x; e[i][x + 1] = f.y; e[i][x + 2] = f.z; e[i][x + 3] = f.w;
-                    }
+                  for (int x = 0; x < 8; x += 4) {
+                    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (w[i] >= 0 && j0 + x < p.rank) f = __ldg(reinterpret_cast<const float4 *>(at + x));
+                    e[i][x] = f.x; e[i][x + 1] = f.y; e[i][x + 2] = f.z; e[i][x + 3] = f.w;
                   }
                 }
+              }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  if (w[i] < 0) continue;
-                  const uint32_t at = ts + (uint32_t)(((set * half_rows + i0 + i) * pad + j0) * 4);
-                  const uint4 t0 = lds_u4(at), t1 = lds_u4(at + 16);
-                  const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
+              for (int i = 0; i < kAtOnce; ++i) {
+                const uint32_t at = ts + (uint32_t)(((w[i] >= 0 ? r[i] : 0) * pad + j0) * 4);
+                const uint4 t0 = lds_u4(at), t1 = lds_u4(at + 16);
+                const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
+                // zeros of the matrix's padding or of a row without an adapter are not multiplied: t may be no number there
 #pragma unroll
-                  for (int x = 0; x < 8; ++x)
-                    if (sizeof(T) == 2 || j0 + x < p.rank) part[i0 + i] = fmaf(__uint_as_float(tv[x]), e[i][x], part[i0 + i]);
-                }
+                for (int x = 0; x < 8; ++x)
+                  if (w[i] >= 0) sum[i] = fmaf(__uint_as_float(tv[x]), e[i][x], sum[i]);
               }
             }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+              if (v0 + i < here) sts_f(part_at(es, r[i]), sum[i]);
           }
         }
         const float b = p.bias && o < p.n ? __ldg(p.bias + (p.bias_each ? (size_t)t.weight * (size_t)p.n : 0) + (size_t)o) : 0.f;
-        auto deliver = [&](int r, float v, float adapters) {       // row r of the tile: its sum, its adapter's part
+        auto deliver = [&](int r, float v) {     // row r of the tile: its sum
           if (r >= count || o >= p.n) return;
           const size_t at = (size_t)(t.row0 + r) * (size_t)p.n + (size_t)o;
-          v += adapters;
+          if (p.rank) v += lds_f(part_at(es, r));
           if (kShort && !(v == v)) v = again<ACROSS>(p, t.row0 + r, t.weight, o);
           v += b;
           if (p.residual) v += to_float(reinterpret_cast<const T *>(p.residual)[at]);
           reinterpret_cast<T *>(p.y)[at] = (T)dc_act_apply(v, p.act);
         };
-        float sum[kFewMost / 2];
+        // a block of eight rows' sums goes to whom they are delivered by
+        auto hand_on = [&](int i0, const float *v) {
+          if (p.split == 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) deliver(set * half_rows + i0 + i, v[i]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = set * half_rows + i0 + i, q = r / p.split;
+              asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_cluster(part_at(parts, share * part_rows + q), (uint32_t)(r - q * p.split))), "f"(v[i]) : "memory");
+            }
+          }
+        };
+        if (p.split > 1 && met++ == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");         // the other CTAs are there
         // a wait that ran out does not end the loop: the barriers above are of all these warps
-        ok = true;
+        float short_sum[kShort ? kFewWide / 2 : 1];
+        if (kShort) {
 #pragma unroll
-        for (int i = 0; i < kFewMost / 2; ++i) sum[i] = 0.f;
-        for (int s = 0; s < (kShort ? max(own_pieces, 1) : 1); ++s, ++turn) {
+          for (int i = 0; i < (kShort ? kFewWide / 2 : 1); ++i) short_sum[i] = 0.f;
+#pragma unroll 1
+          for (int k = 0; k < max(own_pieces, 1); ++k, ++turn) {
+            ok = wait_sums();
+            if (!ok) break;
+            const uint32_t d = sums_at() + (uint32_t)(set * half_rows);
+#pragma unroll
+            for (int i0 = 0; i0 < kFewWide / 2; i0 += 8) {
+              if (i0 >= half_rows) break;
+              float v[8];
+              __syncwarp();
+              tmem_ld8(d + (uint32_t)i0, reinterpret_cast<uint32_t *>(v));
+              tmem_ld_wait();
+              if (own_pieces) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) short_sum[kShort ? i0 + i : 0] += v[i];
+              }
+            }
+            release();
+          }
+          if (ok) {
+#pragma unroll
+            for (int i0 = 0; i0 < (kShort ? kFewWide / 2 : 0); i0 += 8)
+              if (i0 < half_rows) hand_on(i0, short_sum + i0);
+          }
+        } else {
           ok = wait_sums();
-          if (!ok) break;
           const uint32_t d = sums_at() + (uint32_t)(set * half_rows);
-#pragma unroll
-          for (int i0 = 0; i0 < kFewMost / 2; i0 += 8) {
-            if (i0 >= half_rows) break;
+#pragma unroll 1
+          for (int i0 = 0; ok && i0 < half_rows; i0 += 8) {
             float v[8];
             __syncwarp();
             tmem_ld8(d + (uint32_t)i0, reinterpret_cast<uint32_t *>(v));
             tmem_ld_wait();
-            if (own_pieces) {
+            if (i0 + 8 >= half_rows) release();
+            if (!own_pieces) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) sum[i0 + i] += v[i];
+              for (int i = 0; i < 8; ++i) v[i] = 0.f;
             }
+            hand_on(i0, v);
           }
-          release();
+          ++turn;
         }
-        if (p.split == 1) {
-          if (ok) {
-#pragma unroll
-            for (int i = 0; i < kFewMost / 2; ++i)
-              if (i < half_rows) deliver(set * half_rows + i, sum[i], part[i]);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < kFewMost / 2; ++i)
-            if (i < half_rows) sts_f(part_at(sm, set * half_rows + i), sum[i]);
+        if (p.split > 1) {
           __syncwarp();
-          cluster_sync();
-          ++met;
-#pragma unroll
-          for (int i = 0; i < kFewMost / 2; ++i) {
-            const int r = set * half_rows + i;
-            if (!ok || i >= half_rows || r % p.split != share || r >= count) continue;
-            float v = 0.f;
-            for (int k = 0; k < p.split; ++k) v += lds_cluster_f(part_at(map_cluster(sm, (uint32_t)k), r));
-            deliver(r, v, part[i]);
+          if (lane < p.split) arrive_cluster(map_cluster(smem_u32(&bar[kParts]), (uint32_t)lane));
+          if (warp_wait(&bar[kParts], 0, abort_flag, ws, 0x90000u, kLimit) && ok) {
+            mbar_acquire_cluster(&bar[kParts], 0);
+#pragma unroll 1
+            for (int v0 = 0; v0 < here; ++v0) {
+              const int r = row_of(v0);
+              float v = 0.f;
+              for (int k = 0; k < p.split; ++k) v += lds_f(part_at(parts, k * part_rows + r / p.split));
+              deliver(r, v);
+            }
           }
         }
       }
+      if (p.split > 1 && met == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
   } else {
     // ---------------------------------------------------------------- kGrad: rows behind the end of a run are set to zero, once they are there
@@ -1017,8 +1079,17 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
     }
   }
   __syncwarp();
-  if (!P && p.split > 1)
+  if (FORM == kFew) {
+    if (p.split > 1) {
+      if (warp < 2) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+      if (*abort_flag) {                         // parts may still be on their way here: until the other CTAs are done too, or 20 ms
+        const unsigned long long t0 = globaltimer_ns();
+        while (globaltimer_ns() - t0 < 20ull * 1000ull * 1000ull) __nanosleep(1000);
+      }
+    }
+  } else if (!P && p.split > 1) {
     for (; met < 2; ++met) cluster_sync();       // the parts are there; and read
+  }
   if (warp == 1 && *abort_flag) {                // copies and products may still be in flight: give them time to end
     const unsigned long long t0 = globaltimer_ns();
     while (globaltimer_ns() - t0 < 20ull * 1000ull * 1000ull) __nanosleep(1000);
@@ -1084,74 +1155,55 @@ __global__ void __launch_bounds__(256) k_group_rows_of(const __grid_constant__ C
   }
 }
 
-// What rows keep of their adapters where runs are short: a warp to two numbers of a row, the adapter's rows read straight through.
+// What rows keep of their adapters where runs are short: a warp to a number of a row, the adapter's row read straight through.
 // The next launch starts only behind the wait for the one before this: what that one wrote is there for it.
 template <typename T>
 __global__ void __launch_bounds__(256) k_adapter_narrow(const T *__restrict__ x, int x_pitch, const T *__restrict__ a, int a_pitch, int k, int rank,
                                                         const __grid_constant__ Runs runs, const float *__restrict__ scale, bf16 *__restrict__ t) {
-  constexpr int kPer = 16 / (int)sizeof(T);
-  __shared__ int weight_s;
+  constexpr int kPer = 16 / (int)sizeof(T), kAhead = 8, kStep = 32 * kPer;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int row = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-  if (warp == 0) {
-    int w = -1;
-    each_run(runs, row, row + 1, [&](int begin, int end, int weight) { if (begin <= row && row < end) w = weight; });
-    if (lane == 0) weight_s = w;
-  }
-  __syncthreads();
-  const int w = weight_s;
+  const int row = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, j = (int)blockIdx.y * 8 + warp, pad = grp::rank_pad(rank);
+  const T *xr = x + (size_t)row * (size_t)x_pitch;
+  uint4 xv[kAhead], av[kAhead];
+  auto ask = [&](const T *from, uint4 (&to)[kAhead], int i0) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) to[u] = i0 + u * kStep < k ? *reinterpret_cast<const uint4 *>(from + i0 + u * kStep) : make_uint4(0, 0, 0, 0);
+  };
+  ask(xr, xv, lane * kPer);                      // while the run is looked for
+  int w = -1;
+  each_run(runs, row, row + 1, [&](int begin, int end, int weight) { if (begin <= row && row < end) w = weight; });
   if (w < 0) return;
-  const int j = (int)blockIdx.y * 16 + warp * 2, pad = grp::rank_pad(rank);
-  float s[2] = {0.f, 0.f};
-  const T *xr = x + (size_t)row * (size_t)x_pitch, *ar = a + ((size_t)w * (size_t)rank + (size_t)j) * (size_t)a_pitch;
-  const bool two = j + 1 < rank;
+  float s = 0.f;
   if (j < rank) {
-    constexpr int kAhead = 4;
-    for (int i0 = lane * kPer; i0 < k; i0 += kAhead * 32 * kPer) {
-      uint4 v[3][kAhead];
+    const T *ar = a + ((size_t)w * (size_t)rank + (size_t)j) * (size_t)a_pitch;
+    for (int i0 = lane * kPer; i0 < k; i0 += kAhead * kStep) {
+      ask(ar, av, i0);
+      if (i0 >= kAhead * kStep) ask(xr, xv, i0);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int i = i0 + u * 32 * kPer;
-        v[0][u] = v[1][u] = v[2][u] = make_uint4(0, 0, 0, 0);
-        if (i < k) {
-          v[0][u] = *reinterpret_cast<const uint4 *>(xr + i);
-          v[1][u] = *reinterpret_cast<const uint4 *>(ar + i);
-          if (two) v[2][u] = *reinterpret_cast<const uint4 *>(ar + (size_t)a_pitch + i);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        float f[3][8];
-#pragma unroll
-        for (int y = 0; y < 3; ++y) {
-          if (sizeof(T) == 2) unpack8(v[y][u], f[y]);
-          else {
-            f[y][0] = __uint_as_float(v[y][u].x); f[y][1] = __uint_as_float(v[y][u].y);
-            f[y][2] = __uint_as_float(v[y][u].z); f[y][3] = __uint_as_float(v[y][u].w);
-          }
+        float f[2][8];
+        if (sizeof(T) == 2) {
+          unpack8(xv[u], f[0]);
+          unpack8(av[u], f[1]);
+        } else {
+          f[0][0] = __uint_as_float(xv[u].x); f[0][1] = __uint_as_float(xv[u].y); f[0][2] = __uint_as_float(xv[u].z); f[0][3] = __uint_as_float(xv[u].w);
+          f[1][0] = __uint_as_float(av[u].x); f[1][1] = __uint_as_float(av[u].y); f[1][2] = __uint_as_float(av[u].z); f[1][3] = __uint_as_float(av[u].w);
         }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) { s[0] = fmaf(f[0][i], f[1][i], s[0]); s[1] = fmaf(f[0][i], f[2][i], s[1]); }
+        for (int i = 0; i < kPer; ++i) s = fmaf(f[0][i], f[1][i], s);
       }
     }
   }
 #pragma unroll
-  for (int d = 16; d; d >>= 1) {
-    s[0] += __shfl_xor_sync(0xffffffffu, s[0], d);
-    s[1] += __shfl_xor_sync(0xffffffffu, s[1], d);
-  }
-  if (lane == 0) {
+  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  if (lane == 0 && j < pad) {
     constexpr int kKept = sizeof(T) == 4 ? 3 : 2;
-    const float f = scale ? __ldg(scale + w) : 1.f;
+    float term[3];
+    terms_of<T>(j < rank ? s * (scale ? __ldg(scale + w) : 1.f) : 0.f, term);
     bf16 *to = t + (size_t)row * (size_t)(kKept * pad) + (size_t)j;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float term[3];
-      terms_of<T>(j + i < rank ? s[i] * f : 0.f, term);
-#pragma unroll
-      for (int y = 0; y < kKept; ++y) to[y * pad + i] = __float2bfloat16(term[y]);
-    }
+    for (int y = 0; y < kKept; ++y) to[y * pad] = __float2bfloat16(term[y]);
   }
 }
 
@@ -1213,18 +1265,20 @@ int split_of(long long items, int pieces, int least, int n_sm) {
   if (s > pieces / least) s = pieces / least;
   return s < 1 ? 1 : s;
 }
-// Columns to a tile, and whether CTAs work in pairs: the fewest rounds of tiles, each as long as its loads take (an SM takes in some 45 bytes a cycle; of
-// 64 terms of 128 x 256 that is 48 KB, of a pair's half tile 32).
+// Columns to a tile, and whether CTAs work in pairs, by an estimate in cycles: a piece of 64 terms takes its loads (an SM takes in some 45 bytes a cycle) or its
+// instructions, results go out beside the next tile's pieces, and of the last tile behind them.
 struct Shape { int nt; bool pair; };
-Shape shape_of(int n, double rows, double runs, bool wide, int n_sm) {
-  static constexpr struct { int nt; bool pair; double cost; } kinds[4] = {{256, true, 0.72}, {256, false, 1.0}, {128, false, 0.62}, {64, false, 0.45}};
+Shape shape_of(int n, double rows, double runs, double pieces, bool wide, int n_sm) {
+  static constexpr Shape kinds[4] = {{256, true}, {256, false}, {128, false}, {64, false}};
   Shape best = {64, false};
   double least = 1e30;
-  for (const auto &k : kinds) {
+  for (const Shape &k : kinds) {
     if ((wide && k.nt > 128) || (k.nt > 64 && n <= k.nt / 2)) continue;
     const double tiles = (rows / (k.pair ? 256 : 128) + 0.5 * runs) * dc_div_up(n, k.nt), rounds = tiles / (k.pair ? n_sm / 2 : n_sm);
-    const double time = (rounds < 1 ? 1 : rounds + 0.4) * k.cost;
-    if (time < least) { least = time; best = {k.nt, k.pair}; }
+    const double bytes = (128 + (k.pair ? 128 : k.nt)) * 128.0 * (wide ? 3 : 1), sums = k.nt * 2.0 * (wide ? 6 : 1);
+    const double main = pieces * (bytes / 45 > sums ? bytes / 45 : sums), out = 400 + k.nt * 10.0;
+    const double time = (rounds < 1 ? 1 : rounds + 0.4) * (main > out ? main : out) + (main > out ? out : main) + (k.pair ? 800 : 0);
+    if (time < least) { least = time; best = k; }
   }
   return best;
 }
@@ -1261,7 +1315,7 @@ bool narrow_apart(const RowsJob &j) {
   return j.y_terms && !j.w_across && j.rows <= 1024 && j.rows / runs_with_rows(j.runs) <= 8 && (j.dtype == DC_BF16 || j.k % 4 == 0);
 }
 cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st) {
-  const dim3 grid((unsigned)j.rows, (unsigned)dc_div_up(rank_pad(j.n), 16));
+  const dim3 grid((unsigned)j.rows, (unsigned)(rank_pad(j.n) / 8));
   if (j.dtype == DC_BF16)
     return dc_launch_pdl(k_adapter_narrow<bf16>, grid, dim3(256), 0, st, (const bf16 *)j.x, j.x_pitch, (const bf16 *)j.w, j.w_pitch, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
   return dc_launch_pdl(k_adapter_narrow<float>, grid, dim3(256), 0, st, (const float *)j.raw_x, j.k, (const float *)j.raw_w, j.k, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
@@ -1304,17 +1358,18 @@ cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaSt
   if (by_few) {
     const int mean = j.rows / runs;
     p.nt = mean <= (runs == 1 ? 16 : 12) ? 16 : mean <= (runs == 1 ? 32 : 24) ? 32 : 64;
+    if (wide && p.nt > kFewWide) p.nt = kFewWide;
     p.q_bytes = p.nt * 128;
     p.tiles_n = dc_div_up(j.n, 128);
     items = row_tiles(j.runs, p.nt) * p.tiles_n;
     p.split = split_of(items, p.pieces, 4, n_sm);
     p.early = behind_narrow && !j.runs.offsets;
-    lay_out(&p, terms, p.rank ? p.nt * rank_pad(p.rank) * 4 : 0);
+    lay_out(&p, terms, (p.rank ? p.nt * (rank_pad(p.rank) * 4 + 512) : 0) + (p.split > 1 ? (p.nt + p.split) * 512 : 0));
   } else {
     if (j.y_terms) {
       p.nt = rank_pad(j.n);
     } else {
-      const Shape s = shape_of(j.n, j.rows, runs, wide, n_sm);
+      const Shape s = shape_of(j.n, j.rows, runs, p.pieces + (j.t ? 2 : 0), wide, n_sm);
       p.nt = s.nt;
       pair = s.pair;
     }
@@ -1378,7 +1433,7 @@ cudaError_t grad_tc(const GradJob &j, DcWsHeader *ws, cudaStream_t st) {
   } else if (j.q_terms) {
     p.nt = wide ? pad : 2 * pad;
   } else {
-    const Shape s = shape_of(j.n, (double)j.m * weights, 0, wide, n_sm);
+    const Shape s = shape_of(j.n, (double)j.m * weights, 0, (double)j.runs.rows / kPiece / weights + 0.5, wide, n_sm);
     p.nt = s.nt;
     pair = s.pair && j.m > 128;
   }

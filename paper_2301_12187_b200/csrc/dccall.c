@@ -1,4 +1,4 @@
-/* The forward calls of dc.py, and those on 4-bit matrices, without ctypes: arguments are read from the Python objects here and the C entry point is
+/* The forward calls of dc.py, those on 4-bit matrices and those of grouped rows and adapters, without ctypes: arguments are read from the Python objects here and the C entry point is
  * called through its address.  A small layer runs for 3-6 us, and marshalling its call through ctypes took 3.7 us of the host
  * (16 converted arguments, six pointers and the current stream fetched from Python); here about 1.
  *
@@ -18,6 +18,15 @@ typedef int (*q4_product_fn)(const void *, long long, int, const void *, int, in
 typedef int (*q4_forward_fn)(const void *, long long, int, const void *, int, int, float, float, const void *, int, const void *, void *, int, void *,
                              size_t, void *);
 typedef int (*q4_query_fn)(long long, int, int, size_t *);
+typedef int (*group_forward_fn)(const void *, long long, int, const void *, int, const void *, int, const void *, int, void *, int, void *, size_t, void *);
+typedef int (*group_backward_fn)(const void *, const void *, long long, int, const void *, int, const void *, int, void *, void *, void *, int, void *, size_t,
+                                 void *);
+typedef struct { int count, rank; const void *a, *b, *scale; } adapters;          /* dc_adapters */
+typedef int (*adapter_forward_fn)(const void *, long long, int, const void *, int, const adapters *, const void *, const void *, int, const void *, int,
+                                  const void *, void *, void *, int, void *, size_t, void *);
+typedef int (*adapter_backward_fn)(const void *, const void *, long long, int, const void *, int, const adapters *, const void *, const void *, int,
+                                   const void *, void *, void *, void *, int, void *, size_t, void *);
+typedef int (*saved_bytes_fn)(long long, int, int, size_t *);
 typedef int (*block_fn)(const void *, int, int, int, const void *, void *, int, void *, size_t, void *);
 
 static conv_fn g_conv;
@@ -28,6 +37,12 @@ static q4_dequantize_fn g_q4_dequantize;
 static q4_product_fn g_q4_product;
 static q4_forward_fn g_q4_forward;
 static q4_query_fn g_q4_query;
+static group_forward_fn g_group_forward;
+static group_backward_fn g_group_backward;
+static adapter_forward_fn g_adapter_forward;
+static adapter_backward_fn g_adapter_backward;
+static saved_bytes_fn g_saved_bytes;
+static PyObject *g_i32, *s_a, *s_b, *s_scale;
 static PyObject *g_f32, *g_bf16, *g_geom, *g_block_type, *g_get_device, *g_get_stream;
 static PyObject *s_data_ptr, *s_shape, *s_dtype, *s_numel, *s_element_size, *s_cuda_stream;
 static PyObject *s_stride, *s_is_contiguous, *s_get_device, *s_rows, *s_cols, *s_fmt, *s_tensor_scale, *s_data, *s_nbytes;
@@ -330,6 +345,168 @@ static PyObject *bind_q4(PyObject *self, PyObject *args) {
   Py_RETURN_NONE;
 }
 
+/* ---- rows with weights of their own: what dc.py checks of their tensors, as above */
+/* a dense tensor of exactly these `n` dimensions and this dtype code (-1: any; *code is then its own); None passes where `may_lack` */
+static int read_shaped(PyObject *t, long long dev, const long long *dims, int n, int code, int may_lack, void **p) {
+  int c;
+  *p = NULL;
+  if (t == Py_None) return may_lack ? 0 : -1;
+  if (read_dtype(t, &c) || c != code) return -1;
+  PyObject *sh = PyObject_GetAttr(t, s_shape);
+  int bad = !sh || !PyTuple_Check(sh) || PyTuple_GET_SIZE(sh) != n;
+  for (int i = 0; i < n && !bad; ++i) bad = PyLong_AsLongLong(PyTuple_GET_ITEM(sh, i)) != dims[i];
+  Py_XDECREF(sh);
+  if (bad) return -1;
+  PyObject *dense = PyObject_CallMethodNoArgs(t, s_is_contiguous);
+  bad = dense != Py_True;
+  Py_XDECREF(dense);
+  return bad || read_here(t, dev, p) ? -1 : 0;
+}
+static int read_dims(PyObject *t, long long *dims, int n) {
+  PyObject *sh = PyObject_GetAttr(t, s_shape);
+  int bad = !sh || !PyTuple_Check(sh) || PyTuple_GET_SIZE(sh) != n;
+  for (int i = 0; i < n && !bad; ++i) {
+    dims[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(sh, i));
+    bad = dims[i] < 1 || dims[i] > 2147483647LL;
+  }
+  Py_XDECREF(sh);
+  return bad ? -1 : 0;
+}
+/* an array of 32-bit integers: *n of them, or any number where that is -1 */
+static int read_numbers(PyObject *t, long long dev, long long *n, void **p) {
+  PyObject *d = PyObject_GetAttr(t, s_dtype), *sh;
+  Py_XDECREF(d);
+  if (!d || d != g_i32) return -1;
+  sh = PyObject_GetAttr(t, s_shape);
+  int bad = !sh || !PyTuple_Check(sh) || PyTuple_GET_SIZE(sh) != 1;
+  const long long have = bad ? 0 : PyLong_AsLongLong(PyTuple_GET_ITEM(sh, 0));
+  Py_XDECREF(sh);
+  if (bad || have > 2147483647LL || (*n >= 0 && have != *n)) return -1;
+  *n = have;
+  PyObject *dense = PyObject_CallMethodNoArgs(t, s_is_contiguous);
+  bad = dense != Py_True;
+  Py_XDECREF(dense);
+  return bad || read_here(t, dev, p) ? -1 : 0;
+}
+static int read_workspace(PyObject *t, long long dev, void **p, size_t *bytes) { return t == Py_None || read_here(t, dev, p) || read_bytes(t, bytes) ? -1 : 0; }
+
+/* group_forward(x, offsets, w, bias, act, y, workspace, stream) */
+static PyObject *group_forward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  int act, code, st;
+  long long dev, rows = -1, d[3], count;
+  void *x, *off, *w, *b, *y, *ws, *stream;
+  size_t bytes;
+  if (n != 8 || !g_group_forward || current_device(&dev) || read_dims(a[2], d, 3) || read_dtype(a[0], &code) || read_dense(a[0], dev, &rows, d[2], code, 0, &x) ||
+      (count = d[0] + 1, read_numbers(a[1], dev, &count, &off)) || read_shaped(a[2], dev, d, 3, code, 0, &w) || read_shaped(a[3], dev, d, 2, 0, 1, &b) ||
+      read_int(a[4], &act) || read_dense(a[5], dev, &rows, d[1], code, 0, &y) || read_workspace(a[6], dev, &ws, &bytes) || read_stream(a[7], &stream))
+    return other_form();
+  Py_BEGIN_ALLOW_THREADS
+  st = g_group_forward(x, rows, (int)d[2], off, (int)d[0], w, (int)d[1], b, act, y, code, ws, bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+/* group_backward(dy, x, offsets, w, dx, dw, db, workspace, stream) */
+static PyObject *group_backward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  int code, st;
+  long long dev, rows = -1, d[3], count;
+  void *dy, *x, *off, *w, *dx, *dw, *db, *ws, *stream;
+  size_t bytes;
+  if (n != 9 || !g_group_backward || current_device(&dev) || read_dims(a[3], d, 3) || read_dtype(a[0], &code) || read_dense(a[0], dev, &rows, d[1], code, 0, &dy) ||
+      read_dense(a[1], dev, &rows, d[2], code, 1, &x) || (count = d[0] + 1, read_numbers(a[2], dev, &count, &off)) || read_shaped(a[3], dev, d, 3, code, 0, &w) ||
+      read_dense(a[4], dev, &rows, d[2], code, 1, &dx) || read_shaped(a[5], dev, d, 3, code, 1, &dw) || read_shaped(a[6], dev, d, 2, 0, 1, &db) ||
+      read_workspace(a[7], dev, &ws, &bytes) || read_stream(a[8], &stream))
+    return other_form();
+  Py_BEGIN_ALLOW_THREADS
+  st = g_group_backward(dy, x, rows, (int)d[2], off, (int)d[0], w, (int)d[1], dx, dw, db, code, ws, bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+/* an Adapters object of this dtype, and [count, rank, c_in, c_out] */
+static int read_adapters(PyObject *o, long long dev, int code, adapters *out, long long *d) {
+  PyObject *a = PyObject_GetAttr(o, s_a), *b = PyObject_GetAttr(o, s_b), *f = PyObject_GetAttr(o, s_scale);
+  long long db[3];
+  void *p[3];
+  int bad = !a || !b || !f || read_dims(a, d, 3) || read_dims(b, db, 3) || db[0] != d[0] || db[2] != d[1] || read_shaped(a, dev, d, 3, code, 0, &p[0]) ||
+            read_shaped(b, dev, db, 3, code, 0, &p[1]) || read_shaped(f, dev, d, 1, 0, 1, &p[2]);
+  Py_XDECREF(a);
+  Py_XDECREF(b);
+  Py_XDECREF(f);
+  if (bad) return -1;
+  d[3] = db[1];
+  out->count = (int)d[0];
+  out->rank = (int)d[1];
+  out->a = p[0];
+  out->b = p[1];
+  out->scale = p[2];
+  return 0;
+}
+/* the buffer that a forward call leaves for the backward one */
+static int read_saved(PyObject *t, long long dev, long long rows, int rank, int code, int may_lack, void **p) {
+  size_t need, have;
+  *p = NULL;
+  if (t == Py_None) return may_lack ? 0 : -1;
+  if (g_saved_bytes(rows, rank, code, &need) || read_bytes(t, &have) || have < need) return -1;
+  PyObject *dense = PyObject_CallMethodNoArgs(t, s_is_contiguous);
+  const int bad = dense != Py_True;
+  Py_XDECREF(dense);
+  return bad || read_here(t, dev, p) ? -1 : 0;
+}
+/* adapter_forward(x, w, adapters, offsets, which, bias, act, residual, saved, y, workspace, stream) */
+static PyObject *adapter_forward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  int act, code, st;
+  long long dev, rows = -1, d[4], wd[2], runs = -1, count;
+  void *x, *w, *off, *which, *b, *r, *saved, *y, *ws, *stream;
+  adapters ad;
+  size_t bytes;
+  if (n != 12 || !g_adapter_forward || current_device(&dev) || read_dtype(a[0], &code) || read_adapters(a[2], dev, code, &ad, d) ||
+      (wd[0] = d[3], wd[1] = d[2], read_shaped(a[1], dev, wd, 2, code, 1, &w)) || read_dense(a[0], dev, &rows, d[2], code, 0, &x) ||
+      read_numbers(a[4], dev, &runs, &which) || (count = runs + 1, read_numbers(a[3], dev, &count, &off)) || read_bias(a[5], dev, d[3], &b) || read_int(a[6], &act) ||
+      read_dense(a[7], dev, &rows, d[3], code, 1, &r) || read_saved(a[8], dev, rows, ad.rank, code, 0, &saved) || read_dense(a[9], dev, &rows, d[3], code, 0, &y) ||
+      read_workspace(a[10], dev, &ws, &bytes) || read_stream(a[11], &stream))
+    return other_form();
+  Py_BEGIN_ALLOW_THREADS
+  st = g_adapter_forward(x, rows, (int)d[2], w, (int)d[3], &ad, off, which, (int)runs, b, act, r, saved, y, code, ws, bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+/* adapter_backward(dy, x, w, adapters, offsets, which, saved, dx, da, db, workspace, stream) */
+static PyObject *adapter_backward(PyObject *self, PyObject *const *a, Py_ssize_t n) {
+  (void)self;
+  int code, st;
+  long long dev, rows = -1, d[4], wd[3], runs = -1, count;
+  void *dy, *x, *w, *off, *which, *saved, *dx, *da, *db, *ws, *stream;
+  adapters ad;
+  size_t bytes;
+  if (n != 12 || !g_adapter_backward || current_device(&dev) || read_dtype(a[0], &code) || read_adapters(a[3], dev, code, &ad, d) ||
+      (wd[0] = d[3], wd[1] = d[2], read_shaped(a[2], dev, wd, 2, code, 1, &w)) || read_dense(a[0], dev, &rows, d[3], code, 0, &dy) ||
+      read_dense(a[1], dev, &rows, d[2], code, 1, &x) || read_numbers(a[5], dev, &runs, &which) || (count = runs + 1, read_numbers(a[4], dev, &count, &off)) ||
+      read_saved(a[6], dev, rows, ad.rank, code, 1, &saved) || read_dense(a[7], dev, &rows, d[2], code, 1, &dx) || read_shaped(a[8], dev, d, 3, code, 1, &da) ||
+      (wd[0] = d[0], wd[1] = d[3], wd[2] = d[1], read_shaped(a[9], dev, wd, 3, code, 1, &db)) || read_workspace(a[10], dev, &ws, &bytes) || read_stream(a[11], &stream))
+    return other_form();
+  Py_BEGIN_ALLOW_THREADS
+  st = g_adapter_backward(dy, x, rows, (int)d[2], w, (int)d[3], &ad, off, which, (int)runs, saved, dx, da, db, code, ws, bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(st);
+}
+/* bind_group(addresses of group forward and backward, adapter forward and backward, saved bytes; int32) */
+static PyObject *bind_group(PyObject *self, PyObject *args) {
+  unsigned long long f, b, af, ab, s;
+  PyObject *i32;
+  (void)self;
+  if (!PyArg_ParseTuple(args, "KKKKKO", &f, &b, &af, &ab, &s, &i32)) return NULL;
+  Py_INCREF(i32);
+  g_i32 = i32;
+  g_group_forward = (group_forward_fn)(uintptr_t)f;
+  g_group_backward = (group_backward_fn)(uintptr_t)b;
+  g_adapter_forward = (adapter_forward_fn)(uintptr_t)af;
+  g_adapter_backward = (adapter_backward_fn)(uintptr_t)ab;
+  g_saved_bytes = (saved_bytes_fn)(uintptr_t)s;
+  Py_RETURN_NONE;
+}
+
 /* bind(conv address, dwconv address, block address, float32, bfloat16, Geom, Block, current device, current raw stream) */
 static PyObject *bind(PyObject *self, PyObject *args) {
   unsigned long long c, w, b;
@@ -351,7 +528,12 @@ static PyMethodDef methods[] = {{"conv", (PyCFunction)(void (*)(void))conv, METH
                                 {"q4_dequantize", (PyCFunction)(void (*)(void))q4_dequantize, METH_FASTCALL, NULL},
                                 {"q4_product", (PyCFunction)(void (*)(void))q4_product, METH_FASTCALL, NULL},
                                 {"q4_forward", (PyCFunction)(void (*)(void))q4_forward, METH_FASTCALL, NULL},
+                                {"group_forward", (PyCFunction)(void (*)(void))group_forward, METH_FASTCALL, NULL},
+                                {"group_backward", (PyCFunction)(void (*)(void))group_backward, METH_FASTCALL, NULL},
+                                {"adapter_forward", (PyCFunction)(void (*)(void))adapter_forward, METH_FASTCALL, NULL},
+                                {"adapter_backward", (PyCFunction)(void (*)(void))adapter_backward, METH_FASTCALL, NULL},
                                 {"bind", bind, METH_VARARGS, NULL},
+                                {"bind_group", bind_group, METH_VARARGS, NULL},
                                 {"bind_q4", bind_q4, METH_VARARGS, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dccall", NULL, -1, methods, NULL, NULL, NULL, NULL};
@@ -372,6 +554,10 @@ PyMODINIT_FUNC PyInit__dccall(void) {
   s_tensor_scale = PyUnicode_InternFromString("tensor_scale");
   s_data = PyUnicode_InternFromString("data");
   s_nbytes = PyUnicode_InternFromString("nbytes");
+  s_a = PyUnicode_InternFromString("a");
+  s_b = PyUnicode_InternFromString("b");
+  s_scale = PyUnicode_InternFromString("scale");
+  if (!s_a || !s_b || !s_scale) return NULL;
   if (!s_stride || !s_is_contiguous || !s_get_device || !s_rows || !s_cols || !s_fmt || !s_tensor_scale || !s_data || !s_nbytes) return NULL;
   if (!s_data_ptr || !s_shape || !s_dtype || !s_numel || !s_element_size || !s_cuda_stream) return NULL;
   return PyModule_Create(&module);

@@ -43,7 +43,8 @@ struct Parts {
     return at;
   }
   bool apart(int cols) const { return dtype == DC_F32 || cols % 8 != 0; }
-  int pitch(int cols) const { return (int)dc_round_up((size_t)cols, 8); }
+  // whole lines of 128 bytes, which is what a load takes of a row
+  int pitch(int cols) const { return apart(cols) ? (int)dc_round_up((size_t)cols, 64) : cols; }
   void *room(long long rows, int cols) { return add((size_t)rows * (size_t)pitch(cols) * (dtype == DC_BF16 ? 2 : 6)); }
   void reserve(long long rows, int cols) {
     if (apart(cols)) room(rows, cols);

@@ -8,8 +8,8 @@
 //   kTile   128 rows of a run x up to 256 columns of its matrix.
 //   kFew    runs of few rows: 128 columns of the matrix take the place of the 128 rows, so that an instruction is as wide as there are rows and
 //           the matrix streams through once.
-//   kGrad   128 x up to 256 of a gradient: the sum runs over the rows of a weight's runs.  The last piece of a run holds rows of the next one, which a warp
-//           sets to zero in both operands (0 times a NaN is a NaN).
+//   kGrad   128 x up to 256 of a gradient: the sum runs over the rows of a weight's runs.  The last piece of a run holds rows of the next one: those that its last
+//           instruction takes are set to zero by a warp, in both operands (0 times a NaN is a NaN).
 // kTile and kGrad in pairs (cta_group::2): two CTAs multiply 256 x 256, each loads half of either operand.
 // Few tiles: a cluster shares a tile's sum, and adds up its parts through its shared memory.
 // Adapters (kTile): each run's part is added to the same accumulator by instructions that leave the lanes of other rows alone, so that an
@@ -329,12 +329,13 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
     const int piece = lane & 7, r0 = lane >> 3;
     if (piece * 4 >= cols) return;
     const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias) + piece) : make_float4(0.f, 0.f, 0.f, 0.f);
+    uint4 w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = i * 4 + r0;
-      if (row >= rows) break;
-      const uint4 w = lds_u4(stage + (uint32_t)(row * 128 + ((piece ^ (row & 7)) * 16)));
-      float f[4] = {__uint_as_float(w.x) + b.x, __uint_as_float(w.y) + b.y, __uint_as_float(w.z) + b.z, __uint_as_float(w.w) + b.w};
+    for (int i = 0; i < 8; ++i) w[i] = lds_u4(stage + (uint32_t)((i * 4 + r0) * 128 + ((piece ^ ((i * 4 + r0) & 7)) * 16)));
+    T *at = y + (size_t)r0 * pitch + (size_t)(piece * 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i, at += 4 * pitch) {
+      float f[4] = {__uint_as_float(w[i].x) + b.x, __uint_as_float(w[i].y) + b.y, __uint_as_float(w[i].z) + b.z, __uint_as_float(w[i].w) + b.w};
       if (ahead) {
         if (sizeof(T) == 4) {
           const uint4 u = ahead->v[sizeof(T) == 4 ? i : 0];
@@ -348,21 +349,29 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
       }
 #pragma unroll
       for (int x = 0; x < 4; ++x) f[x] = dc_act_apply(f[x], p.act);
-      T *at = y + (size_t)row * pitch + (size_t)(piece * 4);
-      if (sizeof(T) == 4) *reinterpret_cast<float4 *>(at) = make_float4(f[0], f[1], f[2], f[3]);
-      else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+      if (i * 4 + r0 < rows) {
+        if (sizeof(T) == 4) *reinterpret_cast<float4 *>(at) = make_float4(f[0], f[1], f[2], f[3]);
+        else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+      }
     }
     return;
   }
   if (lane >= cols) return;
   const float b = bias ? __ldg(bias + lane) : 0.f;
-#pragma unroll 8
-  for (int row = 0; row < 32; ++row) {
-    if (row >= rows) break;
-    float f = lds_f(stage + (uint32_t)(row * 128 + (((lane >> 2) ^ (row & 7)) * 16) + (lane & 3) * 4)) + b;
-    const size_t at = (size_t)row * pitch + (size_t)lane;
-    if (residual) f += to_float(residual[at]);
-    y[at] = (T)dc_act_apply(f, p.act);
+#pragma unroll 1
+  for (int i0 = 0; i0 < rows; i0 += 8) {         // eight rows at once, so that what one waits for the others do not add to
+    float f[8], r[8];
+    const size_t at = (size_t)i0 * pitch + (size_t)lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      f[i] = lds_f(stage + (uint32_t)((i0 + i) * 128 + (((lane >> 2) ^ i) * 16) + (lane & 3) * 4));
+      r[i] = residual && i0 + i < rows ? to_float(residual[at + (size_t)i * pitch]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = dc_act_apply(f[i] + b + r[i], p.act);
+      if (i0 + i < rows) y[at + (size_t)i * pitch] = (T)v;
+    }
   }
 }
 
@@ -545,7 +554,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
                 any = false;
               }
               if (ok) ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x40000u | (uint32_t)stage, kLimit);
-              if (ok && rows < kPiece) {         // rows of the next run
+              if (ok && rows % 16) {             // the last instruction's terms include rows of the next run
                 if (P) arrive_cluster(map_cluster(smem_u32(&bar[kAsk]), 1));
                 mbar_arrive(&bar[kAsk]);
                 ok = mbar_wait(&bar[kFixed], fixed & 1u, abort_flag, ws, 0x50000u | (uint32_t)stage);
@@ -889,7 +898,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         }
       }
     } else {
-      if (p.early) asm volatile("griddepcontrol.wait;" ::: "memory");
+      bool waited = !p.early;                    // for the launch in front of this one
       grp::Walk walk;
       walk.start();
       Tile t;
@@ -906,60 +915,90 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           const int pad = grp::rank_pad(p.rank);
           bar_sync(1, kEpi * 32);                // the last item's are read
           if (unit < p.nt) weight_s[unit] = unit < count ? adapter_of(p.ext, t.row0 + unit) : -1;
+          bar_sync(1, kEpi * 32);
+          auto matrix_of = [&](int w) {
+            return reinterpret_cast<const T *>(p.e) + (ACROSS ? (size_t)w * (size_t)p.rank * (size_t)p.e_pitch + (size_t)o : ((size_t)w * (size_t)p.n + (size_t)o) * (size_t)p.e_pitch);
+          };
+          if (!ACROSS && !waited && o < p.n) {   // on their way from memory while the launch in front ends
+#pragma unroll 1
+            for (int v0 = 0; v0 < here; ++v0) {
+              const int w = weight_s[row_of(v0)];
+              if (w < 0) continue;
+              for (int j0 = 0; j0 < p.rank; j0 += 128 / (int)sizeof(T)) asm volatile("prefetch.global.L2 [%0];" ::"l"(matrix_of(w) + j0));
+            }
+          }
+          if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+          waited = true;
 #pragma unroll 1
           for (int i = unit; i < count * pad; i += kEpi * 32) {
             const int r = i / pad;
             sts_f(ts + (uint32_t)(i * 4), kept<T>(p.t, t.row0 + r, pad, i - r * pad));
           }
           bar_sync(1, kEpi * 32);
-          constexpr int kAtOnce = 4;             // rows, for as many loads on their way
+          constexpr int kAtOnce = sizeof(T) == 2 && !ACROSS ? 8 : 4;         // rows, for as many loads on their way
 #pragma unroll 1
           for (int v0 = 0; v0 < here; v0 += kAtOnce) {
             int w[kAtOnce], r[kAtOnce];
             float sum[kAtOnce];
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i) {
-              r[i] = row_of(v0 + i);
-              w[i] = v0 + i < here && o < p.n ? weight_s[r[i]] : -1;
+              w[i] = v0 + i < here && o < p.n ? weight_s[row_of(v0 + i)] : -1;
+              r[i] = w[i] >= 0 ? row_of(v0 + i) : 0;
               sum[i] = 0.f;
             }
-#pragma unroll 2
-            for (int j0 = 0; j0 < p.rank; j0 += 8) {
-              float e[kAtOnce][8];
+            // numbers j0 to j0 + 7 of the rank.  Rows without an adapter are not multiplied: t may be no number there.
+            auto add = [&](int i, int j0, const float *e) {
+              const uint32_t at = ts + (uint32_t)((r[i] * pad + j0) * 4);
+              const uint4 t0 = lds_u4(at), t1 = lds_u4(at + 16);
+              const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
-              for (int i = 0; i < kAtOnce; ++i) {
-                const T *at = reinterpret_cast<const T *>(p.e) + (ACROSS ? ((size_t)max(w[i], 0) * (size_t)p.rank + (size_t)j0) * (size_t)p.e_pitch + (size_t)o
-                                                                         : ((size_t)max(w[i], 0) * (size_t)p.n + (size_t)o) * (size_t)p.e_pitch + (size_t)j0);
-                if (ACROSS || (sizeof(T) == 4 && !p.e_vec)) {
+              for (int x = 0; x < 8; ++x)
+                if (w[i] >= 0) sum[i] = fmaf(__uint_as_float(tv[x]), e[x], sum[i]);
+            };
+            if (sizeof(T) == 2 && !ACROSS) {
+#pragma unroll 1
+              for (int j0 = 0; j0 < p.rank; j0 += 16) {
+                uint4 raw[kAtOnce][2];
 #pragma unroll
-                  for (int x = 0; x < 8; ++x) e[i][x] = w[i] >= 0 && j0 + x < p.rank ? to_float(at[(size_t)x * (size_t)(ACROSS ? p.e_pitch : 1)]) : 0.f;
-                } else if (sizeof(T) == 2) {
-                  uint4 raw = make_uint4(0, 0, 0, 0);
-                  if (w[i] >= 0) raw = __ldg(reinterpret_cast<const uint4 *>(at));
-                  unpack8(raw, e[i]);
-                } else {
+                for (int i = 0; i < kAtOnce; ++i)
 #pragma unroll
-                  for (int x = 0; x < 8; x += 4) {
-                    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (w[i] >= 0 && j0 + x < p.rank) f = __ldg(reinterpret_cast<const float4 *>(at + x));
-                    e[i][x] = f.x; e[i][x + 1] = f.y; e[i][x + 2] = f.z; e[i][x + 3] = f.w;
+                  for (int h = 0; h < 2; ++h)
+                    raw[i][h] = w[i] >= 0 && j0 + 8 * h < p.rank ? __ldg(reinterpret_cast<const uint4 *>(matrix_of(w[i]) + j0 + 8 * h)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+                  for (int h = 0; h < 2; ++h) {
+                    float e[8];
+                    unpack8(raw[i][h], e);
+                    add(i, j0 + 8 * h, e);       // (the rank's padding is a multiple of 16: t is 0 there)
+                  }
+              }
+            } else {
+#pragma unroll 1
+              for (int j0 = 0; j0 < p.rank; j0 += 8) {
+                float e[kAtOnce][8];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) {
+                  const T *at = matrix_of(max(w[i], 0)) + (ACROSS ? (size_t)j0 * (size_t)p.e_pitch : (size_t)j0);
+                  if (sizeof(T) == 4 && !ACROSS && p.e_vec) {
+#pragma unroll
+                    for (int x = 0; x < 8; x += 4) {
+                      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+                      if (w[i] >= 0 && j0 + x < p.rank) f = __ldg(reinterpret_cast<const float4 *>(at + x));
+                      e[i][x] = f.x; e[i][x + 1] = f.y; e[i][x + 2] = f.z; e[i][x + 3] = f.w;
+                    }
+                  } else {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) e[i][x] = w[i] >= 0 && j0 + x < p.rank ? to_float(at[(size_t)x * (size_t)(ACROSS ? p.e_pitch : 1)]) : 0.f;
                   }
                 }
-              }
 #pragma unroll
-              for (int i = 0; i < kAtOnce; ++i) {
-                const uint32_t at = ts + (uint32_t)(((w[i] >= 0 ? r[i] : 0) * pad + j0) * 4);
-                const uint4 t0 = lds_u4(at), t1 = lds_u4(at + 16);
-                const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
-                // zeros of the matrix's padding or of a row without an adapter are not multiplied: t may be no number there
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-                  if (w[i] >= 0) sum[i] = fmaf(__uint_as_float(tv[x]), e[i][x], sum[i]);
+                for (int i = 0; i < kAtOnce; ++i) add(i, j0, e[i]);
               }
             }
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i)
-              if (v0 + i < here) sts_f(part_at(es, r[i]), sum[i]);
+              if (v0 + i < here) sts_f(part_at(es, row_of(v0 + i)), sum[i]);
           }
         }
         const float b = p.bias && o < p.n ? __ldg(p.bias + (p.bias_each ? (size_t)t.weight * (size_t)p.n : 0) + (size_t)o) : 0.f;
@@ -1049,6 +1088,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         }
       }
       if (p.split > 1 && met == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+      if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     }
   } else {
     // ---------------------------------------------------------------- kGrad: rows behind the end of a run are set to zero, once they are there
@@ -1057,13 +1097,13 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n;
       const bool sums = p.sums && at - tm * p.tiles_n == p.tiles_n - 1;
       each_piece(p, weight, share, [&](int, int rows) {
-        if (rows < kPiece) {
+        if (rows % 16) {
           ok = warp_wait(&bar[kAsk], asked & 1u, abort_flag, ws, 0x80000u, kLongNs);
           if (!ok) return false;
           if (P) mbar_acquire_cluster(&bar[kAsk], asked & 1u);
           ++asked;
           const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-          const int boxes = N * (2 + (sums ? 0 : p.q_bytes / kBox)), per = (kPiece - rows) * 8;      // 16 bytes each
+          const int boxes = N * (2 + (sums ? 0 : p.q_bytes / kBox)), per = (16 - rows % 16) * 8;     // 16 bytes each
           for (int b = 0; b < boxes; ++b)
             for (int i = lane; i < per; i += 32) sts_u4(a + (uint32_t)(b * kBox + rows * 128 + i * 16), make_uint4(0, 0, 0, 0));
           fence_proxy_async();
@@ -1244,6 +1284,7 @@ cudaError_t launch(Params &p, long long items, int n_sm, const CUtensorMap (&m)[
 }
 template <int FORM, bool ACROSS>
 cudaError_t launch_any(Params &p, bool wide, bool pair, long long items, int n_sm, const CUtensorMap (&m)[4], DcWsHeader *ws, cudaStream_t st) {
+  if (wide && FORM != kFew && pair) return launch<FORM, ACROSS, float, FORM != kFew>(p, items, n_sm, m, ws, st);
   if (wide) return launch<FORM, ACROSS, float, false>(p, items, n_sm, m, ws, st);
   if (FORM != kFew && pair) return launch<FORM, ACROSS, bf16, FORM != kFew>(p, items, n_sm, m, ws, st);
   return launch<FORM, ACROSS, bf16, false>(p, items, n_sm, m, ws, st);
@@ -1266,18 +1307,18 @@ int split_of(long long items, int pieces, int least, int n_sm) {
   return s < 1 ? 1 : s;
 }
 // Columns to a tile, and whether CTAs work in pairs, by an estimate in cycles: a piece of 64 terms takes its loads (an SM takes in some 45 bytes a cycle) or its
-// instructions, results go out beside the next tile's pieces, and of the last tile behind them.
+// instructions, results go out beside the next tile's pieces (fp32: behind this one's, their sums being in registers), and of the last tile behind them.
 struct Shape { int nt; bool pair; };
 Shape shape_of(int n, double rows, double runs, double pieces, bool wide, int n_sm) {
-  static constexpr Shape kinds[4] = {{256, true}, {256, false}, {128, false}, {64, false}};
+  static constexpr Shape kinds[5] = {{256, true}, {128, true}, {256, false}, {128, false}, {64, false}};
   Shape best = {64, false};
   double least = 1e30;
   for (const Shape &k : kinds) {
-    if ((wide && k.nt > 128) || (k.nt > 64 && n <= k.nt / 2)) continue;
+    if ((wide ? k.nt > 128 : k.pair && k.nt < 256) || (k.nt > 64 && n <= k.nt / 2)) continue;
     const double tiles = (rows / (k.pair ? 256 : 128) + 0.5 * runs) * dc_div_up(n, k.nt), rounds = tiles / (k.pair ? n_sm / 2 : n_sm);
-    const double bytes = (128 + (k.pair ? 128 : k.nt)) * 128.0 * (wide ? 3 : 1), sums = k.nt * 2.0 * (wide ? 6 : 1);
+    const double bytes = (128 + (k.pair ? k.nt / 2 : k.nt)) * 128.0 * (wide ? 3 : 1), sums = k.nt * 2.0 * (wide ? 6 : 1);
     const double main = pieces * (bytes / 45 > sums ? bytes / 45 : sums), out = 400 + k.nt * 10.0;
-    const double time = (rounds < 1 ? 1 : rounds + 0.4) * (main > out ? main : out) + (main > out ? out : main) + (k.pair ? 800 : 0);
+    const double time = (rounds < 1 ? 1 : rounds + 0.4) * (wide ? main + out : main > out ? main : out) + (main > out ? out : main) + (k.pair ? 800 : 0);
     if (time < least) { least = time; best = k; }
   }
   return best;

@@ -194,6 +194,8 @@ def lib():
                          Geom, Block, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
                          getattr(torch._C, "_cuda_getCurrentRawStream", None))
             _dccall.bind_q4(at("dc_q4_quantize"), at("dc_q4_dequantize"), at("dc_q4_product"), at("dc_q4_forward"), at("dc_q4_query"))
+            _dccall.bind_group(at("dc_group_forward"), at("dc_group_backward"), at("dc_adapter_forward"), at("dc_adapter_backward"),
+                               at("dc_adapter_saved_bytes"), torch.int32)
             _native = _dccall
         except ImportError:                      # not built for this Python
             _native = _NoNative
@@ -204,6 +206,7 @@ def lib():
 class _NoNative:
     """In the place of the native module: answers as it does for arguments it does not read."""
     conv = dwconv = block = q4_quantize = q4_dequantize = q4_product = q4_forward = staticmethod(lambda *a: None)
+    group_forward = group_backward = adapter_forward = adapter_backward = conv
 
 
 def _load_native():
@@ -719,6 +722,11 @@ def group_workspace_bytes(rows: int, groups: int, c_in: int, c_out: int, dtype: 
 def group_forward(x, offsets, w, bias, act, y, workspace, stream=None):
     """y[r] = act(w[g] x[r] + bias[g]) for the rows offsets[g] <= r < offsets[g + 1] of every group; other rows of y stay as they are.
     x: [..., c_in], w: [groups, c_out, c_in], y: [..., c_out], dense, of one dtype; bias: fp32 [groups, c_out] or None."""
+    st = (_native or _load_native()).group_forward(x, offsets, w, bias, act, y, workspace, stream)
+    if st == OK:
+        return
+    if st is not None:
+        raise DcError(st, "dc_group_forward")
     if w.dim() != 3:
         raise ValueError("group_forward: weights [groups, c_out, c_in] are wanted")
     groups, c_out, c_in = w.shape
@@ -738,6 +746,11 @@ def group_forward(x, offsets, w, bias, act, y, workspace, stream=None):
 def group_backward(dy, x, offsets, w, dx, dw, db, workspace, stream=None):
     """The gradients of group_forward (without activation) for dy: dx as x, dw as w, db fp32 [groups, c_out]; each may be None.  w gives the
     sizes, and is read where dx is wanted."""
+    st = (_native or _load_native()).group_backward(dy, x, offsets, w, dx, dw, db, workspace, stream)
+    if st == OK:
+        return
+    if st is not None:
+        raise DcError(st, "dc_group_backward")
     if w.dim() != 3:
         raise ValueError("group_backward: weights [groups, c_out, c_in] are wanted")
     groups, c_out, c_in = w.shape
@@ -806,6 +819,11 @@ def _adapter_call(what: str, rows: int, w, adapters: Adapters, offsets, which, s
 def adapter_forward(x, w, adapters: Adapters, offsets, which, bias, act, residual, saved, y, workspace, stream=None):
     """y = act(x w^T + bias + residual + the adapters' part): the rows offsets[s] <= r < offsets[s + 1] have adapter which[s] (-1: none).
     w: [c_out, c_in] or None; x: [..., c_in], y (and residual): [..., c_out], dense; bias: fp32 [c_out] or None; saved: adapters.saved(rows)."""
+    st = (_native or _load_native()).adapter_forward(x, w, adapters, offsets, which, bias, act, residual, saved, y, workspace, stream)
+    if st == OK:
+        return
+    if st is not None:
+        raise DcError(st, "dc_adapter_forward")
     rows = x.numel() // adapters.c_in
     _here("adapter_forward", x, w, adapters.a, adapters.b, adapters.scale, offsets, which, bias, residual, saved, y, workspace)
     _adapter_call("adapter_forward", rows, w, adapters, offsets, which, saved, x.dtype)
@@ -820,6 +838,11 @@ def adapter_forward(x, w, adapters: Adapters, offsets, which, bias, act, residua
 
 def adapter_backward(dy, x, w, adapters: Adapters, offsets, which, saved, dx, da, db, workspace, stream=None):
     """The gradients of adapter_forward (without activation) for dy: dx as x, da and db as the adapters' a and b; each may be None."""
+    st = (_native or _load_native()).adapter_backward(dy, x, w, adapters, offsets, which, saved, dx, da, db, workspace, stream)
+    if st == OK:
+        return
+    if st is not None:
+        raise DcError(st, "dc_adapter_backward")
     rows = dy.numel() // adapters.c_out
     _here("adapter_backward", dy, x, w, adapters.a, adapters.b, adapters.scale, offsets, which, saved, dx, da, db, workspace)
     _same_type("adapter_backward", dy.dtype, da, db)

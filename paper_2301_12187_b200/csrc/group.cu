@@ -150,7 +150,7 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
     j.dtype = dtype;
     j.raw_p = dy;
     j.raw_q = x;
-    e = grad_tc(j, (DcWsHeader *)workspace, (cudaStream_t)stream);
+    e = grad_tc(j, dx && rows, (DcWsHeader *)workspace, (cudaStream_t)stream);
   }
   return status(e);
 }
@@ -194,10 +194,9 @@ dc_status check_adapter_call(long long rows, int c_in, int c_out, const void *w,
     return DC_ERR_ALIGNMENT;
   return DC_OK;
 }
-// Rows through the adapters' first matrices -- a, or in the backward pass b read across -- scaled, to `out`.  *apart: by the kernel behind which
-// the next launch may start early.
+// Rows through the adapters' first matrices -- a, or in the backward pass b read across -- scaled, to `out`.
 cudaError_t narrow(const void *raw_x, const void *x, int x_pitch, int rows, int k, const void *m, int m_pitch, bool backward, const dc_adapters *ad, const Runs &runs,
-                   void *out, dc_dtype dtype, void *workspace, cudaStream_t st, bool *apart) {
+                   void *out, dc_dtype dtype, void *workspace, cudaStream_t st) {
   if (runs.count == 0) return cudaSuccess;
   RowsJob j = {};
   j.x = x;
@@ -215,8 +214,7 @@ cudaError_t narrow(const void *raw_x, const void *x, int x_pitch, int rows, int 
   j.y = out;
   j.y_terms = 1;
   j.dtype = dtype;
-  *apart = narrow_apart(j);
-  return *apart ? narrow_tc(j, st) : rows_tc(j, false, (DcWsHeader *)workspace, st);
+  return narrow_apart(j) ? narrow_tc(j, st) : rows_tc(j, false, (DcWsHeader *)workspace, st);
 }
 }  // namespace
 
@@ -239,7 +237,7 @@ extern "C" dc_status dc_adapter_forward(const void *x, long long rows, int c_in,
   const int in = parts.pitch(c_in), of_rank = parts.pitch(adapters->rank);
   bool apart = false;
   cudaError_t e = parts.copy((cudaStream_t)stream);
-  if (e == cudaSuccess) e = narrow(x, x_at, in, (int)rows, c_in, a_at, in, false, adapters, of, saved, dtype, workspace, st, &apart);
+  if (e == cudaSuccess) e = narrow(x, x_at, in, (int)rows, c_in, a_at, in, false, adapters, of, saved, dtype, workspace, st);
   if (e != cudaSuccess) return status(e);
   RowsJob j = {};
   j.x = x_at;
@@ -262,7 +260,7 @@ extern "C" dc_status dc_adapter_forward(const void *x, long long rows, int c_in,
   j.residual = residual;
   j.y = y;
   j.dtype = dtype;
-  return status(rows_tc(j, apart, (DcWsHeader *)workspace, st));
+  return status(rows_tc(j, runs > 0, (DcWsHeader *)workspace, st));
 }
 
 extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int c_in, const void *w, int c_out,
@@ -283,9 +281,24 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
   const void *a_at = dx ? parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in) : nullptr;
   const void *b_at = with_u ? parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank) : nullptr;
   const int in = parts.pitch(c_in), out = parts.pitch(c_out), of_rank = parts.pitch(adapters->rank);
-  cudaError_t e = parts.copy((cudaStream_t)stream);
-  bool apart = false;
-  if (with_u && e == cudaSuccess) e = narrow(dy, dy_at, out, (int)rows, c_out, b_at, of_rank, true, adapters, of, u, dtype, workspace, st, &apart);
+  // One behind the other: u, with db beside it; dx, with da beside it (which reads u from its start: not beside a dx that has not waited for u).
+  const bool dx_early = !db && with_u && runs;
+  cudaError_t e = parts.copy(st);
+  if (with_u && e == cudaSuccess) e = narrow(dy, dy_at, out, (int)rows, c_out, b_at, of_rank, true, adapters, of, u, dtype, workspace, st);
+  GradJob g = {};
+  g.runs = of;
+  g.dtype = dtype;
+  g.q_terms = 1;
+  g.n = adapters->rank;
+  if (db && e == cudaSuccess) {
+    g.p = dy_at;
+    g.raw_p = dy;
+    g.m = c_out;
+    g.p_pitch = out;
+    g.q = saved;
+    g.out = db;
+    e = grad_tc(g, with_u && runs, (DcWsHeader *)workspace, st);
+  }
   if (dx && rows && e == cudaSuccess) {
     RowsJob j = {};
     j.x = dy_at;
@@ -308,13 +321,8 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
     j.ext = of;
     j.y = dx;
     j.dtype = dtype;
-    e = rows_tc(j, apart, (DcWsHeader *)workspace, st);
+    e = rows_tc(j, dx_early, (DcWsHeader *)workspace, st);
   }
-  GradJob g = {};
-  g.runs = of;
-  g.dtype = dtype;
-  g.q_terms = 1;
-  g.n = adapters->rank;
   if (da && e == cudaSuccess) {                  // as x^T u, so that the long side is the instructions' 128 rows
     g.p = x_at;
     g.raw_p = x;
@@ -323,17 +331,7 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
     g.q = u;
     g.out = da;
     g.out_across = 1;
-    e = grad_tc(g, (DcWsHeader *)workspace, st);
-  }
-  if (db && e == cudaSuccess) {
-    g.p = dy_at;
-    g.raw_p = dy;
-    g.m = c_out;
-    g.p_pitch = out;
-    g.q = saved;
-    g.out = db;
-    g.out_across = 0;
-    e = grad_tc(g, (DcWsHeader *)workspace, st);
+    e = grad_tc(g, dx && rows && !dx_early, (DcWsHeader *)workspace, st);
   }
   return status(e);
 }

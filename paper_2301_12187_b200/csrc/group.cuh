@@ -40,35 +40,45 @@ __device__ __forceinline__ Run run_at(const Runs &r, int s) {
 // the same answer; 32 runs are looked at at a time.
 struct Walk {
   int base;                  // runs before it are behind us
-  long long before;          // tiles of theirs
-  __device__ void start() { base = 0; before = 0; }
+  long long before;          // items of theirs
+  Run last;                  // the run of the last answer, and its items
+  int last_index;
+  long long first, after;
+  __device__ void start() { base = 0; before = first = after = 0; }
   // items of a run: row tiles x per_tile.  false: there is no such item
   __device__ bool find(const Runs &r, int tile, int per_tile, long long item, Run *run, int *index, long long *inside) {
-    const int lane = (int)(threadIdx.x & 31u);
-    for (; base < r.count; base += 32) {
-      Run o = {0, 0, -1};
-      if (base + lane < r.count) o = run_at(r, base + lane);
-      const int tiles = o.weight < 0 ? 0 : (int)(((unsigned)(o.end - o.begin) + (unsigned)tile - 1u) / (unsigned)tile);
-      const long long mine = (long long)tiles * per_tile;
-      long long upto = mine;
+    if (item < first || item >= after) {
+      const int lane = (int)(threadIdx.x & 31u);
+      for (;; base += 32) {
+        if (base >= r.count) return false;
+        Run o = {0, 0, -1};
+        if (base + lane < r.count) o = run_at(r, base + lane);
+        const int tiles = o.weight < 0 ? 0 : (int)(((unsigned)(o.end - o.begin) + (unsigned)tile - 1u) / (unsigned)tile);
+        const long long mine = (long long)tiles * per_tile;
+        long long upto = mine;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += v;
+        for (int d = 1; d < 32; d <<= 1) {
+          const long long v = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += v;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, before + upto > item);
+        if (past) {
+          const int at = __ffs(past) - 1;
+          last.begin = __shfl_sync(0xffffffffu, o.begin, at);
+          last.end = __shfl_sync(0xffffffffu, o.end, at);
+          last.weight = __shfl_sync(0xffffffffu, o.weight, at);
+          last_index = base + at;
+          after = before + __shfl_sync(0xffffffffu, upto, at);
+          first = after - __shfl_sync(0xffffffffu, mine, at);
+          break;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
       }
-      const unsigned past = __ballot_sync(0xffffffffu, before + upto > item);
-      if (past) {
-        const int at = __ffs(past) - 1;
-        run->begin = __shfl_sync(0xffffffffu, o.begin, at);
-        run->end = __shfl_sync(0xffffffffu, o.end, at);
-        run->weight = __shfl_sync(0xffffffffu, o.weight, at);
-        *index = base + at;
-        *inside = item - (before + __shfl_sync(0xffffffffu, upto - mine, at));
-        return true;
-      }
-      before += __shfl_sync(0xffffffffu, upto, 31);
     }
-    return false;
+    *run = last;
+    *index = last_index;
+    *inside = item - first;
+    return true;
   }
 };
 
@@ -135,9 +145,11 @@ struct Copy {
 constexpr int kMaxCopies = 5;
 
 cudaError_t copies_tc(const Copy *c, int count, dc_dtype dtype, cudaStream_t st);
-bool narrow_apart(const RowsJob &j);             // y_terms: by a kernel for short runs, behind which rows_tc may start early
+// early: the launch in front of this one, by narrow_tc, rows_tc or grad_tc, writes nothing of what this one reads but `t`, and nothing that it
+// writes; nothing else of the caller's is between them.  Both then run side by side as far as there is room, and this one ends behind that one.
+bool narrow_apart(const RowsJob &j);             // y_terms: by a kernel for short runs
 cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st);
-cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaStream_t st);
-cudaError_t grad_tc(const GradJob &j, DcWsHeader *ws, cudaStream_t st);
+cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st);
+cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t st);
 
 }  // namespace grp

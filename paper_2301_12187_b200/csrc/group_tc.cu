@@ -65,7 +65,7 @@ struct Params {
   const bf16 *t;             // what rows keep
   const void *e;             // kFew: what the reading-out warps take of the adapters
   int e_pitch, e_vec;
-  int early;                 // kFew: what is loaded by TMA was there before the launch in front of this one began
+  int early;                 // all but t was there before the launch in front of this one began, and that one writes nothing that this one does
   int off_out, off_t;        // staged results; kFew: t's numbers in shared memory
   // kGrad
   float *sums;
@@ -124,6 +124,10 @@ __device__ __forceinline__ void commit(uint64_t *bar) {
 }
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// the same for what orders no memory: as a release it would wait for this thread's stores, 1500 cycles where results are on their way
+__device__ __forceinline__ void arrive_cluster_relaxed(uint32_t bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // a phase that has been seen to end: what the cluster's threads wrote before they arrived is visible behind this
 __device__ __forceinline__ void mbar_acquire_cluster(uint64_t *bar, uint32_t parity) {
@@ -335,7 +339,8 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
     T *at = y + (size_t)r0 * pitch + (size_t)(piece * 4);
 #pragma unroll
     for (int i = 0; i < 8; ++i, at += 4 * pitch) {
-      float f[4] = {__uint_as_float(w[i].x) + b.x, __uint_as_float(w[i].y) + b.y, __uint_as_float(w[i].z) + b.z, __uint_as_float(w[i].w) + b.w};
+      float f[4] = {__uint_as_float(w[i].x), __uint_as_float(w[i].y), __uint_as_float(w[i].z), __uint_as_float(w[i].w)};
+      if (bias) { f[0] += b.x; f[1] += b.y; f[2] += b.z; f[3] += b.w; }
       if (ahead) {
         if (sizeof(T) == 4) {
           const uint4 u = ahead->v[sizeof(T) == 4 ? i : 0];
@@ -347,8 +352,10 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
           f[2] += __uint_as_float(u.y << 16); f[3] += __uint_as_float(u.y & 0xffff0000u);
         }
       }
+      if (p.act) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) f[x] = dc_act_apply(f[x], p.act);
+        for (int x = 0; x < 4; ++x) f[x] = dc_act_apply(f[x], DC_ACT_RELU6);
+      }
       if (i * 4 + r0 < rows) {
         if (sizeof(T) == 4) *reinterpret_cast<float4 *>(at) = make_float4(f[0], f[1], f[2], f[3]);
         else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
@@ -404,10 +411,11 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
     if (p.maps >> lane & 1) prefetch_tensormap(lane == 0 ? &map_p : lane == 1 ? &map_q : lane == 2 ? &map_t : &map_e);
   }
   if (FORM == kFew && p.split > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");   // this CTA is there, its barriers too: waited for before parts go out
-  // Tensor memory only behind the wait for the launch before this one, whose CTAs may still have theirs to ask for; the one in front of an
-  // early launch has none.
-  if (FORM == kFew && p.early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  else dc_pdl_enter();
+  // The next launch may start once this one has waited for the one before it: an early launch, which does not wait at its start, then finds
+  // all that was written before this one.  Tensor memory only behind that wait, since CTAs of the launch before may still have theirs to ask for; those of the one in
+  // front of an early launch, one to an SM, have it, or need none.
+  if (!p.early) asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (warp == 1) {
     if (P) {
       asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"((uint32_t)p.tmem_cols) : "memory");
@@ -440,6 +448,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   bool ok = true;
   auto next = [&]() { if (++stage == p.stages) { stage = 0; parity ^= 1u; } };
   // ring uses of an adapter's part: both terms of up to 32 numbers at once, else 64 numbers of one term at a time; fp32 all terms of 64
+  const bool adapters = FORM == kTile && p.rank && share == 0;     // of a shared sum one CTA's
   const int ext_uses = N == 3 ? p.rank_pieces : p.rank <= 32 ? 1 : 2 * p.rank_pieces;
 
   if (warp == 0) {
@@ -501,7 +510,8 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           }
         }
         __syncwarp();
-        if (FORM == kTile && p.rank)
+        if (adapters && p.early && item == team) asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (adapters)
           each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](int, int, int weight) {
             for (int c = 0; c < ext_uses; ++c, next()) {
               if (!lead || !ok) continue;
@@ -628,7 +638,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           for (int c = c0; c < c1; ++c) next();
         }
         __syncwarp();
-        if (FORM == kTile && p.rank)
+        if (adapters)
           each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](int first_row, int last_row, int) {
             uint32_t off[8];                     // lanes of other rows
 #pragma unroll
@@ -678,7 +688,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       tc_fence_before();
       __syncwarp();
       if (elect_one()) {
-        if (P) arrive_cluster(freed + (turn & 1u) * 8u);
+        if (P) arrive_cluster_relaxed(freed + (turn & 1u) * 8u);
         else mbar_arrive(&bar[kDEmpty + (turn & 1u)]);
       }
       __syncwarp();
@@ -834,6 +844,9 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
             ask_block<T>(p, next_residual, reinterpret_cast<const T *>(p.residual) + (size_t)row0 * (size_t)p.n + (size_t)o0, (size_t)p.n, min(32, t.end - row0), min(min(32, p.nt - c), p.n - o0));
         };
         const int c_first = p.split > 1 ? (rank + set * p.split) * 32 : set * 32, c_step = 64 * p.split;
+        if (residual && row < t.end)             // to L2, while the tile is multiplied
+          for (int c = set * 64; c < p.nt; c += 128)
+            if (t.tn * p.nt + c < p.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T *>(p.residual) + (size_t)row * (size_t)p.n + (size_t)(t.tn * p.nt + c)));
         if (!kShort) ask(c_first);               // (fp32 has no registers to spare)
         auto deliver = [&](int c, float (&v)[32]) {
           const int o0 = t.tn * p.nt + c;
@@ -841,8 +854,10 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           const Ahead<T> now = next_residual;
           if (!kShort) ask(c + c_step);
           if (row0 >= t.end) return;
+          if (p.alpha || p.pieces == 0) {
 #pragma unroll
-          for (int x = 0; x < 32; ++x) v[x] = filled ? v[x] * alpha : 0.f;
+            for (int x = 0; x < 32; ++x) v[x] = filled ? v[x] * alpha : 0.f;
+          }
           if (kShort && row < t.end && any_nan(v)) {
 #pragma unroll 1
             for (int x = 0; x < 32; ++x) {
@@ -1088,7 +1103,6 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         }
       }
       if (p.split > 1 && met == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-      if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     }
   } else {
     // ---------------------------------------------------------------- kGrad: rows behind the end of a run are set to zero, once they are there
@@ -1119,6 +1133,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
     }
   }
   __syncwarp();
+  if (p.early) asm volatile("griddepcontrol.wait;" ::: "memory");        // this launch does not end before the one in front of it
   if (FORM == kFew) {
     if (p.split > 1) {
       if (warp < 2) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -1284,7 +1299,6 @@ cudaError_t launch(Params &p, long long items, int n_sm, const CUtensorMap (&m)[
 }
 template <int FORM, bool ACROSS>
 cudaError_t launch_any(Params &p, bool wide, bool pair, long long items, int n_sm, const CUtensorMap (&m)[4], DcWsHeader *ws, cudaStream_t st) {
-  if (wide && FORM != kFew && pair) return launch<FORM, ACROSS, float, FORM != kFew>(p, items, n_sm, m, ws, st);
   if (wide) return launch<FORM, ACROSS, float, false>(p, items, n_sm, m, ws, st);
   if (FORM != kFew && pair) return launch<FORM, ACROSS, bf16, FORM != kFew>(p, items, n_sm, m, ws, st);
   return launch<FORM, ACROSS, bf16, false>(p, items, n_sm, m, ws, st);
@@ -1306,20 +1320,26 @@ int split_of(long long items, int pieces, int least, int n_sm) {
   if (s > pieces / least) s = pieces / least;
   return s < 1 ? 1 : s;
 }
-// Columns to a tile, and whether CTAs work in pairs, by an estimate in cycles: a piece of 64 terms takes its loads (an SM takes in some 45 bytes a cycle) or its
-// instructions, results go out beside the next tile's pieces (fp32: behind this one's, their sums being in registers), and of the last tile behind them.
-struct Shape { int nt; bool pair; };
+// Columns to a tile, whether CTAs work in pairs, and how many share a tile's sum, by an estimate in cycles: a piece of 64 terms takes its loads (an SM takes in some 45
+// bytes a cycle; two stages of fp32 terms wait for them) or its instructions; results go out beside the next tile's pieces (fp32: behind this one's, their
+// sums being in registers), and of the last tile behind them; a cluster meets twice.
+struct Shape { int nt; bool pair; int split; };
 Shape shape_of(int n, double rows, double runs, double pieces, bool wide, int n_sm) {
-  static constexpr Shape kinds[5] = {{256, true}, {128, true}, {256, false}, {128, false}, {64, false}};
-  Shape best = {64, false};
+  static constexpr struct { int nt; bool pair; } kinds[4] = {{256, true}, {256, false}, {128, false}, {64, false}};
+  Shape best = {64, false, 1};
   double least = 1e30;
-  for (const Shape &k : kinds) {
-    if ((wide ? k.nt > 128 : k.pair && k.nt < 256) || (k.nt > 64 && n <= k.nt / 2)) continue;
-    const double tiles = (rows / (k.pair ? 256 : 128) + 0.5 * runs) * dc_div_up(n, k.nt), rounds = tiles / (k.pair ? n_sm / 2 : n_sm);
+  for (const auto &k : kinds) {
+    if ((wide && k.nt > 128) || (k.nt > 64 && n <= k.nt / 2)) continue;
+    const double tiles = (rows / (k.pair ? 256 : 128) + 0.5 * runs) * dc_div_up(n, k.nt);
     const double bytes = (128 + (k.pair ? k.nt / 2 : k.nt)) * 128.0 * (wide ? 3 : 1), sums = k.nt * 2.0 * (wide ? 6 : 1);
-    const double main = pieces * (bytes / 45 > sums ? bytes / 45 : sums), out = 400 + k.nt * 10.0;
-    const double time = (rounds < 1 ? 1 : rounds + 0.4) * (wide ? main + out : main > out ? main : out) + (main > out ? out : main) + (k.pair ? 800 : 0);
-    if (time < least) { least = time; best = k; }
+    double piece = bytes / 45 > sums ? bytes / 45 : sums;
+    if (wide && piece < (sums + 1000 + bytes / 45) / 2) piece = (sums + 1000 + bytes / 45) / 2;
+    for (int split = 1; split <= (k.pair ? 1 : kMaxSplit); ++split) {
+      if (split > 1 && (tiles * split > n_sm || pieces < 4 * split)) break;
+      const double rounds = tiles * split / (k.pair ? n_sm / 2 : n_sm), main = pieces / split * piece, out = (400 + k.nt * 10.0) / split + (split > 1 ? 4000 : 0);
+      const double time = (rounds < 1 ? 1 : rounds + 0.4) * (wide ? main + out : main > out ? main : out) + (main > out ? out : main) + (k.pair ? 800 : 0);
+      if (time < least) { least = time; best = {k.nt, k.pair, split}; }
+    }
   }
   return best;
 }
@@ -1362,7 +1382,7 @@ cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st) {
   return dc_launch_pdl(k_adapter_narrow<float>, grid, dim3(256), 0, st, (const float *)j.raw_x, j.k, (const float *)j.raw_w, j.k, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
 }
 
-cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaStream_t st) {
+cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st) {
   const int n_sm = dc_sm_count();
   const bool wide = j.dtype == DC_F32;
   const int terms = wide ? 3 : 1;
@@ -1404,7 +1424,7 @@ cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaSt
     p.tiles_n = dc_div_up(j.n, 128);
     items = row_tiles(j.runs, p.nt) * p.tiles_n;
     p.split = split_of(items, p.pieces, 4, n_sm);
-    p.early = behind_narrow && !j.runs.offsets;
+    p.early = early;
     lay_out(&p, terms, (p.rank ? p.nt * (rank_pad(p.rank) * 4 + 512) : 0) + (p.split > 1 ? (p.nt + p.split) * 512 : 0));
   } else {
     if (j.y_terms) {
@@ -1413,12 +1433,15 @@ cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaSt
       const Shape s = shape_of(j.n, j.rows, runs, p.pieces + (j.t ? 2 : 0), wide, n_sm);
       p.nt = s.nt;
       pair = s.pair;
+      p.split = s.split;
     }
     const int wide_nt = pair ? p.nt / 2 : p.nt;  // of a CTA
     p.q_bytes = j.w_across || (!j.w && j.e_across) ? dc_div_up(wide_nt, 64) * kBox : wide_nt * 128;
     p.tiles_n = dc_div_up(j.n, p.nt);
     items = row_tiles(j.runs, pair ? 256 : 128) * p.tiles_n;
     if (j.y_terms) p.split = split_of(items, p.pieces, 4, n_sm);
+    else if (p.split > n_sm / items) p.split = items < n_sm ? (int)(n_sm / items) : 1;         // a tile to a cluster
+    p.early = early;
     lay_out(&p, terms, kOut);
   }
   p.pieces_per = dc_div_up(p.pieces, p.split);
@@ -1442,17 +1465,17 @@ cudaError_t rows_tc(const RowsJob &j, bool behind_narrow, DcWsHeader *ws, cudaSt
   return across ? launch_any<kTile, true>(p, wide, pair, items, n_sm, m, ws, st) : launch_any<kTile, false>(p, wide, pair, items, n_sm, m, ws, st);
 }
 
-cudaError_t grad_tc(const GradJob &j, DcWsHeader *ws, cudaStream_t st) {
+cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t st) {
   const int n_sm = dc_sm_count();
   const bool wide = j.dtype == DC_F32;
   if (wide && j.out && j.sums) {                 // two stages of fp32 terms leave no room for the block of ones
     GradJob apart = j;
     apart.out = nullptr;
-    const cudaError_t e = grad_tc(apart, ws, st);
+    const cudaError_t e = grad_tc(apart, early, ws, st);
     if (e != cudaSuccess) return e;
     apart = j;
     apart.sums = nullptr;
-    return grad_tc(apart, ws, st);
+    return grad_tc(apart, true, ws, st);
   }
   const int terms = wide ? 3 : 1, pad = rank_pad(j.n), weights = j.runs.weights;
   Params p = {};
@@ -1477,12 +1500,15 @@ cudaError_t grad_tc(const GradJob &j, DcWsHeader *ws, cudaStream_t st) {
     const Shape s = shape_of(j.n, (double)j.m * weights, 0, (double)j.runs.rows / kPiece / weights + 0.5, wide, n_sm);
     p.nt = s.nt;
     pair = s.pair && j.m > 128;
+    p.split = s.split;
   }
   p.tiles_m = dc_div_up(j.m, pair ? 256 : 128);
   p.q_bytes = dc_div_up(pair ? p.nt / 2 : p.nt, 64) * kBox;
   p.tiles_n = (j.out ? (j.q_terms ? 1 : dc_div_up(j.n, p.nt)) : 0) + (j.sums ? 1 : 0);
   const long long items = (long long)p.tiles_m * p.tiles_n * weights;
-  p.split = pair ? 1 : split_of(items, j.runs.rows / kPiece / weights, 4, n_sm);
+  if (!j.out || j.q_terms) p.split = split_of(items, j.runs.rows / kPiece / weights, 4, n_sm);
+  else if (pair || p.split > n_sm / items) p.split = !pair && items < n_sm ? (int)(n_sm / items) : 1;
+  p.early = early;
   lay_out(&p, terms, kOut + (j.sums ? kBox : 0));
   if (j.sums) p.off_out += kBox;
   CUtensorMap m[4] = {};

@@ -301,6 +301,26 @@ def test_adapter_backward(shared, case, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("case", [4, 6, 14])
+def test_adapter_backward_parts_alone(case, dtype):
+    """Each set of gradients without the others gives the same bits, on workspaces that hold something else: what runs beside what, and waits for what, differs."""
+    x, w, a, b, scale, off, which = adapter_inputs(case, dtype)
+    dt, rows = x.dtype, x.shape[0]
+    dy, ad = rand(rows, b.shape[1], seed=5, dtype=dt), dc.Adapters(a, b, scale)
+    ws, saved = torch.zeros(dc.adapter_workspace_bytes(rows, ad.c_in, ad.c_out, ad, ad.dtype), dtype=torch.uint8, device="cuda"), ad.saved(rows)
+    dc.adapter_forward(x, w, ad, off, which, None, 0, None, saved, torch.empty_like(dy), ws)
+    outs = [torch.empty_like(x), torch.empty_like(a), torch.empty_like(b)]
+    dc.adapter_backward(dy, x, w, ad, off, which, saved, *outs, ws)
+    for wanted in ((0,), (1,), (2,), (0, 1), (0, 2), (1, 2)):
+        for again in range(3):
+            ws[256:] = 0xFF
+            some = [torch.full_like(t, float("nan")) if k in wanted else None for k, t in enumerate(outs)]
+            dc.adapter_backward(dy, x if 1 in wanted else None, w, ad, off, which, saved if 2 in wanted else None, *some, ws)
+            for k in wanted:
+                assert torch.equal(some[k], outs[k]), (wanted, k, again)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 def test_gradients_against_differences(dtype):
     """d/de of <forward(p + e v), dy> in 64 bits against <gradient, v>: the formula is linear in x, and in a and b apart."""
     x, w, a, b, scale, off, which = adapter_inputs(6, dtype)

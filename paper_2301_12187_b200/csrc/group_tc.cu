@@ -7,7 +7,7 @@
 // neighbouring columns of 64 rows, and the instruction takes them the other way round.
 //   kTile   128 rows of a run x up to 256 columns of its matrix.
 //   kFew    runs of few rows: 128 columns of the matrix take the place of the 128 rows, so that an instruction is as wide as there are rows and
-//           the matrix streams through once.
+//           the matrix streams through once.  Adapters' parts of those columns, a row's after a row's, come through a ring of their own.
 //   kGrad   128 x up to 256 of a gradient: the sum runs over the rows of a weight's runs.  The last piece of a run holds rows of the next one: those that its last
 //           instruction takes are set to zero by a warp, in both operands (0 times a NaN is a NaN).
 // kTile and kGrad in pairs (cta_group::2): two CTAs multiply 256 x 256, each loads half of either operand.
@@ -32,8 +32,8 @@ using grp::Runs;
 enum { kTile = 0, kFew = 1, kGrad = 2 };
 constexpr int kEpi = 8;                          // warps reading out
 template <int FORM>
-constexpr int kThreadsOf = (2 + kEpi + (FORM == kGrad ? 1 : 0)) * 32;
-constexpr int kMaxStages = 8, kMaxSplit = 8;
+constexpr int kThreadsOf = (2 + kEpi + (FORM == kTile ? 0 : 1)) * 32;
+constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxSlots = 8;
 constexpr int kSmem = 226 * 1024;                // what the static arrays leave
 constexpr int kPiece = 64;                       // of the sum, 128 bytes of bf16
 constexpr int kP = 128 * 128;                    // bytes of the 128-row operand in a stage
@@ -62,9 +62,11 @@ struct Params {
   int stages, q_bytes, tmem_cols;
   int maps;                  // bits of the tensor maps that there are
   int rank, rank_pieces;     // adapters: pieces of 64 of the rank
+  int t_bytes, e_bytes, e_wide;      // kTile: bytes of a stage's rows of t and e; numbers of the rank in a row (e across: rows)
   const bf16 *t;             // what rows keep
   const void *e;             // kFew: what the reading-out warps take of the adapters
   int e_pitch, e_vec;
+  int slots, slot_bytes;     // kFew, bf16: of an adapter's part of the tile's columns, in shared memory
   int early;                 // all but t was there before the launch in front of this one began, and that one writes nothing that this one does
   int off_out, off_t;        // staged results; kFew: t's numbers in shared memory
   // kGrad
@@ -78,6 +80,14 @@ __device__ __forceinline__ uint64_t desc_along(uint32_t a) {     // rows of 64 a
 }
 __device__ __forceinline__ uint64_t desc_across(uint32_t a) {    // rows of 64 across it: 1024 bytes between groups of 8 rows, kBox between blocks of 64 columns
   return ((uint64_t)(64u | (1u << 14) | (2u << 29)) << 32) | (uint64_t)((a >> 4) & 0x3FFFu) | ((uint64_t)(kBox >> 4) << 16);
+}
+// the same for rows of 16, 32 or 64 along the sum (swizzled over as many bytes), and for blocks of `rows` rows across it
+__device__ __forceinline__ uint64_t desc_narrow(uint32_t a, uint32_t row_bytes) {
+  const uint32_t swizzle = row_bytes == 128u ? 2u : row_bytes == 64u ? 4u : 6u;
+  return ((uint64_t)(row_bytes / 2u | (1u << 14) | (swizzle << 29)) << 32) | (uint64_t)((a >> 4) & 0x3FFFu) | (1u << 16);
+}
+__device__ __forceinline__ uint64_t desc_short(uint32_t a, uint32_t rows) {
+  return ((uint64_t)(64u | (1u << 14) | (2u << 29)) << 32) | (uint64_t)((a >> 4) & 0x3FFFu) | ((uint64_t)(rows * 8u) << 16);
 }
 template <bool ACROSS>
 __device__ __forceinline__ uint64_t desc_of(uint32_t a) { return ACROSS ? desc_across(a) : desc_along(a); }
@@ -166,9 +176,10 @@ __device__ __forceinline__ bool find_tile(const Params &p, int tile, grp::Walk &
   return true;
 }
 
-// Calls f(begin, end, weight) for the runs with an adapter that have rows in [row0, end), all lanes together.
-template <typename F>
-__device__ __forceinline__ void each_run(const Runs &r, int row0, int end, F f) {
+// For the runs with an adapter that have rows in [row0, end), all lanes together: each lane looks at its own run, `mine(run)`, then f(lane) for each of
+// those that count.
+template <typename G, typename F>
+__device__ __forceinline__ void each_run(const Runs &r, int row0, int end, G mine, F f) {
   const int lane = (int)(threadIdx.x & 31u);
   // the first run that ends behind row0: 32 probes at a time
   int lo = 0, n = r.count;
@@ -187,11 +198,13 @@ __device__ __forceinline__ void each_run(const Runs &r, int row0, int end, F f) 
       o = grp::run_at(r, base + lane);
       stop = o.begin >= end;
     }
-    unsigned here = __ballot_sync(0xffffffffu, !stop && o.weight >= 0 && o.end > row0 && o.end > o.begin);
+    const bool counts = !stop && o.weight >= 0 && o.end > row0 && o.end > o.begin;
+    if (counts) mine(o);
+    unsigned here = __ballot_sync(0xffffffffu, counts);
     while (here) {
       const int at = __ffs(here) - 1;
       here &= here - 1;
-      f(__shfl_sync(0xffffffffu, o.begin, at), __shfl_sync(0xffffffffu, o.end, at), __shfl_sync(0xffffffffu, o.weight, at));
+      f(at);
     }
     if (__any_sync(0xffffffffu, stop)) return;
   }
@@ -206,27 +219,41 @@ __device__ __forceinline__ int adapter_of(const Runs &r, int row) {
   return -1;
 }
 
-// Calls f(first row, rows) for this CTA's pieces of 64 rows of a weight's runs: pieces go round the CTAs of a cluster that share a sum.
+// Calls f(begin, end) for the runs of a weight that have rows, all lanes together; of mapped runs 32 are looked at at a time.
 template <typename F>
-__device__ __forceinline__ void each_piece(const Params &p, int weight, int share, F f) {
-  const int first = p.runs.mapped ? 0 : weight, last = p.runs.mapped ? p.runs.count : weight + 1;
-  int turn = 0;
-  for (int s = first; s < last; ++s) {
-    const Run run = grp::run_at(p.runs, s);
-    if (run.weight != weight) continue;
-    for (int r = run.begin; r < run.end; r += kPiece) {
-      if (turn == share && !f(r, min(kPiece, run.end - r))) return;
-      if (++turn == p.split) turn = 0;
+__device__ __forceinline__ void each_run_of(const Runs &r, int weight, F f) {
+  if (!r.mapped) {
+    const Run run = grp::run_at(r, weight);
+    if (run.end > run.begin) f(run.begin, run.end);
+    return;
+  }
+  const int lane = (int)(threadIdx.x & 31u);
+  for (int base = 0; base < r.count; base += 32) {
+    Run o = {0, 0, -1};
+    if (base + lane < r.count) o = grp::run_at(r, base + lane);
+    unsigned here = __ballot_sync(0xffffffffu, o.weight == weight && o.end > o.begin);
+    while (here) {
+      const int at = __ffs(here) - 1;
+      here &= here - 1;
+      f(__shfl_sync(0xffffffffu, o.begin, at), __shfl_sync(0xffffffffu, o.end, at));
     }
   }
 }
+// Calls f(first row, rows) for this CTA's pieces of 64 rows of a weight's runs, all lanes together: pieces go round the CTAs of a cluster that share a sum.
+template <typename F>
+__device__ __forceinline__ void each_piece(const Params &p, int weight, int share, F f) {
+  int turn = 0;
+  each_run_of(p.runs, weight, [&](int begin, int end) {
+    for (int r = begin; r < end; r += kPiece) {
+      if (turn == share) f(r, min(kPiece, end - r));
+      if (++turn == p.split) turn = 0;
+    }
+    __syncwarp();
+  });
+}
 __device__ __forceinline__ int count_pieces(const Params &p, int weight, int share) {
-  const int first = p.runs.mapped ? 0 : weight, last = p.runs.mapped ? p.runs.count : weight + 1;
   int all = 0;
-  for (int s = first; s < last; ++s) {
-    const Run run = grp::run_at(p.runs, s);
-    if (run.weight == weight) all += (run.end - run.begin + kPiece - 1) / kPiece;
-  }
+  each_run_of(p.runs, weight, [&](int begin, int end) { all += (end - begin + kPiece - 1) / kPiece; });
   return all <= share ? 0 : (all - share - 1) / p.split + 1;
 }
 
@@ -382,7 +409,7 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
   }
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kAsk = kDEmpty + 2, kFixed, kParts, kBars };
+enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kAsk = kDEmpty + 2, kFixed, kParts, kEFull, kEEmpty = kEFull + kMaxSlots, kBars = kEEmpty + kMaxSlots };
 
 // P: in pairs.  ACROSS: the matrices' sums run across their rows (of both operands of a gradient always).
 template <int FORM, bool ACROSS, typename T, bool P>
@@ -399,12 +426,12 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kBars];
   __shared__ uint32_t tmem_s, abort_s;
-  __shared__ int weight_s[kFewMost];
+  __shared__ int weight_s[kFewMost], seq_s[kFewMost];           // kFew: the rows' adapters, and their numbers among those of this CTA
   volatile uint32_t *abort_flag = &abort_s;
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sm = (smem_u32(smem_raw) + 1023u) & ~1023u;
   if (warp == 0) {
-    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? (P ? 2 : 1) * kEpi : i == kFixed && P ? 2 : i == kParts ? p.split * kEpi : 1);
+    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? (P ? 2 : 1) * kEpi : i == kFixed && P ? 2 : i == kParts ? p.split * kEpi : i >= kEEmpty ? kEpi / 2 : 1);
     if (lane == 0) abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   } else if (warp == 1 && lane < 4) {
@@ -466,19 +493,18 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n, tn = at - tm * p.tiles_n;
         const bool sums = p.sums && tn == p.tiles_n - 1;
         const int i0 = tm * kRows + half * 128, j0 = tn * p.nt + half * (p.nt / 2);
-        if (lead)
-          each_piece(p, weight, share, [&](int r, int) {
-            const uint32_t full = open(sums ? (uint32_t)(N * kP) : stage_bytes, 0x10000u);
-            if (!full) return false;
+        each_piece(p, weight, share, [&](int r, int) {
+          const uint32_t full = lead && ok ? open(sums ? (uint32_t)(N * kP) : stage_bytes, 0x10000u) : 0u;
+          if (full) {
             uint32_t a = sm + (uint32_t)stage * stage_bytes;
             for (int t = 0; t < N; ++t)
               for (int b = 0; b < 2; ++b, a += kBox) load_box<P>(a, &map_p, full, i0 + b * 64, t, r, 0);
             if (!sums)
               for (int t = 0; t < N; ++t)
                 for (int b = 0; b < p.q_bytes / kBox; ++b, a += kBox) load_box<P>(a, &map_q, full, j0 + b * 64, t, r, 0);
-            next();
-            return true;
-          });
+          }
+          next();
+        });
         ok = __all_sync(0xffffffffu, ok);
       }
     } else {
@@ -511,17 +537,24 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         }
         __syncwarp();
         if (adapters && p.early && item == team) asm volatile("griddepcontrol.wait;" ::: "memory");
+        int run_weight = 0;
         if (adapters)
-          each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](int, int, int weight) {
+          each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](const Run &run) { run_weight = run.weight; }, [&](int from) {
+            const int weight = __shfl_sync(0xffffffffu, run_weight, from);
             for (int c = 0; c < ext_uses; ++c, next()) {
               if (!lead || !ok) continue;
-              const uint32_t full = open(stage_bytes, 0x20000u);
+              const uint32_t full = open((uint32_t)(N * (p.t_bytes + p.e_bytes)), 0x20000u);
               if (!full) continue;
-              const int cc = c % p.rank_pieces;
+              const int cc = c < p.rank_pieces ? c : c - p.rank_pieces;
               const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
               for (int term = 0; term < N; ++term) {
                 load_box<P>(a + (uint32_t)(term * kP), &map_t, full, (c < p.rank_pieces ? 0 : grp::rank_pad(p.rank)) + cc * kPiece, term, row0, 0);
-                load_w(&map_e, b + (uint32_t)(term * p.q_bytes), full, cc * kPiece, term, weight);
+                const uint32_t to = b + (uint32_t)(term * p.q_bytes);
+                if (ACROSS) {
+                  for (int x = 0; x < p.q_bytes / kBox; ++x) load_box<P>(to + (uint32_t)(x * p.e_wide * 128), &map_e, full, n0 + x * 64, term, cc * kPiece, weight);
+                } else {
+                  load_box<P>(to, &map_e, full, cc * kPiece, term, n0, weight);
+                }
               }
             }
           });
@@ -552,47 +585,47 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       for (long long item = team; ok && item < p.most; item += teams) {
         const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n;
         const bool sums = p.sums && at - tm * p.tiles_n == p.tiles_n - 1;
-        if (lead) {
-          bool any = false;
-          begin();
-          const uint32_t idesc = (sums ? (base & ~(0x3Fu << 17)) | (uint32_t)(kRows / 64) << 17 : base) | (1u << 15) | (1u << 16);
-          if (ok)
-            each_piece(p, weight, share, [&](int, int rows) {
-              if (kShort && any) {
-                end(true);
-                begin();
-                any = false;
-              }
-              if (ok) ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x40000u | (uint32_t)stage, kLimit);
-              if (ok && rows % 16) {             // the last instruction's terms include rows of the next run
-                if (P) arrive_cluster(map_cluster(smem_u32(&bar[kAsk]), 1));
-                mbar_arrive(&bar[kAsk]);
-                ok = mbar_wait(&bar[kFixed], fixed & 1u, abort_flag, ws, 0x50000u | (uint32_t)stage);
-                if (P) mbar_acquire_cluster(&bar[kFixed], fixed & 1u);
-                ++fixed;
-              }
-              if (!ok) return false;
-              tc_fence_after();
-              const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
-              const int steps = (rows + 15) / 16;
+        bool any = false;
+        if (lead) begin();
+        const uint32_t idesc = (sums ? (base & ~(0x3Fu << 17)) | (uint32_t)(kRows / 64) << 17 : base) | (1u << 15) | (1u << 16);
+        each_piece(p, weight, share, [&](int, int rows) {
+          if (!lead || !ok) {
+            next();
+            return;
+          }
+          if (kShort && any) {
+            end(true);
+            begin();
+            any = false;
+          }
+          if (ok) ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x40000u | (uint32_t)stage, kLimit);
+          if (ok && rows % 16) {                 // the last instruction's terms include rows of the next run
+            if (P) arrive_cluster(map_cluster(smem_u32(&bar[kAsk]), 1));
+            mbar_arrive(&bar[kAsk]);
+            ok = mbar_wait(&bar[kFixed], fixed & 1u, abort_flag, ws, 0x50000u | (uint32_t)stage);
+            if (P) mbar_acquire_cluster(&bar[kFixed], fixed & 1u);
+            ++fixed;
+          }
+          if (!ok) return;
+          tc_fence_after();
+          const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
+          const int steps = (rows + 15) / 16;
 #pragma unroll
-              for (int x = 0; x < kPairs; ++x) {
-                if (sums && kTermQ[x] != 0) continue;              // of the block of ones there is one term
-                const uint64_t ad = desc_across(a + (uint32_t)(kTermP[x] * kP)), bd = desc_across(sums ? ones : b + (uint32_t)(kTermQ[x] * p.q_bytes));
-                if (steps == 4) {
+          for (int x = 0; x < kPairs; ++x) {
+            if (sums && kTermQ[x] != 0) continue;                  // of the block of ones there is one term
+            const uint64_t ad = desc_across(a + (uint32_t)(kTermP[x] * kP)), bd = desc_across(sums ? ones : b + (uint32_t)(kTermQ[x] * p.q_bytes));
+            if (steps == 4) {
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) umma<P>(d, ad + kStepOf<true> * k, bd + kStepOf<true> * k, idesc, any || k > 0 ? 1u : 0u);
-                } else {
-                  for (int k = 0; k < steps; ++k) umma<P>(d, ad + kStepOf<true> * k, bd + kStepOf<true> * k, idesc, any || k > 0 ? 1u : 0u);
-                }
-                any = true;
-              }
-              commit<P>(&bar[kEmpty + stage]);
-              next();
-              return true;
-            });
-          if (ok) end(any);
-        }
+              for (int k = 0; k < 4; ++k) umma<P>(d, ad + kStepOf<true> * k, bd + kStepOf<true> * k, idesc, any || k > 0 ? 1u : 0u);
+            } else {
+              for (int k = 0; k < steps; ++k) umma<P>(d, ad + kStepOf<true> * k, bd + kStepOf<true> * k, idesc, any || k > 0 ? 1u : 0u);
+            }
+            any = true;
+          }
+          commit<P>(&bar[kEmpty + stage]);
+          next();
+        });
+        if (lead && ok) end(any);
         ok = __all_sync(0xffffffffu, ok);
       }
     } else {
@@ -638,14 +671,18 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           for (int c = c0; c < c1; ++c) next();
         }
         __syncwarp();
+        uint32_t run_off[8];
         if (adapters)
-          each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](int first_row, int last_row, int) {
+          each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](const Run &run) {
+#pragma unroll
+            for (int i = 0; i < 2 * kRows / 64; ++i) {
+              const int lo = max(run.begin - t.row0 - 32 * i, 0), hi = min(run.end - t.row0 - 32 * i, 32);
+              run_off[i] = lo >= hi ? 0xffffffffu : ~((hi - lo == 32 ? 0xffffffffu : (1u << (hi - lo)) - 1u) << lo);
+            }
+          }, [&](int from) {
             uint32_t off[8];                     // lanes of other rows
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int lo = max(first_row - t.row0 - 32 * i, 0), hi = min(last_row - t.row0 - 32 * i, 32);
-              off[i] = lo >= hi ? 0xffffffffu : ~((hi - lo == 32 ? 0xffffffffu : (1u << (hi - lo)) - 1u) << lo);
-            }
+            for (int i = 0; i < 8; ++i) off[i] = i < 2 * kRows / 64 ? __shfl_sync(0xffffffffu, run_off[i], from) : 0u;
             bool first = own_pieces == 0;        // without a shared matrix the run's first instruction sets its lanes
             for (int c = 0; c < ext_uses; ++c, next()) {
               if (!lead || !ok) continue;
@@ -653,14 +690,16 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
               if (!ok) continue;
               tc_fence_after();
               const uint32_t a = sm + (uint32_t)stage * stage_bytes, b = a + (uint32_t)(N * kP);
-              const int steps = min(4, (p.rank - c % p.rank_pieces * kPiece + 15) / 16);
+              const int steps = min(4, (p.rank - (c < p.rank_pieces ? c : c - p.rank_pieces) * kPiece + 15) / 16);
+              const uint32_t t_row = (uint32_t)p.t_bytes / 128u;
+              auto e_desc = [&](uint32_t at) { return ACROSS ? desc_short(at, (uint32_t)p.e_wide) : desc_narrow(at, (uint32_t)p.e_wide * 2u); };
               if (N == 3) {
 #pragma unroll
                 for (int x = 0; x < kPairs; ++x)
                   for (int k = 0; k < steps; ++k, first = false)
-                    umma_lanes<P>(d, desc_along(a + (uint32_t)(kTermP[x] * kP)) + kStepOf<false> * k, desc_of<kB>(b + (uint32_t)(kTermQ[x] * p.q_bytes)) + kStepOf<kB> * k, idesc, first ? 0u : 1u, off);
+                    umma_lanes<P>(d, desc_narrow(a + (uint32_t)(kTermP[x] * kP), t_row) + kStepOf<false> * k, e_desc(b + (uint32_t)(kTermQ[x] * p.q_bytes)) + kStepOf<kB> * k, idesc, first ? 0u : 1u, off);
               } else {
-                const uint64_t ad = desc_along(a), bd = desc_of<kB>(b);
+                const uint64_t ad = desc_narrow(a, t_row), bd = e_desc(b);
                 for (int k = 0; k < steps; ++k, first = false) umma_lanes<P>(d, ad + kStepOf<false> * k, bd + kStepOf<kB> * k, idesc, first ? 0u : 1u, off);
                 if (p.rank <= 32)                // the low terms lie behind the high ones
                   for (int k = 0; k < steps; ++k) umma_lanes<P>(d, ad + kStepOf<false> * (steps + k), bd + kStepOf<kB> * k, idesc, 1u, off);
@@ -918,30 +957,17 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       walk.start();
       Tile t;
       const int half_rows = p.nt / 2;            // of a set of four warps
-      const uint32_t ts = sm + (uint32_t)p.off_t, es = ts + (uint32_t)(p.rank ? p.nt * grp::rank_pad(p.rank) * 4 : 0), parts = es + (uint32_t)(p.rank ? p.nt * 512 : 0);
+      const int pad = grp::rank_pad(p.rank);
+      const uint32_t ts = sm + (uint32_t)p.off_t, es = ts + (uint32_t)(p.nt * pad * 4), parts = es + (uint32_t)(p.rank ? p.nt * 512 : 0);
       const int part_rows = (p.nt + p.split - 1) / p.split;
-      // The rows that this thread delivers, one after the other: of a cluster's CTAs each has every split-th row of the tile.
-      auto row_of = [&](int v) { return p.split == 1 ? set * half_rows + v : share + p.split * (2 * v + set); };
-      auto rows_here = [&](int count) { return p.split == 1 ? min(half_rows, count - set * half_rows) : (count - share - set * p.split + 2 * p.split - 1) / (2 * p.split); };
+      const uint32_t ring = parts + (uint32_t)(p.split > 1 ? p.split * part_rows * 512 : 0);
       for (long long item = team; item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
-        const int o = t.tn * 128 + own, count = min(p.nt, t.end - t.row0), here = rows_here(count);
+        // Of a cluster's CTAs each has every split-th row of the tile; of those each set of four warps every second one.
+        const int o = t.tn * 128 + own, count = min(p.nt, t.end - t.row0), here = count > share ? (count - share - 1) / p.split + 1 : 0;
         if (p.rank) {
-          // the adapters' part of the rows that this thread delivers, while the shared matrix is multiplied
-          const int pad = grp::rank_pad(p.rank);
-          bar_sync(1, kEpi * 32);                // the last item's are read
-          if (unit < p.nt) weight_s[unit] = unit < count ? adapter_of(p.ext, t.row0 + unit) : -1;
-          bar_sync(1, kEpi * 32);
-          auto matrix_of = [&](int w) {
-            return reinterpret_cast<const T *>(p.e) + (ACROSS ? (size_t)w * (size_t)p.rank * (size_t)p.e_pitch + (size_t)o : ((size_t)w * (size_t)p.n + (size_t)o) * (size_t)p.e_pitch);
-          };
-          if (!ACROSS && !waited && o < p.n) {   // on their way from memory while the launch in front ends
-#pragma unroll 1
-            for (int v0 = 0; v0 < here; ++v0) {
-              const int w = weight_s[row_of(v0)];
-              if (w < 0) continue;
-              for (int j0 = 0; j0 < p.rank; j0 += 128 / (int)sizeof(T)) asm volatile("prefetch.global.L2 [%0];" ::"l"(matrix_of(w) + j0));
-            }
-          }
+          // the adapters' part of those rows, while the shared matrix is multiplied
+          bar_sync(1, kEpi * 32 + 32);           // the last item's are read
+          bar_sync(1, kEpi * 32 + 32);           // the rows' adapters are there
           if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
           waited = true;
 #pragma unroll 1
@@ -949,53 +975,73 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
             const int r = i / pad;
             sts_f(ts + (uint32_t)(i * 4), kept<T>(p.t, t.row0 + r, pad, i - r * pad));
           }
-          bar_sync(1, kEpi * 32);
-          constexpr int kAtOnce = sizeof(T) == 2 && !ACROSS ? 8 : 4;         // rows, for as many loads on their way
+          bar_sync(2, kEpi * 32);
+          if (sizeof(T) == 2) {
+            // Rows of the ring's slots would lie in the same banks for neighbouring lanes: each lane begins with another piece of 8 numbers.
+            const int chunks = (p.rank + 7) / 8, turned = own * (p.e_pitch / 8) / 8 % chunks;
 #pragma unroll 1
-          for (int v0 = 0; v0 < here; v0 += kAtOnce) {
-            int w[kAtOnce], r[kAtOnce];
-            float sum[kAtOnce];
-#pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
-              w[i] = v0 + i < here && o < p.n ? weight_s[row_of(v0 + i)] : -1;
-              r[i] = w[i] >= 0 ? row_of(v0 + i) : 0;
-              sum[i] = 0.f;
-            }
-            // numbers j0 to j0 + 7 of the rank.  Rows without an adapter are not multiplied: t may be no number there.
-            auto add = [&](int i, int j0, const float *e) {
-              const uint32_t at = ts + (uint32_t)((r[i] * pad + j0) * 4);
-              const uint4 t0 = lds_u4(at), t1 = lds_u4(at + 16);
-              const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
-#pragma unroll
-              for (int x = 0; x < 8; ++x)
-                if (w[i] >= 0) sum[i] = fmaf(__uint_as_float(tv[x]), e[x], sum[i]);
-            };
-            if (sizeof(T) == 2 && !ACROSS) {
+            for (int q = set; q < here; q += 2) {
+              const int r = share + p.split * q, seq = seq_s[r];
+              float sum = 0.f;
+              if (seq >= 0) {
+                const int slot = seq % p.slots;
+                const uint32_t e = ring + (uint32_t)(slot * p.slot_bytes), tr = ts + (uint32_t)(r * pad * 4);
+                if (warp_wait(&bar[kEFull + slot], (uint32_t)(seq / p.slots) & 1u, abort_flag, ws, 0xA0000u | (uint32_t)slot)) {
+                  if (ACROSS) {
+                    float some[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-              for (int j0 = 0; j0 < p.rank; j0 += 16) {
-                uint4 raw[kAtOnce][2];
+                    for (int j0 = 0; j0 < p.rank; j0 += 8) {
+                      const uint4 t0 = lds_u4(tr + (uint32_t)(j0 * 4)), t1 = lds_u4(tr + (uint32_t)(j0 * 4 + 16));
+                      const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
-                for (int i = 0; i < kAtOnce; ++i)
+                      for (int x = 0; x < 8; ++x) {
+                        uint16_t h;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(e + (uint32_t)(min(j0 + x, p.rank - 1) * 256 + own * 2)) : "memory");
+                        if (j0 + x < p.rank) some[x & 3] = fmaf(__uint_as_float(tv[x]), __uint_as_float((uint32_t)h << 16), some[x & 3]);
+                      }
+                    }
+                    sum = (some[0] + some[1]) + (some[2] + some[3]);
+                  } else {
+                    float some[2] = {0.f, 0.f};
+                    int c = turned;
+#pragma unroll 4
+                    for (int i = 0; i < chunks; ++i) {
+                      const uint4 raw = lds_u4(e + (uint32_t)(own * p.e_pitch * 2 + c * 16)), t0 = lds_u4(tr + (uint32_t)(c * 32)), t1 = lds_u4(tr + (uint32_t)(c * 32 + 16));
+                      const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
+                      float v[8];
+                      unpack8(raw, v);
 #pragma unroll
-                  for (int h = 0; h < 2; ++h)
-                    raw[i][h] = w[i] >= 0 && j0 + 8 * h < p.rank ? __ldg(reinterpret_cast<const uint4 *>(matrix_of(w[i]) + j0 + 8 * h)) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i)
-#pragma unroll
-                  for (int h = 0; h < 2; ++h) {
-                    float e[8];
-                    unpack8(raw[i][h], e);
-                    add(i, j0 + 8 * h, e);       // (the rank's padding is a multiple of 16: t is 0 there)
+                      for (int x = 0; x < 8; ++x) some[x & 1] = fmaf(__uint_as_float(tv[x]), v[x], some[x & 1]);
+                      c = c + 1 == chunks ? 0 : c + 1;
+                    }
+                    sum = some[0] + some[1];
                   }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar[kEEmpty + slot]);
               }
-            } else {
+              sts_f(part_at(es, r), sum);
+            }
+          } else {
+            constexpr int kAtOnce = 4;           // rows, for as many loads on their way
+#pragma unroll 1
+            for (int q0 = set; q0 < here; q0 += 2 * kAtOnce) {
+              int w[kAtOnce], r[kAtOnce];
+              float sum[kAtOnce];
+#pragma unroll
+              for (int i = 0; i < kAtOnce; ++i) {
+                r[i] = q0 + 2 * i < here ? share + p.split * (q0 + 2 * i) : -1;
+                w[i] = r[i] >= 0 && o < p.n ? weight_s[r[i]] : -1;
+                sum[i] = 0.f;
+              }
 #pragma unroll 1
               for (int j0 = 0; j0 < p.rank; j0 += 8) {
                 float e[kAtOnce][8];
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
-                  const T *at = matrix_of(max(w[i], 0)) + (ACROSS ? (size_t)j0 * (size_t)p.e_pitch : (size_t)j0);
-                  if (sizeof(T) == 4 && !ACROSS && p.e_vec) {
+                  const T *at = reinterpret_cast<const T *>(p.e) + (ACROSS ? ((size_t)max(w[i], 0) * (size_t)p.rank + (size_t)j0) * (size_t)p.e_pitch + (size_t)o
+                                                                           : ((size_t)max(w[i], 0) * (size_t)p.n + (size_t)o) * (size_t)p.e_pitch + (size_t)j0);
+                  if (!ACROSS && p.e_vec) {
 #pragma unroll
                     for (int x = 0; x < 8; x += 4) {
                       float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1008,13 +1054,21 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
                   }
                 }
 #pragma unroll
-                for (int i = 0; i < kAtOnce; ++i) add(i, j0, e[i]);
-              }
-            }
+                for (int i = 0; i < kAtOnce; ++i) {
+                  if (w[i] < 0) continue;        // t may be no number there
+                  const uint32_t at = ts + (uint32_t)((r[i] * pad + j0) * 4);
+                  const uint4 t0 = lds_u4(at), t1 = lds_u4(at + 16);
+                  const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i)
-              if (v0 + i < here) sts_f(part_at(es, row_of(v0 + i)), sum[i]);
+                  for (int x = 0; x < 8; ++x) sum[i] = fmaf(__uint_as_float(tv[x]), e[i][x], sum[i]);
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < kAtOnce; ++i)
+                if (r[i] >= 0) sts_f(part_at(es, r[i]), sum[i]);
+            }
           }
+          if (p.split == 1) bar_sync(2, kEpi * 32);       // rows are then delivered by whom their sums lie with
         }
         const float b = p.bias && o < p.n ? __ldg(p.bias + (p.bias_each ? (size_t)t.weight * (size_t)p.n : 0) + (size_t)o) : 0.f;
         auto deliver = [&](int r, float v) {     // row r of the tile: its sum
@@ -1093,17 +1147,72 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           if (warp_wait(&bar[kParts], 0, abort_flag, ws, 0x90000u, kLimit) && ok) {
             mbar_acquire_cluster(&bar[kParts], 0);
 #pragma unroll 1
-            for (int v0 = 0; v0 < here; ++v0) {
-              const int r = row_of(v0);
-              float v = 0.f;
-              for (int k = 0; k < p.split; ++k) v += lds_f(part_at(parts, k * part_rows + r / p.split));
-              deliver(r, v);
+            for (int q0 = set; q0 < here; q0 += 8) {
+              float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+              for (int k = 0; k < p.split; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += q0 + 2 * i < here ? lds_f(part_at(parts, k * part_rows + q0 + 2 * i)) : 0.f;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (q0 + 2 * i < here) deliver(share + p.split * (q0 + 2 * i), v[i]);
             }
           }
         }
       }
       if (p.split > 1 && met == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
+  } else if (FORM == kFew) {
+    // ---------------------------------------------------------------- kFew: which adapters rows have; bf16: their parts of the tile's columns
+    const uint32_t ring = sm + (uint32_t)(p.off_t + p.nt * grp::rank_pad(p.rank) * 4 + p.nt * 512 + (p.split > 1 ? p.split * ((p.nt + p.split - 1) / p.split) * 512 : 0));
+    grp::Walk walk;
+    walk.start();
+    Tile t;
+    int seq = 0;                                 // adapters of rows so far
+    if (p.rank)
+      for (long long item = team; item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
+        const int count = min(p.nt, t.end - t.row0), here = count > share ? (count - share - 1) / p.split + 1 : 0, first = seq, o0 = t.tn * 128;
+        bar_sync(1, kEpi * 32 + 32);
+        for (int i = lane; i < p.nt; i += 32) weight_s[i] = -1;
+        __syncwarp();
+        each_run(p.ext, t.row0, t.row0 + count, [&](const Run &run) {
+          for (int i = max(run.begin - t.row0, 0); i < min(run.end - t.row0, count); ++i) weight_s[i] = run.weight;
+        }, [](int) {});
+        __syncwarp();
+        for (int q0 = 0; q0 < here; q0 += 32) {
+          const int r = share + p.split * (q0 + lane);
+          const bool has = q0 + lane < here && weight_s[r] >= 0;
+          const unsigned all = __ballot_sync(0xffffffffu, has);
+          if (q0 + lane < here) seq_s[r] = has ? seq + __popc(all & ((1u << lane) - 1u)) : -1;
+          seq += __popc(all);
+        }
+        __syncwarp();
+        bar_sync(1, kEpi * 32 + 32);
+        if (sizeof(T) == 2) {
+          int at = first;
+          for (int q = 0; q < here; ++q) {
+            const int w = weight_s[share + p.split * q];
+            if (w < 0) continue;
+            const int slot = at % p.slots;
+            ok = ok && warp_wait(&bar[kEEmpty + slot], ((uint32_t)(at / p.slots) & 1u) ^ 1u, abort_flag, ws, 0xB0000u | (uint32_t)slot);
+            ++at;
+            if (!ok) continue;
+            const uint32_t to = ring + (uint32_t)(slot * p.slot_bytes);
+            const bf16 *e = reinterpret_cast<const bf16 *>(p.e);
+            if (ACROSS) {                        // `rank` rows of the tile's columns
+              const uint32_t bytes = (uint32_t)min(128, p.e_pitch - o0) * 2u;
+              if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)p.rank);
+              __syncwarp();
+              for (int j = lane; j < p.rank; j += 32) bulk_load(to + (uint32_t)(j * 256), e + ((size_t)w * (size_t)p.rank + (size_t)j) * (size_t)p.e_pitch + (size_t)o0, bytes, &bar[kEFull + slot]);
+            } else if (lane == 0) {              // the columns' rows, one piece
+              const uint32_t bytes = (uint32_t)(min(128, p.n - o0) * p.e_pitch) * 2u;
+              mbar_arrive_expect_tx(&bar[kEFull + slot], bytes);
+              bulk_load(to, e + ((size_t)w * (size_t)p.n + (size_t)o0) * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
+            }
+            __syncwarp();
+          }
+        }
+      }
   } else {
     // ---------------------------------------------------------------- kGrad: rows behind the end of a run are set to zero, once they are there
     uint32_t asked = 0;
@@ -1111,9 +1220,9 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n;
       const bool sums = p.sums && at - tm * p.tiles_n == p.tiles_n - 1;
       each_piece(p, weight, share, [&](int, int rows) {
-        if (rows % 16) {
+        if (ok && rows % 16) {
           ok = warp_wait(&bar[kAsk], asked & 1u, abort_flag, ws, 0x80000u, kLongNs);
-          if (!ok) return false;
+          if (!ok) return;
           if (P) mbar_acquire_cluster(&bar[kAsk], asked & 1u);
           ++asked;
           const uint32_t a = sm + (uint32_t)stage * stage_bytes;
@@ -1128,7 +1237,6 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           }
         }
         next();
-        return true;
       });
     }
   }
@@ -1136,7 +1244,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   if (p.early) asm volatile("griddepcontrol.wait;" ::: "memory");        // this launch does not end before the one in front of it
   if (FORM == kFew) {
     if (p.split > 1) {
-      if (warp < 2) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+      if (warp < 2 || warp >= 2 + kEpi) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
       if (*abort_flag) {                         // parts may still be on their way here: until the other CTAs are done too, or 20 ms
         const unsigned long long t0 = globaltimer_ns();
         while (globaltimer_ns() - t0 < 20ull * 1000ull * 1000ull) __nanosleep(1000);
@@ -1227,7 +1335,8 @@ __global__ void __launch_bounds__(256) k_adapter_narrow(const T *__restrict__ x,
   };
   ask(xr, xv, lane * kPer);                      // while the run is looked for
   int w = -1;
-  each_run(runs, row, row + 1, [&](int begin, int end, int weight) { if (begin <= row && row < end) w = weight; });
+  each_run(runs, row, row + 1, [&](const Run &run) { if (run.begin <= row && row < run.end) w = run.weight; }, [](int) {});
+  w = __reduce_max_sync(0xffffffffu, w);
   if (w < 0) return;
   float s = 0.f;
   if (j < rank) {
@@ -1276,15 +1385,15 @@ EncodeTiledFn get_encode_fn() {
   }
   return fn;
 }
-// [outer][rows][terms][cols], rows of a term `pitch` elements: boxes of 64 columns x `box` rows, zeros outside
-bool map_of(CUtensorMap *map, const void *at, long long cols, int terms, long long rows, long long outer, long long pitch, int box) {
+// [outer][rows][terms][cols], rows of a term `pitch` elements: boxes of `wide` columns (16, 32 or 64) x `box` rows, zeros outside
+bool map_of(CUtensorMap *map, const void *at, long long cols, int terms, long long rows, long long outer, long long pitch, int box, int wide = kPiece) {
   EncodeTiledFn encode = get_encode_fn();
   if (!encode) return false;
   const cuuint64_t one = (cuuint64_t)pitch * 2;
   const cuuint64_t dim[4] = {(cuuint64_t)cols, (cuuint64_t)terms, (cuuint64_t)rows, (cuuint64_t)outer}, str[3] = {one, one * (cuuint64_t)terms, one * (cuuint64_t)terms * (cuuint64_t)rows};
-  const cuuint32_t bx[4] = {kPiece, 1, (cuuint32_t)box, 1}, es[4] = {1, 1, 1, 1};
+  const cuuint32_t bx[4] = {(cuuint32_t)wide, 1, (cuuint32_t)box, 1}, es[4] = {1, 1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(at), dim, str, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                wide == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : wide == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int FORM, bool ACROSS, typename T, bool P>
@@ -1419,13 +1528,19 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   if (by_few) {
     const int mean = j.rows / runs;
     p.nt = mean <= (runs == 1 ? 16 : 12) ? 16 : mean <= (runs == 1 ? 32 : 24) ? 32 : 64;
-    if (wide && p.nt > kFewWide) p.nt = kFewWide;
+    if ((wide || j.rank > 64) && p.nt > kFewWide) p.nt = kFewWide;
     p.q_bytes = p.nt * 128;
     p.tiles_n = dc_div_up(j.n, 128);
     items = row_tiles(j.runs, p.nt) * p.tiles_n;
     p.split = split_of(items, p.pieces, 4, n_sm);
     p.early = early;
-    lay_out(&p, terms, (p.rank ? p.nt * (rank_pad(p.rank) * 4 + 512) : 0) + (p.split > 1 ? (p.nt + p.split) * 512 : 0));
+    int apart = (p.rank ? p.nt * (rank_pad(p.rank) * 4 + 512) : 0) + (p.split > 1 ? (p.nt + p.split) * 512 : 0);
+    if (p.rank && !wide) {
+      p.slot_bytes = j.e_across ? p.rank * 256 : 128 * p.e_pitch * 2;
+      p.slots = 65536 / p.slot_bytes < kMaxSlots ? 65536 / p.slot_bytes : kMaxSlots;
+      apart += p.slots * p.slot_bytes;
+    }
+    lay_out(&p, terms, apart);
   } else {
     if (j.y_terms) {
       p.nt = rank_pad(j.n);
@@ -1455,9 +1570,14 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
       return cudaErrorNotSupported;
   }
   if (j.t && !by_few) {
-    const int pad = rank_pad(j.rank);            // bf16: both terms as one row
-    if (!(wide ? map_of(&m[2], j.t, pad, 3, j.rows, 1, pad, 128) : map_of(&m[2], j.t, 2 * pad, 1, j.rows, 1, 2 * pad, 128))) return cudaErrorNotSupported;
-    if (!(j.e_across ? map_of(&m[3], j.e, j.n, terms, j.rank, j.ext.weights, j.e_pitch, 64) : map_of(&m[3], j.e, j.rank, terms, j.n, j.ext.weights, j.e_pitch, box)))
+    // Rows no wider than the rank: what lies outside a box costs a load as much as what is there (16 numbers a row in boxes of 64: 1100 cycles a run).
+    const int pad = rank_pad(j.rank), row = pad <= 16 ? 16 : pad <= 32 ? 32 : 64;
+    p.e_wide = row;
+    p.e_bytes = j.e_across ? p.q_bytes / kBox * row * 128 : box * row * 2;
+    const int t_wide = wide ? row : pad <= 16 ? 32 : 64;             // bf16: both terms as one row
+    p.t_bytes = 128 * t_wide * 2;
+    if (!(wide ? map_of(&m[2], j.t, pad, 3, j.rows, 1, pad, 128, t_wide) : map_of(&m[2], j.t, 2 * pad, 1, j.rows, 1, 2 * pad, 128, t_wide))) return cudaErrorNotSupported;
+    if (!(j.e_across ? map_of(&m[3], j.e, j.n, terms, j.rank, j.ext.weights, j.e_pitch, row) : map_of(&m[3], j.e, j.rank, terms, j.n, j.ext.weights, j.e_pitch, box, row)))
       return cudaErrorNotSupported;
   }
   const bool across = j.w ? j.w_across : j.e_across;

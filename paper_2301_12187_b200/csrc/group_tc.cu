@@ -324,31 +324,22 @@ static __device__ __noinline__ float again_grad(const Params &p, int weight, int
   return s;
 }
 
-// What a lane delivers of a block of 32 rows x 32 columns: 4 columns of every fourth row.  Its part of the residual, asked for ahead:
+// What a lane delivers of a block of 32 rows x 32 columns: 4 columns of every fourth row.  bf16: its part of the residual, asked for ahead (fp32 has no registers
+// to spare: what it asks for ahead is nothing).
 template <typename T>
-struct Ahead { uint4 v[sizeof(T) == 4 ? 8 : 4]; };
+struct Ahead { uint2 v[sizeof(T) == 4 ? 1 : 8]; };
 template <typename T>
-__device__ __forceinline__ void ask_block(const Params &p, Ahead<T> &a, const T *residual, size_t pitch, int rows, int cols) {
+__device__ __forceinline__ void ask_block(Ahead<T> &a, const T *residual, size_t pitch, int rows, int cols) {
   const int lane = (int)(threadIdx.x & 31u), piece = lane & 7, r0 = lane >> 3;
+  const T *at = residual + (size_t)r0 * pitch + (size_t)(piece * 4);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = i * 4 + r0;
-    const bool here = residual && row < rows && piece * 4 < cols;
-    const T *at = residual + (size_t)row * pitch + (size_t)(piece * 4);
-    if (sizeof(T) == 4) {
-      a.v[sizeof(T) == 4 ? i : 0] = here ? *reinterpret_cast<const uint4 *>(at) : make_uint4(0, 0, 0, 0);
-    } else {
-      const uint2 u = here ? *reinterpret_cast<const uint2 *>(at) : make_uint2(0, 0);
-      uint4 &w = a.v[i >> 1];
-      if (i & 1) { w.z = u.x; w.w = u.y; }
-      else { w.x = u.x; w.y = u.y; }
-    }
-  }
+  for (int i = 0; i < 8; ++i, at += 4 * pitch)
+    if (sizeof(T) == 2) a.v[sizeof(T) == 2 ? i : 0] = i * 4 + r0 < rows && piece * 4 < cols ? *reinterpret_cast<const uint2 *>(at) : make_uint2(0, 0);
 }
 // 32 sums of each lane's row -> rows of y, `rows` x `cols` of them, through shared memory: a row's results then go out side by side
 template <typename T>
 __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, const float (&v)[32], T *y, size_t pitch, int rows, int cols, const float *bias, const T *residual,
-                                            const Ahead<T> *ahead) {
+                                            const Ahead<T> &ahead) {
   const int lane = (int)(threadIdx.x & 31u);
   __syncwarp();
 #pragma unroll
@@ -360,32 +351,42 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
     const int piece = lane & 7, r0 = lane >> 3;
     if (piece * 4 >= cols) return;
     const float4 b = bias ? __ldg(reinterpret_cast<const float4 *>(bias) + piece) : make_float4(0.f, 0.f, 0.f, 0.f);
-    uint4 w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = lds_u4(stage + (uint32_t)((i * 4 + r0) * 128 + ((piece ^ ((i * 4 + r0) & 7)) * 16)));
+    constexpr int kAtOnce = sizeof(T) == 4 ? 4 : 8;
     T *at = y + (size_t)r0 * pitch + (size_t)(piece * 4);
+    const T *res = residual + (size_t)r0 * pitch + (size_t)(piece * 4);
 #pragma unroll
-    for (int i = 0; i < 8; ++i, at += 4 * pitch) {
-      float f[4] = {__uint_as_float(w[i].x), __uint_as_float(w[i].y), __uint_as_float(w[i].z), __uint_as_float(w[i].w)};
-      if (bias) { f[0] += b.x; f[1] += b.y; f[2] += b.z; f[3] += b.w; }
-      if (ahead) {
-        if (sizeof(T) == 4) {
-          const uint4 u = ahead->v[sizeof(T) == 4 ? i : 0];
-          f[0] += __uint_as_float(u.x); f[1] += __uint_as_float(u.y); f[2] += __uint_as_float(u.z); f[3] += __uint_as_float(u.w);
-        } else {
-          const uint4 w2 = ahead->v[i >> 1];
-          const uint2 u = i & 1 ? make_uint2(w2.z, w2.w) : make_uint2(w2.x, w2.y);
-          f[0] += __uint_as_float(u.x << 16); f[1] += __uint_as_float(u.x & 0xffff0000u);
-          f[2] += __uint_as_float(u.y << 16); f[3] += __uint_as_float(u.y & 0xffff0000u);
+    for (int i0 = 0; i0 < 8; i0 += kAtOnce) {
+      uint4 w[kAtOnce], r[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int row = (i0 + i) * 4 + r0;
+        w[i] = lds_u4(stage + (uint32_t)(row * 128 + ((piece ^ (row & 7)) * 16)));
+        if (sizeof(T) == 4 && residual) {
+          r[i] = row < rows ? *reinterpret_cast<const uint4 *>(res) : make_uint4(0, 0, 0, 0);
+          res += 4 * pitch;
         }
       }
-      if (p.act) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) f[x] = dc_act_apply(f[x], DC_ACT_RELU6);
-      }
-      if (i * 4 + r0 < rows) {
-        if (sizeof(T) == 4) *reinterpret_cast<float4 *>(at) = make_float4(f[0], f[1], f[2], f[3]);
-        else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+      for (int i = 0; i < kAtOnce; ++i, at += 4 * pitch) {
+        float f[4] = {__uint_as_float(w[i].x), __uint_as_float(w[i].y), __uint_as_float(w[i].z), __uint_as_float(w[i].w)};
+        if (bias) { f[0] += b.x; f[1] += b.y; f[2] += b.z; f[3] += b.w; }
+        if (residual) {
+          if (sizeof(T) == 4) {
+            f[0] += __uint_as_float(r[i].x); f[1] += __uint_as_float(r[i].y); f[2] += __uint_as_float(r[i].z); f[3] += __uint_as_float(r[i].w);
+          } else {
+            const uint2 u = ahead.v[sizeof(T) == 2 ? i : 0];
+            f[0] += __uint_as_float(u.x << 16); f[1] += __uint_as_float(u.x & 0xffff0000u);
+            f[2] += __uint_as_float(u.y << 16); f[3] += __uint_as_float(u.y & 0xffff0000u);
+          }
+        }
+        if (p.act) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) f[x] = dc_act_apply(f[x], DC_ACT_RELU6);
+        }
+        if ((i0 + i) * 4 + r0 < rows) {
+          if (sizeof(T) == 4) *reinterpret_cast<float4 *>(at) = make_float4(f[0], f[1], f[2], f[3]);
+          else *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+        }
       }
     }
     return;
@@ -846,7 +847,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
                 if (j0 + x < p.n && c + x < cols) out[(size_t)(j0 + x) * (size_t)p.k + (size_t)i] = (T)v[x];
             }
           } else if (i0 < p.k) {
-            store_block<T>(p, staged, v, out + (size_t)i0 * (size_t)p.n + (size_t)j0, (size_t)p.n, min(32, p.k - i0), min(min(32, cols - c), p.n - j0), nullptr, nullptr, nullptr);
+            store_block<T>(p, staged, v, out + (size_t)i0 * (size_t)p.n + (size_t)j0, (size_t)p.n, min(32, p.k - i0), min(min(32, cols - c), p.n - j0), nullptr, (const T *)nullptr, Ahead<T>());
           }
         };
         if (P || p.split == 1) {
@@ -879,19 +880,18 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         const bool residual = p.residual && p.vec;
         auto ask = [&](int c) {
           const int o0 = t.tn * p.nt + c;
-          if (residual && row0 < t.end && c < p.nt && o0 < p.n)
-            ask_block<T>(p, next_residual, reinterpret_cast<const T *>(p.residual) + (size_t)row0 * (size_t)p.n + (size_t)o0, (size_t)p.n, min(32, t.end - row0), min(min(32, p.nt - c), p.n - o0));
+          if (sizeof(T) == 2 && residual && row0 < t.end && c < p.nt && o0 < p.n)
+            ask_block<T>(next_residual, reinterpret_cast<const T *>(p.residual) + (size_t)row0 * (size_t)p.n + (size_t)o0, (size_t)p.n, min(32, t.end - row0), min(min(32, p.nt - c), p.n - o0));
         };
         const int c_first = p.split > 1 ? (rank + set * p.split) * 32 : set * 32, c_step = 64 * p.split;
         if (residual && row < t.end)             // to L2, while the tile is multiplied
           for (int c = set * 64; c < p.nt; c += 128)
             if (t.tn * p.nt + c < p.n) asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const T *>(p.residual) + (size_t)row * (size_t)p.n + (size_t)(t.tn * p.nt + c)));
-        if (!kShort) ask(c_first);               // (fp32 has no registers to spare)
+        ask(c_first);
         auto deliver = [&](int c, float (&v)[32]) {
           const int o0 = t.tn * p.nt + c;
-          if (kShort) ask(c);
           const Ahead<T> now = next_residual;
-          if (!kShort) ask(c + c_step);
+          ask(c + c_step);
           if (row0 >= t.end) return;
           if (p.alpha || p.pieces == 0) {
 #pragma unroll
@@ -933,7 +933,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           }
           const size_t at = (size_t)row0 * (size_t)p.n + (size_t)o0;
           store_block<T>(p, staged, v, reinterpret_cast<T *>(p.y) + at, (size_t)p.n, min(32, t.end - row0), min(min(32, p.nt - c), p.n - o0), bias ? bias + o0 : nullptr,
-                         p.residual ? reinterpret_cast<const T *>(p.residual) + at : nullptr, residual ? &now : nullptr);
+                         p.residual ? reinterpret_cast<const T *>(p.residual) + at : nullptr, now);
         };
         if (P || p.split == 1) {
           ok = read_out(max(own_pieces, 1), false, p.nt, 0, deliver);
@@ -1004,7 +1004,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
                   } else {
                     float some[2] = {0.f, 0.f};
                     int c = turned;
-#pragma unroll 4
+#pragma unroll 2
                     for (int i = 0; i < chunks; ++i) {
                       const uint4 raw = lds_u4(e + (uint32_t)(own * p.e_pitch * 2 + c * 16)), t0 = lds_u4(tr + (uint32_t)(c * 32)), t1 = lds_u4(tr + (uint32_t)(c * 32 + 16));
                       const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};

@@ -410,7 +410,7 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
   }
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kDFull = 2 * kMaxStages, kDEmpty = kDFull + 2, kAsk = kDEmpty + 2, kFixed, kParts, kEFull, kEEmpty = kEFull + kMaxSlots, kBars = kEEmpty + kMaxSlots };
+enum { kFull = 0, kEmpty = kMaxStages, kTail = 2 * kMaxStages, kReady = 3 * kMaxStages, kDFull = 4 * kMaxStages, kDEmpty = kDFull + 2, kParts = kDEmpty + 2, kEFull, kEEmpty = kEFull + kMaxSlots, kBars = kEEmpty + kMaxSlots };
 
 // P: in pairs.  ACROSS: the matrices' sums run across their rows (of both operands of a gradient always).
 template <int FORM, bool ACROSS, typename T, bool P>
@@ -432,7 +432,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sm = (smem_u32(smem_raw) + 1023u) & ~1023u;
   if (warp == 0) {
-    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? (P ? 2 : 1) * kEpi : i == kFixed && P ? 2 : i == kParts ? p.split * kEpi : i >= kEEmpty ? kEpi / 2 : 1);
+    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? (P ? 2 : 1) * kEpi : i >= kReady && i < kReady + kMaxStages && P ? 2 : i == kParts ? p.split * kEpi : i >= kEEmpty ? kEpi / 2 : 1);
     if (lane == 0) abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   } else if (warp == 1 && lane < 4) {
@@ -483,9 +483,13 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
     // ---------------------------------------------------------------- load
     const bool lead = elect_one();
     // waits for the next stage: its barrier's address for loads, or 0
-    auto open = [&](uint32_t bytes, uint32_t site) -> uint32_t {
+    auto open = [&](uint32_t bytes, uint32_t site, bool tail = false) -> uint32_t {
       ok = mbar_wait(&bar[kEmpty + stage], parity ^ 1u, abort_flag, ws, site | (uint32_t)stage, kLimit);
       if (!ok) return 0u;
+      if (FORM == kGrad && tail) {               // passed on by a warp of this CTA
+        mbar_arrive_expect_tx(&bar[kTail + stage], bytes);
+        return P ? map_cluster(smem_u32(&bar[kTail + stage]), (uint32_t)rank) : smem_u32(&bar[kTail + stage]);
+      }
       if (!P || rank == 0) mbar_arrive_expect_tx(&bar[kFull + stage], (P ? 2u : 1u) * bytes);
       return P ? map_cluster(smem_u32(&bar[kFull + stage]), 0) : smem_u32(&bar[kFull + stage]);
     };
@@ -494,8 +498,8 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n, tn = at - tm * p.tiles_n;
         const bool sums = p.sums && tn == p.tiles_n - 1;
         const int i0 = tm * kRows + half * 128, j0 = tn * p.nt + half * (p.nt / 2);
-        each_piece(p, weight, share, [&](int r, int) {
-          const uint32_t full = lead && ok ? open(sums ? (uint32_t)(N * kP) : stage_bytes, 0x10000u) : 0u;
+        each_piece(p, weight, share, [&](int r, int rows) {
+          const uint32_t full = lead && ok ? open(sums ? (uint32_t)(N * kP) : stage_bytes, 0x10000u, rows % 16 != 0) : 0u;
           if (full) {
             uint32_t a = sm + (uint32_t)stage * stage_bytes;
             for (int t = 0; t < N; ++t)
@@ -565,7 +569,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   } else if (warp == 1) {
     // ---------------------------------------------------------------- multiply: one lane issues, without the others (of a pair, the first CTA's)
     const bool lead = elect_one() && (!P || rank == 0);
-    uint32_t fixed = 0;                          // pieces with rows that were set to zero
+    uint32_t fulls = 0, tails = 0;               // kGrad: phases of each stage's barriers, of whole pieces and of those at a run's end
     const uint32_t base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows >> 4) << 24) | ((uint32_t)(p.nt >> 3) << 17);
     uint32_t d = 0;
     auto begin = [&]() {                         // the next accumulator
@@ -599,13 +603,14 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
             begin();
             any = false;
           }
-          if (ok) ok = mbar_wait(&bar[kFull + stage], parity, abort_flag, ws, 0x40000u | (uint32_t)stage, kLimit);
-          if (ok && rows % 16) {                 // the last instruction's terms include rows of the next run
-            if (P) arrive_cluster(map_cluster(smem_u32(&bar[kAsk]), 1));
-            mbar_arrive(&bar[kAsk]);
-            ok = mbar_wait(&bar[kFixed], fixed & 1u, abort_flag, ws, 0x50000u | (uint32_t)stage);
-            if (P) mbar_acquire_cluster(&bar[kFixed], fixed & 1u);
-            ++fixed;
+          if (rows % 16) {                       // the last instruction's terms include rows of the next run: set to zero before it is passed on
+            const uint32_t phase = tails >> stage & 1u;
+            ok = ok && mbar_wait(&bar[kReady + stage], phase, abort_flag, ws, 0x50000u | (uint32_t)stage, kLimit);
+            if (P && ok) mbar_acquire_cluster(&bar[kReady + stage], phase);
+            tails ^= 1u << stage;
+          } else {
+            ok = ok && mbar_wait(&bar[kFull + stage], fulls >> stage & 1u, abort_flag, ws, 0x40000u | (uint32_t)stage, kLimit);
+            fulls ^= 1u << stage;
           }
           if (!ok) return;
           tc_fence_after();
@@ -1214,26 +1219,27 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         }
       }
   } else {
-    // ---------------------------------------------------------------- kGrad: rows behind the end of a run are set to zero, once they are there
-    uint32_t asked = 0;
+    // ---------------------------------------------------------------- kGrad: pieces at a run's end are passed on once the rows behind it are zeros.  (Asked for by
+    // the warp that multiplies, where it came to such a piece, this took a tile 1.6 us: 131 us in the place of 109 for 8 groups of 1041 or 1007 rows.)
+    uint32_t tails = 0;
     for (long long item = team; ok && item < p.most; item += teams) {
       const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n;
       const bool sums = p.sums && at - tm * p.tiles_n == p.tiles_n - 1;
       each_piece(p, weight, share, [&](int, int rows) {
-        if (ok && rows % 16) {
-          ok = warp_wait(&bar[kAsk], asked & 1u, abort_flag, ws, 0x80000u, kLongNs);
-          if (!ok) return;
-          if (P) mbar_acquire_cluster(&bar[kAsk], asked & 1u);
-          ++asked;
-          const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-          const int boxes = N * (2 + (sums ? 0 : p.q_bytes / kBox)), per = (16 - rows % 16) * 8;     // 16 bytes each
-          for (int b = 0; b < boxes; ++b)
-            for (int i = lane; i < per; i += 32) sts_u4(a + (uint32_t)(b * kBox + rows * 128 + i * 16), make_uint4(0, 0, 0, 0));
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) {
-            if (P) arrive_cluster(map_cluster(smem_u32(&bar[kFixed]), 0));
-            else mbar_arrive(&bar[kFixed]);
+        if (rows % 16) {
+          ok = ok && warp_wait(&bar[kTail + stage], tails >> stage & 1u, abort_flag, ws, 0x80000u | (uint32_t)stage, kLimit);
+          tails ^= 1u << stage;
+          if (ok) {
+            const uint32_t a = sm + (uint32_t)stage * stage_bytes;
+            const int boxes = N * (2 + (sums ? 0 : p.q_bytes / kBox)), per = (16 - rows % 16) * 8;     // 16 bytes each
+            for (int b = 0; b < boxes; ++b)
+              for (int i = lane; i < per; i += 32) sts_u4(a + (uint32_t)(b * kBox + rows * 128 + i * 16), make_uint4(0, 0, 0, 0));
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+              if (P) arrive_cluster(map_cluster(smem_u32(&bar[kReady + stage]), 0));
+              else mbar_arrive(&bar[kReady + stage]);
+            }
           }
         }
         next();

@@ -521,6 +521,19 @@ dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int
                               const dc_adapters *adapters, const int *offsets, const int *which, int runs, const void *saved, void *dx,
                               void *da, void *db, dc_dtype dtype, void *workspace, size_t workspace_bytes, dc_stream stream);
 
+/*
+ * Host only, launches nothing: how the products of a call would run, for reports and tests.  rank 0: dc_group_forward and dc_group_backward with
+ * `runs` groups; else dc_adapter_forward and dc_adapter_backward with `runs` runs, a shared matrix and as many adapters of that rank.
+ */
+typedef enum { DC_GROUP_FORWARD = 0, DC_GROUP_DX = 1, DC_GROUP_DW = 2 } dc_group_part;   /* y; dx; dw (of adapters da) */
+typedef enum {
+  DC_GROUP_TILES = 0,        /* tiles of 128 rows and up to 256 columns, by one CTA, or their sums by a cluster of `split` */
+  DC_GROUP_PAIRS = 1,        /* tiles of 256 x 256 by two CTAs */
+  DC_GROUP_FEW_ROWS = 2      /* tiles of 128 columns and tile_cols (16 to 64) rows */
+} dc_group_form;
+typedef struct { dc_group_form form; int tile_cols, split, stages; } dc_group_plan;
+dc_status dc_group_plan_query(long long rows, int runs, int c_in, int c_out, int rank, dc_dtype dtype, dc_group_part part, dc_group_plan *plan);
+
 /* ---------------------------------------------------------------------------------------------
  * The selector's two dynamic programmes (Sec. 4.3).  Host only: every pointer is host memory, no
  * device call is made.  Boundaries are 0..L for a network of L layers; tables are row-major

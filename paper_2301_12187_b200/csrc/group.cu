@@ -335,3 +335,38 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
   }
   return status(e);
 }
+
+extern "C" dc_status dc_group_plan_query(long long rows, int runs, int c_in, int c_out, int rank, dc_dtype dtype, dc_group_part part,
+                                         dc_group_plan *plan) {
+  const dc_status s = check_sizes(rows, c_in, c_out, dtype);
+  if (s != DC_OK) return s;
+  if (rows < 1 || runs < 1 || rank < 0 || !plan || part < DC_GROUP_FORWARD || part > DC_GROUP_DW) return DC_ERR_INVALID_ARG;
+  if (runs > kMaxRuns || rank > kMaxRank) return DC_ERR_UNSUPPORTED;
+  // addresses that say what there is, and are not looked at
+  int offsets = 0;
+  const void *there = &offsets;
+  const Runs of = {&offsets, rank ? &offsets : nullptr, runs, (int)rows, runs, rank > 0}, all = {nullptr, nullptr, 1, (int)rows, 1, 0};
+  if (part == DC_GROUP_DW) {
+    GradJob j = {};
+    j.m = rank ? c_in : c_out;
+    j.n = rank ? rank : c_in;
+    j.q_terms = rank > 0;
+    j.runs = of;
+    j.out = &offsets;
+    j.dtype = dtype;
+    return grad_tc(j, false, nullptr, nullptr, plan) == cudaSuccess ? DC_OK : DC_ERR_CUDA;
+  }
+  RowsJob j = {};
+  j.rows = (int)rows;
+  j.k = part == DC_GROUP_DX ? c_out : c_in;
+  j.n = part == DC_GROUP_DX ? c_in : c_out;
+  j.w = there;
+  j.w_across = j.e_across = part == DC_GROUP_DX;
+  j.runs = rank ? all : of;
+  j.t = rank ? there : nullptr;
+  j.rank = rank;
+  j.e_pitch = dtype == DC_BF16 && rank % 8 == 0 ? (part == DC_GROUP_DX ? c_in : rank) : 64;
+  j.ext = of;
+  j.dtype = dtype;
+  return rows_tc(j, false, nullptr, nullptr, plan) == cudaSuccess ? DC_OK : DC_ERR_CUDA;
+}

@@ -149,7 +149,8 @@ cudaError_t copies_tc(const Copy *c, int count, dc_dtype dtype, cudaStream_t st)
 // writes; nothing else of the caller's is between them.  Both then run side by side as far as there is room, and this one ends behind that one.
 bool narrow_apart(const RowsJob &j);             // y_terms: by a kernel for short runs
 cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st);
-cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st);
-cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t st);
+// with `plan`: says how, and launches nothing
+cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan = nullptr);
+cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan = nullptr);
 
 }  // namespace grp

@@ -1497,7 +1497,7 @@ cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st) {
   return dc_launch_pdl(k_adapter_narrow<float>, grid, dim3(256), 0, st, (const float *)j.raw_x, j.k, (const float *)j.raw_w, j.k, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
 }
 
-cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st) {
+cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan) {
   const int n_sm = dc_sm_count();
   const bool wide = j.dtype == DC_F32;
   const int terms = wide ? 3 : 1;
@@ -1567,6 +1567,10 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   }
   p.pieces_per = dc_div_up(p.pieces, p.split);
   while (p.split > 1 && p.pieces_per * (p.split - 1) >= p.pieces) { --p.split; p.pieces_per = dc_div_up(p.pieces, p.split); }
+  if (plan) {
+    *plan = {by_few ? DC_GROUP_FEW_ROWS : pair ? DC_GROUP_PAIRS : DC_GROUP_TILES, p.nt, p.split, p.stages};
+    return cudaSuccess;
+  }
   CUtensorMap m[4] = {};
   p.maps = (j.w ? 3 : 0) | (j.t && !by_few ? 12 : 0);
   const int box = pair ? p.nt / 2 : p.nt;
@@ -1591,10 +1595,10 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   return across ? launch_any<kTile, true>(p, wide, pair, items, n_sm, m, ws, st) : launch_any<kTile, false>(p, wide, pair, items, n_sm, m, ws, st);
 }
 
-cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t st) {
+cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan) {
   const int n_sm = dc_sm_count();
   const bool wide = j.dtype == DC_F32;
-  if (wide && j.out && j.sums) {                 // two stages of fp32 terms leave no room for the block of ones
+  if (wide && j.out && j.sums && !plan) {                 // two stages of fp32 terms leave no room for the block of ones
     GradJob apart = j;
     apart.out = nullptr;
     const cudaError_t e = grad_tc(apart, early, ws, st);
@@ -1637,6 +1641,10 @@ cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   p.early = early;
   lay_out(&p, terms, kOut + (j.sums ? kBox : 0));
   if (j.sums) p.off_out += kBox;
+  if (plan) {
+    *plan = {pair ? DC_GROUP_PAIRS : DC_GROUP_TILES, p.nt, p.split, p.stages};
+    return cudaSuccess;
+  }
   CUtensorMap m[4] = {};
   p.maps = j.runs.rows ? (j.out ? 3 : 1) : 0;
   if (j.runs.rows) {                             // without rows nothing is loaded

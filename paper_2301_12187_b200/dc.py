@@ -23,6 +23,8 @@ ALGO_AUTO, ALGO_TCGEN05, ALGO_SIMT = 0, 1, 2
 MERGE_AUTO, MERGE_STEPS = 0, 1
 MX4, NV4 = 0, 1
 Q4_TILES, Q4_PAIRS, Q4_FEW_ROWS, Q4_STREAM = range(4)
+GROUP_FORWARD, GROUP_DX, GROUP_DW = range(3)
+GROUP_TILES, GROUP_PAIRS, GROUP_FEW_ROWS = range(3)
 
 _FP = C.POINTER(C.c_float)
 
@@ -65,6 +67,10 @@ class Q4Plan(C.Structure):
 
 class AdapterSet(C.Structure):
     _fields_ = [("count", C.c_int), ("rank", C.c_int), ("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class GroupPlan(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("form", "tile_cols", "split", "stages")]
 
 
 class Q4Layout(C.Structure):
@@ -140,6 +146,7 @@ EXPORTS = {
     "dc_adapter_backward": (C.c_int, [C.c_void_p, C.c_void_p, C.c_longlong, C.c_int, C.c_void_p, C.c_int, C.POINTER(AdapterSet), C.c_void_p,
                                       C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t,
                                       C.c_void_p]),
+    "dc_group_plan_query": (C.c_int, [C.c_longlong, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(GroupPlan)]),
     "dc_workspace_status": (C.c_int, [C.c_void_p, C.c_void_p]),
     "dc_workspace_status_where": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_uint), C.POINTER(C.c_uint)]),
     "dc_selftest_bounded_wait": (C.c_int, [C.c_void_p, C.c_size_t, C.c_uint, C.c_void_p]),
@@ -855,6 +862,13 @@ def adapter_backward(dy, x, w, adapters: Adapters, offsets, which, saved, dx, da
     _check(lib().dc_adapter_backward(_ptr(dy), _ptr(x), rows, adapters.c_in, _ptr(w), adapters.c_out, C.byref(adapters.c), _ptr(offsets),
                                      _ptr(which), which.numel(), _ptr(saved), _ptr(dx), _ptr(da), _ptr(db), dtype_code(dy.dtype),
                                      _ptr(workspace), _nbytes(workspace), _stream(stream)), "dc_adapter_backward")
+
+
+def group_plan(rows: int, runs: int, c_in: int, c_out: int, rank: int, dtype: int, part: int) -> GroupPlan:
+    """How the products of a call of this size would run (rank 0: grouped, else with adapters); see include/dc.h."""
+    plan = GroupPlan()
+    _check(lib().dc_group_plan_query(rows, runs, c_in, c_out, rank, dtype, part, C.byref(plan)), "dc_group_plan_query")
+    return plan
 
 
 def workspace_status(workspace, stream=None) -> int:

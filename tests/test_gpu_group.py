@@ -14,6 +14,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2301_12187_b200 import dc
+from tests.group_sizes import ADAPTER_FORMS, GROUP_FORMS, spread
 from tests.parity_util import Guarded
 
 TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -98,7 +99,7 @@ GROUPS = [
     ([700, 260, 515], 9, 520, 776),
     ([2500, 1, 0, 1303], 5, 1032, 2056),         # pairs of CTAs
     ([1900, 1501], 3, 1031, 1100),
-]
+] + [(spread(rows, n, i), 0, c_in, c_out) for i, (rows, n, c_in, c_out) in enumerate(GROUP_FORMS)]
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
@@ -197,7 +198,8 @@ ADAPTERS = [
     ([(450, 0)], 0, 1, 48, 264, 1032),
     ([(2500, 0), (3, 1), (1300, 1), (200, -1)], 7, 2, 48, 1032, 2056),         # pairs of CTAs
     ([(1, 0)] * 30 + [(1900, 2), (1, 1), (1, -1), (1500, 0)], 3, 3, 16, 1100, 1032),
-]
+] + [([(k, (i + j) % 4 - (j % 7 == 3)) for j, k in enumerate(spread(rows, n, i))], 0, 4, r, c_in, c_out)
+     for i, (rows, n, r, c_in, c_out) in enumerate(ADAPTER_FORMS)]
 
 
 def adapter_inputs(case, dtype, shared=True):
@@ -348,3 +350,309 @@ def test_gradients_against_differences(dtype):
         # each element of the gradient is off by its rounding and a little; signs are random, the sum of all is a bound
         room = float((grad.double() * v).abs().sum()) * (half_step(dt) + 2.0 ** -15)
         assert abs(float((grad.double() * v).sum()) - slope) <= room, (k, slope, room)
+
+
+# --------------------------------------------------------------------------- what masks leave out
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("runs", [[(1, i) for i in range(6)], [(3, 0), (60, 1), (5, 2), (1, 3), (200, 4), (7, 5)]])
+def test_an_adapter_that_is_no_number_stays_in_its_rows(runs, dtype):
+    """Infinities and NaN in one adapter, and in the rows of a request without one: other rows, and the gradients of other adapters, do not change."""
+    dt, rows, c_in, c_out, r = TYPES[dtype], sum(k for k, _ in runs), 136, 264, 16
+    x, w, dy = rand(rows, c_in, seed=1, dtype=dt), rand(c_out, c_in, seed=2, dtype=dt), rand(rows, c_out, seed=3, dtype=dt)
+    a, b = rand(6, r, c_in, seed=4, dtype=dt), rand(6, c_out, r, seed=5, dtype=dt)
+    off, which = offsets_of([k for k, _ in runs]), torch.tensor([k for _, k in runs], dtype=torch.int32, device="cuda")
+    which[2] = -1
+    lo, hi = runs_of(off)[2]
+    ws = torch.zeros(dc.adapter_workspace_bytes(rows, c_in, c_out, dc.Adapters(a, b), dc.dtype_code(dt)), dtype=torch.uint8, device="cuda")
+
+    def run(x, dy, a, b):
+        ad = dc.Adapters(a, b)
+        saved, y, dx, da, db = ad.saved(rows), torch.empty_like(dy), torch.empty_like(x), torch.empty_like(a), torch.empty_like(b)
+        saved.fill_(0xFF)
+        dc.adapter_forward(x, w, ad, off, which, None, 0, None, saved, y, ws)
+        dc.adapter_backward(dy, x, w, ad, off, which, saved, dx, da, db, ws)
+        torch.cuda.synchronize()
+        assert dc.workspace_status(ws) == dc.OK
+        return y, dx, da, db
+
+    good = run(x, dy, a, b)
+    a2, b2, x2, dy2 = a.clone(), b.clone(), x.clone(), dy.clone()
+    a2[4, 3], b2[4, 7, 2], b2[4, 9] = float("nan"), float("inf"), float("-inf")
+    a2[2], b2[2] = float("nan"), float("inf")     # an adapter that no run has
+    x2[lo:hi], dy2[lo:hi] = float("nan"), float("inf")
+    bad = run(x2, dy2, a2, b2)
+    others = torch.ones(rows, dtype=torch.bool, device="cuda")
+    others[lo:hi] = False
+    for (p, q), i in zip(runs_of(off), which.tolist()):
+        if i == 4:
+            others[p:q] = False
+    for k in (0, 1):
+        assert torch.equal(good[k][others], bad[k][others]) and not bool(torch.isfinite(bad[k][lo:hi].float()).any())
+    for k in (2, 3):
+        assert torch.equal(good[k][[0, 1, 3, 5]], bad[k][[0, 1, 3, 5]]) and not bool(bad[k][2].any())
+    p, q = runs_of(off)[4]
+    assert bool((bad[0][p:q, 9].float().isnan() | bad[0][p:q, 9].float().isinf()).all())
+
+
+def test_groups_beside_rows_that_are_no_numbers():
+    """A group of NaN and infinities between two others: neither their results nor their gradients change."""
+    for dt in TYPES.values():
+        x, dy = rand(150, 72, seed=1, dtype=dt), rand(150, 264, seed=2, dtype=dt)
+        w, off = rand(3, 264, 72, seed=3, dtype=dt), offsets_of([45, 30, 75])
+        ws = torch.zeros(dc.group_workspace_bytes(150, 3, 72, 264, dc.dtype_code(dt)), dtype=torch.uint8, device="cuda")
+
+        def run(x, dy):
+            y, dx, dw, db = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w), torch.empty(3, 264, device="cuda")
+            dc.group_forward(x, off, w, None, 0, y, ws)
+            dc.group_backward(dy, x, off, w, dx, dw, db, ws)
+            torch.cuda.synchronize()
+            return y, dx, dw, db
+
+        good = run(x, dy)
+        x[45:75], dy[45:75] = float("nan"), float("-inf")
+        bad = run(x, dy)
+        for k in (0, 1):
+            assert torch.equal(good[k][:45], bad[k][:45]) and torch.equal(good[k][75:], bad[k][75:])
+        for k in (2, 3):
+            assert torch.equal(good[k][[0, 2]], bad[k][[0, 2]])
+        assert bool(bad[3][1].isinf().all()) and bool(bad[0][45:75].isnan().all())
+
+
+def test_fp32_results_that_are_no_numbers():
+    """fp32 products go by terms of bf16, of which an infinity has none: what comes out is what FMAs give, in all three products and of few rows and many."""
+    for sizes, c_in, c_out in (([3, 2], 72, 40), ([200, 90], 200, 136)):
+        rows = sum(sizes)
+        x, dy = rand(rows, c_in, seed=1, dtype=torch.float32), rand(rows, c_out, seed=2, dtype=torch.float32)
+        w, off = rand(2, c_out, c_in, seed=3, dtype=torch.float32), offsets_of(sizes)
+        x[0, 5], x[1, 7], x[sizes[0], 3] = float("inf"), float("nan"), 3.4e38
+        dy[0, 2], dy[2, 1] = float("-inf"), float("inf")
+        w[0, 4, 5], w[1, 1, 3] = 0.0, 0.5
+        ws = torch.zeros(dc.group_workspace_bytes(rows, 2, c_in, c_out, dc.F32), dtype=torch.uint8, device="cuda")
+        y, dx, dw, db = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w), torch.empty(2, c_out, device="cuda")
+        dc.group_forward(x, off, w, None, 0, y, ws)
+        dc.group_backward(dy, x, off, w, dx, dw, db, ws)
+        torch.cuda.synchronize()
+        assert dc.workspace_status(ws) == dc.OK
+        for g, (lo, hi) in enumerate(runs_of(off)):
+            a, b, m = x[lo:hi].double(), dy[lo:hi].double(), w[g].double()
+            for got, p, q in ((y[lo:hi], a, m.t()), (dx[lo:hi], b, m), (dw[g], b.t(), a), (db[g][:, None], b.t(), torch.ones(hi - lo, 1, dtype=torch.float64, device="cuda"))):
+                want = (p[:, :, None] * q[None]).sum(1).float()      # element by element: a library product may skip a NaN
+                assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+                fine = want.isfinite()
+                assert torch.equal(torch.sign(got[~fine]).nan_to_num(), torch.sign(want[~fine]).nan_to_num())
+                assert bool(((got - want)[fine].abs() <= 1e-4 * want[fine].abs() + 1e-3).all())
+
+
+def test_offsets_out_of_order_stay_inside():
+    """What such offsets give is undefined, but inside the arrays."""
+    for dt in TYPES.values():
+        for numbers in ([0, 900, 3, 12], [-5, 4, 2, 7], [7, 7, 7, 7], [12, 10, 5, 0], [2 ** 31 - 1, -2 ** 31, 9, 11], [3, 9, 10 ** 9, 6]):
+            off = torch.tensor(numbers, dtype=torch.int32, device="cuda")
+            x, dy = rand(11, 40, seed=1, dtype=dt), rand(11, 72, seed=2, dtype=dt)
+            w = rand(3, 72, 40, seed=3, dtype=dt)
+            g = [Guarded(torch, s, t, fill=0) for s, t in (((11, 72), dt), ((11, 40), dt), ((3, 72, 40), dt), ((3, 72), torch.float32))]
+            ws = workspace(dc.group_workspace_bytes(11, 3, 40, 72, dc.dtype_code(dt)))
+            dc.group_forward(x, off, w, None, 0, g[0].t, ws.t)
+            dc.group_backward(dy, x, off, w, g[1].t, g[2].t, g[3].t, ws.t)
+            a, b = rand(2, 8, 40, seed=4, dtype=dt), rand(2, 72, 8, seed=5, dtype=dt)
+            ad, which = dc.Adapters(a, b), torch.tensor([1, 77, -3], dtype=torch.int32, device="cuda")
+            ws2, saved = workspace(dc.adapter_workspace_bytes(11, 40, 72, ad, ad.dtype)), Guarded(torch, (ad.saved(11).numel(),), torch.uint8, fill=0)
+            da, db = Guarded(torch, (2, 8, 40), dt, fill=0), Guarded(torch, (2, 72, 8), dt, fill=0)
+            dc.adapter_forward(x, w[0].contiguous(), ad, off, which, None, 0, None, saved.t, g[0].t, ws2.t)
+            dc.adapter_backward(dy, x, w[0].contiguous(), ad, off, which, saved.t, g[1].t, da.t, db.t, ws2.t)
+            torch.cuda.synchronize()
+            for q in g + [ws, ws2, saved, da, db]:
+                q.check(str(numbers))
+            assert dc.workspace_status(ws.t) == dc.OK and dc.workspace_status(ws2.t) == dc.OK
+
+
+# --------------------------------------------------------------------------- streams, graphs, sizes
+
+
+class Step:
+    """A training step of two adapters beside a shared matrix, and of groups behind it, on buffers of its own."""
+
+    def __init__(self, seed, dt=torch.bfloat16, rows=700):
+        self.off, self.which = offsets_of([rows // 2, 1, rows - rows // 2 - 1]), torch.tensor([0, 1, 1], dtype=torch.int32, device="cuda")
+        self.goff = offsets_of([rows // 3, 0, rows - rows // 3])
+        self.w, self.wg = rand(256, 200, seed=1, dtype=dt, scale=0.1), rand(3, 136, 256, seed=2, dtype=dt, scale=0.1)
+        self.ad = dc.Adapters(rand(2, 16, 200, seed=3, dtype=dt, scale=0.1), rand(2, 256, 16, seed=4, dtype=dt))
+        self.x, self.dz = torch.empty(rows, 200, dtype=dt, device="cuda"), torch.empty(rows, 136, dtype=dt, device="cuda")
+        self.fill(seed)
+        self.saved, self.y, self.z = self.ad.saved(rows), torch.empty(rows, 256, dtype=dt, device="cuda"), torch.empty_like(self.dz)
+        self.dy, self.dx, self.dwg = torch.empty_like(self.y), torch.empty_like(self.x), torch.empty_like(self.wg)
+        self.da, self.db, self.dbg = torch.empty_like(self.ad.a), torch.empty_like(self.ad.b), torch.empty(3, 136, device="cuda")
+        size = max(dc.adapter_workspace_bytes(rows, 200, 256, self.ad, self.ad.dtype), dc.group_workspace_bytes(rows, 3, 256, 136, self.ad.dtype))
+        self.ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+
+    def fill(self, seed):
+        self.x.copy_(rand(*self.x.shape, seed=seed, dtype=torch.float32)), self.dz.copy_(rand(*self.dz.shape, seed=seed + 1, dtype=torch.float32))
+
+    def __call__(self, stream=None):
+        dc.adapter_forward(self.x, self.w, self.ad, self.off, self.which, None, 0, None, self.saved, self.y, self.ws, stream)
+        dc.group_forward(self.y, self.goff, self.wg, None, 0, self.z, self.ws, stream)
+        dc.group_backward(self.dz, self.y, self.goff, self.wg, self.dy, self.dwg, self.dbg, self.ws, stream)
+        dc.adapter_backward(self.dy, self.x, self.w, self.ad, self.off, self.which, self.saved, self.dx, self.da, self.db, self.ws, stream)
+
+    def outputs(self):
+        torch.cuda.synchronize()
+        assert dc.workspace_status(self.ws) == dc.OK
+        return [t.clone() for t in (self.y, self.z, self.dy, self.dwg, self.dbg, self.dx, self.da, self.db)]
+
+
+@pytest.mark.parametrize("rows", [30, 700])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_step_repeats_itself_and_in_a_graph(dtype, rows):
+    """The same bits every time, alone, on another stream, and replayed from a graph with other inputs than it was captured with."""
+    step = Step(5, TYPES[dtype], rows)
+    step()
+    first = step.outputs()
+    for _ in range(20):
+        step()
+    assert all(torch.equal(a, b) for a, b in zip(first, step.outputs()))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    step(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, step.outputs()))
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            for _ in range(3):
+                step()
+    step.fill(77)
+    torch.cuda.synchronize()
+    step()
+    other = step.outputs()
+    step.fill(5)
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(first, step.outputs()))
+    step.fill(77)
+    for _ in range(5):
+        graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(other, step.outputs()))
+    assert not all(torch.equal(a, b) for a, b in zip(first, other))
+
+
+def test_steps_on_two_streams_at_once():
+    steps, streams = [Step(5), Step(9)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    want = []
+    for s in steps:
+        s()
+        want.append(s.outputs())
+    for _ in range(30):
+        for s, st in zip(steps, streams):
+            s(st)
+    for s, w in zip(steps, want):
+        assert all(torch.equal(a, b) for a, b in zip(w, s.outputs()))
+
+
+def test_a_step_follows_what_writes_its_inputs():
+    """Calls right behind kernels of other libraries that write what they read, and in front of such that read what they write."""
+    step = Step(5)
+    step()
+    want = step.outputs()
+    x, dz = step.x.clone(), step.dz.clone()
+    total = None
+    for _ in range(30):
+        step.x.zero_(), step.dz.zero_(), step.y.fill_(3.0), step.saved.fill_(0xFF)
+        step.x.copy_(x), step.dz.copy_(dz)
+        step()
+        s = step.dx.double().sum() + step.da.double().sum() + step.dwg.double().sum()
+        total = s if total is None else torch.stack((total, s)).max()
+        assert bool(total == s)
+    assert all(torch.equal(a, b) for a, b in zip(want, step.outputs()))
+
+
+def test_beside_a_projection_in_4_bits():
+    """A layer whose own weights are held in 4 bits, with adapters added in place, in front of experts: each stage from what the one before gave."""
+    dt, rows, c_in, c_out = torch.bfloat16, 133, 256, 512
+    of_type(dt)
+    x, w = rand(rows, c_in, seed=1, dtype=dt), rand(c_out, c_in, seed=2, dtype=torch.float32, scale=c_in ** -0.5)
+    q = dc.Q4Matrix(c_out, c_in, dc.NV4, dc.q4_tensor_scale(float(w.abs().max())))
+    dc.q4_quantize(w, q)
+    y = torch.empty(rows, c_out, dtype=dt, device="cuda")
+    qws = torch.zeros(dc.q4_workspace_bytes(rows, c_in, dc.NV4), dtype=torch.uint8, device="cuda")
+    dc.q4_forward(x, q, dc.q4_tensor_scale(float(x.abs().max())), None, 0, None, y, qws)
+    base = y.clone()
+    a, b = rand(3, 16, c_in, seed=3, dtype=dt, scale=c_in ** -0.5), rand(3, c_out, 16, seed=4, dtype=dt, scale=0.25)
+    ad, off, which = dc.Adapters(a, b), offsets_of([1, 100, 2, 30]), torch.tensor([2, 0, -1, 1], dtype=torch.int32, device="cuda")
+    ws = torch.zeros(dc.adapter_workspace_bytes(rows, c_in, c_out, ad, dc.BF16), dtype=torch.uint8, device="cuda")
+    dc.adapter_forward(x, None, ad, off, which, None, dc.ACT_RELU6, y, ad.saved(rows), y, ws)
+    want, slack, _ = adapter_want(x, None, a, b, None, off, which)
+    want, slack = want + base.double(), slack + 4 * U * (base.double().abs() + want.abs())
+    check(y, want.clamp(0, 6), slack, "beside 4 bits")
+    experts, goff, z = rand(2, 136, c_out, seed=6, dtype=dt, scale=c_out ** -0.5), offsets_of([60, 73]), torch.empty(rows, 136, dtype=dt, device="cuda")
+    dc.group_forward(y, goff, experts, None, 0, z, torch.zeros(dc.group_workspace_bytes(rows, 2, c_out, 136, dc.BF16), dtype=torch.uint8, device="cuda"))
+    want, slack, _ = group_want(y, goff, experts, None, 0)
+    check(z, want, slack, "experts")
+
+
+def test_arrays_beyond_32_bits():
+    """x, y and the matrices each with more than 2^32 elements; rows, groups and adapters behind that."""
+    dt = torch.bfloat16
+    of_type(dt)
+    free = torch.cuda.mem_get_info()[0]
+    if free < 60 << 30:
+        pytest.skip("not enough memory")
+    rows, c = (1 << 20) + 70000, 4096            # 4.6e9 elements
+    x = torch.zeros(rows, c, dtype=dt, device="cuda")
+    x[-300:] = rand(300, c, seed=1, dtype=dt)
+    w = rand(2, 64, c, seed=2, dtype=dt, scale=c ** -0.5)
+    off = torch.tensor([0, rows - 300, rows], dtype=torch.int32, device="cuda")
+    y, ws = torch.empty(rows, 64, dtype=dt, device="cuda"), torch.zeros(dc.group_workspace_bytes(rows, 2, c, 64, dc.BF16), dtype=torch.uint8, device="cuda")
+    dc.group_forward(x, off, w, None, 0, y, ws)
+    want, slack, _ = group_want(x[-300:], offsets_of([0, 300]), w, None, 0)
+    check(y[-300:], want, slack, "x beyond 32 bits")
+    assert not bool(y[:-300].any())
+    dw = torch.empty_like(w)
+    dc.group_backward(y, x, off, w, None, dw, None, ws)
+    a, b = y[-300:].double(), x[-300:].double()
+    check(dw[1], a.t() @ b, 304 * U * (a.abs().t() @ b.abs()), "dw")
+    assert not bool(dw[0].any())
+    back = rand(2, c, 64, seed=9, dtype=dt, scale=0.125)                 # and y beyond 32 bits
+    dc.group_forward(y, off, back, None, 0, x, torch.zeros(dc.group_workspace_bytes(rows, 2, 64, c, dc.BF16), dtype=torch.uint8, device="cuda"))
+    want, slack, _ = group_want(y[-300:], offsets_of([0, 300]), back, None, 0)
+    check(x[-300:], want, slack, "y beyond 32 bits")
+    del x, y
+    groups = 260                                  # 4.4e9 elements of matrices
+    w = torch.zeros(groups, c, c, dtype=dt, device="cuda")
+    w[-1] = rand(c, c, seed=3, dtype=dt, scale=c ** -0.5)
+    for n in (3, 200):
+        x, y = rand(n, c, seed=4, dtype=dt), torch.empty(n, c, dtype=dt, device="cuda")
+        off = torch.zeros(groups + 1, dtype=torch.int32, device="cuda")
+        off[-1] = n
+        ws = torch.zeros(dc.group_workspace_bytes(n, groups, c, c, dc.BF16), dtype=torch.uint8, device="cuda")
+        dc.group_forward(x, off, w, None, 0, y, ws)
+        want, slack, _ = group_want(x, offsets_of([n]), w[-1:], None, 0)
+        check(y, want, slack, "matrices beyond 32 bits")
+        dw = torch.full_like(w, 5.0)
+        dc.group_backward(y, x, off, w, None, dw, None, ws)
+        a, b = y.double(), x.double()
+        check(dw[-1], a.t() @ b, (n + 4) * U * (a.abs().t() @ b.abs()), "dw")
+        assert not bool(dw[:-1].any())
+        del dw
+
+
+def test_tensors_of_the_host_are_refused():
+    step = Step(5)
+    with pytest.raises(ValueError):
+        dc.group_forward(step.y, step.goff.cpu(), step.wg, None, 0, step.z, step.ws)
+    with pytest.raises(ValueError):
+        dc.group_backward(step.dz, step.y.cpu(), step.goff, step.wg, step.dy, step.dwg, None, step.ws)
+    with pytest.raises(ValueError):
+        dc.adapter_forward(step.x, step.w, step.ad, step.off, step.which.cpu(), None, 0, None, step.saved, step.y, step.ws)
+    with pytest.raises(ValueError):
+        dc.adapter_backward(step.dy, step.x, step.w, step.ad, step.off, step.which, step.saved.cpu(), step.dx, step.da, step.db, step.ws)
+
+
+def test_without_the_native_marshalling(monkeypatch):
+    step = Step(5)
+    step()
+    want = step.outputs()
+    dc.lib()
+    monkeypatch.setattr(dc, "_native", dc._NoNative)
+    step.y.zero_(), step.da.zero_(), step.dwg.zero_()
+    step()
+    assert all(torch.equal(a, b) for a, b in zip(want, step.outputs()))

@@ -19,6 +19,7 @@
 // their nine products are above 2^-24 of the result, small ones first.  The tensor core cuts its sums instead of rounding them, so a piece's
 // sum is read out and added up in fp32 registers.  A result that is a NaN is worked out again by FMAs: an infinity, or a value
 // beyond the largest bf16, has a NaN among its terms.
+#include <math.h>
 #include <string.h>
 
 #include "group.cuh"
@@ -33,7 +34,7 @@ enum { kTile = 0, kFew = 1, kGrad = 2 };
 constexpr int kEpi = 8;                          // warps reading out
 template <int FORM>
 constexpr int kThreadsOf = (2 + kEpi + (FORM == kTile ? 0 : 1)) * 32;
-constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxSlots = 8;
+constexpr int kMaxStages = 8, kMaxSplit = 8, kMaxSlots = 8, kMaxAccs = 4;
 constexpr int kSmem = 226 * 1024;                // what the static arrays leave
 constexpr int kPiece = 64;                       // of the sum, 128 bytes of bf16
 constexpr int kP = 128 * 128;                    // bytes of the 128-row operand in a stage
@@ -46,6 +47,8 @@ constexpr unsigned long long kLongNs = 20ull * 1000ull * 1000ull * 1000ull;     
 typedef __nv_bfloat16 bf16;
 template <typename T>
 constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;
+template <typename T>
+constexpr int kAccs = sizeof(T) == 4 ? 4 : 2;   // accumulators: fp32 takes one for each piece, so that four of the next tile's are multiplied while results go out
 
 struct Params {
   int rows, k, n;            // kGrad: m in the place of k
@@ -66,7 +69,7 @@ struct Params {
   const bf16 *t;             // what rows keep
   const void *e;             // kFew: what the reading-out warps take of the adapters
   int e_pitch, e_vec;
-  int slots, slot_bytes;     // kFew, bf16: of an adapter's part of the tile's columns, in shared memory
+  int slots, slot_rows, row_bytes;       // kFew, bf16: of adapters' parts of the tile's columns in shared memory, slot_rows rows' to a slot
   int early;                 // all but t was there before the launch in front of this one began, and that one writes nothing that this one does
   int off_out, off_t;        // staged results; kFew: t's numbers in shared memory
   // kGrad
@@ -410,7 +413,7 @@ __device__ __forceinline__ void store_block(const Params &p, uint32_t stage, con
   }
 }
 
-enum { kFull = 0, kEmpty = kMaxStages, kTail = 2 * kMaxStages, kReady = 3 * kMaxStages, kDFull = 4 * kMaxStages, kDEmpty = kDFull + 2, kParts = kDEmpty + 2, kEFull, kEEmpty = kEFull + kMaxSlots, kBars = kEEmpty + kMaxSlots };
+enum { kFull = 0, kEmpty = kMaxStages, kTail = 2 * kMaxStages, kReady = 3 * kMaxStages, kDFull = 4 * kMaxStages, kDEmpty = kDFull + kMaxAccs, kParts = kDEmpty + kMaxAccs, kEFull, kEEmpty = kEFull + kMaxSlots, kBars = kEEmpty + kMaxSlots };
 
 // P: in pairs.  ACROSS: the matrices' sums run across their rows (of both operands of a gradient always).
 template <int FORM, bool ACROSS, typename T, bool P>
@@ -419,6 +422,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
            const __grid_constant__ CUtensorMap map_e, const __grid_constant__ Params p, DcWsHeader *ws) {
   constexpr int N = kTerms<T>;
   constexpr bool kShort = N == 3;                // sums of a piece
+  constexpr uint32_t kAcc = kAccs<T> - 1, kAccLog = kShort ? 2 : 1;
   constexpr unsigned long long kLimit = FORM == kGrad || kShort ? kLongNs : kWaitLimitNs;
   // products of terms, small ones first
   constexpr int kPairs = N == 3 ? 6 : 1;
@@ -427,12 +431,12 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t bar[kBars];
   __shared__ uint32_t tmem_s, abort_s;
-  __shared__ int weight_s[kFewMost], seq_s[kFewMost];           // kFew: the rows' adapters, and their numbers among those of this CTA
+  __shared__ int weight_s[kFewMost], list_s[kFewMost], listed_s;        // kFew: the rows' adapters, and which of this CTA's rows have one
   volatile uint32_t *abort_flag = &abort_s;
   const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sm = (smem_u32(smem_raw) + 1023u) & ~1023u;
   if (warp == 0) {
-    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + 2 ? (P ? 2 : 1) * kEpi : i >= kReady && i < kReady + kMaxStages && P ? 2 : i == kParts ? p.split * kEpi : i >= kEEmpty ? kEpi / 2 : 1);
+    for (int i = lane; i < kBars; i += 32) mbar_init(&bar[i], i >= kDEmpty && i < kDEmpty + kMaxAccs ? (P ? 2 : 1) * kEpi : i >= kReady && i < kReady + kMaxStages && P ? 2 : i == kParts ? p.split * kEpi : i >= kEEmpty ? kEpi / 2 : 1);
     if (lane == 0) abort_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   } else if (warp == 1 && lane < 4) {
@@ -573,16 +577,16 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
     const uint32_t base = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kRows >> 4) << 24) | ((uint32_t)(p.nt >> 3) << 17);
     uint32_t d = 0;
     auto begin = [&]() {                         // the next accumulator
-      ok = ok && mbar_wait(&bar[kDEmpty + (turn & 1u)], (turn >> 1 & 1u) ^ 1u, abort_flag, ws, 0x30000u | (turn & 1u), kLimit);
+      ok = ok && mbar_wait(&bar[kDEmpty + (turn & kAcc)], (turn >> kAccLog & 1u) ^ 1u, abort_flag, ws, 0x30000u | (turn & kAcc), kLimit);
       tc_fence_after();
-      d = tmem + (turn & 1u) * (uint32_t)p.acc;
+      d = tmem + (turn & kAcc) * (uint32_t)p.acc;
     };
     auto end = [&](bool any) {
       if (any) {
-        commit<P>(&bar[kDFull + (turn & 1u)]);
+        commit<P>(&bar[kDFull + (turn & kAcc)]);
       } else {
-        mbar_arrive(&bar[kDFull + (turn & 1u)]);
-        if (P) arrive_cluster(map_cluster(smem_u32(&bar[kDFull + (turn & 1u)]), 1));
+        mbar_arrive(&bar[kDFull + (turn & kAcc)]);
+        if (P) arrive_cluster(map_cluster(smem_u32(&bar[kDFull + (turn & kAcc)]), 1));
       }
       ++turn;
     };
@@ -724,17 +728,17 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
     const uint32_t lanes = (uint32_t)(quad * 32) << 16, staged = sm + (uint32_t)(p.off_out + (warp - 2) * 32 * 128);
     const uint32_t freed = P ? map_cluster(smem_u32(&bar[kDEmpty]), 0) : 0u;
     auto wait_sums = [&]() {
-      const bool there = warp_wait(&bar[kDFull + (turn & 1u)], turn >> 1 & 1u, abort_flag, ws, 0x70000u | (turn & 1u), kLimit);
+      const bool there = warp_wait(&bar[kDFull + (turn & kAcc)], turn >> kAccLog & 1u, abort_flag, ws, 0x70000u | (turn & kAcc), kLimit);
       tc_fence_after();
       return there;
     };
-    auto sums_at = [&]() { return tmem + (turn & 1u) * (uint32_t)p.acc + lanes; };
+    auto sums_at = [&]() { return tmem + (turn & kAcc) * (uint32_t)p.acc + lanes; };
     auto release = [&]() {                       // the accumulator is read
       tc_fence_before();
       __syncwarp();
       if (elect_one()) {
-        if (P) arrive_cluster_relaxed(freed + (turn & 1u) * 8u);
-        else mbar_arrive(&bar[kDEmpty + (turn & 1u)]);
+        if (P) arrive_cluster_relaxed(freed + (turn & kAcc) * 8u);
+        else mbar_arrive(&bar[kDEmpty + (turn & kAcc)]);
       }
       __syncwarp();
     };
@@ -878,7 +882,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       for (long long item = team; item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
         const int row0 = t.row0 + half * 128 + quad * 32, row = row0 + lane;
         const float alpha = p.alpha ? __ldg(p.alpha + t.weight) : 1.f;
-        bool filled = true;                      // without a shared matrix: whether an adapter has set this lane
+        bool filled = p.pieces > 0;              // without a shared matrix: whether an adapter has set this lane
         if (p.rank && p.pieces == 0) filled = row < t.end && adapter_of(p.ext, row) >= 0;
         const float *bias = p.bias ? p.bias + (p.bias_each ? (size_t)t.weight * (size_t)p.n : 0) : nullptr;
         Ahead<T> next_residual;
@@ -966,6 +970,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       const uint32_t ts = sm + (uint32_t)p.off_t, es = ts + (uint32_t)(p.nt * pad * 4), parts = es + (uint32_t)(p.rank ? p.nt * 512 : 0);
       const int part_rows = (p.nt + p.split - 1) / p.split;
       const uint32_t ring = parts + (uint32_t)(p.split > 1 ? p.split * part_rows * 512 : 0);
+      int groups = 0;                            // slots of the ring so far
       for (long long item = team; item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
         // Of a cluster's CTAs each has every split-th row of the tile; of those each set of four warps every second one.
         const int o = t.tn * 128 + own, count = min(p.nt, t.end - t.row0), here = count > share ? (count - share - 1) / p.split + 1 : 0;
@@ -982,51 +987,51 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           }
           bar_sync(2, kEpi * 32);
           if (sizeof(T) == 2) {
-            // Rows of the ring's slots would lie in the same banks for neighbouring lanes: each lane begins with another piece of 8 numbers.
-            const int chunks = (p.rank + 7) / 8, turned = own * (p.e_pitch / 8) / 8 % chunks;
-#pragma unroll 1
-            for (int q = set; q < here; q += 2) {
-              const int r = share + p.split * q, seq = seq_s[r];
-              float sum = 0.f;
-              if (seq >= 0) {
-                const int slot = seq % p.slots;
-                const uint32_t e = ring + (uint32_t)(slot * p.slot_bytes), tr = ts + (uint32_t)(r * pad * 4);
-                if (warp_wait(&bar[kEFull + slot], (uint32_t)(seq / p.slots) & 1u, abort_flag, ws, 0xA0000u | (uint32_t)slot)) {
-                  if (ACROSS) {
-                    float some[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-                    for (int j0 = 0; j0 < p.rank; j0 += 8) {
-                      const uint4 t0 = lds_u4(tr + (uint32_t)(j0 * 4)), t1 = lds_u4(tr + (uint32_t)(j0 * 4 + 16));
-                      const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
-#pragma unroll
-                      for (int x = 0; x < 8; ++x) {
-                        uint16_t h;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(e + (uint32_t)(min(j0 + x, p.rank - 1) * 256 + own * 2)) : "memory");
-                        if (j0 + x < p.rank) some[x & 3] = fmaf(__uint_as_float(tv[x]), __uint_as_float((uint32_t)h << 16), some[x & 3]);
-                      }
-                    }
-                    sum = (some[0] + some[1]) + (some[2] + some[3]);
-                  } else {
-                    float some[2] = {0.f, 0.f};
-                    int c = turned;
+            // Slots go to the sets of warps in turn.  Rows of a slot would lie in the same banks for neighbouring lanes: each lane begins with another piece of 8 numbers.
+            const int chunks = (p.rank + 7) / 8, turned = own * (p.e_pitch / 8) / 8 % chunks, listed = listed_s;
+            for (int q = set; q < here; q += 2) sts_f(part_at(es, share + p.split * q), 0.f);
+            bar_sync(2, kEpi * 32);
+            for (int i0 = set * p.slot_rows; i0 < listed; i0 += 2 * p.slot_rows) {
+              const int group = groups + i0 / p.slot_rows, slot = group % p.slots;
+              const uint32_t e0 = ring + (uint32_t)(slot * p.slot_rows * p.row_bytes);
+              const bool there = warp_wait(&bar[kEFull + slot], (uint32_t)(group / p.slots) & 1u, abort_flag, ws, 0xA0000u | (uint32_t)slot);
 #pragma unroll 2
-                    for (int i = 0; i < chunks; ++i) {
-                      const uint4 raw = lds_u4(e + (uint32_t)(own * p.e_pitch * 2 + c * 16)), t0 = lds_u4(tr + (uint32_t)(c * 32)), t1 = lds_u4(tr + (uint32_t)(c * 32 + 16));
-                      const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
-                      float v[8];
-                      unpack8(raw, v);
+              for (int i = i0; i < min(listed, i0 + p.slot_rows); ++i) {
+                const int r = list_s[i];
+                const uint32_t e = e0 + (uint32_t)((i - i0) * p.row_bytes), tr = ts + (uint32_t)(r * pad * 4);
+                float some[4] = {0.f, 0.f, 0.f, 0.f};
+                if (ACROSS) {
+#pragma unroll 1
+                  for (int j0 = 0; j0 < p.rank; j0 += 8) {
+                    const uint4 t0 = lds_u4(tr + (uint32_t)(j0 * 4)), t1 = lds_u4(tr + (uint32_t)(j0 * 4 + 16));
+                    const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
 #pragma unroll
-                      for (int x = 0; x < 8; ++x) some[x & 1] = fmaf(__uint_as_float(tv[x]), v[x], some[x & 1]);
-                      c = c + 1 == chunks ? 0 : c + 1;
+                    for (int x = 0; x < 8; ++x) {
+                      uint16_t h;
+                      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(e + (uint32_t)(min(j0 + x, p.rank - 1) * 256 + own * 2)) : "memory");
+                      if (j0 + x < p.rank) some[x & 3] = fmaf(__uint_as_float(tv[x]), __uint_as_float((uint32_t)h << 16), some[x & 3]);
                     }
-                    sum = some[0] + some[1];
+                  }
+                } else {
+                  int c = turned;
+#pragma unroll 2
+                  for (int y = 0; y < chunks; ++y) {
+                    const uint4 raw = lds_u4(e + (uint32_t)(own * p.e_pitch * 2 + c * 16)), t0 = lds_u4(tr + (uint32_t)(c * 32)), t1 = lds_u4(tr + (uint32_t)(c * 32 + 16));
+                    const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
+                    float v[8];
+                    unpack8(raw, v);
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) some[x & 3] = fmaf(__uint_as_float(tv[x]), v[x], some[x & 3]);
+                    c = c + 1 == chunks ? 0 : c + 1;
                   }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bar[kEEmpty + slot]);
+                if (there) sts_f(part_at(es, r), (some[0] + some[1]) + (some[2] + some[3]));
               }
-              sts_f(part_at(es, r), sum);
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&bar[kEEmpty + slot]);
             }
+            groups += (listed + p.slot_rows - 1) / p.slot_rows;
+            if (p.split > 1) bar_sync(2, kEpi * 32);        // rows are delivered by others than those who worked their parts out
           } else {
             constexpr int kAtOnce = 4;           // rows, for as many loads on their way
 #pragma unroll 1
@@ -1173,10 +1178,10 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
     grp::Walk walk;
     walk.start();
     Tile t;
-    int seq = 0;                                 // adapters of rows so far
+    int group = 0;                               // slots of the ring so far
     if (p.rank)
       for (long long item = team; item < p.most && find_tile(p, tile_rows, walk, item, &t); item += teams) {
-        const int count = min(p.nt, t.end - t.row0), here = count > share ? (count - share - 1) / p.split + 1 : 0, first = seq, o0 = t.tn * 128;
+        const int count = min(p.nt, t.end - t.row0), here = count > share ? (count - share - 1) / p.split + 1 : 0, o0 = t.tn * 128;
         bar_sync(1, kEpi * 32 + 32);
         for (int i = lane; i < p.nt; i += 32) weight_s[i] = -1;
         __syncwarp();
@@ -1184,39 +1189,41 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           for (int i = max(run.begin - t.row0, 0); i < min(run.end - t.row0, count); ++i) weight_s[i] = run.weight;
         }, [](int) {});
         __syncwarp();
+        int listed = 0;
         for (int q0 = 0; q0 < here; q0 += 32) {
           const int r = share + p.split * (q0 + lane);
           const bool has = q0 + lane < here && weight_s[r] >= 0;
           const unsigned all = __ballot_sync(0xffffffffu, has);
-          if (q0 + lane < here) seq_s[r] = has ? seq + __popc(all & ((1u << lane) - 1u)) : -1;
-          seq += __popc(all);
+          if (has) list_s[listed + __popc(all & ((1u << lane) - 1u))] = r;
+          listed += __popc(all);
         }
+        if (lane == 0) listed_s = listed;
         __syncwarp();
         bar_sync(1, kEpi * 32 + 32);
-        if (sizeof(T) == 2) {
-          int at = first;
-          for (int q = 0; q < here; ++q) {
-            const int w = weight_s[share + p.split * q];
-            if (w < 0) continue;
-            const int slot = at % p.slots;
-            ok = ok && warp_wait(&bar[kEEmpty + slot], ((uint32_t)(at / p.slots) & 1u) ^ 1u, abort_flag, ws, 0xB0000u | (uint32_t)slot);
-            ++at;
+        if (sizeof(T) == 2)
+          for (int i0 = 0; i0 < listed; i0 += p.slot_rows, ++group) {
+            const int slot = group % p.slots, rows = min(p.slot_rows, listed - i0);
+            ok = ok && warp_wait(&bar[kEEmpty + slot], ((uint32_t)(group / p.slots) & 1u) ^ 1u, abort_flag, ws, 0xB0000u | (uint32_t)slot);
             if (!ok) continue;
-            const uint32_t to = ring + (uint32_t)(slot * p.slot_bytes);
+            const uint32_t to = ring + (uint32_t)(slot * p.slot_rows * p.row_bytes);
             const bf16 *e = reinterpret_cast<const bf16 *>(p.e);
             if (ACROSS) {                        // `rank` rows of the tile's columns
               const uint32_t bytes = (uint32_t)min(128, p.e_pitch - o0) * 2u;
-              if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)p.rank);
+              if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)(p.rank * rows));
               __syncwarp();
-              for (int j = lane; j < p.rank; j += 32) bulk_load(to + (uint32_t)(j * 256), e + ((size_t)w * (size_t)p.rank + (size_t)j) * (size_t)p.e_pitch + (size_t)o0, bytes, &bar[kEFull + slot]);
-            } else if (lane == 0) {              // the columns' rows, one piece
+              for (int i = 0; i < rows; ++i) {
+                const bf16 *from = e + (size_t)weight_s[list_s[i0 + i]] * (size_t)p.rank * (size_t)p.e_pitch + (size_t)o0;
+                for (int j = lane; j < p.rank; j += 32) bulk_load(to + (uint32_t)(i * p.row_bytes + j * 256), from + (size_t)j * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
+              }
+            } else {                             // the columns' rows, one piece
               const uint32_t bytes = (uint32_t)(min(128, p.n - o0) * p.e_pitch) * 2u;
-              mbar_arrive_expect_tx(&bar[kEFull + slot], bytes);
-              bulk_load(to, e + ((size_t)w * (size_t)p.n + (size_t)o0) * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
+              if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)rows);
+              __syncwarp();
+              if (lane < rows)
+                bulk_load(to + (uint32_t)(lane * p.row_bytes), e + ((size_t)weight_s[list_s[i0 + lane]] * (size_t)p.n + (size_t)o0) * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
             }
             __syncwarp();
           }
-        }
       }
   } else {
     // ---------------------------------------------------------------- kGrad: pieces at a run's end are passed on once the rows behind it are zeros.  (Asked for by
@@ -1377,6 +1384,73 @@ __global__ void __launch_bounds__(256) k_adapter_narrow(const T *__restrict__ x,
   }
 }
 
+// The same for u = dy B, B read across: a CTA to a row, its eight warps to as many parts of the sum; a lane takes 8 of the rank's numbers (and as many lanes
+// as that needs the whole rank) of every 32 / lanes-th row of B.
+template <typename T>
+__global__ void __launch_bounds__(256) k_adapter_narrow_across(const T *__restrict__ x, int x_pitch, const T *__restrict__ b, int b_pitch, int k, int rank,
+                                                               const __grid_constant__ Runs runs, const float *__restrict__ scale, bf16 *__restrict__ t) {
+  __shared__ float part[8][grp::kMaxRank];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int row = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, pad = grp::rank_pad(rank), groups = (rank + 7) / 8;
+  int across = 1;                                // lanes to a row of B
+  while (across < groups) across *= 2;
+  int w = -1;
+  each_run(runs, row, row + 1, [&](const Run &run) { if (run.begin <= row && row < run.end) w = run.weight; }, [](int) {});
+  w = __reduce_max_sync(0xffffffffu, w);
+  if (w < 0) return;
+  const int g = lane & (across - 1), step = 32 / across;
+  const T *xr = x + (size_t)row * (size_t)x_pitch, *br = b + (size_t)w * (size_t)k * (size_t)b_pitch + (size_t)(g * 8);
+  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  constexpr int kAhead = 4;
+  if (g < groups)
+    for (int i0 = warp * step + lane / across; i0 < k; i0 += kAhead * 8 * step) {
+      float xv[kAhead], v[kAhead][8];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = i0 + u * 8 * step;
+        const bool here = i < k;
+        xv[u] = here ? to_float(xr[i]) : 0.f;
+        const T *at = br + (size_t)i * (size_t)b_pitch;
+        if (sizeof(T) == 2) {
+          const uint4 raw = here ? *reinterpret_cast<const uint4 *>(at) : make_uint4(0, 0, 0, 0);
+          unpack8(raw, v[u]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; j += 4) {
+            const float4 f = here && g * 8 + j < rank ? *reinterpret_cast<const float4 *>(at + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v[u][j] = f.x; v[u][j + 1] = f.y; v[u][j + 2] = f.z; v[u][j + 3] = f.w;
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = fmaf(xv[u], v[u][j], s[j]);
+    }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    for (int d = across; d < 32; d *= 2) s[j] += __shfl_xor_sync(0xffffffffu, s[j], d);
+  if (lane < groups) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[warp][lane * 8 + j] = s[j];
+  }
+  __syncthreads();
+  const int j = (int)threadIdx.x;
+  if (j < pad) {
+    constexpr int kKept = sizeof(T) == 4 ? 3 : 2;
+    float all = 0.f, term[3];
+    if (j < rank) {
+      for (int u = 0; u < 8; ++u) all += part[u][j];
+      if (scale) all *= __ldg(scale + w);
+    }
+    terms_of<T>(all, term);
+    bf16 *to = t + (size_t)row * (size_t)(kKept * pad) + (size_t)j;
+#pragma unroll
+    for (int y = 0; y < kKept; ++y) to[y * pad] = __float2bfloat16(term[y]);
+  }
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -1423,37 +1497,65 @@ cudaError_t launch_any(Params &p, bool wide, bool pair, long long items, int n_s
 void lay_out(Params *p, int terms, int apart) {
   p->acc = (int)dc_round_up((size_t)p->nt, 32);
   p->tmem_cols = 32;
-  while (p->tmem_cols < 2 * p->acc) p->tmem_cols *= 2;
+  while (p->tmem_cols < (terms == 3 ? kAccs<float> : kAccs<bf16>) * p->acc) p->tmem_cols *= 2;
   const int stage = terms * (kP + p->q_bytes);
   p->stages = (kSmem - 1024 - apart) / stage;
   if (p->stages > kMaxStages) p->stages = kMaxStages;
   p->off_out = p->off_t = p->stages * stage;
 }
-// CTAs that share a tile's sum of `pieces`: as many as keep all SMs busy, each with `least` pieces at least
-int split_of(long long items, int pieces, int least, int n_sm) {
-  int s = items > 0 ? (int)(n_sm / items < kMaxSplit ? n_sm / items : kMaxSplit) : 1;
-  if (s > pieces / least) s = pieces / least;
-  return s < 1 ? 1 : s;
+// Clusters of so many CTAs, one to an SM, that run at once on 148 SMs.
+int clusters_at_once(int split, int n_sm) {
+  static constexpr int kAt148[kMaxSplit + 1] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
+  return kAt148[split] * n_sm / 148;
 }
+// CTAs that share a tile's sum of `pieces`: as many as keep all SMs busy at once, each with `least` pieces at least
+int split_of(long long items, int pieces, int least, int n_sm) {
+  int s = kMaxSplit;
+  while (s > 1 && (items > clusters_at_once(s, n_sm) || s > pieces / least)) --s;
+  return s;
+}
+struct Shape { int nt; bool pair; int split; double us; };
 // Columns to a tile, whether CTAs work in pairs, and how many share a tile's sum, by an estimate in cycles: a piece of 64 terms takes its loads (an SM takes in some 45
-// bytes a cycle; two stages of fp32 terms wait for them) or its instructions; results go out beside the next tile's pieces (fp32: behind this one's, their
-// sums being in registers), and of the last tile behind them; a cluster meets twice.
-struct Shape { int nt; bool pair; int split; };
-Shape shape_of(int n, double rows, double runs, double pieces, bool wide, int n_sm) {
+// bytes a cycle; two stages of fp32 terms wait for them) or its instructions; results go out beside the next tile's pieces, and of the last tile behind
+// them; a cluster meets twice, and reads each other's parts.  `matrices`: bytes that come from memory (at 4.4 TB/s with the rows that come with them); `more`: cycles
+// that a tile's adapters take.
+Shape shape_of(int n, double rows, double runs, double pieces, double matrices, double more, bool wide, int n_sm) {
   static constexpr struct { int nt; bool pair; } kinds[4] = {{256, true}, {256, false}, {128, false}, {64, false}};
-  Shape best = {64, false, 1};
-  double least = 1e30;
+  Shape best = {64, false, 1, 1e30};
   for (const auto &k : kinds) {
     if ((wide && k.nt > 128) || (k.nt > 64 && n <= k.nt / 2)) continue;
-    const double tiles = (rows / (k.pair ? 256 : 128) + 0.5 * runs) * dc_div_up(n, k.nt);
+    const double tiles = (rows / (k.pair ? 256 : 128) + 0.5 * runs) * dc_div_up(n, k.nt), most = (floor(rows / 128) + runs) * dc_div_up(n, k.nt);
     const double bytes = (128 + (k.pair ? k.nt / 2 : k.nt)) * 128.0 * (wide ? 3 : 1), sums = k.nt * 2.0 * (wide ? 6 : 1);
     double piece = bytes / 45 > sums ? bytes / 45 : sums;
     if (wide && piece < (sums + 1000 + bytes / 45) / 2) piece = (sums + 1000 + bytes / 45) / 2;
     for (int split = 1; split <= (k.pair ? 1 : kMaxSplit); ++split) {
-      if (split > 1 && (tiles * split > n_sm || pieces < 4 * split)) break;
-      const double rounds = tiles * split / (k.pair ? n_sm / 2 : n_sm), main = pieces / split * piece, out = (400 + k.nt * 10.0) / split + (split > 1 ? 4000 : 0);
-      const double time = (rounds < 1 ? 1 : rounds + 0.4) * (wide ? main + out : main > out ? main : out) + (main > out ? out : main) + (k.pair ? 800 : 0);
-      if (time < least) { least = time; best = {k.nt, k.pair, split}; }
+      if (split > 1 && (most > clusters_at_once(split, n_sm) || pieces < 4 * split)) break;
+      const double rounds = tiles * split / (k.pair ? n_sm / 2 : n_sm), main = pieces / split * piece + more, out = (800 + k.nt * 14.0) / split + (split > 1 ? 3000 + k.nt * 8.0 : 0);
+      double cycles = (rounds < 1 ? 1 : rounds + 0.4) * (main > out ? main : out) + (main > out ? out : main) + (k.pair ? 800 : 0);
+      if (cycles < matrices / 2.3e3) cycles = matrices / 2.3e3;
+      if (cycles / 1.9e3 < best.us) best = {k.nt, k.pair, split, cycles / 1.9e3};
+    }
+  }
+  return best;
+}
+// The same for short runs: rows to a tile, and CTAs to its sum, in microseconds.  The matrix comes once for each tile of rows (82 GB/s to an SM), the rows'
+// adapters 0.3 a row or at 40 GB/s, in two sets of warps; a cluster meets.
+Shape few_shape_of(const grp::RowsJob &j, int runs, long long (*row_tiles)(const Runs &, int), int pieces, double matrices, bool wide, int n_sm) {
+  const int mean = j.rows / runs, terms = wide ? 3 : 1;
+  Shape best = {16, false, 1, 1e30};
+  for (int nt = 16; nt <= ((wide || j.rank > 64) && j.t ? kFewWide : wide ? kFewWide : kFewMost); nt *= 2) {
+    if (runs > 1 && nt > 16 && mean <= nt * 3 / 8) break;
+    const long long all = row_tiles(j.runs, nt) * dc_div_up(j.n, 128);
+    const double tiles = ((double)j.rows / nt + (runs > 1 ? 0.7 : 0.5) * runs) * dc_div_up(j.n, 128);
+    for (int split = 1; split <= kMaxSplit; ++split) {
+      if (split > 1 && (all > clusters_at_once(split, n_sm) || (pieces ? split > pieces / 4 : !j.t || split > nt / 4))) break;
+      const double rounds = (runs > 1 && split == 1 ? tiles : (double)all) * split / n_sm, rows = (double)(j.rows < nt ? j.rows : nt) / split / 2;
+      const double stream = (double)dc_div_up(pieces, split) * terms * (kP + nt * 128) / 82e3, memory = matrices / 6.5e6;
+      const double row = 256.0 * grp::rank_pad(j.rank) / 40e3, ext = j.t ? 2.0 + rows * (row > 0.3 ? row : 0.3) : 0.0;
+      const double work = stream > ext ? stream : ext, out = 0.6 + nt * 0.02;
+      const double all_of = (rounds < 1 ? 1 : rounds + 0.3) * (work > out ? work : out) + 0.3 * (memory < work ? memory : work) + (split > 1 ? 1.2 : 0.5);
+      const double us = all_of > memory ? all_of : memory;
+      if (us < best.us) best = {nt, false, split, us};
     }
   }
   return best;
@@ -1482,19 +1584,27 @@ cudaError_t copies_tc(const Copy *c, int count, dc_dtype dtype, cudaStream_t st)
   return dtype == DC_BF16 ? dc_launch_pdl(k_group_rows_of<bf16>, grid, dim3(256), 0, st, all) : dc_launch_pdl(k_group_rows_of<float>, grid, dim3(256), 0, st, all);
 }
 
-// Rows whose runs are this short go by kFew (rows through it again for each tile of 64; 128 columns of a matrix are a tile's whatever its rows).
-static bool few(const RowsJob &j) {
-  if (j.y_terms) return false;
-  return j.runs.offsets ? j.rows / runs_with_rows(j.runs) <= 48 : j.rows <= 128;
-}
+// By the kernels for short runs: each row reads all of its adapter's matrix, 3 us and what that takes from L2 at 3 MB a us; tiles take 6 us, the last two of them for a cluster's
+// parts, and 0.25 for a piece.
 bool narrow_apart(const RowsJob &j) {
-  return j.y_terms && !j.w_across && j.rows <= 1024 && j.rows / runs_with_rows(j.runs) <= 8 && (j.dtype == DC_BF16 || j.k % 4 == 0);
+  if (!j.y_terms || (j.dtype == DC_F32 && (j.w_across ? j.n % 4 : j.k % 4) != 0)) return false;
+  const int n_sm = dc_sm_count(), pieces = dc_div_up(j.k, kPiece);
+  const double wide = j.dtype == DC_F32 ? 2.0 : 1.0, apart = 3.0 + (double)j.rows * rank_pad(j.n) * j.k * 2.0 * wide / 3e6;
+  const long long items = row_tiles(j.runs, 128);
+  const int split = split_of(items, pieces, 4, n_sm);
+  const double tiles = 6.0 + dc_div_up((int)(items < (1 << 20) ? items : 1 << 20) * split, n_sm) * (double)dc_div_up(pieces, split) * 0.25 * (wide > 1.0 ? 4.0 : 1.0);
+  return apart < tiles;
 }
 cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st) {
-  const dim3 grid((unsigned)j.rows, (unsigned)(rank_pad(j.n) / 8));
-  if (j.dtype == DC_BF16)
-    return dc_launch_pdl(k_adapter_narrow<bf16>, grid, dim3(256), 0, st, (const bf16 *)j.x, j.x_pitch, (const bf16 *)j.w, j.w_pitch, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
-  return dc_launch_pdl(k_adapter_narrow<float>, grid, dim3(256), 0, st, (const float *)j.raw_x, j.k, (const float *)j.raw_w, j.k, j.k, j.n, j.runs, j.alpha, (bf16 *)j.y);
+  const dim3 grid((unsigned)j.rows, j.w_across ? 1u : (unsigned)(rank_pad(j.n) / 8));
+  bf16 *y = (bf16 *)j.y;
+  if (j.dtype == DC_BF16) {
+    if (j.w_across) return dc_launch_pdl(k_adapter_narrow_across<bf16>, grid, dim3(256), 0, st, (const bf16 *)j.x, j.x_pitch, (const bf16 *)j.w, j.w_pitch, j.k, j.n, j.runs, j.alpha, y);
+    return dc_launch_pdl(k_adapter_narrow<bf16>, grid, dim3(256), 0, st, (const bf16 *)j.x, j.x_pitch, (const bf16 *)j.w, j.w_pitch, j.k, j.n, j.runs, j.alpha, y);
+  }
+  const float *x = (const float *)j.raw_x, *w = (const float *)j.raw_w;
+  if (j.w_across) return dc_launch_pdl(k_adapter_narrow_across<float>, grid, dim3(256), 0, st, x, j.k, w, j.n, j.k, j.n, j.runs, j.alpha, y);
+  return dc_launch_pdl(k_adapter_narrow<float>, grid, dim3(256), 0, st, x, j.k, w, j.k, j.k, j.n, j.runs, j.alpha, y);
 }
 
 cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan) {
@@ -1527,46 +1637,46 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
     p.e_pitch = wide ? (j.e_across ? j.n : j.rank) : j.e_pitch;
     p.e_vec = !wide || j.rank % 4 == 0;
   }
-  const bool by_few = few(j);
   const int runs = runs_with_rows(j.runs);
+  const double matrices = j.w ? (double)runs * j.n * j.k * 2 * terms : 0.0;
+  // an adapter's instructions, and the way to the next one, of the runs that a tile has rows of
+  const double per_tile = j.t ? 1.0 + 128.0 * j.ext.count / j.rows : 0.0, more = 850.0 * (per_tile < 129.0 ? per_tile : 129.0) * (wide ? 2.0 : 1.0);
+  const Shape tile = j.y_terms ? Shape{rank_pad(j.n), false, 1, 0.0} : shape_of(j.n, j.rows, runs, p.pieces, matrices, more, wide, n_sm);
+  // runs of up to 128 rows: 128 columns of a matrix in the place of 128 rows, where that is faster
+  Shape shape = tile;
+  bool by_few = false;
+  if (!j.y_terms && j.rows / runs <= 128) {
+    const Shape f = few_shape_of(j, runs, row_tiles, p.pieces, matrices, wide, n_sm);
+    by_few = f.us <= tile.us;
+    if (by_few) shape = f;
+  }
   long long items;
-  bool pair = false;
+  const bool pair = shape.pair;
+  p.nt = shape.nt;
+  p.split = shape.split;
+  p.early = early;
   if (by_few) {
-    const int mean = j.rows / runs;
-    p.nt = mean <= (runs == 1 ? 16 : 12) ? 16 : mean <= (runs == 1 ? 32 : 24) ? 32 : 64;
-    if ((wide || j.rank > 64) && p.nt > kFewWide) p.nt = kFewWide;
     p.q_bytes = p.nt * 128;
     p.tiles_n = dc_div_up(j.n, 128);
     items = row_tiles(j.runs, p.nt) * p.tiles_n;
-    p.split = split_of(items, p.pieces, 4, n_sm);
-    p.early = early;
     int apart = (p.rank ? p.nt * (rank_pad(p.rank) * 4 + 512) : 0) + (p.split > 1 ? (p.nt + p.split) * 512 : 0);
     if (p.rank && !wide) {
-      p.slot_bytes = j.e_across ? p.rank * 256 : 128 * p.e_pitch * 2;
-      p.slots = 65536 / p.slot_bytes < kMaxSlots ? 65536 / p.slot_bytes : kMaxSlots;
-      apart += p.slots * p.slot_bytes;
+      p.row_bytes = j.e_across ? p.rank * 256 : 128 * p.e_pitch * 2;
+      p.slot_rows = 16384 / p.row_bytes < 1 ? 1 : 16384 / p.row_bytes < 8 ? 16384 / p.row_bytes : 8;
+      p.slots = 65536 / (p.slot_rows * p.row_bytes) < kMaxSlots ? 65536 / (p.slot_rows * p.row_bytes) : kMaxSlots;
+      apart += p.slots * p.slot_rows * p.row_bytes;
     }
     lay_out(&p, terms, apart);
   } else {
-    if (j.y_terms) {
-      p.nt = rank_pad(j.n);
-    } else {
-      const Shape s = shape_of(j.n, j.rows, runs, p.pieces + (j.t ? 2 : 0), wide, n_sm);
-      p.nt = s.nt;
-      pair = s.pair;
-      p.split = s.split;
-    }
     const int wide_nt = pair ? p.nt / 2 : p.nt;  // of a CTA
     p.q_bytes = j.w_across || (!j.w && j.e_across) ? dc_div_up(wide_nt, 64) * kBox : wide_nt * 128;
     p.tiles_n = dc_div_up(j.n, p.nt);
     items = row_tiles(j.runs, pair ? 256 : 128) * p.tiles_n;
     if (j.y_terms) p.split = split_of(items, p.pieces, 4, n_sm);
-    else if (p.split > n_sm / items) p.split = items < n_sm ? (int)(n_sm / items) : 1;         // a tile to a cluster
-    p.early = early;
     lay_out(&p, terms, kOut);
   }
   p.pieces_per = dc_div_up(p.pieces, p.split);
-  while (p.split > 1 && p.pieces_per * (p.split - 1) >= p.pieces) { --p.split; p.pieces_per = dc_div_up(p.pieces, p.split); }
+  while (p.split > 1 && p.pieces && p.pieces_per * (p.split - 1) >= p.pieces) { --p.split; p.pieces_per = dc_div_up(p.pieces, p.split); }
   if (plan) {
     *plan = {by_few ? DC_GROUP_FEW_ROWS : pair ? DC_GROUP_PAIRS : DC_GROUP_TILES, p.nt, p.split, p.stages};
     return cudaSuccess;
@@ -1627,7 +1737,7 @@ cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   } else if (j.q_terms) {
     p.nt = wide ? pad : 2 * pad;
   } else {
-    const Shape s = shape_of(j.n, (double)j.m * weights, 0, (double)j.runs.rows / kPiece / weights + 0.5, wide, n_sm);
+    const Shape s = shape_of(j.n, (double)dc_div_up(j.m, 128) * 128 * weights, 0, (double)j.runs.rows / kPiece / weights + 0.5, 0.0, 0.0, wide, n_sm);
     p.nt = s.nt;
     pair = s.pair && j.m > 128;
     p.split = s.split;
@@ -1637,7 +1747,8 @@ cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   p.tiles_n = (j.out ? (j.q_terms ? 1 : dc_div_up(j.n, p.nt)) : 0) + (j.sums ? 1 : 0);
   const long long items = (long long)p.tiles_m * p.tiles_n * weights;
   if (!j.out || j.q_terms) p.split = split_of(items, j.runs.rows / kPiece / weights, 4, n_sm);
-  else if (pair || p.split > n_sm / items) p.split = !pair && items < n_sm ? (int)(n_sm / items) : 1;
+  else if (pair) p.split = 1;
+  else while (p.split > 1 && items > clusters_at_once(p.split, n_sm)) --p.split;
   p.early = early;
   lay_out(&p, terms, kOut + (j.sums ? kBox : 0));
   if (j.sums) p.off_out += kBox;

@@ -4,12 +4,13 @@ among these)."""
 import random
 
 # rows, groups, c_in, c_out
-GROUP_FORMS = [(4, 1, 16, 16), (844, 1, 16, 24), (19, 1, 16, 16), (35, 1, 16, 568), (40, 1, 536, 16), (1, 1, 464, 488), (49, 1, 16, 928), (351, 7, 2128, 16),
-               (28, 2, 528, 1512), (1500, 2, 136, 1281), (1774, 26, 1156, 79), (1339, 7, 184, 2512), (4769, 4, 408, 432), (19, 27, 131, 667), (1466, 3, 2000, 144)]
+GROUP_FORMS = [(3, 1, 16, 16), (681, 1, 16, 24), (141, 35, 488, 16), (2, 1, 80, 472), (290, 22, 1248, 16), (2335, 24, 16, 16), (317, 22, 16, 1080),
+               (138, 1, 16, 624), (151, 1, 600, 24), (7550, 5, 392, 16), (101, 3, 1704, 712), (2108, 63, 24, 528), (2281, 20, 149, 18), (1267, 1, 2853, 139),
+               (2385, 45, 240, 216), (138, 1, 2168, 1760), (174, 7, 481, 3782)]
 # rows, requests, rank, c_in, c_out
-ADAPTER_FORMS = [(1, 1, 2, 16, 40), (550, 1, 38, 24, 16), (27, 1, 8, 24, 16), (1, 1, 8, 616, 528), (40, 4, 8, 552, 16), (70, 2, 8, 17, 484), (138, 2, 8, 824, 16),
-                 (167, 2, 32, 16, 632), (23, 1, 8, 524, 626), (3104, 8, 59, 592, 72), (3215, 2, 128, 72, 688), (4840, 4, 8, 672, 16), (4360, 10, 8, 16, 784),
-                 (3078, 3, 8, 16, 1400), (1118, 6, 28, 3880, 16), (165, 1, 16, 1760, 2080)]
+ADAPTER_FORMS = [(2, 2, 2, 24, 16), (750, 1, 8, 16, 16), (1, 1, 8, 928, 880), (139, 1, 8, 16, 672), (151, 1, 16, 712, 16), (18, 2, 32, 975, 2169),
+                 (7932, 3, 16, 16, 144), (7779, 4, 64, 144, 16), (104, 11, 16, 3656, 24), (138, 1, 32, 1040, 1512), (127, 127, 8, 16, 3080),
+                 (33, 2, 16, 3576, 912), (7165, 5, 16, 400, 16), (5485, 5, 8, 16, 536), (3162, 3, 64, 1184, 136), (3158, 2, 64, 136, 1256)]
 
 
 def spread(rows, runs, seed):

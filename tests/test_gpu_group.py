@@ -195,6 +195,7 @@ ADAPTERS = [
     ([(20, 1), (90, 0)], 4, 2, 100, 131, 67),
     ([(1, 0), (1, 1)], 0, 2, 12, 33, 1001),
     ([], 9, 2, 16, 64, 64),
+    ([], 400, 2, 16, 64, 200),
     ([(450, 0)], 0, 1, 48, 264, 1032),
     ([(2500, 0), (3, 1), (1300, 1), (200, -1)], 7, 2, 48, 1032, 2056),         # pairs of CTAs
     ([(1, 0)] * 30 + [(1900, 2), (1, 1), (1, -1), (1500, 0)], 3, 3, 16, 1100, 1032),
@@ -303,7 +304,7 @@ def test_adapter_backward(shared, case, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("case", [4, 6, 14])
+@pytest.mark.parametrize("case", [4, 6, 15])
 def test_adapter_backward_parts_alone(case, dtype):
     """Each set of gradients without the others gives the same bits, on workspaces that hold something else: what runs beside what, and waits for what, differs."""
     x, w, a, b, scale, off, which = adapter_inputs(case, dtype)

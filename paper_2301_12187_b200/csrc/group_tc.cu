@@ -8,8 +8,8 @@
 //   kTile   128 rows of a run x up to 256 columns of its matrix.
 //   kFew    runs of few rows: 128 columns of the matrix take the place of the 128 rows, so that an instruction is as wide as there are rows and
 //           the matrix streams through once.  Adapters' parts of those columns, a row's after a row's, come through a ring of their own.
-//   kGrad   128 x up to 256 of a gradient: the sum runs over the rows of a weight's runs.  The last piece of a run holds rows of the next one: those that its last
-//           instruction takes are set to zero by a warp, in both operands (0 times a NaN is a NaN).
+//   kGrad   128 x up to 256 of a gradient: the sum runs over the rows of a weight's runs.  Where a run ends inside a piece, rows of other weights in it are set to zero by
+//           a warp, in both operands (0 times a NaN is a NaN).
 // kTile and kGrad in pairs (cta_group::2): two CTAs multiply 256 x 256, each loads half of either operand.
 // Few tiles: a cluster shares a tile's sum, and adds up its parts through its shared memory.
 // Adapters (kTile): each run's part is added to the same accumulator by instructions that leave the lanes of other rows alone, so that an
@@ -242,22 +242,50 @@ __device__ __forceinline__ void each_run_of(const Runs &r, int weight, F f) {
     }
   }
 }
-// Calls f(first row, rows) for this CTA's pieces of 64 rows of a weight's runs, all lanes together: pieces go round the CTAs of a cluster that share a sum.
+// Calls f(first row, rows, mask) for this CTA's pieces of a weight's runs, all lanes together: 64 rows from the first one on, of which those in the mask are the
+// weight's, the last of them row `rows` - 1.  What a run leaves of 64 rows shares a piece with the runs that begin inside it (single rows of many requests
+// are 64 to a piece then, not one).  Pieces go round the CTAs of a cluster that share a sum.
+__device__ __forceinline__ uint64_t row_bits(int lo, int hi) { return (hi - lo >= 64 ? ~0ull : (1ull << (hi - lo)) - 1ull) << lo; }
 template <typename F>
 __device__ __forceinline__ void each_piece(const Params &p, int weight, int share, F f) {
-  int turn = 0;
+  int turn = 0, first = 0;
+  bool open = false;
+  uint64_t mask = 0;
+  auto close = [&]() {
+    if (turn == share) f(first, 64 - __clzll((long long)mask), mask);
+    if (++turn == p.split) turn = 0;
+    open = false;
+  };
   each_run_of(p.runs, weight, [&](int begin, int end) {
-    for (int r = begin; r < end; r += kPiece) {
-      if (turn == share) f(r, min(kPiece, end - r));
-      if (++turn == p.split) turn = 0;
+    if (open) {
+      if (begin < first + kPiece) {
+        const int lo = max(begin - first, 0), hi = min(end - first, kPiece);
+        if (hi > lo) mask |= row_bits(lo, hi);
+        if (end < first + kPiece) return;
+        begin = first + kPiece;
+      }
+      close();
     }
-    __syncwarp();
+    const int whole = (end - begin) / kPiece;
+    int k = share - turn;
+    if (k < 0) k += p.split;
+    for (; k < whole; k += p.split) f(begin + k * kPiece, kPiece, ~0ull);
+    turn = (turn + whole) % p.split;
+    first = begin + whole * kPiece;
+    if (first < end) {
+      open = true;
+      mask = row_bits(0, end - first);
+    }
   });
+  if (open) close();
+  __syncwarp();
 }
+// whether rows that the instructions of a piece take have to be set to zero
+__device__ __forceinline__ bool has_holes(int rows, uint64_t mask) { return mask != row_bits(0, (rows + 15) / 16 * 16); }
 __device__ __forceinline__ int count_pieces(const Params &p, int weight, int share) {
   int all = 0;
-  each_run_of(p.runs, weight, [&](int begin, int end) { all += (end - begin + kPiece - 1) / kPiece; });
-  return all <= share ? 0 : (all - share - 1) / p.split + 1;
+  each_piece(p, weight, share, [&](int, int, uint64_t) { ++all; });
+  return all;
 }
 
 __device__ __forceinline__ void unpack8(uint4 w, float *v) {
@@ -502,8 +530,8 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n, tn = at - tm * p.tiles_n;
         const bool sums = p.sums && tn == p.tiles_n - 1;
         const int i0 = tm * kRows + half * 128, j0 = tn * p.nt + half * (p.nt / 2);
-        each_piece(p, weight, share, [&](int r, int rows) {
-          const uint32_t full = lead && ok ? open(sums ? (uint32_t)(N * kP) : stage_bytes, 0x10000u, rows % 16 != 0) : 0u;
+        each_piece(p, weight, share, [&](int r, int rows, uint64_t mask) {
+          const uint32_t full = lead && ok ? open(sums ? (uint32_t)(N * kP) : stage_bytes, 0x10000u, has_holes(rows, mask)) : 0u;
           if (full) {
             uint32_t a = sm + (uint32_t)stage * stage_bytes;
             for (int t = 0; t < N; ++t)
@@ -597,7 +625,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         bool any = false;
         if (lead) begin();
         const uint32_t idesc = (sums ? (base & ~(0x3Fu << 17)) | (uint32_t)(kRows / 64) << 17 : base) | (1u << 15) | (1u << 16);
-        each_piece(p, weight, share, [&](int, int rows) {
+        each_piece(p, weight, share, [&](int, int rows, uint64_t mask) {
           if (!lead || !ok) {
             next();
             return;
@@ -607,7 +635,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
             begin();
             any = false;
           }
-          if (rows % 16) {                       // the last instruction's terms include rows of the next run: set to zero before it is passed on
+          if (has_holes(rows, mask)) {           // rows of other weights: set to zero before the piece is passed on
             const uint32_t phase = tails >> stage & 1u;
             ok = ok && mbar_wait(&bar[kReady + stage], phase, abort_flag, ws, 0x50000u | (uint32_t)stage, kLimit);
             if (P && ok) mbar_acquire_cluster(&bar[kReady + stage], phase);
@@ -1226,21 +1254,22 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           }
       }
   } else {
-    // ---------------------------------------------------------------- kGrad: pieces at a run's end are passed on once the rows behind it are zeros.  (Asked for by
+    // ---------------------------------------------------------------- kGrad: pieces with rows of other weights are passed on once those are zeros.  (Asked for by
     // the warp that multiplies, where it came to such a piece, this took a tile 1.6 us: 131 us in the place of 109 for 8 groups of 1041 or 1007 rows.)
     uint32_t tails = 0;
     for (long long item = team; ok && item < p.most; item += teams) {
       const int weight = (int)(item / per_weight), at = (int)(item - (long long)weight * per_weight), tm = at / p.tiles_n;
       const bool sums = p.sums && at - tm * p.tiles_n == p.tiles_n - 1;
-      each_piece(p, weight, share, [&](int, int rows) {
-        if (rows % 16) {
+      each_piece(p, weight, share, [&](int, int rows, uint64_t mask) {
+        if (has_holes(rows, mask)) {
           ok = ok && warp_wait(&bar[kTail + stage], tails >> stage & 1u, abort_flag, ws, 0x80000u | (uint32_t)stage, kLimit);
           tails ^= 1u << stage;
           if (ok) {
             const uint32_t a = sm + (uint32_t)stage * stage_bytes;
-            const int boxes = N * (2 + (sums ? 0 : p.q_bytes / kBox)), per = (16 - rows % 16) * 8;     // 16 bytes each
-            for (int b = 0; b < boxes; ++b)
-              for (int i = lane; i < per; i += 32) sts_u4(a + (uint32_t)(b * kBox + rows * 128 + i * 16), make_uint4(0, 0, 0, 0));
+            const int boxes = N * (2 + (sums ? 0 : p.q_bytes / kBox));
+            for (int r = lane >> 3; r < (rows + 15) / 16 * 16; r += 4)       // 16 bytes each
+              if (!(mask >> r & 1ull))
+                for (int b = 0; b < boxes; ++b) sts_u4(a + (uint32_t)(b * kBox + r * 128 + (lane & 7) * 16), make_uint4(0, 0, 0, 0));
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
@@ -1584,12 +1613,12 @@ cudaError_t copies_tc(const Copy *c, int count, dc_dtype dtype, cudaStream_t st)
   return dtype == DC_BF16 ? dc_launch_pdl(k_group_rows_of<bf16>, grid, dim3(256), 0, st, all) : dc_launch_pdl(k_group_rows_of<float>, grid, dim3(256), 0, st, all);
 }
 
-// By the kernels for short runs: each row reads all of its adapter's matrix, 3 us and what that takes from L2 at 3 MB a us; tiles take 6 us, the last two of them for a cluster's
+// By the kernels for short runs: each row reads all of its adapter's matrix, 3 us, 2.5 for each eight CTAs of an SM, and what they take from L2 at 3 MB a us; tiles take 6 us, the last two of them for a cluster's
 // parts, and 0.25 for a piece.
 bool narrow_apart(const RowsJob &j) {
   if (!j.y_terms || (j.dtype == DC_F32 && (j.w_across ? j.n % 4 : j.k % 4) != 0)) return false;
   const int n_sm = dc_sm_count(), pieces = dc_div_up(j.k, kPiece);
-  const double wide = j.dtype == DC_F32 ? 2.0 : 1.0, apart = 3.0 + (double)j.rows * rank_pad(j.n) * j.k * 2.0 * wide / 3e6;
+  const double wide = j.dtype == DC_F32 ? 2.0 : 1.0, apart = 3.0 + (double)j.rows * (j.w_across ? 1.0 : rank_pad(j.n) / 8) / (8.0 * n_sm) * 2.5 + (double)j.rows * rank_pad(j.n) * j.k * 2.0 * wide / 3e6;
   const long long items = row_tiles(j.runs, 128);
   const int split = split_of(items, pieces, 4, n_sm);
   const double tiles = 6.0 + dc_div_up((int)(items < (1 << 20) ? items : 1 << 20) * split, n_sm) * (double)dc_div_up(pieces, split) * 0.25 * (wide > 1.0 ? 4.0 : 1.0);

@@ -529,7 +529,8 @@ typedef enum { DC_GROUP_FORWARD = 0, DC_GROUP_DX = 1, DC_GROUP_DW = 2 } dc_group
 typedef enum {
   DC_GROUP_TILES = 0,        /* tiles of 128 rows and up to 256 columns, by one CTA, or their sums by a cluster of `split` */
   DC_GROUP_PAIRS = 1,        /* tiles of 256 x 256 by two CTAs */
-  DC_GROUP_FEW_ROWS = 2      /* tiles of 128 columns and tile_cols (16 to 64) rows */
+  DC_GROUP_FEW_ROWS = 2,     /* tiles of 128 columns and tile_cols (16 to 64) rows */
+  DC_GROUP_FMAS = 3          /* fp32 by FMAs, from the arrays as they lie: tile_cols (4, 8 or 16) rows; split: sets of four warps to a tile */
 } dc_group_form;
 typedef struct { dc_group_form form; int tile_cols, split, stages; } dc_group_plan;
 dc_status dc_group_plan_query(long long rows, int runs, int c_in, int c_out, int rank, dc_dtype dtype, dc_group_part part, dc_group_plan *plan);

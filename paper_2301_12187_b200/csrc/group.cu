@@ -57,6 +57,15 @@ struct Parts {
   }
   cudaError_t copy(cudaStream_t st) { return copies_tc(copies, count, dtype, st); }
 };
+// Whether fp32 rows go by FMAs, straight from the caller's arrays: by terms x and all matrices are copied first, 10 bytes a number and a launch.
+bool direct(const RowsJob &j) {
+  if (j.dtype != DC_F32) return false;
+  double us = 0.0;
+  rows_tc(j, false, nullptr, nullptr, nullptr, &us);
+  const double numbers = j.w ? (double)j.rows * j.k + (double)j.runs.weights * j.n * j.k : 0.0;
+  return rows_few_us(j) < us + 3.0 + 3.0 + numbers * 10 / 4.5e6;
+}
+
 }  // namespace
 
 extern "C" dc_status dc_group_workspace_bytes(long long rows, int groups, int c_in, int c_out, dc_dtype dtype, size_t *bytes) {
@@ -85,11 +94,11 @@ extern "C" dc_status dc_group_forward(const void *x, long long rows, int c_in, c
   if (rows == 0) return DC_OK;
   Parts parts(workspace, dtype);
   RowsJob j = {};
-  j.x = parts.rows_of(x, rows, c_in);
+  j.x = x;
   j.rows = (int)rows;
   j.k = c_in;
   j.n = c_out;
-  j.w = parts.rows_of(w, (long long)groups * c_out, c_in);
+  j.w = w;
   j.x_pitch = j.w_pitch = parts.pitch(c_in);
   j.raw_x = x;
   j.raw_w = w;
@@ -99,6 +108,9 @@ extern "C" dc_status dc_group_forward(const void *x, long long rows, int c_in, c
   j.act = (int)act;
   j.y = y;
   j.dtype = dtype;
+  if (direct(j)) return status(rows_few(j, (cudaStream_t)stream));
+  j.x = parts.rows_of(x, rows, c_in);
+  j.w = parts.rows_of(w, (long long)groups * c_out, c_in);
   cudaError_t e = parts.copy((cudaStream_t)stream);
   if (e == cudaSuccess) e = rows_tc(j, false, (DcWsHeader *)workspace, (cudaStream_t)stream);
   return status(e);
@@ -116,26 +128,24 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
   if (rows == 0 && !dw && !db) return DC_OK;
   const Runs runs = {offsets, nullptr, groups, (int)rows, groups, 0};
   Parts parts(workspace, dtype);
-  const void *dy_at = parts.rows_of(dy, rows, c_out), *x_at = dw ? parts.rows_of(x, rows, c_in) : nullptr;
-  const void *w_at = dx ? parts.rows_of(w, (long long)groups * c_out, c_in) : nullptr;
+  RowsJob j = {};
+  j.x = j.raw_x = dy;
+  j.rows = (int)rows;
+  j.k = c_out;
+  j.n = c_in;
+  j.w = j.raw_w = w;
+  j.w_across = 1;
+  j.x_pitch = parts.pitch(c_out);
+  j.w_pitch = parts.pitch(c_in);
+  j.runs = runs;
+  j.y = dx;
+  j.dtype = dtype;
+  const bool with_dx = dx && rows, fmas = with_dx && direct(j);
+  const void *dy_at = dw || db || !fmas ? parts.rows_of(dy, rows, c_out) : nullptr, *x_at = dw ? parts.rows_of(x, rows, c_in) : nullptr;
+  j.x = dy_at;
+  if (with_dx && !fmas) j.w = parts.rows_of(w, (long long)groups * c_out, c_in);
   cudaError_t e = parts.copy((cudaStream_t)stream);
-  if (dx && rows && e == cudaSuccess) {
-    RowsJob j = {};
-    j.x = dy_at;
-    j.rows = (int)rows;
-    j.k = c_out;
-    j.n = c_in;
-    j.w = w_at;
-    j.w_across = 1;
-    j.x_pitch = parts.pitch(c_out);
-    j.w_pitch = parts.pitch(c_in);
-    j.runs = runs;
-    j.y = dx;
-    j.dtype = dtype;
-    j.raw_x = dy;
-    j.raw_w = w;
-    e = rows_tc(j, false, (DcWsHeader *)workspace, (cudaStream_t)stream);
-  }
+  if (with_dx && e == cudaSuccess) e = fmas ? rows_few(j, (cudaStream_t)stream) : rows_tc(j, false, (DcWsHeader *)workspace, (cudaStream_t)stream);
   if ((dw || db) && e == cudaSuccess) {
     GradJob j = {};
     j.p = dy_at;
@@ -150,7 +160,7 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
     j.dtype = dtype;
     j.raw_p = dy;
     j.raw_q = x;
-    e = grad_tc(j, dx && rows, (DcWsHeader *)workspace, (cudaStream_t)stream);
+    e = grad_tc(j, with_dx, (DcWsHeader *)workspace, (cudaStream_t)stream);
   }
   return status(e);
 }
@@ -195,25 +205,25 @@ dc_status check_adapter_call(long long rows, int c_in, int c_out, const void *w,
   return DC_OK;
 }
 // Rows through the adapters' first matrices -- a, or in the backward pass b read across -- scaled, to `out`.
-cudaError_t narrow(const void *raw_x, const void *x, int x_pitch, int rows, int k, const void *m, int m_pitch, bool backward, const dc_adapters *ad, const Runs &runs,
-                   void *out, dc_dtype dtype, void *workspace, cudaStream_t st) {
-  if (runs.count == 0) return cudaSuccess;
+RowsJob narrow_job(const void *x, int x_pitch, int rows, int k, int m_pitch, bool backward, const dc_adapters *ad, const Runs &runs, void *out, dc_dtype dtype) {
   RowsJob j = {};
-  j.x = x;
+  j.x = j.raw_x = x;
   j.rows = rows;
   j.k = k;
   j.n = ad->rank;
-  j.w = m;
+  j.w = j.raw_w = backward ? ad->b : ad->a;
   j.w_across = backward;
   j.x_pitch = x_pitch;
   j.w_pitch = m_pitch;
-  j.raw_x = raw_x;
-  j.raw_w = backward ? ad->b : ad->a;
   j.runs = runs;
   j.alpha = ad->scale;
   j.y = out;
   j.y_terms = 1;
   j.dtype = dtype;
+  return j;
+}
+cudaError_t narrow(const RowsJob &j, void *workspace, cudaStream_t st) {
+  if (j.runs.count == 0) return cudaSuccess;
   return narrow_apart(j) ? narrow_tc(j, st) : rows_tc(j, false, (DcWsHeader *)workspace, st);
 }
 }  // namespace
@@ -231,36 +241,37 @@ extern "C" dc_status dc_adapter_forward(const void *x, long long rows, int c_in,
   const Runs of = {offsets, which, runs, (int)rows, adapters->count, 1}, all = {nullptr, nullptr, 1, (int)rows, 1, 0};
   const cudaStream_t st = (cudaStream_t)stream;
   Parts parts(workspace, dtype);
-  const void *x_at = parts.rows_of(x, rows, c_in), *w_at = parts.rows_of(w, c_out, c_in);
-  const void *a_at = parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in);
-  const void *b_at = parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank);
   const int in = parts.pitch(c_in), of_rank = parts.pitch(adapters->rank);
-  bool apart = false;
-  cudaError_t e = parts.copy((cudaStream_t)stream);
-  if (e == cudaSuccess) e = narrow(x, x_at, in, (int)rows, c_in, a_at, in, false, adapters, of, saved, dtype, workspace, st);
-  if (e != cudaSuccess) return status(e);
-  RowsJob j = {};
-  j.x = x_at;
+  RowsJob t = narrow_job(x, in, (int)rows, c_in, in, false, adapters, of, saved, dtype), j = {};
+  j.x = j.raw_x = x;
   j.rows = (int)rows;
   j.k = c_in;
   j.n = c_out;
-  j.w = w_at;
+  j.w = j.raw_w = w;
   j.x_pitch = j.w_pitch = in;
   j.runs = all;
   j.t = runs ? saved : nullptr;
-  j.e = b_at;
+  j.e = j.raw_e = adapters->b;
   j.e_pitch = of_rank;
-  j.raw_x = x;
-  j.raw_w = w;
-  j.raw_e = adapters->b;
   j.rank = adapters->rank;
   j.ext = of;
+  j.dtype = dtype;
+  // what the kernels read is copied first, unless they read fp32 as it lies
+  const bool fmas = direct(j), raw = dtype == DC_F32 && (!runs || narrow_apart(t));
+  if (!fmas || !raw) j.x = t.x = parts.rows_of(x, rows, c_in);
+  if (!raw) t.w = parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in);
+  if (!fmas) {
+    j.w = parts.rows_of(w, c_out, c_in);
+    j.e = parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank);
+  }
+  cudaError_t e = parts.copy(st);
+  if (e == cudaSuccess) e = narrow(t, workspace, st);
+  if (e != cudaSuccess) return status(e);
   j.bias = bias;
   j.act = (int)act;
   j.residual = residual;
   j.y = y;
-  j.dtype = dtype;
-  return status(rows_tc(j, runs > 0, (DcWsHeader *)workspace, st));
+  return status(fmas ? rows_few(j, st) : rows_tc(j, runs > 0, (DcWsHeader *)workspace, st));
 }
 
 extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int c_in, const void *w, int c_out,
@@ -277,14 +288,37 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
   Parts parts(workspace, dtype);
   void *u = parts.add(saved_bytes(rows, adapters->rank, dtype));
   const bool with_u = (dx || da) && rows;
-  const void *dy_at = parts.rows_of(dy, rows, c_out), *x_at = da ? parts.rows_of(x, rows, c_in) : nullptr, *w_at = dx ? parts.rows_of(w, c_out, c_in) : nullptr;
-  const void *a_at = dx ? parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in) : nullptr;
-  const void *b_at = with_u ? parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank) : nullptr;
   const int in = parts.pitch(c_in), out = parts.pitch(c_out), of_rank = parts.pitch(adapters->rank);
+  RowsJob t = narrow_job(dy, out, (int)rows, c_out, of_rank, true, adapters, of, u, dtype), j = {};
+  j.x = j.raw_x = dy;
+  j.rows = (int)rows;
+  j.k = c_out;
+  j.n = c_in;
+  j.w = j.raw_w = w;
+  j.w_across = 1;
+  j.x_pitch = out;
+  j.w_pitch = in;
+  j.runs = all;
+  j.t = runs ? u : nullptr;
+  j.e = j.raw_e = adapters->a;
+  j.e_across = 1;
+  j.e_pitch = in;
+  j.rank = adapters->rank;
+  j.ext = of;
+  j.y = dx;
+  j.dtype = dtype;
+  const bool with_dx = dx && rows, fmas = with_dx && direct(j), raw = dtype == DC_F32 && (!with_u || !runs || narrow_apart(t));
+  const void *dy_at = (with_dx && !fmas) || (with_u && !raw) || db ? parts.rows_of(dy, rows, c_out) : nullptr, *x_at = da ? parts.rows_of(x, rows, c_in) : nullptr;
+  j.x = t.x = dy_at;
+  if (with_u && !raw) t.w = parts.rows_of(adapters->b, (long long)adapters->count * c_out, adapters->rank);
+  if (with_dx && !fmas) {
+    j.w = parts.rows_of(w, c_out, c_in);
+    j.e = parts.rows_of(adapters->a, (long long)adapters->count * adapters->rank, c_in);
+  }
   // One behind the other: u, with db beside it; dx, with da beside it (which reads u from its start: not beside a dx that has not waited for u).
-  const bool dx_early = !db && with_u && runs;
+  const bool dx_early = !db && with_u && runs && !fmas;
   cudaError_t e = parts.copy(st);
-  if (with_u && e == cudaSuccess) e = narrow(dy, dy_at, out, (int)rows, c_out, b_at, of_rank, true, adapters, of, u, dtype, workspace, st);
+  if (with_u && e == cudaSuccess) e = narrow(t, workspace, st);
   GradJob g = {};
   g.runs = of;
   g.dtype = dtype;
@@ -299,30 +333,7 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
     g.out = db;
     e = grad_tc(g, with_u && runs, (DcWsHeader *)workspace, st);
   }
-  if (dx && rows && e == cudaSuccess) {
-    RowsJob j = {};
-    j.x = dy_at;
-    j.rows = (int)rows;
-    j.k = c_out;
-    j.n = c_in;
-    j.w = w_at;
-    j.w_across = 1;
-    j.x_pitch = out;
-    j.w_pitch = in;
-    j.runs = all;
-    j.t = runs ? u : nullptr;
-    j.e = a_at;
-    j.e_across = 1;
-    j.e_pitch = in;
-    j.raw_x = dy;
-    j.raw_w = w;
-    j.raw_e = adapters->a;
-    j.rank = adapters->rank;
-    j.ext = of;
-    j.y = dx;
-    j.dtype = dtype;
-    e = rows_tc(j, dx_early, (DcWsHeader *)workspace, st);
-  }
+  if (with_dx && e == cudaSuccess) e = fmas ? rows_few(j, st) : rows_tc(j, dx_early, (DcWsHeader *)workspace, st);
   if (da && e == cudaSuccess) {                  // as x^T u, so that the long side is the instructions' 128 rows
     g.p = x_at;
     g.raw_p = x;
@@ -331,7 +342,7 @@ extern "C" dc_status dc_adapter_backward(const void *dy, const void *x, long lon
     g.q = u;
     g.out = da;
     g.out_across = 1;
-    e = grad_tc(g, dx && rows && !dx_early, (DcWsHeader *)workspace, st);
+    e = grad_tc(g, with_dx && !dx_early, (DcWsHeader *)workspace, st);
   }
   return status(e);
 }
@@ -368,5 +379,10 @@ extern "C" dc_status dc_group_plan_query(long long rows, int runs, int c_in, int
   j.e_pitch = dtype == DC_BF16 && rank % 8 == 0 ? (part == DC_GROUP_DX ? c_in : rank) : 64;
   j.ext = of;
   j.dtype = dtype;
+  j.raw_w = there;
+  if (direct(j)) {
+    *plan = {DC_GROUP_FMAS, rows_few_tile(j), rows_few_sets(j), 3};
+    return DC_OK;
+  }
   return rows_tc(j, false, nullptr, nullptr, plan) == cudaSuccess ? DC_OK : DC_ERR_CUDA;
 }

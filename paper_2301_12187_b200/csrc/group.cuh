@@ -149,8 +149,14 @@ cudaError_t copies_tc(const Copy *c, int count, dc_dtype dtype, cudaStream_t st)
 // writes; nothing else of the caller's is between them.  Both then run side by side as far as there is room, and this one ends behind that one.
 bool narrow_apart(const RowsJob &j);             // y_terms: by a kernel for short runs
 cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st);
-// with `plan`: says how, and launches nothing
-cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan = nullptr);
+// with `plan`: says how, and launches nothing; with `us`: how long tiles of 128 rows would take
+cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan = nullptr, double *us = nullptr);
 cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan = nullptr);
+
+// fp32 rows of short runs by FMAs, from the caller's arrays (group_few.cu); like those above it lets the next launch begin behind its own wait
+double rows_few_us(const RowsJob &j);            // estimated
+int rows_few_tile(const RowsJob &j);             // rows of its tiles
+int rows_few_sets(const RowsJob &j);             // of four warps to a tile
+cudaError_t rows_few(const RowsJob &j, cudaStream_t st);
 
 }  // namespace grp

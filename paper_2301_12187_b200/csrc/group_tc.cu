@@ -6,7 +6,7 @@
 // Matrices that the sum runs across ([k][n], and both operands of a gradient, [rows][...]) are read as they lie: pieces are then 64
 // neighbouring columns of 64 rows, and the instruction takes them the other way round.
 //   kTile   128 rows of a run x up to 256 columns of its matrix.
-//   kFew    runs of few rows: 128 columns of the matrix take the place of the 128 rows, so that an instruction is as wide as there are rows and
+//   kFew    runs of few rows (bf16): 128 columns of the matrix take the place of the 128 rows, so that an instruction is as wide as there are rows and
 //           the matrix streams through once.  Adapters' parts of those columns, a row's after a row's, come through a ring of their own.
 //   kGrad   128 x up to 256 of a gradient: the sum runs over the rows of a weight's runs.  Where a run ends inside a piece, rows of other weights in it are set to zero by
 //           a warp, in both operands (0 times a NaN is a NaN).
@@ -41,7 +41,7 @@ constexpr int kP = 128 * 128;                    // bytes of the 128-row operand
 constexpr int kBox = 64 * 128;                   // 64 columns of 64 rows
 constexpr int kOut = kEpi * 32 * 128;            // staged results: 32 rows x 32 sums a warp
 constexpr int kSuper = 16;                       // rows of tiles that are walked together: 16 x 9 tiles at once read a twelfth of what a row or column of them would
-constexpr int kFewMost = 64, kFewWide = 32;     // rows of a tile of kFew; of fp32, whose sums are kept in registers
+constexpr int kFewMost = 64, kFewWide = 32;     // rows of a tile of kFew; of adapters of a high rank, which then have as many slots
 constexpr unsigned long long kLongNs = 20ull * 1000ull * 1000ull * 1000ull;      // a gradient's tile may take seconds (a sum over 2^30 rows), and so may NaN by FMAs
 
 typedef __nv_bfloat16 bf16;
@@ -67,9 +67,9 @@ struct Params {
   int rank, rank_pieces;     // adapters: pieces of 64 of the rank
   int t_bytes, e_bytes, e_wide;      // kTile: bytes of a stage's rows of t and e; numbers of the rank in a row (e across: rows)
   const bf16 *t;             // what rows keep
-  const void *e;             // kFew: what the reading-out warps take of the adapters
-  int e_pitch, e_vec;
-  int slots, slot_rows, row_bytes;       // kFew, bf16: of adapters' parts of the tile's columns in shared memory, slot_rows rows' to a slot
+  const void *e;             // kFew: the adapters' matrices; fp32: as the caller has them
+  int e_pitch;
+  int slots, slot_rows, row_bytes;       // kFew: of adapters' parts of the tile's columns in shared memory, slot_rows rows' to a slot
   int early;                 // all but t was there before the launch in front of this one began, and that one writes nothing that this one does
   int off_out, off_t;        // staged results; kFew: t's numbers in shared memory
   // kGrad
@@ -1014,7 +1014,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
             sts_f(ts + (uint32_t)(i * 4), kept<T>(p.t, t.row0 + r, pad, i - r * pad));
           }
           bar_sync(2, kEpi * 32);
-          if (sizeof(T) == 2) {
+          {
             // Slots go to the sets of warps in turn.  Rows of a slot would lie in the same banks for neighbouring lanes: each lane begins with another piece of 8 numbers.
             const int chunks = (p.rank + 7) / 8, turned = own * (p.e_pitch / 8) / 8 % chunks, listed = listed_s;
             for (int q = set; q < here; q += 2) sts_f(part_at(es, share + p.split * q), 0.f);
@@ -1060,51 +1060,6 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
             }
             groups += (listed + p.slot_rows - 1) / p.slot_rows;
             if (p.split > 1) bar_sync(2, kEpi * 32);        // rows are delivered by others than those who worked their parts out
-          } else {
-            constexpr int kAtOnce = 4;           // rows, for as many loads on their way
-#pragma unroll 1
-            for (int q0 = set; q0 < here; q0 += 2 * kAtOnce) {
-              int w[kAtOnce], r[kAtOnce];
-              float sum[kAtOnce];
-#pragma unroll
-              for (int i = 0; i < kAtOnce; ++i) {
-                r[i] = q0 + 2 * i < here ? share + p.split * (q0 + 2 * i) : -1;
-                w[i] = r[i] >= 0 && o < p.n ? weight_s[r[i]] : -1;
-                sum[i] = 0.f;
-              }
-#pragma unroll 1
-              for (int j0 = 0; j0 < p.rank; j0 += 8) {
-                float e[kAtOnce][8];
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i) {
-                  const T *at = reinterpret_cast<const T *>(p.e) + (ACROSS ? ((size_t)max(w[i], 0) * (size_t)p.rank + (size_t)j0) * (size_t)p.e_pitch + (size_t)o
-                                                                           : ((size_t)max(w[i], 0) * (size_t)p.n + (size_t)o) * (size_t)p.e_pitch + (size_t)j0);
-                  if (!ACROSS && p.e_vec) {
-#pragma unroll
-                    for (int x = 0; x < 8; x += 4) {
-                      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-                      if (w[i] >= 0 && j0 + x < p.rank) f = __ldg(reinterpret_cast<const float4 *>(at + x));
-                      e[i][x] = f.x; e[i][x + 1] = f.y; e[i][x + 2] = f.z; e[i][x + 3] = f.w;
-                    }
-                  } else {
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) e[i][x] = w[i] >= 0 && j0 + x < p.rank ? to_float(at[(size_t)x * (size_t)(ACROSS ? p.e_pitch : 1)]) : 0.f;
-                  }
-                }
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i) {
-                  if (w[i] < 0) continue;        // t may be no number there
-                  const uint32_t at = ts + (uint32_t)((r[i] * pad + j0) * 4);
-                  const uint4 t0 = lds_u4(at), t1 = lds_u4(at + 16);
-                  const uint32_t tv[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
-#pragma unroll
-                  for (int x = 0; x < 8; ++x) sum[i] = fmaf(__uint_as_float(tv[x]), e[i][x], sum[i]);
-                }
-              }
-#pragma unroll
-              for (int i = 0; i < kAtOnce; ++i)
-                if (r[i] >= 0) sts_f(part_at(es, r[i]), sum[i]);
-            }
           }
           if (p.split == 1) bar_sync(2, kEpi * 32);       // rows are then delivered by whom their sums lie with
         }
@@ -1113,7 +1068,6 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           if (r >= count || o >= p.n) return;
           const size_t at = (size_t)(t.row0 + r) * (size_t)p.n + (size_t)o;
           if (p.rank) v += lds_f(part_at(es, r));
-          if (kShort && !(v == v)) v = again<ACROSS>(p, t.row0 + r, t.weight, o);
           v += b;
           if (p.residual) v += to_float(reinterpret_cast<const T *>(p.residual)[at]);
           reinterpret_cast<T *>(p.y)[at] = (T)dc_act_apply(v, p.act);
@@ -1133,35 +1087,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         };
         if (p.split > 1 && met++ == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");         // the other CTAs are there
         // a wait that ran out does not end the loop: the barriers above are of all these warps
-        float short_sum[kShort ? kFewWide / 2 : 1];
-        if (kShort) {
-#pragma unroll
-          for (int i = 0; i < (kShort ? kFewWide / 2 : 1); ++i) short_sum[i] = 0.f;
-#pragma unroll 1
-          for (int k = 0; k < max(own_pieces, 1); ++k, ++turn) {
-            ok = wait_sums();
-            if (!ok) break;
-            const uint32_t d = sums_at() + (uint32_t)(set * half_rows);
-#pragma unroll
-            for (int i0 = 0; i0 < kFewWide / 2; i0 += 8) {
-              if (i0 >= half_rows) break;
-              float v[8];
-              __syncwarp();
-              tmem_ld8(d + (uint32_t)i0, reinterpret_cast<uint32_t *>(v));
-              tmem_ld_wait();
-              if (own_pieces) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) short_sum[kShort ? i0 + i : 0] += v[i];
-              }
-            }
-            release();
-          }
-          if (ok) {
-#pragma unroll
-            for (int i0 = 0; i0 < (kShort ? kFewWide / 2 : 0); i0 += 8)
-              if (i0 < half_rows) hand_on(i0, short_sum + i0);
-          }
-        } else {
+        {
           ok = wait_sums();
           const uint32_t d = sums_at() + (uint32_t)(set * half_rows);
 #pragma unroll 1
@@ -1201,7 +1127,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
       if (p.split > 1 && met == 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     }
   } else if (FORM == kFew) {
-    // ---------------------------------------------------------------- kFew: which adapters rows have; bf16: their parts of the tile's columns
+    // ---------------------------------------------------------------- kFew: which adapters rows have, and their parts of the tile's columns
     const uint32_t ring = sm + (uint32_t)(p.off_t + p.nt * grp::rank_pad(p.rank) * 4 + p.nt * 512 + (p.split > 1 ? p.split * ((p.nt + p.split - 1) / p.split) * 512 : 0));
     grp::Walk walk;
     walk.start();
@@ -1228,30 +1154,29 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         if (lane == 0) listed_s = listed;
         __syncwarp();
         bar_sync(1, kEpi * 32 + 32);
-        if (sizeof(T) == 2)
-          for (int i0 = 0; i0 < listed; i0 += p.slot_rows, ++group) {
-            const int slot = group % p.slots, rows = min(p.slot_rows, listed - i0);
-            ok = ok && warp_wait(&bar[kEEmpty + slot], ((uint32_t)(group / p.slots) & 1u) ^ 1u, abort_flag, ws, 0xB0000u | (uint32_t)slot);
-            if (!ok) continue;
-            const uint32_t to = ring + (uint32_t)(slot * p.slot_rows * p.row_bytes);
-            const bf16 *e = reinterpret_cast<const bf16 *>(p.e);
-            if (ACROSS) {                        // `rank` rows of the tile's columns
-              const uint32_t bytes = (uint32_t)min(128, p.e_pitch - o0) * 2u;
-              if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)(p.rank * rows));
-              __syncwarp();
-              for (int i = 0; i < rows; ++i) {
-                const bf16 *from = e + (size_t)weight_s[list_s[i0 + i]] * (size_t)p.rank * (size_t)p.e_pitch + (size_t)o0;
-                for (int j = lane; j < p.rank; j += 32) bulk_load(to + (uint32_t)(i * p.row_bytes + j * 256), from + (size_t)j * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
-              }
-            } else {                             // the columns' rows, one piece
-              const uint32_t bytes = (uint32_t)(min(128, p.n - o0) * p.e_pitch) * 2u;
-              if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)rows);
-              __syncwarp();
-              if (lane < rows)
-                bulk_load(to + (uint32_t)(lane * p.row_bytes), e + ((size_t)weight_s[list_s[i0 + lane]] * (size_t)p.n + (size_t)o0) * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
-            }
+        for (int i0 = 0; i0 < listed; i0 += p.slot_rows, ++group) {
+          const int slot = group % p.slots, rows = min(p.slot_rows, listed - i0);
+          ok = ok && warp_wait(&bar[kEEmpty + slot], ((uint32_t)(group / p.slots) & 1u) ^ 1u, abort_flag, ws, 0xB0000u | (uint32_t)slot);
+          if (!ok) continue;
+          const uint32_t to = ring + (uint32_t)(slot * p.slot_rows * p.row_bytes);
+          const bf16 *e = reinterpret_cast<const bf16 *>(p.e);
+          if (ACROSS) {                        // `rank` rows of the tile's columns
+            const uint32_t bytes = (uint32_t)min(128, p.e_pitch - o0) * 2u;
+            if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)(p.rank * rows));
             __syncwarp();
+            for (int i = 0; i < rows; ++i) {
+              const bf16 *from = e + (size_t)weight_s[list_s[i0 + i]] * (size_t)p.rank * (size_t)p.e_pitch + (size_t)o0;
+              for (int j = lane; j < p.rank; j += 32) bulk_load(to + (uint32_t)(i * p.row_bytes + j * 256), from + (size_t)j * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
+            }
+          } else {                             // the columns' rows, one piece
+            const uint32_t bytes = (uint32_t)(min(128, p.n - o0) * p.e_pitch) * 2u;
+            if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)rows);
+            __syncwarp();
+            if (lane < rows)
+              bulk_load(to + (uint32_t)(lane * p.row_bytes), e + ((size_t)weight_s[list_s[i0 + lane]] * (size_t)p.n + (size_t)o0) * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
           }
+          __syncwarp();
+        }
       }
   } else {
     // ---------------------------------------------------------------- kGrad: pieces with rows of other weights are passed on once those are zeros.  (Asked for by
@@ -1517,8 +1442,10 @@ cudaError_t launch(Params &p, long long items, int n_sm, const CUtensorMap (&m)[
 }
 template <int FORM, bool ACROSS>
 cudaError_t launch_any(Params &p, bool wide, bool pair, long long items, int n_sm, const CUtensorMap (&m)[4], DcWsHeader *ws, cudaStream_t st) {
-  if (wide) return launch<FORM, ACROSS, float, false>(p, items, n_sm, m, ws, st);
-  if (FORM != kFew && pair) return launch<FORM, ACROSS, bf16, FORM != kFew>(p, items, n_sm, m, ws, st);
+  if constexpr (FORM != kFew) {
+    if (wide) return launch<FORM, ACROSS, float, false>(p, items, n_sm, m, ws, st);
+    if (pair) return launch<FORM, ACROSS, bf16, true>(p, items, n_sm, m, ws, st);
+  }
   return launch<FORM, ACROSS, bf16, false>(p, items, n_sm, m, ws, st);
 }
 
@@ -1569,17 +1496,17 @@ Shape shape_of(int n, double rows, double runs, double pieces, double matrices, 
 }
 // The same for short runs: rows to a tile, and CTAs to its sum, in microseconds.  The matrix comes once for each tile of rows (82 GB/s to an SM), the rows'
 // adapters 0.3 a row or at 40 GB/s, in two sets of warps; a cluster meets.
-Shape few_shape_of(const grp::RowsJob &j, int runs, long long (*row_tiles)(const Runs &, int), int pieces, double matrices, bool wide, int n_sm) {
-  const int mean = j.rows / runs, terms = wide ? 3 : 1;
+Shape few_shape_of(const grp::RowsJob &j, int runs, long long (*row_tiles)(const Runs &, int), int pieces, double matrices, int n_sm) {
+  const int mean = j.rows / runs;
   Shape best = {16, false, 1, 1e30};
-  for (int nt = 16; nt <= ((wide || j.rank > 64) && j.t ? kFewWide : wide ? kFewWide : kFewMost); nt *= 2) {
+  for (int nt = 16; nt <= (j.rank > 64 && j.t ? kFewWide : kFewMost); nt *= 2) {
     if (runs > 1 && nt > 16 && mean <= nt * 3 / 8) break;
     const long long all = row_tiles(j.runs, nt) * dc_div_up(j.n, 128);
     const double tiles = ((double)j.rows / nt + (runs > 1 ? 0.7 : 0.5) * runs) * dc_div_up(j.n, 128);
     for (int split = 1; split <= kMaxSplit; ++split) {
       if (split > 1 && (all > clusters_at_once(split, n_sm) || (pieces ? split > pieces / 4 : !j.t || split > nt / 4))) break;
       const double rounds = (runs > 1 && split == 1 ? tiles : (double)all) * split / n_sm, rows = (double)(j.rows < nt ? j.rows : nt) / split / 2;
-      const double stream = (double)dc_div_up(pieces, split) * terms * (kP + nt * 128) / 82e3, memory = matrices / 6.5e6;
+      const double stream = (double)dc_div_up(pieces, split) * (kP + nt * 128) / 82e3, memory = matrices / 6.5e6;
       const double row = 256.0 * grp::rank_pad(j.rank) / 40e3, ext = j.t ? 2.0 + rows * (row > 0.3 ? row : 0.3) : 0.0;
       const double work = stream > ext ? stream : ext, out = 0.6 + nt * 0.02;
       const double all_of = (rounds < 1 ? 1 : rounds + 0.3) * (work > out ? work : out) + 0.3 * (memory < work ? memory : work) + (split > 1 ? 1.2 : 0.5);
@@ -1636,7 +1563,7 @@ cudaError_t narrow_tc(const RowsJob &j, cudaStream_t st) {
   return dc_launch_pdl(k_adapter_narrow<float>, grid, dim3(256), 0, st, x, j.k, w, j.k, j.k, j.n, j.runs, j.alpha, y);
 }
 
-cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan) {
+cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t st, dc_group_plan *plan, double *us) {
   const int n_sm = dc_sm_count();
   const bool wide = j.dtype == DC_F32;
   const int terms = wide ? 3 : 1;
@@ -1663,8 +1590,7 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
     p.rank_pieces = dc_div_up(j.rank, kPiece);
     p.t = (const bf16 *)j.t;
     p.e = wide ? j.raw_e : j.e;
-    p.e_pitch = wide ? (j.e_across ? j.n : j.rank) : j.e_pitch;
-    p.e_vec = !wide || j.rank % 4 == 0;
+    p.e_pitch = j.e_pitch;
   }
   const int runs = runs_with_rows(j.runs);
   const double matrices = j.w ? (double)runs * j.n * j.k * 2 * terms : 0.0;
@@ -1672,10 +1598,14 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   const double per_tile = j.t ? 1.0 + 128.0 * j.ext.count / j.rows : 0.0, more = 850.0 * (per_tile < 129.0 ? per_tile : 129.0) * (wide ? 2.0 : 1.0);
   const Shape tile = j.y_terms ? Shape{rank_pad(j.n), false, 1, 0.0} : shape_of(j.n, j.rows, runs, p.pieces, matrices, more, wide, n_sm);
   // runs of up to 128 rows: 128 columns of a matrix in the place of 128 rows, where that is faster
+  if (us) {
+    *us = tile.us;
+    return cudaSuccess;
+  }
   Shape shape = tile;
   bool by_few = false;
-  if (!j.y_terms && j.rows / runs <= 128) {
-    const Shape f = few_shape_of(j, runs, row_tiles, p.pieces, matrices, wide, n_sm);
+  if (!j.y_terms && !wide && j.rows / runs <= 128) {
+    const Shape f = few_shape_of(j, runs, row_tiles, p.pieces, matrices, n_sm);
     by_few = f.us <= tile.us;
     if (by_few) shape = f;
   }
@@ -1689,7 +1619,7 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
     p.tiles_n = dc_div_up(j.n, 128);
     items = row_tiles(j.runs, p.nt) * p.tiles_n;
     int apart = (p.rank ? p.nt * (rank_pad(p.rank) * 4 + 512) : 0) + (p.split > 1 ? (p.nt + p.split) * 512 : 0);
-    if (p.rank && !wide) {
+    if (p.rank) {
       p.row_bytes = j.e_across ? p.rank * 256 : 128 * p.e_pitch * 2;
       p.slot_rows = 16384 / p.row_bytes < 1 ? 1 : 16384 / p.row_bytes < 8 ? 16384 / p.row_bytes : 8;
       p.slots = 65536 / (p.slot_rows * p.row_bytes) < kMaxSlots ? 65536 / (p.slot_rows * p.row_bytes) : kMaxSlots;

@@ -24,7 +24,7 @@ MERGE_AUTO, MERGE_STEPS = 0, 1
 MX4, NV4 = 0, 1
 Q4_TILES, Q4_PAIRS, Q4_FEW_ROWS, Q4_STREAM = range(4)
 GROUP_FORWARD, GROUP_DX, GROUP_DW = range(3)
-GROUP_TILES, GROUP_PAIRS, GROUP_FEW_ROWS = range(3)
+GROUP_TILES, GROUP_PAIRS, GROUP_FEW_ROWS, GROUP_FMAS = range(4)
 
 _FP = C.POINTER(C.c_float)
 

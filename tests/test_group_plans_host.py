@@ -48,12 +48,15 @@ def test_plans_are_in_range():
                 rng.choice([dc.BF16, dc.F32]))
         for part in range(3):
             p = dc.group_plan(*args, part)
+            if p.form == dc.GROUP_FMAS:
+                assert p.tile_cols in (4, 8, 16) and part != dc.GROUP_DW and args[5] == dc.F32
+                continue
             assert p.form in (dc.GROUP_TILES, dc.GROUP_PAIRS, dc.GROUP_FEW_ROWS) and 16 <= p.tile_cols <= 256 and p.tile_cols % 16 == 0, args
             assert 1 <= p.split <= 8 and 1 <= p.stages <= 8, (args, part, p.stages)
             if p.form == dc.GROUP_PAIRS:
                 assert p.tile_cols == 256 and p.split == 1
             if p.form == dc.GROUP_FEW_ROWS:
-                assert p.tile_cols <= 64 and part != dc.GROUP_DW
+                assert p.tile_cols <= 64 and part != dc.GROUP_DW and args[5] == dc.BF16
 
 
 def test_plan_query_refuses():

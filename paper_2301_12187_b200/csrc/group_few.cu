@@ -7,7 +7,7 @@
 //   across  it runs across them: eight lanes to the 32 columns, H x 16 such sets share the sum.
 // The next step's weights are on their way into registers and two steps' rows into shared memory.  Partial sums meet by shuffles that halve what a
 // lane holds, and in shared memory.  Two CTAs to an SM, as what they wait for is longer than what they add: 64 groups of 16 rows, 2048 -> 1408,
-// take 254 us (one of eight warps: 348; rows read through L1: 332; by terms 554; 114 for the weights' bytes).  Weights that few rows share come
+// take 241 us (one of eight warps: 348; rows read through L1: 332; by terms 554; 114 for the weights' bytes).  Weights that few rows share come
 // at the rate of memory: 64 groups of 2 rows in 134 us (by terms 525).
 #include <math.h>
 
@@ -53,6 +53,29 @@ __device__ __forceinline__ void halve(float *v, int lane, int &first) {
       halve<1, FROM / 2, TO>(v, lane, first);
     }
   }
+}
+
+// An adapter's part of one value along the adapters' rows, 32 of the rank at a time.  (As further numbers of the sum, by the lanes that share it, most of
+// which a low rank leaves without any: 379 rows of rank 6, 152 -> 600, 23 us for 17.)
+__device__ __forceinline__ float of_adapter(const RowsJob &j, int a, const float *t, int o) {
+  if (a < 0) return 0.f;                         // t may be no number there
+  const float *e = reinterpret_cast<const float *>(j.raw_e) + ((size_t)a * (size_t)j.n + (size_t)o) * (size_t)j.rank;
+  float sum = 0.f;
+#pragma unroll 1
+  for (int q = 0; q < j.rank; q += 32) {
+    float v[32];
+    if (j.rank % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 4) load4<true, 0>(e + q + i, 0, j.rank - q - i, *reinterpret_cast<float (*)[4]>(v + i));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = q + i < j.rank ? __ldg(e + q + i) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (q + i < j.rank) sum = fmaf(t[q + i], v[i], sum);
+  }
+  return sum;
 }
 
 __device__ __forceinline__ void deliver(const RowsJob &j, int row, int weight, int o, float v) {
@@ -148,28 +171,18 @@ __device__ __forceinline__ void tile(const RowsJob &j, float *xs, float *parts, 
       }
     }
   }
-  if (j.t) {
+  if (ACROSS && j.t) {                           // the adapters' rows are further numbers of the sum
     const float *e = reinterpret_cast<const float *>(j.raw_e);
-    const int pad = grp::rank_pad(j.rank);
+#pragma unroll 1
+    for (int q = set; q < j.rank; q += 16 * H) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int a = adapter[r];
-      if (a < 0) continue;                       // t may be no number there
+      for (int r = 0; r < R; ++r) {
+        const bool is = adapter[r] >= 0;         // t may be no number where there is no adapter
+        float v[4];
+        load4<VEC, 8>(e + ((size_t)max(adapter[r], 0) * (size_t)j.rank + (size_t)q) * (size_t)j.n + (size_t)o0, oct, is ? cols : 0, v);
+        const float t = is ? ts[r * grp::rank_pad(j.rank) + q] : 0.f;
 #pragma unroll
-      for (int u = 0; u < (ACROSS ? 8 / H : 4); ++u) {
-        const int q = ACROSS ? set + 16 * H * u : half + lane + 32 * u;            // along: ranks go to 128, the other half has none
-        if (q >= j.rank) break;
-        const float t = ts[r * pad + q];
-        if (ACROSS) {
-          float v[4];
-          load4<VEC, 8>(e + ((size_t)a * (size_t)j.rank + (size_t)q) * (size_t)j.n + (size_t)o0, oct, cols, v);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[r][c] = fmaf(t, v[c], acc[r][c]);
-        } else {
-#pragma unroll
-          for (int c = 0; c < kOwn; ++c)
-            acc[r][c] = fmaf(t, __ldg(e + ((size_t)a * (size_t)j.n + (size_t)(o0 + min(own + c, cols - 1))) * (size_t)j.rank + (size_t)q), acc[r][c]);
-        }
+        for (int c = 0; c < 4; ++c) acc[r][c] = fmaf(t, v[c], acc[r][c]);
       }
     }
   }
@@ -185,6 +198,7 @@ __device__ __forceinline__ void tile(const RowsJob &j, float *xs, float *parts, 
     for (int i = 0; i < R / 4; ++i) parts[((warp >> 2) * R + (first + i) / 8) * kCols + own + (first + i) % 8] = sums[i];
   }
   __syncthreads();
+#pragma unroll 1
   for (int i = tid; i < rows * kCols; i += kThreads) {
     const int r = i / kCols, o = i - r * kCols;
     float v = parts[i];
@@ -194,7 +208,9 @@ __device__ __forceinline__ void tile(const RowsJob &j, float *xs, float *parts, 
     } else if (H == 2) {
       v += parts[R * kCols + i];
     }
-    if (o < cols) deliver(j, row0 + r, weight, o0 + o, v);
+    if (o >= cols) continue;
+    if (!ACROSS && j.t) v += of_adapter(j, adapter[r], ts + r * grp::rank_pad(j.rank), o0 + o);
+    deliver(j, row0 + r, weight, o0 + o, v);
   }
 }
 

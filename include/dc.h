@@ -458,7 +458,7 @@ dc_status dc_q4_plan_query(long long rows, int c_in, int c_out, dc_q4_format for
  * decreasing, from 0 to at most `rows`.  A run may be empty, and rows in front of the first or behind the last run belong to none.  (Offsets are cut to
  * [0, rows]; where they decrease, rows may be written twice, with no order between the two, and none outside the arrays.)
  * Rows are dense, of `dtype`, and multiplied on the tensor core with fp32 sums: DC_BF16 as they are, DC_F32 as products of bf16 terms as described at
- * dc_merge_chain (results that are no numbers come out as FMAs give them, which takes long).  Results are rounded once.
+ * dc_merge_chain (results that are no numbers come out as FMAs give them, which takes long), or where runs are short by FMAs.  Results are rounded once.
  * rows: 0 to 2^30; without rows, forward calls write nothing.  Widths: 1 to 2^20.  Workspaces: device, the bytes that the query
  * says, the first 256 zeroed once by the caller; a bounded wait that runs out is latched there (dc_workspace_status).  Calls that may run at
  * once need a workspace each.
@@ -528,8 +528,8 @@ dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int
 typedef enum { DC_GROUP_FORWARD = 0, DC_GROUP_DX = 1, DC_GROUP_DW = 2 } dc_group_part;   /* y; dx; dw (of adapters da) */
 typedef enum {
   DC_GROUP_TILES = 0,        /* tiles of 128 rows and up to 256 columns, by one CTA, or their sums by a cluster of `split` */
-  DC_GROUP_PAIRS = 1,        /* tiles of 256 x 256 by two CTAs */
-  DC_GROUP_FEW_ROWS = 2,     /* tiles of 128 columns and tile_cols (16 to 64) rows */
+  DC_GROUP_PAIRS = 1,        /* bf16: tiles of 256 x 256 by two CTAs */
+  DC_GROUP_FEW_ROWS = 2,     /* bf16: tiles of 128 columns and tile_cols (16 to 64) rows */
   DC_GROUP_FMAS = 3          /* fp32 by FMAs, from the arrays as they lie: tile_cols (4, 8 or 16) rows; split: sets of four warps to a tile */
 } dc_group_form;
 typedef struct { dc_group_form form; int tile_cols, split, stages; } dc_group_plan;

@@ -153,6 +153,47 @@ def test_group_backward(case, dtype):
     assert bool((dx.t[~mine] == 55.0).all())
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("most", [1, 9, 40])
+def test_more_runs_than_one_look_finds(most, dtype):
+    """1500 groups of up to `most` rows, many of them empty: tiles are found by walking over the runs, and a CTA has several."""
+    dt, n, c_in, c_out = TYPES[dtype], 1500, 24, 72
+    of_type(dt)
+    g = torch.Generator().manual_seed(most)
+    sizes = torch.randint(0, most + 1, (n,), generator=g).tolist()
+    rows, off = sum(sizes), offsets_of(sizes)
+    of = torch.repeat_interleave(torch.arange(n), torch.tensor(sizes)).cuda()
+    x, dy, w = rand(rows, c_in, seed=1, dtype=dt), rand(rows, c_out, seed=2, dtype=dt), rand(n, c_out, c_in, seed=3, dtype=dt)
+    ws = workspace(dc.group_workspace_bytes(rows, n, c_in, c_out, dc.dtype_code(dt)))
+    y, dx, dw = Guarded(torch, (rows, c_out), dt, fill=7.0), Guarded(torch, (rows, c_in), dt, fill=7.0), Guarded(torch, (n, c_out, c_in), dt, fill=7.0)
+    db = Guarded(torch, (n, c_out), torch.float32, fill=7.0)
+    dc.group_forward(x, off, w, None, 0, y.t, ws.t)
+    dc.group_backward(dy, x, off, w, dx.t, dw.t, db.t, ws.t)
+    ad, which = dc.Adapters(w[:40, :8].contiguous(), w[:40, :, :8].contiguous()), torch.arange(n, dtype=torch.int32, device="cuda") % 41 - 1
+    saved, z, aws = ad.saved(rows), Guarded(torch, (rows, c_out), dt, fill=7.0), workspace(dc.adapter_workspace_bytes(rows, c_in, c_out, ad, ad.dtype))
+    dc.adapter_forward(x, w[0].contiguous(), ad, off, which, None, 0, None, saved, z.t, aws.t)
+    torch.cuda.synchronize()
+    for q in (y, dx, dw, db, z, ws, aws):
+        q.check("many runs")
+    assert dc.workspace_status(ws.t) == dc.OK and dc.workspace_status(aws.t) == dc.OK
+    xd, dd, wr = x.double(), dy.double(), w.double()[of]
+    check(y.t, torch.einsum("rk,rok->ro", xd, wr), (c_in + 4) * U * torch.einsum("rk,rok->ro", xd.abs(), wr.abs()), "y")
+    check(dx.t, torch.einsum("ro,rok->rk", dd, wr), (c_out + 4) * U * torch.einsum("ro,rok->rk", dd.abs(), wr.abs()), "dx")
+    each = torch.einsum("ro,rk->rok", dd, xd)
+    sums, room = torch.zeros(n, c_out, c_in, dtype=torch.float64, device="cuda"), torch.zeros(n, c_out, c_in, dtype=torch.float64, device="cuda")
+    check(dw.t, sums.index_add_(0, of, each), (most + 4) * U * room.index_add_(0, of, each.abs()), "dw")
+    sums, room = torch.zeros(n, c_out, dtype=torch.float64, device="cuda"), torch.zeros(n, c_out, dtype=torch.float64, device="cuda")
+    assert bool(((db.t.double() - sums.index_add_(0, of, dd)).abs() <= (most + 4) * U * room.index_add_(0, of, dd.abs())).all())
+    want, slack = torch.zeros(rows, c_out, dtype=torch.float64, device="cuda"), (c_in + 16) * U * (xd.abs() @ w[0].double().abs().t())
+    a, b, mine = ad.a.double(), ad.b.double(), which.long()[of]
+    for i in range(40):
+        r = mine == i
+        t, m = xd[r] @ a[i].t(), xd[r].abs() @ a[i].abs().t()
+        want[r] = t @ b[i].t()
+        slack[r] += ((c_in + 4) * U * m + keeps(dt) * t.abs()) @ b[i].abs().t() + (c_in + 24) * U * (t.abs() @ b[i].abs().t())
+    check(z.t, want + xd @ w[0].double().t(), slack, "z")
+
+
 def test_group_backward_parts_alone():
     """Each gradient without the others, and without what it does not need, gives the same bits."""
     sizes, c_in, c_out = [33, 0, 130], 72, 264

@@ -301,10 +301,13 @@ __device__ __forceinline__ void unpack8(uint4 w, float *v) {
 __device__ __forceinline__ uint4 pack8(const float *v) {
   return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
-// What a row keeps, as terms of bf16 that add up: two (16 bits together), or of fp32 rows three.  Of an infinity or a NaN the first is itself, the others 0.
+// What a row keeps, as terms of bf16 that add up: two (16 bits together), or of fp32 rows three.  Of an infinity or a NaN the first is itself, the others 0; of
+// a number that would round to an infinity the first is the largest bf16.
 template <typename T>
 __device__ __forceinline__ void terms_of(float v, float (&t)[3]) {
+  constexpr float kLargest = 3.38953138925153547e38f;
   t[0] = __bfloat162float(__float2bfloat16(v));
+  if (fabsf(v) > kLargest && fabsf(v) <= 3.402823466e38f) t[0] = copysignf(kLargest, v);
   float left = v - t[0];
   left = left - left == 0.f ? left : 0.f;
   t[1] = __bfloat162float(__float2bfloat16(left));
@@ -1602,11 +1605,11 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   // an adapter's instructions, and the way to the next one, of the runs that a tile has rows of
   const double per_tile = j.t ? 1.0 + 128.0 * j.ext.count / j.rows : 0.0, more = 850.0 * (per_tile < 129.0 ? per_tile : 129.0) * (wide ? 2.0 : 1.0);
   const Shape tile = j.y_terms ? Shape{rank_pad(j.n), false, 1, 0.0} : shape_of(j.n, j.rows, runs, p.pieces, matrices, more, wide, n_sm);
-  // runs of up to 128 rows: 128 columns of a matrix in the place of 128 rows, where that is faster
   if (us) {
     *us = tile.us;
     return cudaSuccess;
   }
+  // runs of up to 128 rows: 128 columns of a matrix in the place of 128 rows, where that is faster
   Shape shape = tile;
   bool by_few = false;
   if (!j.y_terms && !wide && j.rows / runs <= 128) {

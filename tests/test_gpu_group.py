@@ -487,6 +487,32 @@ def test_fp32_results_that_are_no_numbers():
                 assert bool(((got - want)[fine].abs() <= 1e-4 * want[fine].abs() + 1e-3).all())
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows", [1, 20, 400])
+def test_what_rows_keep_up_to_the_largest_number(rows, dtype):
+    """t beyond the largest bf16, where its first term alone would be an infinity: a number still, and so is what is made of it."""
+    dt = TYPES[dtype]
+    of_type(dt)
+    for sign in (1.0, -1.0):
+        x = torch.zeros(rows, 64, dtype=dt, device="cuda")
+        x[:, 0], x[:, 1] = sign * 2.0 ** 127, sign * 127.0 / 128 * 2.0 ** 127
+        x[:, 2] = sign * 0.75 * 2.0 ** 120       # together (2 - 2^-7 + 0.75 2^-7) 2^127: beyond (2 - 2^-7) 2^127, in fp32's range
+        a, b = torch.zeros(1, 4, 64, dtype=dt, device="cuda"), torch.zeros(1, 72, 4, dtype=dt, device="cuda")
+        a[0, 0, :3], b[0, :, 0] = 1.0, 2.0 ** -20
+        ad, off, which = dc.Adapters(a, b), offsets_of([rows]), torch.zeros(1, dtype=torch.int32, device="cuda")
+        y, ws = Guarded(torch, (rows, 72), dt, fill=0), workspace(dc.adapter_workspace_bytes(rows, 64, 72, ad, ad.dtype))
+        saved = ad.saved(rows)
+        dc.adapter_forward(x, None, ad, off, which, None, 0, None, saved, y.t, ws.t)
+        db = torch.empty_like(b)
+        dy = torch.full((rows, 72), 2.0 ** -20 / rows, dtype=dt, device="cuda")
+        dc.adapter_backward(dy, None, None, ad, off, which, saved, None, None, db, ws.t)
+        torch.cuda.synchronize()
+        want, slack, _ = adapter_want(x, None, a, b, None, off, which)
+        check(y.t, want, slack, "y")
+        t = (x.double() @ a[0].double().t())
+        check(db[0], dy.double().t() @ t, (keeps(dt) + (rows + 70) * U) * (dy.double().abs().t() @ t.abs()), "db")
+
+
 def test_offsets_out_of_order_stay_inside():
     """What such offsets give is undefined, but inside the arrays."""
     for dt in TYPES.values():

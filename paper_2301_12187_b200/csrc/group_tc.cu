@@ -20,10 +20,11 @@
 // sum is read out and added up in fp32 registers.  A result that is a NaN is worked out again by FMAs: an infinity, or a value
 // beyond the largest bf16, has a NaN among its terms.
 //
-// What bounds it: many rows, the tensor core under the power cap (8192 rows, 4096 -> 4096 in one group 184 us, 1.49 PFLOP/s; 16384 ragged rows of 16 groups 486
-// us, 1.13); few rows, the weights' bytes (256 rows of 64 groups, 2048 -> 2048, 82 to 85 us, 6.4 TB/s); fp32, what an SM takes in, 45 bytes a cycle (a
-// piece of 128 x 128, 96 KB, 1.2 us, its products 0.4); single rows, a chain of launch, offsets, loads and a cluster's meeting (4 rows of
-// 8 groups, 1024 -> 1024, 6.7 us).
+// What bounds it: many rows, the tensor core under the power cap (8192 rows, 4096 -> 4096 in one group 184 us, 1.49 PFLOP/s; 16384 ragged rows of 16
+// groups 401 us a launch by itself, 486 one behind the other); few rows, the weights' bytes (256 rows of 64 groups, 2048 -> 2048, 82 to 85 us, 6.4 TB/s); fp32,
+// its six products and what an SM takes in, 45 bytes a cycle (a piece of 128 x 128: 0.8 us of products, 96 KB, 1.2 in all; in pairs of 256 x 256, for half the
+// bytes, 2048 x 2048 x 2048 took 96 us for 98, but 16 groups of 256 rows, 512 -> 512, 40 for 26); single rows, a chain of launch, offsets, loads and a
+// cluster's meeting (4 rows of 8 groups, 1024 -> 1024, 6.7 us).
 #include <math.h>
 #include <string.h>
 
@@ -1443,6 +1444,7 @@ cudaError_t launch(Params &p, long long items, int n_sm, const CUtensorMap (&m)[
   static unsigned char attr_done[kDcMaxDevices];
   const cudaError_t e = dc_set_max_smem_once(k_group_tc<FORM, ACROSS, T, P>, kSmem, attr_done);
   if (e != cudaSuccess) return e;
+  if (p.tmem_cols > 512 || p.stages < 1) return cudaErrorNotSupported;        // no such form: a rule above would be wrong
   const int group = P ? 2 : p.split;
   const long long teams = items < n_sm / group ? items : n_sm / group;
   p.most = FORM == kGrad ? items : group > 1 && !P ? teams : 1ll << 62;

@@ -65,6 +65,18 @@ bool direct(const RowsJob &j) {
   const double numbers = j.w ? (double)j.rows * j.k + (double)j.runs.weights * j.n * j.k : 0.0;
   return rows_few_us(j) < us + 3.0 + 3.0 + numbers * 10 / 4.5e6;
 }
+// A grouped product's sizes: forward, or of the rows' gradients.
+RowsJob group_job(long long rows, int c_in, int c_out, const int *offsets, int groups, const void *w, bool backward, dc_dtype dtype) {
+  RowsJob j = {};
+  j.rows = (int)rows;
+  j.k = backward ? c_out : c_in;
+  j.n = backward ? c_in : c_out;
+  j.w = j.raw_w = w;
+  j.w_across = backward;
+  j.runs = {offsets, nullptr, groups, (int)rows, groups, 0};
+  j.dtype = dtype;
+  return j;
+}
 
 }  // namespace
 
@@ -93,21 +105,13 @@ extern "C" dc_status dc_group_forward(const void *x, long long rows, int c_in, c
   if (!aligned({x, w, bias, y, workspace}) || (reinterpret_cast<uintptr_t>(offsets) & 3u)) return DC_ERR_ALIGNMENT;
   if (rows == 0) return DC_OK;
   Parts parts(workspace, dtype);
-  RowsJob j = {};
-  j.x = x;
-  j.rows = (int)rows;
-  j.k = c_in;
-  j.n = c_out;
-  j.w = w;
+  RowsJob j = group_job(rows, c_in, c_out, offsets, groups, w, false, dtype);
+  j.x = j.raw_x = x;
   j.x_pitch = j.w_pitch = parts.pitch(c_in);
-  j.raw_x = x;
-  j.raw_w = w;
-  j.runs = {offsets, nullptr, groups, (int)rows, groups, 0};
   j.bias = bias;
   j.bias_each = 1;
   j.act = (int)act;
   j.y = y;
-  j.dtype = dtype;
   if (direct(j)) return status(rows_few(j, (cudaStream_t)stream));
   j.x = parts.rows_of(x, rows, c_in);
   j.w = parts.rows_of(w, (long long)groups * c_out, c_in);
@@ -128,18 +132,11 @@ extern "C" dc_status dc_group_backward(const void *dy, const void *x, long long 
   if (rows == 0 && !dw && !db) return DC_OK;
   const Runs runs = {offsets, nullptr, groups, (int)rows, groups, 0};
   Parts parts(workspace, dtype);
-  RowsJob j = {};
+  RowsJob j = group_job(rows, c_in, c_out, offsets, groups, w, true, dtype);
   j.x = j.raw_x = dy;
-  j.rows = (int)rows;
-  j.k = c_out;
-  j.n = c_in;
-  j.w = j.raw_w = w;
-  j.w_across = 1;
   j.x_pitch = parts.pitch(c_out);
   j.w_pitch = parts.pitch(c_in);
-  j.runs = runs;
   j.y = dx;
-  j.dtype = dtype;
   const bool with_dx = dx && rows, fmas = with_dx && direct(j);
   const void *dy_at = dw || db || !fmas ? parts.rows_of(dy, rows, c_out) : nullptr, *x_at = dw ? parts.rows_of(x, rows, c_in) : nullptr;
   j.x = dy_at;

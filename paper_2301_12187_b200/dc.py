@@ -792,7 +792,11 @@ class Adapters:
         self.count, self.rank, self.c_in = (int(v) for v in a.shape)
         self.c_out = int(b.shape[1])
         self.dtype = dtype_code(a.dtype)
-        self.c = AdapterSet(self.count, self.rank, _ptr(a), _ptr(b), _ptr(scale))
+
+    @property
+    def c(self) -> AdapterSet:
+        """Of the tensors as they are now: they may have moved since."""
+        return AdapterSet(self.count, self.rank, _ptr(self.a), _ptr(self.b), _ptr(self.scale))
 
     def saved(self, rows: int):
         """A buffer in which adapter_forward leaves for adapter_backward what its gradients need."""

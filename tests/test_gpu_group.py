@@ -703,6 +703,28 @@ def test_arrays_beyond_32_bits():
         del dw
 
 
+def test_fp32_matrices_beyond_32_bits():
+    """Read as they lie."""
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("not enough memory")
+    dt, groups, n, c = torch.float32, 260, 3, 4096
+    of_type(dt)
+    w = torch.zeros(groups, c, c, device="cuda")
+    w[-1] = rand(c, c, seed=3, dtype=dt, scale=c ** -0.5)
+    x, dy = rand(n, c, seed=4, dtype=dt), rand(n, c, seed=5, dtype=dt)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    off = torch.zeros(groups + 1, dtype=torch.int32, device="cuda")
+    off[-1] = n
+    assert dc.group_plan(n, groups, c, c, 0, dc.F32, dc.GROUP_FORWARD).form == dc.GROUP_FMAS
+    ws = torch.empty(dc.group_workspace_bytes(n, groups, c, c, dc.F32), dtype=torch.uint8, device="cuda")
+    ws[:256] = 0
+    dc.group_forward(x, off, w, None, 0, y, ws)
+    dc.group_backward(dy, None, off, w, dx, None, None, ws)
+    wd = w[-1].double()
+    check(y, x.double() @ wd.t(), (c + 4) * U * (x.double().abs() @ wd.abs().t()), "y")
+    check(dx, dy.double() @ wd, (c + 4) * U * (dy.double().abs() @ wd.abs()), "dx")
+
+
 def test_tensors_of_the_host_are_refused():
     step = Step(5)
     with pytest.raises(ValueError):

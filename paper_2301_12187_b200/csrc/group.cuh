@@ -94,6 +94,39 @@ __device__ __forceinline__ int first_run_behind(const Runs &r, int row) {
   return lo;
 }
 
+// For the runs with an adapter that have rows in [row0, end), all lanes together: each lane looks at its own run, `mine(run)`, then f(lane) for each of
+// those that count.
+template <typename G, typename F>
+__device__ __forceinline__ void each_run(const Runs &r, int row0, int end, G mine, F f) {
+  const int lane = (int)(threadIdx.x & 31u);
+  // the first run that ends behind row0: 32 probes at a time
+  int lo = 0, n = r.count;
+  while (n > 32) {
+    const int step = (n + 31) >> 5, probe = min((lane + 1) * step, n);
+    const unsigned past = __ballot_sync(0xffffffffu, __ldg(r.offsets + lo + probe) > row0);
+    if (!past) return;
+    const int at = __ffs(past) - 1;
+    lo += at * step;
+    n = min(step, n - at * step);
+  }
+  for (int base = lo; base < r.count; base += 32) {
+    Run o = {0, 0, -1};
+    bool stop = base + lane >= r.count;
+    if (!stop) {
+      o = run_at(r, base + lane);
+      stop = o.begin >= end;
+    }
+    const bool counts = !stop && o.weight >= 0 && o.end > row0 && o.end > o.begin;
+    if (counts) mine(o);
+    unsigned here = __ballot_sync(0xffffffffu, counts);
+    while (here) {
+      const int at = __ffs(here) - 1;
+      here &= here - 1;
+      f(at);
+    }
+    if (__any_sync(0xffffffffu, stop)) return;
+  }
+}
 // What a row keeps of an adapter: `rank` numbers, padded with zeros to a multiple of 16, as terms of bf16 that add up to them: all high ones, then all
 // low ones.  bf16 rows: two, 16 bits together (with one bf16 the adapter's part of a result would be as far off as the result's own rounding, 2^-9,
 // and so would its gradients); fp32 rows: three.

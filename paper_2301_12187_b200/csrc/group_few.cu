@@ -19,9 +19,18 @@ using grp::RowsJob;
 
 constexpr int kCols = 32, kStages = 3;
 
-__device__ __forceinline__ float kept(const __nv_bfloat16 *t, int row, int pad, int j) {
+// eight neighbours of what a row keeps
+__device__ __forceinline__ void kept8(const __nv_bfloat16 *t, int row, int pad, int j, float *to) {
   const __nv_bfloat16 *at = t + (size_t)row * (size_t)(3 * pad) + (size_t)j;
-  return __bfloat162float(at[0]) + (__bfloat162float(at[pad]) + __bfloat162float(at[2 * pad]));
+  uint4 w[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) w[k] = *reinterpret_cast<const uint4 *>(at + k * pad);
+  const uint32_t u[3][4] = {{w[0].x, w[0].y, w[0].z, w[0].w}, {w[1].x, w[1].y, w[1].z, w[1].w}, {w[2].x, w[2].y, w[2].z, w[2].w}};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    to[2 * i] = __uint_as_float(u[0][i] << 16) + (__uint_as_float(u[1][i] << 16) + __uint_as_float(u[2][i] << 16));
+    to[2 * i + 1] = __uint_as_float(u[0][i] & 0xffff0000u) + (__uint_as_float(u[1][i] & 0xffff0000u) + __uint_as_float(u[2][i] & 0xffff0000u));
+  }
 }
 // four values: neighbours from 4 * i on (VEC), or every STRIDE-th from i on; zeros from `end` on
 template <bool VEC, int STRIDE>
@@ -55,27 +64,27 @@ __device__ __forceinline__ void halve(float *v, int lane, int &first) {
   }
 }
 
-// An adapter's part of one value along the adapters' rows, 32 of the rank at a time.  (As further numbers of the sum, by the lanes that share it, most of
-// which a low rank leaves without any: 379 rows of rank 6, 152 -> 600, 23 us for 17.)
-__device__ __forceinline__ float of_adapter(const RowsJob &j, int a, const float *t, int o) {
-  if (a < 0) return 0.f;                         // t may be no number there
-  const float *e = reinterpret_cast<const float *>(j.raw_e) + ((size_t)a * (size_t)j.n + (size_t)o) * (size_t)j.rank;
-  float sum = 0.f;
+// An adapter's part of a row's 32 columns, along the adapter's rows: a lane to a number of the rank, so that loads are neighbours, and the 32 columns' sums over
+// the lanes by halving.  Each lane is left with column `first`.  (A column to a lane: 111 rows of rank 64, 224 -> 3279, 48 us for 39.)
+__device__ __forceinline__ float of_adapter(const RowsJob &j, int a, const float *t, int o0, int cols, int lane, int &first) {
+  const float *e = reinterpret_cast<const float *>(j.raw_e) + ((size_t)a * (size_t)j.n + (size_t)o0) * (size_t)j.rank;
+  float v[kCols];
+#pragma unroll
+  for (int c = 0; c < kCols; ++c) v[c] = 0.f;
 #pragma unroll 1
-  for (int q = 0; q < j.rank; q += 32) {
-    float v[32];
-    if (j.rank % 4 == 0) {
+  for (int q = lane; q - lane < j.rank; q += 32) {
+    const bool is = q < j.rank;
+    const float f = is ? t[q] : 0.f;
+    const float *at = e + min(q, j.rank - 1);
+    float w[kCols];
 #pragma unroll
-      for (int i = 0; i < 32; i += 4) load4<true, 0>(e + q + i, 0, j.rank - q - i, *reinterpret_cast<float (*)[4]>(v + i));
-    } else {
+    for (int c = 0; c < kCols; ++c) w[c] = __ldg(at + min(c, cols - 1) * j.rank);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = q + i < j.rank ? __ldg(e + q + i) : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (q + i < j.rank) sum = fmaf(t[q + i], v[i], sum);
+    for (int c = 0; c < kCols; ++c) v[c] = fmaf(f, is ? w[c] : 0.f, v[c]);
   }
-  return sum;
+  first = 0;
+  halve<kCols, 16, 1>(v, lane, first);
+  return v[0];
 }
 
 __device__ __forceinline__ void deliver(const RowsJob &j, int row, int weight, int o, float v) {
@@ -198,6 +207,15 @@ __device__ __forceinline__ void tile(const RowsJob &j, float *xs, float *parts, 
     for (int i = 0; i < R / 4; ++i) parts[((warp >> 2) * R + (first + i) / 8) * kCols + own + (first + i) % 8] = sums[i];
   }
   __syncthreads();
+  if (!ACROSS && j.t) {
+#pragma unroll 1
+    for (int r = warp; r < rows; r += kWarps) {
+      if (adapter[r] < 0) continue;              // t may be no number there
+      const float sum = of_adapter(j, adapter[r], ts + r * grp::rank_pad(j.rank), o0, cols, lane, first);
+      parts[r * kCols + first] += sum;
+    }
+    __syncthreads();
+  }
 #pragma unroll 1
   for (int i = tid; i < rows * kCols; i += kThreads) {
     const int r = i / kCols, o = i - r * kCols;
@@ -209,7 +227,6 @@ __device__ __forceinline__ void tile(const RowsJob &j, float *xs, float *parts, 
       v += parts[R * kCols + i];
     }
     if (o >= cols) continue;
-    if (!ACROSS && j.t) v += of_adapter(j, adapter[r], ts + r * grp::rank_pad(j.rank), o0 + o);
     deliver(j, row0 + r, weight, o0 + o, v);
   }
 }
@@ -243,18 +260,14 @@ __global__ void __launch_bounds__(128 * H, (R == 4 ? 4 : 2) / H) k_group_few_f32
     const int row0 = found[1], rows = min(R, found[2] - row0), weight = found[3];
     if (j.t) {
       const int pad = grp::rank_pad(j.rank);
-      if ((int)threadIdx.x < R) {
-        int a = -1;
-        const int row = row0 + (int)threadIdx.x;
-        if ((int)threadIdx.x < rows)
-          for (int s = grp::first_run_behind(j.ext, row); s < j.ext.count; ++s) {
-            const Run run = grp::run_at(j.ext, s);
-            if (run.begin > row) break;
-            if (run.end > row) { a = run.weight; break; }
-          }
-        adapter[threadIdx.x] = a;
+      if (threadIdx.x < 32) {
+        if ((int)threadIdx.x < R) adapter[threadIdx.x] = -1;
+        __syncwarp();
+        grp::each_run(j.ext, row0, row0 + rows, [&](const Run &run) {
+          for (int i = max(run.begin - row0, 0); i < min(run.end - row0, rows); ++i) adapter[i] = run.weight;
+        }, [](int) {});
       }
-      for (int i = (int)threadIdx.x; i < rows * pad; i += kThreads) ts[i] = kept(reinterpret_cast<const __nv_bfloat16 *>(j.t), row0 + i / pad, pad, i % pad);
+      for (int i = (int)threadIdx.x * 8; i < rows * pad; i += kThreads * 8) kept8(reinterpret_cast<const __nv_bfloat16 *>(j.t), row0 + i / pad, pad, i % pad, ts + i);
       __syncthreads();
     }
     tile<R, H, ACROSS, VEC>(j, xs, parts, ts, adapter, row0, rows, weight, (int)blockIdx.x * kCols);
@@ -270,7 +283,8 @@ cudaError_t launch(const RowsJob &j, dim3 grid, int most, cudaStream_t st) {
 }
 template <int R>
 cudaError_t launch(const RowsJob &j, dim3 grid, int most, int sets, bool across, bool vec, cudaStream_t st) {
-  if (!vec) return across ? launch<R, 1, true, false>(j, grid, most, st) : launch<R, 1, false, false>(j, grid, most, st);
+  if (!vec && across) return launch<R, 1, true, false>(j, grid, most, st);
+  if (!vec) return sets == 2 ? launch<R, 2, false, false>(j, grid, most, st) : launch<R, 1, false, false>(j, grid, most, st);
   if (across) return sets == 2 ? launch<R, 2, true, true>(j, grid, most, st) : launch<R, 1, true, true>(j, grid, most, st);
   return sets == 2 ? launch<R, 2, false, true>(j, grid, most, st) : launch<R, 1, false, true>(j, grid, most, st);
 }
@@ -298,7 +312,12 @@ double rows_few_us(const RowsJob &j) {
   return 4.0 + (j.t ? 2.5 : 0.0) + fmax(fma, fmax(memory, steps));
 }
 
-int rows_few_sets(const RowsJob &j) { return vec_of(j) && (long long)dc_div_up(j.n, kCols) * most_tiles(j) < 2 * dc_sm_count() ? 2 : 1; }
+// Two where there are fewer CTAs than two to an SM; of rows that begin anywhere, fewer than one (2 x 55: 32 us with one set, 25 with two; 35 x 5: 16 and 22),
+// and across them never (2 x 84: 11 and 16).
+int rows_few_sets(const RowsJob &j) {
+  const long long tiles = (long long)dc_div_up(j.n, kCols) * most_tiles(j);
+  return tiles < (vec_of(j) ? 2 : across_of(j) ? 0 : 1) * dc_sm_count() ? 2 : 1;
+}
 
 cudaError_t rows_few(const RowsJob &j, cudaStream_t st) {
   const int rows = rows_few_tile(j), most = most_tiles(j), sets = rows_few_sets(j);

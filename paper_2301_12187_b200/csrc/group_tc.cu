@@ -185,39 +185,6 @@ __device__ __forceinline__ bool find_tile(const Params &p, int tile, grp::Walk &
   return true;
 }
 
-// For the runs with an adapter that have rows in [row0, end), all lanes together: each lane looks at its own run, `mine(run)`, then f(lane) for each of
-// those that count.
-template <typename G, typename F>
-__device__ __forceinline__ void each_run(const Runs &r, int row0, int end, G mine, F f) {
-  const int lane = (int)(threadIdx.x & 31u);
-  // the first run that ends behind row0: 32 probes at a time
-  int lo = 0, n = r.count;
-  while (n > 32) {
-    const int step = (n + 31) >> 5, probe = min((lane + 1) * step, n);
-    const unsigned past = __ballot_sync(0xffffffffu, __ldg(r.offsets + lo + probe) > row0);
-    if (!past) return;
-    const int at = __ffs(past) - 1;
-    lo += at * step;
-    n = min(step, n - at * step);
-  }
-  for (int base = lo; base < r.count; base += 32) {
-    Run o = {0, 0, -1};
-    bool stop = base + lane >= r.count;
-    if (!stop) {
-      o = grp::run_at(r, base + lane);
-      stop = o.begin >= end;
-    }
-    const bool counts = !stop && o.weight >= 0 && o.end > row0 && o.end > o.begin;
-    if (counts) mine(o);
-    unsigned here = __ballot_sync(0xffffffffu, counts);
-    while (here) {
-      const int at = __ffs(here) - 1;
-      here &= here - 1;
-      f(at);
-    }
-    if (__any_sync(0xffffffffu, stop)) return;
-  }
-}
 // the adapter of a row, -1: none.  One thread.
 __device__ __forceinline__ int adapter_of(const Runs &r, int row) {
   for (int s = grp::first_run_behind(r, row); s < r.count; ++s) {        // empty runs in between
@@ -585,7 +552,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         if (adapters && p.early && item == team) asm volatile("griddepcontrol.wait;" ::: "memory");
         int run_weight = 0;
         if (adapters)
-          each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](const Run &run) { run_weight = run.weight; }, [&](int from) {
+          grp::each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](const Run &run) { run_weight = run.weight; }, [&](int from) {
             const int weight = __shfl_sync(0xffffffffu, run_weight, from);
             for (int c = 0; c < ext_uses; ++c, next()) {
               if (!lead || !ok) continue;
@@ -720,7 +687,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         __syncwarp();
         uint32_t run_off[8];
         if (adapters)
-          each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](const Run &run) {
+          grp::each_run(p.ext, t.row0, min(t.end, t.row0 + kRows), [&](const Run &run) {
 #pragma unroll
             for (int i = 0; i < 2 * kRows / 64; ++i) {
               const int lo = max(run.begin - t.row0 - 32 * i, 0), hi = min(run.end - t.row0 - 32 * i, 32);
@@ -1148,7 +1115,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         bar_sync(1, kEpi * 32 + 32);
         for (int i = lane; i < p.nt; i += 32) weight_s[i] = -1;
         __syncwarp();
-        each_run(p.ext, t.row0, t.row0 + count, [&](const Run &run) {
+        grp::each_run(p.ext, t.row0, t.row0 + count, [&](const Run &run) {
           for (int i = max(run.begin - t.row0, 0); i < min(run.end - t.row0, count); ++i) weight_s[i] = run.weight;
         }, [](int) {});
         __syncwarp();
@@ -1169,14 +1136,10 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
           if (!ok) continue;
           const uint32_t to = ring + (uint32_t)(slot * p.slot_rows * p.row_bytes);
           const bf16 *e = reinterpret_cast<const bf16 *>(p.e);
-          if (ACROSS) {                        // `rank` rows of the tile's columns
-            const uint32_t bytes = (uint32_t)min(128, p.e_pitch - o0) * 2u;
-            if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)(p.rank * rows));
+          if (ACROSS) {                        // `rank` rows of the tile's columns (row by row, 14 rows' adapters of rank 64, 192 -> 2224, took 41 us for 16)
+            if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], (uint32_t)(p.row_bytes * rows));
             __syncwarp();
-            for (int i = 0; i < rows; ++i) {
-              const bf16 *from = e + (size_t)weight_s[list_s[i0 + i]] * (size_t)p.rank * (size_t)p.e_pitch + (size_t)o0;
-              for (int j = lane; j < p.rank; j += 32) bulk_load(to + (uint32_t)(i * p.row_bytes + j * 256), from + (size_t)j * (size_t)p.e_pitch, bytes, &bar[kEFull + slot]);
-            }
+            if (lane < rows) load_box<false>(to + (uint32_t)(lane * p.row_bytes), &map_e, smem_u32(&bar[kEFull + slot]), o0, 0, 0, weight_s[list_s[i0 + lane]]);
           } else {                             // the columns' rows, one piece
             const uint32_t bytes = (uint32_t)(min(128, p.n - o0) * p.e_pitch) * 2u;
             if (lane == 0) mbar_arrive_expect_tx(&bar[kEFull + slot], bytes * (uint32_t)rows);
@@ -1436,7 +1399,7 @@ bool map_of(CUtensorMap *map, const void *at, long long cols, int terms, long lo
   const cuuint64_t dim[4] = {(cuuint64_t)cols, (cuuint64_t)terms, (cuuint64_t)rows, (cuuint64_t)outer}, str[3] = {one, one * (cuuint64_t)terms, one * (cuuint64_t)terms * (cuuint64_t)rows};
   const cuuint32_t bx[4] = {(cuuint32_t)wide, 1, (cuuint32_t)box, 1}, es[4] = {1, 1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(at), dim, str, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                wide == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : wide == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                wide == 128 ? CU_TENSOR_MAP_SWIZZLE_NONE : wide == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : wide == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int FORM, bool ACROSS, typename T, bool P>
@@ -1651,13 +1614,14 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
     return cudaSuccess;
   }
   CUtensorMap m[4] = {};
-  p.maps = (j.w ? 3 : 0) | (j.t && !by_few ? 12 : 0);
+  p.maps = (j.w ? 3 : 0) | (j.t && !by_few ? 12 : 0) | (j.t && by_few && j.e_across ? 8 : 0);
   const int box = pair ? p.nt / 2 : p.nt;
   if (j.w) {
     if (!map_of(&m[0], j.x, j.k, terms, j.rows, 1, j.x_pitch, by_few ? p.nt : 128)) return cudaErrorNotSupported;
     if (!(j.w_across ? map_of(&m[1], j.w, j.n, terms, j.k, j.runs.weights, j.w_pitch, 64) : map_of(&m[1], j.w, j.k, terms, j.n, j.runs.weights, j.w_pitch, by_few ? 128 : box)))
       return cudaErrorNotSupported;
   }
+  if (j.t && by_few && j.e_across && !map_of(&m[3], j.e, j.n, 1, j.rank, j.ext.weights, j.e_pitch, j.rank, 128)) return cudaErrorNotSupported;
   if (j.t && !by_few) {
     // Rows no wider than the rank: what lies outside a box costs a load as much as what is there (16 numbers a row in boxes of 64: 1100 cycles a run).
     const int pad = rank_pad(j.rank), row = pad <= 16 ? 16 : pad <= 32 ? 32 : 64;

@@ -6,15 +6,17 @@ import random
 # rows, groups, c_in, c_out
 GROUP_FORMS = [(3, 1, 16, 16), (2, 1, 73, 67), (681, 1, 16, 24), (4, 1, 16, 472), (9, 1, 544, 17), (164, 10, 2264, 16), (2, 1, 16, 33),
                (8, 1, 23, 22), (2, 1, 37, 20), (17, 1, 19, 24), (8, 2, 24, 18), (38, 3, 17, 18), (12, 2, 26, 24), (132, 10, 16, 2064),
-               (266, 30, 1768, 16), (486, 1, 16, 802), (218, 64, 88, 72), (2412, 2, 67, 1633), (53, 6, 16, 840), (2942, 31, 232, 224),
-               (26, 11, 16, 675), (150, 32, 20, 175), (1267, 1, 2853, 139), (2231, 42, 16, 136), (2281, 20, 149, 18), (481, 12, 16, 1808),
-               (690, 13, 1520, 16), (138, 1, 2168, 1760), (2322, 55, 339, 419)]
+               (266, 30, 1768, 16), (136, 1, 29, 597), (218, 64, 88, 72), (1042, 24, 16, 1446), (156, 40, 27, 33), (2122, 17, 18, 20),
+               (70, 22, 19, 100), (101, 18, 18, 132), (370, 62, 18, 46), (1998, 2, 1448, 80), (53, 6, 16, 840), (2942, 31, 232, 224),
+               (26, 11, 16, 675), (150, 32, 20, 175), (2047, 2, 144, 1712), (2231, 42, 16, 136), (2281, 20, 149, 18), (229, 2, 1195, 1602),
+               (2026, 2, 1913, 133)]
 # rows, requests, rank, c_in, c_out
 ADAPTER_FORMS = [(2, 2, 2, 24, 16), (750, 1, 8, 16, 16), (1, 1, 16, 834, 913), (138, 2, 27, 585, 17), (1, 1, 1, 20, 115), (4, 1, 8, 24, 16),
                  (4, 1, 8, 19, 32), (7, 1, 8, 27, 22), (1, 1, 16, 22, 16), (14, 2, 8, 25, 32), (45, 1, 32, 16, 21), (6, 4, 9, 56, 22),
-                 (179, 2, 8, 16, 1312), (3122, 1, 128, 16, 16), (143, 1, 8, 1296, 16), (7019, 2, 32, 212, 26), (7932, 3, 16, 16, 144),
-                 (49, 1, 32, 2680, 1536), (18, 2, 32, 975, 2169), (104, 11, 16, 3656, 24), (138, 1, 32, 1040, 1512), (7165, 5, 16, 400, 16),
-                 (5485, 5, 8, 16, 536), (127, 127, 8, 16, 3080), (3162, 3, 64, 1184, 136), (3158, 2, 64, 136, 1256)]
+                 (179, 2, 8, 16, 1312), (3122, 1, 128, 16, 16), (143, 1, 8, 1296, 16), (3485, 3, 16, 415, 18), (1181, 7, 8, 17, 68),
+                 (7932, 3, 16, 16, 144), (3862, 7, 16, 16, 39), (49, 1, 32, 2680, 1536), (18, 2, 32, 975, 2169), (104, 11, 16, 3656, 24),
+                 (138, 1, 32, 1040, 1512), (7165, 5, 16, 400, 16), (5485, 5, 8, 16, 536), (127, 127, 8, 16, 3080), (3162, 3, 64, 1184, 136),
+                 (3158, 2, 64, 136, 1256)]
 
 
 def spread(rows, runs, seed):

@@ -1424,7 +1424,10 @@ cudaError_t launch_any(Params &p, bool wide, bool pair, long long items, int n_s
 
 // Shared and tensor memory; `apart`: bytes beside the ring and the staged results
 void lay_out(Params *p, int terms, int apart) {
-  p->acc = (int)dc_round_up((size_t)p->nt, 32);
+  // An accumulator is read 32 columns at a time, and of a bf16 gradient with terms each half so, from its own first column on: what is read
+  // belongs to it, beyond its last column too (rank 16: 16 + 16 columns, of which 16 to 47 are the second read).
+  const int half = p->q_terms && terms == 1 ? p->nt / 2 : 0;
+  p->acc = (int)dc_round_up((size_t)(half ? half + (int)dc_round_up((size_t)half, 32) : p->nt), 32);
   p->tmem_cols = 32;
   while (p->tmem_cols < (terms == 3 ? kAccs<float> : kAccs<bf16>) * p->acc) p->tmem_cols *= 2;
   const int stage = terms * (kP + p->q_bytes);

@@ -1,0 +1,47 @@
+"""Grouped products and adapters on the GPU: gradients of which a CTA makes several tiles, one behind the other.  Tolerances as in test_gpu_group.py."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2301_12187_b200 import dc
+from tests.group_sizes import spread
+from tests.parity_util import Guarded
+from tests.test_gpu_group import TYPES, U, adapter_want, check, of_type, offsets_of, rand, workspace
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rank", [1, 8, 16, 17, 48, 80, 112, 128])
+def test_more_tiles_of_gradients_than_ctas(rank, dtype):
+    """64 adapters, of which a third have no rows, beside 1024 -> 1160: 512 and 640 tiles of gradients, more than three to an SM, of runs that end inside pieces."""
+    dt, n, c_in, c_out, rows = TYPES[dtype], 64, 1024, 1160, 700
+    of_type(dt)
+    sizes = spread(rows, 90, rank)
+    off = offsets_of(sizes)
+    which = torch.tensor([(i * 7) % n if (i * 7) % 3 else -1 for i in range(len(sizes))], dtype=torch.int32, device="cuda")
+    x, dy = rand(rows, c_in, seed=1, dtype=dt), rand(rows, c_out, seed=2, dtype=dt)
+    a, b = rand(n, rank, c_in, seed=3, dtype=dt, scale=c_in ** -0.5), rand(n, c_out, rank, seed=4, dtype=dt, scale=rank ** -0.5)
+    scale = 0.25 + rand(n, seed=5, dtype=torch.float32).abs()
+    ad = dc.Adapters(a, b, scale)
+    ws, saved = workspace(dc.adapter_workspace_bytes(rows, c_in, c_out, ad, ad.dtype)), Guarded(torch, (ad.saved(rows).numel(),), torch.uint8, fill=0xFF)
+    dc.adapter_forward(x, None, ad, off, which, None, 0, None, saved.t, torch.empty_like(dy), ws.t)
+    da, db = Guarded(torch, tuple(a.shape), dt, fill=float("nan")), Guarded(torch, tuple(b.shape), dt, fill=float("nan"))
+    dc.adapter_backward(dy, x, None, ad, off, which, saved.t, None, da.t, db.t, ws.t)
+    torch.cuda.synchronize()
+    for g in (da, db, ws, saved):
+        g.check("gradients")
+    assert dc.workspace_status(ws.t) == dc.OK
+    _, _, ahead = adapter_want(x, None, a, b, scale, off, which)
+    _, _, back = adapter_want(dy, None, b.transpose(1, 2).contiguous(), a.transpose(1, 2).contiguous(), scale, off, which)
+    zeros = [torch.zeros(t.shape, dtype=torch.float64, device="cuda") for t in (a, a, b, b)]
+    da_want, da_slack, db_want, db_slack = zeros
+    for (lo, hi, i, t, off_t), (_, _, _, u, off_u) in zip(ahead, back):
+        xs, ds = x[lo:hi].double(), dy[lo:hi].double()
+        da_want[i] += u.t() @ xs
+        da_slack[i] += off_u.t() @ xs.abs() + (rows + 8) * U * (u.abs().t() @ xs.abs())
+        db_want[i] += ds.t() @ t
+        db_slack[i] += ds.abs().t() @ off_t + (rows + 8) * U * (ds.abs().t() @ t.abs())
+    check(da.t, da_want, da_slack, "da")
+    check(db.t, db_want, db_slack, "db")
+    without = sorted(set(range(n)) - {i for _, _, i, _, _ in ahead})
+    assert len(without) >= n // 3 and not bool(da.t[without].any()) and not bool(db.t[without].any())

@@ -48,7 +48,8 @@ constexpr int kBox = 64 * 128;                   // 64 columns of 64 rows
 constexpr int kOut = kEpi * 32 * 128;            // staged results: 32 rows x 32 sums a warp
 constexpr int kSuper = 16;                       // rows of tiles that are walked together: 16 x 9 tiles at once read a twelfth of what a row or column of them would
 constexpr int kFewMost = 64, kFewWide = 32;     // rows of a tile of kFew; of adapters of a high rank, which then have as many slots
-constexpr unsigned long long kLongNs = 20ull * 1000ull * 1000ull * 1000ull;      // a gradient's tile may take seconds (a sum over 2^30 rows), and so may NaN by FMAs
+// A gradient's tile may take seconds (2^30 rows are 17 million pieces), and so may results that are worked out again by FMAs: 0.8 s a million rows of one weight.
+constexpr unsigned long long kLongNs = 20ull * 1000ull * 1000ull * 1000ull;
 
 typedef __nv_bfloat16 bf16;
 template <typename T>
@@ -298,37 +299,129 @@ __device__ __forceinline__ bool any_nan(const float (&v)[32]) {
   for (int i = 0; i < 32; ++i) nan |= !(v[i] == v[i]);
   return nan;
 }
-// A result that came out as a NaN, by FMAs.  It stays one as soon as it is one.
-template <bool ACROSS>
-static __device__ __noinline__ float again(const Params &p, int row, int weight, int o) {
-  float s = 0.f;
-  if (p.pieces) {
-    const float *x = reinterpret_cast<const float *>(p.raw_p) + (size_t)row * (size_t)p.k;
-    const float *w = reinterpret_cast<const float *>(p.raw_q) + (size_t)weight * (size_t)p.n * (size_t)p.k + (ACROSS ? (size_t)o : (size_t)o * (size_t)p.k);
-    for (int i = 0; i < p.k && s == s; ++i) s = fmaf(x[i], w[(size_t)i * (size_t)(ACROSS ? p.n : 1)], s);
-    if (p.alpha) s *= __ldg(p.alpha + weight);
-  }
-  if (p.rank) {
-    const int a = adapter_of(p.ext, row);
-    if (a >= 0) {
-      const float *e = reinterpret_cast<const float *>(p.e) + (size_t)a * (size_t)p.n * (size_t)p.rank + (ACROSS ? (size_t)o : (size_t)o * (size_t)p.rank);
-      for (int j = 0; j < p.rank && s == s; ++j) s = fmaf(kept<float>(p.t, row, grp::rank_pad(p.rank), j), e[(size_t)j * (size_t)(ACROSS ? p.n : 1)], s);
+// Results that came out as NaN, by FMAs: a warp together, 32 rows, one to a lane, x 8 columns at a time, results of a lane as it put them to its 128 bytes of shared
+// memory (in registers they, and more columns at a time, would cost what the usual way needs).  A term's 8 numbers that all lanes multiply by are asked for by 8 lanes, 4
+// terms to a load.  It ends as soon as all that is wanted is a NaN.  65536 rows with an infinity, gradients of 128 x 128: 55 ms (each element by its own lane 880 to
+// 1120, which of two million rows is more than waits allow); 512 rows, 4096 -> 1024, one of them with an infinity: 2.2 ms (9.8).
+constexpr int kAgain = 8;                        // columns, and terms, at once
+struct Again {
+  uint32_t wanted;
+  float s[kAgain];
+  __device__ __forceinline__ bool start(uint32_t at, bool valid, int count) {
+    wanted = 0;
+#pragma unroll
+    for (int x = 0; x < kAgain; ++x) {
+      const float v = lds_f(at + (uint32_t)(x * 4));
+      if (valid && x < count && !(v == v)) wanted |= 1u << x;
+      s[x] = 0.f;
     }
+    return __any_sync(0xffffffffu, wanted != 0) != 0;
   }
-  return s;
+  __device__ __forceinline__ bool open() const {
+    bool is = false;
+#pragma unroll
+    for (int x = 0; x < kAgain; ++x) is |= (wanted >> x & 1u) && s[x] == s[x];
+    return __any_sync(0xffffffffu, is) != 0;
+  }
+  // a: this lane's row, kAgain terms; b: terms lane / 8 and lane / 8 + 4 of column lane % 8
+  __device__ __forceinline__ void add(const float (&a)[kAgain], const float (&b)[2]) {
+#pragma unroll
+    for (int u = 0; u < kAgain; ++u)
+#pragma unroll
+      for (int x = 0; x < kAgain; ++x) s[x] = fmaf(a[u], __shfl_sync(0xffffffffu, b[u >> 2], (u & 3) * 8 + x), s[x]);
+  }
+  __device__ __forceinline__ void end(uint32_t at) const {
+#pragma unroll
+    for (int x = 0; x < kAgain; ++x)
+      if (wanted >> x & 1u) sts_f(at + (uint32_t)(x * 4), s[x]);
+  }
+};
+template <bool ACROSS, typename T>
+static __device__ __noinline__ void again(const Params &p, uint32_t at, int row, int end, int weight, int o0, int count) {
+  const int lane = (int)(threadIdx.x & 31u);
+  const bool valid = row < end;
+  row = min(row, end - 1);
+#pragma unroll 1
+  for (; count > 0; count -= kAgain, o0 += kAgain, at += kAgain * 4) {
+    Again f;
+    if (!f.start(at, valid, count)) continue;
+    if (p.pieces) {
+      const size_t o = (size_t)min(o0 + (lane & 7), p.n - 1), step = ACROSS ? (size_t)p.n : 1;
+      const T *x = reinterpret_cast<const T *>(p.raw_p) + (size_t)row * (size_t)p.k;
+      const T *w = reinterpret_cast<const T *>(p.raw_q) + (size_t)weight * (size_t)p.n * (size_t)p.k + (ACROSS ? o : o * (size_t)p.k);
+#pragma unroll 1
+      for (int i0 = 0; i0 < p.k && f.open(); i0 += kAgain) {
+        float a[kAgain], b[2];
+#pragma unroll
+        for (int u = 0; u < kAgain; ++u) a[u] = i0 + u < p.k ? to_float(x[i0 + u]) : 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int i = i0 + u * 4 + (lane >> 3);
+          b[u] = i < p.k ? to_float(w[(size_t)i * step]) : 0.f;
+        }
+        f.add(a, b);
+      }
+    }
+    if (p.alpha) {
+      const float alpha = __ldg(p.alpha + weight);
+#pragma unroll
+      for (int x = 0; x < kAgain; ++x) f.s[x] *= alpha;
+    }
+    const int adapter = p.rank && f.wanted ? adapter_of(p.ext, row) : -1;
+    if (adapter >= 0) {                          // each lane's own
+      const T *e = reinterpret_cast<const T *>(p.e) + (size_t)adapter * (size_t)p.n * (size_t)p.rank + (ACROSS ? (size_t)o0 : (size_t)o0 * (size_t)p.rank);
+      const size_t column = ACROSS ? 1 : (size_t)p.rank, step = ACROSS ? (size_t)p.n : 1;
+#pragma unroll 1
+      for (int j = 0; j < p.rank; ++j) {
+        const float t = kept<T>(p.t, row, grp::rank_pad(p.rank), j);
+#pragma unroll
+        for (int x = 0; x < kAgain; ++x) f.s[x] = fmaf(t, to_float(e[(size_t)min(x, p.n - 1 - o0) * column + (size_t)j * step]), f.s[x]);
+      }
+    }
+    f.end(at);
+  }
 }
-static __device__ __noinline__ float again_grad(const Params &p, int weight, int i, int j, bool sums) {
-  float s = 0.f;
-  const int first = p.runs.mapped ? 0 : weight, last = p.runs.mapped ? p.runs.count : weight + 1;
-  for (int r = first; r < last; ++r) {
-    const Run run = grp::run_at(p.runs, r);
-    if (run.weight != weight) continue;
-    for (int row = run.begin; row < run.end && s == s; ++row) {
-      const float a = reinterpret_cast<const float *>(p.raw_p)[(size_t)row * (size_t)p.k + (size_t)i];
-      s = sums ? s + a : fmaf(a, p.q_terms ? kept<float>(p.t, row, grp::rank_pad(p.n), j) : reinterpret_cast<const float *>(p.raw_q)[(size_t)row * (size_t)p.n + (size_t)j], s);
-    }
+// The same of a gradient, from row i (a lane's own) and column j0 on; `sums`: its first column is the sum of p.
+template <typename T>
+static __device__ __noinline__ void again_grad(const Params &p, uint32_t at, int weight, int i, int j0, bool sums, int count) {
+  const int lane = (int)(threadIdx.x & 31u), pad = grp::rank_pad(p.n);
+  const T *a_at = reinterpret_cast<const T *>(p.raw_p) + (size_t)min(i, p.k - 1);
+#pragma unroll 1
+  for (; count > 0; count -= kAgain, j0 += kAgain, at += kAgain * 4) {
+    Again f;
+    if (!f.start(at, i < p.k, count)) continue;
+    const int j = min(j0 + (lane & 7), p.n - 1);
+    const T *b_at = reinterpret_cast<const T *>(p.raw_q) + (size_t)j;
+    each_run_of(p.runs, weight, [&](int begin, int end) {
+#pragma unroll 1
+      for (int r0 = begin; r0 < end && f.open(); r0 += kAgain) {
+        float a[kAgain], b[2];
+#pragma unroll
+        for (int u = 0; u < kAgain; ++u) a[u] = r0 + u < end ? to_float(a_at[(size_t)(r0 + u) * (size_t)p.k]) : 0.f;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int row = r0 + u * 4 + (lane >> 3);
+          b[u] = row >= end ? 0.f : sums ? 1.f : p.q_terms ? kept<T>(p.t, row, pad, j) : to_float(b_at[(size_t)row * (size_t)p.n]);
+        }
+        f.add(a, b);
+      }
+    });
+    f.end(at);
   }
-  return s;
+}
+// 32 results of a lane to its 128 bytes, and back
+__device__ __forceinline__ void put_lane(uint32_t at, const float (&v)[32]) {
+  __syncwarp();                                  // others have read what was there
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    sts_u4(at + (uint32_t)(i * 16), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+}
+__device__ __forceinline__ void get_lane(uint32_t at, float (&v)[32]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint4 u = lds_u4(at + (uint32_t)(i * 16));
+    v[4 * i] = __uint_as_float(u.x); v[4 * i + 1] = __uint_as_float(u.y); v[4 * i + 2] = __uint_as_float(u.z); v[4 * i + 3] = __uint_as_float(u.w);
+  }
 }
 
 // What a lane delivers of a block of 32 rows x 32 columns: 4 columns of every fourth row.  bf16: its part of the residual, asked for ahead (fp32 has no registers
@@ -839,17 +932,11 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         T *out = reinterpret_cast<T *>(p.y) + (size_t)weight * (size_t)p.k * (size_t)p.n;
         auto deliver = [&](int c, float (&v)[32]) {                 // columns c on of this thread's row
           const int j0 = tn * p.nt + c;
-          if (kShort && i < p.k && any_nan(v)) {
-#pragma unroll 1
-            for (int x = 0; x < 32; ++x) {
-              float f = 0.f;
-#pragma unroll
-              for (int u = 0; u < 32; ++u) f = u == x ? v[u] : f;
-              if (f == f || (sums ? x > 0 : j0 + x >= p.n || c + x >= cols)) continue;
-              f = again_grad(p, weight, i, j0 + x, sums);
-#pragma unroll
-              for (int u = 0; u < 32; ++u) v[u] = u == x ? f : v[u];
-            }
+          if (kShort && __any_sync(0xffffffffu, any_nan(v))) {
+            const uint32_t at = staged + (uint32_t)(lane * 128);
+            put_lane(at, v);
+            again_grad<T>(p, at, weight, i, j0, sums, sums ? (c == 0 ? 1 : 0) : min(min(32, cols - c), p.n - j0));
+            get_lane(at, v);
           }
           if (sums) {
             if (c == 0 && i < p.k) p.sums[(size_t)weight * (size_t)p.k + (size_t)i] = v[0];
@@ -910,17 +997,11 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
 #pragma unroll
             for (int x = 0; x < 32; ++x) v[x] = filled ? v[x] * alpha : 0.f;
           }
-          if (kShort && row < t.end && any_nan(v)) {
-#pragma unroll 1
-            for (int x = 0; x < 32; ++x) {
-              float f = 0.f;
-#pragma unroll
-              for (int u = 0; u < 32; ++u) f = u == x ? v[u] : f;
-              if (f == f || o0 + x >= p.n || c + x >= p.nt) continue;
-              f = again<ACROSS>(p, row, t.weight, o0 + x);
-#pragma unroll
-              for (int u = 0; u < 32; ++u) v[u] = u == x ? f : v[u];
-            }
+          if (kShort && __any_sync(0xffffffffu, any_nan(v))) {
+            const uint32_t at = staged + (uint32_t)(lane * 128);
+            put_lane(at, v);
+            again<ACROSS, T>(p, at, row, t.end, t.weight, o0, min(min(32, p.nt - c), p.n - o0));
+            get_lane(at, v);
           }
           if (p.y_terms) {
             constexpr int kKept = N == 3 ? 3 : 2;

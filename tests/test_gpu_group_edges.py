@@ -45,3 +45,35 @@ def test_more_tiles_of_gradients_than_ctas(rank, dtype):
     check(db.t, db_want, db_slack, "db")
     without = sorted(set(range(n)) - {i for _, _, i, _, _ in ahead})
     assert len(without) == 13 and not bool(da.t[without].any()) and not bool(db.t[without].any())
+
+
+def test_an_infinity_among_many_rows():
+    """fp32 gradients of a group of two million rows with infinities in dy and in x: what it makes of a gradient is worked out again by FMAs, over all rows, and comes
+    in the time that the waits for it allow."""
+    dt, rows, c_in, c_out = torch.float32, 1 << 21, 72, 136
+    of_type(dt)
+    x, dy = rand(rows, c_in, seed=1, dtype=dt), rand(rows, c_out, seed=2, dtype=dt)
+    off, w = offsets_of([rows]), torch.empty(1, c_out, c_in, device="cuda")
+    ws = torch.zeros(dc.group_workspace_bytes(rows, 1, c_in, c_out, dc.F32), dtype=torch.uint8, device="cuda")
+    a, b = dy.double(), x.double()
+    want, slack = a.t() @ b, (rows + 4) * U * (a.abs().t() @ b.abs())
+    sums, room = a.sum(0), (rows + 4) * U * a.abs().sum(0)
+    for r, i, value in ((rows // 2 + 11, 77, float("inf")), (rows - 3, 5, float("-inf"))):
+        want[i], sums[i] = torch.sign(b[r]) * value, value
+        dy[r, i] = value
+    keep = want[[77, 5], 40].clone()
+    want[:, 40] = torch.sign(a[17]) * float("inf")
+    want[[77, 5], 40] += keep                    # of the other sign: no number
+    x[17, 40] = float("inf")
+    dw, db = Guarded(torch, (1, c_out, c_in), dt, fill=7.0), Guarded(torch, (1, c_out), dt, fill=7.0)
+    dc.group_backward(dy, x, off, w, None, dw.t, db.t, ws)
+    torch.cuda.synchronize()
+    dw.check("dw"), db.check("db")
+    assert dc.workspace_status(ws) == dc.OK
+    got = dw.t[0].double()
+    fine = want.isfinite()
+    assert torch.equal(got[~fine].nan_to_num(), want[~fine].nan_to_num()) and torch.equal(got.isnan(), want.isnan())
+    check(torch.where(fine, got, 0.0).float(), torch.where(fine, want, 0.0), slack, "dw")
+    assert torch.equal(db.t[0][[77, 5]].double(), sums[[77, 5]])
+    fine = sums.isfinite()
+    assert bool(((db.t[0].double() - sums).abs()[fine] <= room[fine]).all())

@@ -18,7 +18,8 @@
 // fp32: a value is three bf16 terms that add up to it (split_tc), laid out one behind the other, and a stage holds all three of both operands: six of
 // their nine products are above 2^-24 of the result, small ones first.  The tensor core cuts its sums instead of rounding them, so a piece's
 // sum is read out and added up in fp32 registers.  A result that is a NaN is worked out again by FMAs: an infinity, or a value
-// beyond the largest bf16, has a NaN among its terms.
+// beyond the largest bf16, has a NaN among its terms.  So are results of adapters in bf16, and their gradients: what rows keep is two terms, and an infinity times
+// both is a NaN where the low one is 0 or has the other sign.
 //
 // What bounds it: many rows, the tensor core under the power cap (8192 rows, 4096 -> 4096 in one group 184 us, 1.49 PFLOP/s; 16384 ragged rows of 16
 // groups 401 us a launch by itself, 486 one behind the other); few rows, the weights' bytes (256 rows of 64 groups, 2048 -> 2048, 82 to 85 us, 6.4 TB/s); fp32,
@@ -74,7 +75,7 @@ struct Params {
   int rank, rank_pieces;     // adapters: pieces of 64 of the rank
   int t_bytes, e_bytes, e_wide;      // kTile: bytes of a stage's rows of t and e; numbers of the rank in a row (e across: rows)
   const bf16 *t;             // what rows keep
-  const void *e;             // kFew: the adapters' matrices; fp32: as the caller has them
+  const void *e;             // the adapters' matrices; kTile: as the caller has them
   int e_pitch;
   int slots, slot_rows, row_bytes;       // kFew: of adapters' parts of the tile's columns in shared memory, slot_rows rows' to a slot
   int early;                 // all but t was there before the launch in front of this one began, and that one writes nothing that this one does
@@ -82,7 +83,7 @@ struct Params {
   // kGrad
   float *sums;
   int q_terms, out_across;   // out_across: out is [n][m]
-  const void *raw_p, *raw_q; // fp32: the operands themselves
+  const void *raw_p, *raw_q; // the operands as the caller has them
 };
 
 __device__ __forceinline__ uint64_t desc_along(uint32_t a) {     // rows of 64 along the sum, 1024 bytes between groups of 8 rows
@@ -339,8 +340,10 @@ struct Again {
 template <bool ACROSS, typename T>
 static __device__ __noinline__ void again(const Params &p, uint32_t at, int row, int end, int weight, int o0, int count) {
   const int lane = (int)(threadIdx.x & 31u);
-  const bool valid = row < end;
+  bool valid = row < end;
   row = min(row, end - 1);
+  const int adapter = p.rank && valid ? adapter_of(p.ext, row) : -1;
+  if (sizeof(T) == 2) valid = adapter >= 0;      // a shared product is one of bf16 numbers: its NaN is one
 #pragma unroll 1
   for (; count > 0; count -= kAgain, o0 += kAgain, at += kAgain * 4) {
     Again f;
@@ -367,8 +370,7 @@ static __device__ __noinline__ void again(const Params &p, uint32_t at, int row,
 #pragma unroll
       for (int x = 0; x < kAgain; ++x) f.s[x] *= alpha;
     }
-    const int adapter = p.rank && f.wanted ? adapter_of(p.ext, row) : -1;
-    if (adapter >= 0) {                          // each lane's own
+    if (adapter >= 0 && f.wanted) {              // each lane's own
       const T *e = reinterpret_cast<const T *>(p.e) + (size_t)adapter * (size_t)p.n * (size_t)p.rank + (ACROSS ? (size_t)o0 : (size_t)o0 * (size_t)p.rank);
       const size_t column = ACROSS ? 1 : (size_t)p.rank, step = ACROSS ? (size_t)p.n : 1;
 #pragma unroll 1
@@ -520,7 +522,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   constexpr int N = kTerms<T>;
   constexpr bool kShort = N == 3;                // sums of a piece
   constexpr uint32_t kAcc = kAccs<T> - 1, kAccLog = kShort ? 2 : 1;
-  constexpr unsigned long long kLimit = FORM == kGrad || kShort ? kLongNs : kWaitLimitNs;
+  constexpr unsigned long long kLimit = FORM == kFew ? kWaitLimitNs : kLongNs;
   // products of terms, small ones first
   constexpr int kPairs = N == 3 ? 6 : 1;
   constexpr int kTermP[6] = {N == 3 ? 2 : 0, 0, 1, 1, 0, 0}, kTermQ[6] = {0, 2, 1, 0, 1, 0};
@@ -932,7 +934,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         T *out = reinterpret_cast<T *>(p.y) + (size_t)weight * (size_t)p.k * (size_t)p.n;
         auto deliver = [&](int c, float (&v)[32]) {                 // columns c on of this thread's row
           const int j0 = tn * p.nt + c;
-          if (kShort && __any_sync(0xffffffffu, any_nan(v))) {
+          if ((kShort || p.q_terms) && __any_sync(0xffffffffu, any_nan(v))) {
             const uint32_t at = staged + (uint32_t)(lane * 128);
             put_lane(at, v);
             again_grad<T>(p, at, weight, i, j0, sums, sums ? (c == 0 ? 1 : 0) : min(min(32, cols - c), p.n - j0));
@@ -997,7 +999,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
 #pragma unroll
             for (int x = 0; x < 32; ++x) v[x] = filled ? v[x] * alpha : 0.f;
           }
-          if (kShort && __any_sync(0xffffffffu, any_nan(v))) {
+          if ((kShort || p.rank) && __any_sync(0xffffffffu, any_nan(v))) {
             const uint32_t at = staged + (uint32_t)(lane * 128);
             put_lane(at, v);
             again<ACROSS, T>(p, at, row, t.end, t.weight, o0, min(min(32, p.nt - c), p.n - o0));
@@ -1646,7 +1648,6 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
     p.rank = j.rank;
     p.rank_pieces = dc_div_up(j.rank, kPiece);
     p.t = (const bf16 *)j.t;
-    p.e = wide ? j.raw_e : j.e;
     p.e_pitch = j.e_pitch;
   }
   const int runs = runs_with_rows(j.runs);
@@ -1671,6 +1672,7 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   p.nt = shape.nt;
   p.split = shape.split;
   p.early = early;
+  p.e = by_few ? j.e : j.raw_e;
   if (by_few) {
     p.q_bytes = p.nt * 128;
     p.tiles_n = dc_div_up(j.n, 128);

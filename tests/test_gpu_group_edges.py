@@ -77,3 +77,81 @@ def test_an_infinity_among_many_rows():
     assert torch.equal(db.t[0][[77, 5]].double(), sums[[77, 5]])
     fine = sums.isfinite()
     assert bool(((db.t[0].double() - sums).abs()[fine] <= room[fine]).all())
+
+
+def each_by_each(p, q):
+    """p [m, k] times q [k, n] in 64 bits, element by element: a library product may skip a NaN."""
+    out = [(p[i:i + 16, :, None].double() * q[None].double()).sum(1) for i in range(0, p.shape[0], 16)]
+    return torch.cat(out)
+
+
+def finite_part(*tensors):
+    return [torch.where(t.isfinite(), t, torch.zeros_like(t)) for t in tensors]
+
+
+def check_class(got, want, slack, what):
+    got = got.double()
+    assert torch.equal(got.isnan(), want.isnan()), "%s: NaN in %d places, not %d" % (what, int(got.isnan().sum()), int(want.isnan().sum()))
+    far = want.isinf()
+    assert torch.equal(got.isinf(), far) and torch.equal(got[far], want[far]), "%s: infinities" % what
+    fine = want.isfinite()
+    check(torch.where(fine, got, 0.0).float(), torch.where(fine, want, 0.0), slack, what)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rank", [8, 48])
+@pytest.mark.parametrize("sizes", [[1, 1, 1, 1], [20, 1, 8, 31], [150, 3, 100, 147]])
+@pytest.mark.parametrize("shared", [True, False])
+def test_infinities_are_what_the_formula_makes_of_them(shared, sizes, rank, dtype):
+    """Infinities in an adapter's matrices, in x and in dy: infinities, and NaN where infinities cancel, in y, dx, da and db, whichever way rows go.  What a row keeps
+    of its adapter may lie on a bf16 number, so that its low terms are 0, or between two."""
+    dt, rows, c_in, c_out = TYPES[dtype], sum(sizes), 136, 264
+    of_type(dt)
+    x, dy, w = rand(rows, c_in, seed=1, dtype=dt), rand(rows, c_out, seed=2, dtype=dt), rand(c_out, c_in, seed=3, dtype=dt) if shared else None
+    a, b = rand(4, rank, c_in, seed=4, dtype=dt), rand(4, c_out, rank, seed=5, dtype=dt)
+    off, which = offsets_of(sizes), torch.arange(4, dtype=torch.int32, device="cuda")
+    runs = list(zip(off.tolist()[:-1], off.tolist()[1:]))
+    x[0], dy[0] = 0.0, 0.0
+    x[0, 0] = dy[0, 0] = 1.0                     # t and u are a column of the adapter's
+    b[0, 5, 2], b[0, 6, 1], b[0, 7, :2] = float("inf"), float("-inf"), float("inf")
+    a[0, 1, 9], a[0, 2, 10], a[1, 3, 4] = float("inf"), float("-inf"), float("inf")
+    x[runs[2][0], 9], dy[runs[3][1] - 1, 11] = float("inf"), float("-inf")
+    ad = dc.Adapters(a, b)
+    ws, saved = workspace(dc.adapter_workspace_bytes(rows, c_in, c_out, ad, ad.dtype)), ad.saved(rows)
+    y, y6 = torch.empty_like(dy), torch.empty_like(dy)
+    dx, da, db = torch.empty_like(x), torch.empty_like(a), torch.empty_like(b)
+    dc.adapter_forward(x, w, ad, off, which, None, dc.ACT_RELU6, None, saved, y6, ws.t)
+    dc.adapter_forward(x, w, ad, off, which, None, 0, None, saved, y, ws.t)
+    dc.adapter_backward(dy, x, w, ad, off, which, saved, dx, da, db, ws.t)
+    torch.cuda.synchronize()
+    assert dc.workspace_status(ws.t) == dc.OK
+    ws.check("workspace")
+    y_want, dx_want = torch.zeros(rows, c_out, dtype=torch.float64, device="cuda"), torch.zeros(rows, c_in, dtype=torch.float64, device="cuda")
+    if shared:
+        y_want, dx_want = each_by_each(x, w.t()), each_by_each(dy, w)
+    da_want, db_want = a.double(), b.double()
+    fx, fdy, fa, fb = finite_part(x, dy, a, b)
+    _, y_slack, ahead = adapter_want(fx, w, fa, fb, None, off, which)
+    _, dx_slack, back = adapter_want(fdy, w.t().contiguous() if shared else None, fb.transpose(1, 2).contiguous(), fa.transpose(1, 2).contiguous(), None, off, which)
+    da_slack, db_slack = torch.zeros_like(da_want), torch.zeros_like(db_want)
+    for i, (lo, hi) in enumerate(runs):
+        t, u = each_by_each(x[lo:hi], a[i].t()), each_by_each(dy[lo:hi], b[i])
+        y_want[lo:hi] += each_by_each(t, b[i].t())
+        dx_want[lo:hi] += each_by_each(u, a[i])
+        da_want[i], db_want[i] = each_by_each(u.t(), x[lo:hi]), each_by_each(dy[lo:hi].t(), t)
+        (_, _, _, t, off_t), (_, _, _, u, off_u) = ahead[i], back[i]
+        xs, ds = fx[lo:hi].double(), fdy[lo:hi].double()
+        da_slack[i] = off_u.t() @ xs.abs() + (rows + 8) * U * (u.abs().t() @ xs.abs())
+        db_slack[i] = ds.abs().t() @ off_t + (rows + 8) * U * (ds.abs().t() @ t.abs())
+    assert all(bool(t.isinf().any()) and bool(t.isnan().any()) for t in (y_want, dx_want)) and all(bool(t.isinf().any()) for t in (da_want, db_want))
+    check_class(y, y_want, y_slack, "y")
+    check_class(dx, dx_want, dx_slack, "dx")
+    check_class(da, da_want, da_slack, "da")
+    check_class(db, db_want, db_slack, "db")
+    check_class(y6, torch.where(y_want.isnan(), 0.0, y_want.clamp(0, 6)), y_slack, "y under ReLU6")      # a NaN is 0 there, as in all of the library
+
+
+def test_those_sizes_take_both_ways():
+    """The sizes above go by short runs and by tiles."""
+    forms = {dc.group_plan(n, 4, 136, 264, 8, dc.BF16, dc.GROUP_FORWARD).form for n in (4, 60, 400)}
+    assert {dc.GROUP_FEW_ROWS, dc.GROUP_TILES} <= forms

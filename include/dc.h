@@ -458,8 +458,8 @@ dc_status dc_q4_plan_query(long long rows, int c_in, int c_out, dc_q4_format for
  * decreasing, from 0 to at most `rows`.  A run may be empty, and rows in front of the first or behind the last run belong to none.  (Offsets are cut to
  * [0, rows]; where they decrease, rows may be written twice, with no order between the two, and none outside the arrays.)
  * Rows are dense, of `dtype`, and multiplied on the tensor core with fp32 sums: DC_BF16 as they are, DC_F32 as products of bf16 terms as described at
- * dc_merge_chain, or where runs are short by FMAs.  Results are rounded once.  Results of fp32, and of adapters and their gradients, that come out as no
- * numbers are worked out again by FMAs, as infinities have no terms: they are what the formula makes of them.  That takes long (gradients of a weight with a
+ * dc_merge_chain, or where runs are short by FMAs.  Results are rounded once.  Infinities make of results what the formula says, beside adapters too.  fp32
+ * results of terms that come out as no numbers are worked out again by FMAs, as infinities have no terms; that takes long (gradients of a weight with a
  * million rows, an infinity among them, 0.8 s; beyond some 2^24 rows a wait runs out).
  * rows: 0 to 2^30; without rows, forward calls write nothing.  Widths: 1 to 2^20.  Workspaces: device, the bytes that the query
  * says, the first 256 zeroed once by the caller; a bounded wait that runs out is latched there (dc_workspace_status).  Calls that may run at

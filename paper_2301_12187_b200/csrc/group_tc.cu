@@ -18,8 +18,7 @@
 // fp32: a value is three bf16 terms that add up to it (split_tc), laid out one behind the other, and a stage holds all three of both operands: six of
 // their nine products are above 2^-24 of the result, small ones first.  The tensor core cuts its sums instead of rounding them, so a piece's
 // sum is read out and added up in fp32 registers.  A result that is a NaN is worked out again by FMAs: an infinity, or a value
-// beyond the largest bf16, has a NaN among its terms.  So are results of adapters in bf16, and their gradients: what rows keep is two terms, and an infinity times
-// both is a NaN where the low one is 0 or has the other sign.
+// beyond the largest bf16, has a NaN among its terms.
 //
 // What bounds it: many rows, the tensor core under the power cap (8192 rows, 4096 -> 4096 in one group 184 us, 1.49 PFLOP/s; 16384 ragged rows of 16
 // groups 401 us a launch by itself, 486 one behind the other); few rows, the weights' bytes (256 rows of 64 groups, 2048 -> 2048, 82 to 85 us, 6.4 TB/s); fp32,
@@ -75,7 +74,7 @@ struct Params {
   int rank, rank_pieces;     // adapters: pieces of 64 of the rank
   int t_bytes, e_bytes, e_wide;      // kTile: bytes of a stage's rows of t and e; numbers of the rank in a row (e across: rows)
   const bf16 *t;             // what rows keep
-  const void *e;             // the adapters' matrices; kTile: as the caller has them
+  const void *e;             // kFew: the adapters' matrices; fp32: as the caller has them
   int e_pitch;
   int slots, slot_rows, row_bytes;       // kFew: of adapters' parts of the tile's columns in shared memory, slot_rows rows' to a slot
   int early;                 // all but t was there before the launch in front of this one began, and that one writes nothing that this one does
@@ -83,7 +82,7 @@ struct Params {
   // kGrad
   float *sums;
   int q_terms, out_across;   // out_across: out is [n][m]
-  const void *raw_p, *raw_q; // the operands as the caller has them
+  const void *raw_p, *raw_q; // fp32: the operands themselves
 };
 
 __device__ __forceinline__ uint64_t desc_along(uint32_t a) {     // rows of 64 along the sum, 1024 bytes between groups of 8 rows
@@ -271,10 +270,22 @@ __device__ __forceinline__ void unpack8(uint4 w, float *v) {
 __device__ __forceinline__ uint4 pack8(const float *v) {
   return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
-// What a row keeps, as terms of bf16 that add up: two (16 bits together), or of fp32 rows three.  Of an infinity or a NaN the first is itself, the others 0; of
-// a number that would round to an infinity the first is the largest bf16.
+// What a row keeps, as terms of bf16 that add up: two, or of fp32 rows three.
+// Two: the first is cut off, not rounded, and one step less where nothing is left, so that both have the number's sign and neither is 0 (numbers below 2^-118
+// aside): an infinity times the number is then the infinity of both products.  (Rounded, with a low term of 0 or of the other sign, their sum was a NaN.)  What is left is
+// below 2^-7 of the number and rounded to 2^-9 of itself: 16 bits.  Of an infinity or a NaN both are itself.
+// Three: rounded, 24 bits.  Of an infinity or a NaN the first is itself, the others 0; of a number that would round to an infinity the first is the largest bf16.
 template <typename T>
 __device__ __forceinline__ void terms_of(float v, float (&t)[3]) {
+  if (sizeof(T) == 2) {
+    uint32_t u = __float_as_uint(v) & 0xffff0000u;
+    if (u == __float_as_uint(v) && v != 0.f) u -= 0x10000u;
+    const bool finite = v - v == 0.f;
+    t[0] = finite ? __uint_as_float(u) : v;
+    t[1] = finite ? v - t[0] : v;                // stored rounded
+    t[2] = 0.f;
+    return;
+  }
   constexpr float kLargest = 3.38953138925153547e38f;
   t[0] = __bfloat162float(__float2bfloat16(v));
   if (fabsf(v) > kLargest && fabsf(v) <= 3.402823466e38f) t[0] = copysignf(kLargest, v);
@@ -337,30 +348,28 @@ struct Again {
       if (wanted >> x & 1u) sts_f(at + (uint32_t)(x * 4), s[x]);
   }
 };
-template <bool ACROSS, typename T>
+template <bool ACROSS>
 static __device__ __noinline__ void again(const Params &p, uint32_t at, int row, int end, int weight, int o0, int count) {
   const int lane = (int)(threadIdx.x & 31u);
-  bool valid = row < end;
+  const bool valid = row < end;
   row = min(row, end - 1);
-  const int adapter = p.rank && valid ? adapter_of(p.ext, row) : -1;
-  if (sizeof(T) == 2) valid = adapter >= 0;      // a shared product is one of bf16 numbers: its NaN is one
 #pragma unroll 1
   for (; count > 0; count -= kAgain, o0 += kAgain, at += kAgain * 4) {
     Again f;
     if (!f.start(at, valid, count)) continue;
     if (p.pieces) {
       const size_t o = (size_t)min(o0 + (lane & 7), p.n - 1), step = ACROSS ? (size_t)p.n : 1;
-      const T *x = reinterpret_cast<const T *>(p.raw_p) + (size_t)row * (size_t)p.k;
-      const T *w = reinterpret_cast<const T *>(p.raw_q) + (size_t)weight * (size_t)p.n * (size_t)p.k + (ACROSS ? o : o * (size_t)p.k);
+      const float *x = reinterpret_cast<const float *>(p.raw_p) + (size_t)row * (size_t)p.k;
+      const float *w = reinterpret_cast<const float *>(p.raw_q) + (size_t)weight * (size_t)p.n * (size_t)p.k + (ACROSS ? o : o * (size_t)p.k);
 #pragma unroll 1
       for (int i0 = 0; i0 < p.k && f.open(); i0 += kAgain) {
         float a[kAgain], b[2];
 #pragma unroll
-        for (int u = 0; u < kAgain; ++u) a[u] = i0 + u < p.k ? to_float(x[i0 + u]) : 0.f;
+        for (int u = 0; u < kAgain; ++u) a[u] = i0 + u < p.k ? x[i0 + u] : 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int i = i0 + u * 4 + (lane >> 3);
-          b[u] = i < p.k ? to_float(w[(size_t)i * step]) : 0.f;
+          b[u] = i < p.k ? w[(size_t)i * step] : 0.f;
         }
         f.add(a, b);
       }
@@ -370,40 +379,40 @@ static __device__ __noinline__ void again(const Params &p, uint32_t at, int row,
 #pragma unroll
       for (int x = 0; x < kAgain; ++x) f.s[x] *= alpha;
     }
-    if (adapter >= 0 && f.wanted) {              // each lane's own
-      const T *e = reinterpret_cast<const T *>(p.e) + (size_t)adapter * (size_t)p.n * (size_t)p.rank + (ACROSS ? (size_t)o0 : (size_t)o0 * (size_t)p.rank);
+    const int adapter = p.rank && f.wanted ? adapter_of(p.ext, row) : -1;
+    if (adapter >= 0) {                          // each lane's own
+      const float *e = reinterpret_cast<const float *>(p.e) + (size_t)adapter * (size_t)p.n * (size_t)p.rank + (ACROSS ? (size_t)o0 : (size_t)o0 * (size_t)p.rank);
       const size_t column = ACROSS ? 1 : (size_t)p.rank, step = ACROSS ? (size_t)p.n : 1;
 #pragma unroll 1
       for (int j = 0; j < p.rank; ++j) {
-        const float t = kept<T>(p.t, row, grp::rank_pad(p.rank), j);
+        const float t = kept<float>(p.t, row, grp::rank_pad(p.rank), j);
 #pragma unroll
-        for (int x = 0; x < kAgain; ++x) f.s[x] = fmaf(t, to_float(e[(size_t)min(x, p.n - 1 - o0) * column + (size_t)j * step]), f.s[x]);
+        for (int x = 0; x < kAgain; ++x) f.s[x] = fmaf(t, e[(size_t)min(x, p.n - 1 - o0) * column + (size_t)j * step], f.s[x]);
       }
     }
     f.end(at);
   }
 }
 // The same of a gradient, from row i (a lane's own) and column j0 on; `sums`: its first column is the sum of p.
-template <typename T>
 static __device__ __noinline__ void again_grad(const Params &p, uint32_t at, int weight, int i, int j0, bool sums, int count) {
   const int lane = (int)(threadIdx.x & 31u), pad = grp::rank_pad(p.n);
-  const T *a_at = reinterpret_cast<const T *>(p.raw_p) + (size_t)min(i, p.k - 1);
+  const float *a_at = reinterpret_cast<const float *>(p.raw_p) + (size_t)min(i, p.k - 1);
 #pragma unroll 1
   for (; count > 0; count -= kAgain, j0 += kAgain, at += kAgain * 4) {
     Again f;
     if (!f.start(at, i < p.k, count)) continue;
     const int j = min(j0 + (lane & 7), p.n - 1);
-    const T *b_at = reinterpret_cast<const T *>(p.raw_q) + (size_t)j;
+    const float *b_at = reinterpret_cast<const float *>(p.raw_q) + (size_t)j;
     each_run_of(p.runs, weight, [&](int begin, int end) {
 #pragma unroll 1
       for (int r0 = begin; r0 < end && f.open(); r0 += kAgain) {
         float a[kAgain], b[2];
 #pragma unroll
-        for (int u = 0; u < kAgain; ++u) a[u] = r0 + u < end ? to_float(a_at[(size_t)(r0 + u) * (size_t)p.k]) : 0.f;
+        for (int u = 0; u < kAgain; ++u) a[u] = r0 + u < end ? a_at[(size_t)(r0 + u) * (size_t)p.k] : 0.f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int row = r0 + u * 4 + (lane >> 3);
-          b[u] = row >= end ? 0.f : sums ? 1.f : p.q_terms ? kept<T>(p.t, row, pad, j) : to_float(b_at[(size_t)row * (size_t)p.n]);
+          b[u] = row >= end ? 0.f : sums ? 1.f : p.q_terms ? kept<float>(p.t, row, pad, j) : b_at[(size_t)row * (size_t)p.n];
         }
         f.add(a, b);
       }
@@ -522,7 +531,7 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
   constexpr int N = kTerms<T>;
   constexpr bool kShort = N == 3;                // sums of a piece
   constexpr uint32_t kAcc = kAccs<T> - 1, kAccLog = kShort ? 2 : 1;
-  constexpr unsigned long long kLimit = FORM == kFew ? kWaitLimitNs : kLongNs;
+  constexpr unsigned long long kLimit = FORM == kGrad || kShort ? kLongNs : kWaitLimitNs;
   // products of terms, small ones first
   constexpr int kPairs = N == 3 ? 6 : 1;
   constexpr int kTermP[6] = {N == 3 ? 2 : 0, 0, 1, 1, 0, 0}, kTermQ[6] = {0, 2, 1, 0, 1, 0};
@@ -934,10 +943,10 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
         T *out = reinterpret_cast<T *>(p.y) + (size_t)weight * (size_t)p.k * (size_t)p.n;
         auto deliver = [&](int c, float (&v)[32]) {                 // columns c on of this thread's row
           const int j0 = tn * p.nt + c;
-          if ((kShort || p.q_terms) && __any_sync(0xffffffffu, any_nan(v))) {
+          if (kShort && __any_sync(0xffffffffu, any_nan(v))) {
             const uint32_t at = staged + (uint32_t)(lane * 128);
             put_lane(at, v);
-            again_grad<T>(p, at, weight, i, j0, sums, sums ? (c == 0 ? 1 : 0) : min(min(32, cols - c), p.n - j0));
+            again_grad(p, at, weight, i, j0, sums, sums ? (c == 0 ? 1 : 0) : min(min(32, cols - c), p.n - j0));
             get_lane(at, v);
           }
           if (sums) {
@@ -999,10 +1008,10 @@ k_group_tc(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CU
 #pragma unroll
             for (int x = 0; x < 32; ++x) v[x] = filled ? v[x] * alpha : 0.f;
           }
-          if ((kShort || p.rank) && __any_sync(0xffffffffu, any_nan(v))) {
+          if (kShort && __any_sync(0xffffffffu, any_nan(v))) {
             const uint32_t at = staged + (uint32_t)(lane * 128);
             put_lane(at, v);
-            again<ACROSS, T>(p, at, row, t.end, t.weight, o0, min(min(32, p.nt - c), p.n - o0));
+            again<ACROSS>(p, at, row, t.end, t.weight, o0, min(min(32, p.nt - c), p.n - o0));
             get_lane(at, v);
           }
           if (p.y_terms) {
@@ -1648,6 +1657,7 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
     p.rank = j.rank;
     p.rank_pieces = dc_div_up(j.rank, kPiece);
     p.t = (const bf16 *)j.t;
+    p.e = wide ? j.raw_e : j.e;
     p.e_pitch = j.e_pitch;
   }
   const int runs = runs_with_rows(j.runs);
@@ -1672,7 +1682,6 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   p.nt = shape.nt;
   p.split = shape.split;
   p.early = early;
-  p.e = by_few ? j.e : j.raw_e;
   if (by_few) {
     p.q_bytes = p.nt * 128;
     p.tiles_n = dc_div_up(j.n, 128);

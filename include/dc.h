@@ -455,7 +455,7 @@ dc_status dc_q4_plan_query(long long rows, int c_in, int c_out, dc_q4_format for
  * products of rows with weights, as in the section above -- whose weights depend on the row.)
  *
  * Runs.  Rows come sorted: run s is rows offsets[s] <= r < offsets[s + 1], offsets an array of 32-bit integers on the DEVICE, not
- * decreasing, from 0 to at most `rows`.  A run may be empty, and rows in front of the first or behind the last run belong to none.  (Offsets are cut to
+ * decreasing, each 0 to `rows`.  A run may be empty; rows in front of the first run (offsets[0] above 0) or behind the last one belong to none.  (Offsets are cut to
  * [0, rows]; where they decrease, rows may be written twice, with no order between the two, and none outside the arrays.)
  * Rows are dense, of `dtype`, and multiplied on the tensor core with fp32 sums: DC_BF16 as they are, DC_F32 as products of bf16 terms as described at
  * dc_merge_chain, or where runs are short by FMAs.  Results are rounded once.  Infinities make of results what the formula says, beside adapters too.  fp32

@@ -1,4 +1,5 @@
-"""Grouped products and adapters on the GPU: gradients of which a CTA makes several tiles, one behind the other.  Tolerances as in test_gpu_group.py."""
+"""Grouped products and adapters on the GPU: gradients of which a CTA makes several tiles, infinities, rows in front of the first run.  Tolerances as in
+test_gpu_group.py."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -7,7 +8,7 @@ pytestmark = pytest.mark.gpu
 from paper_2301_12187_b200 import dc
 from tests.group_sizes import spread
 from tests.parity_util import Guarded
-from tests.test_gpu_group import TYPES, U, adapter_want, check, of_type, offsets_of, rand, workspace
+from tests.test_gpu_group import TYPES, U, adapter_want, check, group_want, of_type, offsets_of, rand, workspace
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
@@ -155,3 +156,59 @@ def test_those_sizes_take_both_ways():
     """The sizes above go by short runs and by tiles."""
     forms = {dc.group_plan(n, 4, 136, 264, 8, dc.BF16, dc.GROUP_FORWARD).form for n in (4, 60, 400)}
     assert {dc.GROUP_FEW_ROWS, dc.GROUP_TILES} <= forms
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("front,sizes,c_in,c_out", [(1, [1, 2], 72, 40), (5, [3, 0, 2], 136, 264), (70, [30, 0, 100], 72, 136), (129, [300, 1, 270], 520, 264),
+                                                     (3, [1] * 40, 264, 1032)])
+def test_rows_in_front_of_the_first_run(front, sizes, c_in, c_out, dtype):
+    """The first offset above 0: rows in front of it belong to no group, and stay as they were; to no adapter's run, and go without.  They hold NaN where nothing may read them."""
+    dt, n, rows = TYPES[dtype], len(sizes), front + sum(sizes) + 4
+    of_type(dt)
+    off = (offsets_of(sizes) + front).int()
+    lo, hi = front, rows - 4
+    x, dy = rand(rows, c_in, seed=1, dtype=dt), rand(rows, c_out, seed=2, dtype=dt)
+    w = rand(n, c_out, c_in, seed=3, dtype=dt)
+    xn, dyn = x.clone(), dy.clone()
+    for t in (xn, dyn):
+        t[:lo], t[hi:] = float("nan"), float("inf")
+    ws = workspace(dc.group_workspace_bytes(rows, n, c_in, c_out, dc.dtype_code(dt)))
+    y, dx, dw = Guarded(torch, (rows, c_out), dt, fill=7.0), Guarded(torch, (rows, c_in), dt, fill=7.0), Guarded(torch, (n, c_out, c_in), dt, fill=7.0)
+    db = Guarded(torch, (n, c_out), torch.float32, fill=7.0)
+    dc.group_forward(xn, off, w, None, 0, y.t, ws.t)
+    dc.group_backward(dyn, xn, off, w, dx.t, dw.t, db.t, ws.t)
+    torch.cuda.synchronize()
+    for q in (y, dx, dw, db, ws):
+        q.check("groups")
+    want, slack, mine = group_want(x, off, w, None, 0)
+    check(y.t[mine], want[mine], slack[mine], "y")
+    assert bool((y.t[~mine] == 7.0).all()) and bool((dx.t[~mine] == 7.0).all()) and int(mine.sum()) == hi - lo
+    for g, (p, q) in enumerate(zip(off.tolist()[:-1], off.tolist()[1:])):
+        a, b, m = dy[p:q].double(), x[p:q].double(), w[g].double()
+        check(dx.t[p:q], a @ m, (c_out + 4) * U * (a.abs() @ m.abs()), "dx")
+        check(dw.t[g], a.t() @ b, (q - p + 4) * U * (a.abs().t() @ b.abs()), "dw")
+        assert bool(((db.t[g].double() - a.sum(0)).abs() <= (q - p + 4) * U * a.abs().sum(0)).all())
+    # adapters
+    a, b, shared = rand(n, 16, c_in, seed=4, dtype=dt), rand(n, c_out, 16, seed=5, dtype=dt), w[0].contiguous()
+    ad, which = dc.Adapters(a, b), torch.arange(n, dtype=torch.int32, device="cuda")
+    ws, saved = workspace(dc.adapter_workspace_bytes(rows, c_in, c_out, ad, ad.dtype)), Guarded(torch, (ad.saved(rows).numel(),), torch.uint8, fill=0xFF)
+    da, db = Guarded(torch, tuple(a.shape), dt, fill=7.0), Guarded(torch, tuple(b.shape), dt, fill=7.0)
+    dc.adapter_forward(x, shared, ad, off, which, None, 0, None, saved.t, y.t, ws.t)
+    dc.adapter_backward(dy, x, shared, ad, off, which, saved.t, dx.t, da.t, db.t, ws.t)
+    torch.cuda.synchronize()
+    for q in (y, dx, da, db, ws, saved):
+        q.check("adapters")
+    want, slack, ahead = adapter_want(x, shared, a, b, None, off, which)
+    check(y.t, want, slack, "y of adapters")
+    want, slack, back = adapter_want(dy, shared.t().contiguous(), b.transpose(1, 2).contiguous(), a.transpose(1, 2).contiguous(), None, off, which)
+    check(dx.t, want, slack, "dx of adapters")
+    da_first, db_first = da.t.clone(), db.t.clone()
+    dc.adapter_forward(xn, shared, ad, off, which, None, 0, None, saved.t, y.t, ws.t)
+    dc.adapter_backward(dyn, xn, shared, ad, off, which, saved.t, dx.t, da.t, db.t, ws.t)
+    torch.cuda.synchronize()
+    assert torch.equal(da.t, da_first) and torch.equal(db.t, db_first)
+    for (p, q, i, t, off_t), (_, _, _, u, off_u) in zip(ahead, back):
+        xs, ds = x[p:q].double(), dy[p:q].double()
+        check(da.t[i], u.t() @ xs, off_u.t() @ xs.abs() + (rows + 8) * U * (u.abs().t() @ xs.abs()), "da")
+        check(db.t[i], ds.t() @ t, ds.abs().t() @ off_t + (rows + 8) * U * (ds.abs().t() @ t.abs()), "db")
+    assert dc.workspace_status(ws.t) == dc.OK

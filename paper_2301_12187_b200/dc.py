@@ -778,24 +778,32 @@ def group_backward(dy, x, offsets, w, dx, dw, db, workspace, stream=None):
 
 class Adapters:
     """Low-rank adapters of a layer: a [count, rank, c_in], b [count, c_out, rank] of one dtype, scale fp32 [count] or None; `.c` is the
-    dc_adapters.  The tensors are the caller's, and are read by each call."""
+    dc_adapters.  The tensors are the caller's, and are read and looked at by each call: others may have taken their place."""
 
     def __init__(self, a, b, scale=None):
+        self.a, self.b, self.scale = a, b, scale
+        self.check()
+
+    def check(self):
+        """Raises where the tensors do not belong together."""
         import torch
+        a, b, scale = self.a, self.b, self.scale
         if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2] or a.dtype != b.dtype:
             raise ValueError("Adapters: a [count, rank, c_in] and b [count, c_out, rank] of one dtype are wanted")
         if not a.is_contiguous() or not b.is_contiguous():
             raise ValueError("Adapters: dense tensors are wanted")
         if scale is not None and (scale.dtype != torch.float32 or tuple(scale.shape) != (a.shape[0],) or not scale.is_contiguous()):
             raise ValueError("Adapters: scales must be %d fp32 values" % a.shape[0])
-        self.a, self.b, self.scale = a, b, scale
-        self.count, self.rank, self.c_in = (int(v) for v in a.shape)
-        self.c_out = int(b.shape[1])
-        self.dtype = dtype_code(a.dtype)
+        dtype_code(a.dtype)
+
+    count = property(lambda self: int(self.a.shape[0]))
+    rank = property(lambda self: int(self.a.shape[1]))
+    c_in = property(lambda self: int(self.a.shape[2]))
+    c_out = property(lambda self: int(self.b.shape[1]))
+    dtype = property(lambda self: dtype_code(self.a.dtype))
 
     @property
     def c(self) -> AdapterSet:
-        """Of the tensors as they are now: they may have moved since."""
         return AdapterSet(self.count, self.rank, _ptr(self.a), _ptr(self.b), _ptr(self.scale))
 
     def saved(self, rows: int):
@@ -835,6 +843,7 @@ def adapter_forward(x, w, adapters: Adapters, offsets, which, bias, act, residua
         return
     if st is not None:
         raise DcError(st, "dc_adapter_forward")
+    adapters.check()
     rows = x.numel() // adapters.c_in
     _here("adapter_forward", x, w, adapters.a, adapters.b, adapters.scale, offsets, which, bias, residual, saved, y, workspace)
     _adapter_call("adapter_forward", rows, w, adapters, offsets, which, saved, x.dtype)
@@ -854,6 +863,7 @@ def adapter_backward(dy, x, w, adapters: Adapters, offsets, which, saved, dx, da
         return
     if st is not None:
         raise DcError(st, "dc_adapter_backward")
+    adapters.check()
     rows = dy.numel() // adapters.c_out
     _here("adapter_backward", dy, x, w, adapters.a, adapters.b, adapters.scale, offsets, which, saved, dx, da, db, workspace)
     _same_type("adapter_backward", dy.dtype, da, db)

@@ -42,11 +42,10 @@ struct Walk {
   int base;                  // runs before it are behind us
   long long before;          // items of theirs
   Run last;                  // the run of the last answer, and its items
-  int last_index;
   long long first, after;
   __device__ void start() { base = 0; before = first = after = 0; }
   // items of a run: row tiles x per_tile.  false: there is no such item
-  __device__ bool find(const Runs &r, int tile, int per_tile, long long item, Run *run, int *index, long long *inside) {
+  __device__ bool find(const Runs &r, int tile, int per_tile, long long item, Run *run, long long *inside) {
     if (item < first || item >= after) {
       const int lane = (int)(threadIdx.x & 31u);
       for (;; base += 32) {
@@ -67,7 +66,6 @@ struct Walk {
           last.begin = __shfl_sync(0xffffffffu, o.begin, at);
           last.end = __shfl_sync(0xffffffffu, o.end, at);
           last.weight = __shfl_sync(0xffffffffu, o.weight, at);
-          last_index = base + at;
           after = before + __shfl_sync(0xffffffffu, upto, at);
           first = after - __shfl_sync(0xffffffffu, mine, at);
           break;
@@ -76,15 +74,13 @@ struct Walk {
       }
     }
     *run = last;
-    *index = last_index;
     *inside = item - first;
     return true;
   }
 };
 
-// The first run that ends behind `row` (runs in order: the one that holds it, or the next); runs.count: none.  One thread.
+// The first run, of those between offsets, that ends behind `row` (runs in order: the one that holds it, or the next); runs.count: none.  One thread.
 __device__ __forceinline__ int first_run_behind(const Runs &r, int row) {
-  if (!r.offsets) return row < r.rows ? 0 : 1;
   int lo = 0, hi = r.count;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;

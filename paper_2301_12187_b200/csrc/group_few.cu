@@ -1,7 +1,7 @@
 // Grouped products and adapters of short runs in fp32: FMAs, each weight read once from memory as it lies.
 //
-// The tensor core's kernels want fp32 as three terms of bf16, which makes 16 bytes of traffic out of a weight's four; with up to 16 rows to a weight
-// FMAs keep up with memory (64 of them a cycle and SM for 32 bytes).  A CTA of four warps, or of H x four where there are
+// The tensor core's kernels want fp32 as three terms of bf16, which makes 16 bytes of traffic out of a weight's four.  Of a few rows to a weight FMAs keep
+// up with memory; of 16 they, and what comes with them, take twice as long as the bytes (below), and still less than terms.  A CTA of four warps, or of H x four where there are
 // fewer than two to an SM, works out R rows of a run x 32 columns, H x 128 numbers of the sum a step.
 //   along   the sum runs along the matrix's rows: a warp to eight columns and 128 numbers of a step, its lanes share the sum.
 //   across  it runs across them: eight lanes to the 32 columns, H x 16 such sets share the sum.
@@ -245,9 +245,8 @@ __global__ void __launch_bounds__(128 * H, (R == 4 ? 4 : 2) / H) k_group_few_f32
     __syncthreads();
     if (threadIdx.x < 32) {
       Run run = {0, 0, -1};
-      int index = 0;
       long long inside = 0;
-      const bool is = walk.find(j.runs, R, 1, item, &run, &index, &inside);
+      const bool is = walk.find(j.runs, R, 1, item, &run, &inside);
       if (threadIdx.x == 0) {
         found[0] = is ? 1 : 0;
         found[1] = run.begin + (int)inside * R;

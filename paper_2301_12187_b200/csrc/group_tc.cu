@@ -46,8 +46,8 @@ constexpr int kPiece = 64;                       // of the sum, 128 bytes of bf1
 constexpr int kP = 128 * 128;                    // bytes of the 128-row operand in a stage
 constexpr int kBox = 64 * 128;                   // 64 columns of 64 rows
 constexpr int kOut = kEpi * 32 * 128;            // staged results: 32 rows x 32 sums a warp
-constexpr int kSuper = 16;                       // rows of tiles that are walked together: 16 x 9 tiles at once read a twelfth of what a row or column of them would
-constexpr int kFewMost = 64, kFewWide = 32;     // rows of a tile of kFew; of adapters of a high rank, which then have as many slots
+constexpr int kSuper = 16;                       // rows of tiles that are walked together: of 128 x 256, 16 x 9 at once read a quarter of what a column of as many would, a ninth of a row
+constexpr int kFewMost = 64, kFewWide = 32;     // rows of a tile of kFew; of adapters of a rank above 64, each of which takes more shared memory
 // A gradient's tile may take seconds (2^30 rows are 17 million pieces), and so may results that are worked out again by FMAs: 0.8 s a million rows of one weight.
 constexpr unsigned long long kLongNs = 20ull * 1000ull * 1000ull * 1000ull;
 
@@ -58,7 +58,7 @@ template <typename T>
 constexpr int kAccs = sizeof(T) == 4 ? 4 : 2;   // accumulators: fp32 takes one for each piece, so that four of the next tile's are multiplied while results go out
 
 struct Params {
-  int rows, k, n;            // kGrad: m in the place of k
+  int k, n;                  // kGrad: m in the place of k
   Runs runs, ext;
   const float *alpha, *bias;
   int bias_each, act;
@@ -145,7 +145,8 @@ __device__ __forceinline__ void commit(uint64_t *bar) {
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// the same for what orders no memory: as a release it would wait for this thread's stores, 1500 cycles where results are on their way
+// The same for what orders no memory: as a release it would wait for this thread's stores, 1500 cycles where results are on their way.  Of an accumulator that is given back
+// nothing but what was read passes, and that is in registers: tcgen05.wait::ld stands before it, and the fence for the other thread's instructions.
 __device__ __forceinline__ void arrive_cluster_relaxed(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -173,9 +174,8 @@ struct Tile {
 };
 __device__ __forceinline__ bool find_tile(const Params &p, int tile, grp::Walk &walk, long long item, Tile *t) {
   Run run;
-  int index;
   long long inside;
-  if (!walk.find(p.runs, tile, p.tiles_n, item, &run, &index, &inside)) return false;
+  if (!walk.find(p.runs, tile, p.tiles_n, item, &run, &inside)) return false;
   const int tiles_m = (run.end - run.begin + tile - 1) / tile;
   const int band = (int)(inside / ((long long)kSuper * p.tiles_n)), rem = (int)(inside - (long long)band * kSuper * p.tiles_n);
   const int deep = min(kSuper, tiles_m - band * kSuper);
@@ -1636,7 +1636,6 @@ cudaError_t rows_tc(const RowsJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   const bool wide = j.dtype == DC_F32;
   const int terms = wide ? 3 : 1;
   Params p = {};
-  p.rows = j.rows;
   p.k = j.k;
   p.n = j.n;
   p.runs = j.runs;
@@ -1747,7 +1746,6 @@ cudaError_t grad_tc(const GradJob &j, bool early, DcWsHeader *ws, cudaStream_t s
   }
   const int terms = wide ? 3 : 1, pad = rank_pad(j.n), weights = j.runs.weights;
   Params p = {};
-  p.rows = j.runs.rows;
   p.k = j.m;
   p.n = j.n;
   p.runs = j.runs;

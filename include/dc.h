@@ -517,7 +517,8 @@ dc_status dc_adapter_forward(const void *x, long long rows, int c_in, const void
  *   dx[r] = W^T dy[r] + A_a^T u[r],  u[r] = scale_a B_a^T dy[r];  da_a = sum_r u[r] x[r]^T,  db_a = sum_r dy[r] t[r]^T over the rows of all
  * runs with the adapter, 0 of an adapter without rows.  W is frozen, and so is the scale.  dx: [rows][c_in] (w NULL: the adapters' part
  * alone); da: [count][rank][c_in], db: [count][c_out][rank], of `dtype`.  What is not wanted is NULL, and so may be what it alone is made
- * of (x for da, saved for db, w for dx).  Outputs overlap nothing.
+ * of (x for da, saved for db, w for dx).  Outputs overlap nothing.  Each 128 columns of an adapter's gradient look through all runs, so that time grows with
+ * adapters x runs (widths of 256: 512 of each 84 us, 4096 4.5 ms, 16384 69 ms).
  */
 dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int c_in, const void *w, int c_out,
                               const dc_adapters *adapters, const int *offsets, const int *which, int runs, const void *saved, void *dx,

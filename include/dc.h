@@ -526,7 +526,8 @@ dc_status dc_adapter_backward(const void *dy, const void *x, long long rows, int
 
 /*
  * Host only, launches nothing: how the products of a call would run, for reports and tests.  rank 0: dc_group_forward and dc_group_backward with
- * `runs` groups; else dc_adapter_forward and dc_adapter_backward with `runs` runs, a shared matrix and as many adapters of that rank.
+ * `runs` groups; else dc_adapter_forward and dc_adapter_backward with `runs` runs, a shared matrix and as many adapters of that rank (with
+ * another number of adapters gradients may be shared by other numbers of CTAs, and without a shared matrix rows may go another way).
  */
 typedef enum { DC_GROUP_FORWARD = 0, DC_GROUP_DX = 1, DC_GROUP_DW = 2 } dc_group_part;   /* y; dx; dw (of adapters da) */
 typedef enum {

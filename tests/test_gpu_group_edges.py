@@ -1,5 +1,7 @@
-"""Grouped products and adapters on the GPU: gradients of which a CTA makes several tiles, infinities, rows in front of the first run.  Tolerances as in
-test_gpu_group.py."""
+"""Grouped products and adapters on the GPU: gradients of which a CTA makes several tiles, infinities, rows in front of the first run.
+
+Tolerances as in test_gpu_group.py.  What a bf16 row keeps of an adapter, t, is two terms of its sign: the first t cut off to 8 bits, which leaves r < 2^-7 of t's leading
+bit, the second r rounded to 8 bits, half a last place of it at most 2^-9 of 2^-7: 2^-16 of t.  Where r is 0 the first is a step less, and r that step, which is exact."""
 import pytest
 
 torch = pytest.importorskip("torch")
